@@ -387,6 +387,123 @@ sfda_status_t sfda_chunk_solve_monitor(const void* k, const void* alpha, const v
                                        int H, int T, int m, sfda_dtype_t in_dtype,
                                        sfda_stream_t stream);
 
+/*
+ * Operators around the attention: rotary positions, linear attention with one decay for each head
+ * (real channels, no erase) and the group norm that follows it.  One dtype for a call's activations (float32 or
+ * bfloat16); states, decays, tables, weights and their gradients are float32; sums are float32.
+ *
+ * Strides: these calls take their activations with element strides, the last axis contiguous:
+ * `strides` points to the strides of the outer axes, tensor after tensor in the order given at each
+ * call, or is NULL for contiguous tensors.  Strides are >= 0 (SFDA_ERR_SHAPE otherwise); inputs may
+ * repeat elements (stride 0), an output's elements must lie apart (SFDA_ERR_ALIAS).  Pointers need
+ * only their element's alignment (SFDA_ERR_ALIGN).  No output may share memory with an input or
+ * another output but where a call says so (SFDA_ERR_ALIAS; slices of one buffer with the same
+ * strides are told apart exactly, other tensors by the ranges they span).
+ */
+
+/*
+ * sfda_rotary -- queries and keys turned by their tokens' positions.  Channel pairs (a, b) number i < rot / 2 are
+ * (i, i + rot / 2), or (2i, 2i + 1) if interleaved; with c, s = cos, sin[position][i]
+ *   a' = a c - b s,  b' = a s + b c      (inverse: s negated, which is also the gradient's turn)
+ * and channels from rot on are copied.
+ *   q, qo [B, Hq, T, D], k, ko [B, Hk, T, D] (k NULL: queries only); strides: (b, h, t) of q, k, qo, ko.
+ *          qo == q and ko == k (same strides) is allowed and turns them in place.
+ *   cos, sin : [P, rot / 2] float32.
+ *   positions : [B, T] of position_bits (32 or 64) wide integers, rows position_stride elements apart
+ *          (0: the same for every sequence), or NULL for offset, offset + 1, ... (offset >= 0,
+ *          offset + T <= P; SFDA_ERR_SHAPE otherwise).  A position outside [0, P) turns its
+ *          token's channels into NaN.
+ *   1 <= D <= 4096, rot even in [2, D], P >= 1.
+ */
+sfda_status_t sfda_rotary(const void* q, const void* k, const float* cos, const float* sin,
+                          const void* positions, int position_bits, long long position_stride,
+                          long long offset, void* qo, void* ko, int B, int Hq, int Hk, int T, int D,
+                          int rot, int P, int interleaved, int inverse, const long long* strides,
+                          sfda_dtype_t dtype, sfda_stream_t stream);
+
+/*
+ * sfda_decay_attn_fwd -- linear attention with a decay for each head, lambda_h = exp(log_decay[h]):
+ *   S_t = lambda_h S_{t-1} + k_t v_t^T      (S_t in R^{dk x dv}),      o_t = scale S_t^T q_t
+ * over T tokens, evaluated in blocks on the matrix cores.
+ *   q, k [B, H, T, dk], v, o [B, H, T, dv]; strides: (b, h, t) of q, k, v, o.
+ *   log_decay : [H] float32, meant to be <= 0; 0 keeps everything, -inf only the token itself.
+ *   lengths : [B] int32 or NULL.  Sequence b has min(max(lengths[b], 0), T) tokens; what q, k, v
+ *          hold past them is not used, o is 0 there and S_T is the state after the last token (S0 at length 0).
+ *   S0, S_T : [B, H, dk, dv] contiguous float32, each may be NULL (zero state; not wanted).
+ *          S_T == S0 is allowed.
+ *   workspace : with at least sfda_decay_attn_fwd_workspace_bytes(...) bytes (0 where one workgroup
+ *          for a head and 64 value columns fills the device) the sequences are cut into segments that are scanned
+ *          in parallel; with less, or NULL, they are scanned whole.  The same result up to rounding.
+ *   1 <= dk, dv <= 256.  bfloat16: the block's scores and the state are rounded to bfloat16 as operands of
+ *   the products that give o; the state itself is carried in float32 from exact products.  A token with a
+ *   value that is not finite makes the rows of its block (32 or 64 tokens) before it NaN too.
+ */
+size_t sfda_decay_attn_fwd_workspace_bytes(int B, int H, int T, int dk, int dv);
+
+sfda_status_t sfda_decay_attn_fwd(const void* q, const void* k, const void* v,
+                                  const float* log_decay, const int* lengths, const float* S0,
+                                  void* o, float* S_T, int B, int H, int T, int dk, int dv,
+                                  float scale, const long long* strides, sfda_dtype_t dtype,
+                                  void* workspace, size_t workspace_bytes, sfda_stream_t stream);
+
+/*
+ * sfda_decay_attn_bwd -- gradients of a real loss through sfda_decay_attn_fwd, given dO = dL/do and
+ * dS_T = dL/dS_T (NULL: zero).  With U_t = dL/dS_t = lambda_h U_{t+1} + scale q_t dO_t^T:
+ *   dq_t = scale S_t dO_t,  dk_t = U_t v_t,  dv_t = U_t^T k_t,  dS0 = lambda_h U_1
+ * (three scans in one launch, S_t and U_t formed on the way).  The decays are constants: they get no gradient.
+ *   dq, dk, dv : as q, k, v, zero past a sequence's length; dS0 [B, H, dk, dv] float32 or NULL.
+ *   strides: (b, h, t) of q, k, v, dO, dq, dk, dv.  Other arguments as the forward's.
+ */
+size_t sfda_decay_attn_bwd_workspace_bytes(int B, int H, int T, int dk, int dv);
+
+sfda_status_t sfda_decay_attn_bwd(const void* q, const void* k, const void* v,
+                                  const float* log_decay, const int* lengths, const float* S0,
+                                  const void* dO, const float* dS_T, void* dq, void* dk_out,
+                                  void* dv_out, float* dS0, int B, int H, int T, int dk, int dv,
+                                  float scale, const long long* strides, sfda_dtype_t dtype,
+                                  void* workspace, size_t workspace_bytes, sfda_stream_t stream);
+
+/*
+ * sfda_decay_attn_step -- one token: S <- lambda_h S + k v^T in place, o = scale S^T q.
+ *   q, k [B, H, dk], v, o [B, H, dv]; strides: (b, h) of q, k, v, o; S [B, H, dk, dv] contiguous float32.
+ */
+sfda_status_t sfda_decay_attn_step(const void* q, const void* k, const void* v,
+                                   const float* log_decay, float* S, void* o, int B, int H, int dk,
+                                   int dv, float scale, const long long* strides,
+                                   sfda_dtype_t dtype, sfda_stream_t stream);
+
+/*
+ * sfda_group_norm -- every token's H groups of D channels normalised, scaled and activated:
+ *   x^ = (x - mean) / sqrt(var + eps) over the D channels of a head of a token,
+ *   n = x^ weight + bias,   y = act(n) without a gate, n act(gate) with one,
+ *   act(z) = z (SFDA_ACT_NONE) or z / (1 + exp(-z)) (SFDA_ACT_SILU).
+ *   x [B, H, T, D] (an attention's output, or channels-last [B, T, H D] by its strides);
+ *   gate (or NULL), y [B, T, H D]; weight, bias [H D] float32, each may be NULL (1; 0).
+ *   strides: (b, h, t) of x, then (b, t) of gate and y.  1 <= D <= 2048, eps >= 0.
+ */
+enum { SFDA_ACT_NONE = 0, SFDA_ACT_SILU = 1 };
+
+sfda_status_t sfda_group_norm(const void* x, const float* weight, const float* bias,
+                              const void* gate, void* y, int B, int H, int T, int D,
+                              int activation, float eps, const long long* strides,
+                              sfda_dtype_t dtype, sfda_stream_t stream);
+
+/*
+ * sfda_group_norm_bwd -- gradients of a real loss through sfda_group_norm, given dy = dL/dy [B, T, H D].
+ *   dx as x, dgate as gate (required with a gate), dweight, dbias [H D] float32 or NULL (not wanted).
+ *   strides: (b, h, t) of x, (b, t) of gate and dy, (b, h, t) of dx, (b, t) of dgate.
+ *   workspace : sfda_group_norm_bwd_workspace_bytes(...) bytes where dweight or dbias is wanted (their partial
+ *          sums; SFDA_ERR_SHAPE if smaller), 4-byte aligned.
+ */
+size_t sfda_group_norm_bwd_workspace_bytes(int B, int H, int T, int D, sfda_dtype_t dtype);
+
+sfda_status_t sfda_group_norm_bwd(const void* dy, const void* x, const float* weight,
+                                  const float* bias, const void* gate, void* dx, void* dgate,
+                                  float* dweight, float* dbias, int B, int H, int T, int D,
+                                  int activation, float eps, const long long* strides,
+                                  sfda_dtype_t dtype, void* workspace, size_t workspace_bytes,
+                                  sfda_stream_t stream);
+
 /* SFDA_ABI_VERSION of the built library. */
 int sfda_abi_version(void);
 

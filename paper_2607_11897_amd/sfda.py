@@ -28,7 +28,10 @@ EXPORTS = ("sfda_chunk_fwd", "sfda_chunk_fwd_sliced", "sfda_chunk_fwd_gated", "s
            "sfda_chunk_bwd", "sfda_chunk_bwd_workspace_bytes",
            "sfda_chunk_bwd_auto_workspace_bytes", "sfda_chunk_fwd_auto_factored",
            "sfda_chunk_solve_monitor",
-           "sfda_step", "sfda_status_string", "sfda_abi_version")
+           "sfda_step", "sfda_status_string", "sfda_abi_version",
+           "sfda_rotary", "sfda_decay_attn_fwd", "sfda_decay_attn_fwd_workspace_bytes", "sfda_decay_attn_bwd",
+           "sfda_decay_attn_bwd_workspace_bytes", "sfda_decay_attn_step", "sfda_group_norm", "sfda_group_norm_bwd",
+           "sfda_group_norm_bwd_workspace_bytes")
 
 _lib = None
 
@@ -99,6 +102,20 @@ def load_library(path: str = LIB_PATH):
     lib.sfda_chunk_bwd_auto_workspace_bytes.restype = ctypes.c_size_t
     lib.sfda_step.argtypes = [vp] * 8 + [i] * 4 + [i, i, vp]
     lib.sfda_step.restype = i
+    sz, ll = ctypes.c_size_t, ctypes.c_longlong
+    lib.sfda_rotary.argtypes = [vp] * 5 + [i, ll, ll] + [vp] * 2 + [i] * 9 + [vp, i, vp]
+    lib.sfda_decay_attn_fwd.argtypes = [vp] * 8 + [i] * 5 + [f, vp, i, vp, sz, vp]
+    lib.sfda_decay_attn_bwd.argtypes = [vp] * 12 + [i] * 5 + [f, vp, i, vp, sz, vp]
+    lib.sfda_decay_attn_step.argtypes = [vp] * 6 + [i] * 4 + [f, vp, i, vp]
+    lib.sfda_group_norm.argtypes = [vp] * 5 + [i] * 5 + [f, vp, i, vp]
+    lib.sfda_group_norm_bwd.argtypes = [vp] * 9 + [i] * 5 + [f, vp, i, vp, sz, vp]
+    for fn in (lib.sfda_rotary, lib.sfda_decay_attn_fwd, lib.sfda_decay_attn_bwd, lib.sfda_decay_attn_step,
+               lib.sfda_group_norm, lib.sfda_group_norm_bwd):
+        fn.restype = i
+    for fn in (lib.sfda_decay_attn_fwd_workspace_bytes, lib.sfda_decay_attn_bwd_workspace_bytes,
+               lib.sfda_group_norm_bwd_workspace_bytes):
+        fn.argtypes = [i] * 5
+        fn.restype = sz
     lib.sfda_status_string.argtypes = [i]
     lib.sfda_status_string.restype = ctypes.c_char_p
     lib.sfda_abi_version.restype = i
@@ -493,3 +510,296 @@ def step(q, k, v, alpha, theta, beta, S, *, o=None, out_dtype=None, stream=None)
     if st != 0:
         raise SfdaError(st, "sfda_step")
     return o
+
+
+# ------------------------------------------------------------------ operators around the attention
+# Activations may have any strides with a contiguous last axis; float32 states, tables and weights are contiguous.
+
+_ACT = {"none": 0, "silu": 1}
+_STRIDES = {n: ctypes.c_longlong * n for n in (7, 8, 12, 21)}
+
+
+def _rows(t) -> Optional[int]:
+    """The pointer of an activation whose last axis is contiguous."""
+    if t is None:
+        return None
+    if t.stride(-1) != 1 and t.shape[-1] > 1:
+        raise ValueError("the last axis of an activation must be contiguous")
+    return t.data_ptr()
+
+
+def _same_dtype(x, **named) -> int:
+    code = _dtype_code(x)
+    for name, t in named.items():
+        if t is not None and t.dtype != x.dtype:
+            raise TypeError(f"{name} must be {x.dtype} as the other activations (got {t.dtype})")
+    return code
+
+
+def _int32(name, t) -> None:
+    import torch
+    if t is not None and t.dtype != torch.int32:
+        raise TypeError(f"{name} must be int32 (got {t.dtype})")
+
+
+def _empty(shape, dtype, device, stream):
+    """An output, from the memory of the stream that writes it."""
+    import torch
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(stream.cuda_stream, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def rotary_tables(positions: int, rot: int, *, base: float = 10000.0, scaling: Optional[dict] = None, device="cuda"):
+    """The tables of `rotary`: cos and sin [positions, rot / 2] float32 of position * frequency, formed in
+    float64, frequency_i = base^(-2i / rot).  `scaling` stretches them past the length L that a
+    model was trained at, by a factor s:
+      dict(kind="linear", factor=s)              positions divided by s
+      dict(kind="ntk", factor=s)                 base * s^(rot / (rot - 2)): the fastest pair keeps its frequency,
+                                                 the slowest is divided by s
+      dict(kind="yarn", factor=s, length=L, fast=32, slow=1, amplitude=None)
+                                                 pairs that turn more than `fast` times over L keep their frequency,
+                                                 those that turn less than `slow` times are divided by s, linear in the
+                                                 pair's number between; both tables times the amplitude
+                                                 (0.1 log s + 1 if None)."""
+    import math
+    import torch
+    if rot < 2 or rot % 2 or positions < 1:
+        raise ValueError(f"rot must be even and at least 2, positions at least 1 (got {rot}, {positions})")
+    pair = torch.arange(rot // 2, dtype=torch.float64)
+    freq = base ** (-2.0 * pair / rot)
+    amplitude = 1.0
+    if scaling is not None:
+        kind, s = scaling["kind"], float(scaling["factor"])
+        if not s > 0:
+            raise ValueError(f"the factor must be positive (got {s})")
+        if kind == "linear":
+            freq = freq / s
+        elif kind == "ntk":
+            if rot < 4:
+                raise ValueError("ntk scaling needs at least two pairs")
+            freq = (base * s ** (rot / (rot - 2))) ** (-2.0 * pair / rot)
+        elif kind == "yarn":
+            length = float(scaling["length"])
+            # the (fractional) pair that turns n times over the length
+            at = lambda n: rot * math.log(length / (2 * math.pi * n)) / (2 * math.log(base))  # noqa: E731
+            low = max(math.floor(at(float(scaling.get("fast", 32)))), 0)
+            high = min(math.ceil(at(float(scaling.get("slow", 1)))), rot // 2 - 1)
+            keep = 1.0 - ((pair - low) / max(high - low, 1e-3)).clamp(0.0, 1.0)
+            freq = freq * keep + freq / s * (1.0 - keep)
+            amplitude = scaling.get("amplitude")
+            amplitude = (0.1 * math.log(s) + 1.0 if s > 1 else 1.0) if amplitude is None else float(amplitude)
+        else:
+            raise ValueError(f"scaling must be linear, ntk or yarn, not {kind!r}")
+    angle = torch.arange(positions, dtype=torch.float64)[:, None] * freq
+    return tuple((amplitude * t).to(torch.float32).to(device) for t in (angle.cos(), angle.sin()))
+
+
+def rotary(q, k, cos, sin, positions=None, *, offset: int = 0, interleaved: bool = False, inverse: bool = False,
+           q_out=None, k_out=None, stream=None) -> Tuple:
+    """Queries and keys turned by their tokens' positions (sfda_rotary).  q: [B,Hq,T,D]; k: [B,Hk,T,D] or None (float32 or
+    bfloat16, any strides with a contiguous last axis); cos, sin: [P, rot / 2] float32 (rotary_tables): the first
+    rot channels turn, as pairs (i, i + rot / 2) or, interleaved, (2i, 2i + 1); positions: int32 or int64 [T] or [B,T],
+    else offset, offset + 1, ....  inverse turns back: the gradient of the outputs becomes that of the inputs.
+    Returns (q_out, k_out), new contiguous tensors if not given; q_out=q, k_out=k turns in place."""
+    import torch
+    lib = load_library()
+    if q.dim() != 4 or cos.dim() != 2:
+        raise ValueError("q must be [B,H,T,D] and cos [P, rot / 2]")
+    B, Hq, T, D = q.shape
+    Hk = 0 if k is None else k.shape[1]
+    code = _same_dtype(q, k=k, q_out=q_out, k_out=k_out)
+    _need_f32(cos=cos, sin=sin)
+    P, half = cos.shape
+    if q_out is None:
+        q_out = _empty((B, Hq, T, D), q.dtype, q.device, stream)
+    if k is None:
+        k_out = None
+    elif k_out is None:
+        k_out = _empty((B, Hk, T, D), q.dtype, q.device, stream)
+    bits, pstride = 0, 0
+    if positions is not None:
+        if positions.dtype not in (torch.int32, torch.int64):
+            raise TypeError(f"positions must be int32 or int64 (got {positions.dtype})")
+        bits = 32 if positions.dtype == torch.int32 else 64
+        pstride = positions.stride(0) if positions.dim() == 2 and B > 1 else 0
+    _check(dict(q=(q, (B, Hq, T, D)), k=(k, (B, Hk, T, D)), cos=(cos, (P, half)), sin=(sin, (P, half)),
+                q_out=(q_out, (B, Hq, T, D)), k_out=(k_out, (B, Hk, T, D)),
+                positions=(positions, (T,) if positions is not None and positions.dim() == 1 else (B, T))))
+    kk, ko = (q, q_out) if k is None else (k, k_out)
+    st = lib.sfda_rotary(_rows(q), _rows(k), _ptr(cos), _ptr(sin), _rows(positions), bits, pstride, offset, _rows(q_out),
+                         _rows(k_out), B, Hq, Hk, T, D, 2 * half, P, interleaved, inverse,
+                         _STRIDES[12](*q.stride()[:3], *kk.stride()[:3], *q_out.stride()[:3], *ko.stride()[:3]),
+                         code, _stream(stream))
+    if st != 0:
+        raise SfdaError(st, "sfda_rotary")
+    return q_out, k_out
+
+
+def decay_attn_fwd(q, k, v, log_decay, S0=None, *, scale: float = 1.0, lengths=None, o=None, S_T=None,
+                   want_state: bool = True, workspace=None, stream=None) -> Tuple:
+    """Linear attention with one decay for each head (sfda_decay_attn_fwd): S_t = exp(log_decay) S_(t-1) + k_t v_t^T,
+    o_t = scale S_t^T q_t.  q, k: [B,H,T,dk]; v: [B,H,T,dv] (float32 or bfloat16, any strides with a contiguous last
+    axis: a [B,T,H,D] projection is passed as its transpose(1, 2)); log_decay: [H] float32; S0: [B,H,dk,dv] float32
+    or None; lengths: [B] int32 or None (all T).  Returns (o [B,H,T,dv], S_T [B,H,dk,dv] float32 or None).  `workspace`: a
+    uint8 device tensor (fastest with decay_attn_fwd_workspace_bytes(...) bytes, which are allocated here if it is None)."""
+    import torch
+    lib = load_library()
+    if q.dim() != 4 or v.dim() != 4:
+        raise ValueError("q and v must have 4 dimensions")
+    B, H, T, dk = q.shape
+    dv = v.shape[3]
+    code = _same_dtype(q, k=k, v=v, o=o)
+    if o is None:
+        o = _empty((B, H, T, dv), q.dtype, q.device, stream)
+    if S_T is None and want_state:
+        S_T = _empty((B, H, dk, dv), torch.float32, q.device, stream)
+    _need_f32(S0=S0, S_T=S_T, log_decay=log_decay)
+    _int32("lengths", lengths)
+    _check(dict(q=(q, (B, H, T, dk)), k=(k, (B, H, T, dk)), v=(v, (B, H, T, dv)), log_decay=(log_decay, (H,)),
+                lengths=(lengths, (B,)), S0=(S0, (B, H, dk, dv)), o=(o, (B, H, T, dv)), S_T=(S_T, (B, H, dk, dv)),
+                workspace=(workspace, tuple(workspace.shape) if workspace is not None else ())))
+    if workspace is None:
+        nws = lib.sfda_decay_attn_fwd_workspace_bytes(B, H, T, dk, dv)
+        workspace = _try_workspace(nws, q.device, stream) if nws else None
+    st = lib.sfda_decay_attn_fwd(_rows(q), _rows(k), _rows(v), _ptr(log_decay), _ptr(lengths), _ptr(S0), _rows(o), _ptr(S_T),
+                                 B, H, T, dk, dv, scale,
+                                 _STRIDES[12](*q.stride()[:3], *k.stride()[:3], *v.stride()[:3], *o.stride()[:3]),
+                                 code, _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
+                                 _stream(stream))
+    if st != 0:
+        raise SfdaError(st, "sfda_decay_attn_fwd")
+    return o, S_T
+
+
+def decay_attn_bwd(q, k, v, log_decay, S0, dO, dS_T=None, *, scale: float = 1.0, lengths=None, want_dS0: bool = True,
+                   dq=None, dk=None, dv=None, workspace=None, stream=None) -> dict:
+    """Gradients of a real loss through decay_attn_fwd (sfda_decay_attn_bwd), given dO = dL/do [B,H,T,dv] (the inputs'
+    dtype, any strides) and dS_T = dL/dS_T [B,H,dk,dv] float32 or None.  Inputs as decay_attn_fwd; the decays are constants.
+    Returns dq, dk, dv (new contiguous tensors if not given) and dS0 (float32, or None without want_dS0)."""
+    import torch
+    lib = load_library()
+    if q.dim() != 4 or v.dim() != 4:
+        raise ValueError("q and v must have 4 dimensions")
+    B, H, T, nk = q.shape
+    nv = v.shape[3]
+    code = _same_dtype(q, k=k, v=v, dO=dO, dq=dq, dk=dk, dv=dv)
+    dq = _empty((B, H, T, nk), q.dtype, q.device, stream) if dq is None else dq
+    dk = _empty((B, H, T, nk), q.dtype, q.device, stream) if dk is None else dk
+    dv = _empty((B, H, T, nv), q.dtype, q.device, stream) if dv is None else dv
+    dS0 = _empty((B, H, nk, nv), torch.float32, q.device, stream) if want_dS0 else None
+    _need_f32(S0=S0, dS_T=dS_T, log_decay=log_decay)
+    _int32("lengths", lengths)
+    tk, tv, ts = (B, H, T, nk), (B, H, T, nv), (B, H, nk, nv)
+    _check(dict(q=(q, tk), k=(k, tk), v=(v, tv), log_decay=(log_decay, (H,)), lengths=(lengths, (B,)), S0=(S0, ts),
+                dO=(dO, tv), dS_T=(dS_T, ts), dq=(dq, tk), dk=(dk, tk), dv=(dv, tv),
+                workspace=(workspace, tuple(workspace.shape) if workspace is not None else ())))
+    if workspace is None:
+        nws = lib.sfda_decay_attn_bwd_workspace_bytes(B, H, T, nk, nv)
+        workspace = _try_workspace(nws, q.device, stream) if nws else None
+    strides = _STRIDES[21](*q.stride()[:3], *k.stride()[:3], *v.stride()[:3], *dO.stride()[:3], *dq.stride()[:3],
+                                       *dk.stride()[:3], *dv.stride()[:3])
+    st = lib.sfda_decay_attn_bwd(_rows(q), _rows(k), _rows(v), _ptr(log_decay), _ptr(lengths), _ptr(S0), _rows(dO), _ptr(dS_T),
+                                 _rows(dq), _rows(dk), _rows(dv), _ptr(dS0), B, H, T, nk, nv, scale, strides, code,
+                                 _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
+                                 _stream(stream))
+    if st != 0:
+        raise SfdaError(st, "sfda_decay_attn_bwd")
+    return dict(dq=dq, dk=dk, dv=dv, dS0=dS0)
+
+
+def decay_attn_fwd_workspace_bytes(B: int, H: int, T: int, dk: int, dv: int) -> int:
+    return int(load_library().sfda_decay_attn_fwd_workspace_bytes(B, H, T, dk, dv))
+
+
+def decay_attn_bwd_workspace_bytes(B: int, H: int, T: int, dk: int, dv: int) -> int:
+    return int(load_library().sfda_decay_attn_bwd_workspace_bytes(B, H, T, dk, dv))
+
+
+def decay_attn_step(q, k, v, log_decay, S, *, scale: float = 1.0, o=None, stream=None):
+    """One token of decay_attn_fwd (sfda_decay_attn_step).  q, k: [B,H,dk]; v: [B,H,dv] (any strides with a contiguous
+    last axis); S: [B,H,dk,dv] float32, updated in place.  Returns o [B,H,dv]."""
+    lib = load_library()
+    if q.dim() != 3 or v.dim() != 3:
+        raise ValueError("q and v must have 3 dimensions")
+    B, H, dk = q.shape
+    dv = v.shape[2]
+    code = _same_dtype(q, k=k, v=v, o=o)
+    if o is None:
+        o = _empty((B, H, dv), q.dtype, q.device, stream)
+    _need_f32(S=S, log_decay=log_decay)
+    _check(dict(q=(q, (B, H, dk)), k=(k, (B, H, dk)), v=(v, (B, H, dv)), log_decay=(log_decay, (H,)),
+                S=(S, (B, H, dk, dv)), o=(o, (B, H, dv))))
+    st = lib.sfda_decay_attn_step(_rows(q), _rows(k), _rows(v), _ptr(log_decay), _ptr(S), _rows(o), B, H, dk, dv, scale,
+                                  _STRIDES[8](*q.stride()[:2], *k.stride()[:2], *v.stride()[:2], *o.stride()[:2]),
+                                  code, _stream(stream))
+    if st != 0:
+        raise SfdaError(st, "sfda_decay_attn_step")
+    return o
+
+
+def group_norm(x, weight=None, bias=None, gate=None, *, activation: str = "none", eps: float = 1e-5, y=None, stream=None):
+    """Every token's heads normalised over their channels, scaled and activated (sfda_group_norm): n = x^ weight + bias,
+    y = act(n), or n act(gate) with a gate; activation "none" or "silu".  x: [B,H,T,D] (any strides with a contiguous last
+    axis; a channels-last [B,T,C] is passed as view(B,T,H,D).transpose(1, 2)); gate: [B,T,H*D]; weight, bias: [H*D]
+    float32 or None.  Returns y [B,T,H*D]."""
+    lib = load_library()
+    if x.dim() != 4:
+        raise ValueError("x must have 4 dimensions")
+    B, H, T, D = x.shape
+    code = _same_dtype(x, gate=gate, y=y)
+    if activation not in _ACT:
+        raise ValueError(f"activation must be 'none' or 'silu', not {activation!r}")
+    if y is None:
+        y = _empty((B, T, H * D), x.dtype, x.device, stream)
+    _need_f32(weight=weight, bias=bias)
+    _check(dict(x=(x, (B, H, T, D)), weight=(weight, (H * D,)), bias=(bias, (H * D,)), gate=(gate, (B, T, H * D)),
+                y=(y, (B, T, H * D))))
+    g = y if gate is None else gate
+    st = lib.sfda_group_norm(_rows(x), _ptr(weight), _ptr(bias), _rows(gate), _rows(y), B, H, T, D, _ACT[activation], eps,
+                             _STRIDES[7](*x.stride()[:3], *g.stride()[:2], *y.stride()[:2]), code, _stream(stream))
+    if st != 0:
+        raise SfdaError(st, "sfda_group_norm")
+    return y
+
+
+def group_norm_bwd(dy, x, weight=None, bias=None, gate=None, *, activation: str = "none", eps: float = 1e-5, dx=None,
+                   dgate=None, workspace=None, stream=None) -> dict:
+    """Gradients of a real loss through group_norm (sfda_group_norm_bwd), given dy = dL/dy [B,T,H*D].  Returns dx (new and
+    contiguous if not given), dgate, dweight, dbias (float32); None for what was not given.  `workspace`: a uint8 device
+    tensor of at least sfda_group_norm_bwd_workspace_bytes, allocated here if None."""
+    import torch
+    lib = load_library()
+    if x.dim() != 4:
+        raise ValueError("x must have 4 dimensions")
+    B, H, T, D = x.shape
+    code = _same_dtype(x, dy=dy, gate=gate, dx=dx, dgate=dgate)
+    if activation not in _ACT:
+        raise ValueError(f"activation must be 'none' or 'silu', not {activation!r}")
+    if dx is None:
+        dx = _empty((B, H, T, D), x.dtype, x.device, stream)
+    if gate is None:
+        dgate = None
+    elif dgate is None:
+        dgate = _empty((B, T, H * D), x.dtype, x.device, stream)
+    dweight = None if weight is None else _empty((H * D,), torch.float32, x.device, stream)
+    dbias = None if bias is None else _empty((H * D,), torch.float32, x.device, stream)
+    _need_f32(weight=weight, bias=bias)
+    tc, w = (B, T, H * D), (H * D,)
+    _check(dict(x=(x, (B, H, T, D)), dy=(dy, tc), weight=(weight, w), bias=(bias, w), gate=(gate, tc), dx=(dx, (B, H, T, D)),
+                dgate=(dgate, tc), workspace=(workspace, tuple(workspace.shape) if workspace is not None else ())))
+    if workspace is None and (dweight is not None or dbias is not None):
+        workspace = _workspace(lib.sfda_group_norm_bwd_workspace_bytes(B, H, T, D, code), x.device, stream)
+    g, dg = (dy, dy) if gate is None else (gate, dgate)
+    st = lib.sfda_group_norm_bwd(_rows(dy), _rows(x), _ptr(weight), _ptr(bias), _rows(gate), _rows(dx), _rows(dgate),
+                                 _ptr(dweight), _ptr(dbias), B, H, T, D, _ACT[activation], eps,
+                                 _STRIDES[12](*x.stride()[:3], *g.stride()[:2], *dy.stride()[:2], *dx.stride()[:3],
+                                                          *dg.stride()[:2]),
+                                 code, _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
+                                 _stream(stream))
+    if st != 0:
+        raise SfdaError(st, "sfda_group_norm_bwd")
+    return dict(dx=dx, dgate=dgate, dweight=dweight, dbias=dbias)

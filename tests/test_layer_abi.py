@@ -1,0 +1,183 @@
+"""Refusals of the operators around the attention: the C entry points' argument checks (no pointer is
+dereferenced, nothing is launched) and the binding's (CPU only)."""
+from __future__ import annotations
+
+import ctypes
+
+import pytest
+
+from gpu_util import ensure_built
+
+A = 1 << 24
+INF = float("inf")
+
+
+@pytest.fixture(scope="module")
+def lib():
+    return ensure_built()
+
+
+def arr(*x):
+    return (ctypes.c_longlong * len(x))(*x)
+
+
+def fwd(lib, q=A, k=2 * A, v=3 * A, g=4 * A, n=None, S0=5 * A, o=6 * A, S_T=7 * A, B=1, H=2, T=8, dk=16, dv=8, strides=None, dt=0,
+        ws=None, nws=0):
+    return lib.sfda_decay_attn_fwd(q, k, v, g, n, S0, o, S_T, B, H, T, dk, dv, 1.0, strides, dt, ws, nws, None)
+
+
+def test_decay_attn_fwd(lib):
+    assert fwd(lib, dt=2) == 4
+    for bad in (dict(B=-1), dict(H=-1), dict(T=-1), dict(dk=0), dict(dk=257), dict(dv=0), dict(dv=257), dict(B=1 << 20, H=1 << 10),
+                dict(T=(1 << 31) - 1)):
+        assert fwd(lib, **bad) == 2, bad
+    for name in ("q", "k", "v", "g", "o"):
+        assert fwd(lib, **{name: None}) == 1, name
+    assert fwd(lib, q=A + 2) == 5 and fwd(lib, q=A + 2, dt=1, T=0, B=0) == 0
+    assert fwd(lib, g=4 * A + 1) == 5 and fwd(lib, S_T=7 * A + 2) == 5 and fwd(lib, n=8 * A + 2) == 5
+    # o over an input, S_T partly over S0, S_T over o, o over the decays
+    assert fwd(lib, o=A) == 6 and fwd(lib, o=3 * A + 4) == 6 and fwd(lib, S_T=5 * A + 16) == 6
+    assert fwd(lib, S_T=6 * A) == 6 and fwd(lib, g=6 * A) == 6
+    assert fwd(lib, B=0, q=None) == 0 and fwd(lib, H=0, q=None) == 0
+
+
+def test_decay_attn_strides(lib):
+    # [B, T, H, D] of q, k, v, o
+    s = [8 * 2 * 16, 16, 2 * 16] * 2 + [8 * 2 * 8, 8, 2 * 8] * 2
+    bad = list(s)
+    bad[2] = -1
+    assert fwd(lib, strides=arr(*bad)) == 2
+    bad = list(s)
+    bad[0] = 1 << 50
+    assert fwd(lib, strides=arr(*bad), B=2) == 2
+    bad = list(s)
+    bad[10] = 0                                     # the heads of o in one place
+    assert fwd(lib, strides=arr(*bad)) == 6
+    bad = list(s)
+    bad[11] = 12                                    # tokens of o 12 apart: heads of 8 overlap the next token's
+    assert fwd(lib, strides=arr(*bad)) == 6
+    # o in a slice of the buffer that holds v ([B, T, 2, H, D]): apart, and one row off
+    p = [8 * 2 * 16, 16, 2 * 16] * 2 + [8 * 2 * 2 * 8, 8, 2 * 2 * 8] * 2
+    assert fwd(lib, strides=arr(*p), v=3 * A, o=3 * A + 8 * 4) == 6
+    assert fwd(lib, strides=arr(*p), v=3 * A, o=3 * A + 2 * 8 * 4 - 4) == 6
+
+
+def bwd(lib, **kw):
+    a = dict(q=A, k=2 * A, v=3 * A, g=4 * A, n=None, S0=5 * A, dO=6 * A, dS_T=7 * A, dq=8 * A, dk_=9 * A, dv_=10 * A, dS0=11 * A, B=1, H=2,
+             T=8, dk=16, dv=8, dt=0) | kw
+    return lib.sfda_decay_attn_bwd(*(a[x] for x in ("q", "k", "v", "g", "n", "S0", "dO", "dS_T", "dq", "dk_", "dv_", "dS0", "B", "H", "T",
+                                                   "dk", "dv")), 1.0, None, a["dt"], None, 0, None)
+
+
+def test_decay_attn_bwd(lib):
+    assert bwd(lib, dt=-1) == 4 and bwd(lib, dk=300) == 2 and bwd(lib, T=-4) == 2
+    for name in ("q", "k", "v", "g", "dO", "dq", "dk_", "dv_"):
+        assert bwd(lib, **{name: None}) == 1, name
+    assert bwd(lib, dq=A) == 6 and bwd(lib, dk_=8 * A) == 6 and bwd(lib, dS0=7 * A) == 6 and bwd(lib, dv_=10 * A + 2) == 5
+    assert bwd(lib, H=0) == 0
+
+
+def test_decay_attn_step(lib):
+    def step(q=A, k=2 * A, v=3 * A, g=4 * A, S=5 * A, o=6 * A, B=1, H=2, dk=16, dv=8, dt=0):
+        return lib.sfda_decay_attn_step(q, k, v, g, S, o, B, H, dk, dv, 1.0, None, dt, None)
+    assert step(dt=7) == 4 and step(dk=0) == 2 and step(dv=300) == 2 and step(B=-1) == 2
+    for name in ("q", "k", "v", "g", "S", "o"):
+        assert step(**{name: None}) == 1, name
+    assert step(S=A) == 6 and step(o=5 * A) == 6 and step(S=5 * A + 1) == 5
+    assert step(B=0) == 0
+
+
+def test_workspaces(lib):
+    f = lib.sfda_decay_attn_fwd_workspace_bytes
+    assert f(8, 16, 4096, 128, 128) == 0 and f(1, 1, 256, 128, 128) == 0 and f(1, 1, 0, 8, 8) == 0 and f(0, 1, 5000, 8, 8) == 0
+    assert f(1, 1, 4096, 128, 128) > 0 and f(1, 1, 4096, 257, 8) == 0 and f(-1, 1, 64, 8, 8) == 0
+    assert lib.sfda_decay_attn_bwd_workspace_bytes(1, 1, 4096, 128, 128) > 0
+    g = lib.sfda_group_norm_bwd_workspace_bytes
+    assert g(2, 3, 5, 16, 0) >= 2 * 3 * 16 * 4 and g(2, 3, 5, 4096, 0) == 0 and g(2, 3, 5, 16, 9) == 0 and g(2, 0, 5, 16, 0) == 0
+
+
+def rot(lib, **kw):
+    a = dict(q=A, k=2 * A, cos=3 * A, sin=4 * A, pos=None, bits=0, pstride=0, off=0, qo=5 * A, ko=6 * A, B=1, Hq=2, Hk=2, T=8, D=16, rot=8,
+             P=32, strides=None, dt=0) | kw
+    return lib.sfda_rotary(a["q"], a["k"], a["cos"], a["sin"], a["pos"], a["bits"], a["pstride"], a["off"], a["qo"], a["ko"], a["B"], a["Hq"],
+                           a["Hk"], a["T"], a["D"], a["rot"], a["P"], 0, 0, a["strides"], a["dt"], None)
+
+
+def test_rotary(lib):
+    assert rot(lib, dt=2) == 4
+    for bad in (dict(rot=7), dict(rot=0), dict(rot=18), dict(D=0), dict(D=5000), dict(T=-1), dict(P=0), dict(off=-1), dict(off=25),
+                dict(pos=7 * A, bits=16), dict(pos=7 * A, bits=32, pstride=-1), dict(B=1 << 20, T=1 << 20)):
+        assert rot(lib, **bad) == 2, bad
+    for name in ("q", "cos", "sin", "qo", "ko"):
+        assert rot(lib, **{name: None}) == 1, name
+    assert rot(lib, cos=3 * A + 2) == 5 and rot(lib, pos=7 * A + 4, bits=64) == 5
+    assert rot(lib, qo=2 * A) == 6 and rot(lib, qo=A + 64) == 6 and rot(lib, ko=5 * A) == 6 and rot(lib, qo=3 * A) == 6
+    # in place, but with other strides
+    assert rot(lib, qo=A, strides=arr(*([256, 128, 16] * 2 + [256, 16, 32] + [256, 128, 16]))) == 6
+    assert rot(lib, T=0) == 0 and rot(lib, B=0, q=None) == 0
+
+
+def norm(lib, **kw):
+    a = dict(x=A, w=2 * A, b=3 * A, z=4 * A, y=5 * A, B=1, H=2, T=8, D=16, act=1, eps=1e-5, dt=0) | kw
+    return lib.sfda_group_norm(a["x"], a["w"], a["b"], a["z"], a["y"], a["B"], a["H"], a["T"], a["D"], a["act"], a["eps"], None, a["dt"], None)
+
+
+def norm_bwd(lib, **kw):
+    a = dict(dy=A, x=2 * A, w=3 * A, b=4 * A, z=5 * A, dx=6 * A, dz=7 * A, dw=8 * A, db=9 * A, B=1, H=2, T=8, D=16, act=1, eps=1e-5, dt=0,
+             ws=10 * A, nws=1 << 20) | kw
+    return lib.sfda_group_norm_bwd(a["dy"], a["x"], a["w"], a["b"], a["z"], a["dx"], a["dz"], a["dw"], a["db"], a["B"], a["H"], a["T"], a["D"],
+                                   a["act"], a["eps"], None, a["dt"], a["ws"], a["nws"], None)
+
+
+def test_group_norm(lib):
+    assert norm(lib, dt=3) == 4
+    for bad in (dict(D=0), dict(D=2049), dict(act=2), dict(eps=-1.0), dict(eps=float("nan")), dict(T=-1)):
+        assert norm(lib, **bad) == 2 and norm_bwd(lib, **bad) == 2, bad
+    assert norm(lib, x=None) == 1 and norm(lib, y=None) == 1 and norm(lib, y=A) == 6 and norm(lib, y=2 * A) == 6 and norm(lib, w=2 * A + 1) == 5
+    assert norm(lib, B=0) == 0
+    for name in ("dy", "x", "dx", "dz", "ws"):
+        assert norm_bwd(lib, **{name: None}) == 1, name
+    assert norm_bwd(lib, nws=16) == 2 and norm_bwd(lib, dx=2 * A) == 6 and norm_bwd(lib, dw=9 * A) == 6 and norm_bwd(lib, ws=6 * A) == 6
+    assert norm_bwd(lib, H=0) == 0
+
+
+def test_binding(lib):
+    import torch
+    from paper_2607_11897_amd import sfda
+    B, H, T, dk, dv = 1, 2, 8, 16, 8
+    q, k, v, g = torch.zeros(B, H, T, dk), torch.zeros(B, H, T, dk), torch.zeros(B, H, T, dv), torch.zeros(H)
+    with pytest.raises(ValueError, match="GPU tensor"):
+        sfda.decay_attn_fwd(q, k, v, g)
+    with pytest.raises(ValueError, match="shape"):
+        sfda.decay_attn_fwd(q, k[:, :, :4], v, g)
+    with pytest.raises(ValueError, match="shape"):
+        sfda.decay_attn_fwd(q, k, v, g[:1])
+    with pytest.raises(TypeError, match="k must be"):
+        sfda.decay_attn_fwd(q, k.bfloat16(), v, g)
+    with pytest.raises(TypeError, match="log_decay must be float32"):
+        sfda.decay_attn_fwd(q, k, v, g.double())
+    with pytest.raises(TypeError, match="lengths must be int32"):
+        sfda.decay_attn_fwd(q, k, v, g, lengths=torch.zeros(B, dtype=torch.int64))
+    with pytest.raises(TypeError, match="S0 must be float32"):
+        sfda.decay_attn_fwd(q, k, v, g, torch.zeros(B, H, dk, dv, dtype=torch.bfloat16))
+    with pytest.raises(TypeError, match="unsupported dtype"):
+        sfda.decay_attn_fwd(q.half(), k.half(), v.half(), g)
+    with pytest.raises(ValueError, match="shape"):
+        sfda.decay_attn_bwd(q, k, v, g, None, q)
+    with pytest.raises(ValueError, match="shape"):
+        sfda.decay_attn_step(q[:, :, 0], k[:, :, 0], v[:, :, 0], g, torch.zeros(B, H, dk, dv + 1))
+    c = torch.zeros(32, 4)
+    with pytest.raises(ValueError, match="GPU tensor"):
+        sfda.rotary(q, k, c, c)
+    with pytest.raises(TypeError, match="positions"):
+        sfda.rotary(q, k, c, c, torch.zeros(T))
+    with pytest.raises(ValueError, match="shape"):
+        sfda.rotary(q, k, c, c[:3])
+    with pytest.raises(ValueError, match="activation"):
+        sfda.group_norm(q, activation="gelu")
+    with pytest.raises(ValueError, match="shape"):
+        sfda.group_norm(q, weight=torch.zeros(dk))
+    with pytest.raises(TypeError, match="gate must be"):
+        sfda.group_norm(q, gate=torch.zeros(B, T, H * dk).bfloat16())
+    with pytest.raises(ValueError, match="shape"):
+        sfda.group_norm_bwd(torch.zeros(B, T, dk), q)

@@ -1,0 +1,175 @@
+"""Pins of the oracle of the operators around the attention (float64, CPU): closed forms, invariants and
+central differences; planted mistakes in copies of the formulas fail them.  And the tables of the rotary positions."""
+from __future__ import annotations
+
+import math
+
+import numpy as np
+import pytest
+
+from oracle import layer as O
+
+
+def rng(seed):
+    return np.random.Generator(np.random.PCG64(seed))
+
+
+def differences(f, x, at, h=1e-5):
+    """Central differences of the scalar f at some places of the array x (changed and restored)."""
+    out = []
+    for i in at:
+        keep = x.flat[i]
+        x.flat[i] = keep + h
+        up = f()
+        x.flat[i] = keep - h
+        out.append((up - f()) / (2 * h))
+        x.flat[i] = keep
+    return np.array(out)
+
+
+def attn_inputs(seed, B=2, H=3, T=7, dk=4, dv=3):
+    r = rng(seed)
+    q, k, v = (r.standard_normal((B, H, T, d)) for d in (dk, dk, dv))
+    return q, k, v, np.array([0.0, -0.3, -2.0])[:H], r.standard_normal((B, H, dk, dv))
+
+
+def test_decay_attn_closed_form():
+    q, k, v, g, S0 = attn_inputs(1)
+    T = q.shape[2]
+    o, S = O.decay_attn(q, k, v, g, S0, scale=0.5)
+    t = np.arange(T)
+    for h in range(3):
+        D = np.where(t[:, None] >= t, np.exp(g[h] * (t[:, None] - t)), 0.0)
+        A = np.einsum("btd,bsd->bts", q[:, h], k[:, h]) * D
+        want = 0.5 * (A @ v[:, h] + np.exp(g[h] * (t + 1))[:, None] * (q[:, h] @ S0[:, h]))
+        assert np.max(np.abs(o[:, h] - want)) < 1e-12
+        last = np.exp(g[h] * T) * S0[:, h] + np.einsum("bt,btd,bte->bde", np.exp(g[h] * (T - 1 - t))[None].repeat(2, 0), k[:, h], v[:, h])
+        assert np.max(np.abs(S[:, h] - last)) < 1e-12
+
+
+def test_decay_attn_limits_and_lengths():
+    q, k, v, _, S0 = attn_inputs(2)
+    g = np.array([-np.inf, 0.0, -0.1])
+    o, S = O.decay_attn(q, k, v, g, S0)
+    assert np.allclose(o[:, 0], (q[:, 0] * k[:, 0]).sum(-1, keepdims=True) * v[:, 0])     # only the token itself
+    assert np.allclose(S[:, 1], S0[:, 1] + np.einsum("btd,bte->bde", k[:, 1], v[:, 1]))    # everything
+    o2, S2 = O.decay_attn(q, k, v, g, S0, lengths=[0, 3])
+    assert np.array_equal(S2[0], S0[0]) and not o2[0].any() and not o2[1, :, 3:].any()
+    part, Sp = O.decay_attn(q[:, :, :3], k[:, :, :3], v[:, :, :3], g, S0)
+    assert np.array_equal(o2[1, :, :3], part[1]) and np.array_equal(S2[1], Sp[1])
+    rest, Se = O.decay_attn(q[:, :, 3:], k[:, :, 3:], v[:, :, 3:], g, Sp)                  # and resumed
+    assert np.allclose(rest, o[:, :, 3:]) and np.allclose(Se, S)
+
+
+@pytest.mark.parametrize("seed,lengths", [(3, None), (4, [5, 0]), (5, [1, 7])])
+def test_decay_attn_backward_differences(seed, lengths):
+    q, k, v, g, S0 = attn_inputs(seed)
+    r = rng(seed + 100)
+    dO, dS = r.standard_normal(v.shape), r.standard_normal(S0.shape)
+
+    def loss():
+        o, S = O.decay_attn(q, k, v, g, S0, 0.7, lengths)
+        return float((o * dO).sum() + (S * dS).sum())
+    got = O.decay_attn_backward(q, k, v, g, S0, dO, dS, 0.7, lengths)
+    for name, x in (("dq", q), ("dk", k), ("dv", v), ("dS0", S0)):
+        at = r.choice(x.size, 40, replace=False)
+        assert np.max(np.abs(differences(loss, x, at) - got[name].flat[at])) < 1e-7, name
+
+
+@pytest.mark.parametrize("gate", [False, True])
+@pytest.mark.parametrize("act", ["none", "silu"])
+def test_group_norm_backward_differences(gate, act):
+    r = rng(7)
+    B, H, T, D = 2, 3, 4, 5
+    x, w, b = r.standard_normal((B, H, T, D)), r.standard_normal(H * D), r.standard_normal(H * D)
+    z = r.standard_normal((B, T, H * D)) if gate else None
+    dy = r.standard_normal((B, T, H * D))
+    loss = lambda: float((O.group_norm(x, w, b, z, act, 1e-3) * dy).sum())  # noqa: E731
+    got = O.group_norm_backward(dy, x, w, b, z, act, 1e-3)
+    for name, t in (("dx", x), ("dweight", w), ("dbias", b), ("dgate", z)):
+        if t is None:
+            assert got[name] is None
+            continue
+        at = np.arange(t.size)[:60]
+        assert np.max(np.abs(differences(loss, t, at) - got[name].flat[at])) < 1e-7, name
+
+
+def test_group_norm_definition():
+    r = rng(8)
+    x = r.standard_normal((2, 3, 4, 16)) * 5 + 3
+    y = O.group_norm(x, eps=0.0).reshape(2, 4, 3, 16)
+    assert np.max(np.abs(y.mean(-1))) < 1e-12 and np.max(np.abs(y.var(-1) - 1)) < 1e-12
+    assert np.allclose(O.group_norm(2 * x + 7, eps=0.0), y.reshape(2, 4, 48))
+    import torch
+    t = torch.nn.functional.group_norm(torch.from_numpy(x).permute(0, 2, 1, 3).reshape(8, 48), 3, eps=1e-5)
+    assert np.allclose(O.group_norm(x).reshape(8, 48), t.numpy())
+
+
+def tables(P, rot, **kw):
+    from paper_2607_11897_amd import sfda
+    c, s = sfda.rotary_tables(P, rot, device="cpu", **kw)
+    return c.double().numpy(), s.double().numpy()
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_rotary_invariants(interleaved):
+    r = rng(9)
+    q, k = r.standard_normal((2, 1, 2, 6, 10))
+    c, s = tables(64, 8)
+    at = np.arange(6)
+    a, b = O.rotary(q, c, s, at, interleaved), O.rotary(k, c, s, at, interleaved)
+    assert np.array_equal(a[..., 8:], q[..., 8:])
+    assert np.allclose(O.rotary(a, c, s, at, interleaved, inverse=True), q, atol=1e-6)
+    # scores depend on the distance of the positions alone (to the float32 of the tables)
+    far = [O.rotary(x, c, s, at + 31, interleaved) for x in (q, k)]
+    assert np.max(np.abs(a @ b.swapaxes(-1, -2) - far[0] @ far[1].swapaxes(-1, -2))) < 1e-5
+    # and the turn is the complex product
+    i, j = O._pairs(10, 8, interleaved)
+    z = (q[..., i] + 1j * q[..., j]) * (c + 1j * s)[at]
+    assert np.allclose(a[..., i], z.real) and np.allclose(a[..., j], z.imag)
+
+
+def test_rotary_tables():
+    pos = np.arange(300.0)[:, None]
+    freq = 10000.0 ** (-2.0 * np.arange(8) / 16)
+    c, s = tables(300, 16)
+    assert np.max(np.abs(c - np.cos(pos * freq))) < 6.1e-8 and np.max(np.abs(s - np.sin(pos * freq))) < 6.1e-8    # half an ulp of 1
+    lin = tables(300, 16, scaling=dict(kind="linear", factor=4.0))
+    assert np.allclose(lin[0][::4], c[:75], atol=1e-7)
+    ntk = tables(300, 16, scaling=dict(kind="ntk", factor=4.0))
+    assert np.allclose(ntk[0][:, 0], c[:, 0], atol=1e-7) and np.allclose(ntk[0][::4, 7], c[:75, 7], atol=1e-7)
+    yarn = tables(300, 16, scaling=dict(kind="yarn", factor=4.0, length=4096))
+    m = 0.1 * math.log(4.0) + 1.0
+    assert np.allclose(yarn[0][:, 0], m * c[:, 0], atol=2e-7) and np.allclose(yarn[0][::4, 7], m * c[:75, 7], atol=2e-7)
+    # between: pairs of between 32 and 1 turns over the length lie between both
+    turns = 4096 * freq / (2 * math.pi)
+    mid = [i for i in range(8) if 1.5 < turns[i] < 30]
+    f = np.arctan2(yarn[1][1], yarn[0][1])
+    assert mid and all(freq[i] / 4 < f[i] < freq[i] for i in mid)
+    one = tables(20, 2, scaling=dict(kind="yarn", factor=2.0, length=100, amplitude=1.0))
+    assert np.isfinite(one[0]).all() and np.max(np.abs(one[0])) <= 1.0
+    from paper_2607_11897_amd import sfda
+    for bad in (dict(rot=3), dict(rot=0), dict(scaling=dict(kind="other", factor=2.0)), dict(scaling=dict(kind="linear", factor=0.0)),
+                dict(rot=2, scaling=dict(kind="ntk", factor=2.0)), dict(positions=0)):
+        with pytest.raises(ValueError):
+            sfda.rotary_tables(**(dict(positions=4, rot=4, device="cpu") | bad))
+
+
+@pytest.mark.parametrize("mistake", ["decay_after", "no_scale", "early_state", "reverse_decay"])
+def test_planted_mistakes_fail(mistake):
+    """Copies of the recurrence or its reverse sweep with one mistake each differ from the closed form or from differences."""
+    q, k, v, g, S0 = attn_inputs(11, B=1)
+    o, S = O.decay_attn(q, k, v, g, S0, scale=0.7)
+    lam = np.exp(g)
+    o2, S2 = np.zeros_like(o), S0.copy()
+    for h in range(3):
+        for t in range(q.shape[2]):
+            kv = np.outer(k[0, h, t], v[0, h, t])
+            if mistake == "early_state":
+                o2[0, h, t] = 0.7 * (q[0, h, t] @ S2[0, h])
+            S2[0, h] = lam[h] * (S2[0, h] + kv) if mistake == "decay_after" else lam[h] * S2[0, h] + kv
+            if mistake == "reverse_decay":
+                S2[0, h] = S2[0, h] * lam[h] + 0.0
+            if mistake != "early_state":
+                o2[0, h, t] = (1.0 if mistake == "no_scale" else 0.7) * (q[0, h, t] @ S2[0, h])
+    assert np.max(np.abs(o2 - o)) > 1e-2 * np.max(np.abs(o))
