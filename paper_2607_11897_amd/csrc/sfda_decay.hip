@@ -20,8 +20,10 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int NT = 256;                  // threads of a scan workgroup
-constexpr int NS = DECAY_SLICE;          // its value columns, 16 for each wave
+constexpr int NT = 512;                  // threads of a scan workgroup, two waves on a SIMD
+constexpr int NW = NT / 64;
+constexpr int NS = DECAY_SLICE;          // its value columns
+constexpr int NJ = 256;                  // threads of the small kernels
 
 // two float32 as a pair of bfloat16, each to nearest even
 __device__ __forceinline__ uint32_t pack2(float a, float b)
@@ -38,27 +40,22 @@ __device__ __forceinline__ float hi_f32(uint32_t w) { return __uint_as_float(w &
 // What the element type decides.  C: tokens of a block; VE: elements of a 16-byte vector; KB: the
 // contraction length of one operand fragment; PAD: elements a row in LDS is longer than its channels (keeps
 // the 16 rows of a fragment on different banks).
-// Lane l of a fragment has index c = l % 16 of the free axis and, of the contraction, the
-// places 4 g .. 4 g + 3 (g = l / 16) of each 16: what an accumulator tile holds of its
-// rows, so that a tile becomes an operand without leaving its lane.
+// Lane l of a fragment has index c = l % 16 of the free axis and KB / 4 places of the contraction for its
+// group g = l / 16.  Sums over channels take VE neighbours (rows: one 16-byte read); sums over tokens take
+// the places 4 g .. 4 g + 3 of each 16, which is what an accumulator tile holds of its rows, so that scores become
+// an operand without leaving their lane.
 template <typename E> struct Ops;
 
 template <> struct Ops<uint16_t> {
     static constexpr int C = 64, VE = 8, KB = 32, PAD = 8;
     typedef bf16x8 Frag;
-    // row-major [free][contraction]: two 8-byte reads
-    static __device__ __forceinline__ Frag rows(const uint16_t* p)
-    {
-        u32x4 w;
-        w.lo = *reinterpret_cast<const u32x2*>(p);
-        w.hi = *reinterpret_cast<const u32x2*>(p + 16);
-        return __builtin_bit_cast(Frag, w);
-    }
+    // row-major [free][contraction]
+    static __device__ __forceinline__ Frag rows(const uint16_t* p) { return __builtin_bit_cast(Frag, *reinterpret_cast<const u32x4*>(p)); }
     // row-major [contraction][free]: the transposing LDS read takes, from each group of 16 lanes,
-    // 4 rows of 16 (lane l: row l / 4, 4 elements from 4 (l % 4)) and gives lane l column l
-    static __device__ __forceinline__ Frag cols(const uint16_t* base, int stride, int lane)
+    // 4 rows of 16 (lane l: row l / 4, 4 elements) and gives lane l column l.  p: the lane's own 4 elements in
+    // row 4 g + c / 4
+    static __device__ __forceinline__ Frag cols(const uint16_t* p, int stride)
     {
-        const uint16_t* p = base + (4 * (lane >> 4) + ((lane >> 2) & 3)) * stride + 4 * (lane & 3);
         typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
         const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p));
         const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 16 * stride));
@@ -67,6 +64,8 @@ template <> struct Ops<uint16_t> {
         w.hi = __builtin_bit_cast(u32x2, b);
         return __builtin_bit_cast(Frag, w);
     }
+    // offset of the lane's own elements for cols: 4 of column block c % 4 whose blocks are `step` apart
+    static __device__ __forceinline__ int cols_at(int stride, int step, int c, int g) { return (4 * g + (c >> 2)) * stride + step * (c & 3); }
     // from the accumulator tiles t[0], t[1] whose rows are the contraction
     static __device__ __forceinline__ Frag acc(const f32x4* t)
     {
@@ -77,11 +76,7 @@ template <> struct Ops<uint16_t> {
     {
         d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, d, 0, 0, 0);
     }
-    static __device__ __forceinline__ void store4(uint16_t* p, const f32x4& x)
-    {
-        const u32x2 w = {pack2(x[0], x[1]), pack2(x[2], x[3])};
-        memcpy(p, &w, 8);
-    }
+    static __device__ __forceinline__ u32x2 pack4(const f32x4& x) { return u32x2{pack2(x[0], x[1]), pack2(x[2], x[3])}; }
     static __device__ __forceinline__ void store1(uint16_t* p, float x) { *p = f32_to_bf16_bits(x); }
     // the weighted values as a sum of bfloat16 parts: the state has to keep 32 bits' worth of them, and one
     // rounding of the product to bfloat16 would leave 8 bits
@@ -108,18 +103,15 @@ template <> struct Ops<float> {
     static constexpr int C = 32, VE = 4, KB = 16, PAD = 4;
     typedef f32x4 Frag;
     static __device__ __forceinline__ Frag rows(const float* p) { return *reinterpret_cast<const Frag*>(p); }
-    static __device__ __forceinline__ Frag cols(const float* base, int stride, int lane)
-    {
-        const float* p = base + 4 * (lane >> 4) * stride + (lane & 15);
-        return Frag{p[0], p[stride], p[2 * stride], p[3 * stride]};
-    }
+    static __device__ __forceinline__ Frag cols(const float* p, int stride) { return Frag{p[0], p[stride], p[2 * stride], p[3 * stride]}; }
+    static __device__ __forceinline__ int cols_at(int stride, int step, int c, int g) { return 4 * g * stride + step * (c >> 2) + (c & 3); }
     static __device__ __forceinline__ Frag acc(const f32x4* t) { return t[0]; }
     static __device__ __forceinline__ void mma(f32x4& d, const Frag& a, const Frag& b)
     {
 #pragma unroll
         for (int s = 0; s < 4; ++s) d = __builtin_amdgcn_mfma_f32_16x16x4f32(a[s], b[s], d, 0, 0, 0);
     }
-    static __device__ __forceinline__ void store4(float* p, const f32x4& x) { memcpy(p, &x, 16); }
+    static __device__ __forceinline__ f32x4 pack4(const f32x4& x) { return x; }
     static __device__ __forceinline__ void store1(float* p, float x) { *p = x; }
     static constexpr int PARTS = 1;
     static __device__ __forceinline__ void weighted(Frag (&out)[PARTS], const Frag& v, const float (&w)[4])
@@ -152,9 +144,10 @@ __device__ __forceinline__ int seq_length(const int* lengths, int b, int T)
 
 // A block's rows of one tensor on their way to LDS: ROWS tokens x COLS channels (COLS padded), 16-byte
 // vectors held in registers between the load and the write.  Loads are unconditional and in bounds: rows
-// past the block's n are clamped to its last, the vector that would cross a row's end is moved
-// back to end with it (the write then goes by elements), and padding is never loaded.
-template <typename E, int ROWS, int COLS> struct Tile {
+// past the block's n are clamped to its last, and padding is clamped to channel 0 and never written.
+// EXACT: the channels are whole vectors.  Otherwise the vector that would cross a row's end is moved back to end with it (the
+// write then goes by elements), and rows shorter than a vector are read by elements.
+template <typename E, int ROWS, int COLS, bool EXACT> struct Tile {
     static constexpr int VE = Ops<E>::VE, VPR = COLS / VE, RPP = NT / VPR, N = ROWS / RPP, STRIDE = COLS + Ops<E>::PAD;
     static_assert(ROWS % RPP == 0 && NT % VPR == 0, "whole passes");
     u32x4 x[N];
@@ -163,8 +156,8 @@ template <typename E, int ROWS, int COLS> struct Tile {
     __device__ __forceinline__ void load(const E* p, long long st, int cols, int n, int tid)
     {
         const int col = (tid % VPR) * VE;
-        if (cols >= VE) {
-            const int at = col + VE <= cols ? col : cols - VE;
+        if (EXACT || cols >= VE) {
+            const int at = col + VE <= cols ? col : EXACT ? 0 : cols - VE;
 #pragma unroll
             for (int u = 0; u < N; ++u) {
                 const int r = tid / VPR + u * RPP;
@@ -190,7 +183,7 @@ template <typename E, int ROWS, int COLS> struct Tile {
             const int r = tid / VPR + u * RPP;
             const u32x4 z = {0, 0, 0, 0};
             const u32x4 w = r < n ? x[u] : z;
-            if (col + VE <= cols || cols < VE) {
+            if (EXACT || col + VE <= cols || cols < VE) {
                 *reinterpret_cast<u32x4*>(lds + r * STRIDE + col) = w;
             } else {
                 E e[VE];
@@ -202,29 +195,73 @@ template <typename E, int ROWS, int COLS> struct Tile {
     }
 };
 
-// LDS of a scan: a block's q, k, v and scores, and the powers of lambda
+// A fragment's 16 bytes of a row of `cols` channels, from channel `col` on, on their way from global memory:
+// loaded in bounds (as a tile's vectors) and put in place when it is used, zero past the row.
+template <typename E, bool EXACT> __device__ __forceinline__ u32x4 row_load(const E* row, int col, int cols)
+{
+    constexpr int VE = Ops<E>::VE;
+    u32x4 x = {0, 0, 0, 0};
+    if (EXACT || cols >= VE) {
+        memcpy(&x, row + (col + VE <= cols ? col : EXACT ? 0 : cols - VE), 16);
+    } else if (col == 0) {
+        E e[VE] = {};
+        for (int i = 0; i < VE - 1; ++i)
+            if (i < cols) e[i] = row[i];
+        memcpy(&x, e, 16);
+    }
+    return x;
+}
+template <typename E, bool EXACT> __device__ __forceinline__ u32x4 row_place(u32x4 x, int col, int cols)
+{
+    constexpr int VE = Ops<E>::VE;
+    typedef unsigned long long u64;
+    const u32x4 zero = {0, 0, 0, 0};
+    if (col >= cols) return zero;
+    if (EXACT || cols < VE || col + VE <= cols) return x;
+    const int s = (col + VE - cols) * 8 * static_cast<int>(sizeof(E));      // 16 .. 112 bits
+    u64 lo = (static_cast<u64>(x[1]) << 32) | x[0], hi = (static_cast<u64>(x[3]) << 32) | x[2];
+    if (s >= 64) {
+        lo = hi >> (s - 64);
+        hi = 0;
+    } else {
+        lo = (lo >> s) | (hi << (64 - s));
+        hi >>= s;
+    }
+    return u32x4{static_cast<uint32_t>(lo), static_cast<uint32_t>(lo >> 32), static_cast<uint32_t>(hi), static_cast<uint32_t>(hi >> 32)};
+}
+
+// LDS of a scan: the keys and values of a block and of the next, the state as an operand ([column][channel], twice where
+// it fits, so that a block needs one barrier), and the powers of lambda
 template <typename E, int DAP> struct Smem {
     static constexpr int C = Ops<E>::C, P = Ops<E>::PAD;
-    E q[C * (DAP + P)], k[C * (DAP + P)], v[C * (NS + P)], a[C * (C + P)];
+    static constexpr int KV = C * (DAP + P) + C * (NS + P), ST = NS * (DAP + P);
+    static constexpr int SB = (2 * KV + 2 * ST) * sizeof(E) <= 158 * 1024 ? 2 : 1;
+    E k[2][C * (DAP + P)], v[2][C * (NS + P)], s[SB][ST];
     float pw[C + 1];
 };
 
-// One workgroup scans the tokens of one segment of one head for 64 value columns of one role.  Wave w
-// owns 16 of the columns: its part of the state stays in accumulator tiles S[d-tile] (rows d, columns n).
-// STATES: only the segment's state from zero, to the workspace.
-template <typename E, int DAP, bool STATES>
+// One workgroup scans the tokens of one segment of one head for 64 value columns of one role.  Its 8 waves
+// are CT row tiles (16 tokens each) x CG groups of 16 NP columns.  For a block, a wave forms the outputs of its row tile and its
+// columns: scores against the keys of earlier tiles and its own, kept in registers as the operand of the
+// product with the values, and the queries (which no other row tile needs: from global memory straight into
+// fragments) times the state.  Then it updates its share of the state, DTW of the channel tiles for its columns,
+// and puts it into LDS as the next block's operand.  STATES: only the segment's state from zero, to the workspace.
+template <typename E, int DAP, bool STATES, bool EXACT>
 __global__ __launch_bounds__(NT) void decay_scan_kernel(DecayLaunch L)
 {
     typedef Ops<E> O;
     typedef typename O::Frag Frag;
-    constexpr int C = O::C, KB = O::KB, CT = C / 16, DT = DAP / 16, TPF = KB / 16;   // tiles of 16 in a fragment
-    constexpr int SQ = DAP + O::PAD, SV = NS + O::PAD, SA = C + O::PAD;
-    constexpr int SCORES = CT * (CT + 1) / 2, SPW = (SCORES + 3) / 4;                // causal score tiles; a wave's
     typedef Smem<E, DAP> Mem;
+    constexpr int C = O::C, KB = O::KB, VE = O::VE, CT = C / 16, CG = NW / CT, NP = NS / CG / 16;
+    constexpr int DT = DAP / 16, DTW = DT / CT, DF = DAP / KB, CF = C / KB, TPF = KB / 16;
+    constexpr int SK = DAP + O::PAD, SV = NS + O::PAD, SB = Mem::SB;
+    static_assert(DT % CT == 0 && NP * CG * 16 == NS, "tiles");
     extern __shared__ __align__(16) unsigned char smem[];
     Mem& M = *reinterpret_cast<Mem*>(smem);
 
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 15, g = lane >> 4;
+    // (waves w and w + 4 share a SIMD: the row tiles of a pair add up to the same number of score tiles)
+    const int rt = CT == 4 ? (w < 4 ? w : 7 - w) : (w ^ (w >> 2)) & 1, cg = w / CT;
     int total = 0;
     for (int r = 0; r < L.roles; ++r) total += L.role[r].slices;
     long bh;
@@ -253,26 +290,33 @@ __global__ __launch_bounds__(NT) void decay_scan_kernel(DecayLaunch L)
     kp += tok0 * R.k_s[2];
     vp += tok0 * R.v_s[2];
 
-    {   // padding of the tiles, and the score tiles above the diagonal that a fragment reads, stay zero
+    {   // padding stays zero
         u32x4* z = reinterpret_cast<u32x4*>(smem);
         const u32x4 zero = {0, 0, 0, 0};
         for (int i = tid; i < static_cast<int>(offsetof(Mem, pw)) / 16; i += NT) z[i] = zero;
         if (tid <= C) M.pw[tid] = tid == 0 ? 1.f : expf(static_cast<float>(tid) * gl);
     }
 
-    Tile<E, C, DAP> tq, tk;
-    Tile<E, C, NS> tv;
-    int n = end - begin < C ? end - begin : C;
-    if (n > 0) {
-        if (!STATES) tq.load(qp + begin * qst, qst, da, n, tid);
-        tk.load(kp + begin * kst, kst, da, n, tid);
-        tv.load(vp + begin * vst, vst, dbs, n, tid);
-    }
+    Tile<E, C, DAP, EXACT> tk;
+    Tile<E, C, NS, EXACT> tv;
+    u32x4 qn[DF];
+    auto load = [&](int at) {
+        const int n = end - at < C ? end - at : C;
+        tk.load(kp + at * kst, kst, da, n, tid);
+        tv.load(vp + at * vst, vst, dbs, n, tid);
+        if (!STATES) {
+            const int i = 16 * rt + c;
+            const E* row = qp + (at + (i < n ? i : n - 1)) * qst;
+#pragma unroll
+            for (int f = 0; f < DF; ++f) qn[f] = row_load<E, EXACT>(row, KB * f + VE * g, da);
+        }
+    };
+    if (begin < end) load(begin);
 
-    // the state's tiles: lane (c, g) has rows 16 d + 4 g + r of column 16 w + c
-    f32x4 S[DT];
-    const int col = 16 * w + c;
-    const bool scol = col < dbs;
+    // the wave's columns: tile p has column (c, p); a lane's 4 NP columns of its outputs are neighbours
+    const int col0 = 16 * NP * cg + 4 * NP * (c >> 2) + (c & 3);      // + 4 p
+    // its state: lane (c, g) has rows 16 (rt DTW + d) + 4 g + r of that column
+    f32x4 S[DTW][NP];
     {
         const float* src = nullptr;
         long long rs = 0, cs = 0;
@@ -288,34 +332,30 @@ __global__ __launch_bounds__(NT) void decay_scan_kernel(DecayLaunch L)
             }
         }
 #pragma unroll
-        for (int d = 0; d < DT; ++d)
+        for (int d = 0; d < DTW; ++d)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int row = 16 * d + 4 * g + r;
-                S[d][r] = src != nullptr && scol && row < da ? src[row * rs + (n0 + col) * cs] : 0.f;
-            }
+            for (int p = 0; p < NP; ++p)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int row = 16 * (rt * DTW + d) + 4 * g + r, col = col0 + 4 * p;
+                    S[d][p][r] = src != nullptr && col < dbs && row < da ? src[row * rs + (n0 + col) * cs] : 0.f;
+                }
     }
     __syncthreads();
 
     // weights that are the same for every whole block: of the scores, of the start state's rows, of the values
-    float wd[SPW][4], wi[CT], wv[C / KB][KB / 4];
+    float wd[CT][4], wi = 0.f, wv[CF][KB / 4];
 #pragma unroll
-    for (int s = 0; s < SPW; ++s) {
-        const int id = w + 4 * s;
-        int ti = 0;
-        while ((ti + 1) * (ti + 2) / 2 <= id) ++ti;
-        const int tj = id - ti * (ti + 1) / 2;
+    for (int t = 0; t < CT; ++t)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const int far = 16 * (ti - tj) + c - (4 * g + r);
-            wd[s][r] = far >= 0 && far <= C ? R.intra * M.pw[far] : 0.f;
+            const int far = 16 * (rt - t) + c - (4 * g + r);
+            wd[t][r] = far >= 0 ? R.intra * M.pw[far] : 0.f;
         }
-    }
-#pragma unroll
-    for (int t = 0; t < CT; ++t) wi[t] = R.inter * M.pw[16 * t + c + (R.reverse ? 0 : 1)];
+    wi = R.inter * M.pw[16 * rt + c + (R.reverse ? 0 : 1)];
     auto value_weights = [&](int m) {
 #pragma unroll
-        for (int f = 0; f < C / KB; ++f)
+        for (int f = 0; f < CF; ++f)
 #pragma unroll
             for (int e = 0; e < KB / 4; ++e) {
                 const int j = KB * f + 16 * (e / 4) + 4 * g + (e & 3), far = m - 1 - j + (R.reverse ? 1 : 0);
@@ -325,88 +365,120 @@ __global__ __launch_bounds__(NT) void decay_scan_kernel(DecayLaunch L)
     value_weights(C);
     Pow lam = decay_pow(C, gl);
 
-    for (int at = begin; at < end; at += C) {
-        n = end - at < C ? end - at : C;
-        if (!STATES) tq.store(M.q, da, n, tid);
-        tk.store(M.k, da, n, tid);
-        tv.store(M.v, dbs, n, tid);
-        const int next = at + C;
-        if (next < end) {
-            const int m = end - next < C ? end - next : C;
-            if (!STATES) tq.load(qp + next * qst, qst, da, m, tid);
-            tk.load(kp + next * kst, kst, da, m, tid);
-            tv.load(vp + next * vst, vst, dbs, m, tid);
+    // the state, rounded to the element type, as the operand of its product with the queries
+    auto state_out = [&](E* to) {
+#pragma unroll
+        for (int d = 0; d < DTW; ++d)
+#pragma unroll
+            for (int p = 0; p < NP; ++p) {
+                const auto x = O::pack4(S[d][p]);
+                memcpy(to + (col0 + 4 * p) * SK + 16 * (rt * DTW + d) + 4 * g, &x, sizeof(x));
+            }
+    };
+    if (begin < end) {
+        const int n = end - begin < C ? end - begin : C;
+        tk.store(M.k[0], da, n, tid);
+        tv.store(M.v[0], dbs, n, tid);
+        if (!STATES) state_out(M.s[0]);
+    }
+    __syncthreads();
+
+    int buf = 0;
+    for (int at = begin; at < end; at += C, buf ^= 1) {
+        const int n = end - at < C ? end - at : C, next = at + C;
+        const E *K = M.k[buf], *V = M.v[buf], *SL = M.s[SB == 2 ? buf : 0];
+        Frag qf[DF];
+        if (!STATES) {
+#pragma unroll
+            for (int f = 0; f < DF; ++f) qf[f] = __builtin_bit_cast(Frag, row_place<E, EXACT>(qn[f], KB * f + VE * g, da));
         }
+        if (next < end) load(next);
         if (n < C) {
             value_weights(n);
             lam = decay_pow(n, gl);
         }
-        __syncthreads();
-
-        Frag vf[C / KB];
+        Frag vf[CF][NP];
 #pragma unroll
-        for (int f = 0; f < C / KB; ++f) vf[f] = O::cols(M.v + KB * f * SV + 16 * w, SV, lane);
+        for (int f = 0; f < CF; ++f)
+#pragma unroll
+            for (int p = 0; p < NP; ++p)
+                vf[f][p] = O::cols(V + KB * f * SV + 16 * NP * cg + 4 * p + O::cols_at(SV, 4 * NP, c, g), SV);
         if (!STATES) {
-            // scores, transposed: rows j, columns i, so that a lane writes four of a row
+            // outputs, transposed: rows are columns of v, columns are tokens
+            f32x4 x[NP];
 #pragma unroll
-            for (int s = 0; s < SPW; ++s) {
-                const int id = w + 4 * s;
-                if (id < SCORES) {
-                    int ti = 0;
-                    while ((ti + 1) * (ti + 2) / 2 <= id) ++ti;
-                    const int tj = id - ti * (ti + 1) / 2;
-                    f32x4 x = zero4();
+            for (int p = 0; p < NP; ++p) x[p] = zero4();
 #pragma unroll
-                    for (int f = 0; f < DAP / KB; ++f)
-                        O::mma(x, O::rows(M.k + (16 * tj + c) * SQ + KB * f + 4 * g), O::rows(M.q + (16 * ti + c) * SQ + KB * f + 4 * g));
+            for (int f = 0; f < DF; ++f)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) x[r] = ti > tj || c >= 4 * g + r ? x[r] * wd[s][r] : 0.f;
-                    // one rounding to the element type: the scores are an operand of the product with v
-                    O::store4(M.a + (16 * ti + c) * SA + 16 * tj + 4 * g, x);
-                }
-            }
-            __syncthreads();
-
-            Frag sf[DAP / KB];      // the state as an operand, rounded to the element type
+                for (int p = 0; p < NP; ++p) O::mma(x[p], O::rows(SL + (col0 + 4 * p) * SK + KB * f + VE * g), qf[f]);
 #pragma unroll
-            for (int f = 0; f < DAP / KB; ++f) sf[f] = O::acc(&S[TPF * f]);
+            for (int p = 0; p < NP; ++p)
 #pragma unroll
-            for (int t = 0; t < CT; ++t) {
-                // O^T: rows n, columns i
-                f32x4 x = zero4();
+                for (int r = 0; r < 4; ++r) x[p][r] *= wi;
+            // scores, transposed: rows are keys; rounded once to the element type, as the operand of the product with v
 #pragma unroll
-                for (int f = 0; f < DAP / KB; ++f)
-                    O::mma(x, sf[f], O::rows(M.q + (16 * t + c) * SQ + KB * f + 4 * g));
+            for (int f = 0; f < CF; ++f) {
+                if (TPF * f > rt) continue;
+                f32x4 sc[TPF];
 #pragma unroll
-                for (int r = 0; r < 4; ++r) x[r] *= wi[t];
+                for (int u = 0; u < TPF; ++u) {
+                    const int t = TPF * f + u;
+                    sc[u] = zero4();
+                    if (t <= rt) {
 #pragma unroll
-                for (int f = 0; f < C / KB; ++f)
-                    if (KB * f < 16 * (t + 1)) O::mma(x, vf[f], O::rows(M.a + (16 * t + c) * SA + KB * f + 4 * g));
-                const int i = 16 * t + c, at_n = 16 * w + 4 * g;
-                if (i < n) {
-                    E* p = op + (tok0 * R.o_s[2] + (at + i) * ost) + at_n;
-                    if (at_n + 4 <= dbs) {
-                        O::store4(p, x);
-                    } else {
-                        for (int r = 0; r < 4; ++r)
-                            if (at_n + r < dbs) O::store1(p + r, x[r]);
+                        for (int e = 0; e < DF; ++e) O::mma(sc[u], O::rows(K + (16 * t + c) * SK + KB * e + VE * g), qf[e]);
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) sc[u][r] = t < rt || c >= 4 * g + r ? sc[u][r] * wd[t][r] : 0.f;
                     }
+                }
+                const Frag a = O::acc(sc);
+#pragma unroll
+                for (int p = 0; p < NP; ++p) O::mma(x[p], vf[f][p], a);
+            }
+            const int i = 16 * rt + c, at_n = 16 * NP * cg + 4 * NP * g;
+            if (i < n) {
+                E* to = op + (tok0 * R.o_s[2] + (at + i) * ost) + at_n;
+                if (at_n + 4 * NP <= dbs) {
+                    decltype(O::pack4(x[0])) y[NP];
+#pragma unroll
+                    for (int p = 0; p < NP; ++p) y[p] = O::pack4(x[p]);
+                    memcpy(to, y, sizeof(y));
+                } else if (!EXACT) {
+#pragma unroll
+                    for (int p = 0; p < NP; ++p)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+                            if (at_n + 4 * p + r < dbs) O::store1(to + 4 * p + r, x[p][r]);
                 }
             }
         }
-        Frag vw[C / KB][O::PARTS];
+        if (SB == 1 && !STATES) __syncthreads();
 #pragma unroll
-        for (int f = 0; f < C / KB; ++f) O::weighted(vw[f], vf[f], wv[f]);
+        for (int d = 0; d < DTW; ++d)
 #pragma unroll
-        for (int d = 0; d < DT; ++d) {
+            for (int p = 0; p < NP; ++p)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) S[d][r] = __builtin_fmaf(S[d][r], lam.hi, S[d][r] * lam.lo);
+                for (int r = 0; r < 4; ++r) S[d][p][r] = __builtin_fmaf(S[d][p][r], lam.hi, S[d][p][r] * lam.lo);
 #pragma unroll
-            for (int f = 0; f < C / KB; ++f) {
-                const Frag kf = O::cols(M.k + KB * f * SQ + 16 * d, SQ, lane);
+        for (int f = 0; f < CF; ++f) {
+            Frag vw[NP][O::PARTS];
 #pragma unroll
-                for (int s = O::PARTS - 1; s >= 0; --s) O::mma(S[d], kf, vw[f][s]);
+            for (int p = 0; p < NP; ++p) O::weighted(vw[p], vf[f][p], wv[f]);
+#pragma unroll
+            for (int d = 0; d < DTW; ++d) {
+                const Frag kf = O::cols(K + KB * f * SK + 16 * (rt * DTW + d) + O::cols_at(SK, 4, c, g), SK);
+#pragma unroll
+                for (int p = 0; p < NP; ++p)
+#pragma unroll
+                    for (int s = O::PARTS - 1; s >= 0; --s) O::mma(S[d][p], kf, vw[p][s]);
             }
+        }
+        if (next < end) {
+            const int m = end - next < C ? end - next : C;
+            if (!STATES) state_out(M.s[SB == 2 ? buf ^ 1 : 0]);
+            tk.store(M.k[buf ^ 1], da, m, tid);
+            tv.store(M.v[buf ^ 1], dbs, m, tid);
         }
         __syncthreads();
     }
@@ -422,29 +494,31 @@ __global__ __launch_bounds__(NT) void decay_scan_kernel(DecayLaunch L)
         rs = R.s_row;
         cs = R.s_col;
     }
-    if (dst != nullptr && scol) {
+    if (dst != nullptr) {
 #pragma unroll
-        for (int d = 0; d < DT; ++d)
+        for (int d = 0; d < DTW; ++d)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int row = 16 * d + 4 * g + r;
-                if (row < da) dst[row * rs + (n0 + col) * cs] = S[d][r];
-            }
+            for (int p = 0; p < NP; ++p)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int row = 16 * (rt * DTW + d) + 4 * g + r, col = col0 + 4 * p;
+                    if (row < da && col < dbs) dst[row * rs + (n0 + col) * cs] = S[d][p][r];
+                }
     }
     if (!STATES && len < L.T) {     // tokens past the sequence's length
         const long long hi = first + L.seg_tokens < L.T ? first + L.seg_tokens : L.T;
-        for (long long t = (first < len ? len : first) + w; t < hi; t += NT / 64)
+        for (long long t = (first < len ? len : first) + w; t < hi; t += NW)
             if (lane < dbs) O::store1(op + t * R.o_s[2] + lane, 0.f);
     }
 }
 
 // The segments' states from zero become the states that enter them: one thread for an element of a
 // head's state, in place.
-__global__ __launch_bounds__(NT) void decay_join_kernel(DecayLaunch L)
+__global__ __launch_bounds__(NJ) void decay_join_kernel(DecayLaunch L)
 {
     const DecayRole& R = L.role[blockIdx.z];
     const long long size = static_cast<long long>(R.da) * R.db, heads = static_cast<long long>(L.B) * L.H;
-    const long long at = static_cast<long long>(blockIdx.x) * NT + threadIdx.x, bh = at / size, e = at - bh * size;
+    const long long at = static_cast<long long>(blockIdx.x) * NJ + threadIdx.x, bh = at / size, e = at - bh * size;
     if (bh >= heads) return;
     const int b = static_cast<int>(bh / L.H), h = static_cast<int>(bh - static_cast<long long>(b) * L.H);
     const int len = seq_length(L.lengths, b, L.T);
@@ -462,21 +536,28 @@ __global__ __launch_bounds__(NT) void decay_join_kernel(DecayLaunch L)
     }
 }
 
-template <typename E, int DAP> hipError_t scan(const DecayLaunch& L, unsigned groups, bool states, hipStream_t st)
+template <typename E, int DAP, bool STATES, bool EXACT> hipError_t scan(const DecayLaunch& L, unsigned groups, hipStream_t st)
 {
     constexpr size_t bytes = sizeof(Smem<E, DAP>);
     static_assert(bytes <= 160 * 1024, "one compute unit's LDS");
-    if (states)
-        hipLaunchKernelGGL((decay_scan_kernel<E, DAP, true>), dim3(groups, L.segments - 1), dim3(NT), bytes, st, L);
-    else
-        hipLaunchKernelGGL((decay_scan_kernel<E, DAP, false>), dim3(groups, L.segments), dim3(NT), bytes, st, L);
+    hipLaunchKernelGGL((decay_scan_kernel<E, DAP, STATES, EXACT>), dim3(groups, STATES ? L.segments - 1 : L.segments), dim3(NT), bytes, st, L);
     return hipGetLastError();
 }
 
-template <typename E> hipError_t scan_da(const DecayLaunch& L, int da, unsigned groups, bool states, hipStream_t st)
+template <typename E, bool STATES, bool EXACT> hipError_t scan_da(const DecayLaunch& L, int da, unsigned groups, hipStream_t st)
 {
-    return da <= 64 ? scan<E, 64>(L, groups, states, st) : da <= 128 ? scan<E, 128>(L, groups, states, st)
-                                                                      : scan<E, 256>(L, groups, states, st);
+    return da <= 64 ? scan<E, 64, STATES, EXACT>(L, groups, st) : da <= 128 ? scan<E, 128, STATES, EXACT>(L, groups, st)
+                                                                             : scan<E, 256, STATES, EXACT>(L, groups, st);
+}
+
+// EXACT where every role's channels are whole 16-byte vectors: the general kernels' loads and stores by parts cost them
+// registers and instructions
+template <typename E> hipError_t scan_any(const DecayLaunch& L, int da, unsigned groups, bool states, hipStream_t st)
+{
+    bool exact = true;
+    for (int r = 0; r < L.roles; ++r) exact = exact && L.role[r].da % Ops<E>::VE == 0 && L.role[r].db % Ops<E>::VE == 0;
+    if (exact) return states ? scan_da<E, true, true>(L, da, groups, st) : scan_da<E, false, true>(L, da, groups, st);
+    return states ? scan_da<E, true, false>(L, da, groups, st) : scan_da<E, false, false>(L, da, groups, st);
 }
 
 // ------------------------------------------------------------------ decode step
@@ -484,9 +565,9 @@ template <typename E> hipError_t scan_da(const DecayLaunch& L, int da, unsigned 
 // groups of a workgroup each take every 16th row, and their parts of o are added through LDS.
 constexpr int SW = 64;      // value columns of a workgroup
 template <typename E>
-__global__ __launch_bounds__(NT) void decay_step_kernel(DecayStepLaunch L, int slices)
+__global__ __launch_bounds__(NJ) void decay_step_kernel(DecayStepLaunch L, int slices)
 {
-    __shared__ float part[NT / 16][SW];
+    __shared__ float part[NJ / 16][SW];
     const int tid = threadIdx.x, cg = tid & 15, rg = tid >> 4;
     const long long bh = blockIdx.x / slices;
     const int sl = static_cast<int>(blockIdx.x - bh * slices), n = sl * SW + 4 * cg;
@@ -501,7 +582,7 @@ __global__ __launch_bounds__(NT) void decay_step_kernel(DecayStepLaunch L, int s
 #pragma unroll
     for (int e = 0; e < 4; ++e) vv[e] = e < m ? Elem<E>::load(v, n + e) : 0.f;
     if (m > 0)
-        for (int d = rg; d < L.dk; d += NT / 16) {
+        for (int d = rg; d < L.dk; d += NJ / 16) {
             float* row = S + static_cast<long long>(d) * L.dv + n;
             const float kd = Elem<E>::load(k, d), qd = Elem<E>::load(q, d);
             f32x4 s = zero4();
@@ -526,7 +607,7 @@ __global__ __launch_bounds__(NT) void decay_step_kernel(DecayStepLaunch L, int s
     __syncthreads();
     if (tid < SW && sl * SW + tid < L.dv) {
         float x = 0.f;
-        for (int i = 0; i < NT / 16; ++i) x += part[i][tid];
+        for (int i = 0; i < NJ / 16; ++i) x += part[i][tid];
         Ops<E>::store1(static_cast<E*>(L.o) + b * L.o_s[0] + h * L.o_s[1] + sl * SW + tid, L.scale * x);
     }
 }
@@ -544,8 +625,8 @@ hipError_t launch_decay(const DecayLaunch& L, hipStream_t st)
                 const long long size = static_cast<long long>(L.role[r].da) * L.role[r].db;
                 most = size > most ? size : most;
             }
-            hipLaunchKernelGGL(decay_join_kernel, dim3(static_cast<unsigned>((most * heads + NT - 1) / NT), 1, L.roles),
-                               dim3(NT), 0, st, L);
+            hipLaunchKernelGGL(decay_join_kernel, dim3(static_cast<unsigned>((most * heads + NJ - 1) / NJ), 1, L.roles),
+                               dim3(NJ), 0, st, L);
             const hipError_t e = hipGetLastError();
             if (e != hipSuccess) return e;
             continue;
@@ -561,7 +642,7 @@ hipError_t launch_decay(const DecayLaunch& L, hipStream_t st)
                 }
             if (P.roles == 0) continue;
             const unsigned groups = static_cast<unsigned>(heads * slices);
-            const hipError_t e = L.bf16 ? scan_da<uint16_t>(P, lim, groups, pass == 0, st) : scan_da<float>(P, lim, groups, pass == 0, st);
+            const hipError_t e = L.bf16 ? scan_any<uint16_t>(P, lim, groups, pass == 0, st) : scan_any<float>(P, lim, groups, pass == 0, st);
             if (e != hipSuccess) return e;
         }
     }
@@ -573,9 +654,9 @@ hipError_t launch_decay_step(const DecayStepLaunch& L, hipStream_t st)
     const int slices = (L.dv + SW - 1) / SW;
     const unsigned groups = static_cast<unsigned>(static_cast<long long>(L.B) * L.H * slices);
     if (L.bf16)
-        hipLaunchKernelGGL(decay_step_kernel<uint16_t>, dim3(groups), dim3(NT), 0, st, L, slices);
+        hipLaunchKernelGGL(decay_step_kernel<uint16_t>, dim3(groups), dim3(NJ), 0, st, L, slices);
     else
-        hipLaunchKernelGGL(decay_step_kernel<float>, dim3(groups), dim3(NT), 0, st, L, slices);
+        hipLaunchKernelGGL(decay_step_kernel<float>, dim3(groups), dim3(NJ), 0, st, L, slices);
     return hipGetLastError();
 }
 
