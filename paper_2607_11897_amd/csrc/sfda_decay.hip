@@ -13,6 +13,8 @@
 #include <stddef.h>
 #include <string.h>
 
+#include <type_traits>
+
 namespace sfda {
 namespace {
 
@@ -24,6 +26,27 @@ constexpr int NT = 512;                  // threads of a scan workgroup, two wav
 constexpr int NW = NT / 64;
 constexpr int NS = DECAY_SLICE;          // its value columns
 constexpr int NJ = 256;                  // threads of the small kernels
+
+// 16 bytes at any address (global memory takes unaligned vectors)
+typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(1), may_alias));
+__device__ __forceinline__ u32x4 load16(const char* p) { return *reinterpret_cast<const u32x4_any*>(p); }
+
+// the first `cols` (fewer than fill them) elements of a row as 16 bytes, zeros behind them
+template <typename E> __device__ __forceinline__ u32x4 load_few(const char* p, int cols)
+{
+    constexpr int PER = 4 / sizeof(E);
+    u32x4 x = {0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < 4 * PER - 1; ++i)
+        if (i < cols) {
+            E e;
+            memcpy(&e, p + i * sizeof(E), sizeof(E));
+            uint32_t u = 0;
+            memcpy(&u, &e, sizeof(E));
+            x[i / PER] |= u << (i % PER * 16);
+        }
+    return x;
+}
 
 // two float32 as a pair of bfloat16, each to nearest even
 __device__ __forceinline__ uint32_t pack2(float a, float b)
@@ -38,8 +61,10 @@ __device__ __forceinline__ float lo_f32(uint32_t w) { return __uint_as_float(w <
 __device__ __forceinline__ float hi_f32(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 
 // What the element type decides.  C: tokens of a block; VE: elements of a 16-byte vector; KB: the
-// contraction length of one operand fragment; PAD: elements a row in LDS is longer than its channels (keeps
-// the 16 rows of a fragment on different banks).
+// contraction length of one operand fragment; KP, SP, VP: elements that rows of keys, of the state and of values in LDS are
+// longer than their channels, so that what a read takes at a time lies on different banks (bfloat16: 4 token rows of 32
+// bytes for the transposing read of keys, 8 rows of 16 bytes for the state, 4 rows of 64 bytes, every other
+// 8 of them, for values).
 // Lane l of a fragment has index c = l % 16 of the free axis and KB / 4 places of the contraction for its
 // group g = l / 16.  Sums over channels take VE neighbours (rows: one 16-byte read); sums over tokens take
 // the places 4 g .. 4 g + 3 of each 16, which is what an accumulator tile holds of its rows, so that scores become
@@ -47,7 +72,7 @@ __device__ __forceinline__ float hi_f32(uint32_t w) { return __uint_as_float(w &
 template <typename E> struct Ops;
 
 template <> struct Ops<uint16_t> {
-    static constexpr int C = 64, VE = 8, KB = 32, PAD = 8;
+    static constexpr int C = 64, VE = 8, KB = 32, KP = 16, SP = 8, VP = 32;
     typedef bf16x8 Frag;
     // row-major [free][contraction]
     static __device__ __forceinline__ Frag rows(const uint16_t* p) { return __builtin_bit_cast(Frag, *reinterpret_cast<const u32x4*>(p)); }
@@ -100,7 +125,7 @@ template <> struct Ops<uint16_t> {
 };
 
 template <> struct Ops<float> {
-    static constexpr int C = 32, VE = 4, KB = 16, PAD = 4;
+    static constexpr int C = 32, VE = 4, KB = 16, KP = 4, SP = 4, VP = 4;
     typedef f32x4 Frag;
     static __device__ __forceinline__ Frag rows(const float* p) { return *reinterpret_cast<const Frag*>(p); }
     static __device__ __forceinline__ Frag cols(const float* p, int stride) { return Frag{p[0], p[stride], p[2 * stride], p[3 * stride]}; }
@@ -142,39 +167,48 @@ __device__ __forceinline__ int seq_length(const int* lengths, int b, int T)
     return n < 0 ? 0 : n > T ? T : n;
 }
 
+// Where a block's rows are: a uniform address and 32-bit offsets of a lane's 16-byte vectors, which are the same
+// for every whole block.  The first block of a segment may be short: its tokens then take its last rows, and the `pad`
+// rows before them are clamped to its first token, so that loads are unconditional and in bounds.
+struct Rows {
+    const char* p;          // the sequence's first place in scan order
+    long long st;           // bytes from a place to the next (negative: reversed)
+    __device__ __forceinline__ const char* base(int at, int n) const { return p + (at + (st < 0 ? n - 1 : 0)) * st; }
+    __device__ __forceinline__ uint32_t offset(int row, int pad, int n) const
+    {
+        const int r = row > pad ? row - pad : 0;
+        return static_cast<uint32_t>(st < 0 ? (n - 1 - r) * -st : r * st);
+    }
+};
+
 // A block's rows of one tensor on their way to LDS: ROWS tokens x COLS channels (COLS padded), 16-byte
-// vectors held in registers between the load and the write.  Loads are unconditional and in bounds: rows
-// past the block's n are clamped to its last, and padding is clamped to channel 0 and never written.
+// vectors held in registers between the load and the write.  Padding channels are clamped to channel 0 and never written.
 // EXACT: the channels are whole vectors.  Otherwise the vector that would cross a row's end is moved back to end with it (the
 // write then goes by elements), and rows shorter than a vector are read by elements.
-template <typename E, int ROWS, int COLS, bool EXACT> struct Tile {
-    static constexpr int VE = Ops<E>::VE, VPR = COLS / VE, RPP = NT / VPR, N = ROWS / RPP, STRIDE = COLS + Ops<E>::PAD;
+template <typename E, int ROWS, int COLS, int STRIDE, bool EXACT> struct Tile {
+    static constexpr int VE = Ops<E>::VE, VPR = COLS / VE, RPP = NT / VPR, N = ROWS / RPP;
     static_assert(ROWS % RPP == 0 && NT % VPR == 0, "whole passes");
     u32x4 x[N];
+    uint32_t off[N];
 
-    // row i at p + i * st (st may be negative); `cols` channels; n >= 1
-    __device__ __forceinline__ void load(const E* p, long long st, int cols, int n, int tid)
+    __device__ __forceinline__ void place(const Rows& R, int cols, int pad, int tid)
     {
-        const int col = (tid % VPR) * VE;
+        const int col = (tid % VPR) * VE, at = col + VE <= cols ? col : EXACT || cols < VE ? 0 : cols - VE;
+#pragma unroll
+        for (int u = 0; u < N; ++u) off[u] = R.offset(tid / VPR + u * RPP, pad, ROWS - pad) + at * static_cast<uint32_t>(sizeof(E));
+    }
+    __device__ __forceinline__ void load(const char* base, int cols, int tid)
+    {
         if (EXACT || cols >= VE) {
-            const int at = col + VE <= cols ? col : EXACT ? 0 : cols - VE;
 #pragma unroll
-            for (int u = 0; u < N; ++u) {
-                const int r = tid / VPR + u * RPP;
-                memcpy(&x[u], p + (r < n ? r : n - 1) * st + at, 16);
-            }
-        } else if (col == 0) {
+            for (int u = 0; u < N; ++u) x[u] = load16(base + off[u]);
+        } else if ((tid % VPR) == 0) {
 #pragma unroll
-            for (int u = 0; u < N; ++u) {
-                const int r = tid / VPR + u * RPP;
-                E e[VE] = {};
-                for (int i = 0; i < VE - 1; ++i)
-                    if (i < cols) e[i] = p[(r < n ? r : n - 1) * st + i];
-                memcpy(&x[u], e, 16);
-            }
+            for (int u = 0; u < N; ++u) x[u] = load_few<E>(base + off[u], cols);
         }
     }
-    __device__ __forceinline__ void store(E* lds, int cols, int n, int tid) const
+    // rows before `pad` are zero
+    template <bool WHOLE> __device__ __forceinline__ void store(E* lds, int cols, int pad, int tid) const
     {
         const int col = (tid % VPR) * VE;
         if (col >= cols) return;
@@ -182,42 +216,43 @@ template <typename E, int ROWS, int COLS, bool EXACT> struct Tile {
         for (int u = 0; u < N; ++u) {
             const int r = tid / VPR + u * RPP;
             const u32x4 z = {0, 0, 0, 0};
-            const u32x4 w = r < n ? x[u] : z;
+            const u32x4 w = WHOLE || r >= pad ? x[u] : z;
             if (EXACT || col + VE <= cols || cols < VE) {
                 *reinterpret_cast<u32x4*>(lds + r * STRIDE + col) = w;
             } else {
-                E e[VE];
-                memcpy(e, &w, 16);
 #pragma unroll
-                for (int i = 0; i < VE; ++i) lds[r * STRIDE + cols - VE + i] = e[i];
+                for (int i = 0; i < VE; ++i) {
+                    constexpr int PER = 4 / static_cast<int>(sizeof(E));
+                    const uint32_t e = w[i / PER] >> (i % PER * 16);
+                    memcpy(lds + r * STRIDE + cols - VE + i, &e, sizeof(E));
+                }
             }
         }
     }
 };
 
 // A fragment's 16 bytes of a row of `cols` channels, from channel `col` on, on their way from global memory:
-// loaded in bounds (as a tile's vectors) and put in place when it is used, zero past the row.
-template <typename E, bool EXACT> __device__ __forceinline__ u32x4 row_load(const E* row, int col, int cols)
+// loaded in bounds (as a tile's vectors) and put in place when it is used.  Past the row: zero, but with EXACT what the
+// clamped vector holds, the row's own first channels, whose partners in LDS are zero.
+template <typename E, bool EXACT> __device__ __forceinline__ uint32_t row_at(int col, int cols)
 {
     constexpr int VE = Ops<E>::VE;
-    u32x4 x = {0, 0, 0, 0};
-    if (EXACT || cols >= VE) {
-        memcpy(&x, row + (col + VE <= cols ? col : EXACT ? 0 : cols - VE), 16);
-    } else if (col == 0) {
-        E e[VE] = {};
-        for (int i = 0; i < VE - 1; ++i)
-            if (i < cols) e[i] = row[i];
-        memcpy(&x, e, 16);
-    }
-    return x;
+    return (col + VE <= cols ? col : EXACT || cols < VE ? 0 : cols - VE) * static_cast<uint32_t>(sizeof(E));
+}
+template <typename E, bool EXACT> __device__ __forceinline__ u32x4 row_load(const char* p, int col, int cols)
+{
+    constexpr int VE = Ops<E>::VE;
+    if (EXACT || cols >= VE) return load16(p);
+    return col == 0 ? load_few<E>(p, cols) : u32x4{0, 0, 0, 0};
 }
 template <typename E, bool EXACT> __device__ __forceinline__ u32x4 row_place(u32x4 x, int col, int cols)
 {
     constexpr int VE = Ops<E>::VE;
     typedef unsigned long long u64;
     const u32x4 zero = {0, 0, 0, 0};
+    if (EXACT) return x;
     if (col >= cols) return zero;
-    if (EXACT || cols < VE || col + VE <= cols) return x;
+    if (cols < VE || col + VE <= cols) return x;
     const int s = (col + VE - cols) * 8 * static_cast<int>(sizeof(E));      // 16 .. 112 bits
     u64 lo = (static_cast<u64>(x[1]) << 32) | x[0], hi = (static_cast<u64>(x[3]) << 32) | x[2];
     if (s >= 64) {
@@ -233,10 +268,10 @@ template <typename E, bool EXACT> __device__ __forceinline__ u32x4 row_place(u32
 // LDS of a scan: the keys and values of a block and of the next, the state as an operand ([column][channel], twice where
 // it fits, so that a block needs one barrier), and the powers of lambda
 template <typename E, int DAP> struct Smem {
-    static constexpr int C = Ops<E>::C, P = Ops<E>::PAD;
-    static constexpr int KV = C * (DAP + P) + C * (NS + P), ST = NS * (DAP + P);
+    typedef Ops<E> O;
+    static constexpr int C = O::C, SK = DAP + O::KP, SV = NS + O::VP, SS = DAP + O::SP, KV = C * (SK + SV), ST = NS * SS;
     static constexpr int SB = (2 * KV + 2 * ST) * sizeof(E) <= 158 * 1024 ? 2 : 1;
-    E k[2][C * (DAP + P)], v[2][C * (NS + P)], s[SB][ST];
+    E k[2][C * SK], v[2][C * SV], s[SB][ST];
     float pw[C + 1];
 };
 
@@ -244,8 +279,9 @@ template <typename E, int DAP> struct Smem {
 // are CT row tiles (16 tokens each) x CG groups of 16 NP columns.  For a block, a wave forms the outputs of its row tile and its
 // columns: scores against the keys of earlier tiles and its own, kept in registers as the operand of the
 // product with the values, and the queries (which no other row tile needs: from global memory straight into
-// fragments) times the state.  Then it updates its share of the state, DTW of the channel tiles for its columns,
-// and puts it into LDS as the next block's operand.  STATES: only the segment's state from zero, to the workspace.
+// fragments) times the state.  Then it updates its share of the state, half of the channel tiles for 16 of its columns (so
+// that the weighted values, whose parts cost the vector unit more than anything else, are formed by two
+// waves and not by four), and puts it into LDS as the next block's operand.  STATES: only the segment's state from zero, to the workspace.
 template <typename E, int DAP, bool STATES, bool EXACT>
 __global__ __launch_bounds__(NT) void decay_scan_kernel(DecayLaunch L)
 {
@@ -253,15 +289,15 @@ __global__ __launch_bounds__(NT) void decay_scan_kernel(DecayLaunch L)
     typedef typename O::Frag Frag;
     typedef Smem<E, DAP> Mem;
     constexpr int C = O::C, KB = O::KB, VE = O::VE, CT = C / 16, CG = NW / CT, NP = NS / CG / 16;
-    constexpr int DT = DAP / 16, DTW = DT / CT, DF = DAP / KB, CF = C / KB, TPF = KB / 16;
-    constexpr int SK = DAP + O::PAD, SV = NS + O::PAD, SB = Mem::SB;
-    static_assert(DT % CT == 0 && NP * CG * 16 == NS, "tiles");
+    constexpr int DT = DAP / 16, DTW = DT / 2, DF = DAP / KB, CF = C / KB, TPF = KB / 16, ES = sizeof(E);
+    constexpr int SK = Mem::SK, SV = Mem::SV, SS = Mem::SS, SB = Mem::SB;
+    static_assert(DT % 2 == 0 && NP * CG * 16 == NS && CT == 2 * NP, "tiles");
     extern __shared__ __align__(16) unsigned char smem[];
     Mem& M = *reinterpret_cast<Mem*>(smem);
 
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 15, g = lane >> 4;
     // (waves w and w + 4 share a SIMD: the row tiles of a pair add up to the same number of score tiles)
-    const int rt = CT == 4 ? (w < 4 ? w : 7 - w) : (w ^ (w >> 2)) & 1, cg = w / CT;
+    const int wave_rt = CT == 4 ? (w < 4 ? w : 7 - w) : (w ^ (w >> 2)) & 1, cg = w / CT;
     int total = 0;
     for (int r = 0; r < L.roles; ++r) total += L.role[r].slices;
     long bh;
@@ -275,20 +311,16 @@ __global__ __launch_bounds__(NT) void decay_scan_kernel(DecayLaunch L)
     const int begin = first < len ? static_cast<int>(first) : len;
     const int end = first + L.seg_tokens < len ? static_cast<int>(first) + L.seg_tokens : len;
     const int n0 = sl * NS, dbs = R.db - n0 < NS ? R.db - n0 : NS;
-    const int da = R.da;
+    const int da = R.da, reverse = R.reverse;
     const float gl = L.log_decay[h];
 
     // token of scan place i: i, or len - 1 - i
-    const int dir = R.reverse ? -1 : 1;
-    const long long tok0 = R.reverse ? len - 1 : 0;
-    const E* qp = static_cast<const E*>(R.q) + b * R.q_s[0] + h * R.q_s[1];
-    const E* kp = static_cast<const E*>(R.k) + b * R.k_s[0] + h * R.k_s[1];
-    const E* vp = static_cast<const E*>(R.v) + b * R.v_s[0] + h * R.v_s[1] + n0;
-    E* op = static_cast<E*>(R.o) + b * R.o_s[0] + h * R.o_s[1] + n0;
-    const long long qst = dir * R.q_s[2], kst = dir * R.k_s[2], vst = dir * R.v_s[2], ost = dir * R.o_s[2];
-    qp += tok0 * R.q_s[2];
-    kp += tok0 * R.k_s[2];
-    vp += tok0 * R.v_s[2];
+    const long long tok0 = reverse ? len - 1 : 0, dir = reverse ? -ES : ES;
+    const Rows qr = {static_cast<const char*>(R.q) + (b * R.q_s[0] + h * R.q_s[1] + tok0 * R.q_s[2]) * ES, dir * R.q_s[2]};
+    const Rows kr = {static_cast<const char*>(R.k) + (b * R.k_s[0] + h * R.k_s[1] + tok0 * R.k_s[2]) * ES, dir * R.k_s[2]};
+    const Rows vr = {static_cast<const char*>(R.v) + (b * R.v_s[0] + h * R.v_s[1] + tok0 * R.v_s[2] + n0) * ES, dir * R.v_s[2]};
+    E* const op = static_cast<E*>(R.o) + b * R.o_s[0] + h * R.o_s[1] + n0;
+    const Rows orow = {reinterpret_cast<const char*>(op) + tok0 * R.o_s[2] * ES, dir * R.o_s[2]};
 
     {   // padding stays zero
         u32x4* z = reinterpret_cast<u32x4*>(smem);
@@ -297,26 +329,38 @@ __global__ __launch_bounds__(NT) void decay_scan_kernel(DecayLaunch L)
         if (tid <= C) M.pw[tid] = tid == 0 ? 1.f : expf(static_cast<float>(tid) * gl);
     }
 
-    Tile<E, C, DAP, EXACT> tk;
-    Tile<E, C, NS, EXACT> tv;
+    Tile<E, C, DAP, SK, EXACT> tk;
+    Tile<E, C, NS, SV, EXACT> tv;
     u32x4 qn[DF];
-    auto load = [&](int at) {
-        const int n = end - at < C ? end - at : C;
-        tk.load(kp + at * kst, kst, da, n, tid);
-        tv.load(vp + at * vst, vst, dbs, n, tid);
+    uint32_t qoff[DF];
+    // blocks end where the segment ends; the first one has `pad` rows too many
+    const int pad = begin < end ? (C - (end - begin) % C) % C : 0;
+    auto place = [&](int pad) {
+        tk.place(kr, da, pad, tid);
+        tv.place(vr, dbs, pad, tid);
         if (!STATES) {
-            const int i = 16 * rt + c;
-            const E* row = qp + (at + (i < n ? i : n - 1)) * qst;
+            const uint32_t row = qr.offset(16 * wave_rt + c, pad, C - pad);
 #pragma unroll
-            for (int f = 0; f < DF; ++f) qn[f] = row_load<E, EXACT>(row, KB * f + VE * g, da);
+            for (int f = 0; f < DF; ++f) qoff[f] = row + row_at<E, EXACT>(KB * f + VE * g, da);
         }
     };
-    if (begin < end) load(begin);
+    auto load = [&](int at, int n) {
+        tk.load(kr.base(at, n), da, tid);
+        tv.load(vr.base(at, n), dbs, tid);
+        if (!STATES) {
+            const char* p = qr.base(at, n);
+#pragma unroll
+            for (int f = 0; f < DF; ++f) qn[f] = row_load<E, EXACT>(p + qoff[f], KB * f + VE * g, da);
+        }
+    };
+    place(pad);
+    if (begin < end) load(begin, C - pad);
 
     // the wave's columns: tile p has column (c, p); a lane's 4 NP columns of its outputs are neighbours
     const int col0 = 16 * NP * cg + 4 * NP * (c >> 2) + (c & 3);      // + 4 p
-    // its state: lane (c, g) has rows 16 (rt DTW + d) + 4 g + r of that column
-    f32x4 S[DTW][NP];
+    // its share of the state: column (c, sp), lane (c, g) has rows srow + 16 d + r
+    const int scol = col0 + 4 * (wave_rt % NP), srow = 16 * DTW * (wave_rt / NP) + 4 * g;
+    f32x4 S[DTW];
     {
         const float* src = nullptr;
         long long rs = 0, cs = 0;
@@ -334,153 +378,154 @@ __global__ __launch_bounds__(NT) void decay_scan_kernel(DecayLaunch L)
 #pragma unroll
         for (int d = 0; d < DTW; ++d)
 #pragma unroll
-            for (int p = 0; p < NP; ++p)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int row = 16 * (rt * DTW + d) + 4 * g + r, col = col0 + 4 * p;
-                    S[d][p][r] = src != nullptr && col < dbs && row < da ? src[row * rs + (n0 + col) * cs] : 0.f;
-                }
+            for (int r = 0; r < 4; ++r) {
+                const int row = srow + 16 * d + r;
+                S[d][r] = src != nullptr && scol < dbs && row < da ? src[row * rs + (n0 + scol) * cs] : 0.f;
+            }
     }
     __syncthreads();
 
     // weights that are the same for every whole block: of the scores, of the start state's rows, of the values
-    float wd[CT][4], wi = 0.f, wv[CF][KB / 4];
+    float wd[CT][4], wv[CF][KB / 4];
 #pragma unroll
     for (int t = 0; t < CT; ++t)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const int far = 16 * (rt - t) + c - (4 * g + r);
+            const int far = 16 * (wave_rt - t) + c - (4 * g + r);
             wd[t][r] = far >= 0 ? R.intra * M.pw[far] : 0.f;
         }
-    wi = R.inter * M.pw[16 * rt + c + (R.reverse ? 0 : 1)];
-    auto value_weights = [&](int m) {
+    const float upd = R.upd;
 #pragma unroll
-        for (int f = 0; f < CF; ++f)
+    for (int f = 0; f < CF; ++f)
 #pragma unroll
-            for (int e = 0; e < KB / 4; ++e) {
-                const int j = KB * f + 16 * (e / 4) + 4 * g + (e & 3), far = m - 1 - j + (R.reverse ? 1 : 0);
-                wv[f][e] = R.upd * M.pw[far < 0 ? 0 : far];
-            }
-    };
-    value_weights(C);
-    Pow lam = decay_pow(C, gl);
+        for (int e = 0; e < KB / 4; ++e)
+            wv[f][e] = upd * M.pw[C - 1 - (KB * f + 16 * (e / 4) + 4 * g + (e & 3)) + (reverse ? 1 : 0)];
+    // the first block's decays of the state that enters it are those of its tokens
+    const int after = 16 * wave_rt + c + (reverse ? 0 : 1);
+    const float wi_whole = R.inter * M.pw[after];
+    float wi = R.inter * M.pw[after > pad ? after - pad : 0];
+    const Pow lam_whole = decay_pow(C, gl);
+    Pow lam = pad > 0 ? decay_pow(C - pad, gl) : lam_whole;
+    int low = pad;                  // first row with a token
+    const uint32_t ooff = orow.offset(16 * wave_rt + c, 0, C);
 
     // the state, rounded to the element type, as the operand of its product with the queries
     auto state_out = [&](E* to) {
 #pragma unroll
-        for (int d = 0; d < DTW; ++d)
-#pragma unroll
-            for (int p = 0; p < NP; ++p) {
-                const auto x = O::pack4(S[d][p]);
-                memcpy(to + (col0 + 4 * p) * SK + 16 * (rt * DTW + d) + 4 * g, &x, sizeof(x));
-            }
+        for (int d = 0; d < DTW; ++d) {
+            const auto x = O::pack4(S[d]);
+            *reinterpret_cast<std::remove_const_t<decltype(x)>*>(to + scol * SS + srow + 16 * d) = x;
+        }
     };
     if (begin < end) {
-        const int n = end - begin < C ? end - begin : C;
-        tk.store(M.k[0], da, n, tid);
-        tv.store(M.v[0], dbs, n, tid);
+        tk.template store<false>(M.k[0], da, pad, tid);
+        tv.template store<false>(M.v[0], dbs, pad, tid);
         if (!STATES) state_out(M.s[0]);
+        place(0);
     }
     __syncthreads();
 
-    int buf = 0;
-    for (int at = begin; at < end; at += C, buf ^= 1) {
-        const int n = end - at < C ? end - at : C, next = at + C;
-        const E *K = M.k[buf], *V = M.v[buf], *SL = M.s[SB == 2 ? buf : 0];
-        Frag qf[DF];
-        if (!STATES) {
+    // The blocks, for the waves of row tile rt: one barrier a block (two with one state buffer), the same for all of them.
+    auto blocks = [&](auto rtc) __attribute__((always_inline)) {
+        constexpr int rt = decltype(rtc)::value, sp = rt % NP;
+        int buf = 0;
+        for (int at = begin - pad; at < end; at += C, buf ^= 1) {
+            const int next = at + C;
+            const E *K = M.k[buf], *V = M.v[buf], *SL = M.s[SB == 2 ? buf : 0];
+            Frag qf[DF];
+            if (!STATES) {
 #pragma unroll
-            for (int f = 0; f < DF; ++f) qf[f] = __builtin_bit_cast(Frag, row_place<E, EXACT>(qn[f], KB * f + VE * g, da));
-        }
-        if (next < end) load(next);
-        if (n < C) {
-            value_weights(n);
-            lam = decay_pow(n, gl);
-        }
-        Frag vf[CF][NP];
-#pragma unroll
-        for (int f = 0; f < CF; ++f)
-#pragma unroll
-            for (int p = 0; p < NP; ++p)
-                vf[f][p] = O::cols(V + KB * f * SV + 16 * NP * cg + 4 * p + O::cols_at(SV, 4 * NP, c, g), SV);
-        if (!STATES) {
-            // outputs, transposed: rows are columns of v, columns are tokens
-            f32x4 x[NP];
-#pragma unroll
-            for (int p = 0; p < NP; ++p) x[p] = zero4();
-#pragma unroll
-            for (int f = 0; f < DF; ++f)
-#pragma unroll
-                for (int p = 0; p < NP; ++p) O::mma(x[p], O::rows(SL + (col0 + 4 * p) * SK + KB * f + VE * g), qf[f]);
-#pragma unroll
-            for (int p = 0; p < NP; ++p)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) x[p][r] *= wi;
-            // scores, transposed: rows are keys; rounded once to the element type, as the operand of the product with v
-#pragma unroll
-            for (int f = 0; f < CF; ++f) {
-                if (TPF * f > rt) continue;
-                f32x4 sc[TPF];
-#pragma unroll
-                for (int u = 0; u < TPF; ++u) {
-                    const int t = TPF * f + u;
-                    sc[u] = zero4();
-                    if (t <= rt) {
-#pragma unroll
-                        for (int e = 0; e < DF; ++e) O::mma(sc[u], O::rows(K + (16 * t + c) * SK + KB * e + VE * g), qf[e]);
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) sc[u][r] = t < rt || c >= 4 * g + r ? sc[u][r] * wd[t][r] : 0.f;
-                    }
-                }
-                const Frag a = O::acc(sc);
-#pragma unroll
-                for (int p = 0; p < NP; ++p) O::mma(x[p], vf[f][p], a);
+                for (int f = 0; f < DF; ++f) qf[f] = __builtin_bit_cast(Frag, row_place<E, EXACT>(qn[f], KB * f + VE * g, da));
             }
-            const int i = 16 * rt + c, at_n = 16 * NP * cg + 4 * NP * g;
-            if (i < n) {
-                E* to = op + (tok0 * R.o_s[2] + (at + i) * ost) + at_n;
-                if (at_n + 4 * NP <= dbs) {
-                    decltype(O::pack4(x[0])) y[NP];
+            if (next < end) load(next, C);
+            Frag vf[CF][NP];
 #pragma unroll
-                    for (int p = 0; p < NP; ++p) y[p] = O::pack4(x[p]);
-                    memcpy(to, y, sizeof(y));
-                } else if (!EXACT) {
+            for (int f = 0; f < CF; ++f)
 #pragma unroll
-                    for (int p = 0; p < NP; ++p)
+                for (int p = 0; p < NP; ++p)
+                    if ((!STATES && TPF * f <= rt) || p == sp)
+                        vf[f][p] = O::cols(V + KB * f * SV + 16 * NP * cg + 4 * p + O::cols_at(SV, 4 * NP, c, g), SV);
+            if (!STATES) {
+                // outputs, transposed: rows are columns of v, columns are tokens
+                f32x4 x[NP];
 #pragma unroll
-                        for (int r = 0; r < 4; ++r)
-                            if (at_n + 4 * p + r < dbs) O::store1(to + 4 * p + r, x[p][r]);
-                }
-            }
-        }
-        if (SB == 1 && !STATES) __syncthreads();
+                for (int p = 0; p < NP; ++p) x[p] = zero4();
 #pragma unroll
-        for (int d = 0; d < DTW; ++d)
+                for (int f = 0; f < DF; ++f)
 #pragma unroll
-            for (int p = 0; p < NP; ++p)
+                    for (int p = 0; p < NP; ++p) O::mma(x[p], O::rows(SL + (col0 + 4 * p) * SS + KB * f + VE * g), qf[f]);
+                // scores, transposed: rows are keys; rounded once to the element type, as the operand of the product with v
+                f32x4 sc[TPF * ((rt + TPF) / TPF)];
 #pragma unroll
-                for (int r = 0; r < 4; ++r) S[d][p][r] = __builtin_fmaf(S[d][p][r], lam.hi, S[d][p][r] * lam.lo);
+                for (int t = 0; t < TPF * ((rt + TPF) / TPF); ++t) sc[t] = zero4();
 #pragma unroll
-        for (int f = 0; f < CF; ++f) {
-            Frag vw[NP][O::PARTS];
+                for (int e = 0; e < DF; ++e)
 #pragma unroll
-            for (int p = 0; p < NP; ++p) O::weighted(vw[p], vf[f][p], wv[f]);
+                    for (int t = 0; t <= rt; ++t) O::mma(sc[t], O::rows(K + (16 * t + c) * SK + KB * e + VE * g), qf[e]);
 #pragma unroll
-            for (int d = 0; d < DTW; ++d) {
-                const Frag kf = O::cols(K + KB * f * SK + 16 * (rt * DTW + d) + O::cols_at(SK, 4, c, g), SK);
+                for (int t = 0; t <= rt; ++t)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) sc[t][r] = t < rt || c >= 4 * g + r ? sc[t][r] * wd[t][r] : 0.f;
 #pragma unroll
                 for (int p = 0; p < NP; ++p)
 #pragma unroll
-                    for (int s = O::PARTS - 1; s >= 0; --s) O::mma(S[d][p], kf, vw[p][s]);
+                    for (int r = 0; r < 4; ++r) x[p][r] *= wi;
+#pragma unroll
+                for (int f = 0; TPF * f <= rt; ++f) {
+                    const Frag a = O::acc(&sc[TPF * f]);
+#pragma unroll
+                    for (int p = 0; p < NP; ++p) O::mma(x[p], vf[f][p], a);
+                }
+                const int at_n = 16 * NP * cg + 4 * NP * g;
+                if (16 * rt + c >= low) {
+                    E* to = reinterpret_cast<E*>(const_cast<char*>(orow.base(at, C)) + ooff) + at_n;
+                    if (at_n + 4 * NP <= dbs) {
+                        decltype(O::pack4(x[0])) y[NP];
+#pragma unroll
+                        for (int p = 0; p < NP; ++p) y[p] = O::pack4(x[p]);
+                        memcpy(to, y, sizeof(y));
+                    } else if (!EXACT) {
+#pragma unroll
+                        for (int p = 0; p < NP; ++p)
+#pragma unroll
+                            for (int r = 0; r < 4; ++r)
+                                if (at_n + 4 * p + r < dbs) O::store1(to + 4 * p + r, x[p][r]);
+                    }
+                }
+                if (SB == 1) __syncthreads();
+                wi = wi_whole;
+                low = 0;
             }
+#pragma unroll
+            for (int d = 0; d < DTW; ++d)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) S[d][r] = __builtin_fmaf(S[d][r], lam.hi, S[d][r] * lam.lo);
+#pragma unroll
+            for (int f = 0; f < CF; ++f) {
+                Frag vw[O::PARTS];
+                O::weighted(vw, vf[f][sp], wv[f]);
+#pragma unroll
+                for (int d = 0; d < DTW; ++d) {
+                    const Frag kf = O::cols(K + KB * f * SK + srow - 4 * g + 16 * d + O::cols_at(SK, 4, c, g), SK);
+#pragma unroll
+                    for (int s = O::PARTS - 1; s >= 0; --s) O::mma(S[d], kf, vw[s]);
+                }
+            }
+            lam = lam_whole;
+            if (next < end) {
+                if (!STATES) state_out(M.s[SB == 2 ? buf ^ 1 : 0]);
+                tk.template store<true>(M.k[buf ^ 1], da, 0, tid);
+                tv.template store<true>(M.v[buf ^ 1], dbs, 0, tid);
+            }
+            __syncthreads();
         }
-        if (next < end) {
-            const int m = end - next < C ? end - next : C;
-            if (!STATES) state_out(M.s[SB == 2 ? buf ^ 1 : 0]);
-            tk.store(M.k[buf ^ 1], da, m, tid);
-            tv.store(M.v[buf ^ 1], dbs, m, tid);
-        }
-        __syncthreads();
+    };
+    if (STATES && NP == 1) blocks(std::integral_constant<int, 0>{});     // (only the columns' tile matters)
+    else if (wave_rt == 0 || (STATES && wave_rt == 2)) blocks(std::integral_constant<int, 0>{});
+    else if (wave_rt == 1 || STATES) blocks(std::integral_constant<int, 1>{});
+    else if constexpr (CT == 4) {
+        if (wave_rt == 2) blocks(std::integral_constant<int, 2>{});
+        else blocks(std::integral_constant<int, 3>{});
     }
 
     float* dst = nullptr;
@@ -498,12 +543,10 @@ __global__ __launch_bounds__(NT) void decay_scan_kernel(DecayLaunch L)
 #pragma unroll
         for (int d = 0; d < DTW; ++d)
 #pragma unroll
-            for (int p = 0; p < NP; ++p)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int row = 16 * (rt * DTW + d) + 4 * g + r, col = col0 + 4 * p;
-                    if (row < da && col < dbs) dst[row * rs + (n0 + col) * cs] = S[d][p][r];
-                }
+            for (int r = 0; r < 4; ++r) {
+                const int row = srow + 16 * d + r;
+                if (row < da && scol < dbs) dst[row * rs + (n0 + scol) * cs] = S[d][r];
+            }
     }
     if (!STATES && len < L.T) {     // tokens past the sequence's length
         const long long hi = first + L.seg_tokens < L.T ? first + L.seg_tokens : L.T;
