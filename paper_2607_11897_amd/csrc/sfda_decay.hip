@@ -30,6 +30,7 @@ constexpr int NJ = 256;                  // threads of the small kernels
 // 16 bytes at any address (global memory takes unaligned vectors)
 typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(1), may_alias));
 __device__ __forceinline__ u32x4 load16(const char* p) { return *reinterpret_cast<const u32x4_any*>(p); }
+__device__ __forceinline__ void store16(char* p, u32x4 x) { *reinterpret_cast<u32x4_any*>(p) = x; }
 
 // the first `cols` (fewer than fill them) elements of a row as 16 bytes, zeros behind them
 template <typename E> __device__ __forceinline__ u32x4 load_few(const char* p, int cols)
@@ -102,6 +103,10 @@ template <> struct Ops<uint16_t> {
         d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, d, 0, 0, 0);
     }
     static __device__ __forceinline__ u32x2 pack4(const f32x4& x) { return u32x2{pack2(x[0], x[1]), pack2(x[2], x[3])}; }
+    static __device__ __forceinline__ u32x4 pack16(const f32x4* x)
+    {
+        return u32x4{pack2(x[0][0], x[0][1]), pack2(x[0][2], x[0][3]), pack2(x[1][0], x[1][1]), pack2(x[1][2], x[1][3])};
+    }
     static __device__ __forceinline__ void store1(uint16_t* p, float x) { *p = f32_to_bf16_bits(x); }
     // the weighted values as a sum of bfloat16 parts: the state has to keep 32 bits' worth of them, and one
     // rounding of the product to bfloat16 would leave 8 bits
@@ -115,8 +120,10 @@ template <> struct Ops<uint16_t> {
             float a = lo_f32(x[e]) * w[2 * e], b = hi_f32(x[e]) * w[2 * e + 1];
 #pragma unroll
             for (int s = 0; s < PARTS; ++s) {
-                o[s][e] = pack2(a, b);
-                if (s + 1 < PARTS) { a -= lo_f32(o[s][e]); b -= hi_f32(o[s][e]); }
+                uint32_t p = pack2(a, b);
+                asm("" : "+v"(p));      // (or the halves are converted once more, one by one)
+                o[s][e] = p;
+                if (s + 1 < PARTS) { a -= lo_f32(p); b -= hi_f32(p); }
             }
         }
 #pragma unroll
@@ -137,6 +144,7 @@ template <> struct Ops<float> {
         for (int s = 0; s < 4; ++s) d = __builtin_amdgcn_mfma_f32_16x16x4f32(a[s], b[s], d, 0, 0, 0);
     }
     static __device__ __forceinline__ f32x4 pack4(const f32x4& x) { return x; }
+    static __device__ __forceinline__ u32x4 pack16(const f32x4* x) { return __builtin_bit_cast(u32x4, x[0]); }
     static __device__ __forceinline__ void store1(float* p, float x) { *p = x; }
     static constexpr int PARTS = 1;
     static __device__ __forceinline__ void weighted(Frag (&out)[PARTS], const Frag& v, const float (&w)[4])
@@ -480,10 +488,7 @@ __global__ __launch_bounds__(NT) void decay_scan_kernel(DecayLaunch L)
                 if (16 * rt + c >= low) {
                     E* to = reinterpret_cast<E*>(const_cast<char*>(orow.base(at, C)) + ooff) + at_n;
                     if (at_n + 4 * NP <= dbs) {
-                        decltype(O::pack4(x[0])) y[NP];
-#pragma unroll
-                        for (int p = 0; p < NP; ++p) y[p] = O::pack4(x[p]);
-                        memcpy(to, y, sizeof(y));
+                        store16(reinterpret_cast<char*>(to), O::pack16(x));
                     } else if (!EXACT) {
 #pragma unroll
                         for (int p = 0; p < NP; ++p)
@@ -502,14 +507,15 @@ __global__ __launch_bounds__(NT) void decay_scan_kernel(DecayLaunch L)
                 for (int r = 0; r < 4; ++r) S[d][r] = __builtin_fmaf(S[d][r], lam.hi, S[d][r] * lam.lo);
 #pragma unroll
             for (int f = 0; f < CF; ++f) {
-                Frag vw[O::PARTS];
+                Frag vw[O::PARTS], kf[DTW];
+#pragma unroll
+                for (int d = 0; d < DTW; ++d)
+                    kf[d] = O::cols(K + KB * f * SK + srow - 4 * g + 16 * d + O::cols_at(SK, 4, c, g), SK);
                 O::weighted(vw, vf[f][sp], wv[f]);
 #pragma unroll
-                for (int d = 0; d < DTW; ++d) {
-                    const Frag kf = O::cols(K + KB * f * SK + srow - 4 * g + 16 * d + O::cols_at(SK, 4, c, g), SK);
+                for (int s = O::PARTS - 1; s >= 0; --s)
 #pragma unroll
-                    for (int s = O::PARTS - 1; s >= 0; --s) O::mma(S[d], kf, vw[s]);
-                }
+                    for (int d = 0; d < DTW; ++d) O::mma(S[d], kf[d], vw[s]);
             }
             lam = lam_whole;
             if (next < end) {
