@@ -22,9 +22,11 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int NT = 512;                  // threads of a scan workgroup, two waves on a SIMD
-constexpr int NW = NT / 64;
-constexpr int NS = DECAY_SLICE;          // its value columns
+constexpr int NS = DECAY_SLICE;          // value columns of a scan workgroup
+// Waves of a scan workgroup.  Four (one on a SIMD) form no scores and no weighted values twice, eight hide more
+// latency and have half the registers' worth of work each.  Forward B8 H16 T4096 bfloat16 d 128: 161 us with four, 182 with
+// eight; float32 B4 H8 T2048: 143 and 136; with 256 channels four do not have the registers.
+template <typename E> constexpr int waves(int dap) { return sizeof(E) == 2 && dap <= 128 ? 4 : 8; }
 constexpr int NJ = 256;                  // threads of the small kernels
 
 // 16 bytes at any address (global memory takes unaligned vectors)
@@ -103,9 +105,9 @@ template <> struct Ops<uint16_t> {
         d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, d, 0, 0, 0);
     }
     static __device__ __forceinline__ u32x2 pack4(const f32x4& x) { return u32x2{pack2(x[0], x[1]), pack2(x[2], x[3])}; }
-    static __device__ __forceinline__ u32x4 pack16(const f32x4* x)
+    static __device__ __forceinline__ u32x4 pack8(const f32x4& x, const f32x4& y)
     {
-        return u32x4{pack2(x[0][0], x[0][1]), pack2(x[0][2], x[0][3]), pack2(x[1][0], x[1][1]), pack2(x[1][2], x[1][3])};
+        return u32x4{pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(y[0], y[1]), pack2(y[2], y[3])};
     }
     static __device__ __forceinline__ void store1(uint16_t* p, float x) { *p = f32_to_bf16_bits(x); }
     // the weighted values as a sum of bfloat16 parts: the state has to keep 32 bits' worth of them, and one
@@ -144,7 +146,6 @@ template <> struct Ops<float> {
         for (int s = 0; s < 4; ++s) d = __builtin_amdgcn_mfma_f32_16x16x4f32(a[s], b[s], d, 0, 0, 0);
     }
     static __device__ __forceinline__ f32x4 pack4(const f32x4& x) { return x; }
-    static __device__ __forceinline__ u32x4 pack16(const f32x4* x) { return __builtin_bit_cast(u32x4, x[0]); }
     static __device__ __forceinline__ void store1(float* p, float x) { *p = x; }
     static constexpr int PARTS = 1;
     static __device__ __forceinline__ void weighted(Frag (&out)[PARTS], const Frag& v, const float (&w)[4])
@@ -175,9 +176,9 @@ __device__ __forceinline__ int seq_length(const int* lengths, int b, int T)
     return n < 0 ? 0 : n > T ? T : n;
 }
 
-// Where a block's rows are: a uniform address and 32-bit offsets of a lane's 16-byte vectors, which are the same
-// for every whole block.  The first block of a segment may be short: its tokens then take its last rows, and the `pad`
-// rows before them are clamped to its first token, so that loads are unconditional and in bounds.
+// Where a block's rows are: an address that is the same for all lanes and 32-bit offsets of their 16-byte vectors, which
+// are the same for every whole block.  The first block of a segment may be short: its tokens then take its last rows,
+// and the `pad` rows before them are clamped to its first token, so that loads are unconditional and in bounds.
 struct Rows {
     const char* p;          // the sequence's first place in scan order
     long long st;           // bytes from a place to the next (negative: reversed)
@@ -189,31 +190,65 @@ struct Rows {
     }
 };
 
+__device__ __forceinline__ uint64_t same_for_all(uint64_t x)
+{
+    const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(x)), hi = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(x >> 32));
+    return static_cast<uint64_t>(hi) << 32 | lo;
+}
+// 16 bytes at base + off + more, more the same for all lanes.  ALIGNED: to 4 bytes, and less than 2^31 bytes from the base.
+template <bool ALIGNED> struct From {
+    const char* p;
+    __device__ __forceinline__ explicit From(const char* base) : p(base) {}
+    __device__ __forceinline__ u32x4 load(uint32_t off, uint32_t more) const { return load16(p + off + more); }
+    __device__ __forceinline__ void store(uint32_t off, uint32_t more, u32x4 x) const { store16(const_cast<char*>(p) + off + more, x); }
+};
+template <> struct From<true> {
+    __amdgpu_buffer_rsrc_t r;
+    __device__ __forceinline__ explicit From(const char* base)
+        : r(__builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(same_for_all(reinterpret_cast<uint64_t>(base))), 0, 0x7fffffff, 0x00020000)) {}
+    __device__ __forceinline__ u32x4 load(uint32_t off, uint32_t more) const { return __builtin_amdgcn_raw_buffer_load_b128(r, off, more, 0); }
+    __device__ __forceinline__ void store(uint32_t off, uint32_t more, u32x4 x) const { __builtin_amdgcn_raw_buffer_store_b128(x, r, off, more, 0); }
+};
+
 // A block's rows of one tensor on their way to LDS: ROWS tokens x COLS channels (COLS padded), 16-byte
 // vectors held in registers between the load and the write.  Padding channels are clamped to channel 0 and never written.
 // EXACT: the channels are whole vectors.  Otherwise the vector that would cross a row's end is moved back to end with it (the
 // write then goes by elements), and rows shorter than a vector are read by elements.
-template <typename E, int ROWS, int COLS, int STRIDE, bool EXACT> struct Tile {
+template <typename E, int NT, int ROWS, int COLS, int STRIDE, bool EXACT> struct Tile {
     static constexpr int VE = Ops<E>::VE, VPR = COLS / VE, RPP = NT / VPR, N = ROWS / RPP;
     static_assert(ROWS % RPP == 0 && NT % VPR == 0, "whole passes");
     u32x4 x[N];
-    uint32_t off[N];
+    uint32_t off, step;     // a whole block's first vector in memory order, and from a pass to the next
 
-    __device__ __forceinline__ void place(const Rows& R, int cols, int pad, int tid)
+    __device__ __forceinline__ static uint32_t at(int cols, int tid)
     {
-        const int col = (tid % VPR) * VE, at = col + VE <= cols ? col : EXACT || cols < VE ? 0 : cols - VE;
-#pragma unroll
-        for (int u = 0; u < N; ++u) off[u] = R.offset(tid / VPR + u * RPP, pad, ROWS - pad) + at * static_cast<uint32_t>(sizeof(E));
+        const int col = (tid % VPR) * VE;
+        return (col + VE <= cols ? col : EXACT || cols < VE ? 0 : cols - VE) * static_cast<uint32_t>(sizeof(E));
     }
-    __device__ __forceinline__ void load(const char* base, int cols, int tid)
+    __device__ __forceinline__ void place(const Rows& R, int cols, int tid)
     {
-        if (EXACT || cols >= VE) {
-#pragma unroll
-            for (int u = 0; u < N; ++u) x[u] = load16(base + off[u]);
-        } else if ((tid % VPR) == 0) {
-#pragma unroll
-            for (int u = 0; u < N; ++u) x[u] = load_few<E>(base + off[u], cols);
+        off = R.offset(tid / VPR + (R.st < 0 ? (N - 1) * RPP : 0), 0, ROWS) + at(cols, tid);
+        step = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(RPP * (R.st < 0 ? -R.st : R.st)));
+    }
+    __device__ __forceinline__ u32x4 one(const From<EXACT>& from, uint32_t o, uint32_t more, int cols, int tid) const
+    {
+        if constexpr (!EXACT) {
+            if (cols < VE) return tid % VPR == 0 ? load_few<E>(from.p + o + more, cols) : u32x4{0, 0, 0, 0};
         }
+        return from.load(o, more);
+    }
+    __device__ __forceinline__ void load(const char* base, bool back, int cols, int tid)
+    {
+        const From<EXACT> from(base);
+#pragma unroll
+        for (int u = 0; u < N; ++u) x[u] = one(from, off, __builtin_amdgcn_readfirstlane((back ? N - 1 - u : u) * step), cols, tid);
+    }
+    // a segment's first block, from its first token on
+    __device__ __forceinline__ void load_first(const Rows& R, int begin, int pad, int cols, int tid)
+    {
+        const From<EXACT> from(R.base(begin, ROWS - pad));
+#pragma unroll
+        for (int u = 0; u < N; ++u) x[u] = one(from, R.offset(tid / VPR + u * RPP, pad, ROWS - pad) + at(cols, tid), 0, cols, tid);
     }
     // rows before `pad` are zero
     template <bool WHOLE> __device__ __forceinline__ void store(E* lds, int cols, int pad, int tid) const
@@ -247,11 +282,12 @@ template <typename E, bool EXACT> __device__ __forceinline__ uint32_t row_at(int
     constexpr int VE = Ops<E>::VE;
     return (col + VE <= cols ? col : EXACT || cols < VE ? 0 : cols - VE) * static_cast<uint32_t>(sizeof(E));
 }
-template <typename E, bool EXACT> __device__ __forceinline__ u32x4 row_load(const char* p, int col, int cols)
+template <typename E, bool EXACT> __device__ __forceinline__ u32x4 row_load(const From<EXACT>& from, uint32_t off, int col, int cols)
 {
-    constexpr int VE = Ops<E>::VE;
-    if (EXACT || cols >= VE) return load16(p);
-    return col == 0 ? load_few<E>(p, cols) : u32x4{0, 0, 0, 0};
+    if constexpr (!EXACT) {
+        if (cols < Ops<E>::VE) return col == 0 ? load_few<E>(from.p + off, cols) : u32x4{0, 0, 0, 0};
+    }
+    return from.load(off, 0);
 }
 template <typename E, bool EXACT> __device__ __forceinline__ u32x4 row_place(u32x4 x, int col, int cols)
 {
@@ -283,38 +319,29 @@ template <typename E, int DAP> struct Smem {
     float pw[C + 1];
 };
 
-// One workgroup scans the tokens of one segment of one head for 64 value columns of one role.  Its 8 waves
-// are CT row tiles (16 tokens each) x CG groups of 16 NP columns.  For a block, a wave forms the outputs of its row tile and its
-// columns: scores against the keys of earlier tiles and its own, kept in registers as the operand of the
-// product with the values, and the queries (which no other row tile needs: from global memory straight into
-// fragments) times the state.  Then it updates its share of the state, half of the channel tiles for 16 of its columns (so
-// that the weighted values, whose parts cost the vector unit more than anything else, are formed by two
-// waves and not by four), and puts it into LDS as the next block's operand.  STATES: only the segment's state from zero, to the workspace.
-template <typename E, int DAP, bool STATES, bool EXACT>
-__global__ __launch_bounds__(NT) void decay_scan_kernel(DecayLaunch L)
+// One workgroup scans the tokens of one segment of one head for 64 value columns of one role.  For a block, a wave
+// forms the outputs of one row tile (16 of the block's tokens) for 16 NP columns: scores against the keys of earlier
+// tiles and its own, kept in registers as the operand of the product with the values, and the queries (which no
+// other row tile needs: from global memory straight into fragments) times the state.  Then it updates its share of
+// the state, DTW of the channel tiles for 16 columns, and puts it into LDS as the next block's operand.
+// STATES: only the segment's state from zero, to the workspace.
+// RT: the wave's row tile.  Every wave runs the copy of its own, straight-line code in the loop; all of them have the same barriers, one
+// a block (two with one state buffer).
+template <typename E, int DAP, int NW, bool STATES, bool EXACT, int RT>
+__device__ __forceinline__ void decay_scan(const DecayLaunch& L, const DecayRole R, long bh, int sl, unsigned char* smem, int w)
 {
     typedef Ops<E> O;
     typedef typename O::Frag Frag;
     typedef Smem<E, DAP> Mem;
-    constexpr int C = O::C, KB = O::KB, VE = O::VE, CT = C / 16, CG = NW / CT, NP = NS / CG / 16;
-    constexpr int DT = DAP / 16, DTW = DT / 2, DF = DAP / KB, CF = C / KB, TPF = KB / 16, ES = sizeof(E);
+    constexpr int NT = 64 * NW, C = O::C, KB = O::KB, VE = O::VE, CT = C / 16, CG = NW / CT, NP = NS / 16 / CG;
+    constexpr int DT = DAP / 16, DTW = DT * NP / CT, DF = DAP / KB, CF = C / KB, TPF = KB / 16, ES = sizeof(E);
     constexpr int SK = Mem::SK, SV = Mem::SV, SS = Mem::SS, SB = Mem::SB;
-    static_assert(DT % 2 == 0 && NP * CG * 16 == NS && CT == 2 * NP, "tiles");
-    extern __shared__ __align__(16) unsigned char smem[];
+    static_assert(NP * CG * 16 == NS && CT % NP == 0, "tiles");
     Mem& M = *reinterpret_cast<Mem*>(smem);
 
-    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 15, g = lane >> 4;
-    // (waves w and w + 4 share a SIMD: the row tiles of a pair add up to the same number of score tiles)
-    const int wave_rt = CT == 4 ? (w < 4 ? w : 7 - w) : (w ^ (w >> 2)) & 1, cg = w / CT;
-    int total = 0;
-    for (int r = 0; r < L.roles; ++r) total += L.role[r].slices;
-    long bh;
-    int sl, ri = 0;
-    head_slice(blockIdx.x, total, static_cast<long>(L.B) * L.H, bh, sl);
-    while (sl >= L.role[ri].slices) sl -= L.role[ri++].slices;
-    const DecayRole& R = L.role[ri];
-    const int b = static_cast<int>(bh / L.H), h = static_cast<int>(bh - static_cast<long>(b) * L.H);
-    const int seg = blockIdx.y, len = seq_length(L.lengths, b, L.T);
+    const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, g = lane >> 4, cg = w / CT;
+    const int b = __builtin_amdgcn_readfirstlane(static_cast<int>(bh / L.H)), h = static_cast<int>(bh - static_cast<long>(b) * L.H);
+    const int seg = blockIdx.y, len = __builtin_amdgcn_readfirstlane(seq_length(L.lengths, b, L.T));
     const long long first = static_cast<long long>(seg) * L.seg_tokens;              // in scan order
     const int begin = first < len ? static_cast<int>(first) : len;
     const int end = first + L.seg_tokens < len ? static_cast<int>(first) + L.seg_tokens : len;
@@ -337,37 +364,30 @@ __global__ __launch_bounds__(NT) void decay_scan_kernel(DecayLaunch L)
         if (tid <= C) M.pw[tid] = tid == 0 ? 1.f : expf(static_cast<float>(tid) * gl);
     }
 
-    Tile<E, C, DAP, SK, EXACT> tk;
-    Tile<E, C, NS, SV, EXACT> tv;
+    Tile<E, NT, C, DAP, SK, EXACT> tk;
+    Tile<E, NT, C, NS, SV, EXACT> tv;
     u32x4 qn[DF];
-    uint32_t qoff[DF];
     // blocks end where the segment ends; the first one has `pad` rows too many
     const int pad = begin < end ? (C - (end - begin) % C) % C : 0;
-    auto place = [&](int pad) {
-        tk.place(kr, da, pad, tid);
-        tv.place(vr, dbs, pad, tid);
-        if (!STATES) {
-            const uint32_t row = qr.offset(16 * wave_rt + c, pad, C - pad);
+    tk.place(kr, da, tid);
+    tv.place(vr, dbs, tid);
+    auto load_queries = [&](const char* base, uint32_t row) {
+        const From<EXACT> from(base);
 #pragma unroll
-            for (int f = 0; f < DF; ++f) qoff[f] = row + row_at<E, EXACT>(KB * f + VE * g, da);
-        }
+        for (int f = 0; f < DF; ++f) qn[f] = row_load<E, EXACT>(from, row + row_at<E, EXACT>(KB * f + VE * g, da), KB * f + VE * g, da);
     };
-    auto load = [&](int at, int n) {
-        tk.load(kr.base(at, n), da, tid);
-        tv.load(vr.base(at, n), dbs, tid);
-        if (!STATES) {
-            const char* p = qr.base(at, n);
-#pragma unroll
-            for (int f = 0; f < DF; ++f) qn[f] = row_load<E, EXACT>(p + qoff[f], KB * f + VE * g, da);
-        }
-    };
-    place(pad);
-    if (begin < end) load(begin, C - pad);
+    if (begin < end) {
+        tk.load_first(kr, begin, pad, da, tid);
+        tv.load_first(vr, begin, pad, dbs, tid);
+        if (!STATES) load_queries(qr.base(begin, C - pad), qr.offset(16 * RT + c, pad, C - pad));
+    }
+    const uint32_t qoff = STATES ? 0 : qr.offset(16 * RT + c, 0, C);
 
-    // the wave's columns: tile p has column (c, p); a lane's 4 NP columns of its outputs are neighbours
-    const int col0 = 16 * NP * cg + 4 * NP * (c >> 2) + (c & 3);      // + 4 p
+    // the wave's columns: lane c of tile p has column col0 + col_of(p), so that a lane's outputs of two tiles are 8 neighbours
+    const int col0 = 16 * NP * cg + (NP == 1 ? c : 8 * (c >> 2) + (c & 3));
+    auto col_of = [](int p) { return 32 * (p >> 1) + 4 * (p & 1); };
     // its share of the state: column (c, sp), lane (c, g) has rows srow + 16 d + r
-    const int scol = col0 + 4 * (wave_rt % NP), srow = 16 * DTW * (wave_rt / NP) + 4 * g;
+    const int scol = col0 + col_of(RT % NP), srow = 16 * DTW * (RT / NP) + 4 * g;
     f32x4 S[DTW];
     {
         const float* src = nullptr;
@@ -384,12 +404,17 @@ __global__ __launch_bounds__(NT) void decay_scan_kernel(DecayLaunch L)
             }
         }
 #pragma unroll
-        for (int d = 0; d < DTW; ++d)
+        for (int d = 0; d < DTW; ++d) S[d] = zero4();
+        if (src != nullptr) {
+            src += (n0 + (scol < dbs ? scol : 0)) * cs;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int row = srow + 16 * d + r;
-                S[d][r] = src != nullptr && scol < dbs && row < da ? src[row * rs + (n0 + scol) * cs] : 0.f;
-            }
+            for (int d = 0; d < DTW; ++d)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int row = srow + 16 * d + r;
+                    S[d][r] = masked(scol < dbs && row < da, src[(row < da ? row : 0) * rs]);
+                }
+        }
     }
     __syncthreads();
 
@@ -399,7 +424,7 @@ __global__ __launch_bounds__(NT) void decay_scan_kernel(DecayLaunch L)
     for (int t = 0; t < CT; ++t)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const int far = 16 * (wave_rt - t) + c - (4 * g + r);
+            const int far = 16 * (RT - t) + c - (4 * g + r);
             wd[t][r] = far >= 0 ? R.intra * M.pw[far] : 0.f;
         }
     const float upd = R.upd;
@@ -409,13 +434,14 @@ __global__ __launch_bounds__(NT) void decay_scan_kernel(DecayLaunch L)
         for (int e = 0; e < KB / 4; ++e)
             wv[f][e] = upd * M.pw[C - 1 - (KB * f + 16 * (e / 4) + 4 * g + (e & 3)) + (reverse ? 1 : 0)];
     // the first block's decays of the state that enters it are those of its tokens
-    const int after = 16 * wave_rt + c + (reverse ? 0 : 1);
+    const int after = 16 * RT + c + (reverse ? 0 : 1);
     const float wi_whole = R.inter * M.pw[after];
     float wi = R.inter * M.pw[after > pad ? after - pad : 0];
-    const Pow lam_whole = decay_pow(C, gl);
-    Pow lam = pad > 0 ? decay_pow(C - pad, gl) : lam_whole;
+    // hi is what a block multiplies the state by; lo is carried until it moves the rounded factor
+    const Pow lam = decay_pow(C, gl), lam_first = pad > 0 ? decay_pow(C - pad, gl) : lam;
+    float factor = lam_first.hi, carry = lam_first.lo;
     int low = pad;                  // first row with a token
-    const uint32_t ooff = orow.offset(16 * wave_rt + c, 0, C);
+    const uint32_t ooff = orow.offset(16 * RT + c, 0, C);
 
     // the state, rounded to the element type, as the operand of its product with the queries
     auto state_out = [&](E* to) {
@@ -429,14 +455,15 @@ __global__ __launch_bounds__(NT) void decay_scan_kernel(DecayLaunch L)
         tk.template store<false>(M.k[0], da, pad, tid);
         tv.template store<false>(M.v[0], dbs, pad, tid);
         if (!STATES) state_out(M.s[0]);
-        place(0);
     }
     __syncthreads();
 
-    // The blocks, for the waves of row tile rt: one barrier a block (two with one state buffer), the same for all of them.
-    auto blocks = [&](auto rtc) __attribute__((always_inline)) {
-        constexpr int rt = decltype(rtc)::value, sp = rt % NP;
+    constexpr int sp = RT % NP;
+    {
+        const char *kbase = kr.base(begin - pad, C), *vbase = vr.base(begin - pad, C), *qbase = qr.base(begin - pad, C);
+        const char* obase = orow.base(begin - pad, C);
         int buf = 0;
+#pragma clang loop unroll(disable)
         for (int at = begin - pad; at < end; at += C, buf ^= 1) {
             const int next = at + C;
             const E *K = M.k[buf], *V = M.v[buf], *SL = M.s[SB == 2 ? buf : 0];
@@ -445,14 +472,23 @@ __global__ __launch_bounds__(NT) void decay_scan_kernel(DecayLaunch L)
 #pragma unroll
                 for (int f = 0; f < DF; ++f) qf[f] = __builtin_bit_cast(Frag, row_place<E, EXACT>(qn[f], KB * f + VE * g, da));
             }
-            if (next < end) load(next, C);
+            if (next < end) {
+                kbase += kr.st * C;
+                vbase += vr.st * C;
+                tk.load(kbase, reverse, da, tid);
+                tv.load(vbase, reverse, dbs, tid);
+                if (!STATES) {
+                    qbase += qr.st * C;
+                    load_queries(qbase, qoff);
+                }
+            }
             Frag vf[CF][NP];
 #pragma unroll
             for (int f = 0; f < CF; ++f)
 #pragma unroll
                 for (int p = 0; p < NP; ++p)
-                    if ((!STATES && TPF * f <= rt) || p == sp)
-                        vf[f][p] = O::cols(V + KB * f * SV + 16 * NP * cg + 4 * p + O::cols_at(SV, 4 * NP, c, g), SV);
+                    if ((!STATES && TPF * f <= RT) || p == sp)
+                        vf[f][p] = O::cols(V + KB * f * SV + 16 * NP * cg + col_of(p) + O::cols_at(SV, NP == 1 ? 4 : 8, c, g), SV);
             if (!STATES) {
                 // outputs, transposed: rows are columns of v, columns are tokens
                 f32x4 x[NP];
@@ -461,42 +497,56 @@ __global__ __launch_bounds__(NT) void decay_scan_kernel(DecayLaunch L)
 #pragma unroll
                 for (int f = 0; f < DF; ++f)
 #pragma unroll
-                    for (int p = 0; p < NP; ++p) O::mma(x[p], O::rows(SL + (col0 + 4 * p) * SS + KB * f + VE * g), qf[f]);
+                    for (int p = 0; p < NP; ++p) O::mma(x[p], O::rows(SL + (col0 + col_of(p)) * SS + KB * f + VE * g), qf[f]);
+                __builtin_amdgcn_sched_barrier(0);
                 // scores, transposed: rows are keys; rounded once to the element type, as the operand of the product with v
-                f32x4 sc[TPF * ((rt + TPF) / TPF)];
+                f32x4 sc[TPF * ((RT + TPF) / TPF)];
 #pragma unroll
-                for (int t = 0; t < TPF * ((rt + TPF) / TPF); ++t) sc[t] = zero4();
+                for (int t = 0; t < TPF * ((RT + TPF) / TPF); ++t) sc[t] = zero4();
 #pragma unroll
                 for (int e = 0; e < DF; ++e)
 #pragma unroll
-                    for (int t = 0; t <= rt; ++t) O::mma(sc[t], O::rows(K + (16 * t + c) * SK + KB * e + VE * g), qf[e]);
+                    for (int t = 0; t <= RT; ++t) O::mma(sc[t], O::rows(K + (16 * t + c) * SK + KB * e + VE * g), qf[e]);
 #pragma unroll
-                for (int t = 0; t <= rt; ++t)
+                for (int t = 0; t <= RT; ++t)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) sc[t][r] = t < rt || c >= 4 * g + r ? sc[t][r] * wd[t][r] : 0.f;
+                    for (int r = 0; r < 4; ++r) sc[t][r] = t < RT || c >= 4 * g + r ? sc[t][r] * wd[t][r] : 0.f;
 #pragma unroll
                 for (int p = 0; p < NP; ++p)
 #pragma unroll
                     for (int r = 0; r < 4; ++r) x[p][r] *= wi;
 #pragma unroll
-                for (int f = 0; TPF * f <= rt; ++f) {
+                for (int f = 0; TPF * f <= RT; ++f) {
                     const Frag a = O::acc(&sc[TPF * f]);
 #pragma unroll
                     for (int p = 0; p < NP; ++p) O::mma(x[p], vf[f][p], a);
                 }
-                const int at_n = 16 * NP * cg + 4 * NP * g;
-                if (16 * rt + c >= low) {
-                    E* to = reinterpret_cast<E*>(const_cast<char*>(orow.base(at, C)) + ooff) + at_n;
-                    if (at_n + 4 * NP <= dbs) {
-                        store16(reinterpret_cast<char*>(to), O::pack16(x));
-                    } else if (!EXACT) {
+                __builtin_amdgcn_sched_barrier(0);
+                if (16 * RT + c >= low) {
+                    const From<EXACT> out(obase);
 #pragma unroll
-                        for (int p = 0; p < NP; ++p)
+                    for (int u = 0; u < (NP + 1) / 2; ++u) {
+                        constexpr int PN = NP == 1 ? 4 : 8;         // neighbours
+                        const int at_n = 16 * NP * cg + 32 * u + PN * g;
+                        const uint32_t off = ooff + at_n * ES;
+                        if (at_n + PN <= dbs) {
+                            if constexpr (ES == 2) {
+                                out.store(off, 0, O::pack8(x[2 * u], x[2 * u + 1]));
+                            } else {
+                                out.store(off, 0, __builtin_bit_cast(u32x4, x[2 * u]));
+                                if constexpr (NP > 1) out.store(off, 16, __builtin_bit_cast(u32x4, x[2 * u + 1]));
+                            }
+                        } else if (EXACT) {
+                            if (VE == 4 && at_n < dbs) out.store(off, 0, __builtin_bit_cast(u32x4, x[2 * u]));
+                        } else {
+                            E* to = reinterpret_cast<E*>(const_cast<char*>(obase) + off);
 #pragma unroll
-                            for (int r = 0; r < 4; ++r)
-                                if (at_n + 4 * p + r < dbs) O::store1(to + 4 * p + r, x[p][r]);
+                            for (int i = 0; i < PN; ++i)
+                                if (at_n + i < dbs) O::store1(to + i, x[2 * u + i / 4][i % 4]);
+                        }
                     }
                 }
+                obase += orow.st * C;
                 if (SB == 1) __syncthreads();
                 wi = wi_whole;
                 low = 0;
@@ -504,7 +554,7 @@ __global__ __launch_bounds__(NT) void decay_scan_kernel(DecayLaunch L)
 #pragma unroll
             for (int d = 0; d < DTW; ++d)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) S[d][r] = __builtin_fmaf(S[d][r], lam.hi, S[d][r] * lam.lo);
+                for (int r = 0; r < 4; ++r) S[d][r] *= factor;
 #pragma unroll
             for (int f = 0; f < CF; ++f) {
                 Frag vw[O::PARTS], kf[DTW];
@@ -517,7 +567,9 @@ __global__ __launch_bounds__(NT) void decay_scan_kernel(DecayLaunch L)
 #pragma unroll
                     for (int d = 0; d < DTW; ++d) O::mma(S[d], kf[d], vw[s]);
             }
-            lam = lam_whole;
+            carry += lam.lo;
+            factor = lam.hi + carry;
+            carry -= factor - lam.hi;
             if (next < end) {
                 if (!STATES) state_out(M.s[SB == 2 ? buf ^ 1 : 0]);
                 tk.template store<true>(M.k[buf ^ 1], da, 0, tid);
@@ -525,13 +577,6 @@ __global__ __launch_bounds__(NT) void decay_scan_kernel(DecayLaunch L)
             }
             __syncthreads();
         }
-    };
-    if (STATES && NP == 1) blocks(std::integral_constant<int, 0>{});     // (only the columns' tile matters)
-    else if (wave_rt == 0 || (STATES && wave_rt == 2)) blocks(std::integral_constant<int, 0>{});
-    else if (wave_rt == 1 || STATES) blocks(std::integral_constant<int, 1>{});
-    else if constexpr (CT == 4) {
-        if (wave_rt == 2) blocks(std::integral_constant<int, 2>{});
-        else blocks(std::integral_constant<int, 3>{});
     }
 
     float* dst = nullptr;
@@ -561,6 +606,39 @@ __global__ __launch_bounds__(NT) void decay_scan_kernel(DecayLaunch L)
     }
 }
 
+template <typename E, int DAP, int NW, bool STATES, bool EXACT>
+__global__ __launch_bounds__(64 * NW, 2) void decay_scan_kernel(DecayLaunch L)
+{
+    extern __shared__ __align__(16) unsigned char smem[];
+    constexpr int CT = Ops<E>::C / 16;
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    // (waves w and w + 4 share a SIMD: their row tiles add up to the same number of score tiles)
+    const int rt = CT == 4 ? (w < 4 ? w : 7 - w) : (w ^ (w >> 2)) & 1;
+    // (the roles are told apart by constants: an argument indexed at run time would be copied to memory, and its fields would no
+    // longer be known to be the same for all lanes; divisions run on the vector unit, with the same result)
+    int total = 0;
+#pragma unroll
+    for (int r = 0; r < DECAY_ROLES; ++r) total += r < L.roles ? L.role[r].slices : 0;
+    long bh;
+    int sl;
+    head_slice(blockIdx.x, total, static_cast<long>(L.B) * L.H, bh, sl);
+    bh = static_cast<long>(same_for_all(static_cast<uint64_t>(bh)));
+    sl = __builtin_amdgcn_readfirstlane(sl);
+    DecayRole R = L.role[0];
+    if (sl >= R.slices && L.roles > 1) {
+        sl -= R.slices;
+        R = L.role[1];
+        if (sl >= R.slices && L.roles > 2) {
+            sl -= R.slices;
+            R = L.role[2];
+        }
+    }
+    if (rt == 0) decay_scan<E, DAP, NW, STATES, EXACT, 0>(L, R, bh, sl, smem, w);
+    else if (CT == 2 || rt == 1) decay_scan<E, DAP, NW, STATES, EXACT, 1>(L, R, bh, sl, smem, w);
+    else if (rt == 2) decay_scan<E, DAP, NW, STATES, EXACT, CT == 4 ? 2 : 0>(L, R, bh, sl, smem, w);
+    else decay_scan<E, DAP, NW, STATES, EXACT, CT == 4 ? 3 : 0>(L, R, bh, sl, smem, w);
+}
+
 // The segments' states from zero become the states that enter them: one thread for an element of a
 // head's state, in place.
 __global__ __launch_bounds__(NJ) void decay_join_kernel(DecayLaunch L)
@@ -587,9 +665,11 @@ __global__ __launch_bounds__(NJ) void decay_join_kernel(DecayLaunch L)
 
 template <typename E, int DAP, bool STATES, bool EXACT> hipError_t scan(const DecayLaunch& L, unsigned groups, hipStream_t st)
 {
+    constexpr int NW = waves<E>(DAP);
     constexpr size_t bytes = sizeof(Smem<E, DAP>);
     static_assert(bytes <= 160 * 1024, "one compute unit's LDS");
-    hipLaunchKernelGGL((decay_scan_kernel<E, DAP, STATES, EXACT>), dim3(groups, STATES ? L.segments - 1 : L.segments), dim3(NT), bytes, st, L);
+    hipLaunchKernelGGL((decay_scan_kernel<E, DAP, NW, STATES, EXACT>), dim3(groups, STATES ? L.segments - 1 : L.segments), dim3(64 * NW), bytes,
+                       st, L);
     return hipGetLastError();
 }
 
@@ -599,13 +679,24 @@ template <typename E, bool STATES, bool EXACT> hipError_t scan_da(const DecayLau
                                                                              : scan<E, 256, STATES, EXACT>(L, groups, st);
 }
 
-// EXACT where every role's channels are whole 16-byte vectors: the general kernels' loads and stores by parts cost them
-// registers and instructions
+// EXACT where every role's channels are whole 16-byte vectors at 4-byte addresses and a block's rows lie within 2^31 bytes: the
+// general kernels' loads and stores by parts, and their 64-bit addresses, cost them registers and instructions
+template <typename E> bool exact(const void* p, const long long (&st)[3], int n)
+{
+    constexpr long long ES = sizeof(E);
+    if (n % Ops<E>::VE != 0 || reinterpret_cast<uintptr_t>(p) % 4 != 0) return false;
+    for (long long s : st)
+        if (s * ES % 4 != 0) return false;
+    return st[2] <= ((1LL << 31) - 65536) / (Ops<E>::C * ES);
+}
 template <typename E> hipError_t scan_any(const DecayLaunch& L, int da, unsigned groups, bool states, hipStream_t st)
 {
-    bool exact = true;
-    for (int r = 0; r < L.roles; ++r) exact = exact && L.role[r].da % Ops<E>::VE == 0 && L.role[r].db % Ops<E>::VE == 0;
-    if (exact) return states ? scan_da<E, true, true>(L, da, groups, st) : scan_da<E, false, true>(L, da, groups, st);
+    bool all = true;
+    for (int r = 0; r < L.roles; ++r) {
+        const DecayRole& R = L.role[r];
+        all = all && exact<E>(R.q, R.q_s, R.da) && exact<E>(R.k, R.k_s, R.da) && exact<E>(R.v, R.v_s, R.db) && exact<E>(R.o, R.o_s, R.db);
+    }
+    if (all) return states ? scan_da<E, true, true>(L, da, groups, st) : scan_da<E, false, true>(L, da, groups, st);
     return states ? scan_da<E, true, false>(L, da, groups, st) : scan_da<E, false, false>(L, da, groups, st);
 }
 
