@@ -432,13 +432,14 @@ sfda_status_t sfda_rotary(const void* q, const void* k, const float* cos, const 
  *   S0, S_T : [B, H, dk, dv] contiguous float32, each may be NULL (zero state; not wanted).
  *          S_T == S0 is allowed.
  *   workspace : with at least sfda_decay_attn_fwd_workspace_bytes(...) bytes (0 where one workgroup
- *          for a head and 64 value columns fills the device) the sequences are cut into segments that are scanned
+ *          for a head and 32 or 64 value columns fills the device) the sequences are cut into segments that are scanned
  *          in parallel; with less, or NULL, they are scanned whole.  The same result up to rounding.
  *   1 <= dk, dv <= 256.  bfloat16: the block's scores and the state are rounded to bfloat16 as operands of
  *   the products that give o; the state itself is carried in float32 from exact products.  A token with a
  *   value that is not finite makes the rows of its block (32 or 64 tokens) before it NaN too.
  */
-size_t sfda_decay_attn_fwd_workspace_bytes(int B, int H, int T, int dk, int dv);
+size_t sfda_decay_attn_fwd_workspace_bytes(int B, int H, int T, int dk, int dv,
+                                           sfda_dtype_t dtype);
 
 sfda_status_t sfda_decay_attn_fwd(const void* q, const void* k, const void* v,
                                   const float* log_decay, const int* lengths, const float* S0,
@@ -454,7 +455,8 @@ sfda_status_t sfda_decay_attn_fwd(const void* q, const void* k, const void* v,
  *   dq, dk, dv : as q, k, v, zero past a sequence's length; dS0 [B, H, dk, dv] float32 or NULL.
  *   strides: (b, h, t) of q, k, v, dO, dq, dk, dv.  Other arguments as the forward's.
  */
-size_t sfda_decay_attn_bwd_workspace_bytes(int B, int H, int T, int dk, int dv);
+size_t sfda_decay_attn_bwd_workspace_bytes(int B, int H, int T, int dk, int dv,
+                                           sfda_dtype_t dtype);
 
 sfda_status_t sfda_decay_attn_bwd(const void* q, const void* k, const void* v,
                                   const float* log_decay, const int* lengths, const float* S0,

@@ -22,11 +22,6 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int NS = DECAY_SLICE;          // value columns of a scan workgroup
-// Waves of a scan workgroup.  Four (one on a SIMD) form no scores and no weighted values twice, eight hide more
-// latency and have half the registers' worth of work each.  Forward B8 H16 T4096 bfloat16 d 128: 161 us with four, 182 with
-// eight; float32 B4 H8 T2048: 143 and 136; with 256 channels four do not have the registers.
-template <typename E> constexpr int waves(int dap) { return sizeof(E) == 2 && dap <= 128 ? 4 : 8; }
 constexpr int NJ = 256;                  // threads of the small kernels
 
 // 16 bytes at any address (global memory takes unaligned vectors)
@@ -211,7 +206,7 @@ template <> struct From<true> {
 };
 
 // A block's rows of one tensor on their way to LDS: ROWS tokens x COLS channels (COLS padded), 16-byte
-// vectors held in registers between the load and the write.  Padding channels are clamped to channel 0 and never written.
+// vectors held in registers between the load and the write.  Padding channels are clamped to channel 0, and never written.
 // EXACT: the channels are whole vectors.  Otherwise the vector that would cross a row's end is moved back to end with it (the
 // write then goes by elements), and rows shorter than a vector are read by elements.
 template <typename E, int NT, int ROWS, int COLS, int STRIDE, bool EXACT> struct Tile {
@@ -253,8 +248,9 @@ template <typename E, int NT, int ROWS, int COLS, int STRIDE, bool EXACT> struct
     // rows before `pad` are zero
     template <bool WHOLE> __device__ __forceinline__ void store(E* lds, int cols, int pad, int tid) const
     {
-        const int col = (tid % VPR) * VE;
-        if (col >= cols) return;
+        int col = (tid % VPR) * VE;
+        if (EXACT) col = col < cols ? col : 0;      // (padding lanes hold channel 0's vector, and write it once more)
+        else if (col >= cols) return;
 #pragma unroll
         for (int u = 0; u < N; ++u) {
             const int r = tid / VPR + u * RPP;
@@ -309,12 +305,21 @@ template <typename E, bool EXACT> __device__ __forceinline__ u32x4 row_place(u32
     return u32x4{static_cast<uint32_t>(lo), static_cast<uint32_t>(lo >> 32), static_cast<uint32_t>(hi), static_cast<uint32_t>(hi >> 32)};
 }
 
-// LDS of a scan: the keys and values of a block and of the next, the state as an operand ([column][channel], twice where
-// it fits, so that a block needs one barrier), and the powers of lambda
-template <typename E, int DAP> struct Smem {
+// A scan workgroup's value columns and waves, for the type and the (padded) channels of the state.
+//  * bfloat16: 64 columns; four waves (one on a SIMD) form no scores and no weighted values twice, eight hide more latency and have
+//    half the registers' worth of work each.  Forward B8 H16 T4096 d 128: 161 us with four, 182 with eight (and 197 with
+//    32 columns); with 256 channels four do not have the registers.
+//  * float32: 32 columns and four waves where two such workgroups share a compute unit (their LDS): forward B4 H8 T2048 d 128
+//    122 us, with 64 columns and eight waves 134.
+template <typename E> constexpr int waves(int dap) { return dap <= 128 ? 4 : 8; }
+template <typename E> constexpr int slice(int dap) { return decay_slice(sizeof(E) == 2, dap); }
+
+// LDS of a scan: the keys and values of a block and of the next, the state as an operand ([column][channel]; twice with SB 2, so
+// that a block needs one barrier), and the powers of lambda
+template <typename E, int DAP, int SB> struct Smem {
     typedef Ops<E> O;
+    static constexpr int NS = slice<E>(DAP);
     static constexpr int C = O::C, SK = DAP + O::KP, SV = NS + O::VP, SS = DAP + O::SP, KV = C * (SK + SV), ST = NS * SS;
-    static constexpr int SB = (2 * KV + 2 * ST) * sizeof(E) <= 158 * 1024 ? 2 : 1;
     E k[2][C * SK], v[2][C * SV], s[SB][ST];
     float pw[C + 1];
 };
@@ -327,15 +332,15 @@ template <typename E, int DAP> struct Smem {
 // STATES: only the segment's state from zero, to the workspace.
 // RT: the wave's row tile.  Every wave runs the copy of its own, straight-line code in the loop; all of them have the same barriers, one
 // a block (two with one state buffer).
-template <typename E, int DAP, int NW, bool STATES, bool EXACT, int RT>
+template <typename E, int DAP, int SB, bool STATES, bool EXACT, int RT>
 __device__ __forceinline__ void decay_scan(const DecayLaunch& L, const DecayRole R, long bh, int sl, unsigned char* smem, int w)
 {
     typedef Ops<E> O;
     typedef typename O::Frag Frag;
-    typedef Smem<E, DAP> Mem;
-    constexpr int NT = 64 * NW, C = O::C, KB = O::KB, VE = O::VE, CT = C / 16, CG = NW / CT, NP = NS / 16 / CG;
+    typedef Smem<E, DAP, SB> Mem;
+    constexpr int NW = waves<E>(DAP), NS = Mem::NS, NT = 64 * NW, C = O::C, KB = O::KB, VE = O::VE, CT = C / 16, CG = NW / CT, NP = NS / 16 / CG;
     constexpr int DT = DAP / 16, DTW = DT * NP / CT, DF = DAP / KB, CF = C / KB, TPF = KB / 16, ES = sizeof(E);
-    constexpr int SK = Mem::SK, SV = Mem::SV, SS = Mem::SS, SB = Mem::SB;
+    constexpr int SK = Mem::SK, SV = Mem::SV, SS = Mem::SS;
     static_assert(NP * CG * 16 == NS && CT % NP == 0, "tiles");
     Mem& M = *reinterpret_cast<Mem*>(smem);
 
@@ -498,7 +503,7 @@ __device__ __forceinline__ void decay_scan(const DecayLaunch& L, const DecayRole
                 for (int f = 0; f < DF; ++f)
 #pragma unroll
                     for (int p = 0; p < NP; ++p) O::mma(x[p], O::rows(SL + (col0 + col_of(p)) * SS + KB * f + VE * g), qf[f]);
-                __builtin_amdgcn_sched_barrier(0);
+                __builtin_amdgcn_sched_barrier(0);     // (phases kept apart: mixed, they measure 2 to 5% more)
                 // scores, transposed: rows are keys; rounded once to the element type, as the operand of the product with v
                 f32x4 sc[TPF * ((RT + TPF) / TPF)];
 #pragma unroll
@@ -522,28 +527,34 @@ __device__ __forceinline__ void decay_scan(const DecayLaunch& L, const DecayRole
                     for (int p = 0; p < NP; ++p) O::mma(x[p], vf[f][p], a);
                 }
                 __builtin_amdgcn_sched_barrier(0);
-                if (16 * RT + c >= low) {
-                    const From<EXACT> out(obase);
+                const From<EXACT> out(obase);
+                const bool row = 16 * RT + c >= low;
+                constexpr int PN = NP == 1 ? 4 : 8;         // neighbours
 #pragma unroll
-                    for (int u = 0; u < (NP + 1) / 2; ++u) {
-                        constexpr int PN = NP == 1 ? 4 : 8;         // neighbours
-                        const int at_n = 16 * NP * cg + 32 * u + PN * g;
-                        const uint32_t off = ooff + at_n * ES;
-                        if (at_n + PN <= dbs) {
-                            if constexpr (ES == 2) {
-                                out.store(off, 0, O::pack8(x[2 * u], x[2 * u + 1]));
-                            } else {
-                                out.store(off, 0, __builtin_bit_cast(u32x4, x[2 * u]));
-                                if constexpr (NP > 1) out.store(off, 16, __builtin_bit_cast(u32x4, x[2 * u + 1]));
-                            }
-                        } else if (EXACT) {
-                            if (VE == 4 && at_n < dbs) out.store(off, 0, __builtin_bit_cast(u32x4, x[2 * u]));
+                for (int u = 0; u < (NP + 1) / 2; ++u) {
+                    const int at_n = 16 * NP * cg + 32 * u + PN * g;
+                    const uint32_t off = ooff + at_n * ES;
+                    if constexpr (EXACT) {      // (stores past the resource's range are dropped)
+                        constexpr uint32_t NOWHERE = 0x80000000u;
+                        if constexpr (ES == 2) {
+                            out.store(row && at_n < dbs ? off : NOWHERE, 0, O::pack8(x[2 * u], x[2 * u + 1]));
                         } else {
-                            E* to = reinterpret_cast<E*>(const_cast<char*>(obase) + off);
-#pragma unroll
-                            for (int i = 0; i < PN; ++i)
-                                if (at_n + i < dbs) O::store1(to + i, x[2 * u + i / 4][i % 4]);
+                            out.store(row && at_n < dbs ? off : NOWHERE, 0, __builtin_bit_cast(u32x4, x[2 * u]));
+                            if constexpr (NP > 1)
+                                out.store(row && at_n + 4 < dbs ? off + 16 : NOWHERE, 0, __builtin_bit_cast(u32x4, x[2 * u + 1]));
                         }
+                    } else if (row && at_n + PN <= dbs) {
+                        if constexpr (ES == 2) {
+                            out.store(off, 0, O::pack8(x[2 * u], x[2 * u + 1]));
+                        } else {
+                            out.store(off, 0, __builtin_bit_cast(u32x4, x[2 * u]));
+                            if constexpr (NP > 1) out.store(off, 16, __builtin_bit_cast(u32x4, x[2 * u + 1]));
+                        }
+                    } else if (row) {
+                        E* to = reinterpret_cast<E*>(const_cast<char*>(obase) + off);
+#pragma unroll
+                        for (int i = 0; i < PN; ++i)
+                            if (at_n + i < dbs) O::store1(to + i, x[2 * u + i / 4][i % 4]);
                     }
                 }
                 obase += orow.st * C;
@@ -570,7 +581,8 @@ __device__ __forceinline__ void decay_scan(const DecayLaunch& L, const DecayRole
             carry += lam.lo;
             factor = lam.hi + carry;
             carry -= factor - lam.hi;
-            if (next < end) {
+            // (after the last block what is written is not read: no branch splits the block's instructions)
+            if (EXACT || next < end) {
                 if (!STATES) state_out(M.s[SB == 2 ? buf ^ 1 : 0]);
                 tk.template store<true>(M.k[buf ^ 1], da, 0, tid);
                 tv.template store<true>(M.v[buf ^ 1], dbs, 0, tid);
@@ -606,8 +618,8 @@ __device__ __forceinline__ void decay_scan(const DecayLaunch& L, const DecayRole
     }
 }
 
-template <typename E, int DAP, int NW, bool STATES, bool EXACT>
-__global__ __launch_bounds__(64 * NW, 2) void decay_scan_kernel(DecayLaunch L)
+template <typename E, int DAP, int SB, bool STATES, bool EXACT>
+__global__ __launch_bounds__(64 * waves<E>(DAP), 2) void decay_scan_kernel(DecayLaunch L)
 {
     extern __shared__ __align__(16) unsigned char smem[];
     constexpr int CT = Ops<E>::C / 16;
@@ -633,10 +645,10 @@ __global__ __launch_bounds__(64 * NW, 2) void decay_scan_kernel(DecayLaunch L)
             R = L.role[2];
         }
     }
-    if (rt == 0) decay_scan<E, DAP, NW, STATES, EXACT, 0>(L, R, bh, sl, smem, w);
-    else if (CT == 2 || rt == 1) decay_scan<E, DAP, NW, STATES, EXACT, 1>(L, R, bh, sl, smem, w);
-    else if (rt == 2) decay_scan<E, DAP, NW, STATES, EXACT, CT == 4 ? 2 : 0>(L, R, bh, sl, smem, w);
-    else decay_scan<E, DAP, NW, STATES, EXACT, CT == 4 ? 3 : 0>(L, R, bh, sl, smem, w);
+    if (rt == 0) decay_scan<E, DAP, SB, STATES, EXACT, 0>(L, R, bh, sl, smem, w);
+    else if (CT == 2 || rt == 1) decay_scan<E, DAP, SB, STATES, EXACT, 1>(L, R, bh, sl, smem, w);
+    else if (rt == 2) decay_scan<E, DAP, SB, STATES, EXACT, CT == 4 ? 2 : 0>(L, R, bh, sl, smem, w);
+    else decay_scan<E, DAP, SB, STATES, EXACT, CT == 4 ? 3 : 0>(L, R, bh, sl, smem, w);
 }
 
 // The segments' states from zero become the states that enter them: one thread for an element of a
@@ -663,14 +675,28 @@ __global__ __launch_bounds__(NJ) void decay_join_kernel(DecayLaunch L)
     }
 }
 
+template <typename E, int DAP, int SB, bool STATES, bool EXACT> hipError_t scan_sb(const DecayLaunch& L, unsigned groups, hipStream_t st)
+{
+    constexpr size_t bytes = sizeof(Smem<E, DAP, SB>);
+    static_assert(bytes <= 160 * 1024, "one compute unit's LDS");
+    hipLaunchKernelGGL((decay_scan_kernel<E, DAP, SB, STATES, EXACT>), dim3(groups, STATES ? L.segments - 1 : L.segments),
+                       dim3(64 * waves<E>(DAP)), bytes, st, L);
+    return hipGetLastError();
+}
+
+// One state buffer or two.  Two where a second workgroup fits beside it all the same, or where there is none: with
+// bfloat16 and 128 channels one buffer lets two workgroups share a compute unit (forward B8 H16 T4096, 256 workgroups: 168 us with two
+// buffers, 177 with one; backward, 768 workgroups: 443 and 404).  The segments' states need no buffer.
 template <typename E, int DAP, bool STATES, bool EXACT> hipError_t scan(const DecayLaunch& L, unsigned groups, hipStream_t st)
 {
-    constexpr int NW = waves<E>(DAP);
-    constexpr size_t bytes = sizeof(Smem<E, DAP>);
-    static_assert(bytes <= 160 * 1024, "one compute unit's LDS");
-    hipLaunchKernelGGL((decay_scan_kernel<E, DAP, NW, STATES, EXACT>), dim3(groups, STATES ? L.segments - 1 : L.segments), dim3(64 * NW), bytes,
-                       st, L);
-    return hipGetLastError();
+    constexpr size_t HALF = 80 * 1024;
+    if constexpr (!STATES && sizeof(Smem<E, DAP, 2>) <= HALF)
+        return scan_sb<E, DAP, 2, STATES, EXACT>(L, groups, st);
+    else if constexpr (!STATES && sizeof(Smem<E, DAP, 1>) <= HALF)
+        return static_cast<long long>(groups) * L.segments <= L.cus ? scan_sb<E, DAP, 2, STATES, EXACT>(L, groups, st)
+                                                                    : scan_sb<E, DAP, 1, STATES, EXACT>(L, groups, st);
+    else
+        return scan_sb<E, DAP, 1, STATES, EXACT>(L, groups, st);
 }
 
 template <typename E, bool STATES, bool EXACT> hipError_t scan_da(const DecayLaunch& L, int da, unsigned groups, hipStream_t st)
@@ -778,7 +804,7 @@ hipError_t launch_decay(const DecayLaunch& L, hipStream_t st)
             for (int r = 0; r < L.roles; ++r)
                 if (L.role[r].da > low && L.role[r].da <= lim) {
                     P.role[P.roles++] = L.role[r];
-                    slices += L.role[r].slices;
+                    slices += P.role[P.roles - 1].slices = decay_slices(L.bf16, lim, L.role[r].db);
                 }
             if (P.roles == 0) continue;
             const unsigned groups = static_cast<unsigned>(heads * slices);

@@ -22,7 +22,7 @@ struct DecayRole {
     long long q_s[3], k_s[3], v_s[3], o_s[3];   // element strides of b, h, t
     int da, db;
     long long s_row, s_col;  // element strides of S0 and S_T inside a head (of da * db elements)
-    int slices;              // workgroups over the value columns
+    int slices;              // workgroups over the value columns (set by the launcher)
     int reverse;
     float intra, inter, upd;
 };
@@ -36,9 +36,12 @@ struct DecayLaunch {
     int B, H, T;
     int seg_tokens;          // tokens of a segment (T or more: one segment)
     int segments;
+    int cus;                 // compute units of the device
     bool bf16;
 };
-constexpr int DECAY_SLICE = 64;    // value columns of a workgroup
+// value columns of a scan workgroup, and workgroups over db columns, for a state of da channels
+constexpr int decay_slice(bool bf16, int da) { return bf16 || da > 128 ? 64 : 32; }
+constexpr int decay_slices(bool bf16, int da, int db) { return (db + decay_slice(bf16, da) - 1) / decay_slice(bf16, da); }
 hipError_t launch_decay(const DecayLaunch& L, hipStream_t st);
 
 struct DecayStepLaunch {

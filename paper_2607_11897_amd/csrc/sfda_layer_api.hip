@@ -4,6 +4,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <atomic>
 
 #include "../../include/sfda.h"
 #include "sfda_layer.h"
@@ -184,11 +185,15 @@ void strides3(ll (&out)[3], const ll* given, int which, ll H, ll T, ll D)
     }
 }
 
+// compute units of the current device, looked up once for each
 int cus()
 {
+    static std::atomic<int> known[64];
     int dev = -1, v = 0;
-    if (hipGetDevice(&dev) != hipSuccess || hipDeviceGetAttribute(&v, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || v <= 0)
-        return 256;
+    if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return 256;
+    if ((v = known[dev].load(std::memory_order_relaxed)) > 0) return v;
+    if (hipDeviceGetAttribute(&v, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || v <= 0) return 256;
+    known[dev].store(v, std::memory_order_relaxed);
     return v;
 }
 
@@ -196,11 +201,10 @@ constexpr int MAX_D = 256;              // key and value channels of a decay att
 bool decay_sizes(int B, int H, int T, int dk, int dv)
 {
     if (B < 0 || H < 0 || T < 0 || dk < 1 || dk > MAX_D || dv < 1 || dv > MAX_D) return false;
-    // workgroups of 256 threads in launches of less than 2^32; tokens are counted in 32 bits with room for a block
-    return static_cast<ll>(B) * H * 3 * MAX_D / sfda::DECAY_SLICE * 256 < (1LL << 32) && T <= INT_MAX - 1024;
+    // at most 8 threads for a head and value column of a role, in launches of less than 2^32; tokens are counted in 32 bits with
+    // room for a block
+    return static_cast<ll>(B) * H * 3 * MAX_D * 8 < (1LL << 32) && T <= INT_MAX - 1024;
 }
-
-int slices_of(int db) { return (db + sfda::DECAY_SLICE - 1) / sfda::DECAY_SLICE; }
 
 // Segments of a sequence: where one workgroup for a head and 64 value columns would leave compute units
 // idle, each head's tokens are cut so that there are about two workgroups for each, in segments of at
@@ -260,12 +264,13 @@ sfda_status_t sfda_rotary(const void* q, const void* k, const float* cos, const 
     return sfda::launch_rotary(L, static_cast<hipStream_t>(stream)) == hipSuccess ? SFDA_OK : SFDA_ERR_HIP;
 }
 
-size_t sfda_decay_attn_fwd_workspace_bytes(int B, int H, int T, int dk, int dv)
+size_t sfda_decay_attn_fwd_workspace_bytes(int B, int H, int T, int dk, int dv, sfda_dtype_t dtype)
 {
-    if (!decay_sizes(B, H, T, dk, dv)) return 0;
+    if (!dtype_ok(dtype) || !decay_sizes(B, H, T, dk, dv)) return 0;
     const ll heads = static_cast<ll>(B) * H;
+    const bool bf16 = dtype == SFDA_BF16;
     if (heads == 0) return 0;
-    const Cut c = cut_of(heads * slices_of(dv), T);
+    const Cut c = cut_of(heads * sfda::decay_slices(bf16, dk, dv), T);
     return c.segments > 1 ? static_cast<size_t>(c.segments) * heads * dk * dv * 4 : 0;
 }
 
@@ -277,6 +282,7 @@ sfda_status_t sfda_decay_attn_fwd(const void* q, const void* k, const void* v, c
     if (!dtype_ok(dtype)) return SFDA_ERR_DTYPE;
     if (!decay_sizes(B, H, T, dk, dv)) return SFDA_ERR_SHAPE;
     const ll heads = static_cast<ll>(B) * H, e = esize(dtype), state = heads * dk * dv * 4;
+    const bool bf16 = dtype == SFDA_BF16;
     if (heads == 0) return SFDA_OK;
     sfda::DecayLaunch L{};
     sfda::DecayRole& R = L.role[0];
@@ -284,7 +290,7 @@ sfda_status_t sfda_decay_attn_fwd(const void* q, const void* k, const void* v, c
     strides3(R.k_s, strides, 1, H, T, dk);
     strides3(R.v_s, strides, 2, H, T, dv);
     strides3(R.o_s, strides, 3, H, T, dv);
-    const size_t need = sfda_decay_attn_fwd_workspace_bytes(B, H, T, dk, dv);
+    const size_t need = sfda_decay_attn_fwd_workspace_bytes(B, H, T, dk, dv, dtype);
     const bool cut = need > 0 && workspace != nullptr && workspace_bytes >= need;
     Call c;
     c.input(box(q, e, dk, {B, H, T}, R.q_s), e);
@@ -298,25 +304,27 @@ sfda_status_t sfda_decay_attn_fwd(const void* q, const void* k, const void* v, c
     c.output(flat(cut ? workspace : nullptr, static_cast<ll>(need)), 4, false);
     const sfda_status_t st = c.done();
     if (st != SFDA_OK) return st;
-    const Cut segs = cut_of(heads * slices_of(dv), T);
+    const Cut segs = cut_of(heads * sfda::decay_slices(bf16, dk, dv), T);
     R.q = q; R.k = k; R.v = v; R.o = o; R.S0 = S0; R.S_T = S_T;
-    R.da = dk; R.db = dv; R.s_row = dv; R.s_col = 1; R.slices = slices_of(dv);
+    R.da = dk; R.db = dv; R.s_row = dv; R.s_col = 1;
     R.intra = scale; R.inter = scale; R.upd = 1.f;
     R.ws = cut ? static_cast<float*>(workspace) : nullptr;
     L.roles = 1; L.log_decay = log_decay; L.lengths = lengths; L.B = B; L.H = H; L.T = T;
     L.seg_tokens = cut ? segs.tokens : std::max(T, 1);
     L.segments = cut ? segs.segments : 1;
-    L.bf16 = dtype == SFDA_BF16;
+    L.cus = cus();
+    L.bf16 = bf16;
     return sfda::launch_decay(L, static_cast<hipStream_t>(stream)) == hipSuccess ? SFDA_OK : SFDA_ERR_HIP;
 }
 
 // dq and dk have dk columns, dv has dv; the dk and dv scans need dS_T, the dq scan S0
-size_t sfda_decay_attn_bwd_workspace_bytes(int B, int H, int T, int dk, int dv)
+size_t sfda_decay_attn_bwd_workspace_bytes(int B, int H, int T, int dk, int dv, sfda_dtype_t dtype)
 {
-    if (!decay_sizes(B, H, T, dk, dv)) return 0;
+    if (!dtype_ok(dtype) || !decay_sizes(B, H, T, dk, dv)) return 0;
     const ll heads = static_cast<ll>(B) * H;
+    const bool bf16 = dtype == SFDA_BF16;
     if (heads == 0) return 0;
-    const Cut c = cut_of(heads * (2 * slices_of(dk) + slices_of(dv)), T);
+    const Cut c = cut_of(heads * (2 * sfda::decay_slices(bf16, dv, dk) + sfda::decay_slices(bf16, dk, dv)), T);
     return c.segments > 1 ? 3 * static_cast<size_t>(c.segments) * heads * dk * dv * 4 : 0;
 }
 
@@ -328,6 +336,7 @@ sfda_status_t sfda_decay_attn_bwd(const void* q, const void* k, const void* v, c
     if (!dtype_ok(dtype)) return SFDA_ERR_DTYPE;
     if (!decay_sizes(B, H, T, dk, dv)) return SFDA_ERR_SHAPE;
     const ll heads = static_cast<ll>(B) * H, e = esize(dtype), state = heads * dk * dv * 4;
+    const bool bf16 = dtype == SFDA_BF16;
     if (heads == 0) return SFDA_OK;
     ll qs[3], ks[3], vs[3], gs[3], dqs[3], dks[3], dvs[3];
     strides3(qs, strides, 0, H, T, dk);
@@ -337,7 +346,7 @@ sfda_status_t sfda_decay_attn_bwd(const void* q, const void* k, const void* v, c
     strides3(dqs, strides, 4, H, T, dk);
     strides3(dks, strides, 5, H, T, dk);
     strides3(dvs, strides, 6, H, T, dv);
-    const size_t need = sfda_decay_attn_bwd_workspace_bytes(B, H, T, dk, dv);
+    const size_t need = sfda_decay_attn_bwd_workspace_bytes(B, H, T, dk, dv, dtype);
     const bool cut = need > 0 && workspace != nullptr && workspace_bytes >= need;
     Call c;
     c.input(box(q, e, dk, {B, H, T}, qs), e);
@@ -355,7 +364,7 @@ sfda_status_t sfda_decay_attn_bwd(const void* q, const void* k, const void* v, c
     c.output(flat(cut ? workspace : nullptr, static_cast<ll>(need)), 4, false);
     const sfda_status_t st = c.done();
     if (st != SFDA_OK) return st;
-    const Cut segs = cut_of(heads * (2 * slices_of(dk) + slices_of(dv)), T);
+    const Cut segs = cut_of(heads * (2 * sfda::decay_slices(bf16, dv, dk) + sfda::decay_slices(bf16, dk, dv)), T);
     const int segments = cut ? segs.segments : 1;
     sfda::DecayLaunch L{};
     auto put = [](ll (&to)[3], const ll (&from)[3]) { std::copy(from, from + 3, to); };
@@ -364,7 +373,7 @@ sfda_status_t sfda_decay_attn_bwd(const void* q, const void* k, const void* v, c
         sfda::DecayRole& R = L.role[i];
         R.q = a; R.k = b; R.v = x; R.o = out;
         put(R.q_s, as); put(R.k_s, bs); put(R.v_s, xs); put(R.o_s, os);
-        R.da = da; R.db = db; R.slices = slices_of(db);
+        R.da = da; R.db = db;
         R.s_row = transposed ? 1 : dv; R.s_col = transposed ? dv : 1;
         R.S0 = reverse ? dS_T : S0; R.S_T = nullptr; R.reverse = reverse;
         R.intra = scale; R.inter = reverse ? 1.f : scale; R.upd = reverse ? scale : 1.f;
@@ -377,7 +386,8 @@ sfda_status_t sfda_decay_attn_bwd(const void* q, const void* k, const void* v, c
     L.roles = 3; L.log_decay = log_decay; L.lengths = lengths; L.B = B; L.H = H; L.T = T;
     L.seg_tokens = cut ? segs.tokens : std::max(T, 1);
     L.segments = segments;
-    L.bf16 = dtype == SFDA_BF16;
+    L.cus = cus();
+    L.bf16 = bf16;
     return sfda::launch_decay(L, static_cast<hipStream_t>(stream)) == hipSuccess ? SFDA_OK : SFDA_ERR_HIP;
 }
 

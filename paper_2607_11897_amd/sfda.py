@@ -114,7 +114,7 @@ def load_library(path: str = LIB_PATH):
         fn.restype = i
     for fn in (lib.sfda_decay_attn_fwd_workspace_bytes, lib.sfda_decay_attn_bwd_workspace_bytes,
                lib.sfda_group_norm_bwd_workspace_bytes):
-        fn.argtypes = [i] * 5
+        fn.argtypes = [i] * (5 if fn is lib.sfda_group_norm_bwd_workspace_bytes else 6)
         fn.restype = sz
     lib.sfda_status_string.argtypes = [i]
     lib.sfda_status_string.restype = ctypes.c_char_p
@@ -663,7 +663,7 @@ def decay_attn_fwd(q, k, v, log_decay, S0=None, *, scale: float = 1.0, lengths=N
                 lengths=(lengths, (B,)), S0=(S0, (B, H, dk, dv)), o=(o, (B, H, T, dv)), S_T=(S_T, (B, H, dk, dv)),
                 workspace=(workspace, tuple(workspace.shape) if workspace is not None else ())))
     if workspace is None:
-        nws = lib.sfda_decay_attn_fwd_workspace_bytes(B, H, T, dk, dv)
+        nws = lib.sfda_decay_attn_fwd_workspace_bytes(B, H, T, dk, dv, code)
         workspace = _try_workspace(nws, q.device, stream) if nws else None
     st = lib.sfda_decay_attn_fwd(_rows(q), _rows(k), _rows(v), _ptr(log_decay), _ptr(lengths), _ptr(S0), _rows(o), _ptr(S_T),
                                  B, H, T, dk, dv, scale,
@@ -698,7 +698,7 @@ def decay_attn_bwd(q, k, v, log_decay, S0, dO, dS_T=None, *, scale: float = 1.0,
                 dO=(dO, tv), dS_T=(dS_T, ts), dq=(dq, tk), dk=(dk, tk), dv=(dv, tv),
                 workspace=(workspace, tuple(workspace.shape) if workspace is not None else ())))
     if workspace is None:
-        nws = lib.sfda_decay_attn_bwd_workspace_bytes(B, H, T, nk, nv)
+        nws = lib.sfda_decay_attn_bwd_workspace_bytes(B, H, T, nk, nv, code)
         workspace = _try_workspace(nws, q.device, stream) if nws else None
     strides = _STRIDES[21](*q.stride()[:3], *k.stride()[:3], *v.stride()[:3], *dO.stride()[:3], *dq.stride()[:3],
                                        *dk.stride()[:3], *dv.stride()[:3])
@@ -711,12 +711,16 @@ def decay_attn_bwd(q, k, v, log_decay, S0, dO, dS_T=None, *, scale: float = 1.0,
     return dict(dq=dq, dk=dk, dv=dv, dS0=dS0)
 
 
-def decay_attn_fwd_workspace_bytes(B: int, H: int, T: int, dk: int, dv: int) -> int:
-    return int(load_library().sfda_decay_attn_fwd_workspace_bytes(B, H, T, dk, dv))
+def decay_attn_fwd_workspace_bytes(B: int, H: int, T: int, dk: int, dv: int, dtype: str = "f32") -> int:
+    """The workspace at which decay_attn_fwd is fastest; dtype: the activations' ("f32" or "bf16")."""
+    code = {"f32": SFDA_F32, "bf16": SFDA_BF16}[dtype]
+    return int(load_library().sfda_decay_attn_fwd_workspace_bytes(B, H, T, dk, dv, code))
 
 
-def decay_attn_bwd_workspace_bytes(B: int, H: int, T: int, dk: int, dv: int) -> int:
-    return int(load_library().sfda_decay_attn_bwd_workspace_bytes(B, H, T, dk, dv))
+def decay_attn_bwd_workspace_bytes(B: int, H: int, T: int, dk: int, dv: int, dtype: str = "f32") -> int:
+    """The workspace at which decay_attn_bwd is fastest; dtype: the activations' ("f32" or "bf16")."""
+    code = {"f32": SFDA_F32, "bf16": SFDA_BF16}[dtype]
+    return int(load_library().sfda_decay_attn_bwd_workspace_bytes(B, H, T, dk, dv, code))
 
 
 def decay_attn_step(q, k, v, log_decay, S, *, scale: float = 1.0, o=None, stream=None):

@@ -178,7 +178,7 @@ def test_decay_attn_segments_agree_and_resume(dtype):
     say("decay_attn_fwd segments", dtype)
     B, H, T, dk, dv = 1, 3, 900, 48, 72
     x = attn(9, B, H, T, dk, dv, dtype)
-    assert sfda.decay_attn_fwd_workspace_bytes(B, H, T, dk, dv) > 0
+    assert sfda.decay_attn_fwd_workspace_bytes(B, H, T, dk, dv, dtype) > 0
     a = run_fwd(x, dtype, "bhtd", 1.0)
     b = run_fwd(x, dtype, "bhtd", 1.0, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
     assert rel_err(a[0], b[0]) <= ATTN[dtype] and rel_err(a[1], b[1]) <= SUM
