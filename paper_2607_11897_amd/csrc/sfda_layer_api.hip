@@ -237,8 +237,9 @@ sfda_status_t sfda_rotary(const void* q, const void* k, const float* cos, const 
     if (static_cast<ll>(Hq) + Hk > INT_MAX - 64) return SFDA_ERR_SHAPE;
     if (B == 0 || T == 0 || Hq + Hk == 0) return SFDA_OK;
     const ll e = esize(dtype);
-    // a thread for four heads and at least four channels of a token, less than 2^32 in a launch
-    if ((static_cast<double>(Hq) + Hk + 3) / 4 * B * T * (D / (16. / e) + 3) >= 4294967296. - 256.) return SFDA_ERR_SHAPE;
+    // a thread for four heads or four tokens of a 16-byte unit of channels, less than 2^32 in a launch
+    const double H = static_cast<double>(Hq) + Hk, rows = std::max((H + 6) / 4 * T, H * ((T + 3.) / 4)) * B;
+    if (rows * (D * e / 16. + 3) >= 4294967296. - 1024.) return SFDA_ERR_SHAPE;
     sfda::RotaryLaunch L{};
     strides3(L.q_s, strides, 0, Hq, T, D);
     strides3(L.k_s, strides, 1, Hk, T, D);
@@ -498,7 +499,8 @@ sfda_status_t sfda_group_norm_bwd(const void* dy, const void* x, const float* we
     L.dy = dy; L.x = x; L.weight = weight; L.bias = bias; L.gate = gate;
     L.dx = dx; L.dgate = dgate; L.dweight = dweight; L.dbias = dbias;
     L.partial = dweight != nullptr || dbias != nullptr ? static_cast<float*>(workspace) : nullptr;
-    L.B = B; L.H = H; L.T = T; L.D = D; L.silu = activation == SFDA_ACT_SILU; L.eps = eps; L.bf16 = dtype == SFDA_BF16;
+    L.B = T > 0 ? B : 0; L.H = H; L.T = std::max(T, 1); L.D = D;      // (no tokens: the weights' gradients are zeros)
+    L.silu = activation == SFDA_ACT_SILU; L.eps = eps; L.bf16 = dtype == SFDA_BF16;
     return sfda::launch_norm_bwd(L, static_cast<hipStream_t>(stream)) == hipSuccess ? SFDA_OK : SFDA_ERR_HIP;
 }
 

@@ -2,62 +2,42 @@
 //   x^ = (x - mean) / sqrt(var + eps) over the D channels of one head of one token,  n = x^ w + b,
 //   y = act(n) without a gate, n act(z) with one;  act(z) = z or z sigmoid(z).
 // Memory-bound.  A group of lanes holds a row in registers (two-pass variance, float32), a workgroup keeps
-// one head's weights in registers over its strip of tokens, and in the backward their gradients too.
-#include "sfda_device.h"
+// one head's weights in registers over its strip of tokens, and in the backward their gradients too.  The next row's vectors
+// are requested before a row's arithmetic, so that the reductions do not leave the memory idle.
 #include "sfda_layer.h"
-
-#include <string.h>
+#include "sfda_vec.h"
 
 namespace sfda {
 namespace {
 
+using namespace vec;
+
 constexpr int NT = 256;
 
-template <typename E> struct Vec;
-template <> struct Vec<uint16_t> { static constexpr int N = 8; };
-template <> struct Vec<float> { static constexpr int N = 4; };
-
-template <typename E> __device__ __forceinline__ void get(float* x, const E* p, int n)
+template <int CTRL> __device__ __forceinline__ float dpp(float x)
 {
-    constexpr int N = Vec<E>::N;
-    E e[N] = {};
-    if (n >= N) {
-        memcpy(e, p, 16);
-    } else {
-        for (int i = 0; i < N; ++i)
-            if (i < n) e[i] = p[i];
-    }
-#pragma unroll
-    for (int i = 0; i < N; ++i) x[i] = Elem<E>::load(e, i);
+    return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), CTRL, 0xF, 0xF, false));
 }
-__device__ __forceinline__ void to(float& e, float x) { e = x; }
-__device__ __forceinline__ void to(uint16_t& e, float x) { e = __builtin_bit_cast(uint16_t, static_cast<__bf16>(x)); }
-template <typename E> __device__ __forceinline__ void put(E* p, const float* x, int n)
-{
-    constexpr int N = Vec<E>::N;
-    E e[N];
-#pragma unroll
-    for (int i = 0; i < N; ++i) to(e[i], x[i]);
-    if (n >= N) {
-        memcpy(p, e, 16);
-    } else {
-        for (int i = 0; i < N; ++i)
-            if (i < n) p[i] = e[i];
-    }
-}
-
-// sum over a group of `lpg` (a power of two) neighbouring lanes, in the same order for every lane
+// sum over a group of `lpg` (a power of two) neighbouring lanes, the same for every lane of it.  Within 16 lanes by data-parallel
+// moves: the quad's neighbours, then mirrored halves, whose lanes already hold equal sums.
 __device__ __forceinline__ float group_sum(float x, int lpg)
 {
-    for (int m = 1; m < lpg; m <<= 1) x += __shfl_xor(x, m);
+    if (lpg > 1) x += dpp<0xB1>(x);         // quad [1, 0, 3, 2]
+    if (lpg > 2) x += dpp<0x4E>(x);         // quad [2, 3, 0, 1]
+    if (lpg > 4) x += dpp<0x141>(x);        // half row mirrored
+    if (lpg > 8) x += dpp<0x140>(x);        // row mirrored
+    if (lpg > 16) x += __shfl_xor(x, 16);
+    if (lpg > 32) x += __shfl_xor(x, 32);
     return x;
 }
 
-// act and its derivative (at infinities their limits: the product with 0 is taken of a finite number)
-__device__ __forceinline__ void silu(float z, int on, float& f, float& df)
+// act and its derivative.  The sigmoid by the hardware's exponential and reciprocal (an ulp each, and |z| 2^-24 of the
+// exponent's own rounding); at infinities the limits: the product with 0 is taken of a finite number.
+template <bool SILU> __device__ __forceinline__ void act(float z, float& f, float& df)
 {
-    if (on) {
-        const float s = 1.f / (1.f + expf(-z)), most = 3e38f, zc = z < -most ? -most : z > most ? most : z;
+    if constexpr (SILU) {
+        const float s = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * -1.44269504089f));
+        const float most = 3e38f, zc = z < -most ? -most : z > most ? most : z;
         f = (z < 0.f ? zc : z) * s;
         df = s * (1.f + zc * (1.f - s));
     } else {
@@ -67,52 +47,76 @@ __device__ __forceinline__ void silu(float z, int on, float& f, float& df)
 }
 
 // V: vectors of a lane.  A workgroup takes one head and every strips-th block of rows (b, t).
-template <typename E, int V, bool BWD>
-__global__ __launch_bounds__(NT) void norm_kernel(NormLaunch L, int lpg, int strips)
+template <typename E, int V, bool BWD, bool GATE, bool SILU>
+__device__ __forceinline__ void norm_rows(const NormLaunch& L, int lpg, int strips, float (&dw)[V][Vec<E>::N], float (&db)[V][Vec<E>::N])
 {
     constexpr int N = Vec<E>::N;
-    __shared__ float red[BWD ? NT * N : 1];
     const int tid = threadIdx.x, gl = tid & (lpg - 1), gi = tid / lpg, groups = NT / lpg;
     const int h = blockIdx.x % L.H, strip = blockIdx.x / L.H, D = L.D;
-    float w[V][N], bias[V][N], dw[V][N], db[V][N];
+    const long long hc = static_cast<long long>(h) * D;
+    float w[V][N], bias[V][N];
 #pragma unroll
     for (int k = 0; k < V; ++k) {
         const int ch = (gl + k * lpg) * N;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const bool in = ch + i < D;
-            const long long at = static_cast<long long>(h) * D + (in ? ch + i : 0);
+            const long long at = hc + (in ? ch + i : 0);
             w[k][i] = L.weight != nullptr ? L.weight[at] : 1.f;
             bias[k][i] = L.bias != nullptr ? L.bias[at] : 0.f;
             if (!in) w[k][i] = bias[k][i] = 0.f;
-            dw[k][i] = db[k][i] = 0.f;
         }
     }
-    const long long rows = static_cast<long long>(L.B) * L.T;
+    const long long rows = static_cast<long long>(L.B) * L.T, stride = static_cast<long long>(strips) * groups;
     const float inv = 1.f / D;
-    for (long long r0 = static_cast<long long>(strip) * groups; r0 < rows; r0 += static_cast<long long>(strips) * groups) {
-        const long long row = r0 + gi;
-        const bool there = row < rows;
-        const long long rr = there ? row : rows - 1;        // (a group without a row repeats the last one and writes nothing)
-        const long long b = rr / L.T, t = rr - b * L.T;
+    // (b, t) of a row, moved on by `stride` rows at a time
+    const long long first = static_cast<long long>(strip) * groups + gi;
+    const int step_b = static_cast<int>(stride / L.T), step_t = static_cast<int>(stride - static_cast<long long>(step_b) * L.T);
+    long long b = first / L.T, t = first - b * L.T;
+
+    u32x4 rx[V], rz[V], rd[V];
+    auto fetch = [&](long long b, long long t) {
         const E* xp = static_cast<const E*>(L.x) + b * L.x_s[0] + h * L.x_s[1] + t * L.x_s[2];
-        const long long hc = static_cast<long long>(h) * D;
-        float x[V][N], z[V][N], dy[V][N];
-        float sum = 0.f;
+        const E* zp = static_cast<const E*>(L.gate) + b * L.g_s[0] + t * L.g_s[1] + hc;
+        const E* dp = static_cast<const E*>(L.dy) + b * L.y_s[0] + t * L.y_s[1] + hc;
 #pragma unroll
         for (int k = 0; k < V; ++k) {
             const int ch = (gl + k * lpg) * N, n = D - ch;
             if (n > 0) {
-                get<E>(x[k], xp + ch, n);
-                if (L.gate != nullptr) get<E>(z[k], static_cast<const E*>(L.gate) + b * L.g_s[0] + t * L.g_s[1] + hc + ch, n);
-                if (BWD) get<E>(dy[k], static_cast<const E*>(L.dy) + b * L.y_s[0] + t * L.y_s[1] + hc + ch, n);
-            } else {
-#pragma unroll
-                for (int i = 0; i < N; ++i) x[k][i] = z[k][i] = dy[k][i] = 0.f;
+                rx[k] = load<E>(xp + ch, n);
+                if (GATE) rz[k] = load<E>(zp + ch, n);
+                if (BWD) rd[k] = load<E>(dp + ch, n);
             }
+        }
+    };
+    const u32x4 none = {0, 0, 0, 0};
+#pragma unroll
+    for (int k = 0; k < V; ++k) rx[k] = rz[k] = rd[k] = none;       // (lanes past D keep zeros)
+    if (first < rows) fetch(b, t);
+    // every group of a wave makes the same number of turns (their sums need all lanes); one past the last row writes nothing
+    for (long long r = static_cast<long long>(strip) * groups; r < rows; r += stride) {
+        const bool there = r + gi < rows;
+        float x[V][N], z[V][N], dy[V][N];
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+            unpack<E>(x[k], rx[k]);
+            if (GATE) unpack<E>(z[k], rz[k]);
+            if (BWD) unpack<E>(dy[k], rd[k]);
+        }
+        const long long tb = b, tt = t;
+        b += step_b;
+        t += step_t;
+        if (t >= L.T) {
+            t -= L.T;
+            ++b;
+        }
+        if (r + stride + gi < rows) fetch(b, t);
+
+        float sum = 0.f;
+#pragma unroll
+        for (int k = 0; k < V; ++k)
 #pragma unroll
             for (int i = 0; i < N; ++i) sum += x[k][i];     // (elements past D are zero)
-        }
         const float mean = group_sum(sum, lpg) * inv;
         float sq = 0.f;
 #pragma unroll
@@ -123,8 +127,9 @@ __global__ __launch_bounds__(NT) void norm_kernel(NormLaunch L, int lpg, int str
                 x[k][i] = d;
                 sq = __builtin_fmaf(d, d, sq);
             }
-        const float rstd = 1.f / sqrtf(group_sum(sq, lpg) * inv + L.eps);
-        if (!BWD) {
+        const float rstd = __builtin_amdgcn_rsqf(group_sum(sq, lpg) * inv + L.eps);
+        if constexpr (!BWD) {
+            E* yp = static_cast<E*>(L.y) + tb * L.y_s[0] + tt * L.y_s[1] + hc;
 #pragma unroll
             for (int k = 0; k < V; ++k) {
                 const int ch = (gl + k * lpg) * N, n = D - ch;
@@ -132,10 +137,10 @@ __global__ __launch_bounds__(NT) void norm_kernel(NormLaunch L, int lpg, int str
                 for (int i = 0; i < N; ++i) {
                     const float nn = __builtin_fmaf(x[k][i] * rstd, w[k][i], bias[k][i]);
                     float f, df;
-                    silu(L.gate != nullptr ? z[k][i] : nn, L.silu, f, df);
-                    x[k][i] = L.gate != nullptr ? nn * f : f;
+                    act<SILU>(GATE ? z[k][i] : nn, f, df);
+                    x[k][i] = GATE ? nn * f : f;
                 }
-                if (there && n > 0) put<E>(static_cast<E*>(L.y) + b * L.y_s[0] + t * L.y_s[1] + hc + ch, x[k], n);
+                if (there && n > 0) store<E>(yp + ch, pack<E>(x[k]), n);
             }
         } else {
             float s1 = 0.f, s2 = 0.f;
@@ -145,17 +150,16 @@ __global__ __launch_bounds__(NT) void norm_kernel(NormLaunch L, int lpg, int str
                 for (int i = 0; i < N; ++i) {
                     const float xn = x[k][i] * rstd, nn = __builtin_fmaf(xn, w[k][i], bias[k][i]);
                     float f, df, dn;
-                    silu(L.gate != nullptr ? z[k][i] : nn, L.silu, f, df);
-                    if (L.gate != nullptr) {
+                    act<SILU>(GATE ? z[k][i] : nn, f, df);
+                    if (GATE) {
                         dn = dy[k][i] * f;
                         z[k][i] = dy[k][i] * nn * df;
                     } else {
                         dn = dy[k][i] * df;
                     }
-                    if (there) {
-                        dw[k][i] = __builtin_fmaf(dn, xn, dw[k][i]);
-                        db[k][i] += dn;
-                    }
+                    if (!there) dn = 0.f;
+                    dw[k][i] = __builtin_fmaf(dn, xn, dw[k][i]);
+                    db[k][i] += dn;
                     const float dxn = dn * w[k][i];
                     x[k][i] = xn;
                     dy[k][i] = dxn;
@@ -164,50 +168,75 @@ __global__ __launch_bounds__(NT) void norm_kernel(NormLaunch L, int lpg, int str
                 }
             s1 = group_sum(s1, lpg) * inv;
             s2 = group_sum(s2, lpg) * inv;
+            E* dxp = static_cast<E*>(L.dx) + tb * L.dx_s[0] + h * L.dx_s[1] + tt * L.dx_s[2];
+            E* dzp = static_cast<E*>(L.dgate) + tb * L.dg_s[0] + tt * L.dg_s[1] + hc;
 #pragma unroll
             for (int k = 0; k < V; ++k) {
                 const int ch = (gl + k * lpg) * N, n = D - ch;
 #pragma unroll
                 for (int i = 0; i < N; ++i) x[k][i] = rstd * (dy[k][i] - s1 - x[k][i] * s2);
                 if (there && n > 0) {
-                    put<E>(static_cast<E*>(L.dx) + b * L.dx_s[0] + h * L.dx_s[1] + t * L.dx_s[2] + ch, x[k], n);
-                    if (L.gate != nullptr)
-                        put<E>(static_cast<E*>(L.dgate) + b * L.dg_s[0] + t * L.dg_s[1] + hc + ch, z[k], n);
+                    store<E>(dxp + ch, pack<E>(x[k]), n);
+                    if (GATE) store<E>(dzp + ch, pack<E>(z[k]), n);
                 }
             }
         }
     }
-    if (BWD && L.partial != nullptr) {
+}
+
+template <typename E, int V, bool BWD>
+__global__ __launch_bounds__(NT) void norm_kernel(NormLaunch L, int lpg, int strips)
+{
+    constexpr int N = Vec<E>::N;
+    float dw[V][N] = {}, db[V][N] = {};
+    if (L.gate != nullptr) {
+        if (L.silu) norm_rows<E, V, BWD, true, true>(L, lpg, strips, dw, db);
+        else norm_rows<E, V, BWD, true, false>(L, lpg, strips, dw, db);
+    } else {
+        if (L.silu) norm_rows<E, V, BWD, false, true>(L, lpg, strips, dw, db);
+        else norm_rows<E, V, BWD, false, false>(L, lpg, strips, dw, db);
+    }
+    if constexpr (BWD) {
+        if (L.partial == nullptr) return;
         // the workgroup's sums of dw and db, groups added in order
-        const long long HD = static_cast<long long>(L.H) * D;
+        __shared__ float red[NT * N];
+        const int tid = threadIdx.x, groups = NT / lpg, h = blockIdx.x % L.H, strip = blockIdx.x / L.H;
+        const long long HD = static_cast<long long>(L.H) * L.D;
         for (int which = 0; which < 2; ++which)
 #pragma unroll
             for (int k = 0; k < V; ++k) {
                 __syncthreads();
 #pragma unroll
-                for (int i = 0; i < N; ++i) red[(gi * lpg + gl) * N + i] = which ? db[k][i] : dw[k][i];
+                for (int i = 0; i < N; ++i) red[tid * N + i] = which ? db[k][i] : dw[k][i];
                 __syncthreads();
                 for (int e = tid; e < lpg * N; e += NT) {
                     const int ch = k * lpg * N + e;
-                    if (ch >= D) continue;
+                    if (ch >= L.D) continue;
                     float s = 0.f;
                     for (int j = 0; j < groups; ++j) s += red[j * lpg * N + e];
-                    L.partial[(static_cast<long long>(strip) * 2 + which) * HD + static_cast<long long>(h) * D + ch] = s;
+                    L.partial[(static_cast<long long>(strip) * 2 + which) * HD + static_cast<long long>(h) * L.D + ch] = s;
                 }
             }
     }
 }
 
-// dweight and dbias: the strips' sums, added in order
+// dweight and dbias: the strips' sums.  A workgroup for 64 of them; its four waves take every fourth strip, and their parts
+// are added in order.
 __global__ __launch_bounds__(NT) void norm_join_kernel(NormLaunch L, int strips)
 {
-    const long long HD = static_cast<long long>(L.H) * L.D, at = static_cast<long long>(blockIdx.x) * NT + threadIdx.x;
-    if (at >= 2 * HD) return;
-    float* out = at < HD ? L.dweight : L.dbias;
-    if (out == nullptr) return;
+    __shared__ float part[NT];
+    const long long HD = static_cast<long long>(L.H) * L.D, at = static_cast<long long>(blockIdx.x) * 64 + (threadIdx.x & 63);
     float s = 0.f;
-    for (int i = 0; i < strips; ++i) s += L.partial[static_cast<long long>(i) * 2 * HD + at];
-    out[at < HD ? at : at - HD] = s;
+    if (at < 2 * HD) {
+#pragma unroll 8
+        for (int i = threadIdx.x >> 6; i < strips; i += 4) s += L.partial[static_cast<long long>(i) * 2 * HD + at];
+    }
+    part[threadIdx.x] = s;
+    __syncthreads();
+    if (threadIdx.x >= 64 || at >= 2 * HD) return;
+    s = part[threadIdx.x] + part[threadIdx.x + 64] + part[threadIdx.x + 128] + part[threadIdx.x + 192];
+    float* out = at < HD ? L.dweight : L.dbias;
+    if (out != nullptr) out[at < HD ? at : at - HD] = s;
 }
 
 struct Shape { int lpg, v; };
@@ -237,7 +266,7 @@ template <typename E, bool BWD> hipError_t go(const NormLaunch& L, hipStream_t s
     hipError_t e = hipGetLastError();
     if (BWD && e == hipSuccess && L.partial != nullptr) {
         const long long n = 2LL * L.H * L.D;
-        hipLaunchKernelGGL(norm_join_kernel, dim3(static_cast<unsigned>((n + NT - 1) / NT)), block, 0, st, L, strips);
+        hipLaunchKernelGGL(norm_join_kernel, dim3(static_cast<unsigned>((n + 63) / 64)), block, 0, st, L, strips);
         e = hipGetLastError();
     }
     return e;
