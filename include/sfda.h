@@ -434,7 +434,7 @@ sfda_status_t sfda_rotary(const void* q, const void* k, const float* cos, const 
  *   workspace : with at least sfda_decay_attn_fwd_workspace_bytes(...) bytes (0 where one workgroup
  *          for a head and 32 or 64 value columns fills the device) the sequences are cut into segments that are scanned
  *          in parallel; with less, or NULL, they are scanned whole.  The same result up to rounding.
- *   1 <= dk, dv <= 256.  bfloat16: the block's scores and the state are rounded to bfloat16 as operands of
+ *   1 <= dk, dv <= 256; 64 tokens' rows of a tensor lie within 2^31 bytes (SFDA_ERR_SHAPE otherwise).  bfloat16: the block's scores and the state are rounded to bfloat16 as operands of
  *   the products that give o; the state itself is carried in float32 from exact products.  A token with a
  *   value that is not finite makes the rows of its block (32 or 64 tokens) before it NaN too.
  */

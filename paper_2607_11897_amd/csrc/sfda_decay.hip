@@ -32,18 +32,19 @@ __device__ __forceinline__ void store16(char* p, u32x4 x) { *reinterpret_cast<u3
 // the first `cols` (fewer than fill them) elements of a row as 16 bytes, zeros behind them
 template <typename E> __device__ __forceinline__ u32x4 load_few(const char* p, int cols)
 {
-    constexpr int PER = 4 / sizeof(E);
-    u32x4 x = {0, 0, 0, 0};
-#pragma unroll
-    for (int i = 0; i < 4 * PER - 1; ++i)
-        if (i < cols) {
-            E e;
-            memcpy(&e, p + i * sizeof(E), sizeof(E));
-            uint32_t u = 0;
-            memcpy(&u, &e, sizeof(E));
-            x[i / PER] |= u << (i % PER * 16);
-        }
-    return x;
+    typedef unsigned long long u64;
+    constexpr int BITS = 8 * sizeof(E);
+    u64 lo = 0, hi = 0;
+#pragma clang loop unroll(disable)
+    for (int i = cols - 1; i >= 0; --i) {
+        E e;
+        memcpy(&e, p + i * sizeof(E), sizeof(E));
+        uint32_t u = 0;
+        memcpy(&u, &e, sizeof(E));
+        hi = hi << BITS | lo >> (64 - BITS);
+        lo = lo << BITS | u;
+    }
+    return u32x4{static_cast<uint32_t>(lo), static_cast<uint32_t>(lo >> 32), static_cast<uint32_t>(hi), static_cast<uint32_t>(hi >> 32)};
 }
 
 // two float32 as a pair of bfloat16, each to nearest even
@@ -190,12 +191,13 @@ __device__ __forceinline__ uint64_t same_for_all(uint64_t x)
     const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(x)), hi = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(x >> 32));
     return static_cast<uint64_t>(hi) << 32 | lo;
 }
-// 16 bytes at base + off + more, more the same for all lanes.  ALIGNED: to 4 bytes, and less than 2^31 bytes from the base.
+// 16 bytes at base + off + more, more the same for all lanes; less than 2^31 bytes from the base (off may be negative where the
+// bytes before the base are the row's own).  ALIGNED: to 4 bytes, by a buffer resource.
 template <bool ALIGNED> struct From {
     const char* p;
     __device__ __forceinline__ explicit From(const char* base) : p(base) {}
-    __device__ __forceinline__ u32x4 load(uint32_t off, uint32_t more) const { return load16(p + off + more); }
-    __device__ __forceinline__ void store(uint32_t off, uint32_t more, u32x4 x) const { store16(const_cast<char*>(p) + off + more, x); }
+    __device__ __forceinline__ u32x4 load(uint32_t off, uint32_t more) const { return load16(p + static_cast<int>(off + more)); }
+    __device__ __forceinline__ void store(uint32_t off, uint32_t more, u32x4 x) const { store16(const_cast<char*>(p) + static_cast<int>(off + more), x); }
 };
 template <> struct From<true> {
     __amdgpu_buffer_rsrc_t r;
@@ -207,28 +209,33 @@ template <> struct From<true> {
 
 // A block's rows of one tensor on their way to LDS: ROWS tokens x COLS channels (COLS padded), 16-byte
 // vectors held in registers between the load and the write.  Padding channels are clamped to channel 0, and never written.
-// EXACT: the channels are whole vectors.  Otherwise the vector that would cross a row's end is moved back to end with it (the
-// write then goes by elements), and rows shorter than a vector are read by elements.
+// EXACT: the channels are whole vectors.  Otherwise the vector that would cross a row's end is moved back to end with it (into
+// the `before` channels that the row has before these, where they are few; the write then goes by elements), and rows
+// shorter than a vector are read by elements.
 template <typename E, int NT, int ROWS, int COLS, int STRIDE, bool EXACT> struct Tile {
     static constexpr int VE = Ops<E>::VE, VPR = COLS / VE, RPP = NT / VPR, N = ROWS / RPP;
     static_assert(ROWS % RPP == 0 && NT % VPR == 0, "whole passes");
     u32x4 x[N];
     uint32_t off, step;     // a whole block's first vector in memory order, and from a pass to the next
 
-    __device__ __forceinline__ static uint32_t at(int cols, int tid)
+    bool few;               // by elements
+
+    __device__ __forceinline__ uint32_t at(int cols, int tid) const
     {
         const int col = (tid % VPR) * VE;
-        return (col + VE <= cols ? col : EXACT || cols < VE ? 0 : cols - VE) * static_cast<uint32_t>(sizeof(E));
+        return (col + VE <= cols ? col : EXACT || few ? 0 : cols - VE) * static_cast<int>(sizeof(E));
     }
-    __device__ __forceinline__ void place(const Rows& R, int cols, int tid)
+    __device__ __forceinline__ void place(const Rows& R, int cols, int before, int tid)
     {
-        off = R.offset(tid / VPR + (R.st < 0 ? (N - 1) * RPP : 0), 0, ROWS) + at(cols, tid);
+        few = !EXACT && cols + before < VE;
+        off = R.offset(tid / VPR + (R.st < 0 ? (N - 1) * RPP : 0), 0, ROWS);
         step = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(RPP * (R.st < 0 ? -R.st : R.st)));
+        off += at(cols, tid);       // (a vector moved back before the slice: the sum is still past the row's start, which the base is not)
     }
     __device__ __forceinline__ u32x4 one(const From<EXACT>& from, uint32_t o, uint32_t more, int cols, int tid) const
     {
         if constexpr (!EXACT) {
-            if (cols < VE) return tid % VPR == 0 ? load_few<E>(from.p + o + more, cols) : u32x4{0, 0, 0, 0};
+            if (few) return tid % VPR == 0 ? load_few<E>(from.p + static_cast<int>(o + more), cols) : u32x4{0, 0, 0, 0};
         }
         return from.load(o, more);
     }
@@ -256,14 +263,14 @@ template <typename E, int NT, int ROWS, int COLS, int STRIDE, bool EXACT> struct
             const int r = tid / VPR + u * RPP;
             const u32x4 z = {0, 0, 0, 0};
             const u32x4 w = WHOLE || r >= pad ? x[u] : z;
-            if (EXACT || col + VE <= cols || cols < VE) {
+            if (EXACT || col + VE <= cols || few) {
                 *reinterpret_cast<u32x4*>(lds + r * STRIDE + col) = w;
             } else {
 #pragma unroll
                 for (int i = 0; i < VE; ++i) {
                     constexpr int PER = 4 / static_cast<int>(sizeof(E));
                     const uint32_t e = w[i / PER] >> (i % PER * 16);
-                    memcpy(lds + r * STRIDE + cols - VE + i, &e, sizeof(E));
+                    if (cols - VE + i >= 0) memcpy(lds + r * STRIDE + cols - VE + i, &e, sizeof(E));
                 }
             }
         }
@@ -362,20 +369,13 @@ __device__ __forceinline__ void decay_scan(const DecayLaunch& L, const DecayRole
     E* const op = static_cast<E*>(R.o) + b * R.o_s[0] + h * R.o_s[1] + n0;
     const Rows orow = {reinterpret_cast<const char*>(op) + tok0 * R.o_s[2] * ES, dir * R.o_s[2]};
 
-    {   // padding stays zero
-        u32x4* z = reinterpret_cast<u32x4*>(smem);
-        const u32x4 zero = {0, 0, 0, 0};
-        for (int i = tid; i < static_cast<int>(offsetof(Mem, pw)) / 16; i += NT) z[i] = zero;
-        if (tid <= C) M.pw[tid] = tid == 0 ? 1.f : expf(static_cast<float>(tid) * gl);
-    }
-
     Tile<E, NT, C, DAP, SK, EXACT> tk;
     Tile<E, NT, C, NS, SV, EXACT> tv;
     u32x4 qn[DF];
     // blocks end where the segment ends; the first one has `pad` rows too many
     const int pad = begin < end ? (C - (end - begin) % C) % C : 0;
-    tk.place(kr, da, tid);
-    tv.place(vr, dbs, tid);
+    tk.place(kr, da, 0, tid);
+    tv.place(vr, dbs, n0, tid);
     auto load_queries = [&](const char* base, uint32_t row) {
         const From<EXACT> from(base);
 #pragma unroll
@@ -388,37 +388,45 @@ __device__ __forceinline__ void decay_scan(const DecayLaunch& L, const DecayRole
     }
     const uint32_t qoff = STATES ? 0 : qr.offset(16 * RT + c, 0, C);
 
+    {   // padding stays zero (and with whole rows none is read)
+        u32x4* z = reinterpret_cast<u32x4*>(smem);
+        const u32x4 zero = {0, 0, 0, 0};
+        if (da < DAP || dbs < NS)
+            for (int i = tid; i < static_cast<int>(offsetof(Mem, pw)) / 16; i += NT) z[i] = zero;
+        if (tid <= C) M.pw[tid] = tid == 0 ? 1.f : expf(static_cast<float>(tid) * gl);
+    }
+
     // the wave's columns: lane c of tile p has column col0 + col_of(p), so that a lane's outputs of two tiles are 8 neighbours
     const int col0 = 16 * NP * cg + (NP == 1 ? c : 8 * (c >> 2) + (c & 3));
     auto col_of = [](int p) { return 32 * (p >> 1) + 4 * (p & 1); };
     // its share of the state: column (c, sp), lane (c, g) has rows srow + 16 d + r
     const int scol = col0 + col_of(RT % NP), srow = 16 * DTW * (RT / NP) + 4 * g;
     f32x4 S[DTW];
+    // where the state comes from and goes to: elements of 4 bytes at row * rs + column * cs of da * db; a lane's first one, and
+    // what is past the rows or columns nowhere
+    constexpr uint32_t NOWHERE = 0x80000000u;
+    auto state_at = [&](int rs, int cs) { return scol < dbs ? static_cast<uint32_t>(srow * rs + (n0 + scol) * cs) * 4u : NOWHERE; };
+    const long long cells = static_cast<long long>(da) * R.db;
+    const long long ws_at = (static_cast<long long>(seg) * L.B * L.H + bh) * cells;
     {
         const float* src = nullptr;
-        long long rs = 0, cs = 0;
+        int rs = 0, cs = 0;
         if (!STATES) {
-            if (R.ws != nullptr) {
-                src = R.ws + (static_cast<long long>(seg) * L.B * L.H + bh) * da * R.db;
-                rs = R.db;
-                cs = 1;
-            } else if (R.S0 != nullptr) {
-                src = R.S0 + bh * da * static_cast<long long>(R.db);
-                rs = R.s_row;
-                cs = R.s_col;
-            }
+            src = R.ws != nullptr ? R.ws + ws_at : R.S0 != nullptr ? R.S0 + bh * cells : nullptr;
+            rs = R.ws != nullptr ? R.db : static_cast<int>(R.s_row);
+            cs = R.ws != nullptr ? 1 : static_cast<int>(R.s_col);
         }
 #pragma unroll
         for (int d = 0; d < DTW; ++d) S[d] = zero4();
         if (src != nullptr) {
-            src += (n0 + (scol < dbs ? scol : 0)) * cs;
+            const From<true> from(reinterpret_cast<const char*>(src));
+            const uint32_t at = state_at(rs, cs);
 #pragma unroll
             for (int d = 0; d < DTW; ++d)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int row = srow + 16 * d + r;
-                    S[d][r] = masked(scol < dbs && row < da, src[(row < da ? row : 0) * rs]);
-                }
+                for (int r = 0; r < 4; ++r)
+                    S[d][r] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(
+                        from.r, srow + 16 * d + r < da ? at : NOWHERE, __builtin_amdgcn_readfirstlane((16 * d + r) * rs * 4), 0));
         }
     }
     __syncthreads();
@@ -535,7 +543,6 @@ __device__ __forceinline__ void decay_scan(const DecayLaunch& L, const DecayRole
                     const int at_n = 16 * NP * cg + 32 * u + PN * g;
                     const uint32_t off = ooff + at_n * ES;
                     if constexpr (EXACT) {      // (stores past the resource's range are dropped)
-                        constexpr uint32_t NOWHERE = 0x80000000u;
                         if constexpr (ES == 2) {
                             out.store(row && at_n < dbs ? off : NOWHERE, 0, O::pack8(x[2 * u], x[2 * u + 1]));
                         } else {
@@ -592,24 +599,23 @@ __device__ __forceinline__ void decay_scan(const DecayLaunch& L, const DecayRole
     }
 
     float* dst = nullptr;
-    long long rs = 0, cs = 0;
+    int rs = R.db, cs = 1;
     if (STATES) {
-        dst = R.ws + (static_cast<long long>(seg) * L.B * L.H + bh) * da * R.db;
-        rs = R.db;
-        cs = 1;
+        dst = R.ws + ws_at;
     } else if (seg == L.segments - 1 && R.S_T != nullptr) {
-        dst = R.S_T + bh * da * static_cast<long long>(R.db);
-        rs = R.s_row;
-        cs = R.s_col;
+        dst = R.S_T + bh * cells;
+        rs = static_cast<int>(R.s_row);
+        cs = static_cast<int>(R.s_col);
     }
     if (dst != nullptr) {
+        const From<true> to(reinterpret_cast<const char*>(dst));
+        const uint32_t at = state_at(rs, cs);
 #pragma unroll
         for (int d = 0; d < DTW; ++d)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int row = srow + 16 * d + r;
-                if (row < da && scol < dbs) dst[row * rs + (n0 + scol) * cs] = S[d][r];
-            }
+            for (int r = 0; r < 4; ++r)
+                __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(S[d][r]), to.r, srow + 16 * d + r < da ? at : NOWHERE,
+                                                      __builtin_amdgcn_readfirstlane((16 * d + r) * rs * 4), 0);
     }
     if (!STATES && len < L.T) {     // tokens past the sequence's length
         const long long hi = first + L.seg_tokens < L.T ? first + L.seg_tokens : L.T;
@@ -652,26 +658,34 @@ __global__ __launch_bounds__(64 * waves<E>(DAP), 2) void decay_scan_kernel(Decay
 }
 
 // The segments' states from zero become the states that enter them: one thread for an element of a
-// head's state, in place.
+// head's state, in place; eight segments' values are requested at a time.
 __global__ __launch_bounds__(NJ) void decay_join_kernel(DecayLaunch L)
 {
-    const DecayRole& R = L.role[blockIdx.z];
-    const long long size = static_cast<long long>(R.da) * R.db, heads = static_cast<long long>(L.B) * L.H;
-    const long long at = static_cast<long long>(blockIdx.x) * NJ + threadIdx.x, bh = at / size, e = at - bh * size;
+    const DecayRole R = blockIdx.z == 0 ? L.role[0] : blockIdx.z == 1 ? L.role[1] : L.role[2];
+    const unsigned size = static_cast<unsigned>(R.da) * R.db, heads = static_cast<unsigned>(L.B) * L.H;
+    const unsigned at = blockIdx.x * NJ + threadIdx.x, bh = at / size, e = at - bh * size;
     if (bh >= heads) return;
-    const int b = static_cast<int>(bh / L.H), h = static_cast<int>(bh - static_cast<long long>(b) * L.H);
+    const int b = static_cast<int>(bh / static_cast<unsigned>(L.H)), h = static_cast<int>(bh - static_cast<unsigned>(b) * L.H);
     const int len = seq_length(L.lengths, b, L.T);
     const float gl = L.log_decay[h];
-    const long long row = e / R.db, col = e - row * R.db;
-    float s = R.S0 == nullptr ? 0.f : R.S0[bh * size + row * R.s_row + col * R.s_col];
+    const unsigned row = e / R.db, col = e - row * R.db;
+    float s = R.S0 == nullptr ? 0.f : R.S0[bh * static_cast<long long>(size) + row * R.s_row + col * R.s_col];
     const Pow whole = decay_pow(L.seg_tokens, gl);
-    float* p = R.ws + bh * size + e;
-    for (int i = 0; i < L.segments; ++i, p += heads * size) {
-        const long long left = len - static_cast<long long>(i) * L.seg_tokens;
-        const Pow lam = left >= L.seg_tokens ? whole : decay_pow(left < 0 ? 0 : static_cast<int>(left), gl);
-        const float add = i + 1 < L.segments ? *p : 0.f;
-        *p = s;
-        s = __builtin_fmaf(s, lam.hi, __builtin_fmaf(s, lam.lo, add));
+    const long long step = static_cast<long long>(heads) * size;
+    float* p = R.ws + bh * static_cast<long long>(size) + e;
+    constexpr int K = 8;
+    for (int i = 0; i < L.segments; i += K, p += K * step) {
+        float add[K];
+#pragma unroll
+        for (int k = 0; k < K; ++k) add[k] = i + k + 1 < L.segments ? p[k * step] : 0.f;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            if (i + k >= L.segments) break;
+            const long long left = len - static_cast<long long>(i + k) * L.seg_tokens;
+            const Pow lam = left >= L.seg_tokens ? whole : decay_pow(left < 0 ? 0 : static_cast<int>(left), gl);
+            p[k * step] = s;
+            s = __builtin_fmaf(s, lam.hi, __builtin_fmaf(s, lam.lo, add[k]));
+        }
     }
 }
 
@@ -705,15 +719,15 @@ template <typename E, bool STATES, bool EXACT> hipError_t scan_da(const DecayLau
                                                                              : scan<E, 256, STATES, EXACT>(L, groups, st);
 }
 
-// EXACT where every role's channels are whole 16-byte vectors at 4-byte addresses and a block's rows lie within 2^31 bytes: the
-// general kernels' loads and stores by parts, and their 64-bit addresses, cost them registers and instructions
+// EXACT where every role's channels are whole 16-byte vectors at 4-byte addresses: the general kernels' loads and stores by
+// parts, and their 64-bit addresses, cost them registers and instructions
 template <typename E> bool exact(const void* p, const long long (&st)[3], int n)
 {
     constexpr long long ES = sizeof(E);
     if (n % Ops<E>::VE != 0 || reinterpret_cast<uintptr_t>(p) % 4 != 0) return false;
     for (long long s : st)
         if (s * ES % 4 != 0) return false;
-    return st[2] <= ((1LL << 31) - 65536) / (Ops<E>::C * ES);
+    return true;
 }
 template <typename E> hipError_t scan_any(const DecayLaunch& L, int da, unsigned groups, bool states, hipStream_t st)
 {

@@ -206,17 +206,23 @@ bool decay_sizes(int B, int H, int T, int dk, int dv)
     return static_cast<ll>(B) * H * 3 * MAX_D * 8 < (1LL << 32) && T <= INT_MAX - 1024;
 }
 
+// a block's rows (at most 64 tokens) are addressed with 32-bit byte offsets
+bool rows_fit(const ll (&st)[3], int T, ll e) { return T <= 1 || st[2] <= ((1LL << 31) - 65536) / (64 * e); }
+
 // Segments of a sequence: where one workgroup for a head and 64 value columns would leave compute units
 // idle, each head's tokens are cut so that there are about two workgroups for each, in segments of at
 // least 256 tokens (a segment costs its keys and values a second reading).
+#ifndef MIN_SEG
+#define MIN_SEG 256
+#endif
 struct Cut { int tokens, segments; };
 Cut cut_of(ll groups, int T)
 {
     const ll want = 2LL * cus();
-    if (groups >= cus() || T <= 256) return {T > 0 ? T : 1, 1};
+    if (groups >= cus() || T <= MIN_SEG) return {T > 0 ? T : 1, 1};
     const ll segs = (want + groups - 1) / groups;
     ll tokens = (T + segs - 1) / segs;
-    tokens = std::max<ll>(256, (tokens + 63) / 64 * 64);
+    tokens = std::max<ll>(MIN_SEG, (tokens + 63) / 64 * 64);
     return {static_cast<int>(tokens), static_cast<int>((T + tokens - 1) / tokens)};
 }
 
@@ -291,6 +297,7 @@ sfda_status_t sfda_decay_attn_fwd(const void* q, const void* k, const void* v, c
     strides3(R.k_s, strides, 1, H, T, dk);
     strides3(R.v_s, strides, 2, H, T, dv);
     strides3(R.o_s, strides, 3, H, T, dv);
+    if (!rows_fit(R.q_s, T, e) || !rows_fit(R.k_s, T, e) || !rows_fit(R.v_s, T, e) || !rows_fit(R.o_s, T, e)) return SFDA_ERR_SHAPE;
     const size_t need = sfda_decay_attn_fwd_workspace_bytes(B, H, T, dk, dv, dtype);
     const bool cut = need > 0 && workspace != nullptr && workspace_bytes >= need;
     Call c;
@@ -347,6 +354,8 @@ sfda_status_t sfda_decay_attn_bwd(const void* q, const void* k, const void* v, c
     strides3(dqs, strides, 4, H, T, dk);
     strides3(dks, strides, 5, H, T, dk);
     strides3(dvs, strides, 6, H, T, dv);
+    for (const auto* st : {&qs, &ks, &vs, &gs, &dqs, &dks, &dvs})
+        if (!rows_fit(*st, T, e)) return SFDA_ERR_SHAPE;
     const size_t need = sfda_decay_attn_bwd_workspace_bytes(B, H, T, dk, dv, dtype);
     const bool cut = need > 0 && workspace != nullptr && workspace_bytes >= need;
     Call c;
