@@ -209,21 +209,30 @@ bool decay_sizes(int B, int H, int T, int dk, int dv)
 // a block's rows (at most 64 tokens) are addressed with 32-bit byte offsets
 bool rows_fit(const ll (&st)[3], int T, ll e) { return T <= 1 || st[2] <= ((1LL << 31) - 65536) / (64 * e); }
 
-// Segments of a sequence: where one workgroup for a head and 64 value columns would leave compute units
-// idle, each head's tokens are cut so that there are about two workgroups for each, in segments of at
-// least 256 tokens (a segment costs its keys and values a second reading).
-#ifndef MIN_SEG
-#define MIN_SEG 256
-#endif
+// Segments of a sequence.  A scan without them takes c us for 64 tokens, whatever the number of heads, until the workgroups fill the
+// compute units.  Cut into S parts it takes a pass for their states (another s us) and a join, all of them on an S-th of the
+// tokens, with one or two workgroups on each unit.  Estimates in us, d 128 (256 channels take twice that on both sides).
+// Measured, whole / cut: bfloat16 forward 16 heads T 512 22/24, 15 heads T 1003 43/26, 4 heads T 2048 79/24, 32 heads
+// T 2048 80/47; backward 16 heads T 512 23/35, 32 heads T 2048 75/96; float32 forward 4 heads T 512 55/22, 16 heads
+// T 512 58/34, 32 heads T 2048 200/113.
 struct Cut { int tokens, segments; };
-Cut cut_of(ll groups, int T)
+Cut cut_of(ll groups, int T, bool bf16)
 {
-    const ll want = 2LL * cus();
-    if (groups >= cus() || T <= MIN_SEG) return {T > 0 ? T : 1, 1};
-    const ll segs = (want + groups - 1) / groups;
-    ll tokens = (T + segs - 1) / segs;
-    tokens = std::max<ll>(MIN_SEG, (tokens + 63) / 64 * 64);
-    return {static_cast<int>(tokens), static_cast<int>((T + tokens - 1) / tokens)};
+    const double c = bf16 ? 2.4 : 6.2, s = bf16 ? 1.5 : 2.6, shared = bf16 ? 1.6 : 1.35;     // two on a unit: each slower
+    const ll steps = (static_cast<ll>(T) + 63) / 64;
+    Cut best{std::max(T, 1), 1};
+    double least = 0.9 * (steps * c + 5.);
+    for (int on_unit = 1; on_unit <= 2; ++on_unit) {
+        const ll most = on_unit * static_cast<ll>(cus()) / groups;
+        if (most < 2 || steps < 2) continue;
+        const ll each = (steps + most - 1) / most;                  // steps of a segment
+        const double us = each * (c + s) * (on_unit == 2 ? shared : 1.) + 20.;
+        if (us < least) {
+            least = us;
+            best = {static_cast<int>(each * 64), static_cast<int>((steps + each - 1) / each)};
+        }
+    }
+    return best;
 }
 
 }  // namespace
@@ -277,7 +286,7 @@ size_t sfda_decay_attn_fwd_workspace_bytes(int B, int H, int T, int dk, int dv, 
     const ll heads = static_cast<ll>(B) * H;
     const bool bf16 = dtype == SFDA_BF16;
     if (heads == 0) return 0;
-    const Cut c = cut_of(heads * sfda::decay_slices(bf16, dk, dv), T);
+    const Cut c = cut_of(heads * sfda::decay_slices(bf16, dk, dv), T, bf16);
     return c.segments > 1 ? static_cast<size_t>(c.segments) * heads * dk * dv * 4 : 0;
 }
 
@@ -312,7 +321,7 @@ sfda_status_t sfda_decay_attn_fwd(const void* q, const void* k, const void* v, c
     c.output(flat(cut ? workspace : nullptr, static_cast<ll>(need)), 4, false);
     const sfda_status_t st = c.done();
     if (st != SFDA_OK) return st;
-    const Cut segs = cut_of(heads * sfda::decay_slices(bf16, dk, dv), T);
+    const Cut segs = cut_of(heads * sfda::decay_slices(bf16, dk, dv), T, bf16);
     R.q = q; R.k = k; R.v = v; R.o = o; R.S0 = S0; R.S_T = S_T;
     R.da = dk; R.db = dv; R.s_row = dv; R.s_col = 1;
     R.intra = scale; R.inter = scale; R.upd = 1.f;
@@ -332,7 +341,7 @@ size_t sfda_decay_attn_bwd_workspace_bytes(int B, int H, int T, int dk, int dv, 
     const ll heads = static_cast<ll>(B) * H;
     const bool bf16 = dtype == SFDA_BF16;
     if (heads == 0) return 0;
-    const Cut c = cut_of(heads * (2 * sfda::decay_slices(bf16, dv, dk) + sfda::decay_slices(bf16, dk, dv)), T);
+    const Cut c = cut_of(heads * (2 * sfda::decay_slices(bf16, dv, dk) + sfda::decay_slices(bf16, dk, dv)), T, bf16);
     return c.segments > 1 ? 3 * static_cast<size_t>(c.segments) * heads * dk * dv * 4 : 0;
 }
 
@@ -374,7 +383,7 @@ sfda_status_t sfda_decay_attn_bwd(const void* q, const void* k, const void* v, c
     c.output(flat(cut ? workspace : nullptr, static_cast<ll>(need)), 4, false);
     const sfda_status_t st = c.done();
     if (st != SFDA_OK) return st;
-    const Cut segs = cut_of(heads * (2 * sfda::decay_slices(bf16, dv, dk) + sfda::decay_slices(bf16, dk, dv)), T);
+    const Cut segs = cut_of(heads * (2 * sfda::decay_slices(bf16, dv, dk) + sfda::decay_slices(bf16, dk, dv)), T, bf16);
     const int segments = cut ? segs.segments : 1;
     sfda::DecayLaunch L{};
     auto put = [](ll (&to)[3], const ll (&from)[3]) { std::copy(from, from + 3, to); };

@@ -89,7 +89,7 @@ def test_decay_attn_step(lib):
 
 def test_workspaces(lib):
     f = lib.sfda_decay_attn_fwd_workspace_bytes
-    assert f(8, 16, 4096, 128, 128, 1) == 0 and f(1, 1, 256, 128, 128, 0) == 0 and f(1, 1, 0, 8, 8, 0) == 0 and f(0, 1, 5000, 8, 8, 0) == 0
+    assert f(8, 16, 4096, 128, 128, 1) == 0 and f(1, 1, 64, 128, 128, 0) == 0 and f(1, 1, 0, 8, 8, 0) == 0 and f(0, 1, 5000, 8, 8, 0) == 0
     assert f(1, 1, 4096, 128, 128, 0) > 0 and f(1, 1, 4096, 257, 8, 0) == 0 and f(-1, 1, 64, 8, 8, 0) == 0 and f(1, 1, 4096, 8, 8, 2) == 0
     assert lib.sfda_decay_attn_bwd_workspace_bytes(1, 1, 4096, 128, 128, 1) > 0
     g = lib.sfda_group_norm_bwd_workspace_bytes
