@@ -528,6 +528,18 @@ def _rows(t) -> Optional[int]:
     return t.data_ptr()
 
 
+def _fit(*pairs) -> None:
+    """_check of (name, tensor or None, shape) triples; in one pass where everything is as it should be."""
+    index = pairs[0][1].get_device()
+    if index >= 0:
+        for _, t, shape in pairs:
+            if t is not None and (t.shape != shape or t.get_device() != index):
+                break
+        else:
+            return
+    _check({name: (t, shape) for name, t, shape in pairs})
+
+
 def _same_dtype(x, **named) -> int:
     code = _dtype_code(x)
     for name, t in named.items():
@@ -542,6 +554,14 @@ def _int32(name, t) -> None:
         raise TypeError(f"{name} must be int32 (got {t.dtype})")
 
 
+def _strides(outer: int, *tensors):
+    """The strides of the outer axes, tensor after tensor, or None where all of them are contiguous."""
+    for t in tensors:
+        if not t.is_contiguous():
+            return _STRIDES[outer * len(tensors)](*[s for t in tensors for s in t.stride()[:outer]])
+    return None
+
+
 def _empty(shape, dtype, device, stream):
     """An output, from the memory of the stream that writes it."""
     import torch
@@ -551,6 +571,14 @@ def _empty(shape, dtype, device, stream):
         stream = torch.cuda.ExternalStream(stream.cuda_stream, device=device)
     with torch.cuda.stream(stream):
         return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _empty_as(x, shape, stream):
+    """An output of x's type and a shape of its own or x's."""
+    import torch
+    if stream is None and x.shape == shape and x.is_contiguous():
+        return torch.empty_like(x)
+    return _empty(shape, x.dtype, x.device, stream)
 
 
 def rotary_tables(positions: int, rot: int, *, base: float = 10000.0, scaling: Optional[dict] = None, device="cuda"):
@@ -614,26 +642,25 @@ def rotary(q, k, cos, sin, positions=None, *, offset: int = 0, interleaved: bool
     code = _same_dtype(q, k=k, q_out=q_out, k_out=k_out)
     _need_f32(cos=cos, sin=sin)
     P, half = cos.shape
+    tq, tk = (B, Hq, T, D), (B, Hk, T, D)
     if q_out is None:
-        q_out = _empty((B, Hq, T, D), q.dtype, q.device, stream)
+        q_out = _empty_as(q, tq, stream)
     if k is None:
         k_out = None
     elif k_out is None:
-        k_out = _empty((B, Hk, T, D), q.dtype, q.device, stream)
+        k_out = _empty_as(k, tk, stream)
     bits, pstride = 0, 0
     if positions is not None:
         if positions.dtype not in (torch.int32, torch.int64):
             raise TypeError(f"positions must be int32 or int64 (got {positions.dtype})")
         bits = 32 if positions.dtype == torch.int32 else 64
         pstride = positions.stride(0) if positions.dim() == 2 and B > 1 else 0
-    _check(dict(q=(q, (B, Hq, T, D)), k=(k, (B, Hk, T, D)), cos=(cos, (P, half)), sin=(sin, (P, half)),
-                q_out=(q_out, (B, Hq, T, D)), k_out=(k_out, (B, Hk, T, D)),
-                positions=(positions, (T,) if positions is not None and positions.dim() == 1 else (B, T))))
+    _fit(("q", q, tq), ("k", k, tk), ("cos", cos, (P, half)), ("sin", sin, (P, half)), ("q_out", q_out, tq),
+         ("k_out", k_out, tk), ("positions", positions, (T,) if positions is not None and positions.dim() == 1 else (B, T)))
     kk, ko = (q, q_out) if k is None else (k, k_out)
     st = lib.sfda_rotary(_rows(q), _rows(k), _ptr(cos), _ptr(sin), _rows(positions), bits, pstride, offset, _rows(q_out),
                          _rows(k_out), B, Hq, Hk, T, D, 2 * half, P, interleaved, inverse,
-                         _STRIDES[12](*q.stride()[:3], *kk.stride()[:3], *q_out.stride()[:3], *ko.stride()[:3]),
-                         code, _stream(stream))
+                         _strides(3, q, kk, q_out, ko), code, _stream(stream))
     if st != 0:
         raise SfdaError(st, "sfda_rotary")
     return q_out, k_out
@@ -653,22 +680,20 @@ def decay_attn_fwd(q, k, v, log_decay, S0=None, *, scale: float = 1.0, lengths=N
     B, H, T, dk = q.shape
     dv = v.shape[3]
     code = _same_dtype(q, k=k, v=v, o=o)
+    tk, tv, ts = (B, H, T, dk), (B, H, T, dv), (B, H, dk, dv)
     if o is None:
-        o = _empty((B, H, T, dv), q.dtype, q.device, stream)
+        o = _empty_as(v, tv, stream)
     if S_T is None and want_state:
         S_T = _empty((B, H, dk, dv), torch.float32, q.device, stream)
     _need_f32(S0=S0, S_T=S_T, log_decay=log_decay)
     _int32("lengths", lengths)
-    _check(dict(q=(q, (B, H, T, dk)), k=(k, (B, H, T, dk)), v=(v, (B, H, T, dv)), log_decay=(log_decay, (H,)),
-                lengths=(lengths, (B,)), S0=(S0, (B, H, dk, dv)), o=(o, (B, H, T, dv)), S_T=(S_T, (B, H, dk, dv)),
-                workspace=(workspace, tuple(workspace.shape) if workspace is not None else ())))
+    _fit(("q", q, tk), ("k", k, tk), ("v", v, tv), ("log_decay", log_decay, (H,)), ("lengths", lengths, (B,)), ("S0", S0, ts),
+         ("o", o, tv), ("S_T", S_T, ts), ("workspace", workspace, workspace.shape if workspace is not None else ()))
     if workspace is None:
         nws = lib.sfda_decay_attn_fwd_workspace_bytes(B, H, T, dk, dv, code)
         workspace = _try_workspace(nws, q.device, stream) if nws else None
     st = lib.sfda_decay_attn_fwd(_rows(q), _rows(k), _rows(v), _ptr(log_decay), _ptr(lengths), _ptr(S0), _rows(o), _ptr(S_T),
-                                 B, H, T, dk, dv, scale,
-                                 _STRIDES[12](*q.stride()[:3], *k.stride()[:3], *v.stride()[:3], *o.stride()[:3]),
-                                 code, _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
+                                 B, H, T, dk, dv, scale, _strides(3, q, k, v, o), code, _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
                                  _stream(stream))
     if st != 0:
         raise SfdaError(st, "sfda_decay_attn_fwd")
@@ -687,21 +712,20 @@ def decay_attn_bwd(q, k, v, log_decay, S0, dO, dS_T=None, *, scale: float = 1.0,
     B, H, T, nk = q.shape
     nv = v.shape[3]
     code = _same_dtype(q, k=k, v=v, dO=dO, dq=dq, dk=dk, dv=dv)
-    dq = _empty((B, H, T, nk), q.dtype, q.device, stream) if dq is None else dq
-    dk = _empty((B, H, T, nk), q.dtype, q.device, stream) if dk is None else dk
-    dv = _empty((B, H, T, nv), q.dtype, q.device, stream) if dv is None else dv
+    tk, tv, ts = (B, H, T, nk), (B, H, T, nv), (B, H, nk, nv)
+    dq = _empty_as(q, tk, stream) if dq is None else dq
+    dk = _empty_as(k, tk, stream) if dk is None else dk
+    dv = _empty_as(v, tv, stream) if dv is None else dv
     dS0 = _empty((B, H, nk, nv), torch.float32, q.device, stream) if want_dS0 else None
     _need_f32(S0=S0, dS_T=dS_T, log_decay=log_decay)
     _int32("lengths", lengths)
-    tk, tv, ts = (B, H, T, nk), (B, H, T, nv), (B, H, nk, nv)
-    _check(dict(q=(q, tk), k=(k, tk), v=(v, tv), log_decay=(log_decay, (H,)), lengths=(lengths, (B,)), S0=(S0, ts),
-                dO=(dO, tv), dS_T=(dS_T, ts), dq=(dq, tk), dk=(dk, tk), dv=(dv, tv),
-                workspace=(workspace, tuple(workspace.shape) if workspace is not None else ())))
+    _fit(("q", q, tk), ("k", k, tk), ("v", v, tv), ("log_decay", log_decay, (H,)), ("lengths", lengths, (B,)), ("S0", S0, ts),
+         ("dO", dO, tv), ("dS_T", dS_T, ts), ("dq", dq, tk), ("dk", dk, tk), ("dv", dv, tv),
+         ("workspace", workspace, workspace.shape if workspace is not None else ()))
     if workspace is None:
         nws = lib.sfda_decay_attn_bwd_workspace_bytes(B, H, T, nk, nv, code)
         workspace = _try_workspace(nws, q.device, stream) if nws else None
-    strides = _STRIDES[21](*q.stride()[:3], *k.stride()[:3], *v.stride()[:3], *dO.stride()[:3], *dq.stride()[:3],
-                                       *dk.stride()[:3], *dv.stride()[:3])
+    strides = _strides(3, q, k, v, dO, dq, dk, dv)
     st = lib.sfda_decay_attn_bwd(_rows(q), _rows(k), _rows(v), _ptr(log_decay), _ptr(lengths), _ptr(S0), _rows(dO), _ptr(dS_T),
                                  _rows(dq), _rows(dk), _rows(dv), _ptr(dS0), B, H, T, nk, nv, scale, strides, code,
                                  _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
@@ -732,14 +756,13 @@ def decay_attn_step(q, k, v, log_decay, S, *, scale: float = 1.0, o=None, stream
     B, H, dk = q.shape
     dv = v.shape[2]
     code = _same_dtype(q, k=k, v=v, o=o)
+    tk, tv = (B, H, dk), (B, H, dv)
     if o is None:
-        o = _empty((B, H, dv), q.dtype, q.device, stream)
+        o = _empty_as(v, tv, stream)
     _need_f32(S=S, log_decay=log_decay)
-    _check(dict(q=(q, (B, H, dk)), k=(k, (B, H, dk)), v=(v, (B, H, dv)), log_decay=(log_decay, (H,)),
-                S=(S, (B, H, dk, dv)), o=(o, (B, H, dv))))
+    _fit(("q", q, tk), ("k", k, tk), ("v", v, tv), ("log_decay", log_decay, (H,)), ("S", S, (B, H, dk, dv)), ("o", o, tv))
     st = lib.sfda_decay_attn_step(_rows(q), _rows(k), _rows(v), _ptr(log_decay), _ptr(S), _rows(o), B, H, dk, dv, scale,
-                                  _STRIDES[8](*q.stride()[:2], *k.stride()[:2], *v.stride()[:2], *o.stride()[:2]),
-                                  code, _stream(stream))
+                                  _strides(2, q, k, v, o), code, _stream(stream))
     if st != 0:
         raise SfdaError(st, "sfda_decay_attn_step")
     return o
@@ -760,8 +783,8 @@ def group_norm(x, weight=None, bias=None, gate=None, *, activation: str = "none"
     if y is None:
         y = _empty((B, T, H * D), x.dtype, x.device, stream)
     _need_f32(weight=weight, bias=bias)
-    _check(dict(x=(x, (B, H, T, D)), weight=(weight, (H * D,)), bias=(bias, (H * D,)), gate=(gate, (B, T, H * D)),
-                y=(y, (B, T, H * D))))
+    tc, w = (B, T, H * D), (H * D,)
+    _fit(("x", x, (B, H, T, D)), ("weight", weight, w), ("bias", bias, w), ("gate", gate, tc), ("y", y, tc))
     g = y if gate is None else gate
     st = lib.sfda_group_norm(_rows(x), _ptr(weight), _ptr(bias), _rows(gate), _rows(y), B, H, T, D, _ACT[activation], eps,
                              _STRIDES[7](*x.stride()[:3], *g.stride()[:2], *y.stride()[:2]), code, _stream(stream))
@@ -793,8 +816,8 @@ def group_norm_bwd(dy, x, weight=None, bias=None, gate=None, *, activation: str 
     dbias = None if bias is None else _empty((H * D,), torch.float32, x.device, stream)
     _need_f32(weight=weight, bias=bias)
     tc, w = (B, T, H * D), (H * D,)
-    _check(dict(x=(x, (B, H, T, D)), dy=(dy, tc), weight=(weight, w), bias=(bias, w), gate=(gate, tc), dx=(dx, (B, H, T, D)),
-                dgate=(dgate, tc), workspace=(workspace, tuple(workspace.shape) if workspace is not None else ())))
+    _fit(("x", x, (B, H, T, D)), ("dy", dy, tc), ("weight", weight, w), ("bias", bias, w), ("gate", gate, tc), ("dx", dx, (B, H, T, D)),
+         ("dgate", dgate, tc), ("workspace", workspace, workspace.shape if workspace is not None else ()))
     if workspace is None and (dweight is not None or dbias is not None):
         workspace = _workspace(lib.sfda_group_norm_bwd_workspace_bytes(B, H, T, D, code), x.device, stream)
     g, dg = (dy, dy) if gate is None else (gate, dgate)
