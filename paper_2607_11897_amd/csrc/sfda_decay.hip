@@ -59,48 +59,62 @@ __device__ __forceinline__ uint32_t pack2(float a, float b)
 __device__ __forceinline__ float lo_f32(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float hi_f32(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 
-// What the element type decides.  C: tokens of a block; VE: elements of a 16-byte vector; KB: the
-// contraction length of one operand fragment; KP, SP, VP: elements that rows of keys, of the state and of values in LDS are
-// longer than their channels, so that what a read takes at a time lies on different banks (bfloat16: 4 token rows of 32
-// bytes for the transposing read of keys, 8 rows of 16 bytes for the state, 4 rows of 64 bytes, every other
-// 8 of them, for values).
-// Lane l of a fragment has index c = l % 16 of the free axis and KB / 4 places of the contraction for its
-// group g = l / 16.  Sums over channels take VE neighbours (rows: one 16-byte read); sums over tokens take
+// What the element type decides.  The matrix cores take bfloat16 operands.  A float32 is the sum of three bfloat16 (its 24 bits,
+// 8 in each), so float32 tensors lie in LDS as PL = 3 planes, and a product of two operands is the six products of parts
+// that reach 2^-21 of it (the three left out are below that): 6 x 16 cycles for 16 x 16 x 32 on a SIMD, where the float32 matrix
+// instruction takes 256.  Forward B8 H16 T2048 d 128: 215 us against 301 with float32 instructions, backward 617 and 868; the LDS
+// reads, the matrix instructions and the splitting of operands then take about a third of a block's time each.
+// An infinity in float32 comes out as NaN where it is used (its parts are inf - inf).
+//   VE: elements of a 16-byte vector;  KB: the contraction length of one operand fragment, 8 places in a lane;  KP, SP:
+// elements that rows of keys and of the state in LDS are longer than their channels, so that what a read takes at a time
+// lies on different banks (4 token rows of 32 bytes for the transposing read of keys, 8 rows of 16 bytes for the state).
+// Lane l of a fragment has index c = l % 16 of the free axis and 8 places of the contraction for its
+// group g = l / 16.  Sums over channels take 8 neighbours (rows: one 16-byte read); sums over tokens take
 // the places 4 g .. 4 g + 3 of each 16, which is what an accumulator tile holds of its rows, so that scores become
 // an operand without leaving their lane.
+constexpr int KB = 32, KP = 16, SP = 8;
+
+// row-major [free][contraction]
+__device__ __forceinline__ bf16x8 plane_rows(const uint16_t* p) { return __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(p)); }
+// row-major [contraction][free]: the transposing LDS read takes, from each group of 16 lanes,
+// 4 rows of 16 (lane l: row l / 4, 4 elements) and gives lane l column l.  p: the lane's own 4 elements in
+// row 4 g + c / 4
+__device__ __forceinline__ bf16x8 plane_cols(const uint16_t* p, int stride)
+{
+    typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+    const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p));
+    const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 16 * stride));
+    u32x4 w;
+    w.lo = __builtin_bit_cast(u32x2, a);
+    w.hi = __builtin_bit_cast(u32x2, b);
+    return __builtin_bit_cast(bf16x8, w);
+}
+// offset of the lane's own elements for plane_cols: 4 of column block c % 4 whose blocks are `step` apart
+__device__ __forceinline__ int cols_at(int stride, int step, int c, int g) { return (4 * g + (c >> 2)) * stride + step * (c & 3); }
+__device__ __forceinline__ void mfma(f32x4& d, bf16x8 a, bf16x8 b) { d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, d, 0, 0, 0); }
+
 template <typename E> struct Ops;
 
 template <> struct Ops<uint16_t> {
-    static constexpr int C = 64, VE = 8, KB = 32, KP = 16, SP = 8, VP = 32;
+    static constexpr int VE = 8, PL = 1, QV = 1;        // QV: vectors of a fragment
     typedef bf16x8 Frag;
-    // row-major [free][contraction]
-    static __device__ __forceinline__ Frag rows(const uint16_t* p) { return __builtin_bit_cast(Frag, *reinterpret_cast<const u32x4*>(p)); }
-    // row-major [contraction][free]: the transposing LDS read takes, from each group of 16 lanes,
-    // 4 rows of 16 (lane l: row l / 4, 4 elements) and gives lane l column l.  p: the lane's own 4 elements in
-    // row 4 g + c / 4
-    static __device__ __forceinline__ Frag cols(const uint16_t* p, int stride)
-    {
-        typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-        const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p));
-        const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 16 * stride));
-        u32x4 w;
-        w.lo = __builtin_bit_cast(u32x2, a);
-        w.hi = __builtin_bit_cast(u32x2, b);
-        return __builtin_bit_cast(Frag, w);
-    }
-    // offset of the lane's own elements for cols: 4 of column block c % 4 whose blocks are `step` apart
-    static __device__ __forceinline__ int cols_at(int stride, int step, int c, int g) { return (4 * g + (c >> 2)) * stride + step * (c & 3); }
+    static __device__ __forceinline__ Frag rows(const uint16_t* p, int) { return plane_rows(p); }
+    static __device__ __forceinline__ Frag cols(const uint16_t* p, int stride, int) { return plane_cols(p, stride); }
+    static __device__ __forceinline__ Frag frag(const u32x4* v) { return __builtin_bit_cast(Frag, v[0]); }
     // from the accumulator tiles t[0], t[1] whose rows are the contraction
     static __device__ __forceinline__ Frag acc(const f32x4* t)
     {
         u32x4 w = {pack2(t[0][0], t[0][1]), pack2(t[0][2], t[0][3]), pack2(t[1][0], t[1][1]), pack2(t[1][2], t[1][3])};
         return __builtin_bit_cast(Frag, w);
     }
-    static __device__ __forceinline__ void mma(f32x4& d, const Frag& a, const Frag& b)
+    static constexpr int PAIRS = 1;
+    static __device__ __forceinline__ void mma(int, f32x4& d, const Frag& a, const Frag& b) { mfma(d, a, b); }
+    static __device__ __forceinline__ void put4(uint16_t* to, int, const f32x4& x)
     {
-        d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, d, 0, 0, 0);
+        *reinterpret_cast<u32x2*>(to) = u32x2{pack2(x[0], x[1]), pack2(x[2], x[3])};
     }
-    static __device__ __forceinline__ u32x2 pack4(const f32x4& x) { return u32x2{pack2(x[0], x[1]), pack2(x[2], x[3])}; }
+    static __device__ __forceinline__ void put(uint16_t* to, int, u32x4 w) { *reinterpret_cast<u32x4*>(to) = w; }
+    static __device__ __forceinline__ void put1(uint16_t* to, int, u32x4 w, int i) { *to = static_cast<uint16_t>(w[i / 2] >> (i % 2 * 16)); }
     static __device__ __forceinline__ u32x4 pack8(const f32x4& x, const f32x4& y)
     {
         return u32x4{pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(y[0], y[1]), pack2(y[2], y[3])};
@@ -130,24 +144,92 @@ template <> struct Ops<uint16_t> {
 };
 
 template <> struct Ops<float> {
-    static constexpr int C = 32, VE = 4, KB = 16, KP = 4, SP = 4, VP = 4;
-    typedef f32x4 Frag;
-    static __device__ __forceinline__ Frag rows(const float* p) { return *reinterpret_cast<const Frag*>(p); }
-    static __device__ __forceinline__ Frag cols(const float* p, int stride) { return Frag{p[0], p[stride], p[2 * stride], p[3 * stride]}; }
-    static __device__ __forceinline__ int cols_at(int stride, int step, int c, int g) { return 4 * g * stride + step * (c >> 2) + (c & 3); }
-    static __device__ __forceinline__ Frag acc(const f32x4* t) { return t[0]; }
-    static __device__ __forceinline__ void mma(f32x4& d, const Frag& a, const Frag& b)
+    static constexpr int VE = 4, PL = 3, QV = 2;
+    struct Frag { bf16x8 p[3]; };
+    // a pair as parts: the upper halves of the words (8 bits of each; truncated, so that nothing overflows), then of what is left,
+    // which is exact, twice
+    static __device__ __forceinline__ void split(uint32_t (&p)[3], float a, float b)
     {
 #pragma unroll
-        for (int s = 0; s < 4; ++s) d = __builtin_amdgcn_mfma_f32_16x16x4f32(a[s], b[s], d, 0, 0, 0);
+        for (int s = 0; s < 3; ++s) {
+            p[s] = __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302);
+            if (s < 2) {
+                a -= hi_f32(__float_as_uint(a));
+                b -= hi_f32(__float_as_uint(b));
+            }
+        }
     }
-    static __device__ __forceinline__ f32x4 pack4(const f32x4& x) { return x; }
+    static __device__ __forceinline__ Frag split8(const float (&x)[8])
+    {
+        u32x4 w[3];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            uint32_t p[3];
+            split(p, x[2 * e], x[2 * e + 1]);
+#pragma unroll
+            for (int s = 0; s < 3; ++s) w[s][e] = p[s];
+        }
+        return Frag{{__builtin_bit_cast(bf16x8, w[0]), __builtin_bit_cast(bf16x8, w[1]), __builtin_bit_cast(bf16x8, w[2])}};
+    }
+    static __device__ __forceinline__ Frag rows(const uint16_t* p, int plane)
+    {
+        return Frag{{plane_rows(p), plane_rows(p + plane), plane_rows(p + 2 * plane)}};
+    }
+    static __device__ __forceinline__ Frag cols(const uint16_t* p, int stride, int plane)
+    {
+        return Frag{{plane_cols(p, stride), plane_cols(p + plane, stride), plane_cols(p + 2 * plane, stride)}};
+    }
+    static __device__ __forceinline__ Frag frag(const u32x4* v)
+    {
+        float x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(v[i / 4][i % 4]);
+        return split8(x);
+    }
+    static __device__ __forceinline__ Frag acc(const f32x4* t)
+    {
+        const float x[8] = {t[0][0], t[0][1], t[0][2], t[0][3], t[1][0], t[1][1], t[1][2], t[1][3]};
+        return split8(x);
+    }
+    // pair i of a product's parts, the small ones first: a loop over tiles inside one over pairs has no product wait for the last
+    static constexpr int PAIRS = 6;
+    static __device__ __forceinline__ void mma(int i, f32x4& d, const Frag& a, const Frag& b)
+    {
+        constexpr int A[PAIRS] = {2, 0, 1, 1, 0, 0}, B[PAIRS] = {0, 2, 1, 0, 1, 0};
+        mfma(d, a.p[A[i]], b.p[B[i]]);
+    }
+    static __device__ __forceinline__ void put4(uint16_t* to, int plane, const f32x4& x)
+    {
+        uint32_t a[3], b[3];
+        split(a, x[0], x[1]);
+        split(b, x[2], x[3]);
+#pragma unroll
+        for (int s = 0; s < 3; ++s) *reinterpret_cast<u32x2*>(to + s * plane) = u32x2{a[s], b[s]};
+    }
+    static __device__ __forceinline__ void put(uint16_t* to, int plane, u32x4 w) { put4(to, plane, __builtin_bit_cast(f32x4, w)); }
+    static __device__ __forceinline__ void put1(uint16_t* to, int plane, u32x4 w, int i)
+    {
+        uint32_t p[3];
+        split(p, __uint_as_float(w[i]), 0.f);
+#pragma unroll
+        for (int s = 0; s < 3; ++s) to[s * plane] = static_cast<uint16_t>(p[s]);
+    }
     static __device__ __forceinline__ void store1(float* p, float x) { *p = x; }
     static constexpr int PARTS = 1;
-    static __device__ __forceinline__ void weighted(Frag (&out)[PARTS], const Frag& v, const float (&w)[4])
+    static __device__ __forceinline__ void weighted(Frag (&out)[PARTS], const Frag& v, const float (&w)[8])
     {
+        float x[8];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) out[0][e] = v[e] * w[e];
+        for (int i = 0; i < 8; ++i) {
+            float f[3];
+#pragma unroll
+            for (int s = 0; s < 3; ++s) {
+                const uint32_t u = __builtin_bit_cast(u32x4, v.p[s])[i / 2];
+                f[s] = i & 1 ? hi_f32(u) : lo_f32(u);
+            }
+            x[i] = (f[0] + (f[1] + f[2])) * w[i];       // (the sum is the float32 that was taken apart)
+        }
+        out[0] = split8(x);
     }
 };
 
@@ -213,7 +295,7 @@ template <> struct From<true> {
 // the `before` channels that the row has before these, where they are few; the write then goes by elements), and rows
 // shorter than a vector are read by elements.
 template <typename E, int NT, int ROWS, int COLS, int STRIDE, bool EXACT> struct Tile {
-    static constexpr int VE = Ops<E>::VE, VPR = COLS / VE, RPP = NT / VPR, N = ROWS / RPP;
+    static constexpr int VE = Ops<E>::VE, VPR = COLS / VE, RPP = NT / VPR, N = ROWS / RPP, PLANE = ROWS * STRIDE;
     static_assert(ROWS % RPP == 0 && NT % VPR == 0, "whole passes");
     u32x4 x[N];
     uint32_t off, step;     // a whole block's first vector in memory order, and from a pass to the next
@@ -253,7 +335,7 @@ template <typename E, int NT, int ROWS, int COLS, int STRIDE, bool EXACT> struct
         for (int u = 0; u < N; ++u) x[u] = one(from, R.offset(tid / VPR + u * RPP, pad, ROWS - pad) + at(cols, tid), 0, cols, tid);
     }
     // rows before `pad` are zero
-    template <bool WHOLE> __device__ __forceinline__ void store(E* lds, int cols, int pad, int tid) const
+    template <bool WHOLE> __device__ __forceinline__ void store(uint16_t* lds, int cols, int pad, int tid) const
     {
         int col = (tid % VPR) * VE;
         if (EXACT) col = col < cols ? col : 0;      // (padding lanes hold channel 0's vector, and write it once more)
@@ -264,14 +346,11 @@ template <typename E, int NT, int ROWS, int COLS, int STRIDE, bool EXACT> struct
             const u32x4 z = {0, 0, 0, 0};
             const u32x4 w = WHOLE || r >= pad ? x[u] : z;
             if (EXACT || col + VE <= cols || few) {
-                *reinterpret_cast<u32x4*>(lds + r * STRIDE + col) = w;
+                Ops<E>::put(lds + r * STRIDE + col, PLANE, w);
             } else {
 #pragma unroll
-                for (int i = 0; i < VE; ++i) {
-                    constexpr int PER = 4 / static_cast<int>(sizeof(E));
-                    const uint32_t e = w[i / PER] >> (i % PER * 16);
-                    if (cols - VE + i >= 0) memcpy(lds + r * STRIDE + cols - VE + i, &e, sizeof(E));
-                }
+                for (int i = 0; i < VE; ++i)
+                    if (cols - VE + i >= 0) Ops<E>::put1(lds + r * STRIDE + cols - VE + i, PLANE, w, i);
             }
         }
     }
@@ -312,26 +391,34 @@ template <typename E, bool EXACT> __device__ __forceinline__ u32x4 row_place(u32
     return u32x4{static_cast<uint32_t>(lo), static_cast<uint32_t>(lo >> 32), static_cast<uint32_t>(hi), static_cast<uint32_t>(hi >> 32)};
 }
 
-// A scan workgroup's value columns and waves, for the type and the (padded) channels of the state.
-//  * bfloat16: 64 columns; four waves (one on a SIMD) form no scores and no weighted values twice, eight hide more latency and have
+// A scan workgroup, for the type and the (padded) channels of the state: C tokens of a block, NS value columns, NW waves, KVB
+// buffers of keys and values, VP elements that a row of values in LDS is longer (4 rows of 64 bytes, every other 8 of
+// them, or of 32 bytes, on different banks).
+//  * bfloat16: four waves (one on a SIMD) form no scores and no weighted values twice, eight hide more latency and have
 //    half the registers' worth of work each.  Forward B8 H16 T4096 d 128: 161 us with four, 182 with eight (and 197 with
 //    32 columns); with 256 channels four do not have the registers.
-//  * float32: 32 columns and four waves where two such workgroups share a compute unit (their LDS): forward B4 H8 T2048 d 128
-//    122 us, with 64 columns and eight waves 134.
-template <typename E> constexpr int waves(int dap) { return dap <= 128 ? 4 : 8; }
-template <typename E> constexpr int slice(int dap) { return decay_slice(sizeof(E) == 2, dap); }
-
-// LDS of a scan: the keys and values of a block and of the next, the state as an operand ([column][channel]; twice with SB 2, so
-// that a block needs one barrier), and the powers of lambda
-template <typename E, int DAP, int SB> struct Smem {
-    typedef Ops<E> O;
-    static constexpr int NS = slice<E>(DAP);
-    static constexpr int C = O::C, SK = DAP + O::KP, SV = NS + O::VP, SS = DAP + O::SP, KV = C * (SK + SV), ST = NS * SS;
-    E k[2][C * SK], v[2][C * SV], s[SB][ST];
-    float pw[C + 1];
+//  * float32: three planes fill LDS, so that there is one buffer of them and one workgroup on a compute unit; with 256 channels
+//    half the block and half the columns.  Four waves with the registers of all (forward B8 H16 T2048 d 128: 215 us, 234 with eight;
+//    backward 617 and 667), but eight where rows are not whole vectors, whose address arithmetic they hide (B3 H5
+//    T1003 keys of 88, values of 74: 44 us and 53 with four).
+template <typename E, int DAP, bool EXACT> struct Shape {
+    static constexpr bool HALF = sizeof(E) == 4 && DAP > 128;
+    static constexpr int C = HALF ? 32 : 64, NS = decay_slice(sizeof(E) == 2, DAP), NW = (sizeof(E) == 2 ? DAP > 128 : DAP <= 128 && !EXACT) ? 8 : 4;
+    static constexpr int KVB = sizeof(E) == 2 ? 2 : 1, VP = NS == 64 ? 32 : 16;
+    static constexpr int PER = sizeof(E) == 2 ? 2 : 1;      // workgroups that registers have to allow on a compute unit
 };
 
-// One workgroup scans the tokens of one segment of one head for 64 value columns of one role.  For a block, a wave
+// LDS of a scan: the keys and values of a block (and of the next), the state as an operand ([column][channel]; twice with SB 2, so
+// that a block needs one barrier), and the powers of lambda
+template <typename E, int DAP, int SB> struct Smem {
+    typedef Shape<E, DAP, true> Sh;
+    static constexpr int PL = Ops<E>::PL, SK = DAP + KP, SV = Sh::NS + Sh::VP, SS = DAP + SP;
+    static constexpr int KPL = Sh::C * SK, VPL = Sh::C * SV, SPL = Sh::NS * SS;         // planes
+    uint16_t k[Sh::KVB][PL * KPL], v[Sh::KVB][PL * VPL], s[SB][PL * SPL];
+    float pw[Sh::C + 1];
+};
+
+// One workgroup scans the tokens of one segment of one head for NS value columns of one role.  For a block, a wave
 // forms the outputs of one row tile (16 of the block's tokens) for 16 NP columns: scores against the keys of earlier
 // tiles and its own, kept in registers as the operand of the product with the values, and the queries (which no
 // other row tile needs: from global memory straight into fragments) times the state.  Then it updates its share of
@@ -345,9 +432,11 @@ __device__ __forceinline__ void decay_scan(const DecayLaunch& L, const DecayRole
     typedef Ops<E> O;
     typedef typename O::Frag Frag;
     typedef Smem<E, DAP, SB> Mem;
-    constexpr int NW = waves<E>(DAP), NS = Mem::NS, NT = 64 * NW, C = O::C, KB = O::KB, VE = O::VE, CT = C / 16, CG = NW / CT, NP = NS / 16 / CG;
-    constexpr int DT = DAP / 16, DTW = DT * NP / CT, DF = DAP / KB, CF = C / KB, TPF = KB / 16, ES = sizeof(E);
-    constexpr int SK = Mem::SK, SV = Mem::SV, SS = Mem::SS;
+    typedef Shape<E, DAP, EXACT> Sh;
+    constexpr int NW = Sh::NW, NS = Sh::NS, NT = 64 * NW, C = Sh::C, VE = O::VE, CT = C / 16, CG = NW / CT, NP = NS / 16 / CG;
+    constexpr int DT = DAP / 16, DTW = DT * NP / CT, DF = DAP / KB, CF = C / KB, TPF = KB / 16, ES = sizeof(E), QV = O::QV;
+    constexpr int SK = Mem::SK, SV = Mem::SV, SS = Mem::SS, KPL = Mem::KPL, VPL = Mem::VPL, SPL = Mem::SPL;
+    constexpr bool WIDE = O::PL > 1, ONE = Sh::KVB == 1;
     static_assert(NP * CG * 16 == NS && CT % NP == 0, "tiles");
     Mem& M = *reinterpret_cast<Mem*>(smem);
 
@@ -371,7 +460,7 @@ __device__ __forceinline__ void decay_scan(const DecayLaunch& L, const DecayRole
 
     Tile<E, NT, C, DAP, SK, EXACT> tk;
     Tile<E, NT, C, NS, SV, EXACT> tv;
-    u32x4 qn[DF];
+    u32x4 qn[DF * QV];
     // blocks end where the segment ends; the first one has `pad` rows too many
     const int pad = begin < end ? (C - (end - begin) % C) % C : 0;
     tk.place(kr, da, 0, tid);
@@ -379,7 +468,10 @@ __device__ __forceinline__ void decay_scan(const DecayLaunch& L, const DecayRole
     auto load_queries = [&](const char* base, uint32_t row) {
         const From<EXACT> from(base);
 #pragma unroll
-        for (int f = 0; f < DF; ++f) qn[f] = row_load<E, EXACT>(from, row + row_at<E, EXACT>(KB * f + VE * g, da), KB * f + VE * g, da);
+        for (int i = 0; i < DF * QV; ++i) {
+            const int col = KB * (i / QV) + 8 * g + VE * (i % QV);
+            qn[i] = row_load<E, EXACT>(from, row + row_at<E, EXACT>(col, da), col, da);
+        }
     };
     if (begin < end) {
         tk.load_first(kr, begin, pad, da, tid);
@@ -432,7 +524,7 @@ __device__ __forceinline__ void decay_scan(const DecayLaunch& L, const DecayRole
     __syncthreads();
 
     // weights that are the same for every whole block: of the scores, of the start state's rows, of the values
-    float wd[CT][4], wv[CF][KB / 4];
+    float wd[CT][4], wv[CF][8];
 #pragma unroll
     for (int t = 0; t < CT; ++t)
 #pragma unroll
@@ -444,7 +536,7 @@ __device__ __forceinline__ void decay_scan(const DecayLaunch& L, const DecayRole
 #pragma unroll
     for (int f = 0; f < CF; ++f)
 #pragma unroll
-        for (int e = 0; e < KB / 4; ++e)
+        for (int e = 0; e < 8; ++e)
             wv[f][e] = upd * M.pw[C - 1 - (KB * f + 16 * (e / 4) + 4 * g + (e & 3)) + (reverse ? 1 : 0)];
     // the first block's decays of the state that enters it are those of its tokens
     const int after = 16 * RT + c + (reverse ? 0 : 1);
@@ -456,13 +548,10 @@ __device__ __forceinline__ void decay_scan(const DecayLaunch& L, const DecayRole
     int low = pad;                  // first row with a token
     const uint32_t ooff = orow.offset(16 * RT + c, 0, C);
 
-    // the state, rounded to the element type, as the operand of its product with the queries
-    auto state_out = [&](E* to) {
+    // the state, rounded to the element type (bfloat16), as the operand of its product with the queries
+    auto state_out = [&](uint16_t* to) {
 #pragma unroll
-        for (int d = 0; d < DTW; ++d) {
-            const auto x = O::pack4(S[d]);
-            *reinterpret_cast<std::remove_const_t<decltype(x)>*>(to + scol * SS + srow + 16 * d) = x;
-        }
+        for (int d = 0; d < DTW; ++d) O::put4(to + scol * SS + srow + 16 * d, SPL, S[d]);
     };
     if (begin < end) {
         tk.template store<false>(M.k[0], da, pad, tid);
@@ -479,47 +568,80 @@ __device__ __forceinline__ void decay_scan(const DecayLaunch& L, const DecayRole
 #pragma clang loop unroll(disable)
         for (int at = begin - pad; at < end; at += C, buf ^= 1) {
             const int next = at + C;
-            const E *K = M.k[buf], *V = M.v[buf], *SL = M.s[SB == 2 ? buf : 0];
-            Frag qf[DF];
-            if (!STATES) {
+            const uint16_t *K = M.k[ONE ? 0 : buf], *V = M.v[ONE ? 0 : buf], *SL = M.s[SB == 2 ? buf : 0];
+            // the block's queries as fragments (float32: where they are used, so that the next block's are not requested before)
+            auto query = [&](int f) {
+                u32x4 v[QV];
 #pragma unroll
-                for (int f = 0; f < DF; ++f) qf[f] = __builtin_bit_cast(Frag, row_place<E, EXACT>(qn[f], KB * f + VE * g, da));
+                for (int i = 0; i < QV; ++i) v[i] = row_place<E, EXACT>(qn[QV * f + i], KB * f + 8 * g + VE * i, da);
+                return O::frag(v);
+            };
+            Frag qf[WIDE ? 1 : DF];
+            if (!STATES && !WIDE) {
+#pragma unroll
+                for (int f = 0; f < DF; ++f) qf[f] = query(f);
             }
             if (next < end) {
                 kbase += kr.st * C;
                 vbase += vr.st * C;
+                qbase += qr.st * C;
                 tk.load(kbase, reverse, da, tid);
                 tv.load(vbase, reverse, dbs, tid);
-                if (!STATES) {
-                    qbase += qr.st * C;
-                    load_queries(qbase, qoff);
-                }
+                if (!STATES && !WIDE) load_queries(qbase, qoff);
             }
+            auto values = [&](int f, int p) {
+                return O::cols(V + KB * f * SV + 16 * NP * cg + col_of(p) + cols_at(SV, NP == 1 ? 4 : 8, c, g), SV, VPL);
+            };
             Frag vf[CF][NP];
+            if (!WIDE) {
 #pragma unroll
-            for (int f = 0; f < CF; ++f)
+                for (int f = 0; f < CF; ++f)
 #pragma unroll
-                for (int p = 0; p < NP; ++p)
-                    if ((!STATES && TPF * f <= RT) || p == sp)
-                        vf[f][p] = O::cols(V + KB * f * SV + 16 * NP * cg + col_of(p) + O::cols_at(SV, NP == 1 ? 4 : 8, c, g), SV);
+                    for (int p = 0; p < NP; ++p)
+                        if ((!STATES && TPF * f <= RT) || p == sp) vf[f][p] = values(f, p);
+            }
             if (!STATES) {
                 // outputs, transposed: rows are columns of v, columns are tokens
                 f32x4 x[NP];
 #pragma unroll
                 for (int p = 0; p < NP; ++p) x[p] = zero4();
+                // scores, transposed: rows are keys; rounded once to the element type (bfloat16), as the operand of the product
+                // with v
+                constexpr int ST = TPF * ((RT + TPF) / TPF);
+                f32x4 sc[ST];
 #pragma unroll
-                for (int f = 0; f < DF; ++f)
+                for (int t = 0; t < ST; ++t) sc[t] = zero4();
+                auto states = [&](int f, int p) { return O::rows(SL + (col0 + col_of(p)) * SS + KB * f + 8 * g, SPL); };
+                auto key_rows = [&](int f, int t) { return O::rows(K + (16 * t + c) * SK + KB * f + 8 * g, KPL); };
+                if constexpr (WIDE) {
 #pragma unroll
-                    for (int p = 0; p < NP; ++p) O::mma(x[p], O::rows(SL + (col0 + col_of(p)) * SS + KB * f + VE * g), qf[f]);
-                __builtin_amdgcn_sched_barrier(0);     // (phases kept apart: mixed, they measure 2 to 5% more)
-                // scores, transposed: rows are keys; rounded once to the element type, as the operand of the product with v
-                f32x4 sc[TPF * ((RT + TPF) / TPF)];
+                    for (int f = 0; f < DF; ++f) {
+                        Frag sf[NP], kf[RT + 1];
 #pragma unroll
-                for (int t = 0; t < TPF * ((RT + TPF) / TPF); ++t) sc[t] = zero4();
+                        for (int p = 0; p < NP; ++p) sf[p] = states(f, p);
 #pragma unroll
-                for (int e = 0; e < DF; ++e)
+                        for (int t = 0; t <= RT; ++t) kf[t] = key_rows(f, t);
+                        const Frag q = query(f);
 #pragma unroll
-                    for (int t = 0; t <= RT; ++t) O::mma(sc[t], O::rows(K + (16 * t + c) * SK + KB * e + VE * g), qf[e]);
+                        for (int i = 0; i < O::PAIRS; ++i) {
+#pragma unroll
+                            for (int p = 0; p < NP; ++p) O::mma(i, x[p], sf[p], q);
+#pragma unroll
+                            for (int t = 0; t <= RT; ++t) O::mma(i, sc[t], kf[t], q);
+                        }
+                    }
+                    if (next < end) load_queries(qbase, qoff);
+                } else {
+#pragma unroll
+                    for (int f = 0; f < DF; ++f)
+#pragma unroll
+                        for (int p = 0; p < NP; ++p) O::mma(0, x[p], states(f, p), qf[f]);
+                    __builtin_amdgcn_sched_barrier(0);     // (phases kept apart: mixed, they measure 2 to 5% more)
+#pragma unroll
+                    for (int f = 0; f < DF; ++f)
+#pragma unroll
+                        for (int t = 0; t <= RT; ++t) O::mma(0, sc[t], key_rows(f, t), qf[f]);
+                }
 #pragma unroll
                 for (int t = 0; t <= RT; ++t)
 #pragma unroll
@@ -531,8 +653,14 @@ __device__ __forceinline__ void decay_scan(const DecayLaunch& L, const DecayRole
 #pragma unroll
                 for (int f = 0; TPF * f <= RT; ++f) {
                     const Frag a = O::acc(&sc[TPF * f]);
+                    if constexpr (WIDE) {
 #pragma unroll
-                    for (int p = 0; p < NP; ++p) O::mma(x[p], vf[f][p], a);
+                        for (int p = 0; p < NP; ++p) vf[f][p] = values(f, p);
+                    }
+#pragma unroll
+                    for (int i = 0; i < O::PAIRS; ++i)
+#pragma unroll
+                        for (int p = 0; p < NP; ++p) O::mma(i, x[p], vf[f][p], a);
                 }
                 __builtin_amdgcn_sched_barrier(0);
                 const From<EXACT> out(obase);
@@ -565,7 +693,7 @@ __device__ __forceinline__ void decay_scan(const DecayLaunch& L, const DecayRole
                     }
                 }
                 obase += orow.st * C;
-                if (SB == 1) __syncthreads();
+                if (SB == 1 && !ONE) __syncthreads();
                 wi = wi_whole;
                 low = 0;
             }
@@ -575,24 +703,29 @@ __device__ __forceinline__ void decay_scan(const DecayLaunch& L, const DecayRole
                 for (int r = 0; r < 4; ++r) S[d][r] *= factor;
 #pragma unroll
             for (int f = 0; f < CF; ++f) {
-                Frag vw[O::PARTS], kf[DTW];
+                Frag vw[O::PARTS];
+                auto keys = [&](int d) { return O::cols(K + KB * f * SK + srow - 4 * g + 16 * d + cols_at(SK, 4, c, g), SK, KPL); };
+                Frag kf[DTW];
 #pragma unroll
-                for (int d = 0; d < DTW; ++d)
-                    kf[d] = O::cols(K + KB * f * SK + srow - 4 * g + 16 * d + O::cols_at(SK, 4, c, g), SK);
+                for (int d = 0; d < DTW; ++d) kf[d] = keys(d);
+                if constexpr (WIDE) vf[f][sp] = values(f, sp);
                 O::weighted(vw, vf[f][sp], wv[f]);
 #pragma unroll
                 for (int s = O::PARTS - 1; s >= 0; --s)
 #pragma unroll
-                    for (int d = 0; d < DTW; ++d) O::mma(S[d], kf[d], vw[s]);
+                    for (int i = 0; i < O::PAIRS; ++i)
+#pragma unroll
+                        for (int d = 0; d < DTW; ++d) O::mma(i, S[d], kf[d], vw[s]);
             }
             carry += lam.lo;
             factor = lam.hi + carry;
             carry -= factor - lam.hi;
             // (after the last block what is written is not read: no branch splits the block's instructions)
+            if (ONE) __syncthreads();
             if (EXACT || next < end) {
                 if (!STATES) state_out(M.s[SB == 2 ? buf ^ 1 : 0]);
-                tk.template store<true>(M.k[buf ^ 1], da, 0, tid);
-                tv.template store<true>(M.v[buf ^ 1], dbs, 0, tid);
+                tk.template store<true>(M.k[ONE ? 0 : buf ^ 1], da, 0, tid);
+                tv.template store<true>(M.v[ONE ? 0 : buf ^ 1], dbs, 0, tid);
             }
             __syncthreads();
         }
@@ -625,13 +758,13 @@ __device__ __forceinline__ void decay_scan(const DecayLaunch& L, const DecayRole
 }
 
 template <typename E, int DAP, int SB, bool STATES, bool EXACT>
-__global__ __launch_bounds__(64 * waves<E>(DAP), 2) void decay_scan_kernel(DecayLaunch L)
+__global__ __launch_bounds__((64 * Shape<E, DAP, EXACT>::NW), (Shape<E, DAP, EXACT>::PER)) void decay_scan_kernel(DecayLaunch L)
 {
     extern __shared__ __align__(16) unsigned char smem[];
-    constexpr int CT = Ops<E>::C / 16;
+    constexpr int CT = Shape<E, DAP, EXACT>::C / 16;
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     // (waves w and w + 4 share a SIMD: their row tiles add up to the same number of score tiles)
-    const int rt = CT == 4 ? (w < 4 ? w : 7 - w) : (w ^ (w >> 2)) & 1;
+    const int rt = CT == 2 ? w & 1 : w < 4 ? w : 7 - w;
     // (the roles are told apart by constants: an argument indexed at run time would be copied to memory, and its fields would no
     // longer be known to be the same for all lanes; divisions run on the vector unit, with the same result)
     int total = 0;
@@ -694,7 +827,7 @@ template <typename E, int DAP, int SB, bool STATES, bool EXACT> hipError_t scan_
     constexpr size_t bytes = sizeof(Smem<E, DAP, SB>);
     static_assert(bytes <= 160 * 1024, "one compute unit's LDS");
     hipLaunchKernelGGL((decay_scan_kernel<E, DAP, SB, STATES, EXACT>), dim3(groups, STATES ? L.segments - 1 : L.segments),
-                       dim3(64 * waves<E>(DAP)), bytes, st, L);
+                       dim3(64 * Shape<E, DAP, EXACT>::NW), bytes, st, L);
     return hipGetLastError();
 }
 
@@ -704,7 +837,9 @@ template <typename E, int DAP, int SB, bool STATES, bool EXACT> hipError_t scan_
 template <typename E, int DAP, bool STATES, bool EXACT> hipError_t scan(const DecayLaunch& L, unsigned groups, hipStream_t st)
 {
     constexpr size_t HALF = 80 * 1024;
-    if constexpr (!STATES && sizeof(Smem<E, DAP, 2>) <= HALF)
+    if constexpr (Shape<E, DAP, EXACT>::KVB == 1)
+        return scan_sb<E, DAP, 1, STATES, EXACT>(L, groups, st);
+    else if constexpr (!STATES && sizeof(Smem<E, DAP, 2>) <= HALF)
         return scan_sb<E, DAP, 2, STATES, EXACT>(L, groups, st);
     else if constexpr (!STATES && sizeof(Smem<E, DAP, 1>) <= HALF)
         return static_cast<long long>(groups) * L.segments <= L.cus ? scan_sb<E, DAP, 2, STATES, EXACT>(L, groups, st)
@@ -797,7 +932,15 @@ __global__ __launch_bounds__(NJ) void decay_step_kernel(DecayStepLaunch L, int s
 hipError_t launch_decay(const DecayLaunch& L, hipStream_t st)
 {
     const long heads = static_cast<long>(L.B) * L.H;
-    // roles with the same padded key channels share a launch
+    // Roles with the same padded channels of the state share a launch.  All of them do, with the padding of the largest, where
+    // that leaves each workgroup a compute unit: launches one after the other add up their latencies (backward float32
+    // B2 H6 T509, keys of 72 and values of 58 channels: 43 us in one, 66 in two).
+    int widest = 64;
+    for (int r = 0; r < L.roles; ++r)
+        while (L.role[r].da > widest) widest *= 2;
+    long all = 0;
+    for (int r = 0; r < L.roles; ++r) all += heads * decay_slices(L.bf16, widest, L.role[r].db) * L.segments;
+    const int narrowest = all <= L.cus ? widest : 64;
     for (int pass = L.segments > 1 ? 0 : 2; pass < 3; ++pass) {
         if (pass == 1) {
             long long most = 0;
@@ -811,7 +954,7 @@ hipError_t launch_decay(const DecayLaunch& L, hipStream_t st)
             if (e != hipSuccess) return e;
             continue;
         }
-        for (int lim = 64, low = 0; lim <= 256; low = lim, lim *= 2) {
+        for (int lim = narrowest, low = 0; lim <= widest; low = lim, lim *= 2) {
             DecayLaunch P = L;
             P.roles = 0;
             long slices = 0;

@@ -40,7 +40,7 @@ struct DecayLaunch {
     bool bf16;
 };
 // value columns of a scan workgroup, and workgroups over db columns, for a state of da channels
-constexpr int decay_slice(bool bf16, int da) { return bf16 || da > 128 ? 64 : 32; }
+constexpr int decay_slice(bool bf16, int da) { return bf16 || da <= 128 ? 64 : 32; }
 constexpr int decay_slices(bool bf16, int da, int db) { return (db + decay_slice(bf16, da) - 1) / decay_slice(bf16, da); }
 hipError_t launch_decay(const DecayLaunch& L, hipStream_t st);
 

@@ -211,18 +211,20 @@ bool rows_fit(const ll (&st)[3], int T, ll e) { return T <= 1 || st[2] <= ((1LL 
 
 // Segments of a sequence.  A scan without them takes c us for 64 tokens, whatever the number of heads, until the workgroups fill the
 // compute units.  Cut into S parts it takes a pass for their states (another s us) and a join, all of them on an S-th of the
-// tokens, with one or two workgroups on each unit.  Estimates in us, d 128 (256 channels take twice that on both sides).
-// Measured, whole / cut: bfloat16 forward 16 heads T 512 22/24, 15 heads T 1003 43/26, 4 heads T 2048 79/24, 32 heads
-// T 2048 80/47; backward 16 heads T 512 23/35, 32 heads T 2048 75/96; float32 forward 4 heads T 512 55/22, 16 heads
-// T 512 58/34, 32 heads T 2048 200/113.
+// tokens, with one workgroup on each unit, or with two of bfloat16.  Estimates in us for da channels of the state (bfloat16: 128; 256 take
+// twice that on both sides).
+// Measured, whole / cut, d 128: bfloat16 forward 16 heads T 512 23/27, 4 heads T 256 17/24, 15 heads T 1003 61/33,
+// 32 heads T 2048 72/48; backward 16 heads T 512 24/37, 32 heads T 2048 76/90; float32 forward 4 heads T 512 54/28,
+// 32 heads T 2048 193/97; backward 16 heads T 512 57/61, 32 heads T 2048 199/194; d 64, 16 heads T 2048 122/35; d 256, 4 heads
+// T 512 81/37.
 struct Cut { int tokens, segments; };
-Cut cut_of(ll groups, int T, bool bf16)
+Cut cut_of(ll groups, int T, bool bf16, int da)
 {
-    const double c = bf16 ? 2.4 : 6.2, s = bf16 ? 1.5 : 2.6, shared = bf16 ? 1.6 : 1.35;     // two on a unit: each slower
+    const double c = bf16 ? 2.4 : da <= 64 ? 3.7 : da <= 128 ? 6.2 : 9.3, s = bf16 ? 1.5 : c / 2, shared = 1.6;     // two on a unit: each slower
     const ll steps = (static_cast<ll>(T) + 63) / 64;
     Cut best{std::max(T, 1), 1};
     double least = 0.9 * (steps * c + 5.);
-    for (int on_unit = 1; on_unit <= 2; ++on_unit) {
+    for (int on_unit = 1; on_unit <= (bf16 ? 2 : 1); ++on_unit) {
         const ll most = on_unit * static_cast<ll>(cus()) / groups;
         if (most < 2 || steps < 2) continue;
         const ll each = (steps + most - 1) / most;                  // steps of a segment
@@ -286,7 +288,7 @@ size_t sfda_decay_attn_fwd_workspace_bytes(int B, int H, int T, int dk, int dv, 
     const ll heads = static_cast<ll>(B) * H;
     const bool bf16 = dtype == SFDA_BF16;
     if (heads == 0) return 0;
-    const Cut c = cut_of(heads * sfda::decay_slices(bf16, dk, dv), T, bf16);
+    const Cut c = cut_of(heads * sfda::decay_slices(bf16, dk, dv), T, bf16, dk);
     return c.segments > 1 ? static_cast<size_t>(c.segments) * heads * dk * dv * 4 : 0;
 }
 
@@ -321,7 +323,7 @@ sfda_status_t sfda_decay_attn_fwd(const void* q, const void* k, const void* v, c
     c.output(flat(cut ? workspace : nullptr, static_cast<ll>(need)), 4, false);
     const sfda_status_t st = c.done();
     if (st != SFDA_OK) return st;
-    const Cut segs = cut_of(heads * sfda::decay_slices(bf16, dk, dv), T, bf16);
+    const Cut segs = cut_of(heads * sfda::decay_slices(bf16, dk, dv), T, bf16, dk);
     R.q = q; R.k = k; R.v = v; R.o = o; R.S0 = S0; R.S_T = S_T;
     R.da = dk; R.db = dv; R.s_row = dv; R.s_col = 1;
     R.intra = scale; R.inter = scale; R.upd = 1.f;
@@ -341,7 +343,7 @@ size_t sfda_decay_attn_bwd_workspace_bytes(int B, int H, int T, int dk, int dv, 
     const ll heads = static_cast<ll>(B) * H;
     const bool bf16 = dtype == SFDA_BF16;
     if (heads == 0) return 0;
-    const Cut c = cut_of(heads * (2 * sfda::decay_slices(bf16, dv, dk) + sfda::decay_slices(bf16, dk, dv)), T, bf16);
+    const Cut c = cut_of(heads * (2 * sfda::decay_slices(bf16, dv, dk) + sfda::decay_slices(bf16, dk, dv)), T, bf16, std::max(dk, dv));
     return c.segments > 1 ? 3 * static_cast<size_t>(c.segments) * heads * dk * dv * 4 : 0;
 }
 
@@ -383,7 +385,7 @@ sfda_status_t sfda_decay_attn_bwd(const void* q, const void* k, const void* v, c
     c.output(flat(cut ? workspace : nullptr, static_cast<ll>(need)), 4, false);
     const sfda_status_t st = c.done();
     if (st != SFDA_OK) return st;
-    const Cut segs = cut_of(heads * (2 * sfda::decay_slices(bf16, dv, dk) + sfda::decay_slices(bf16, dk, dv)), T, bf16);
+    const Cut segs = cut_of(heads * (2 * sfda::decay_slices(bf16, dv, dk) + sfda::decay_slices(bf16, dk, dv)), T, bf16, std::max(dk, dv));
     const int segments = cut ? segs.segments : 1;
     sfda::DecayLaunch L{};
     auto put = [](ll (&to)[3], const ll (&from)[3]) { std::copy(from, from + 3, to); };
