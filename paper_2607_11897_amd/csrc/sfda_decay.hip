@@ -114,7 +114,6 @@ template <> struct Ops<uint16_t> {
         *reinterpret_cast<u32x2*>(to) = u32x2{pack2(x[0], x[1]), pack2(x[2], x[3])};
     }
     static __device__ __forceinline__ void put(uint16_t* to, int, u32x4 w) { *reinterpret_cast<u32x4*>(to) = w; }
-    static __device__ __forceinline__ void put1(uint16_t* to, int, u32x4 w, int i) { *to = static_cast<uint16_t>(w[i / 2] >> (i % 2 * 16)); }
     static __device__ __forceinline__ u32x4 pack8(const f32x4& x, const f32x4& y)
     {
         return u32x4{pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(y[0], y[1]), pack2(y[2], y[3])};
@@ -207,13 +206,6 @@ template <> struct Ops<float> {
         for (int s = 0; s < 3; ++s) *reinterpret_cast<u32x2*>(to + s * plane) = u32x2{a[s], b[s]};
     }
     static __device__ __forceinline__ void put(uint16_t* to, int plane, u32x4 w) { put4(to, plane, __builtin_bit_cast(f32x4, w)); }
-    static __device__ __forceinline__ void put1(uint16_t* to, int plane, u32x4 w, int i)
-    {
-        uint32_t p[3];
-        split(p, __uint_as_float(w[i]), 0.f);
-#pragma unroll
-        for (int s = 0; s < 3; ++s) to[s * plane] = static_cast<uint16_t>(p[s]);
-    }
     static __device__ __forceinline__ void store1(float* p, float x) { *p = x; }
     static constexpr int PARTS = 1;
     static __device__ __forceinline__ void weighted(Frag (&out)[PARTS], const Frag& v, const float (&w)[8])
@@ -273,13 +265,13 @@ __device__ __forceinline__ uint64_t same_for_all(uint64_t x)
     const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(x)), hi = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(x >> 32));
     return static_cast<uint64_t>(hi) << 32 | lo;
 }
-// 16 bytes at base + off + more, more the same for all lanes; less than 2^31 bytes from the base (off may be negative where the
-// bytes before the base are the row's own).  ALIGNED: to 4 bytes, by a buffer resource.
+// 16 bytes at base + off + more, base and more the same for all lanes; less than 2^31 bytes from the base.  ALIGNED: to 4 bytes, by a
+// buffer resource.
 template <bool ALIGNED> struct From {
     const char* p;
-    __device__ __forceinline__ explicit From(const char* base) : p(base) {}
-    __device__ __forceinline__ u32x4 load(uint32_t off, uint32_t more) const { return load16(p + static_cast<int>(off + more)); }
-    __device__ __forceinline__ void store(uint32_t off, uint32_t more, u32x4 x) const { store16(const_cast<char*>(p) + static_cast<int>(off + more), x); }
+    __device__ __forceinline__ explicit From(const char* base) : p(reinterpret_cast<const char*>(same_for_all(reinterpret_cast<uint64_t>(base)))) {}
+    __device__ __forceinline__ u32x4 load(uint32_t off, uint32_t more) const { return load16(p + more + off); }
+    __device__ __forceinline__ void store(uint32_t off, uint32_t more, u32x4 x) const { store16(const_cast<char*>(p) + more + off, x); }
 };
 template <> struct From<true> {
     __amdgpu_buffer_rsrc_t r;
@@ -289,10 +281,28 @@ template <> struct From<true> {
     __device__ __forceinline__ void store(uint32_t off, uint32_t more, u32x4 x) const { __builtin_amdgcn_raw_buffer_store_b128(x, r, off, more, 0); }
 };
 
+// 16 bytes `past` elements (fewer than they hold) down, zeros behind: words by selects, bfloat16 by 64-bit shifts, which take
+// more time and fewer registers (B8 H16 T1024 d 127: float32 176 us and 199, bfloat16 78 and 77)
+template <typename E> __device__ __forceinline__ u32x4 move_down(u32x4 x, int past)
+{
+    if constexpr (sizeof(E) == 4) {
+        const bool one = past & 1, two = past & 2;
+        const uint32_t y0 = one ? x[1] : x[0], y1 = one ? x[2] : x[1], y2 = one ? x[3] : x[2], y3 = one ? 0 : x[3];
+        return u32x4{two ? y2 : y0, two ? y3 : y1, two ? 0 : y2, two ? 0 : y3};
+    } else {
+        typedef unsigned long long u64;
+        const u64 lo = static_cast<u64>(x[1]) << 32 | x[0], hi = static_cast<u64>(x[3]) << 32 | x[2];
+        const int t = past * 16 & 63;
+        const u64 l = lo >> t | hi << 1 << (63 - t), h = hi >> t;
+        const u64 a = past < 4 ? l : h, b = past < 4 ? h : 0;
+        return u32x4{static_cast<uint32_t>(a), static_cast<uint32_t>(a >> 32), static_cast<uint32_t>(b), static_cast<uint32_t>(b >> 32)};
+    }
+}
+
 // A block's rows of one tensor on their way to LDS: ROWS tokens x COLS channels (COLS padded), 16-byte
 // vectors held in registers between the load and the write.  Padding channels are clamped to channel 0, and never written.
 // EXACT: the channels are whole vectors.  Otherwise the vector that would cross a row's end is moved back to end with it (into
-// the `before` channels that the row has before these, where they are few; the write then goes by elements), and rows
+// the `before` channels that the row has before these, where they are few) and moved into place when it is written, and rows
 // shorter than a vector are read by elements.
 template <typename E, int NT, int ROWS, int COLS, int STRIDE, bool EXACT> struct Tile {
     static constexpr int VE = Ops<E>::VE, VPR = COLS / VE, RPP = NT / VPR, N = ROWS / RPP, PLANE = ROWS * STRIDE;
@@ -301,38 +311,41 @@ template <typename E, int NT, int ROWS, int COLS, int STRIDE, bool EXACT> struct
     uint32_t off, step;     // a whole block's first vector in memory order, and from a pass to the next
 
     bool few;               // by elements
+    int back;               // elements that the lane's vector was moved back
 
-    __device__ __forceinline__ uint32_t at(int cols, int tid) const
+    __device__ __forceinline__ uint32_t at(int cols, int before, int tid) const
     {
         const int col = (tid % VPR) * VE;
-        return (col + VE <= cols ? col : EXACT || few ? 0 : cols - VE) * static_cast<int>(sizeof(E));
+        return (before + (col + VE <= cols ? col : EXACT || few ? 0 : cols - VE)) * static_cast<int>(sizeof(E));
     }
     __device__ __forceinline__ void place(const Rows& R, int cols, int before, int tid)
     {
         few = !EXACT && cols + before < VE;
         off = R.offset(tid / VPR + (R.st < 0 ? (N - 1) * RPP : 0), 0, ROWS);
         step = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(RPP * (R.st < 0 ? -R.st : R.st)));
-        off += at(cols, tid);       // (a vector moved back before the slice: the sum is still past the row's start, which the base is not)
+        off += at(cols, before, tid);
+        const int past = (tid % VPR) * VE + VE - cols;
+        back = EXACT || few || past <= 0 || past >= VE ? 0 : past;
     }
     __device__ __forceinline__ u32x4 one(const From<EXACT>& from, uint32_t o, uint32_t more, int cols, int tid) const
     {
         if constexpr (!EXACT) {
-            if (few) return tid % VPR == 0 ? load_few<E>(from.p + static_cast<int>(o + more), cols) : u32x4{0, 0, 0, 0};
+            if (few) return tid % VPR == 0 ? load_few<E>(from.p + more + o, cols) : u32x4{0, 0, 0, 0};
         }
         return from.load(o, more);
     }
-    __device__ __forceinline__ void load(const char* base, bool back, int cols, int tid)
+    __device__ __forceinline__ void load(const char* base, bool reverse, int cols, int tid)
     {
         const From<EXACT> from(base);
 #pragma unroll
-        for (int u = 0; u < N; ++u) x[u] = one(from, off, __builtin_amdgcn_readfirstlane((back ? N - 1 - u : u) * step), cols, tid);
+        for (int u = 0; u < N; ++u) x[u] = one(from, off, __builtin_amdgcn_readfirstlane((reverse ? N - 1 - u : u) * step), cols, tid);
     }
     // a segment's first block, from its first token on
-    __device__ __forceinline__ void load_first(const Rows& R, int begin, int pad, int cols, int tid)
+    __device__ __forceinline__ void load_first(const Rows& R, int begin, int pad, int cols, int before, int tid)
     {
         const From<EXACT> from(R.base(begin, ROWS - pad));
 #pragma unroll
-        for (int u = 0; u < N; ++u) x[u] = one(from, R.offset(tid / VPR + u * RPP, pad, ROWS - pad) + at(cols, tid), 0, cols, tid);
+        for (int u = 0; u < N; ++u) x[u] = one(from, R.offset(tid / VPR + u * RPP, pad, ROWS - pad) + at(cols, before, tid), 0, cols, tid);
     }
     // rows before `pad` are zero
     template <bool WHOLE> __device__ __forceinline__ void store(uint16_t* lds, int cols, int pad, int tid) const
@@ -345,13 +358,7 @@ template <typename E, int NT, int ROWS, int COLS, int STRIDE, bool EXACT> struct
             const int r = tid / VPR + u * RPP;
             const u32x4 z = {0, 0, 0, 0};
             const u32x4 w = WHOLE || r >= pad ? x[u] : z;
-            if (EXACT || col + VE <= cols || few) {
-                Ops<E>::put(lds + r * STRIDE + col, PLANE, w);
-            } else {
-#pragma unroll
-                for (int i = 0; i < VE; ++i)
-                    if (cols - VE + i >= 0) Ops<E>::put1(lds + r * STRIDE + cols - VE + i, PLANE, w, i);
-            }
+            Ops<E>::put(lds + r * STRIDE + col, PLANE, EXACT ? w : move_down<E>(w, back));
         }
     }
 };
@@ -374,21 +381,10 @@ template <typename E, bool EXACT> __device__ __forceinline__ u32x4 row_load(cons
 template <typename E, bool EXACT> __device__ __forceinline__ u32x4 row_place(u32x4 x, int col, int cols)
 {
     constexpr int VE = Ops<E>::VE;
-    typedef unsigned long long u64;
-    const u32x4 zero = {0, 0, 0, 0};
     if (EXACT) return x;
-    if (col >= cols) return zero;
-    if (cols < VE || col + VE <= cols) return x;
-    const int s = (col + VE - cols) * 8 * static_cast<int>(sizeof(E));      // 16 .. 112 bits
-    u64 lo = (static_cast<u64>(x[1]) << 32) | x[0], hi = (static_cast<u64>(x[3]) << 32) | x[2];
-    if (s >= 64) {
-        lo = hi >> (s - 64);
-        hi = 0;
-    } else {
-        lo = (lo >> s) | (hi << (64 - s));
-        hi >>= s;
-    }
-    return u32x4{static_cast<uint32_t>(lo), static_cast<uint32_t>(lo >> 32), static_cast<uint32_t>(hi), static_cast<uint32_t>(hi >> 32)};
+    const int past = col + VE - cols;
+    if (past >= VE) return u32x4{0, 0, 0, 0};
+    return move_down<E>(x, past <= 0 || cols < VE ? 0 : past);
 }
 
 // A scan workgroup, for the type and the (padded) channels of the state: C tokens of a block, NS value columns, NW waves, KVB
@@ -400,7 +396,7 @@ template <typename E, bool EXACT> __device__ __forceinline__ u32x4 row_place(u32
 //  * float32: three planes fill LDS, so that there is one buffer of them and one workgroup on a compute unit; with 256 channels
 //    half the block and half the columns.  Four waves with the registers of all (forward B8 H16 T2048 d 128: 215 us, 234 with eight;
 //    backward 617 and 667), but eight where rows are not whole vectors, whose address arithmetic they hide (B3 H5
-//    T1003 keys of 88, values of 74: 44 us and 53 with four).
+//    T1003 keys of 88, values of 74: 44 us and 51 with four).
 template <typename E, int DAP, bool EXACT> struct Shape {
     static constexpr bool HALF = sizeof(E) == 4 && DAP > 128;
     static constexpr int C = HALF ? 32 : 64, NS = decay_slice(sizeof(E) == 2, DAP), NW = (sizeof(E) == 2 ? DAP > 128 : DAP <= 128 && !EXACT) ? 8 : 4;
@@ -454,7 +450,7 @@ __device__ __forceinline__ void decay_scan(const DecayLaunch& L, const DecayRole
     const long long tok0 = reverse ? len - 1 : 0, dir = reverse ? -ES : ES;
     const Rows qr = {static_cast<const char*>(R.q) + (b * R.q_s[0] + h * R.q_s[1] + tok0 * R.q_s[2]) * ES, dir * R.q_s[2]};
     const Rows kr = {static_cast<const char*>(R.k) + (b * R.k_s[0] + h * R.k_s[1] + tok0 * R.k_s[2]) * ES, dir * R.k_s[2]};
-    const Rows vr = {static_cast<const char*>(R.v) + (b * R.v_s[0] + h * R.v_s[1] + tok0 * R.v_s[2] + n0) * ES, dir * R.v_s[2]};
+    const Rows vr = {static_cast<const char*>(R.v) + (b * R.v_s[0] + h * R.v_s[1] + tok0 * R.v_s[2]) * ES, dir * R.v_s[2]};
     E* const op = static_cast<E*>(R.o) + b * R.o_s[0] + h * R.o_s[1] + n0;
     const Rows orow = {reinterpret_cast<const char*>(op) + tok0 * R.o_s[2] * ES, dir * R.o_s[2]};
 
@@ -474,8 +470,8 @@ __device__ __forceinline__ void decay_scan(const DecayLaunch& L, const DecayRole
         }
     };
     if (begin < end) {
-        tk.load_first(kr, begin, pad, da, tid);
-        tv.load_first(vr, begin, pad, dbs, tid);
+        tk.load_first(kr, begin, pad, da, 0, tid);
+        tv.load_first(vr, begin, pad, dbs, n0, tid);
         if (!STATES) load_queries(qr.base(begin, C - pad), qr.offset(16 * RT + c, pad, C - pad));
     }
     const uint32_t qoff = STATES ? 0 : qr.offset(16 * RT + c, 0, C);
@@ -687,9 +683,11 @@ __device__ __forceinline__ void decay_scan(const DecayLaunch& L, const DecayRole
                         }
                     } else if (row) {
                         E* to = reinterpret_cast<E*>(const_cast<char*>(obase) + off);
+                        int left = dbs - at_n;
+                        asm("" : "+v"(left));       // (or the masks of the stores are kept over the blocks, and spilled)
 #pragma unroll
                         for (int i = 0; i < PN; ++i)
-                            if (at_n + i < dbs) O::store1(to + i, x[2 * u + i / 4][i % 4]);
+                            if (i < left) O::store1(to + i, x[2 * u + i / 4][i % 4]);
                     }
                 }
                 obase += orow.st * C;

@@ -5,6 +5,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <initializer_list>
 
 #include "../../include/sfda.h"
 #include "sfda_layer.h"
@@ -211,31 +212,52 @@ bool rows_fit(const ll (&st)[3], int T, ll e) { return T <= 1 || st[2] <= ((1LL 
 
 // Segments of a sequence.  A scan without them takes c us for 64 tokens, whatever the number of heads, until the workgroups fill the
 // compute units.  Cut into S parts it takes a pass for their states (another s us) and a join, all of them on an S-th of the
-// tokens, with one workgroup on each unit, or with two of bfloat16.  Estimates in us for da channels of the state (bfloat16: 128; 256 take
-// twice that on both sides).
+// tokens, with one workgroup on each unit, or with two of bfloat16.  The estimates are in us, for the padded channels of the state
+// and for rows of whole vectors or not; roles of different padding add up, but where they share a launch.
 // Measured, whole / cut, d 128: bfloat16 forward 16 heads T 512 23/27, 4 heads T 256 17/24, 15 heads T 1003 61/33,
 // 32 heads T 2048 72/48; backward 16 heads T 512 24/37, 32 heads T 2048 76/90; float32 forward 4 heads T 512 54/28,
 // 32 heads T 2048 193/97; backward 16 heads T 512 57/61, 32 heads T 2048 199/194; d 64, 16 heads T 2048 122/35; d 256, 4 heads
 // T 512 81/37.
 struct Cut { int tokens, segments; };
-Cut cut_of(ll groups, int T, bool bf16, int da)
+struct State { int da, db; };           // a role's
+Cut cut_of(ll heads, std::initializer_list<State> roles, int T, bool bf16)
 {
-    const double c = bf16 ? 2.4 : da <= 64 ? 3.7 : da <= 128 ? 6.2 : 9.3, s = bf16 ? 1.5 : c / 2, shared = 1.6;     // two on a unit: each slower
+    int widest = 0;
+    bool vectors = true;
+    ll groups[3] = {0, 0, 0}, together = 0;
+    auto padded = [](int da) { return da <= 64 ? 0 : da <= 128 ? 1 : 2; };
+    for (const State& r : roles) {
+        widest = std::max(widest, padded(r.da));
+        groups[padded(r.da)] += heads * sfda::decay_slices(bf16, r.da, r.db);
+        vectors = vectors && (r.da | r.db) % (bf16 ? 8 : 4) == 0;
+    }
+    for (const State& r : roles) together += heads * sfda::decay_slices(bf16, 64 << widest, r.db);
+    auto cost = [&](ll segments) {
+        constexpr double B[3] = {2.4, 2.4, 4.8}, F[3] = {3.7, 6.2, 9.3};
+        double c = 0;
+        for (int i = 0; i < 3; ++i)
+            if (together * segments <= cus() ? i == widest : groups[i] > 0) c += bf16 ? B[i] : F[i];
+        return vectors ? c : 1.5 * c;
+    };
+    const double s = bf16 ? 0.6 : 0.5, shared = 1.6;        // the states' pass to the other; two on a unit: each slower
     const ll steps = (static_cast<ll>(T) + 63) / 64;
     Cut best{std::max(T, 1), 1};
-    double least = 0.9 * (steps * c + 5.);
+    double least = 0.9 * (steps * cost(1) + 5.);
     for (int on_unit = 1; on_unit <= (bf16 ? 2 : 1); ++on_unit) {
-        const ll most = on_unit * static_cast<ll>(cus()) / groups;
+        const ll most = on_unit * static_cast<ll>(cus()) / std::max({groups[0], groups[1], groups[2]});
         if (most < 2 || steps < 2) continue;
-        const ll each = (steps + most - 1) / most;                  // steps of a segment
-        const double us = each * (c + s) * (on_unit == 2 ? shared : 1.) + 20.;
+        const ll each = (steps + most - 1) / most, segments = (steps + each - 1) / each;        // steps of a segment
+        const double us = each * cost(segments) * (1 + s) * (on_unit == 2 ? shared : 1.) + 20.;
         if (us < least) {
             least = us;
-            best = {static_cast<int>(each * 64), static_cast<int>((steps + each - 1) / each)};
+            best = {static_cast<int>(each * 64), static_cast<int>(segments)};
         }
     }
     return best;
 }
+// dq and dk have dk columns, dv has dv
+Cut cut_fwd(ll heads, int T, int dk, int dv, bool bf16) { return cut_of(heads, {{dk, dv}}, T, bf16); }
+Cut cut_bwd(ll heads, int T, int dk, int dv, bool bf16) { return cut_of(heads, {{dv, dk}, {dv, dk}, {dk, dv}}, T, bf16); }
 
 }  // namespace
 
@@ -288,7 +310,7 @@ size_t sfda_decay_attn_fwd_workspace_bytes(int B, int H, int T, int dk, int dv, 
     const ll heads = static_cast<ll>(B) * H;
     const bool bf16 = dtype == SFDA_BF16;
     if (heads == 0) return 0;
-    const Cut c = cut_of(heads * sfda::decay_slices(bf16, dk, dv), T, bf16, dk);
+    const Cut c = cut_fwd(heads, T, dk, dv, bf16);
     return c.segments > 1 ? static_cast<size_t>(c.segments) * heads * dk * dv * 4 : 0;
 }
 
@@ -323,7 +345,7 @@ sfda_status_t sfda_decay_attn_fwd(const void* q, const void* k, const void* v, c
     c.output(flat(cut ? workspace : nullptr, static_cast<ll>(need)), 4, false);
     const sfda_status_t st = c.done();
     if (st != SFDA_OK) return st;
-    const Cut segs = cut_of(heads * sfda::decay_slices(bf16, dk, dv), T, bf16, dk);
+    const Cut segs = cut_fwd(heads, T, dk, dv, bf16);
     R.q = q; R.k = k; R.v = v; R.o = o; R.S0 = S0; R.S_T = S_T;
     R.da = dk; R.db = dv; R.s_row = dv; R.s_col = 1;
     R.intra = scale; R.inter = scale; R.upd = 1.f;
@@ -336,14 +358,14 @@ sfda_status_t sfda_decay_attn_fwd(const void* q, const void* k, const void* v, c
     return sfda::launch_decay(L, static_cast<hipStream_t>(stream)) == hipSuccess ? SFDA_OK : SFDA_ERR_HIP;
 }
 
-// dq and dk have dk columns, dv has dv; the dk and dv scans need dS_T, the dq scan S0
+// the dk and dv scans need dS_T, the dq scan S0
 size_t sfda_decay_attn_bwd_workspace_bytes(int B, int H, int T, int dk, int dv, sfda_dtype_t dtype)
 {
     if (!dtype_ok(dtype) || !decay_sizes(B, H, T, dk, dv)) return 0;
     const ll heads = static_cast<ll>(B) * H;
     const bool bf16 = dtype == SFDA_BF16;
     if (heads == 0) return 0;
-    const Cut c = cut_of(heads * (2 * sfda::decay_slices(bf16, dv, dk) + sfda::decay_slices(bf16, dk, dv)), T, bf16, std::max(dk, dv));
+    const Cut c = cut_bwd(heads, T, dk, dv, bf16);
     return c.segments > 1 ? 3 * static_cast<size_t>(c.segments) * heads * dk * dv * 4 : 0;
 }
 
@@ -385,7 +407,7 @@ sfda_status_t sfda_decay_attn_bwd(const void* q, const void* k, const void* v, c
     c.output(flat(cut ? workspace : nullptr, static_cast<ll>(need)), 4, false);
     const sfda_status_t st = c.done();
     if (st != SFDA_OK) return st;
-    const Cut segs = cut_of(heads * (2 * sfda::decay_slices(bf16, dv, dk) + sfda::decay_slices(bf16, dk, dv)), T, bf16, std::max(dk, dv));
+    const Cut segs = cut_bwd(heads, T, dk, dv, bf16);
     const int segments = cut ? segs.segments : 1;
     sfda::DecayLaunch L{};
     auto put = [](ll (&to)[3], const ll (&from)[3]) { std::copy(from, from + 3, to); };
