@@ -9,59 +9,41 @@
 // roles of one launch.
 #include "sfda_device.h"
 #include "sfda_layer.h"
+#include "sfda_vec.h"
 
 #include <stddef.h>
 #include <string.h>
 
-#include <type_traits>
-
 namespace sfda {
 namespace {
 
+using namespace vec;
+
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int NJ = 256;                  // threads of the small kernels
 
-// 16 bytes at any address (global memory takes unaligned vectors)
-typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(1), may_alias));
-__device__ __forceinline__ u32x4 load16(const char* p) { return *reinterpret_cast<const u32x4_any*>(p); }
-__device__ __forceinline__ void store16(char* p, u32x4 x) { *reinterpret_cast<u32x4_any*>(p) = x; }
-
-// the first `cols` (fewer than fill them) elements of a row as 16 bytes, zeros behind them
-template <typename E> __device__ __forceinline__ u32x4 load_few(const char* p, int cols)
+// the first `cols` (fewer than fill them) elements of a row as 16 bytes, zeros behind them; a loop, for it is rare and the
+// scan short of registers
+template <typename E> __device__ __forceinline__ u32x4 short_row(const char* p, int cols)
 {
     typedef unsigned long long u64;
     constexpr int BITS = 8 * sizeof(E);
     u64 lo = 0, hi = 0;
 #pragma clang loop unroll(disable)
     for (int i = cols - 1; i >= 0; --i) {
-        E e;
-        memcpy(&e, p + i * sizeof(E), sizeof(E));
         uint32_t u = 0;
-        memcpy(&u, &e, sizeof(E));
+        memcpy(&u, p + i * sizeof(E), sizeof(E));
         hi = hi << BITS | lo >> (64 - BITS);
         lo = lo << BITS | u;
     }
     return u32x4{static_cast<uint32_t>(lo), static_cast<uint32_t>(lo >> 32), static_cast<uint32_t>(hi), static_cast<uint32_t>(hi >> 32)};
 }
 
-// two float32 as a pair of bfloat16, each to nearest even
-__device__ __forceinline__ uint32_t pack2(float a, float b)
-{
-    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-    bf16x2 p;
-    p[0] = static_cast<__bf16>(a);
-    p[1] = static_cast<__bf16>(b);
-    return __builtin_bit_cast(uint32_t, p);
-}
-__device__ __forceinline__ float lo_f32(uint32_t w) { return __uint_as_float(w << 16); }
-__device__ __forceinline__ float hi_f32(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
-
 // What the element type decides.  The matrix cores take bfloat16 operands.  A float32 is the sum of three bfloat16 (its 24 bits,
 // 8 in each), so float32 tensors lie in LDS as PL = 3 planes, and a product of two operands is the six products of parts
-// that reach 2^-21 of it (the three left out are below that): 6 x 16 cycles for 16 x 16 x 32 on a SIMD, where the float32 matrix
+// that reach 2^-22 of it (the three left out are below that): 6 x 16 cycles for 16 x 16 x 32 on a SIMD, where the float32 matrix
 // instruction takes 256.  Forward B8 H16 T2048 d 128: 215 us against 301 with float32 instructions, backward 617 and 868; the LDS
 // reads, the matrix instructions and the splitting of operands then take about a third of a block's time each.
 // An infinity in float32 comes out as NaN where it is used (its parts are inf - inf).
@@ -145,18 +127,16 @@ template <> struct Ops<uint16_t> {
 template <> struct Ops<float> {
     static constexpr int VE = 4, PL = 3, QV = 2;
     struct Frag { bf16x8 p[3]; };
-    // a pair as parts: the upper halves of the words (8 bits of each; truncated, so that nothing overflows), then of what is left,
-    // which is exact, twice
+    // a pair as parts, whose sum is exact.  The first ones are truncated (nothing overflows), the others to nearest, so that
+    // the products left out have no sign of their own
     static __device__ __forceinline__ void split(uint32_t (&p)[3], float a, float b)
     {
-#pragma unroll
-        for (int s = 0; s < 3; ++s) {
-            p[s] = __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302);
-            if (s < 2) {
-                a -= hi_f32(__float_as_uint(a));
-                b -= hi_f32(__float_as_uint(b));
-            }
-        }
+        p[0] = __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302);
+        a -= hi_f32(__float_as_uint(a));
+        b -= hi_f32(__float_as_uint(b));
+        p[1] = pack2(a, b);
+        asm("" : "+v"(p[1]));       // (or the halves are converted once more, one by one)
+        p[2] = pack2(a - lo_f32(p[1]), b - hi_f32(p[1]));
     }
     static __device__ __forceinline__ Frag split8(const float (&x)[8])
     {
@@ -330,7 +310,7 @@ template <typename E, int NT, int ROWS, int COLS, int STRIDE, bool EXACT> struct
     __device__ __forceinline__ u32x4 one(const From<EXACT>& from, uint32_t o, uint32_t more, int cols, int tid) const
     {
         if constexpr (!EXACT) {
-            if (few) return tid % VPR == 0 ? load_few<E>(from.p + more + o, cols) : u32x4{0, 0, 0, 0};
+            if (few) return tid % VPR == 0 ? short_row<E>(from.p + more + o, cols) : u32x4{0, 0, 0, 0};
         }
         return from.load(o, more);
     }
@@ -374,7 +354,7 @@ template <typename E, bool EXACT> __device__ __forceinline__ uint32_t row_at(int
 template <typename E, bool EXACT> __device__ __forceinline__ u32x4 row_load(const From<EXACT>& from, uint32_t off, int col, int cols)
 {
     if constexpr (!EXACT) {
-        if (cols < Ops<E>::VE) return col == 0 ? load_few<E>(from.p + off, cols) : u32x4{0, 0, 0, 0};
+        if (cols < Ops<E>::VE) return col == 0 ? short_row<E>(from.p + off, cols) : u32x4{0, 0, 0, 0};
     }
     return from.load(off, 0);
 }
@@ -476,6 +456,10 @@ __device__ __forceinline__ void decay_scan(const DecayLaunch& L, const DecayRole
     }
     const uint32_t qoff = STATES ? 0 : qr.offset(16 * RT + c, 0, C);
 
+#ifdef SFDA_LDS_POISON
+    lds_poison(&M, sizeof(Mem), tid, NT);
+    __syncthreads();
+#endif
     {   // padding stays zero (and with whole rows none is read)
         u32x4* z = reinterpret_cast<u32x4*>(smem);
         const u32x4 zero = {0, 0, 0, 0};
@@ -789,7 +773,7 @@ __global__ __launch_bounds__((64 * Shape<E, DAP, EXACT>::NW), (Shape<E, DAP, EXA
 }
 
 // The segments' states from zero become the states that enter them: one thread for an element of a
-// head's state, in place; eight segments' values are requested at a time.
+// head's state, in place; eight segments' values are requested at a time.  6 us for 32 states of 128 x 128 in 4 segments.
 __global__ __launch_bounds__(NJ) void decay_join_kernel(DecayLaunch L)
 {
     const DecayRole R = blockIdx.z == 0 ? L.role[0] : blockIdx.z == 1 ? L.role[1] : L.role[2];
@@ -875,7 +859,8 @@ template <typename E> hipError_t scan_any(const DecayLaunch& L, int da, unsigned
 
 // ------------------------------------------------------------------ decode step
 // S <- lambda S + k v^T, o = scale S^T q.  One workgroup for a head and 16 float4 columns; the 16 row
-// groups of a workgroup each take every 16th row, and their parts of o are added through LDS.
+// groups of a workgroup each take every 16th row, and their parts of o are added through LDS.  Memory-bound:
+// float32, 16384 states of 128 x 128: 412 us for 2.18 GB read and written, 5.3 TB/s (a large copy: 4.8).
 constexpr int SW = 64;      // value columns of a workgroup
 template <typename E>
 __global__ __launch_bounds__(NJ) void decay_step_kernel(DecayStepLaunch L, int slices)
