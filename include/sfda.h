@@ -434,9 +434,12 @@ sfda_status_t sfda_rotary(const void* q, const void* k, const float* cos, const 
  *   workspace : with at least sfda_decay_attn_fwd_workspace_bytes(...) bytes (0 where one workgroup
  *          for a head and 32 or 64 value columns fills the device) the sequences are cut into segments that are scanned
  *          in parallel; with less, or NULL, they are scanned whole.  The same result up to rounding.
- *   1 <= dk, dv <= 256; 64 tokens' rows of a tensor lie within 2^31 bytes (SFDA_ERR_SHAPE otherwise).  bfloat16: the block's scores and the state are rounded to bfloat16 as operands of
- *   the products that give o; the state itself is carried in float32 from exact products.  A token with a
- *   value that is not finite makes the rows of its block (32 or 64 tokens) before it NaN too.
+ *   1 <= dk, dv <= 256; 64 tokens' rows of a tensor lie within 2^31 bytes (SFDA_ERR_SHAPE otherwise).
+ *   bfloat16: the block's scores and the state are rounded to bfloat16 as operands of the products
+ *   that give o; the state itself is carried in float32 from products exact to 2^-24.
+ *   float32: products to 2^-22 (operands as three bfloat16 parts), sums in float32.
+ *   A token with a value that is not finite makes the rows of its block (32 or 64 tokens) before it NaN
+ *   too; in float32 an infinity acts as NaN.
  */
 size_t sfda_decay_attn_fwd_workspace_bytes(int B, int H, int T, int dk, int dv,
                                            sfda_dtype_t dtype);
@@ -451,7 +454,7 @@ sfda_status_t sfda_decay_attn_fwd(const void* q, const void* k, const void* v,
  * sfda_decay_attn_bwd -- gradients of a real loss through sfda_decay_attn_fwd, given dO = dL/do and
  * dS_T = dL/dS_T (NULL: zero).  With U_t = dL/dS_t = lambda_h U_{t+1} + scale q_t dO_t^T:
  *   dq_t = scale S_t dO_t,  dk_t = U_t v_t,  dv_t = U_t^T k_t,  dS0 = lambda_h U_1
- * (three scans in one launch, S_t and U_t formed on the way).  The decays are constants: they get no gradient.
+ * (three scans, S_t and U_t formed on the way).  The decays are constants: they get no gradient.
  *   dq, dk, dv : as q, k, v, zero past a sequence's length; dS0 [B, H, dk, dv] float32 or NULL.
  *   strides: (b, h, t) of q, k, v, dO, dq, dk, dv.  Other arguments as the forward's.
  */
