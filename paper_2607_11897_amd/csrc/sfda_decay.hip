@@ -371,8 +371,8 @@ template <typename E, bool EXACT> __device__ __forceinline__ u32x4 row_place(u32
 // buffers of keys and values, VP elements that a row of values in LDS is longer (4 rows of 64 bytes, every other 8 of
 // them, or of 32 bytes, on different banks).
 //  * bfloat16: four waves (one on a SIMD) form no scores and no weighted values twice, eight hide more latency and have
-//    half the registers' worth of work each.  Forward B8 H16 T4096 d 128: 161 us with four, 182 with eight (and 197 with
-//    32 columns); with 256 channels four do not have the registers.
+//    half the registers' worth of work each.  B8 H16 T4096 d 128, forward and backward: 177 and 397 us with four, 192 and 481
+//    with eight (slices of 32 columns: a fifth more than 64); with 256 channels four do not have the registers.
 //  * float32: three planes fill LDS, so that there is one buffer of them and one workgroup on a compute unit; with 256 channels
 //    half the block and half the columns.  Four waves with the registers of all (forward B8 H16 T2048 d 128: 215 us, 234 with eight;
 //    backward 617 and 667), but eight where rows are not whole vectors, whose address arithmetic they hide (B3 H5
@@ -814,8 +814,8 @@ template <typename E, int DAP, int SB, bool STATES, bool EXACT> hipError_t scan_
 }
 
 // One state buffer or two.  Two where a second workgroup fits beside it all the same, or where there is none: with
-// bfloat16 and 128 channels one buffer lets two workgroups share a compute unit (forward B8 H16 T4096, 256 workgroups: 168 us with two
-// buffers, 177 with one; backward, 768 workgroups: 443 and 404).  The segments' states need no buffer.
+// bfloat16 and 128 channels one buffer lets two workgroups share a compute unit (forward B8 H16 T4096, 256 workgroups: 177 us with two
+// buffers, 187 with one; backward, 768 workgroups: 415 and 396).  The segments' states need no buffer.
 template <typename E, int DAP, bool STATES, bool EXACT> hipError_t scan(const DecayLaunch& L, unsigned groups, hipStream_t st)
 {
     constexpr size_t HALF = 80 * 1024;

@@ -282,6 +282,13 @@ def test_decay_attn_bwd(B, H, T, dk, dv, dtype, layout, state, lengths):
             assert not any(got[m][i, :, n:].any() for m in ("dq", "dk", "dv"))
 
 
+# states of more than 128 and of at most 64 channels, one launch each: more heads than compute units; segments
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,H,T,dk,dv", [(16, 16, 70, 24, 150), (1, 8, 700, 40, 200), (20, 13, 5, 129, 60)])
+def test_decay_attn_bwd_in_two_launches(B, H, T, dk, dv, dtype):
+    test_decay_attn_bwd(B, H, T, dk, dv, dtype, "bthd", True, None)
+
+
 def test_decay_attn_bwd_against_differences():
     """Directional differences of the GPU's own forward in float32."""
     import torch
