@@ -83,7 +83,7 @@ Order order(const Box& b)
     return o;
 }
 
-// whether some i with -(y.n - 1) <= i <= x.n - 1 on each axis has sum i s = delta
+// whether some i with -(y.n - 1) <= i <= x.n - 1 on each axis has sum i s = delta, s the strides of x
 bool meets(const Box& x, const Box& y, const Order& o, int at, ll delta)
 {
     if (at == x.axes) return delta == 0;
@@ -104,14 +104,16 @@ bool overlap(const Box& x, const Box& y)
     const uintptr_t a = reinterpret_cast<uintptr_t>(x.p), b = reinterpret_cast<uintptr_t>(y.p);
     if (a + static_cast<uintptr_t>(extent(x)) <= b || b + static_cast<uintptr_t>(extent(y)) <= a) return false;
     if (x.axes != y.axes) return true;
-    Box all = x;        // each axis as long as the longer one
+    // each axis as long as the longer one; of an axis of one element the other tensor's stride counts, or none
+    Box all = x, u = x;
     for (int i = 0; i < x.axes; ++i) {
+        if (x.n[i] > 1 && y.n[i] > 1 && x.s[i] != y.s[i]) return true;
         all.n[i] = std::max(x.n[i], y.n[i]);
-        if (all.n[i] > 1 && x.s[i] != y.s[i]) return true;
+        all.s[i] = u.s[i] = x.n[i] > 1 ? x.s[i] : y.n[i] > 1 ? y.s[i] : 0;
     }
     const Order o = order(all);
     if (!o.nested) return true;
-    return meets(x, y, o, 0, b > a ? static_cast<ll>(b - a) : -static_cast<ll>(a - b));
+    return meets(u, y, o, 0, b > a ? static_cast<ll>(b - a) : -static_cast<ll>(a - b));
 }
 
 bool same(const Box& x, const Box& y)

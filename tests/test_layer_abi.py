@@ -62,6 +62,55 @@ def test_decay_attn_strides(lib):
     assert fwd(lib, strides=arr(*p), v=3 * A, o=3 * A + 2 * 8 * 4 - 4) == 6
 
 
+def test_overlaps_of_axes_of_one_element(lib):
+    """The stride of an axis of one element says nothing about where a tensor lies."""
+    def at(b, h, t, dv=8):
+        return arr(*([512, 128, 16] * 2 + [b, h, t] * 2))
+    for one in range(3):                            # o four elements into v, the stride of axis `one` shorter than a row
+        size = [2, 2, 2]
+        size[one] = 1
+        for short in (0, 1, 7, 8, 1 << 20):
+            s = [64, 32, 8]
+            s[one] = short
+            assert fwd(lib, **dict(zip("BHT", size)), v=3 * A, o=3 * A + 4 * 4, strides=at(*s)) == 6, (one, short)
+    # one key head in a buffer of three: over the second query head, not over what lies behind the queries
+    s = arr(*([192, 16, 48] * 4))
+    assert rot(lib, q=A, k=A + 16 * 4, qo=A, ko=A + 16 * 4, Hq=2, Hk=1, strides=s) == 6
+
+
+def test_overlaps_against_every_element(lib):
+    """Slices of one buffer that share an element are refused, whatever the strides of axes of one element."""
+    import itertools
+    import random
+    rng = random.Random(5)
+    met = 0
+    for _ in range(4000):
+        D = rng.randint(2, 5)
+        nq, nk = ([rng.choice([1, 1, 2, 3]) for _ in range(3)] for _ in range(2))
+        nk[0], nk[2] = nq[0], nq[2]
+        order, step, s = rng.sample(range(3), 3), D + rng.randint(0, 3), [0, 0, 0]
+        for a in order:
+            s[a] = step
+            step = step * max(nq[a], nk[a]) + rng.choice([0, 0, 1, 5])
+        t = list(s)
+        for a in range(3):
+            if nq[a] == 1 and rng.random() < 0.5:
+                s[a] = rng.choice([0, 1, 2, D, 64])
+            if nk[a] == 1 and rng.random() < 0.5:
+                t[a] = rng.choice([0, 1, 2, D, 64])
+        off = rng.randint(0, 2 * step)
+
+        def places(n, st, base):
+            return {base + sum(i * x for i, x in zip(at, st)) + d for at in itertools.product(*map(range, n)) for d in range(D)}
+        if places(nq, s, 0) & places(nk, t, off):
+            met += 1
+            # queries and keys of another buffer, qo and ko as drawn
+            far = [1 << 12] * 3
+            assert rot(lib, qo=5 * A, ko=5 * A + 4 * off, B=nq[0], Hq=nq[1], Hk=nk[1], T=nq[2], D=D, rot=2,
+                       strides=arr(*(far * 2 + s + t))) == 6, (nq, nk, s, t, D, off)
+    assert met > 500
+
+
 def bwd(lib, **kw):
     a = dict(q=A, k=2 * A, v=3 * A, g=4 * A, n=None, S0=5 * A, dO=6 * A, dS_T=7 * A, dq=8 * A, dk_=9 * A, dv_=10 * A, dS0=11 * A, B=1, H=2,
              T=8, dk=16, dv=8, dt=0) | kw
