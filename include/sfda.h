@@ -394,7 +394,8 @@ sfda_status_t sfda_chunk_solve_monitor(const void* k, const void* alpha, const v
  *
  * Strides: these calls take their activations with element strides, the last axis contiguous:
  * `strides` points to the strides of the outer axes, tensor after tensor in the order given at each
- * call, or is NULL for contiguous tensors.  Strides are >= 0 (SFDA_ERR_SHAPE otherwise); inputs may
+ * call, or is NULL for contiguous tensors.  Strides are >= 0 (SFDA_ERR_SHAPE otherwise), that of an
+ * axis of one element is not looked at; inputs may
  * repeat elements (stride 0), an output's elements must lie apart (SFDA_ERR_ALIAS).  Pointers need
  * only their element's alignment (SFDA_ERR_ALIGN).  No output may share memory with an input or
  * another output but where a call says so (SFDA_ERR_ALIAS; slices of one buffer with the same

@@ -176,16 +176,16 @@ struct Call {
     }
 };
 
-// strides of a contiguous [B, H, T, D] tensor, or the caller's
-void strides3(ll (&out)[3], const ll* given, int which, ll H, ll T, ll D)
+// The strides of a tensor's outer axes: the caller's, or a contiguous tensor's.  Those of axes of one element, which a caller may
+// give any value, are 0 from here on: the scan reaches its blocks' rows by whole blocks, and a token that is alone lies in one.
+template <int N> void strides_of(ll (&out)[N], const ll* given, const ll (&n)[N], const ll (&contiguous)[N])
 {
-    if (given != nullptr) {
-        for (int i = 0; i < 3; ++i) out[i] = given[3 * which + i];
-    } else {
-        out[0] = H * T * D;
-        out[1] = T * D;
-        out[2] = D;
-    }
+    for (int i = 0; i < N; ++i) out[i] = n[i] <= 1 ? 0 : given != nullptr ? given[i] : contiguous[i];
+}
+// [B, H, T, D], the `which`-th of a call
+void strides3(ll (&out)[3], const ll* given, int which, ll B, ll H, ll T, ll D)
+{
+    strides_of(out, given != nullptr ? given + 3 * which : nullptr, {B, H, T}, {H * T * D, T * D, D});
 }
 
 // compute units of the current device, looked up once for each
@@ -210,7 +210,7 @@ bool decay_sizes(int B, int H, int T, int dk, int dv)
 }
 
 // a block's rows (at most 64 tokens) are addressed with 32-bit byte offsets
-bool rows_fit(const ll (&st)[3], int T, ll e) { return T <= 1 || st[2] <= ((1LL << 31) - 65536) / (64 * e); }
+bool rows_fit(const ll (&st)[3], ll e) { return st[2] <= ((1LL << 31) - 65536) / (64 * e); }
 
 // Segments of a sequence.  A scan without them takes c us for 64 tokens, whatever the number of heads, until the workgroups fill the
 // compute units.  Cut into S parts it takes a pass for their states (another s us) and a join, all of them on an S-th of the
@@ -282,10 +282,10 @@ sfda_status_t sfda_rotary(const void* q, const void* k, const float* cos, const 
     const double H = static_cast<double>(Hq) + Hk, rows = std::max((H + 6) / 4 * T, H * ((T + 3.) / 4)) * B;
     if (rows * (D * e / 16. + 3) >= 4294967296. - 1024.) return SFDA_ERR_SHAPE;
     sfda::RotaryLaunch L{};
-    strides3(L.q_s, strides, 0, Hq, T, D);
-    strides3(L.k_s, strides, 1, Hk, T, D);
-    strides3(L.qo_s, strides, 2, Hq, T, D);
-    strides3(L.ko_s, strides, 3, Hk, T, D);
+    strides3(L.q_s, strides, 0, B, Hq, T, D);
+    strides3(L.k_s, strides, 1, B, Hk, T, D);
+    strides3(L.qo_s, strides, 2, B, Hq, T, D);
+    strides3(L.ko_s, strides, 3, B, Hk, T, D);
     Call c;
     const int iq = c.input(box(q, e, D, {B, Hq, T}, L.q_s), e);
     const int ik = c.input(box(k, e, D, {B, Hk, T}, L.k_s), e);
@@ -328,11 +328,11 @@ sfda_status_t sfda_decay_attn_fwd(const void* q, const void* k, const void* v, c
     if (heads == 0) return SFDA_OK;
     sfda::DecayLaunch L{};
     sfda::DecayRole& R = L.role[0];
-    strides3(R.q_s, strides, 0, H, T, dk);
-    strides3(R.k_s, strides, 1, H, T, dk);
-    strides3(R.v_s, strides, 2, H, T, dv);
-    strides3(R.o_s, strides, 3, H, T, dv);
-    if (!rows_fit(R.q_s, T, e) || !rows_fit(R.k_s, T, e) || !rows_fit(R.v_s, T, e) || !rows_fit(R.o_s, T, e)) return SFDA_ERR_SHAPE;
+    strides3(R.q_s, strides, 0, B, H, T, dk);
+    strides3(R.k_s, strides, 1, B, H, T, dk);
+    strides3(R.v_s, strides, 2, B, H, T, dv);
+    strides3(R.o_s, strides, 3, B, H, T, dv);
+    if (!rows_fit(R.q_s, e) || !rows_fit(R.k_s, e) || !rows_fit(R.v_s, e) || !rows_fit(R.o_s, e)) return SFDA_ERR_SHAPE;
     const size_t need = sfda_decay_attn_fwd_workspace_bytes(B, H, T, dk, dv, dtype);
     const bool cut = need > 0 && workspace != nullptr && workspace_bytes >= need;
     Call c;
@@ -382,15 +382,15 @@ sfda_status_t sfda_decay_attn_bwd(const void* q, const void* k, const void* v, c
     const bool bf16 = dtype == SFDA_BF16;
     if (heads == 0) return SFDA_OK;
     ll qs[3], ks[3], vs[3], gs[3], dqs[3], dks[3], dvs[3];
-    strides3(qs, strides, 0, H, T, dk);
-    strides3(ks, strides, 1, H, T, dk);
-    strides3(vs, strides, 2, H, T, dv);
-    strides3(gs, strides, 3, H, T, dv);
-    strides3(dqs, strides, 4, H, T, dk);
-    strides3(dks, strides, 5, H, T, dk);
-    strides3(dvs, strides, 6, H, T, dv);
+    strides3(qs, strides, 0, B, H, T, dk);
+    strides3(ks, strides, 1, B, H, T, dk);
+    strides3(vs, strides, 2, B, H, T, dv);
+    strides3(gs, strides, 3, B, H, T, dv);
+    strides3(dqs, strides, 4, B, H, T, dk);
+    strides3(dks, strides, 5, B, H, T, dk);
+    strides3(dvs, strides, 6, B, H, T, dv);
     for (const auto* st : {&qs, &ks, &vs, &gs, &dqs, &dks, &dvs})
-        if (!rows_fit(*st, T, e)) return SFDA_ERR_SHAPE;
+        if (!rows_fit(*st, e)) return SFDA_ERR_SHAPE;
     const size_t need = sfda_decay_attn_bwd_workspace_bytes(B, H, T, dk, dv, dtype);
     const bool cut = need > 0 && workspace != nullptr && workspace_bytes >= need;
     Call c;
@@ -448,8 +448,7 @@ sfda_status_t sfda_decay_attn_step(const void* q, const void* k, const void* v, 
     ll (*to[4])[2] = {&L.q_s, &L.k_s, &L.v_s, &L.o_s};
     for (int i = 0; i < 4; ++i) {
         const ll D = i < 2 ? dk : dv;
-        (*to[i])[0] = strides != nullptr ? strides[2 * i] : H * D;
-        (*to[i])[1] = strides != nullptr ? strides[2 * i + 1] : D;
+        strides_of(*to[i], strides != nullptr ? strides + 2 * i : nullptr, {B, H}, {H * D, D});
     }
     Call c;
     c.input(box(q, e, dk, {B, H}, L.q_s), e);
@@ -471,11 +470,10 @@ static bool norm_sizes(int B, int H, int T, int D)
 }
 
 // strides [x: b, h, t][then pairs b, t], or contiguous ones
-static void norm_strides(ll (&x)[3], const ll* given, ll H, ll T, ll D) { strides3(x, given, 0, H, T, D); }
-static void pair_strides(ll (&out)[2], const ll* given, int at, ll H, ll T, ll D)
+static void norm_strides(ll (&x)[3], const ll* given, ll B, ll H, ll T, ll D) { strides3(x, given, 0, B, H, T, D); }
+static void pair_strides(ll (&out)[2], const ll* given, int at, ll B, ll H, ll T, ll D)
 {
-    out[0] = given != nullptr ? given[at] : T * H * D;
-    out[1] = given != nullptr ? given[at + 1] : H * D;
+    strides_of(out, given != nullptr ? given + at : nullptr, {B, T}, {T * H * D, H * D});
 }
 
 sfda_status_t sfda_group_norm(const void* x, const float* weight, const float* bias, const void* gate, void* y, int B, int H,
@@ -487,9 +485,9 @@ sfda_status_t sfda_group_norm(const void* x, const float* weight, const float* b
     if (B == 0 || H == 0 || T == 0) return SFDA_OK;
     const ll e = esize(dtype), HD = static_cast<ll>(H) * D;
     sfda::NormLaunch L{};
-    norm_strides(L.x_s, strides, H, T, D);
-    pair_strides(L.g_s, strides, 3, H, T, D);
-    pair_strides(L.y_s, strides, 5, H, T, D);
+    norm_strides(L.x_s, strides, B, H, T, D);
+    pair_strides(L.g_s, strides, 3, B, H, T, D);
+    pair_strides(L.y_s, strides, 5, B, H, T, D);
     Call c;
     c.input(box(x, e, D, {B, H, T}, L.x_s), e);
     c.input(flat(weight, 4 * HD), 4, false);
@@ -520,12 +518,11 @@ sfda_status_t sfda_group_norm_bwd(const void* dy, const void* x, const float* we
     const ll e = esize(dtype), HD = static_cast<ll>(H) * D;
     const size_t need = dweight != nullptr || dbias != nullptr ? sfda_group_norm_bwd_workspace_bytes(B, H, T, D, dtype) : 0;
     sfda::NormLaunch L{};
-    norm_strides(L.x_s, strides, H, T, D);
-    pair_strides(L.g_s, strides, 3, H, T, D);
-    pair_strides(L.y_s, strides, 5, H, T, D);
-    if (strides != nullptr) std::copy(strides + 7, strides + 10, L.dx_s);
-    else norm_strides(L.dx_s, nullptr, H, T, D);
-    pair_strides(L.dg_s, strides, 10, H, T, D);
+    norm_strides(L.x_s, strides, B, H, T, D);
+    pair_strides(L.g_s, strides, 3, B, H, T, D);
+    pair_strides(L.y_s, strides, 5, B, H, T, D);
+    norm_strides(L.dx_s, strides != nullptr ? strides + 7 : nullptr, B, H, T, D);
+    pair_strides(L.dg_s, strides, 10, B, H, T, D);
     Call c;
     c.input(box(dy, e, HD, {B, T}, L.y_s), e);
     c.input(box(x, e, D, {B, H, T}, L.x_s), e);

@@ -289,6 +289,34 @@ def test_decay_attn_bwd_in_two_launches(B, H, T, dk, dv, dtype):
     test_decay_attn_bwd(B, H, T, dk, dv, dtype, "bthd", True, None)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("dk,dv", [(128, 64), (33, 74)])
+@pytest.mark.parametrize("stride", [1, 1 << 24, (1 << 26) + 8, 1 << 40])
+def test_decay_attn_one_token_of_any_stride(dtype, dk, dv, stride):
+    """One token: the stride of the tokens is whatever the caller's view has, and reaches no address."""
+    import torch
+    from paper_2607_11897_amd import sfda
+    say("decay_attn one token", dtype, dk, dv, stride)
+    x = attn(17, 2, 3, 1, dk, dv, dtype, True, grads=True)
+
+    def far(t):
+        st = t.stride()
+        return t.as_strided(t.shape, (st[0], st[1], stride, st[3]), t.storage_offset())
+    b = {n: Buf(x[n].shape, dt(dtype), "bhtd", x[n]) for n in ("q", "k", "v", "dO")}
+    out = {n: Buf(x[m].shape, dt(dtype), "bhtd") for n, m in (("o", "v"), ("dq", "q"), ("dk", "k"), ("dv", "v"))}
+    i, w = {n: far(t.t) for n, t in b.items()}, {n: far(t.t) for n, t in out.items()}
+    _, S = sfda.decay_attn_fwd(i["q"], i["k"], i["v"], f32(x["g"]), f32(x["S0"]), scale=0.5, o=w["o"])
+    got = sfda.decay_attn_bwd(i["q"], i["k"], i["v"], f32(x["g"]), f32(x["S0"]), i["dO"], f32(x["dS_T"]), scale=0.5,
+                              **{n: w[n] for n in ("dq", "dk", "dv")})
+    torch.cuda.synchronize()
+    for n, t in out.items():
+        t.check(n)
+    o, S_ref = O.decay_attn(x["q"], x["k"], x["v"], x["g"], x["S0"], 0.5)
+    ref = O.decay_attn_backward(x["q"], x["k"], x["v"], x["g"], x["S0"], x["dO"], x["dS_T"], 0.5) | dict(o=o)
+    assert all(rel_err(out[n].numpy(), ref[n]) <= ATTN[dtype] for n in out)
+    assert rel_err(S.double().cpu().numpy(), S_ref) <= SUM and rel_err(got["dS0"].double().cpu().numpy(), ref["dS0"]) <= SUM
+
+
 def test_decay_attn_bwd_against_differences():
     """Directional differences of the GPU's own forward in float32."""
     import torch
