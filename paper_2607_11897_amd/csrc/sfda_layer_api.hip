@@ -32,7 +32,7 @@ Box box(const void* p, ll e, ll D, std::initializer_list<ll> n, const ll* stride
     int i = 0;
     for (ll m : n) {
         b.n[i] = m;
-        b.s[i] = strides[i] * e;
+        b.s[i] = strides[i] < 0 || strides[i] > FAR ? -1 : strides[i] * e;      // (-1: refused by extent)
         ++i;
     }
     b.n[i] = D * e;
@@ -204,9 +204,9 @@ constexpr int MAX_D = 256;              // key and value channels of a decay att
 bool decay_sizes(int B, int H, int T, int dk, int dv)
 {
     if (B < 0 || H < 0 || T < 0 || dk < 1 || dk > MAX_D || dv < 1 || dv > MAX_D) return false;
-    // at most 8 threads for a head and value column of a role, in launches of less than 2^32; tokens are counted in 32 bits with
-    // room for a block
-    return static_cast<ll>(B) * H * 3 * MAX_D * 8 < (1LL << 32) && T <= INT_MAX - 1024;
+    // at most 8 threads for a head and value column of a role, in launches of less than 2^32 (by a division: B H alone may have 62
+    // bits); tokens are counted in 32 bits with room for a block
+    return static_cast<ll>(B) * H <= ((1LL << 32) - 1) / (3 * MAX_D * 8) && T <= INT_MAX - 1024;
 }
 
 // a block's rows (at most 64 tokens) are addressed with 32-bit byte offsets

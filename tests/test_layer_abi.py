@@ -111,6 +111,21 @@ def test_overlaps_against_every_element(lib):
     assert met > 500
 
 
+def test_sizes_and_strides_out_of_range(lib):
+    """Products of sizes and of strides that no 64-bit count holds are refused, not formed."""
+    M, N = (1 << 31) - 1, 1 << 30
+    for B, H in ((M, M), (N, N), (1 << 22, N)):
+        assert fwd(lib, B=B, H=H) == 2 and fwd(lib, B=B, H=H, T=0) == 2 and bwd(lib, B=B, H=H) == 2
+        assert lib.sfda_decay_attn_fwd_workspace_bytes(B, H, 4096, 16, 8, 0) == 0
+        assert lib.sfda_decay_attn_bwd_workspace_bytes(B, H, 4096, 16, 8, 1) == 0
+    for far in (1 << 46, 1 << 61, 1 << 62, (1 << 62) + 16, (1 << 63) - 1):
+        assert fwd(lib, B=2, strides=arr(*([far, 16, 32] + [256, 16, 32] + [128, 8, 16] * 2))) == 2, far
+        assert fwd(lib, B=2, strides=arr(*([256, 16, 32] * 2 + [128, 8, 16] + [far, 8, 16]))) == 2, far
+        assert rot(lib, pos=7 * A, bits=64, pstride=far, B=2) == 2, far
+    for T, H, D in ((M, 1 << 20, 1024), (M, 1 << 23, 128)):
+        assert norm(lib, B=M, T=T, H=H, D=D) == 2 and norm_bwd(lib, B=M, T=T, H=H, D=D) == 2
+
+
 def bwd(lib, **kw):
     a = dict(q=A, k=2 * A, v=3 * A, g=4 * A, n=None, S0=5 * A, dO=6 * A, dS_T=7 * A, dq=8 * A, dk_=9 * A, dv_=10 * A, dS0=11 * A, B=1, H=2,
              T=8, dk=16, dv=8, dt=0) | kw
