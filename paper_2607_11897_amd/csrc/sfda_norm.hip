@@ -128,7 +128,9 @@ __device__ __forceinline__ void norm_rows(const NormLaunch& L, int lpg, int stri
                 x[k][i] = d;
                 sq = __builtin_fmaf(d, d, sq);
             }
-        const float rstd = __builtin_amdgcn_rsqf(group_sum(sq, lpg) * inv + L.eps);
+        float rstd = __builtin_amdgcn_rsqf(group_sum(sq, lpg) * inv + L.eps);
+        // (a group past the last row may hold none at all: with eps = 0 its x^ would be 0 * inf, which no factor 0 of dw takes back)
+        if (BWD && !there) rstd = 0.f;
         if constexpr (!BWD) {
             E* yp = static_cast<E*>(L.y) + tb * L.y_s[0] + tt * L.y_s[1] + hc;
 #pragma unroll

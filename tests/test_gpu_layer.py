@@ -485,6 +485,31 @@ def test_group_norm_extremes():
     assert torch.equal(torch.nan_to_num(dirty)[0, 2:], clean[0, 2:])
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,H,T,D,gate,act", [(1, 2, 1, 128, True, "silu"), (1, 3, 5, 64, False, "silu"), (2, 1, 3, 8, True, "none"),
+                                              (1, 1, 40, 2048, False, "none"), (3, 2, 70, 33, True, "silu")])
+def test_group_norm_without_eps(B, H, T, D, gate, act, dtype):
+    """eps = 0 where every group has a variance: lanes that have no row add nothing to the weights' gradients."""
+    import torch
+    from paper_2607_11897_amd import sfda
+    say("group_norm eps 0", B, H, T, D, gate, act, dtype)
+    rng = np.random.Generator(np.random.PCG64(D + T))
+    x, dy = stored(rng, (B, H, T, D), dtype), stored(rng, (B, T, H * D), dtype)
+    z = stored(rng, dy.shape, dtype) if gate else None
+    w, b = (1 + 0.3 * rng.standard_normal(H * D)).astype(np.float32), rng.standard_normal(H * D).astype(np.float32)
+    X, Y = f32(x).to(dt(dtype)), f32(dy).to(dt(dtype))
+    Z = f32(z).to(dt(dtype)) if gate else None
+    y = sfda.group_norm(X, f32(w), f32(b), Z, activation=act, eps=0.0)
+    got = sfda.group_norm_bwd(Y, X, f32(w), f32(b), Z, activation=act, eps=0.0)
+    torch.cuda.synchronize()
+    assert rel_err(y.double().cpu().numpy(), O.group_norm(x, w, b, z, act, 0.0)) <= NORM[dtype]
+    ref = O.group_norm_backward(dy, x, w, b, z, act, 0.0)
+    for name in ("dx", "dgate", "dweight", "dbias"):
+        if got[name] is not None:
+            bar = SUM if name in ("dweight", "dbias") else NORM[dtype]
+            assert rel_err(got[name].double().cpu().numpy(), ref[name]) <= bar, name
+
+
 # --------------------------------------------------------------------------- streams and graphs
 
 def test_other_stream_and_graph():
