@@ -32,6 +32,16 @@ __device__ __forceinline__ float group_sum(float x, int lpg)
     return x;
 }
 
+// 1 / sqrt(x), x >= 0.  The hardware's instruction takes a subnormal for 0; a variance below 2^-126 (values of 1e-19) is one, and
+// with eps = 0 it counts.  The scaling takes no time that shows (bfloat16 B8 H16 T4096 d 128, in turn: forward 95.4 us and 95.0
+// without, backward 147.5 and 147.6).
+__device__ __forceinline__ float inverse_root(float x)
+{
+    const bool small = x < 0x1p-100f;
+    const float r = __builtin_amdgcn_rsqf(small ? x * 0x1p64f : x);
+    return small ? r * 0x1p32f : r;
+}
+
 // act and its derivative.  The sigmoid by the hardware's exponential and reciprocal (an ulp each, and |z| 2^-24 of the
 // exponent's own rounding); at infinities the limits: the product with 0 is taken of a finite number.
 template <bool SILU> __device__ __forceinline__ void act(float z, float& f, float& df)
@@ -128,7 +138,7 @@ __device__ __forceinline__ void norm_rows(const NormLaunch& L, int lpg, int stri
                 x[k][i] = d;
                 sq = __builtin_fmaf(d, d, sq);
             }
-        float rstd = __builtin_amdgcn_rsqf(group_sum(sq, lpg) * inv + L.eps);
+        float rstd = inverse_root(group_sum(sq, lpg) * inv + L.eps);
         // (a group past the last row may hold none at all: with eps = 0 its x^ would be 0 * inf, which no factor 0 of dw takes back)
         if (BWD && !there) rstd = 0.f;
         if constexpr (!BWD) {

@@ -510,6 +510,24 @@ def test_group_norm_without_eps(B, H, T, D, gate, act, dtype):
             assert rel_err(got[name].double().cpu().numpy(), ref[name]) <= bar, name
 
 
+def test_group_norm_subnormal_variance():
+    """eps = 0 and values of 2^-65: the variance is a subnormal of 19 bits (its sum's terms are rounded to multiples of 2^-149,
+    2^-20 of it), the results are ordinary numbers; dx is some 2^65."""
+    import torch
+    from paper_2607_11897_amd import sfda
+    say("group_norm subnormal variance")
+    rng = np.random.Generator(np.random.PCG64(6))
+    x, dy = stored(rng, (2, 3, 21, 128), "f32"), stored(rng, (2, 21, 384), "f32")
+    x = np.asarray(x, np.float32) * np.float32(2.0 ** -65)
+    w = (1 + 0.3 * rng.standard_normal(384)).astype(np.float32)
+    y = sfda.group_norm(f32(x), f32(w), eps=0.0)
+    got = sfda.group_norm_bwd(f32(dy), f32(x), f32(w), eps=0.0)
+    torch.cuda.synchronize()
+    assert rel_err(y.double().cpu().numpy(), O.group_norm(x, w, eps=0.0)) <= SUM
+    ref = O.group_norm_backward(dy, x, w, eps=0.0)
+    assert all(rel_err(got[n].double().cpu().numpy(), ref[n]) <= SUM for n in ("dx", "dweight"))
+
+
 # --------------------------------------------------------------------------- streams and graphs
 
 def test_other_stream_and_graph():
