@@ -591,8 +591,9 @@ def rotary_tables(positions: int, rot: int, *, base: float = 10000.0, scaling: O
       dict(kind="yarn", factor=s, length=L, fast=32, slow=1, amplitude=None)
                                                  pairs that turn more than `fast` times over L keep their frequency,
                                                  those that turn less than `slow` times are divided by s, linear in the
-                                                 pair's number between; both tables times the amplitude
-                                                 (0.1 log s + 1 if None)."""
+                                                 pair's number between (from the whole number below the pair of `fast`
+                                                 turns to the one above that of `slow`, rot - 1 at most); both tables
+                                                 times the amplitude (0.1 log s + 1 if None)."""
     import math
     import torch
     if rot < 2 or rot % 2 or positions < 1:
@@ -615,7 +616,8 @@ def rotary_tables(positions: int, rot: int, *, base: float = 10000.0, scaling: O
             # the (fractional) pair that turns n times over the length
             at = lambda n: rot * math.log(length / (2 * math.pi * n)) / (2 * math.log(base))  # noqa: E731
             low = max(math.floor(at(float(scaling.get("fast", 32)))), 0)
-            high = min(math.ceil(at(float(scaling.get("slow", 1)))), rot // 2 - 1)
+            # (an end past the last pair stays there: that pair turns more than `slow` times and is divided in part only)
+            high = min(math.ceil(at(float(scaling.get("slow", 1)))), rot - 1)
             keep = 1.0 - ((pair - low) / max(high - low, 1e-3)).clamp(0.0, 1.0)
             freq = freq * keep + freq / s * (1.0 - keep)
             amplitude = scaling.get("amplitude")

@@ -173,3 +173,26 @@ def test_planted_mistakes_fail(mistake):
             if mistake != "early_state":
                 o2[0, h, t] = (1.0 if mistake == "no_scale" else 0.7) * (q[0, h, t] @ S2[0, h])
     assert np.max(np.abs(o2 - o)) > 1e-2 * np.max(np.abs(o))
+
+
+@pytest.mark.parametrize("base,rot,length,factor", [(10000.0, 128, 4096, 16.0), (10000.0, 128, 131072, 4.0), (10000.0, 64, 1 << 20, 8.0),
+                                                    (500000.0, 128, 131072, 2.0), (100.0, 32, 262144, 4.0)])
+def test_yarn_ramp(base, rot, length, factor):
+    """Every pair's frequency by its number of turns over the length: kept past `fast` turns, divided below `slow`, between them on
+    one line in the pair's number whose ends are the whole numbers around those of `fast` and `slow` turns."""
+    fast, slow = 32.0, 1.0
+    c, s = tables(2, rot, base=base, scaling=dict(kind="yarn", factor=factor, length=length, fast=fast, slow=slow, amplitude=1.0))
+    got = np.arctan2(s[1], c[1])                        # one position: the frequencies, below pi
+    for i in range(rot // 2):
+        f = base ** (-2 * i / rot)
+        # the pair of n turns: length base^(-2 i / rot) = 2 pi n
+        ends = [rot / 2 * math.log(length / (2 * math.pi * n), base) for n in (fast, slow)]
+        lo, hi = max(math.floor(ends[0]), 0), min(math.ceil(ends[1]), rot - 1)
+        part = min(max((i - lo) / (hi - lo), 0.0), 1.0)
+        # float32 of tables of values near 1 and of f: 2^-24 each
+        assert abs(got[i] - (f * (1 - part) + f / factor * part)) <= 2e-7 * max(f, 1e-3), i
+        turns = length * f / (2 * math.pi)
+        if turns < 0.9 * slow:
+            assert abs(got[i] * factor - f) <= 2e-7 * factor * max(f, 1e-3)
+        elif turns > slow * base ** (2 / rot) and i < hi:
+            assert got[i] > f / factor                  # not divided in full
