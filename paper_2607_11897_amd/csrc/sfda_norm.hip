@@ -233,23 +233,29 @@ __global__ __launch_bounds__(NT) void norm_kernel(NormLaunch L, int lpg, int str
     }
 }
 
-// dweight and dbias: the strips' sums.  A workgroup for 64 of them; its four waves take every fourth strip, and their parts
-// are added in order.
+// dweight and dbias: the strips' sums.  A workgroup for 64 of them at a time; its four waves take every fourth strip, and their
+// parts are added in order.
+constexpr long long JOIN_GROUPS = 1 << 20;      // (a launch holds less than 2^32 threads)
 __global__ __launch_bounds__(NT) void norm_join_kernel(NormLaunch L, int strips)
 {
     __shared__ float part[NT];
-    const long long HD = static_cast<long long>(L.H) * L.D, at = static_cast<long long>(blockIdx.x) * 64 + (threadIdx.x & 63);
-    float s = 0.f;
-    if (at < 2 * HD) {
+    const long long HD = static_cast<long long>(L.H) * L.D;
+    for (long long base = static_cast<long long>(blockIdx.x) * 64; base < 2 * HD; base += static_cast<long long>(gridDim.x) * 64) {
+        const long long at = base + (threadIdx.x & 63);
+        float s = 0.f;
+        if (at < 2 * HD) {
 #pragma unroll 8
-        for (int i = threadIdx.x >> 6; i < strips; i += 4) s += L.partial[static_cast<long long>(i) * 2 * HD + at];
+            for (int i = threadIdx.x >> 6; i < strips; i += 4) s += L.partial[static_cast<long long>(i) * 2 * HD + at];
+        }
+        part[threadIdx.x] = s;
+        __syncthreads();
+        if (threadIdx.x < 64 && at < 2 * HD) {
+            s = part[threadIdx.x] + part[threadIdx.x + 64] + part[threadIdx.x + 128] + part[threadIdx.x + 192];
+            float* out = at < HD ? L.dweight : L.dbias;
+            if (out != nullptr) out[at < HD ? at : at - HD] = s;
+        }
+        __syncthreads();
     }
-    part[threadIdx.x] = s;
-    __syncthreads();
-    if (threadIdx.x >= 64 || at >= 2 * HD) return;
-    s = part[threadIdx.x] + part[threadIdx.x + 64] + part[threadIdx.x + 128] + part[threadIdx.x + 192];
-    float* out = at < HD ? L.dweight : L.dbias;
-    if (out != nullptr) out[at < HD ? at : at - HD] = s;
 }
 
 struct Shape { int lpg, v; };
@@ -278,8 +284,8 @@ template <typename E, bool BWD> hipError_t go(const NormLaunch& L, hipStream_t s
     }
     hipError_t e = hipGetLastError();
     if (BWD && e == hipSuccess && L.partial != nullptr) {
-        const long long n = 2LL * L.H * L.D;
-        hipLaunchKernelGGL(norm_join_kernel, dim3(static_cast<unsigned>((n + 63) / 64)), block, 0, st, L, strips);
+        const long long need = (2LL * L.H * L.D + 63) / 64;
+        hipLaunchKernelGGL(norm_join_kernel, dim3(static_cast<unsigned>(need < JOIN_GROUPS ? need : JOIN_GROUPS)), block, 0, st, L, strips);
         e = hipGetLastError();
     }
     return e;

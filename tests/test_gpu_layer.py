@@ -528,6 +528,28 @@ def test_group_norm_subnormal_variance():
     assert all(rel_err(got[n].double().cpu().numpy(), ref[n]) <= SUM for n in ("dx", "dweight"))
 
 
+def test_group_norm_bwd_many_channels():
+    """2^29 channels in all: more sums of weight gradients than one launch has places for.  One token: dweight = dy x^, dbias = dy."""
+    import torch
+    from paper_2607_11897_amd import sfda
+    say("group_norm_bwd 2^29 channels")
+    H, D = 1 << 18, 2048
+    gen = torch.Generator(device="cuda").manual_seed(8)
+    x = torch.randn(1, H, 1, D, generator=gen, device="cuda", dtype=torch.bfloat16)
+    dy = torch.randn(1, 1, H * D, generator=gen, device="cuda", dtype=torch.bfloat16)
+    w = torch.ones(H * D, device="cuda")
+    got = sfda.group_norm_bwd(dy, x, w, w)
+    torch.cuda.synchronize()
+    del w
+    assert torch.equal(got["dbias"], dy.view(-1).float())
+    for lo in range(0, H, H // 16):
+        rows = slice(lo, lo + H // 16)
+        f = x[0, rows, 0].double()
+        f = (f - f.mean(-1, keepdim=True)) / (f.var(-1, unbiased=False, keepdim=True) + 1e-5).sqrt()
+        want = f * dy.view(H, D)[rows].double()
+        assert float((got["dweight"].view(H, D)[rows].double() - want).abs().max()) <= SUM * float(want.abs().max())
+
+
 # --------------------------------------------------------------------------- streams and graphs
 
 def test_other_stream_and_graph():
