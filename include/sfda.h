@@ -440,7 +440,7 @@ sfda_status_t sfda_rotary(const void* q, const void* k, const float* cos, const 
  *   that give o; the state itself is carried in float32 from products exact to 2^-24.
  *   float32: products to 2^-22 (operands as three bfloat16 parts), sums in float32.
  *   A token with a value that is not finite makes the rows of its block (32 or 64 tokens) before it NaN
- *   too; in float32 an infinity acts as NaN.
+ *   too.  What an infinity reaches may be NaN or an infinity, for both types: the parts of a value are inf - inf.
  */
 size_t sfda_decay_attn_fwd_workspace_bytes(int B, int H, int T, int dk, int dv,
                                            sfda_dtype_t dtype);

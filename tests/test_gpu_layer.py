@@ -237,6 +237,28 @@ def test_decay_attn_not_finite(dtype):
     assert np.array_equal(o, clean[0]) and np.array_equal(S, clean[1])
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("name,at", [("v", 3), ("k", 5)])
+def test_decay_attn_infinite(dtype, name, at):
+    """An infinite value or key: its column, or with a key every column, of the later blocks is not finite, nor its column or row of
+    S_T.  The earlier blocks, the other heads and sequences and, with a value, the other columns keep their results."""
+    say("decay_attn_fwd inf", dtype, name)
+    x = attn(15, 2, 3, 256, 32, 32, dtype)
+    x["g"][1] = -0.01
+    clean = run_fwd(x, dtype, "bhtd", 1.0)
+    x[name][1, 1, 150, at] = np.inf
+    o, S = run_fwd(x, dtype, "bhtd", 1.0)
+    hit = [at] if name == "v" else list(range(32))
+    assert not np.isfinite(o[1, 1, 192:, hit]).any()
+    assert not np.isfinite(S[1, 1][:, hit] if name == "v" else S[1, 1, at]).any()
+    o[1, 1, 128:, hit] = clean[0][1, 1, 128:, hit]
+    if name == "v":
+        S[1, 1][:, hit] = clean[1][1, 1][:, hit]
+    else:
+        S[1, 1, at] = clean[1][1, 1, at]
+    assert np.array_equal(o, clean[0]) and np.array_equal(S, clean[1])
+
+
 def run_bwd(x, dtype, layout, scale, want_dS0=True, poison=None):
     import torch
     from paper_2607_11897_amd import sfda
