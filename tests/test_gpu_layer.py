@@ -339,6 +339,56 @@ def test_decay_attn_one_token_of_any_stride(dtype, dk, dv, stride):
     assert rel_err(S.double().cpu().numpy(), S_ref) <= SUM and rel_err(got["dS0"].double().cpu().numpy(), ref["dS0"]) <= SUM
 
 
+def by_token(x, scale):
+    """The recurrence and its reverse sweep in float64, all heads at a time: o, S_T, dq, dk, dv, dS0."""
+    import torch
+    q, k, v, dO = (dev(x[n]) for n in ("q", "k", "v", "dO"))
+    T, c = q.shape[2], scale
+    lam = torch.exp(dev(x["g"].astype(np.float64)))[None, :, None, None]
+    n = torch.full((q.shape[0],), T, device="cuda") if x["lengths"] is None else dev(np.clip(x["lengths"], 0, T))
+    o, dq, dk, dv = (torch.zeros_like(t) for t in (v, q, k, v))
+    S, G = dev(x["S0"]), dev(x["dS_T"])
+    for t in range(T):
+        on = (t < n)[:, None, None, None]
+        S = torch.where(on, lam * S + k[:, :, t, :, None] * v[:, :, t, None, :], S)
+        o[:, :, t] = torch.where(on[..., 0], c * (S * q[:, :, t, :, None]).sum(2), 0.0)
+        dq[:, :, t] = torch.where(on[..., 0], c * (S * dO[:, :, t, None, :]).sum(3), 0.0)
+    for t in range(T - 1, -1, -1):
+        on = (t < n)[:, None, None, None]
+        U = G + c * q[:, :, t, :, None] * dO[:, :, t, None, :]
+        dk[:, :, t] = torch.where(on[..., 0], (U * v[:, :, t, None, :]).sum(3), 0.0)
+        dv[:, :, t] = torch.where(on[..., 0], (U * k[:, :, t, :, None]).sum(2), 0.0)
+        G = torch.where(on, lam * U, G)
+    torch.cuda.synchronize()
+    return {m: t.cpu().numpy() for m, t in (("o", o), ("S_T", S), ("dq", dq), ("dk", dk), ("dv", dv), ("dS0", G))}
+
+
+# (more workgroups than compute units, so that a block's state has one buffer, and several blocks a sequence; few heads, so
+# that sequences are cut, into segments of several blocks, and lengths that end inside them)
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,H,T,dk,dv,cut,lengths", [
+    (9, 16, 300, 128, 128, False, None), (9, 16, 260, 126, 127, False, None), (9, 16, 200, 128, 64, False, [200, 0, 1, 64, 65, 127, 128, 129, 199]),
+    (12, 16, 131, 64, 72, False, None), (5, 16, 150, 256, 200, False, None),
+    (4, 4, 4001, 128, 128, True, [4001, 1900, 300, 0]), (2, 8, 3900, 88, 74, True, [3900, 2477]), (1, 3, 6000, 200, 256, True, None)])
+def test_decay_attn_many_blocks(B, H, T, dk, dv, cut, lengths, dtype):
+    from paper_2607_11897_amd import sfda
+    say("decay_attn many blocks", B, H, T, dk, dv, cut, lengths, dtype)
+    for f, states in ((sfda.decay_attn_fwd_workspace_bytes, 1), (sfda.decay_attn_bwd_workspace_bytes, 3)):
+        segments = f(B, H, T, dk, dv, dtype) // (4 * states * B * H * dk * dv)
+        assert (1 < segments <= T // 128) if cut else segments == 0
+    x = attn(61 + T, B, H, T, dk, dv, dtype, True, lengths, grads=True)
+    scale = dk ** -0.5
+    ref = by_token(x, scale)
+    poison = float("nan") if lengths is not None else None
+    o, S = run_fwd(x, dtype, "bthd", scale, poison)
+    got = run_bwd(x, dtype, "bthd", scale, poison=poison) | dict(o=o, S_T=S)
+    err = {m: rel_err(got[m], ref[m]) for m in ref}
+    say(err)
+    assert all(err[m] <= (SUM if m in ("S_T", "dS0") else ATTN[dtype]) for m in ref)
+    for i, n in enumerate(lengths or []):
+        assert not any(got[m][i, :, n:].any() for m in ("o", "dq", "dk", "dv"))
+
+
 def test_decay_attn_bwd_against_differences():
     """Directional differences of the GPU's own forward in float32."""
     import torch
