@@ -82,3 +82,11 @@ def test_training_learns():
     from decay_layer import train
     losses = train(steps=25)
     assert losses[-1] < 0.9 * losses[0] and all(b < 1.5 * losses[0] for b in losses)
+
+
+def test_training_learns_to_remember():
+    """The wanted outputs have variance 1 and say nothing about their own tokens' inputs: without memory zeros are best, a loss of
+    about 1.  Weights that only shrink the output, or gradients of queries, keys or values that are wrong, stay there."""
+    from decay_layer import train
+    losses = train()
+    assert sum(losses[-10:]) / 10 < 0.7 and all(b < 1.5 * losses[0] for b in losses)
