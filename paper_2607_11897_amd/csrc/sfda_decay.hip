@@ -7,6 +7,11 @@
 // The backward is three scans of the same form (dL/dq forward on (dO, v, k) with the state
 // transposed; dL/dk on (v, dO, q) and dL/dv on (k, q, dO) from the last token to the first), run as
 // roles of one launch.
+//
+// Times, as calls among others (a call alone, with a wait behind it, takes 12 to 25 us more): B8 H16 d 128, bfloat16 T4096 forward
+// 151 to 162 us (by the card) and backward 403 to 409, float32 T2048 forward 234 and backward 626.  A chain of blocks bounds them, 2.4 us for 64 tokens in
+// bfloat16: products, LDS reads and vector arithmetic of a block wait for each other with one or two waves on a SIMD.  Below,
+// choices are given as ratios of both sides' times, measured in turn on one card.
 #include "sfda_device.h"
 #include "sfda_layer.h"
 #include "sfda_vec.h"
@@ -44,7 +49,7 @@ template <typename E> __device__ __forceinline__ u32x4 short_row(const char* p, 
 // What the element type decides.  The matrix cores take bfloat16 operands.  A float32 is the sum of three bfloat16 (its 24 bits,
 // 8 in each), so float32 tensors lie in LDS as PL = 3 planes, and a product of two operands is the six products of parts
 // that reach 2^-22 of it (the three left out are below that): 6 x 16 cycles for 16 x 16 x 32 on a SIMD, where the float32 matrix
-// instruction takes 256.  Forward B8 H16 T2048 d 128: 215 us against 301 with float32 instructions, backward 617 and 868; the LDS
+// instruction takes 256.  B8 H16 T2048 d 128: float32 instructions take 1.40 times as long forward, 1.41 times backward; the LDS
 // reads, the matrix instructions and the splitting of operands then take about a third of a block's time each.
 // An infinity in float32 comes out as NaN where it is used (its parts are inf - inf).
 //   VE: elements of a 16-byte vector;  KB: the contraction length of one operand fragment, 8 places in a lane;  KP, SP:
@@ -262,7 +267,7 @@ template <> struct From<true> {
 };
 
 // 16 bytes `past` elements (fewer than they hold) down, zeros behind: words by selects, bfloat16 by 64-bit shifts, which take
-// more time and fewer registers (B8 H16 T1024 d 127: float32 176 us and 199, bfloat16 78 and 77)
+// more time and fewer registers (B8 H16 T1024 d 127: shifts take 1.13 times as long in float32, as long in bfloat16)
 template <typename E> __device__ __forceinline__ u32x4 move_down(u32x4 x, int past)
 {
     if constexpr (sizeof(E) == 4) {
@@ -371,12 +376,12 @@ template <typename E, bool EXACT> __device__ __forceinline__ u32x4 row_place(u32
 // buffers of keys and values, VP elements that a row of values in LDS is longer (4 rows of 64 bytes, every other 8 of
 // them, or of 32 bytes, on different banks).
 //  * bfloat16: four waves (one on a SIMD) form no scores and no weighted values twice, eight hide more latency and have
-//    half the registers' worth of work each.  B8 H16 T4096 d 128, forward and backward: 177 and 397 us with four, 192 and 481
-//    with eight (slices of 32 columns: a fifth more than 64); with 256 channels four do not have the registers.
+//    half the registers' worth of work each.  B8 H16 T4096 d 128: eight take 1.08 times as long forward, 1.21 times backward (slices
+//    of 32 columns: 1.2 times); with 256 channels four do not have the registers.
 //  * float32: three planes fill LDS, so that there is one buffer of them and one workgroup on a compute unit; with 256 channels
-//    half the block and half the columns.  Four waves with the registers of all (forward B8 H16 T2048 d 128: 215 us, 234 with eight;
-//    backward 617 and 667), but eight where rows are not whole vectors, whose address arithmetic they hide (B3 H5
-//    T1003 keys of 88, values of 74: 44 us and 51 with four).
+//    half the block and half the columns.  Four waves with the registers of all (B8 H16 T2048 d 128: eight take 1.09 times as long
+//    forward, 1.08 times backward), but eight where rows are not whole vectors, whose address arithmetic they hide (B3 H5
+//    T1003 keys of 88, values of 74: four take 1.16 times as long).
 template <typename E, int DAP, bool EXACT> struct Shape {
     static constexpr bool HALF = sizeof(E) == 4 && DAP > 128;
     static constexpr int C = HALF ? 32 : 64, NS = decay_slice(sizeof(E) == 2, DAP), NW = (sizeof(E) == 2 ? DAP > 128 : DAP <= 128 && !EXACT) ? 8 : 4;
@@ -528,7 +533,10 @@ __device__ __forceinline__ void decay_scan(const DecayLaunch& L, const DecayRole
     int low = pad;                  // first row with a token
     const uint32_t ooff = orow.offset(16 * RT + c, 0, C);
 
-    // the state, rounded to the element type (bfloat16), as the operand of its product with the queries
+    // The state, rounded to the element type (bfloat16), as the operand of its product with the queries; so are the scores below as
+    // the operand of theirs with the values.  Both in two parts would leave only the result's own rounding, an error of 0.0017 of the
+    // results instead of 0.0023, and take 1.18 times as long forward at B8 H16 T4096 d 128, 1.21 at H16 T65536, 1.33 at B3 H5 T1003, 1.27
+    // backward.  The state that is carried on keeps float32 (see `weighted`); float32 tensors have none of these roundings.
     auto state_out = [&](uint16_t* to) {
 #pragma unroll
         for (int d = 0; d < DTW; ++d) O::put4(to + scol * SS + srow + 16 * d, SPL, S[d]);
@@ -814,8 +822,8 @@ template <typename E, int DAP, int SB, bool STATES, bool EXACT> hipError_t scan_
 }
 
 // One state buffer or two.  Two where a second workgroup fits beside it all the same, or where there is none: with
-// bfloat16 and 128 channels one buffer lets two workgroups share a compute unit (forward B8 H16 T4096, 256 workgroups: 177 us with two
-// buffers, 187 with one; backward, 768 workgroups: 415 and 396).  The segments' states need no buffer.
+// bfloat16 and 128 channels one buffer lets two workgroups share a compute unit (B8 H16 T4096 forward, 256 workgroups:
+// one buffer takes 1.06 times as long; backward, 768 workgroups: two take 1.05 times as long).  The segments' states need no buffer.
 template <typename E, int DAP, bool STATES, bool EXACT> hipError_t scan(const DecayLaunch& L, unsigned groups, hipStream_t st)
 {
     constexpr size_t HALF = 80 * 1024;
@@ -917,7 +925,7 @@ hipError_t launch_decay(const DecayLaunch& L, hipStream_t st)
     const long heads = static_cast<long>(L.B) * L.H;
     // Roles with the same padded channels of the state share a launch.  All of them do, with the padding of the largest, where
     // that leaves each workgroup a compute unit: launches one after the other add up their latencies (backward float32
-    // B2 H6 T509, keys of 72 and values of 58 channels: 43 us in one, 66 in two).
+    // B2 H6 T509, keys of 72 and values of 58 channels: two take 1.5 times as long).
     int widest = 64;
     for (int r = 0; r < L.roles; ++r)
         while (L.role[r].da > widest) widest *= 2;
