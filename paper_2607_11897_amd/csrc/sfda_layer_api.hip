@@ -213,13 +213,13 @@ bool decay_sizes(int B, int H, int T, int dk, int dv)
 bool rows_fit(const ll (&st)[3], ll e) { return st[2] <= ((1LL << 31) - 65536) / (64 * e); }
 
 // Segments of a sequence.  A scan without them takes c us for 64 tokens, whatever the number of heads, until the workgroups fill the
-// compute units.  Cut into S parts it takes a pass for their states (another s us) and a join, all of them on an S-th of the
+// compute units.  Cut into S parts it takes a pass for their states (another s c us) and a join, all of them on an S-th of the
 // tokens, with one workgroup on each unit, or with two of bfloat16.  The estimates are in us, for the padded channels of the state
 // and for rows of whole vectors or not; roles of different padding add up, but where they share a launch.
-// Measured, whole / cut, d 128: bfloat16 forward 16 heads T 512 23/27, 4 heads T 256 17/24, 15 heads T 1003 61/33,
-// 32 heads T 2048 72/48; backward 16 heads T 512 24/37, 32 heads T 2048 76/90; float32 forward 4 heads T 512 54/28,
-// 32 heads T 2048 193/97; backward 16 heads T 512 57/61, 32 heads T 2048 199/194; d 64, 16 heads T 2048 122/35; d 256, 4 heads
-// T 512 81/37.
+// Measured, whole / cut, us of a call among others, d 128: bfloat16 forward 16 heads T 512 23/27, 4 heads T 256 17/24, 15 heads T 1003
+// 39/36 (keys of 88, values of 74: 54/33), 32 heads T 2048 72/48; backward 16 heads T 512 25/37, 32 heads T 2048 72/90; float32
+// forward 4 heads T 512 56/29, 32 heads T 2048 199/98; backward 16 heads T 512 60/61, 32 heads T 2048 201/194; d 64, 16 heads T 2048
+// 125/34; d 256, 4 heads T 512 81/38.
 struct Cut { int tokens, segments; };
 struct State { int da, db; };           // a role's
 Cut cut_of(ll heads, std::initializer_list<State> roles, int T, bool bf16)
