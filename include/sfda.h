@@ -511,6 +511,112 @@ sfda_status_t sfda_group_norm_bwd(const void* dy, const void* x, const float* we
                                   sfda_dtype_t dtype, void* workspace, size_t workspace_bytes,
                                   sfda_stream_t stream);
 
+/*
+ * sfda_rotary_axes -- sfda_rotary for tokens with a position on each of several axes (time, height, width, ...): pair i turns by
+ *   cos, sin[positions[axis(i)][b][t]][i].
+ *   sections : host array of `axes` (1 to 4) numbers of pairs, whose sum is rot / 2 (1 to D / 2).  axis(i): the first sections[0]
+ *          pairs follow axis 0, the next sections[1] axis 1, and so on; with cyclic, pairs are dealt to the axes in turn, 0, 1, ..., those
+ *          that have their number left out.
+ *   positions : [axes, B, T] of position_bits (32 or 64) wide integers, axes axis_stride and sequences position_stride elements
+ *          apart (0: the same).  A position outside [0, P) turns the pairs that follow it into NaN.
+ *   Tables, pairs, channels past rot, inverse, strides and turning in place as sfda_rotary's.
+ */
+sfda_status_t sfda_rotary_axes(const void* q, const void* k, const float* cos, const float* sin,
+                               const void* positions, int position_bits, long long axis_stride,
+                               long long position_stride, const int* sections, int axes, int cyclic,
+                               void* qo, void* ko, int B, int Hq, int Hk, int T, int D, int P,
+                               int interleaved, int inverse, const long long* strides,
+                               sfda_dtype_t dtype, sfda_stream_t stream);
+
+/*
+ * sfda_delta_attn_fwd -- linear attention with the gated delta rule: each token's decay a_t = exp(log_decay_t) and strength beta_t,
+ *   S_t = a_t S_{t-1} + k_t u_t^T,   u_t = beta_t (v_t - a_t S_{t-1}^T k_t)      (S_t in R^{dk x dv}),      o_t = scale S_t^T q_t
+ * over T tokens, evaluated in blocks on the matrix cores.
+ *   q, k [B, Hk, T, dk], v, o [B, H, T, dv], log_decay, beta [B, H, T] float32; H a multiple of Hk: value head h reads key head
+ *          h / (H / Hk).  strides: (b, h, t) of q, k, v, log_decay, beta, o.
+ *   log_decay : meant to be <= 0; 0 keeps everything, -inf nothing.  Keys are taken as they are: of length 1 and with beta in
+ *          [0, 2] no state grows.
+ *   lengths : [B] int32 or NULL.  Sequence b has min(max(lengths[b], 0), T) tokens; what the tensors hold past them is not used, o is
+ *          0 there and S_T is the state after the last token (S0 at length 0).
+ *   S0, S_T : [B, H, dk, dv] contiguous float32, each may be NULL (zero state; not wanted).  S_T == S0 is allowed.
+ *   workspace : at least sfda_delta_attn_fwd_workspace_bytes(...) bytes (SFDA_ERR_SHAPE if smaller), 16-byte aligned.
+ *   1 <= dk, dv <= 256; 64 tokens' rows of q, k or v lie within 2^31 bytes (SFDA_ERR_SHAPE otherwise).
+ *   Products that reach a state are those of operands as three bfloat16 parts, to 2^-22, with sums in float32, for both types.
+ *   bfloat16: the products that give o alone take the state, the scores and the writes rounded to bfloat16.
+ *   A token with a value that is not finite may make its whole block (32 or 64 tokens) NaN, and what follows; magnitudes past
+ *   3.38e38 are taken for infinities.
+ */
+size_t sfda_delta_attn_fwd_workspace_bytes(int B, int H, int T, int dk, int dv, sfda_dtype_t dtype);
+
+sfda_status_t sfda_delta_attn_fwd(const void* q, const void* k, const void* v,
+                                  const float* log_decay, const float* beta, const int* lengths,
+                                  const float* S0, void* o, float* S_T, int B, int H, int Hk, int T,
+                                  int dk, int dv, float scale, const long long* strides,
+                                  sfda_dtype_t dtype, void* workspace, size_t workspace_bytes,
+                                  sfda_stream_t stream);
+
+/*
+ * sfda_delta_attn_bwd -- gradients of a real loss through sfda_delta_attn_fwd, given dO = dL/do and dS_T = dL/dS_T (NULL: zero).
+ *   dq, dk [B, Hk, T, dk] (sums over the value heads that share a key head), dv [B, H, T, dv] as the inputs' type; dlog_decay, dbeta
+ *          [B, H, T] float32; zero past a sequence's length.  dS0 [B, H, dk, dv] float32 or NULL.
+ *   strides: (b, h, t) of q, k, v, log_decay, beta, dO, dq, dk, dv, dlog_decay, dbeta; those of dO's tokens as q's.
+ *   workspace : 16-byte aligned; with sfda_delta_attn_bwd_workspace_bytes(B, H, ...) bytes all heads run at once, with less in passes
+ *          over groups of key heads, as many as fit; at least what the call takes for one, sfda_delta_attn_bwd_workspace_bytes(1,
+ *          H / Hk, 1, ...) (SFDA_ERR_SHAPE if smaller).  The results do not depend on it.
+ *   bfloat16: dq, dk and dv are sums of products of operands rounded to bfloat16; dlog_decay, dbeta and dS0 come from products to
+ *   2^-22.  Other arguments as the forward's.
+ */
+size_t sfda_delta_attn_bwd_workspace_bytes(int B, int H, int Hk, int T, int dk, int dv,
+                                           sfda_dtype_t dtype);
+
+sfda_status_t sfda_delta_attn_bwd(const void* q, const void* k, const void* v,
+                                  const float* log_decay, const float* beta, const int* lengths,
+                                  const float* S0, const void* dO, const float* dS_T, void* dq,
+                                  void* dk_out, void* dv_out, float* dlog_decay, float* dbeta,
+                                  float* dS0, int B, int H, int Hk, int T, int dk, int dv,
+                                  float scale, const long long* strides, sfda_dtype_t dtype,
+                                  void* workspace, size_t workspace_bytes, sfda_stream_t stream);
+
+/*
+ * sfda_delta_attn_step -- one token of sfda_delta_attn_fwd, S updated in place.
+ *   q, k [B, Hk, dk], v, o [B, H, dv], log_decay, beta [B, H]; strides: (b, h) of q, k, v, log_decay, beta, o; S [B, H, dk, dv]
+ *   contiguous float32.
+ */
+sfda_status_t sfda_delta_attn_step(const void* q, const void* k, const void* v,
+                                   const float* log_decay, const float* beta, float* S, void* o,
+                                   int B, int H, int Hk, int dk, int dv, float scale,
+                                   const long long* strides, sfda_dtype_t dtype,
+                                   sfda_stream_t stream);
+
+/*
+ * sfda_layer_norm -- rows of D channels normalised, after the residual sum where there is one:
+ *   t = x + residual, rounded to the type (x itself without a residual),
+ *   y = (t - mean) / sqrt(var + eps) weight + bias.
+ *   x, residual, y, total [B, T, D]; residual may be NULL, then total is not written; weight, bias [D] float32, each may be NULL
+ *   (1; 0).  strides: (b, t) of x, residual, y, total.  total == residual, total == x and, without a residual, y == x are allowed (same
+ *   strides).  1 <= D <= 16384, eps >= 0.
+ */
+sfda_status_t sfda_layer_norm(const void* x, const float* weight, const float* bias,
+                              const void* residual, void* y, void* total, int B, int T, int D,
+                              float eps, const long long* strides, sfda_dtype_t dtype,
+                              sfda_stream_t stream);
+
+/*
+ * sfda_layer_norm_bwd -- gradients of a real loss through sfda_layer_norm, given dy = dL/dy and, or NULL, dtotal, the gradient that
+ * reaches the total by other ways: dx = dL/dt, which is the gradient of x and of the residual alike.
+ *   dy, x (the total, where there was a residual), dtotal, dx [B, T, D]; dweight, dbias [D] float32 or NULL (not wanted).
+ *   strides: (b, t) of dy, x, dtotal, dx.  dx == dy and dx == dtotal are allowed (same strides).
+ *   workspace : sfda_layer_norm_bwd_workspace_bytes(...) bytes where dweight or dbias is wanted (their partial sums;
+ *          SFDA_ERR_SHAPE if smaller), 4-byte aligned.
+ */
+size_t sfda_layer_norm_bwd_workspace_bytes(int B, int T, int D, sfda_dtype_t dtype);
+
+sfda_status_t sfda_layer_norm_bwd(const void* dy, const void* x, const float* weight,
+                                  const void* dtotal, void* dx, float* dweight, float* dbias, int B,
+                                  int T, int D, float eps, const long long* strides,
+                                  sfda_dtype_t dtype, void* workspace, size_t workspace_bytes,
+                                  sfda_stream_t stream);
+
 /* SFDA_ABI_VERSION of the built library. */
 int sfda_abi_version(void);
 

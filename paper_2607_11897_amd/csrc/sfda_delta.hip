@@ -1,0 +1,367 @@
+// Linear attention with the gated delta rule (gfx950): the blocks' inverses, the chunked forward and the decode step.
+#include "sfda_delta.h"
+
+#include <utility>
+
+namespace sfda {
+namespace delta {
+namespace {
+
+// ------------------------------------------------------------------ the blocks' inverses
+
+// 8 channels of a row as a fragment; channels past the row and rows that are not there are zero
+template <typename E> __device__ __forceinline__ u32x4 vector_at(const char* row, int col, int cols, bool there)
+{
+    constexpr int VE = Ops<E>::VE;
+    const u32x4 none = {0, 0, 0, 0};
+    if (cols < VE) {
+        const u32x4 x = short_row<E>(row, cols);
+        return there && col == 0 ? x : none;
+    }
+    const int past = col + VE - cols;
+    const u32x4 x = load16(row + (past <= 0 ? col : cols - VE) * static_cast<int>(sizeof(E)));
+    return !there || past >= VE ? none : past > 0 ? move_down<E>(x, past) : x;
+}
+template <typename E> __device__ __forceinline__ Op<Block<E>::P> key_frag(const char* row, int col, int cols, bool there)
+{
+    Op<Block<E>::P> o;
+    if constexpr (sizeof(E) == 2) {
+        o.p[0] = __builtin_bit_cast(bf16x8, vector_at<E>(row, col, cols, there));
+    } else {
+        float x[8];
+        const u32x4 a = vector_at<E>(row, col, cols, there), b = vector_at<E>(row, col + 4, cols, there);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[i] = __uint_as_float(a[i]);
+            x[4 + i] = __uint_as_float(b[i]);
+        }
+        o = op_of<3>(x);
+    }
+    return o;
+}
+
+// N = (I - X)^(-1) = I + X N for X strictly lower triangular, by forward substitution: lane (c, g) holds row c of X and columns 4 g + k of
+// row c of N; a pivot row is lane s of the lane's own 16.
+template <int S> __device__ __forceinline__ void pivot(float (&n)[4], const float (&x)[16])
+{
+#pragma unroll
+    for (int k = 0; k < 4; ++k) n[k] = __builtin_fmaf(x[S], row_bcast<S>(n[k]), n[k]);
+}
+template <int... S> __device__ __forceinline__ void pivots(float (&n)[4], const float (&x)[16], std::integer_sequence<int, S...>)
+{
+    (pivot<S>(n, x), ...);
+}
+// d += A B, 16 x 16 in float32: a holds row c of A, b column c of B, each at 4 g + r
+__device__ __forceinline__ void mul16(f32x4& d, const f32x4& a, const f32x4& b)
+{
+#pragma unroll
+    for (int r = 0; r < 4; ++r) d = __builtin_amdgcn_mfma_f32_16x16x4f32(a[r], b[r], d, 0, 0, 0);
+}
+
+constexpr int tile_at(int i, int j) { return i * (i + 1) / 2 + j; }
+
+// (I + L diag(beta))^(-1) of every block, for the forward, and with blockIdx.y 1 the transpose of (I + diag(beta) L)^(-1), for the
+// backward: one wave for a block.  Diagonal tiles by substitution, then pairs of them joined, [A 0; X B]^(-1) having -B^(-1) X A^(-1)
+// in its corner, all in float32 (on its matrix instructions), where the states' 24 bits come from.
+template <typename E> __global__ __launch_bounds__(NT) void sfda_delta_prep(DeltaLaunch L)
+{
+    typedef Block<E> B;
+    constexpr int C = B::C, CT = B::CT, P = B::P, TILES = B::TILES, ES = sizeof(E);
+    constexpr int ROW = 20;
+    __shared__ __align__(16) float scratch[NW][16 * ROW];
+    __shared__ __align__(16) float tok[NW][3][C];
+
+    const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int groups = (L.blocks + NW - 1) / NW;
+    const unsigned head = blockIdx.x / static_cast<unsigned>(groups), first = (blockIdx.x - head * groups) * NW;
+    const long long bh = L.first + head;
+    const int b = static_cast<int>(bh / L.H), h = static_cast<int>(bh - static_cast<long long>(b) * L.H), hk = h / (L.H / L.Hk);
+    const int len = __builtin_amdgcn_readfirstlane(seq_length(L.lengths, b, L.T)), blocks = (len + C - 1) / C;
+    if (static_cast<int>(first) >= blocks) return;
+    const bool live = static_cast<int>(first) + w < blocks, by_row = blockIdx.y != 0;
+    const int blk = live ? first + w : blocks - 1, t0 = blk * C, cnt = len - t0 < C ? len - t0 : C;     // (others do the last one again)
+    float* const buf = scratch[w];
+
+    {   // sums of the log decays as hi + lo; past -128 a decay is 0 in any case, and sums of such stay finite
+        const bool there = lane < cnt;
+        const int t = t0 + (there ? lane : 0);
+        float a = L.log_decay[b * L.l_s[0] + h * L.l_s[1] + t * L.l_s[2]];
+        const float be = L.beta[b * L.b_s[0] + h * L.b_s[1] + t * L.b_s[2]];
+        if (a < -128.f) a = -128.f;
+        double s = there ? a : 0.f;
+#pragma unroll
+        for (int d = 1; d < C; d *= 2) {
+            const double o = __shfl_up(s, d);
+            if (lane >= d) s += o;
+        }
+        const float hi = static_cast<float>(s), lo = static_cast<float>(s - hi);
+        if (lane < C) {
+            tok[w][0][lane] = hi;
+            tok[w][1][lane] = lo;
+            tok[w][2][lane] = there ? be : 0.f;
+            if (live && !by_row) L.scalars[(head * static_cast<long long>(L.blocks) + blk) * C + lane] = float4{hi, lo, there ? be : 0.f, 0.f};
+        }
+    }
+
+    // lane (c, g) of tile (i, j): row c, columns 4 g + r of K K^T
+    f32x4 X[TILES];
+#pragma unroll
+    for (int t = 0; t < TILES; ++t) X[t] = zero4();
+    const char* const kp = static_cast<const char*>(L.k) + (b * L.k_s[0] + hk * L.k_s[1] + t0 * L.k_s[2]) * ES;
+#pragma clang loop unroll(disable)
+    for (int f = 0; 32 * f < L.dk; ++f) {
+        Op<P> k[CT];
+#pragma unroll
+        for (int t = 0; t < CT; ++t) {
+            const int r = 16 * t + c;
+            k[t] = key_frag<E>(kp + (r < cnt ? r : cnt - 1) * (L.k_s[2] * ES), 32 * f + 8 * g, L.dk, r < cnt);
+        }
+#pragma unroll
+        for (int i = 0; i < PAIRS<P, P>; ++i)
+#pragma unroll
+            for (int ti = 0; ti < CT; ++ti)
+#pragma unroll
+                for (int tj = 0; tj <= ti; ++tj) mm<P, P>(i, X[tile_at(ti, tj)], k[tj], k[ti]);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int ti = 0; ti < CT; ++ti)
+#pragma unroll
+        for (int tj = 0; tj <= ti; ++tj)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int i = 16 * ti + c, j = 16 * tj + 4 * g + r;
+                const float d = expf((tok[w][0][i] - tok[w][0][j]) + (tok[w][1][i] - tok[w][1][j]));
+                f32x4& x = X[tile_at(ti, tj)];
+                x[r] = j < i ? -x[r] * (d * tok[w][2][by_row ? i : j]) : 0.f;
+            }
+
+    // row c at 4 g .. to column c at 4 g .., and back
+    auto turn = [&](const f32x4& x) {
+        f32x4 y;
+        __syncthreads();
+        *reinterpret_cast<f32x4*>(buf + c * ROW + 4 * g) = x;
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < 4; ++r) y[r] = buf[(4 * g + r) * ROW + c];
+        return y;
+    };
+    f32x4 rows[CT], T[TILES];               // diagonal tiles by rows; all tiles by columns
+#pragma unroll
+    for (int t = 0; t < CT; ++t) {
+        __syncthreads();
+        *reinterpret_cast<f32x4*>(buf + c * ROW + 4 * g) = X[tile_at(t, t)];
+        __syncthreads();
+        float x[16], n[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const f32x4 y = *reinterpret_cast<const f32x4*>(buf + c * ROW + 4 * i);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) x[4 * i + r] = y[r];
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) n[k] = 4 * g + k == c ? 1.f : 0.f;
+        pivots(n, x, std::make_integer_sequence<int, 15>());
+        rows[t] = f32x4{n[0], n[1], n[2], n[3]};
+        T[tile_at(t, t)] = turn(rows[t]);
+    }
+#pragma unroll
+    for (int t = 0; t < CT; t += 2) {
+        f32x4 m = zero4(), n = zero4();
+        mul16(m, X[tile_at(t + 1, t)], T[tile_at(t, t)]);
+        mul16(n, rows[t + 1], m);
+        T[tile_at(t + 1, t)] = n;
+    }
+    if constexpr (CT == 4) {
+        const f32x4 r32 = turn(T[tile_at(3, 2)]);
+        f32x4 m[2][2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                m[i][j] = zero4();
+#pragma unroll
+                for (int k = j; k < 2; ++k) mul16(m[i][j], X[tile_at(2 + i, k)], T[tile_at(k, j)]);
+            }
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            f32x4 a = zero4(), d = zero4();
+            mul16(a, rows[2], m[0][j]);
+            mul16(d, r32, m[0][j]);
+            mul16(d, rows[3], m[1][j]);
+            T[tile_at(2, j)] = a;
+            T[tile_at(3, j)] = d;
+        }
+    }
+    float* const out = (by_row ? L.inv_back : L.inv) + (head * static_cast<long long>(L.blocks) + blk) * (TILES * 256);
+#pragma unroll
+    for (int ti = 0; ti < CT; ++ti)
+#pragma unroll
+        for (int tj = 0; tj <= ti; ++tj) {
+            f32x4 x = T[tile_at(ti, tj)];
+            if (!by_row) x = ti == tj ? rows[ti] : turn(x);
+            if (live) *reinterpret_cast<f32x4*>(out + tile_at(ti, tj) * 256 + c * 16 + 4 * g) = x;
+        }
+}
+
+// ------------------------------------------------------------------ the forward scan
+
+template <typename E, int DKP> __global__ __launch_bounds__(NT) void sfda_delta_fwd(DeltaLaunch L, int slices)
+{
+    extern __shared__ __align__(16) unsigned char smem[];
+    long head;
+    int sl;
+    head_slice(blockIdx.x, slices, L.heads, head, sl);
+    head = static_cast<long>(same_for_all(static_cast<uint64_t>(head)));
+    sl = __builtin_amdgcn_readfirstlane(sl);
+    scan<E, DKP, FWD>(L, head, sl, smem);
+}
+
+template <typename E, int DKP> hipError_t fwd(const DeltaLaunch& L, hipStream_t st)
+{
+    constexpr size_t bytes = sizeof(Mem<E, DKP, FWD>);
+    static_assert(bytes <= 160 * 1024, "one compute unit's LDS");
+    const int slices = (L.dv + SLICE - 1) / SLICE;
+    hipLaunchKernelGGL((sfda_delta_fwd<E, DKP>), dim3(static_cast<unsigned>(L.heads) * slices), dim3(NT), bytes, st, L, slices);
+    return hipGetLastError();
+}
+template <typename E> hipError_t fwd_any(const DeltaLaunch& L, hipStream_t st)
+{
+    return L.dk <= 64 ? fwd<E, 64>(L, st) : L.dk <= 128 ? fwd<E, 128>(L, st) : fwd<E, 256>(L, st);
+}
+
+// ------------------------------------------------------------------ decode step
+// S <- a S + k u^T, u = beta (v - a S^T k), o = scale S^T q = scale (a S^T q + (k . q) u), the state read and written once.  One workgroup for
+// a head and 16 float4 columns, whose 16 row groups hold every 16th row of the state in registers; S^T k and S^T q are added over
+// them through LDS.
+template <typename E, int ROWS> __global__ __launch_bounds__(NT) void sfda_delta_step(DeltaStepLaunch L, int slices)
+{
+    constexpr int RG = NT / 16, SW = 64;
+    __shared__ __align__(16) float part[2][RG][SW + 4];
+    __shared__ float kqs[RG];
+    const int tid = threadIdx.x, cg = tid & 15, rg = tid >> 4;
+    const long long bh = blockIdx.x / static_cast<unsigned>(slices);
+    const int sl = static_cast<int>(blockIdx.x - bh * slices), n = sl * SW + 4 * cg;
+    const int b = static_cast<int>(bh / L.H), h = static_cast<int>(bh - static_cast<long long>(b) * L.H), hk = h / (L.H / L.Hk);
+    const E* q = static_cast<const E*>(L.q) + b * L.q_s[0] + hk * L.q_s[1];
+    const E* k = static_cast<const E*>(L.k) + b * L.k_s[0] + hk * L.k_s[1];
+    const E* v = static_cast<const E*>(L.v) + b * L.v_s[0] + h * L.v_s[1];
+    float* S = L.S + bh * L.dk * static_cast<long long>(L.dv);
+    const float g = L.log_decay[b * L.l_s[0] + h * L.l_s[1]], beta = L.beta[b * L.b_s[0] + h * L.b_s[1]];
+    const int m = L.dv - n < 4 ? L.dv - n : 4;
+
+    f32x4 s[ROWS], p = zero4(), o = zero4();
+    float kd[ROWS], qd[ROWS], kq = 0.f;
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+        const int d = rg + i * RG;
+        const bool there = d < L.dk;
+        s[i] = zero4();
+        kd[i] = there ? Elem<E>::load(k, d) : 0.f;
+        qd[i] = there ? Elem<E>::load(q, d) : 0.f;
+        if (there && m > 0) {
+            const float* row = S + static_cast<long long>(d) * L.dv + n;
+            if (m == 4) {
+                memcpy(&s[i], row, 16);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 3; ++e)
+                    if (e < m) s[i][e] = row[e];
+            }
+        }
+    }
+    float vv[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) vv[e] = e < m ? Elem<E>::load(v, n + e) : 0.f;
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+        kq = __builtin_fmaf(kd[i], qd[i], kq);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            p[e] = __builtin_fmaf(kd[i], s[i][e], p[e]);
+            o[e] = __builtin_fmaf(qd[i], s[i][e], o[e]);
+        }
+    }
+    *reinterpret_cast<f32x4*>(&part[0][rg][4 * cg]) = p;
+    *reinterpret_cast<f32x4*>(&part[1][rg][4 * cg]) = o;
+    if (cg == 0) kqs[rg] = kq;
+    __syncthreads();
+    p = o = zero4();
+    kq = 0.f;
+#pragma unroll
+    for (int i = 0; i < RG; ++i) {
+        const f32x4 a = *reinterpret_cast<const f32x4*>(&part[0][i][4 * cg]), d = *reinterpret_cast<const f32x4*>(&part[1][i][4 * cg]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            p[e] += a[e];
+            o[e] += d[e];
+        }
+        kq += kqs[i];
+    }
+    // the decay as hi + lo, so that a state that keeps nearly all of itself for thousands of tokens keeps its 24 bits
+    const bool near = g > -0.5f && g < 0.5f;
+    const float em = near ? expm1f(g) : 0.f, hi = near ? 1.f + em : expf(g), lo = near ? em - (hi - 1.f) : 0.f;
+    f32x4 u;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) u[e] = beta * (vv[e] - __builtin_fmaf(p[e], hi, p[e] * lo));
+    if (m > 0) {
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i) {
+            const int d = rg + i * RG;
+            if (d >= L.dk) break;
+            float* row = S + static_cast<long long>(d) * L.dv + n;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[i][e] = __builtin_fmaf(kd[i], u[e], __builtin_fmaf(s[i][e], hi, s[i][e] * lo));
+            if (m == 4) {
+                memcpy(row, &s[i], 16);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 3; ++e)
+                    if (e < m) row[e] = s[i][e];
+            }
+        }
+        if (rg == 0) {
+            E* to = static_cast<E*>(L.o) + b * L.o_s[0] + h * L.o_s[1] + n;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (e < m) Ops<E>::store1(to + e, L.scale * __builtin_fmaf(kq, u[e], __builtin_fmaf(o[e], hi, o[e] * lo)));
+        }
+    }
+}
+
+template <typename E> hipError_t step(const DeltaStepLaunch& L, hipStream_t st)
+{
+    const int slices = (L.dv + 63) / 64;
+    const dim3 grid(static_cast<unsigned>(L.B) * L.H * slices), block(NT);
+    if (L.dk <= 64) hipLaunchKernelGGL((sfda_delta_step<E, 4>), grid, block, 0, st, L, slices);
+    else if (L.dk <= 128) hipLaunchKernelGGL((sfda_delta_step<E, 8>), grid, block, 0, st, L, slices);
+    else hipLaunchKernelGGL((sfda_delta_step<E, 16>), grid, block, 0, st, L, slices);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t prep(const DeltaLaunch& L, int inverses, hipStream_t st)
+{
+    if (L.blocks == 0) return hipSuccess;
+    const dim3 grid(static_cast<unsigned>(L.heads) * ((L.blocks + NW - 1) / NW), inverses);
+    if (L.bf16) hipLaunchKernelGGL(sfda_delta_prep<uint16_t>, grid, dim3(NT), 0, st, L);
+    else hipLaunchKernelGGL(sfda_delta_prep<float>, grid, dim3(NT), 0, st, L);
+    return hipGetLastError();
+}
+
+}  // namespace delta
+
+hipError_t launch_delta_fwd(const DeltaLaunch& L, hipStream_t st)
+{
+    const hipError_t e = delta::prep(L, 1, st);
+    if (e != hipSuccess) return e;
+    return L.bf16 ? delta::fwd_any<uint16_t>(L, st) : delta::fwd_any<float>(L, st);
+}
+
+hipError_t launch_delta_step(const DeltaStepLaunch& L, hipStream_t st)
+{
+    return L.bf16 ? delta::step<uint16_t>(L, st) : delta::step<float>(L, st);
+}
+
+}  // namespace sfda

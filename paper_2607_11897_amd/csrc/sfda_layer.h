@@ -56,17 +56,62 @@ struct DecayStepLaunch {
 };
 hipError_t launch_decay_step(const DecayStepLaunch& L, hipStream_t st);
 
+// The gated delta rule of value heads first .. first + heads - 1 (numbered over the batch), H / Hk of them for a key head.  The workspace's
+// parts are counted from `first`; a sequence has room for `blocks` blocks of delta_block tokens.
+struct DeltaLaunch {
+    const void *q, *k, *v, *dO;
+    void *o, *dq, *dk_out, *dv_out;
+    const float *log_decay, *beta;
+    float *dlog_decay, *dbeta;
+    const float *S0, *dS_T;  // may be null (zero)
+    float *S_T, *dS0;        // may be null
+    long long q_s[3], k_s[3], v_s[3], o_s[3], g_s[3];           // element strides of b, h, t (g: dO)
+    long long l_s[3], b_s[3];                                   // log_decay, beta
+    long long dq_s[3], dk_s[3], dv_s[3], dl_s[3], db_s[3];
+    const int* lengths;      // [B] or null
+    int B, H, Hk, T, dk, dv;
+    float scale;
+    long long first;
+    int heads, blocks;
+    float *inv, *inv_back;   // [heads][blocks][tiles of the lower triangle][16][16]
+    float4* scalars;         // [heads][blocks * block]: sum of the block's log decays (hi, lo), beta
+    float *rec_S, *rec_U;    // states before each block and after the last; their gradients after each block
+    float *rec_R, *rec_du;   // [heads][blocks * block][dv]
+    float* odo;              // [heads][parts][blocks * block]
+    int parts;               // 16 columns each
+    bool bf16;
+};
+constexpr int delta_block(bool bf16) { return bf16 ? 64 : 32; }
+constexpr int delta_tiles(bool bf16) { return bf16 ? 10 : 3; }
+hipError_t launch_delta_fwd(const DeltaLaunch& L, hipStream_t st);
+hipError_t launch_delta_bwd(const DeltaLaunch& L, hipStream_t st);
+
+struct DeltaStepLaunch {
+    const void *q, *k, *v;
+    void* o;
+    float* S;
+    const float *log_decay, *beta;
+    long long q_s[2], k_s[2], v_s[2], o_s[2], l_s[2], b_s[2];   // element strides of b, h
+    int B, H, Hk, dk, dv;
+    float scale;
+    bool bf16;
+};
+hipError_t launch_delta_step(const DeltaStepLaunch& L, hipStream_t st);
+
+constexpr int ROTARY_AXES = 4, ROTARY_PAIRS = 2048;
 struct RotaryLaunch {
     const void *q, *k;       // k may be null
     void *qo, *ko;
     long long q_s[3], k_s[3], qo_s[3], ko_s[3];
     const float *cos, *sin;  // [P, rot / 2]
-    const void* positions;   // int32 or int64 [B or 1, T], or null: offset + t
+    const void* positions;   // int32 or int64 [B or 1, T] ([axes, B or 1, T] with axes), or null: offset + t
     int pos64;
-    long long pos_b;         // element stride of positions over b
+    long long pos_a, pos_b;  // element strides of positions over axes and b
     long long offset;
     int B, Hq, Hk, T, D, rot, P;
     int interleaved, inverse;
+    int axes;                // 0: one position for a token
+    unsigned axis[ROTARY_PAIRS / 16];       // each pair's axis, 2 bits
     bool bf16;
 };
 hipError_t launch_rotary(const RotaryLaunch& L, hipStream_t st);
@@ -87,6 +132,24 @@ struct NormLaunch {
 };
 int norm_strips(long rows_bt, int H, int D, bool bf16);     // workgroups of a head
 constexpr int NORM_MAX = 2048;          // channels of a group
+
+// Rows x [B, T, D] (+ residual, rounded: total) normalised over D; backward, dx = the norm's gradient (+ dtotal).
+struct LayerNormLaunch {
+    const void *x, *residual;       // residual may be null
+    const void *dy, *dtotal;        // backward; dtotal may be null
+    void *y, *total, *dx;
+    const float *weight, *bias;     // may be null
+    float *dweight, *dbias;
+    float* partial;          // backward: [strips][2][D]
+    long long x_s[2], r_s[2], y_s[2], t_s[2], dy_s[2], dt_s[2], dx_s[2];     // element strides of b, t
+    int B, T, D;
+    float eps;
+    bool bf16;
+};
+constexpr int LAYER_NORM_MAX = 16384;
+int layer_norm_strips(long long rows, int D, bool bf16);    // workgroups
+hipError_t launch_layer_norm(const LayerNormLaunch& L, hipStream_t st);
+hipError_t launch_layer_norm_bwd(const LayerNormLaunch& L, hipStream_t st);
 hipError_t launch_norm(const NormLaunch& L, hipStream_t st);
 hipError_t launch_norm_bwd(const NormLaunch& L, hipStream_t st);
 

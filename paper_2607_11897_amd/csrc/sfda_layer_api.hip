@@ -265,23 +265,21 @@ Cut cut_bwd(ll heads, int T, int dk, int dv, bool bf16) { return cut_of(heads, {
 
 extern "C" {
 
-sfda_status_t sfda_rotary(const void* q, const void* k, const float* cos, const float* sin, const void* positions,
-                          int position_bits, long long position_stride, long long offset, void* qo, void* ko, int B,
-                          int Hq, int Hk, int T, int D, int rot, int P, int interleaved, int inverse,
-                          const long long* strides, sfda_dtype_t dtype, sfda_stream_t stream)
+// one position for a token, or with L.axes several
+static sfda_status_t rotary_run(sfda::RotaryLaunch& L, const void* q, const void* k, const float* cos, const float* sin, const void* positions,
+                                int position_bits, ll axis_stride, ll position_stride, ll offset, void* qo, void* ko, int B, int Hq, int Hk,
+                                int T, int D, int rot, int P, int interleaved, int inverse, const long long* strides, sfda_dtype_t dtype,
+                                sfda_stream_t stream)
 {
-    if (!dtype_ok(dtype)) return SFDA_ERR_DTYPE;
-    if (B < 0 || Hq < 0 || Hk < 0 || T < 0 || D < 1 || D > 4096 || rot < 2 || rot > D || (rot & 1) || P < 1) return SFDA_ERR_SHAPE;
-    if (positions != nullptr && ((position_bits != 32 && position_bits != 64) || position_stride < 0)) return SFDA_ERR_SHAPE;
-    if (positions == nullptr && T > 0 && (offset < 0 || offset > P - static_cast<ll>(T))) return SFDA_ERR_SHAPE;
     if (k == nullptr) Hk = 0;
     if (static_cast<ll>(Hq) + Hk > INT_MAX - 64) return SFDA_ERR_SHAPE;
     if (B == 0 || T == 0 || Hq + Hk == 0) return SFDA_OK;
+    if (L.axes > 0 && positions == nullptr) return SFDA_ERR_NULL;
+    if (L.axes > 0 && (axis_stride < 0 || position_stride < 0)) return SFDA_ERR_SHAPE;
     const ll e = esize(dtype);
     // a thread for four heads or four tokens of a 16-byte unit of channels, less than 2^32 in a launch
     const double H = static_cast<double>(Hq) + Hk, rows = std::max((H + 6) / 4 * T, H * ((T + 3.) / 4)) * B;
     if (rows * (D * e / 16. + 3) >= 4294967296. - 1024.) return SFDA_ERR_SHAPE;
-    sfda::RotaryLaunch L{};
     strides3(L.q_s, strides, 0, B, Hq, T, D);
     strides3(L.k_s, strides, 1, B, Hk, T, D);
     strides3(L.qo_s, strides, 2, B, Hq, T, D);
@@ -292,18 +290,60 @@ sfda_status_t sfda_rotary(const void* q, const void* k, const float* cos, const 
     c.input(flat(cos, static_cast<ll>(P) * (rot / 2) * 4), 4);
     c.input(flat(sin, static_cast<ll>(P) * (rot / 2) * 4), 4);
     if (positions != nullptr) {
-        const ll ps[1] = {position_stride};
-        c.input(box(positions, position_bits / 8, T, {B}, ps), position_bits / 8);
+        const ll ps[2] = {axis_stride, position_stride};
+        c.input(box(positions, position_bits / 8, T, {std::max(L.axes, 1), B}, ps), position_bits / 8);
     }
     c.output(box(qo, e, D, {B, Hq, T}, L.qo_s), e, true, iq);
     c.output(box(ko, e, D, {B, Hk, T}, L.ko_s), e, true, ik);
     const sfda_status_t st = c.done();
     if (st != SFDA_OK) return st;
     L.q = q; L.k = k; L.qo = qo; L.ko = ko; L.cos = cos; L.sin = sin;
-    L.positions = positions; L.pos64 = position_bits == 64; L.pos_b = position_stride; L.offset = offset;
+    L.positions = positions; L.pos64 = position_bits == 64; L.pos_a = axis_stride; L.pos_b = position_stride; L.offset = offset;
     L.B = B; L.Hq = Hq; L.Hk = Hk; L.T = T; L.D = D; L.rot = rot; L.P = P;
     L.interleaved = interleaved != 0; L.inverse = inverse != 0; L.bf16 = dtype == SFDA_BF16;
     return sfda::launch_rotary(L, static_cast<hipStream_t>(stream)) == hipSuccess ? SFDA_OK : SFDA_ERR_HIP;
+}
+
+sfda_status_t sfda_rotary(const void* q, const void* k, const float* cos, const float* sin, const void* positions,
+                          int position_bits, long long position_stride, long long offset, void* qo, void* ko, int B,
+                          int Hq, int Hk, int T, int D, int rot, int P, int interleaved, int inverse,
+                          const long long* strides, sfda_dtype_t dtype, sfda_stream_t stream)
+{
+    if (!dtype_ok(dtype)) return SFDA_ERR_DTYPE;
+    if (B < 0 || Hq < 0 || Hk < 0 || T < 0 || D < 1 || D > 4096 || rot < 2 || rot > D || (rot & 1) || P < 1) return SFDA_ERR_SHAPE;
+    if (positions != nullptr && ((position_bits != 32 && position_bits != 64) || position_stride < 0)) return SFDA_ERR_SHAPE;
+    if (positions == nullptr && T > 0 && (offset < 0 || offset > P - static_cast<ll>(T))) return SFDA_ERR_SHAPE;
+    sfda::RotaryLaunch L{};
+    return rotary_run(L, q, k, cos, sin, positions, position_bits, 0, position_stride, offset, qo, ko, B, Hq, Hk, T, D, rot, P, interleaved,
+                      inverse, strides, dtype, stream);
+}
+
+sfda_status_t sfda_rotary_axes(const void* q, const void* k, const float* cos, const float* sin, const void* positions,
+                               int position_bits, long long axis_stride, long long position_stride, const int* sections,
+                               int axes, int cyclic, void* qo, void* ko, int B, int Hq, int Hk, int T, int D, int P,
+                               int interleaved, int inverse, const long long* strides, sfda_dtype_t dtype,
+                               sfda_stream_t stream)
+{
+    if (!dtype_ok(dtype)) return SFDA_ERR_DTYPE;
+    if (B < 0 || Hq < 0 || Hk < 0 || T < 0 || D < 1 || D > 2 * sfda::ROTARY_PAIRS || P < 1) return SFDA_ERR_SHAPE;
+    if (axes < 1 || axes > sfda::ROTARY_AXES || (position_bits != 32 && position_bits != 64)) return SFDA_ERR_SHAPE;
+    if (sections == nullptr) return SFDA_ERR_NULL;
+    int left[sfda::ROTARY_AXES] = {}, pairs = 0;
+    for (int a = 0; a < axes; ++a) {
+        if (sections[a] < 0 || sections[a] > D / 2 - pairs) return SFDA_ERR_SHAPE;
+        pairs += left[a] = sections[a];
+    }
+    if (pairs < 1) return SFDA_ERR_SHAPE;
+    sfda::RotaryLaunch L{};
+    L.axes = axes;
+    for (int i = 0, a = 0; i < pairs; ++i) {        // in runs, or dealt to the axes in turn
+        while (left[a] == 0) a = (a + 1) % axes;
+        L.axis[i / 16] |= static_cast<unsigned>(a) << (2 * (i % 16));
+        --left[a];
+        if (cyclic) a = (a + 1) % axes;
+    }
+    return rotary_run(L, q, k, cos, sin, positions, position_bits, axis_stride, position_stride, 0, qo, ko, B, Hq, Hk, T, D, 2 * pairs, P,
+                      interleaved, inverse, strides, dtype, stream);
 }
 
 size_t sfda_decay_attn_fwd_workspace_bytes(int B, int H, int T, int dk, int dv, sfda_dtype_t dtype)
@@ -543,6 +583,264 @@ sfda_status_t sfda_group_norm_bwd(const void* dy, const void* x, const float* we
     L.B = T > 0 ? B : 0; L.H = H; L.T = std::max(T, 1); L.D = D;      // (no tokens: the weights' gradients are zeros)
     L.silu = activation == SFDA_ACT_SILU; L.eps = eps; L.bf16 = dtype == SFDA_BF16;
     return sfda::launch_norm_bwd(L, static_cast<hipStream_t>(stream)) == hipSuccess ? SFDA_OK : SFDA_ERR_HIP;
+}
+
+static bool layer_norm_sizes(int B, int T, int D, float eps)
+{
+    return B >= 0 && T >= 0 && D >= 1 && D <= sfda::LAYER_NORM_MAX && eps >= 0.f;
+}
+
+// the `which`-th [B, T, D] of a call
+static void row_strides(ll (&out)[2], const ll* given, int which, ll B, ll T, ll D)
+{
+    strides_of(out, given != nullptr ? given + 2 * which : nullptr, {B, T}, {T * D, D});
+}
+
+sfda_status_t sfda_layer_norm(const void* x, const float* weight, const float* bias, const void* residual, void* y, void* total, int B,
+                              int T, int D, float eps, const long long* strides, sfda_dtype_t dtype, sfda_stream_t stream)
+{
+    if (!dtype_ok(dtype)) return SFDA_ERR_DTYPE;
+    if (!layer_norm_sizes(B, T, D, eps)) return SFDA_ERR_SHAPE;
+    if (B == 0 || T == 0) return SFDA_OK;
+    const ll e = esize(dtype);
+    sfda::LayerNormLaunch L{};
+    row_strides(L.x_s, strides, 0, B, T, D);
+    row_strides(L.r_s, strides, 1, B, T, D);
+    row_strides(L.y_s, strides, 2, B, T, D);
+    row_strides(L.t_s, strides, 3, B, T, D);
+    Call c;
+    const int ix = c.input(box(x, e, D, {B, T}, L.x_s), e);
+    c.input(flat(weight, 4LL * D), 4, false);
+    c.input(flat(bias, 4LL * D), 4, false);
+    const int ir = c.input(box(residual, e, D, {B, T}, L.r_s), e, false);
+    c.output(box(y, e, D, {B, T}, L.y_s), e, true, residual == nullptr ? ix : -1);
+    if (residual != nullptr) c.output(box(total, e, D, {B, T}, L.t_s), e, true, total == residual ? ir : ix);
+    const sfda_status_t st = c.done();
+    if (st != SFDA_OK) return st;
+    L.x = x; L.residual = residual; L.weight = weight; L.bias = bias; L.y = y; L.total = total;
+    L.B = B; L.T = T; L.D = D; L.eps = eps; L.bf16 = dtype == SFDA_BF16;
+    return sfda::launch_layer_norm(L, static_cast<hipStream_t>(stream)) == hipSuccess ? SFDA_OK : SFDA_ERR_HIP;
+}
+
+size_t sfda_layer_norm_bwd_workspace_bytes(int B, int T, int D, sfda_dtype_t dtype)
+{
+    if (!dtype_ok(dtype) || !layer_norm_sizes(B, T, D, 0.f)) return 0;
+    return static_cast<size_t>(sfda::layer_norm_strips(static_cast<ll>(B) * T, D, dtype == SFDA_BF16)) * 2 * D * 4;
+}
+
+sfda_status_t sfda_layer_norm_bwd(const void* dy, const void* x, const float* weight, const void* dtotal, void* dx, float* dweight,
+                                  float* dbias, int B, int T, int D, float eps, const long long* strides, sfda_dtype_t dtype,
+                                  void* workspace, size_t workspace_bytes, sfda_stream_t stream)
+{
+    if (!dtype_ok(dtype)) return SFDA_ERR_DTYPE;
+    if (!layer_norm_sizes(B, T, D, eps)) return SFDA_ERR_SHAPE;
+    const ll e = esize(dtype);
+    const bool weights = dweight != nullptr || dbias != nullptr;
+    if ((B == 0 || T == 0) && !weights) return SFDA_OK;
+    const size_t need = weights ? sfda_layer_norm_bwd_workspace_bytes(B, T, D, dtype) : 0;
+    sfda::LayerNormLaunch L{};
+    row_strides(L.dy_s, strides, 0, B, T, D);
+    row_strides(L.x_s, strides, 1, B, T, D);
+    row_strides(L.dt_s, strides, 2, B, T, D);
+    row_strides(L.dx_s, strides, 3, B, T, D);
+    Call c;
+    const int idy = c.input(box(dy, e, D, {B, T}, L.dy_s), e);
+    c.input(box(x, e, D, {B, T}, L.x_s), e);
+    c.input(flat(weight, 4LL * D), 4, false);
+    const int idt = c.input(box(dtotal, e, D, {B, T}, L.dt_s), e, false);
+    c.output(box(dx, e, D, {B, T}, L.dx_s), e, true, dx == dtotal ? idt : idy);
+    c.output(flat(dweight, 4LL * D), 4, false);
+    c.output(flat(dbias, 4LL * D), 4, false);
+    if (need > 0) c.output(flat(workspace, static_cast<ll>(need)), 4);
+    sfda_status_t st = c.done();
+    if (st == SFDA_OK && need > 0 && workspace_bytes < need) st = SFDA_ERR_SHAPE;
+    if (st != SFDA_OK) return st;
+    L.dy = dy; L.x = x; L.dtotal = dtotal; L.weight = weight; L.dx = dx; L.dweight = dweight; L.dbias = dbias;
+    L.partial = weights ? static_cast<float*>(workspace) : nullptr;
+    L.B = T > 0 ? B : 0; L.T = std::max(T, 1); L.D = D; L.eps = eps; L.bf16 = dtype == SFDA_BF16;     // (no rows: the weights' gradients are zeros)
+    return sfda::launch_layer_norm_bwd(L, static_cast<hipStream_t>(stream)) == hipSuccess ? SFDA_OK : SFDA_ERR_HIP;
+}
+
+static bool delta_sizes(int B, int H, int Hk, int T, int dk, int dv)
+{
+    return Hk >= 0 && (H == 0 || (Hk > 0 && H > 0 && H % Hk == 0)) && decay_sizes(B, H, T, dk, dv);
+}
+// blocks of a sequence; heads times them stay below 2^31, launches below 2^32 threads
+static ll delta_blocks(int T, bool bf16) { return (static_cast<ll>(T) + sfda::delta_block(bf16) - 1) / sfda::delta_block(bf16); }
+static bool delta_launches(ll heads, ll blocks, int dv) { return heads * std::max(blocks + 4, (dv + 63LL) / 64) < (1LL << 32) / 256; }
+
+// the forward's part of a workspace for `heads` value heads: inverses and scalars
+static ll delta_prep_bytes(ll heads, ll blocks, bool bf16, int inverses)
+{
+    return heads * blocks * (inverses * sfda::delta_tiles(bf16) * 1024LL + sfda::delta_block(bf16) * 16LL);
+}
+
+size_t sfda_delta_attn_fwd_workspace_bytes(int B, int H, int T, int dk, int dv, sfda_dtype_t dtype)
+{
+    if (!dtype_ok(dtype) || !decay_sizes(B, H, T, dk, dv)) return 0;
+    const bool bf16 = dtype == SFDA_BF16;
+    return static_cast<size_t>(delta_prep_bytes(static_cast<ll>(B) * H, delta_blocks(T, bf16), bf16, 1));
+}
+
+sfda_status_t sfda_delta_attn_fwd(const void* q, const void* k, const void* v, const float* log_decay, const float* beta,
+                                  const int* lengths, const float* S0, void* o, float* S_T, int B, int H, int Hk, int T, int dk, int dv,
+                                  float scale, const long long* strides, sfda_dtype_t dtype, void* workspace, size_t workspace_bytes,
+                                  sfda_stream_t stream)
+{
+    if (!dtype_ok(dtype)) return SFDA_ERR_DTYPE;
+    if (!delta_sizes(B, H, Hk, T, dk, dv)) return SFDA_ERR_SHAPE;
+    const ll heads = static_cast<ll>(B) * H, e = esize(dtype), state = heads * dk * dv * 4;
+    const bool bf16 = dtype == SFDA_BF16;
+    if (heads == 0) return SFDA_OK;
+    const ll blocks = delta_blocks(T, bf16);
+    if (!delta_launches(heads, blocks, dv)) return SFDA_ERR_SHAPE;
+    sfda::DeltaLaunch L{};
+    strides3(L.q_s, strides, 0, B, Hk, T, dk);
+    strides3(L.k_s, strides, 1, B, Hk, T, dk);
+    strides3(L.v_s, strides, 2, B, H, T, dv);
+    strides3(L.l_s, strides, 3, B, H, T, 1);
+    strides3(L.b_s, strides, 4, B, H, T, 1);
+    strides3(L.o_s, strides, 5, B, H, T, dv);
+    if (!rows_fit(L.q_s, e) || !rows_fit(L.k_s, e) || !rows_fit(L.v_s, e)) return SFDA_ERR_SHAPE;
+    const size_t need = sfda_delta_attn_fwd_workspace_bytes(B, H, T, dk, dv, dtype);
+    Call c;
+    c.input(box(q, e, dk, {B, Hk, T}, L.q_s), e);
+    c.input(box(k, e, dk, {B, Hk, T}, L.k_s), e);
+    c.input(box(v, e, dv, {B, H, T}, L.v_s), e);
+    c.input(box(log_decay, 4, 1, {B, H, T}, L.l_s), 4);
+    c.input(box(beta, 4, 1, {B, H, T}, L.b_s), 4);
+    c.input(flat(lengths, 4LL * B), 4, false);
+    const int s0 = c.input(flat(S0, state), 4, false);
+    c.output(box(o, e, dv, {B, H, T}, L.o_s), e);
+    c.output(flat(S_T, state), 4, false, s0);
+    if (need > 0) c.output(flat(workspace, static_cast<ll>(need)), 16);
+    sfda_status_t st = c.done();
+    if (st == SFDA_OK && workspace_bytes < need) st = SFDA_ERR_SHAPE;
+    if (st != SFDA_OK) return st;
+    L.q = q; L.k = k; L.v = v; L.log_decay = log_decay; L.beta = beta; L.lengths = lengths; L.S0 = S0; L.o = o; L.S_T = S_T;
+    L.B = B; L.H = H; L.Hk = Hk; L.T = T; L.dk = dk; L.dv = dv; L.scale = scale; L.bf16 = bf16;
+    L.heads = static_cast<int>(heads); L.blocks = static_cast<int>(blocks);
+    L.inv = static_cast<float*>(workspace);
+    L.scalars = reinterpret_cast<float4*>(L.inv + heads * blocks * sfda::delta_tiles(bf16) * 256);
+    return sfda::launch_delta_fwd(L, static_cast<hipStream_t>(stream)) == hipSuccess ? SFDA_OK : SFDA_ERR_HIP;
+}
+
+// what one key head's value heads take: both inverses, the states and their gradients, the rows of R and du, the outputs' parts
+static ll delta_bwd_bytes(ll heads, ll blocks, int dk, int dv, bool bf16)
+{
+    const ll C = sfda::delta_block(bf16), rows = heads * blocks * C;
+    return delta_prep_bytes(heads, blocks, bf16, 2) + heads * (2 * blocks + 1) * dk * dv * 4 + rows * dv * 8 + rows * ((dv + 15) / 16) * 4 + 4 * 16;
+}
+
+size_t sfda_delta_attn_bwd_workspace_bytes(int B, int H, int Hk, int T, int dk, int dv, sfda_dtype_t dtype)
+{
+    if (!dtype_ok(dtype) || !delta_sizes(B, H, Hk, T, dk, dv)) return 0;
+    const bool bf16 = dtype == SFDA_BF16;
+    return static_cast<size_t>(delta_bwd_bytes(static_cast<ll>(B) * H, delta_blocks(T, bf16), dk, dv, bf16));
+}
+
+sfda_status_t sfda_delta_attn_bwd(const void* q, const void* k, const void* v, const float* log_decay, const float* beta,
+                                  const int* lengths, const float* S0, const void* dO, const float* dS_T, void* dq, void* dk_out,
+                                  void* dv_out, float* dlog_decay, float* dbeta, float* dS0, int B, int H, int Hk, int T, int dk, int dv,
+                                  float scale, const long long* strides, sfda_dtype_t dtype, void* workspace, size_t workspace_bytes,
+                                  sfda_stream_t stream)
+{
+    if (!dtype_ok(dtype)) return SFDA_ERR_DTYPE;
+    if (!delta_sizes(B, H, Hk, T, dk, dv)) return SFDA_ERR_SHAPE;
+    const ll heads = static_cast<ll>(B) * H, e = esize(dtype), state = heads * dk * dv * 4;
+    const bool bf16 = dtype == SFDA_BF16;
+    if (heads == 0) return SFDA_OK;
+    const ll blocks = delta_blocks(T, bf16);
+    if (!delta_launches(heads, blocks, dv)) return SFDA_ERR_SHAPE;
+    sfda::DeltaLaunch L{};
+    strides3(L.q_s, strides, 0, B, Hk, T, dk);
+    strides3(L.k_s, strides, 1, B, Hk, T, dk);
+    strides3(L.v_s, strides, 2, B, H, T, dv);
+    strides3(L.l_s, strides, 3, B, H, T, 1);
+    strides3(L.b_s, strides, 4, B, H, T, 1);
+    strides3(L.g_s, strides, 5, B, H, T, dv);
+    strides3(L.dq_s, strides, 6, B, Hk, T, dk);
+    strides3(L.dk_s, strides, 7, B, Hk, T, dk);
+    strides3(L.dv_s, strides, 8, B, H, T, dv);
+    strides3(L.dl_s, strides, 9, B, H, T, 1);
+    strides3(L.db_s, strides, 10, B, H, T, 1);
+    if (!rows_fit(L.q_s, e) || !rows_fit(L.k_s, e) || !rows_fit(L.v_s, e) || !rows_fit(L.g_s, e)) return SFDA_ERR_SHAPE;
+    // key heads of a pass
+    const ll per = H / Hk, one = delta_bwd_bytes(per, blocks, dk, dv, bf16), groups = static_cast<ll>(B) * Hk;
+    ll fit = groups;
+    if (workspace_bytes < static_cast<size_t>(delta_bwd_bytes(heads, blocks, dk, dv, bf16)))
+        fit = static_cast<ll>(std::min<size_t>(workspace_bytes / static_cast<size_t>(one), static_cast<size_t>(groups)));
+    const ll used = delta_bwd_bytes(std::max(fit, 1LL) * per, blocks, dk, dv, bf16);
+    Call c;
+    c.input(box(q, e, dk, {B, Hk, T}, L.q_s), e);
+    c.input(box(k, e, dk, {B, Hk, T}, L.k_s), e);
+    c.input(box(v, e, dv, {B, H, T}, L.v_s), e);
+    c.input(box(log_decay, 4, 1, {B, H, T}, L.l_s), 4);
+    c.input(box(beta, 4, 1, {B, H, T}, L.b_s), 4);
+    c.input(box(dO, e, dv, {B, H, T}, L.g_s), e);
+    c.input(flat(lengths, 4LL * B), 4, false);
+    c.input(flat(S0, state), 4, false);
+    c.input(flat(dS_T, state), 4, false);
+    c.output(box(dq, e, dk, {B, Hk, T}, L.dq_s), e);
+    c.output(box(dk_out, e, dk, {B, Hk, T}, L.dk_s), e);
+    c.output(box(dv_out, e, dv, {B, H, T}, L.dv_s), e);
+    c.output(box(dlog_decay, 4, 1, {B, H, T}, L.dl_s), 4);
+    c.output(box(dbeta, 4, 1, {B, H, T}, L.db_s), 4);
+    c.output(flat(dS0, state), 4, false);
+    c.output(flat(workspace, used), 16);
+    sfda_status_t st = c.done();
+    if (st == SFDA_OK && fit < 1) st = SFDA_ERR_SHAPE;
+    if (st != SFDA_OK) return st;
+    L.q = q; L.k = k; L.v = v; L.dO = dO; L.log_decay = log_decay; L.beta = beta; L.lengths = lengths; L.S0 = S0; L.dS_T = dS_T;
+    L.dq = dq; L.dk_out = dk_out; L.dv_out = dv_out; L.dlog_decay = dlog_decay; L.dbeta = dbeta; L.dS0 = dS0;
+    L.B = B; L.H = H; L.Hk = Hk; L.T = T; L.dk = dk; L.dv = dv; L.scale = scale; L.bf16 = bf16;
+    L.blocks = static_cast<int>(blocks); L.parts = (dv + 15) / 16;
+    for (ll g = 0; g < groups; g += fit) {
+        const ll n = std::min(fit, groups - g) * per, C = sfda::delta_block(bf16), inv = n * blocks * sfda::delta_tiles(bf16) * 256;
+        auto up = [](ll x) { return (x + 3) / 4 * 4; };         // (16 bytes)
+        L.first = g * per; L.heads = static_cast<int>(n);
+        float* p = static_cast<float*>(workspace);
+        L.inv = p; p += inv;
+        L.inv_back = p; p += inv;
+        L.scalars = reinterpret_cast<float4*>(p); p += n * blocks * C * 4;
+        L.rec_S = p; p += up(n * (blocks + 1) * dk * dv);
+        L.rec_U = p; p += up(n * blocks * dk * dv);
+        L.rec_R = p; p += up(n * blocks * C * dv);
+        L.rec_du = p; p += up(n * blocks * C * dv);
+        L.odo = p;
+        if (sfda::launch_delta_bwd(L, static_cast<hipStream_t>(stream)) != hipSuccess) return SFDA_ERR_HIP;
+    }
+    return SFDA_OK;
+}
+
+sfda_status_t sfda_delta_attn_step(const void* q, const void* k, const void* v, const float* log_decay, const float* beta, float* S,
+                                   void* o, int B, int H, int Hk, int dk, int dv, float scale, const long long* strides,
+                                   sfda_dtype_t dtype, sfda_stream_t stream)
+{
+    if (!dtype_ok(dtype)) return SFDA_ERR_DTYPE;
+    if (!delta_sizes(B, H, Hk, 1, dk, dv)) return SFDA_ERR_SHAPE;
+    const ll heads = static_cast<ll>(B) * H, e = esize(dtype);
+    if (heads == 0) return SFDA_OK;
+    if (!delta_launches(heads, 0, dv)) return SFDA_ERR_SHAPE;
+    sfda::DeltaStepLaunch L{};
+    ll (*to[6])[2] = {&L.q_s, &L.k_s, &L.v_s, &L.l_s, &L.b_s, &L.o_s};
+    for (int i = 0; i < 6; ++i) {
+        const ll D = i < 2 ? dk : i == 3 || i == 4 ? 1 : dv, n = i < 2 ? Hk : H;
+        strides_of(*to[i], strides != nullptr ? strides + 2 * i : nullptr, {B, n}, {n * D, D});
+    }
+    Call c;
+    c.input(box(q, e, dk, {B, Hk}, L.q_s), e);
+    c.input(box(k, e, dk, {B, Hk}, L.k_s), e);
+    c.input(box(v, e, dv, {B, H}, L.v_s), e);
+    c.input(box(log_decay, 4, 1, {B, H}, L.l_s), 4);
+    c.input(box(beta, 4, 1, {B, H}, L.b_s), 4);
+    c.output(flat(S, heads * dk * dv * 4), 4);
+    c.output(box(o, e, dv, {B, H}, L.o_s), e);
+    const sfda_status_t st = c.done();
+    if (st != SFDA_OK) return st;
+    L.q = q; L.k = k; L.v = v; L.o = o; L.S = S; L.log_decay = log_decay; L.beta = beta;
+    L.B = B; L.H = H; L.Hk = Hk; L.dk = dk; L.dv = dv; L.scale = scale; L.bf16 = dtype == SFDA_BF16;
+    return sfda::launch_delta_step(L, static_cast<hipStream_t>(stream)) == hipSuccess ? SFDA_OK : SFDA_ERR_HIP;
 }
 
 }  // extern "C"

@@ -6,41 +6,16 @@
 // are requested before a row's arithmetic, so that the reductions do not leave the memory idle.
 // bfloat16 with a silu gate, B8 H16 T4096 d 128: forward 95 us (0.40 GB, 4.2 TB/s), backward 146 us (0.67 GB, 4.6 TB/s).
 #include "sfda_layer.h"
+#include "sfda_rows.h"
 #include "sfda_vec.h"
 
 namespace sfda {
 namespace {
 
+using namespace rows;
 using namespace vec;
 
 constexpr int NT = 256;
-
-template <int CTRL> __device__ __forceinline__ float dpp(float x)
-{
-    return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), CTRL, 0xF, 0xF, false));
-}
-// sum over a group of `lpg` (a power of two) neighbouring lanes, the same for every lane of it.  Within 16 lanes by data-parallel
-// moves: the quad's neighbours, then mirrored halves, whose lanes already hold equal sums.
-__device__ __forceinline__ float group_sum(float x, int lpg)
-{
-    if (lpg > 1) x += dpp<0xB1>(x);         // quad [1, 0, 3, 2]
-    if (lpg > 2) x += dpp<0x4E>(x);         // quad [2, 3, 0, 1]
-    if (lpg > 4) x += dpp<0x141>(x);        // half row mirrored
-    if (lpg > 8) x += dpp<0x140>(x);        // row mirrored
-    if (lpg > 16) x += __shfl_xor(x, 16);
-    if (lpg > 32) x += __shfl_xor(x, 32);
-    return x;
-}
-
-// 1 / sqrt(x), x >= 0.  The hardware's instruction takes a subnormal for 0; a variance below 2^-126 (values of 1e-19) is one, and
-// with eps = 0 it counts.  The scaling takes no time that shows (bfloat16 B8 H16 T4096 d 128, in turn: forward 95.4 us and 95.0
-// without, backward 147.5 and 147.6).
-__device__ __forceinline__ float inverse_root(float x)
-{
-    const bool small = x < 0x1p-100f;
-    const float r = __builtin_amdgcn_rsqf(small ? x * 0x1p64f : x);
-    return small ? r * 0x1p32f : r;
-}
 
 // act and its derivative.  The sigmoid by the hardware's exponential and reciprocal (an ulp each, and |z| 2^-24 of the
 // exponent's own rounding); at infinities the limits: the product with 0 is taken of a finite number.

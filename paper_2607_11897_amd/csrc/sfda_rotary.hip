@@ -2,7 +2,8 @@
 // their row of the tables, (a c - b s, a s + b c) with c, s = cos, sin[p, i]; the inverse turn is the gradient.
 // Memory-bound: every element read and written once, the tables from the caches.  Lanes run along the memory: over a row's
 // units, then over the inner one of the heads and tokens; a thread takes IPT rows of the outer one, their
-// loads before their arithmetic.  bfloat16 q and k of B8 H16 T4096 d 128: 106 us, 5.1 TB/s (a large copy: 4.8); one token of 32 x 16
+// loads before their arithmetic.  With several axes a pair's row is that of its axis' position: a lane reads the rows of the axes that its own
+// pairs follow, most often one, and selects.  bfloat16 q and k of B8 H16 T4096 d 128: 106 us, 5.1 TB/s (a large copy: 4.8); one token of 32 x 16
 // rows: 4 us, a launch's.
 #include "sfda_layer.h"
 #include "sfda_vec.h"
@@ -23,10 +24,34 @@ struct RotarySide {
     unsigned threads;
 };
 
+// cos and sin of a position's pairs from `first` on, zeros past them
+template <int PAIRS> __device__ __forceinline__ void angles(const RotaryLaunch& L, long long pos, int first, int half, float (&c)[PAIRS], float (&s)[PAIRS])
+{
+    const float *cp = L.cos + pos * half + first, *sp = L.sin + pos * half + first;
+#pragma unroll
+    for (int v = 0; v < PAIRS; v += 4) {
+        if (first + v + 4 <= half) {
+            const u32x4 cv = load16(cp + v), sv = load16(sp + v);
+#pragma unroll
+            for (int e = 0; e < 4 && v + e < PAIRS; ++e) {
+                c[v + e] = __uint_as_float(cv[e]);
+                s[v + e] = __uint_as_float(sv[e]);
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4 && v + e < PAIRS; ++e) {
+                const bool is = first + v + e < half;
+                c[v + e] = is ? cp[v + e] : 0.f;
+                s[v + e] = is ? sp[v + e] : 0.f;
+            }
+        }
+    }
+}
+
 // A unit of a row.  INTER: N channels, of which those below `rot` are turned in pairs (2i, 2i + 1).
 // Halves: N pairs (i, i + rot / 2), or, past the pairs' units, N channels that pass through.
 // HIN: heads are the inner axis and a thread's rows are tokens; else the other way round (and its rows share their angles).
-template <typename E, bool INTER, bool HIN>
+template <typename E, bool INTER, bool HIN, bool AXES>
 __device__ __forceinline__ void turn(const RotaryLaunch& L, const RotarySide& S, unsigned id, unsigned units)
 {
     constexpr int N = Vec<E>::N, PAIRS = INTER ? N / 2 : N;
@@ -66,30 +91,37 @@ __device__ __forceinline__ void turn(const RotaryLaunch& L, const RotarySide& S,
         if (!live[i]) break;
         if (pairs) {
             if (HIN || i == 0) {
-                long long pos = L.offset + tok[i];
-                if (L.positions != nullptr) {
-                    const long long at = b * L.pos_b + tok[i];
-                    pos = L.pos64 ? static_cast<const long long*>(L.positions)[at] : static_cast<const int*>(L.positions)[at];
-                }
-                const bool there = pos >= 0 && pos < L.P;       // a position without a row of the tables gives NaN
-                const float *cp = L.cos + (there ? pos * half : 0) + first, *sp = L.sin + (there ? pos * half : 0) + first;
+                bool there = true;
+                if constexpr (AXES) {
+                    // 2 bits for each of the lane's pairs
+                    const unsigned axes = L.axis[first >> 4] >> (2 * (first & 15)) & ((1u << 2 * PAIRS) - 1);
 #pragma unroll
-                for (int v = 0; v < PAIRS; v += 4) {
-                    if (first + v + 4 <= half) {
-                        const u32x4 cv = load16(cp + v), sv = load16(sp + v);
+                    for (int p = 0; p < PAIRS; ++p) c[p] = s[p] = 0.f;
+                    for (int a = 0; a < L.axes; ++a) {
+                        unsigned mine = axes ^ (a * 0x5555u & ((1u << 2 * PAIRS) - 1));     // (00 where a pair follows this axis)
+                        mine = ~(mine | mine >> 1) & 0x5555u & ((1u << 2 * PAIRS) - 1);
+                        if (half - first < PAIRS) mine &= (1u << 2 * (half - first)) - 1;
+                        if (mine == 0) continue;
+                        const long long at = a * L.pos_a + b * L.pos_b + tok[i];
+                        const long long pos = L.pos64 ? static_cast<const long long*>(L.positions)[at] : static_cast<const int*>(L.positions)[at];
+                        const bool ok = pos >= 0 && pos < L.P;
+                        float ca[PAIRS], sa[PAIRS];
+                        angles<PAIRS>(L, ok ? pos : 0, first, half, ca, sa);
 #pragma unroll
-                        for (int e = 0; e < 4 && v + e < PAIRS; ++e) {
-                            c[v + e] = __uint_as_float(cv[e]);
-                            s[v + e] = __uint_as_float(sv[e]);
-                        }
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 4 && v + e < PAIRS; ++e) {
-                            const bool is = first + v + e < half;
-                            c[v + e] = is ? cp[v + e] : 0.f;
-                            s[v + e] = is ? sp[v + e] : 0.f;
-                        }
+                        for (int p = 0; p < PAIRS; ++p)
+                            if (mine >> 2 * p & 1) {
+                                c[p] = ok ? ca[p] : __builtin_nanf("");
+                                s[p] = ok ? sa[p] : __builtin_nanf("");
+                            }
                     }
+                } else {
+                    long long pos = L.offset + tok[i];
+                    if (L.positions != nullptr) {
+                        const long long at = b * L.pos_b + tok[i];
+                        pos = L.pos64 ? static_cast<const long long*>(L.positions)[at] : static_cast<const int*>(L.positions)[at];
+                    }
+                    there = pos >= 0 && pos < L.P;              // a position without a row of the tables gives NaN
+                    angles<PAIRS>(L, there ? pos : 0, first, half, c, s);
                 }
 #pragma unroll
                 for (int p = 0; p < PAIRS; ++p) {
@@ -127,20 +159,20 @@ __device__ __forceinline__ void turn(const RotaryLaunch& L, const RotarySide& S,
 }
 
 // (queries first, then keys; each may have either order of axes)
-template <typename E, bool INTER>
+template <typename E, bool INTER, bool AXES>
 __global__ __launch_bounds__(NT) void rotary_kernel(RotaryLaunch L, RotarySide Q, RotarySide K, unsigned units, int q_heads_in, int k_heads_in)
 {
     const unsigned blocks = (Q.threads + NT - 1) / NT;
     if (blockIdx.x < blocks) {
         const unsigned id = blockIdx.x * NT + threadIdx.x;
         if (id >= Q.threads) return;
-        if (q_heads_in) turn<E, INTER, true>(L, Q, id, units);
-        else turn<E, INTER, false>(L, Q, id, units);
+        if (q_heads_in) turn<E, INTER, true, AXES>(L, Q, id, units);
+        else turn<E, INTER, false, AXES>(L, Q, id, units);
     } else {
         const unsigned id = (blockIdx.x - blocks) * NT + threadIdx.x;
         if (id >= K.threads) return;
-        if (k_heads_in) turn<E, INTER, true>(L, K, id, units);
-        else turn<E, INTER, false>(L, K, id, units);
+        if (k_heads_in) turn<E, INTER, true, AXES>(L, K, id, units);
+        else turn<E, INTER, false, AXES>(L, K, id, units);
     }
 }
 
@@ -173,12 +205,13 @@ hipError_t launch_rotary(const RotaryLaunch& L, hipStream_t st)
     const RotarySide Q = side(L, L.q, L.qo, L.q_s, L.qo_s, L.Hq, units, qin), K = side(L, L.k, L.ko, L.k_s, L.ko_s, L.Hk, units, kin);
     const unsigned blocks = (Q.threads + NT - 1) / NT + (K.threads + NT - 1) / NT;
     const dim3 grid(blocks), block(NT);
-    if (L.bf16) {
-        if (L.interleaved) hipLaunchKernelGGL((rotary_kernel<uint16_t, true>), grid, block, 0, st, L, Q, K, units, qin, kin);
-        else hipLaunchKernelGGL((rotary_kernel<uint16_t, false>), grid, block, 0, st, L, Q, K, units, qin, kin);
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, st, L, Q, K, units, qin, kin); };
+    if (L.axes == 0) {
+        if (L.bf16) L.interleaved ? go(rotary_kernel<uint16_t, true, false>) : go(rotary_kernel<uint16_t, false, false>);
+        else L.interleaved ? go(rotary_kernel<float, true, false>) : go(rotary_kernel<float, false, false>);
     } else {
-        if (L.interleaved) hipLaunchKernelGGL((rotary_kernel<float, true>), grid, block, 0, st, L, Q, K, units, qin, kin);
-        else hipLaunchKernelGGL((rotary_kernel<float, false>), grid, block, 0, st, L, Q, K, units, qin, kin);
+        if (L.bf16) L.interleaved ? go(rotary_kernel<uint16_t, true, true>) : go(rotary_kernel<uint16_t, false, true>);
+        else L.interleaved ? go(rotary_kernel<float, true, true>) : go(rotary_kernel<float, false, true>);
     }
     return hipGetLastError();
 }

@@ -31,7 +31,10 @@ EXPORTS = ("sfda_chunk_fwd", "sfda_chunk_fwd_sliced", "sfda_chunk_fwd_gated", "s
            "sfda_step", "sfda_status_string", "sfda_abi_version",
            "sfda_rotary", "sfda_decay_attn_fwd", "sfda_decay_attn_fwd_workspace_bytes", "sfda_decay_attn_bwd",
            "sfda_decay_attn_bwd_workspace_bytes", "sfda_decay_attn_step", "sfda_group_norm", "sfda_group_norm_bwd",
-           "sfda_group_norm_bwd_workspace_bytes")
+           "sfda_group_norm_bwd_workspace_bytes",
+           "sfda_rotary_axes", "sfda_delta_attn_fwd", "sfda_delta_attn_fwd_workspace_bytes", "sfda_delta_attn_bwd",
+           "sfda_delta_attn_bwd_workspace_bytes", "sfda_delta_attn_step", "sfda_layer_norm", "sfda_layer_norm_bwd",
+           "sfda_layer_norm_bwd_workspace_bytes")
 
 _lib = None
 
@@ -109,9 +112,20 @@ def load_library(path: str = LIB_PATH):
     lib.sfda_decay_attn_step.argtypes = [vp] * 6 + [i] * 4 + [f, vp, i, vp]
     lib.sfda_group_norm.argtypes = [vp] * 5 + [i] * 5 + [f, vp, i, vp]
     lib.sfda_group_norm_bwd.argtypes = [vp] * 9 + [i] * 5 + [f, vp, i, vp, sz, vp]
+    lib.sfda_rotary_axes.argtypes = [vp] * 5 + [i, ll, ll] + [vp] + [i] * 2 + [vp] * 2 + [i] * 8 + [vp, i, vp]
+    lib.sfda_delta_attn_fwd.argtypes = [vp] * 9 + [i] * 6 + [f, vp, i, vp, sz, vp]
+    lib.sfda_delta_attn_bwd.argtypes = [vp] * 15 + [i] * 6 + [f, vp, i, vp, sz, vp]
+    lib.sfda_delta_attn_step.argtypes = [vp] * 7 + [i] * 5 + [f, vp, i, vp]
+    lib.sfda_layer_norm.argtypes = [vp] * 6 + [i] * 3 + [f, vp, i, vp]
+    lib.sfda_layer_norm_bwd.argtypes = [vp] * 7 + [i] * 3 + [f, vp, i, vp, sz, vp]
     for fn in (lib.sfda_rotary, lib.sfda_decay_attn_fwd, lib.sfda_decay_attn_bwd, lib.sfda_decay_attn_step,
-               lib.sfda_group_norm, lib.sfda_group_norm_bwd):
+               lib.sfda_group_norm, lib.sfda_group_norm_bwd, lib.sfda_rotary_axes, lib.sfda_delta_attn_fwd,
+               lib.sfda_delta_attn_bwd, lib.sfda_delta_attn_step, lib.sfda_layer_norm, lib.sfda_layer_norm_bwd):
         fn.restype = i
+    for fn, n in ((lib.sfda_delta_attn_fwd_workspace_bytes, 6), (lib.sfda_delta_attn_bwd_workspace_bytes, 7),
+                  (lib.sfda_layer_norm_bwd_workspace_bytes, 4)):
+        fn.argtypes = [i] * n
+        fn.restype = sz
     for fn in (lib.sfda_decay_attn_fwd_workspace_bytes, lib.sfda_decay_attn_bwd_workspace_bytes,
                lib.sfda_group_norm_bwd_workspace_bytes):
         fn.argtypes = [i] * (5 if fn is lib.sfda_group_norm_bwd_workspace_bytes else 6)
@@ -516,7 +530,7 @@ def step(q, k, v, alpha, theta, beta, S, *, o=None, out_dtype=None, stream=None)
 # Activations may have any strides with a contiguous last axis; float32 states, tables and weights are contiguous.
 
 _ACT = {"none": 0, "silu": 1}
-_STRIDES = {n: ctypes.c_longlong * n for n in (7, 8, 12, 21)}
+_STRIDES = {n: ctypes.c_longlong * n for n in (7, 8, 12, 18, 21, 33)}
 
 
 def _rows(t) -> Optional[int]:
@@ -832,3 +846,227 @@ def group_norm_bwd(dy, x, weight=None, bias=None, gate=None, *, activation: str 
     if st != 0:
         raise SfdaError(st, "sfda_group_norm_bwd")
     return dict(dx=dx, dgate=dgate, dweight=dweight, dbias=dbias)
+
+
+def rotary_axes(q, k, cos, sin, positions, sections, *, cyclic: bool = False, interleaved: bool = False, inverse: bool = False,
+                q_out=None, k_out=None, stream=None) -> Tuple:
+    """rotary for tokens with a position on each of several axes (sfda_rotary_axes): positions int32 or int64 [A,T] or [A,B,T];
+    sections: how many pairs follow each of the A (1 to 4) axes, in runs, or with cyclic dealt to the axes in turn; their sum is
+    rot / 2, the width of cos and sin.  A pair's angle is that of its own column of the tables: rotary_tables(P, rot) runs one set of
+    frequencies through all axes; torch.cat of the axes' own tables along the columns gives each axis its own (with runs).
+    Other arguments and the result as rotary's."""
+    import torch
+    lib = load_library()
+    if q.dim() != 4 or cos.dim() != 2:
+        raise ValueError("q must be [B,H,T,D] and cos [P, rot / 2]")
+    B, Hq, T, D = q.shape
+    Hk = 0 if k is None else k.shape[1]
+    code = _same_dtype(q, k=k, q_out=q_out, k_out=k_out)
+    _need_f32(cos=cos, sin=sin)
+    A, (P, half) = len(sections), cos.shape
+    if sum(sections) != half:
+        raise ValueError(f"sections {tuple(sections)} must add up to the {half} pairs of the tables")
+    if positions.dtype not in (torch.int32, torch.int64):
+        raise TypeError(f"positions must be int32 or int64 (got {positions.dtype})")
+    tq, tk = (B, Hq, T, D), (B, Hk, T, D)
+    if q_out is None:
+        q_out = _empty_as(q, tq, stream)
+    if k is None:
+        k_out = None
+    elif k_out is None:
+        k_out = _empty_as(k, tk, stream)
+    bits = 32 if positions.dtype == torch.int32 else 64
+    astride = positions.stride(0) if A > 1 and positions.dim() > 1 else 0
+    pstride = positions.stride(1) if positions.dim() == 3 and B > 1 else 0
+    _fit(("q", q, tq), ("k", k, tk), ("cos", cos, (P, half)), ("sin", sin, (P, half)), ("q_out", q_out, tq),
+         ("k_out", k_out, tk), ("positions", positions, (A, T) if positions.dim() == 2 else (A, B, T)))
+    kk, ko = (q, q_out) if k is None else (k, k_out)
+    st = lib.sfda_rotary_axes(_rows(q), _rows(k), _ptr(cos), _ptr(sin), _rows(positions), bits, astride, pstride,
+                              (ctypes.c_int * A)(*sections), A, cyclic, _rows(q_out), _rows(k_out), B, Hq, Hk, T, D, P, interleaved,
+                              inverse, _strides(3, q, kk, q_out, ko), code, _stream(stream))
+    if st != 0:
+        raise SfdaError(st, "sfda_rotary_axes")
+    return q_out, k_out
+
+
+def _scalars(t) -> Optional[int]:
+    """The pointer of a [B,H,T] tensor, of any strides."""
+    return None if t is None else t.data_ptr()
+
+
+def _heads_of(q, v) -> Tuple[int, int]:
+    """Value heads and key heads, which have to divide them."""
+    H, Hk = v.shape[1], q.shape[1]
+    if Hk == 0 and H > 0 or Hk > 0 and H % Hk:
+        raise ValueError(f"the heads of v ({H}) must be a multiple of those of q and k ({Hk})")
+    return H, Hk
+
+
+def delta_attn_fwd(q, k, v, log_decay, beta, S0=None, *, scale: float = 1.0, lengths=None, o=None, S_T=None,
+                   want_state: bool = True, workspace=None, stream=None) -> Tuple:
+    """Linear attention with the gated delta rule (sfda_delta_attn_fwd): with a_t = exp(log_decay_t),
+    S_t = a_t S_(t-1) + k_t u_t^T, u_t = beta_t (v_t - a_t S_(t-1)^T k_t), o_t = scale S_t^T q_t.  q, k: [B,Hk,T,dk]; v: [B,H,T,dv]
+    (float32 or bfloat16, any strides with a contiguous last axis: a [B,T,H,D] projection is passed as its transpose(1, 2));
+    H a multiple of Hk; log_decay, beta: [B,H,T] float32 of any strides; S0: [B,H,dk,dv] float32 or None; lengths: [B] int32 or
+    None (all T).  Returns (o [B,H,T,dv], S_T [B,H,dk,dv] float32 or None).  `workspace`: a uint8 device tensor of at least
+    delta_attn_fwd_workspace_bytes(...) bytes, allocated here if it is None."""
+    import torch
+    lib = load_library()
+    if q.dim() != 4 or v.dim() != 4:
+        raise ValueError("q and v must have 4 dimensions")
+    H, Hk = _heads_of(q, v)
+    B, _, T, dk = q.shape
+    dv = v.shape[3]
+    code = _same_dtype(q, k=k, v=v, o=o)
+    tk, tv, tg, ts = (B, Hk, T, dk), (B, H, T, dv), (B, H, T), (B, H, dk, dv)
+    if o is None:
+        o = _empty_as(v, tv, stream)
+    if S_T is None and want_state:
+        S_T = _empty(ts, torch.float32, q.device, stream)
+    _need_f32(S0=S0, S_T=S_T, log_decay=log_decay, beta=beta)
+    _int32("lengths", lengths)
+    _fit(("q", q, tk), ("k", k, tk), ("v", v, tv), ("log_decay", log_decay, tg), ("beta", beta, tg), ("lengths", lengths, (B,)),
+         ("S0", S0, ts), ("o", o, tv), ("S_T", S_T, ts), ("workspace", workspace, workspace.shape if workspace is not None else ()))
+    if workspace is None:
+        nws = lib.sfda_delta_attn_fwd_workspace_bytes(B, H, T, dk, dv, code)
+        workspace = _workspace(nws, q.device, stream) if nws else None
+    st = lib.sfda_delta_attn_fwd(_rows(q), _rows(k), _rows(v), _scalars(log_decay), _scalars(beta), _ptr(lengths), _ptr(S0), _rows(o),
+                                 _ptr(S_T), B, H, Hk, T, dk, dv, scale, _strides(3, q, k, v, log_decay, beta, o), code,
+                                 _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
+                                 _stream(stream))
+    if st != 0:
+        raise SfdaError(st, "sfda_delta_attn_fwd")
+    return o, S_T
+
+
+def delta_attn_bwd(q, k, v, log_decay, beta, S0, dO, dS_T=None, *, scale: float = 1.0, lengths=None, want_dS0: bool = True,
+                   dq=None, dk=None, dv=None, workspace=None, stream=None) -> dict:
+    """Gradients of a real loss through delta_attn_fwd (sfda_delta_attn_bwd), given dO = dL/do [B,H,T,dv] (the inputs' dtype, any
+    strides) and dS_T = dL/dS_T [B,H,dk,dv] float32 or None.  Inputs as delta_attn_fwd.  Returns dq, dk (summed over the value heads
+    that share a key head), dv (new contiguous tensors if not given), dlog_decay, dbeta [B,H,T] float32 and dS0 (float32, or None
+    without want_dS0).  `workspace`: a uint8 device tensor; with delta_attn_bwd_workspace_bytes(...) bytes all heads run at once,
+    with less in passes over groups of heads, with the same results.  If it is None it is allocated here, at most 8 GiB
+    where that holds the least that a call needs."""
+    import torch
+    lib = load_library()
+    if q.dim() != 4 or v.dim() != 4:
+        raise ValueError("q and v must have 4 dimensions")
+    H, Hk = _heads_of(q, v)
+    B, _, T, nk = q.shape
+    nv = v.shape[3]
+    code = _same_dtype(q, k=k, v=v, dO=dO, dq=dq, dk=dk, dv=dv)
+    tk, tv, tg, ts = (B, Hk, T, nk), (B, H, T, nv), (B, H, T), (B, H, nk, nv)
+    dq = _empty_as(q, tk, stream) if dq is None else dq
+    dk = _empty_as(k, tk, stream) if dk is None else dk
+    dv = _empty_as(v, tv, stream) if dv is None else dv
+    dg, db = (_empty(tg, torch.float32, q.device, stream) for _ in range(2))
+    dS0 = _empty(ts, torch.float32, q.device, stream) if want_dS0 else None
+    _need_f32(S0=S0, dS_T=dS_T, log_decay=log_decay, beta=beta)
+    _int32("lengths", lengths)
+    _fit(("q", q, tk), ("k", k, tk), ("v", v, tv), ("log_decay", log_decay, tg), ("beta", beta, tg), ("lengths", lengths, (B,)),
+         ("S0", S0, ts), ("dO", dO, tv), ("dS_T", dS_T, ts), ("dq", dq, tk), ("dk", dk, tk), ("dv", dv, tv),
+         ("workspace", workspace, workspace.shape if workspace is not None else ()))
+    if workspace is None and B * H > 0:
+        nws = lib.sfda_delta_attn_bwd_workspace_bytes(B, H, Hk, T, nk, nv, code)
+        least = lib.sfda_delta_attn_bwd_workspace_bytes(1, H // Hk, 1, T, nk, nv, code)
+        nws = max(min(nws, 8 << 30), least)
+        workspace = _try_workspace(nws, q.device, stream) if nws > least else None
+        if workspace is None and least > 0:
+            workspace = _workspace(least, q.device, stream)
+    st = lib.sfda_delta_attn_bwd(_rows(q), _rows(k), _rows(v), _scalars(log_decay), _scalars(beta), _ptr(lengths), _ptr(S0), _rows(dO),
+                                 _ptr(dS_T), _rows(dq), _rows(dk), _rows(dv), _scalars(dg), _scalars(db), _ptr(dS0), B, H, Hk, T, nk, nv,
+                                 scale, _strides(3, q, k, v, log_decay, beta, dO, dq, dk, dv, dg, db), code, _ptr(workspace),
+                                 0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(stream))
+    if st != 0:
+        raise SfdaError(st, "sfda_delta_attn_bwd")
+    return dict(dq=dq, dk=dk, dv=dv, dlog_decay=dg, dbeta=db, dS0=dS0)
+
+
+def delta_attn_fwd_workspace_bytes(B: int, H: int, T: int, dk: int, dv: int, dtype: str = "f32") -> int:
+    """The workspace of delta_attn_fwd; dtype: the activations' ("f32" or "bf16")."""
+    code = {"f32": SFDA_F32, "bf16": SFDA_BF16}[dtype]
+    return int(load_library().sfda_delta_attn_fwd_workspace_bytes(B, H, T, dk, dv, code))
+
+
+def delta_attn_bwd_workspace_bytes(B: int, H: int, Hk: int, T: int, dk: int, dv: int, dtype: str = "f32") -> int:
+    """The workspace at which delta_attn_bwd runs all heads at once; the least is that of B = 1, H / Hk value heads and one key
+    head.  dtype: the activations' ("f32" or "bf16")."""
+    code = {"f32": SFDA_F32, "bf16": SFDA_BF16}[dtype]
+    return int(load_library().sfda_delta_attn_bwd_workspace_bytes(B, H, Hk, T, dk, dv, code))
+
+
+def delta_attn_step(q, k, v, log_decay, beta, S, *, scale: float = 1.0, o=None, stream=None):
+    """One token of delta_attn_fwd (sfda_delta_attn_step).  q, k: [B,Hk,dk]; v: [B,H,dv] (any strides with a contiguous last axis);
+    log_decay, beta: [B,H] float32 of any strides; S: [B,H,dk,dv] float32, updated in place.  Returns o [B,H,dv]."""
+    lib = load_library()
+    if q.dim() != 3 or v.dim() != 3:
+        raise ValueError("q and v must have 3 dimensions")
+    H, Hk = _heads_of(q, v)
+    B, _, dk = q.shape
+    dv = v.shape[2]
+    code = _same_dtype(q, k=k, v=v, o=o)
+    tk, tv, tg = (B, Hk, dk), (B, H, dv), (B, H)
+    if o is None:
+        o = _empty_as(v, tv, stream)
+    _need_f32(S=S, log_decay=log_decay, beta=beta)
+    _fit(("q", q, tk), ("k", k, tk), ("v", v, tv), ("log_decay", log_decay, tg), ("beta", beta, tg), ("S", S, (B, H, dk, dv)), ("o", o, tv))
+    st = lib.sfda_delta_attn_step(_rows(q), _rows(k), _rows(v), _scalars(log_decay), _scalars(beta), _ptr(S), _rows(o), B, H, Hk, dk, dv,
+                                  scale, _strides(2, q, k, v, log_decay, beta, o), code, _stream(stream))
+    if st != 0:
+        raise SfdaError(st, "sfda_delta_attn_step")
+    return o
+
+
+def layer_norm(x, weight=None, bias=None, residual=None, *, eps: float = 1e-5, y=None, total=None, stream=None) -> Tuple:
+    """Rows normalised over their channels, after the residual sum where there is one (sfda_layer_norm): total = x + residual, rounded
+    to the type; y = (total - mean) / sqrt(var + eps) weight + bias.  x, residual: [B,T,D] (any strides with a contiguous last axis);
+    weight, bias: [D] float32 or None.  Returns (y, total), total None without a residual; total=residual or total=x keeps the
+    stream in place."""
+    lib = load_library()
+    if x.dim() != 3:
+        raise ValueError("x must have 3 dimensions")
+    B, T, D = x.shape
+    code = _same_dtype(x, residual=residual, y=y, total=total)
+    if y is None:
+        y = _empty_as(x, x.shape, stream)
+    if residual is None:
+        total = None
+    elif total is None:
+        total = _empty_as(x, x.shape, stream)
+    _need_f32(weight=weight, bias=bias)
+    _fit(("x", x, (B, T, D)), ("weight", weight, (D,)), ("bias", bias, (D,)), ("residual", residual, (B, T, D)), ("y", y, (B, T, D)),
+         ("total", total, (B, T, D)))
+    r, t = (x, y) if residual is None else (residual, total)
+    st = lib.sfda_layer_norm(_rows(x), _ptr(weight), _ptr(bias), _rows(residual), _rows(y), _rows(total), B, T, D, eps,
+                             _strides(2, x, r, y, t), code, _stream(stream))
+    if st != 0:
+        raise SfdaError(st, "sfda_layer_norm")
+    return y, total
+
+
+def layer_norm_bwd(dy, x, weight=None, bias=None, dtotal=None, *, eps: float = 1e-5, dx=None, workspace=None, stream=None) -> dict:
+    """Gradients of a real loss through layer_norm (sfda_layer_norm_bwd), given dy = dL/dy [B,T,D], x (the total, where there was a
+    residual) and, or None, dtotal: what reaches the total by other ways.  Returns dx, the gradient of x and of the residual alike (new
+    if not given; dx=dy or dx=dtotal is allowed), dweight and dbias (float32; None for what was not given).  `workspace`: a
+    uint8 device tensor of at least sfda_layer_norm_bwd_workspace_bytes, allocated here if None."""
+    import torch
+    lib = load_library()
+    if x.dim() != 3:
+        raise ValueError("x must have 3 dimensions")
+    B, T, D = x.shape
+    code = _same_dtype(x, dy=dy, dtotal=dtotal, dx=dx)
+    if dx is None:
+        dx = _empty_as(x, x.shape, stream)
+    dweight = None if weight is None else _empty((D,), torch.float32, x.device, stream)
+    dbias = None if bias is None else _empty((D,), torch.float32, x.device, stream)
+    _need_f32(weight=weight, bias=bias)
+    _fit(("x", x, (B, T, D)), ("dy", dy, (B, T, D)), ("weight", weight, (D,)), ("bias", bias, (D,)), ("dtotal", dtotal, (B, T, D)),
+         ("dx", dx, (B, T, D)), ("workspace", workspace, workspace.shape if workspace is not None else ()))
+    if workspace is None and (dweight is not None or dbias is not None):
+        workspace = _workspace(lib.sfda_layer_norm_bwd_workspace_bytes(B, T, D, code), x.device, stream)
+    st = lib.sfda_layer_norm_bwd(_rows(dy), _rows(x), _ptr(weight), _rows(dtotal), _rows(dx), _ptr(dweight), _ptr(dbias), B, T, D, eps,
+                                 _strides(2, dy, x, dy if dtotal is None else dtotal, dx), code, _ptr(workspace),
+                                 0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(stream))
+    if st != 0:
+        raise SfdaError(st, "sfda_layer_norm_bwd")
+    return dict(dx=dx, dweight=dweight, dbias=dbias)

@@ -1,0 +1,260 @@
+"""GPU parity of the gated delta block's operators with their float64 oracle.
+
+Error measure: max |x - ref| / max |ref| over a whole tensor.  Bars, from the arithmetic:
+  * float32 sums (states of both types, float32 outputs and gradients, gradients of decays, strengths and weights): products to
+    2^-22 and a few hundred to a few thousand terms of either sign in float32 (2^-24 each), errors growing like the square root of their
+    number, and the block's inverse, whose error a system of a condition below 100 multiplies: 2e-5.
+  * bfloat16 outputs and gradients: 2^-8 of the result's own rounding, and the operands of the products that give them
+    rounded to bfloat16 (the state or its gradient, the scores, the writes): errors of up to 2^-8 of each of many terms of either sign,
+    whose sum stays below their largest result's rounding, for each of the three or four products that make up a result: 2e-2.
+  * layer norm in bfloat16: its own rounding, 4e-3 (2^-8); rotary positions as rotary's.
+Every output lies between canary words, and rows that a call does not own keep theirs."""
+from __future__ import annotations
+
+import numpy as np
+import pytest
+
+from gpu_util import ensure_built, rel_err
+from oracle import delta as O
+from test_gpu_layer import Buf, dev, dt, f32, stored, turned
+
+pytestmark = pytest.mark.gpu
+SUM = 2e-5
+ATTN, NORM = {"f32": SUM, "bf16": 2e-2}, {"f32": SUM, "bf16": 4e-3}
+INF = float("inf")
+
+
+@pytest.fixture(scope="module", autouse=True)
+def lib():
+    import torch
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    return ensure_built()
+
+
+def say(*a):
+    print("[case]", *a, flush=True)
+
+
+# --------------------------------------------------------------------------- gated delta rule
+
+def attn(seed, B, H, Hk, T, dk, dv, dtype, state=True, lengths=None, grads=False):
+    """Keys of length 1, decays from a token's memory to none at all, with a reset and an undecayed run, strengths from 0 to 1."""
+    rng = np.random.Generator(np.random.PCG64(seed))
+
+    def unit(*shape):
+        x = rng.standard_normal(shape)
+        return stored_as(x / np.linalg.norm(x, axis=-1, keepdims=True), dtype)
+    x = dict(q=unit(B, Hk, T, dk), k=unit(B, Hk, T, dk), v=stored(rng, (B, H, T, dv), dtype))
+    g = -np.exp(rng.uniform(-7, 0.5, (B, H, 1)) + 0.5 * rng.standard_normal((B, H, T)))
+    beta = rng.random((B, H, T))
+    if T >= 8:
+        g[:, 0, T // 2] = -np.inf
+        g[:, -1, : T // 3] = 0.0
+        beta[:, 0, 3], beta[:, -1, 5] = 0.0, 1.0
+    x["log_decay"], x["beta"] = (y.astype(np.float32).astype(np.float64) for y in (g, beta))
+    x["S0"] = stored(rng, (B, H, dk, dv), "f32") if state else None
+    if grads:
+        x["dO"] = stored(rng, (B, H, T, dv), dtype)
+        x["dS_T"] = stored(rng, (B, H, dk, dv), "f32") if state else None
+    x["lengths"] = None if lengths is None else np.asarray(lengths, np.int32)
+    return x
+
+
+def stored_as(x, dtype):
+    import torch
+    return torch.from_numpy(x).to(dt(dtype)).double().numpy()
+
+
+def tokens(x, heads_inside):
+    """[B,H,T] float32 on the device, as [B,T,H] in memory or not."""
+    y = f32(x)
+    return y.transpose(1, 2).contiguous().transpose(1, 2) if heads_inside else y
+
+
+def run_fwd(x, dtype, layout, scale, poison=None, **more):
+    import torch
+    from paper_2607_11897_amd import sfda
+    B, H, T, dv = x["v"].shape
+    b = {n: Buf(x[n].shape, dt(dtype), layout, x[n]) for n in "qkv"}
+    g, be = (tokens(x[n], layout == "bthd") for n in ("log_decay", "beta"))
+    if poison is not None:
+        for i, n in enumerate(np.clip(x["lengths"], 0, T)):
+            for t in b.values():
+                t.t[i, :, n:] = poison
+            g[i, :, n:] = poison
+            be[i, :, n:] = poison
+    o = Buf(x["v"].shape, dt(dtype), layout)
+    S = Buf((B, H, x["q"].shape[-1], dv), torch.float32)
+    sfda.delta_attn_fwd(b["q"].t, b["k"].t, b["v"].t, g, be, f32(x["S0"]), scale=scale, lengths=dev(x["lengths"]), o=o.t, S_T=S.t, **more)
+    torch.cuda.synchronize()
+    o.check("o")
+    S.check("S_T")
+    return o.numpy(), S.numpy()
+
+
+def names(x, *more):
+    return {n: x[n] for n in ("q", "k", "v", "log_decay", "beta", "S0", "lengths") + more}
+
+
+CASES = [  # B, H, Hk, T, dk, dv, dtype, layout, state
+    (2, 2, 2, 1, 16, 8, "f32", "bhtd", True), (2, 4, 2, 1, 128, 128, "bf16", "bthd", True), (1, 1, 1, 0, 8, 8, "f32", "bhtd", True),
+    (1, 3, 1, 0, 8, 8, "bf16", "bhtd", False), (2, 3, 3, 31, 1, 1, "f32", "bhtd", True), (2, 3, 1, 33, 3, 5, "f32", "padded", True),
+    (1, 4, 4, 64, 64, 64, "f32", "bthd", False), (2, 3, 3, 97, 65, 66, "f32", "bhtd", True), (1, 2, 1, 130, 256, 256, "f32", "bthd", True),
+    (1, 6, 3, 65, 129, 130, "f32", "padded", True), (1, 2, 2, 200, 128, 128, "f32", "bthd", True),
+    (3, 3, 1, 63, 7, 9, "bf16", "padded", True), (2, 2, 2, 64, 32, 16, "bf16", "bthd", True), (2, 3, 3, 1, 1, 1, "bf16", "bhtd", True),
+    (1, 4, 2, 65, 64, 64, "bf16", "bhtd", False), (2, 3, 3, 200, 128, 128, "bf16", "bthd", True), (1, 3, 1, 129, 88, 74, "bf16", "bthd", True),
+    (1, 2, 2, 190, 256, 250, "bf16", "padded", True), (1, 1, 1, 700, 96, 160, "bf16", "bhtd", True),
+]
+
+
+@pytest.mark.parametrize("B,H,Hk,T,dk,dv,dtype,layout,state", CASES)
+def test_fwd(B, H, Hk, T, dk, dv, dtype, layout, state):
+    say("fwd", B, H, Hk, T, dk, dv, dtype, layout)
+    x = attn(T + dk, B, H, Hk, T, dk, dv, dtype, state)
+    o, S = run_fwd(x, dtype, layout, dk ** -0.5)
+    ro, rS = O.delta_attn(**names(x), scale=dk ** -0.5)
+    assert rel_err(o, ro) <= ATTN[dtype] and rel_err(S, rS) <= SUM
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("poison", [float("nan"), INF])
+def test_fwd_lengths(dtype, poison):
+    say("lengths", dtype, poison)
+    B, H, Hk, T, dk, dv = 6, 4, 2, 150, 40, 24
+    x = attn(9, B, H, Hk, T, dk, dv, dtype, True, [150, 0, -3, 999, 64, 33])
+    o, S = run_fwd(x, dtype, "bthd", 0.5, poison)
+    ro, rS = O.delta_attn(**names(x), scale=0.5)
+    assert rel_err(o, ro) <= ATTN[dtype] and rel_err(S, rS) <= SUM
+    assert np.array_equal(S[1], x["S0"][1]) and np.array_equal(S[2], x["S0"][2])
+    for i, n in enumerate((150, 0, 0, 150, 64, 33)):
+        assert not o[i, :, n:].any()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("dk,dv,Hk", [(128, 128, 3), (1, 1, 1), (37, 70, 3), (64, 256, 1), (256, 3, 3)])
+def test_step(dtype, dk, dv, Hk):
+    import torch
+    from paper_2607_11897_amd import sfda
+    say("step", dtype, dk, dv)
+    B, H, T = 2, 3, 4
+    x = attn(dk, B, H, Hk, T, dk, dv, dtype)
+    x["log_decay"][0, 0, 1], x["beta"][0, 1, 2] = -np.inf, 0.0
+    b = {n: Buf(x[n].shape, dt(dtype), "bthd", x[n]) for n in "qkv"}
+    g, be = (tokens(x[n], True) for n in ("log_decay", "beta"))
+    S = Buf((B, H, dk, dv), torch.float32, values=x["S0"])
+    out = []
+    for t in range(T):
+        o = Buf((B, H, 1, dv), dt(dtype), "bthd")
+        sfda.delta_attn_step(b["q"].t[:, :, t], b["k"].t[:, :, t], b["v"].t[:, :, t], g[:, :, t], be[:, :, t], S.t, scale=0.5, o=o.t[:, :, 0])
+        o.check("o")
+        out.append(o.numpy())
+    torch.cuda.synchronize()
+    S.check("S")
+    ro, rS = O.delta_attn(**names(x), scale=0.5)
+    o = np.concatenate(out, 2)
+    assert rel_err(o, ro) <= (SUM if dtype == "f32" else 4e-3) and rel_err(S.numpy(), rS) <= SUM
+
+
+# --------------------------------------------------------------------------- layer norm
+
+ROWS = [  # B, T, D, dtype, layout
+    (1, 1, 1, "f32", "bhtd"), (2, 5, 7, "f32", "padded"), (1, 33, 1001, "f32", "bhtd"), (3, 7, 64, "bf16", "bhtd"), (1, 9, 2048, "bf16", "bhtd"),
+    (2, 3, 4100, "bf16", "padded"), (1, 5, 8192, "bf16", "bhtd"), (1, 3, 8200, "f32", "bhtd"), (1, 2, 16384, "f32", "padded"),
+    (1, 4, 16384, "bf16", "bhtd"), (1, 0, 8, "f32", "bhtd"), (1, 700, 130, "bf16", "padded"), (2, 600, 257, "f32", "bhtd"),
+    (1, 1300, 520, "bf16", "bhtd"),
+]
+
+
+@pytest.mark.parametrize("B,T,D,dtype,layout", ROWS)
+@pytest.mark.parametrize("residual,affine", [(False, True), (True, True), (True, False)])
+def test_layer_norm(B, T, D, dtype, layout, residual, affine):
+    import torch
+    from paper_2607_11897_amd import sfda
+    say("layer_norm", B, T, D, dtype, layout, residual, affine)
+    rng = np.random.Generator(np.random.PCG64(D + T))
+    x, r = stored(rng, (B, T, D), dtype) + 0.0, stored(rng, (B, T, D), dtype, 3.0)
+    w, b = (1 + 0.3 * stored(rng, (D,), "f32"), stored(rng, (D,), "f32")) if affine else (None, None)
+    w, b = (None if y is None else y.astype(np.float32).astype(np.float64) for y in (w, b))
+    total = stored_as(x + r, dtype) if residual else x
+    bx, br, y, t = Buf((B, T, D), dt(dtype), layout, x), Buf((B, T, D), dt(dtype), layout, r), Buf((B, T, D), dt(dtype), layout), Buf((B, T, D), dt(dtype), layout)
+    got = sfda.layer_norm(bx.t, f32(w), f32(b), br.t if residual else None, eps=1e-3, y=y.t, total=t.t if residual else None)
+    torch.cuda.synchronize()
+    y.check("y")
+    t.check("total")
+    assert (got[1] is None) == (not residual)
+    ref = O.layer_norm(total, w, b, 1e-3)
+    assert rel_err(y.numpy(), ref) <= NORM[dtype]
+    if residual:
+        assert np.array_equal(t.numpy(), total)
+    # backward, in place of dy and of dtotal too
+    dy, d2 = stored(rng, (B, T, D), dtype), stored(rng, (B, T, D), dtype)
+    ref = O.layer_norm_backward(dy, total, w, b, d2 if residual else None, 1e-3)
+    for place in ("new", "dy", "dtotal")[: 3 if residual else 2]:
+        bt, bdy, bd2 = (Buf((B, T, D), dt(dtype), layout, z) for z in (total, dy, d2))
+        dx = {"new": Buf((B, T, D), dt(dtype), layout), "dy": bdy, "dtotal": bd2}[place]
+        g = sfda.layer_norm_bwd(bdy.t, bt.t, f32(w), f32(b), bd2.t if residual else None, eps=1e-3, dx=dx.t)
+        torch.cuda.synchronize()
+        dx.check("dx")
+        assert rel_err(dx.numpy(), ref["dx"]) <= NORM[dtype], place
+        for n in ("dweight", "dbias"):
+            assert (g[n] is None) == (not affine)
+            if affine:
+                assert rel_err(g[n].double().cpu().numpy(), ref[n]) <= SUM, n
+
+
+def test_layer_norm_in_place():
+    import torch
+    from paper_2607_11897_amd import sfda
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    x, r = (torch.randn(3, 50, 200, generator=gen, device="cuda") for _ in range(2))
+    y, t = sfda.layer_norm(x, residual=r)
+    x1, r1 = x.clone(), r.clone()
+    y1, t1 = sfda.layer_norm(x1, residual=r1, total=r1)
+    assert t1 is r1 and torch.equal(t1, t) and torch.equal(y1, y)
+    x2 = x.clone()
+    y2, t2 = sfda.layer_norm(x2, residual=r, total=x2)
+    assert torch.equal(x2, t) and torch.equal(y2, y)
+    y3, _ = sfda.layer_norm(x)
+    assert torch.equal(sfda.layer_norm(x1, y=x1)[0], y3)
+
+
+# --------------------------------------------------------------------------- rotary positions with several axes
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("interleaved,inverse,cyclic", [(False, False, False), (True, False, True), (False, True, True), (True, True, False)])
+@pytest.mark.parametrize("B,Hq,Hk,T,D,sections,layout", [
+    (2, 3, 1, 5, 16, (3, 2, 3), "bhtd"), (1, 4, 4, 17, 128, (16, 24, 24), "bthd"), (2, 2, 2, 9, 90, (10, 0, 13, 12), "padded"), (1, 2, 1, 3, 6, (1,), "bhtd"),
+    (3, 5, 2, 1, 72, (12, 20), "bthd"), (1, 1, 1, 2, 300, (40, 41, 42, 27), "bhtd"), (2, 1, 0, 4, 8, (1, 1, 1, 1), "bhtd"),
+])
+def test_rotary_axes(dtype, interleaved, inverse, cyclic, B, Hq, Hk, T, D, sections, layout):
+    import torch
+    from paper_2607_11897_amd import sfda
+    say("rotary_axes", dtype, interleaved, inverse, cyclic, B, Hq, Hk, T, D, sections, layout)
+    rng = np.random.Generator(np.random.PCG64(D + T))
+    half, P, A = sum(sections), 50, len(sections)
+    cos, sin = sfda.rotary_tables(P, 2 * half)
+    q, k = stored(rng, (B, Hq, T, D), dtype), stored(rng, (B, max(Hk, 1), T, D), dtype)
+    for bits, shape in ((np.int32, (A, B, T)), (np.int64, (A, T))):
+        pos = rng.integers(0, P, shape).astype(bits)
+        bq, bk = Buf(q.shape, dt(dtype), layout, q), Buf(k.shape, dt(dtype), layout, k)
+        oq, ok = Buf(q.shape, dt(dtype), layout), Buf(k.shape, dt(dtype), layout)
+        args = dict(cyclic=cyclic, interleaved=interleaved, inverse=inverse)
+        sfda.rotary_axes(bq.t, bk.t if Hk else None, cos, sin, dev(pos), sections, q_out=oq.t, k_out=ok.t if Hk else None, **args)
+        torch.cuda.synchronize()
+        c, s = (t.double().cpu().numpy() for t in (cos, sin))
+        for x, o in ((q, oq), (k, ok))[: 2 if Hk else 1]:
+            o.check("out")
+            assert turned(o.numpy(), O.rotary_axes(x, c, s, pos, sections, **args), dtype)
+        sfda.rotary_axes(bq.t, None, cos, sin, dev(pos), sections, q_out=bq.t, **args)         # in place
+        assert torch.equal(bq.t, oq.t)
+
+
+def test_rotary_axes_positions_outside():
+    import torch
+    from paper_2607_11897_amd import sfda
+    cos, sin = sfda.rotary_tables(4, 8)
+    q = torch.ones(1, 1, 2, 10, device="cuda")
+    pos = torch.tensor([[0, 4], [-1, 3]], dtype=torch.int32, device="cuda")
+    o, _ = sfda.rotary_axes(q, None, cos, sin, pos, (1, 3))
+    bad = torch.isnan(o[0, 0])
+    assert bad[0].tolist() == [False, True, True, True] * 2 + [False] * 2 and bad[1].tolist() == [True, False, False, False] * 2 + [False] * 2
