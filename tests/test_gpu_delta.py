@@ -258,3 +258,98 @@ def test_rotary_axes_positions_outside():
     o, _ = sfda.rotary_axes(q, None, cos, sin, pos, (1, 3))
     bad = torch.isnan(o[0, 0])
     assert bad[0].tolist() == [False, True, True, True] * 2 + [False] * 2 and bad[1].tolist() == [True, False, False, False] * 2 + [False] * 2
+
+
+# --------------------------------------------------------------------------- gated delta rule, backward
+
+def run_bwd(x, dtype, layout, scale, poison=None, **more):
+    import torch
+    from paper_2607_11897_amd import sfda
+    B, H, T, dv = x["v"].shape
+    b = {n: Buf(x[n].shape, dt(dtype), layout, x[n]) for n in ("q", "k", "v", "dO")}
+    g, be = (tokens(x[n], layout == "bthd") for n in ("log_decay", "beta"))
+    if poison is not None:
+        for i, n in enumerate(np.clip(x["lengths"], 0, T)):
+            for t in b.values():
+                t.t[i, :, n:] = poison
+            g[i, :, n:] = poison
+            be[i, :, n:] = poison
+    out = {n: Buf(x[n[1:]].shape, dt(dtype), layout) for n in ("dq", "dk", "dv")}
+    got = sfda.delta_attn_bwd(b["q"].t, b["k"].t, b["v"].t, g, be, f32(x["S0"]), b["dO"].t, f32(x["dS_T"]), scale=scale,
+                              lengths=dev(x["lengths"]), **{n: y.t for n, y in out.items()}, **more)
+    torch.cuda.synchronize()
+    for n, y in out.items():
+        y.check(n)
+    return {n: y.double().cpu().numpy() for n, y in got.items()}
+
+
+def check_bwd(got, ref, dtype):
+    for n, y in ref.items():
+        bar = ATTN[dtype] if n in ("dq", "dk", "dv") else SUM
+        assert rel_err(got[n], y) <= bar, (n, rel_err(got[n], y))
+
+
+@pytest.mark.parametrize("B,H,Hk,T,dk,dv,dtype,layout,state", CASES)
+def test_bwd(B, H, Hk, T, dk, dv, dtype, layout, state):
+    say("bwd", B, H, Hk, T, dk, dv, dtype, layout)
+    x = attn(T + dk, B, H, Hk, T, dk, dv, dtype, state, grads=True)
+    got = run_bwd(x, dtype, layout, dk ** -0.5)
+    check_bwd(got, O.delta_attn_backward(**names(x, "dO", "dS_T"), scale=dk ** -0.5), dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("poison", [float("nan"), INF])
+def test_bwd_lengths(dtype, poison):
+    say("bwd lengths", dtype, poison)
+    x = attn(9, 6, 4, 2, 150, 40, 24, dtype, True, [150, 0, -3, 999, 64, 33], grads=True)
+    got = run_bwd(x, dtype, "bthd", 0.5, poison)
+    check_bwd(got, O.delta_attn_backward(**names(x, "dO", "dS_T"), scale=0.5), dtype)
+    assert np.array_equal(got["dS0"][1], x["dS_T"][1])
+    for i, n in enumerate((150, 0, 0, 150, 64, 33)):
+        for name in ("dq", "dk", "dv", "dlog_decay", "dbeta"):
+            assert not got[name][i, :, n:].any(), name
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_bwd_in_passes(dtype):
+    """Groups of heads, as many as the workspace holds: the same results, bit by bit."""
+    import torch
+    from paper_2607_11897_amd import sfda
+    say("passes", dtype)
+    B, H, Hk, T, dk, dv = 2, 6, 3, 100, 33, 70
+    x = attn(4, B, H, Hk, T, dk, dv, dtype, grads=True)
+    ref = run_bwd(x, dtype, "bhtd", 0.3)
+    least = sfda.delta_attn_bwd_workspace_bytes(1, H // Hk, 1, T, dk, dv, dtype)
+    for n in (1, 2, 5):
+        got = run_bwd(x, dtype, "bhtd", 0.3, workspace=torch.full((n * least,), 255, dtype=torch.uint8, device="cuda"))
+        for name in ref:
+            assert np.array_equal(got[name], ref[name]), (n, name)
+    with pytest.raises(sfda.SfdaError, match="SHAPE"):
+        run_bwd(x, dtype, "bhtd", 0.3, workspace=torch.empty(least - 16, dtype=torch.uint8, device="cuda"))
+
+
+def test_bwd_against_differences():
+    """float32 gradients against central differences of the library's own forward, on a loss that one token, decay or strength moves."""
+    import torch
+    from paper_2607_11897_amd import sfda
+    say("differences")
+    x = attn(12, 1, 2, 1, 40, 8, 6, "f32", grads=True)
+    t = {n: f32(x[n]) for n in ("q", "k", "v", "log_decay", "beta", "S0")}
+    t["log_decay"][0, 0, 20] = -0.4
+    dO, dS = f32(x["dO"]), f32(x["dS_T"])
+
+    def loss(**kw):
+        o, S = sfda.delta_attn_fwd(**kw, scale=0.6)
+        return (o.double() * dO).sum() + (S.double() * dS).sum()
+    got = sfda.delta_attn_bwd(**t, dO=dO, dS_T=dS, scale=0.6)
+    rng = np.random.default_rng(0)
+    for name, y in t.items():
+        d = torch.from_numpy(rng.standard_normal(tuple(y.shape))).to("cuda")
+        d = (d / d.norm()).float()
+        h = 1e-2
+        up, down = loss(**{**t, name: y + h * d}), loss(**{**t, name: y - h * d})
+        want, have = float(up - down) / (2 * h), float((got["d" + name].double() * d).sum())
+        # off by h^2 / 6 of the third derivative along a direction of length 1, some tens of the loss's scale, and by the
+        # forward's rounding, 2^-22 of a loss of some tens over h
+        scale = float(got["d" + name].double().norm())
+        assert abs(want - have) <= 2e-2 * scale, (name, want, have)
