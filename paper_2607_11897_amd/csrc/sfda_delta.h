@@ -109,9 +109,9 @@ __device__ __forceinline__ int row_of(int f, int h, int c) { return 32 * f + 8 *
 // load and the write.  The vector that would cross a row's end is moved back to end with it and into place when it is written; rows
 // shorter than a vector are read by elements.  Rows past the n that are there are read as the last one and written as zeros; the
 // padding's zeros in LDS are never written.
-template <typename E, int COLS, int C, int STRIDE> struct RowTile {
-    static constexpr int VE = Ops<E>::VE, ES = sizeof(E), VPR = COLS / VE, RPP = NT / VPR, N = C / RPP, PLANE = C * STRIDE;
-    static_assert(NT % VPR == 0 && C % RPP == 0 && N >= 1, "whole passes");
+template <typename E, int COLS, int C, int STRIDE, int THREADS = NT> struct RowTile {
+    static constexpr int VE = Ops<E>::VE, ES = sizeof(E), VPR = COLS / VE, RPP = THREADS / VPR, N = C / RPP, PLANE = C * STRIDE;
+    static_assert(THREADS % VPR == 0 && C % RPP == 0 && N >= 1, "whole passes");
     u32x4 x[N];
 
     __device__ __forceinline__ void load(const char* base, uint32_t st, int n, int cols, int tid)

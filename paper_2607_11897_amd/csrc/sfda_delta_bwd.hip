@@ -8,6 +8,8 @@
 // which records U and du, side by side as roles of one; then all blocks at once form the products above.
 #include "sfda_delta.h"
 
+#include <type_traits>
+
 namespace sfda {
 namespace delta {
 
@@ -38,33 +40,42 @@ constexpr int SLAB = 64;        // value columns at a time
 
 template <typename E, int DKP> struct GradMem {
     typedef Block<E> B;
+    static constexpr int NW = DKP == 64 ? 4 : 8, NT = 64 * NW;
     static constexpr int C = B::C, P = B::P, SK = DKP + 8, SV = SLAB + 8, ST = C + 8;
     static constexpr int KPL = C * SK, VPL = C * SV, TPL = C * ST;
     union {
-        struct { uint16_t o[P * VPL], v[P * VPL], u[P * VPL]; } row;    // dO, dv, u: [token][value column]
+        // dO, dv, u, and times c e, -e, w: [token][value column]
+        struct { uint16_t o[P * VPL], v[P * VPL], u[P * VPL], eo[P * VPL], ev[P * VPL], wu[P * VPL]; } row;
         struct { uint16_t k[P * KPL], q[P * KPL]; } key;
     };
     uint16_t w[P * TPL], m[P * TPL];                                    // c D . dO u^T, and -(M + M^T): [i][j]
-    float e[C], wt[C], beta[C], gh[C], gl[C], db[C], vd[C], dot[NW];
+    float e[C], wt[C], beta[C], gh[C], gl[C], db[C], vd[C], dot[NW], od[NT];
 };
 
-// 4 neighbours of a row of n elements from column `col` on, zeros past them and where the row is not there
-template <typename T> __device__ __forceinline__ f32x4 four(const T* row, int col, int n, bool there)
+// 4 neighbours of a row of n elements from column `col` on, zeros past them and where the row is not there (its address has to be one);
+// WHOLE: n is a multiple of 4.  Without branches, so that loads go out together.
+template <bool WHOLE, typename T> __device__ __forceinline__ f32x4 four(const T* row, int col, int n, bool there)
 {
-    f32x4 x = zero4();
-    if (!there || col >= n) return x;
-    if (col + 4 <= n) {
+    f32x4 x;
+    if constexpr (WHOLE) {
+        const T* p = row + (col < n ? col : 0);
+        there = there && col < n;
         if constexpr (sizeof(T) == 4) {
-            memcpy(&x, row + col, 16);
+            memcpy(&x, p, 16);
         } else {
             u32x2 y;
-            memcpy(&y, row + col, 8);
+            memcpy(&y, p, 8);
             x = f32x4{lo_f32(y[0]), hi_f32(y[0]), lo_f32(y[1]), hi_f32(y[1])};
         }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = there ? x[i] : 0.f;
     } else {
 #pragma unroll
-        for (int i = 0; i < 3; ++i)
-            if (col + i < n) x[i] = value<T>(reinterpret_cast<const char*>(row + col + i));
+        for (int i = 0; i < 4; ++i) {
+            const int at = col + i < n ? col + i : n - 1;
+            const float y = value<T>(reinterpret_cast<const char*>(row + at));
+            x[i] = there && col + i < n ? y : 0.f;
+        }
     }
     return x;
 }
@@ -84,19 +95,28 @@ template <typename E> __device__ __forceinline__ void put_four(E* row, int col, 
     }
 }
 
-// One workgroup for a block of a key head, its value heads one after the other.  A wave owns DKP / 64 tiles of 16 channels of dq and dk
+// The thread's number, as a value of its own at each call: what is computed from it is not kept over the loops (spilled, it took
+// 1.9 of the 2.3 GB that the kernel wrote).
+__device__ __forceinline__ int thread()
+{
+    int x = threadIdx.x;
+    asm volatile("" : "+v"(x));
+    return x;
+}
+
+// One workgroup for a block of a key head, its value heads one after the other.  A wave owns one or two tiles of 16 channels of dq and dk
 // (rows; tokens are the columns), whose rows of the states it alone reads.
-template <typename E, int DKP> __global__ __launch_bounds__(NT) void sfda_delta_grad(DeltaLaunch L)
+template <typename E, int DKP> __global__ __launch_bounds__((GradMem<E, DKP>::NT)) void sfda_delta_grad(DeltaLaunch L)
 {
     typedef Block<E> B;
     typedef GradMem<E, DKP> M_;
-    constexpr int C = B::C, CT = B::CT, CF = B::CF, P = B::P, ES = sizeof(E), DW = DKP / 64;
+    constexpr int NW = M_::NW, NT = M_::NT, C = B::C, CT = B::CT, CF = B::CF, P = B::P, ES = sizeof(E), DW = DKP / 16 / NW;
     constexpr int SK = M_::SK, SV = M_::SV, ST = M_::ST, KPL = M_::KPL, VPL = M_::VPL, TPL = M_::TPL;
-    constexpr int RPP = NT / (SLAB / 4), N = C / RPP, TW = CT * CT / NW;    // rows of a pass, passes, tiles of scores of a wave
+    constexpr int RPP = NT / (SLAB / 4), N = C / RPP, TW = (CT * CT + NW - 1) / NW;    // rows of a pass, passes, tiles of scores of a wave
     extern __shared__ __align__(16) unsigned char smem[];
     M_& M = *reinterpret_cast<M_*>(smem);
 
-    const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, g = lane >> 4, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const unsigned group = blockIdx.x / static_cast<unsigned>(L.blocks);
     const int blk = static_cast<int>(blockIdx.x - group * static_cast<unsigned>(L.blocks)), per = L.H / L.Hk;
     const long long key = L.first / per + group;
@@ -105,6 +125,7 @@ template <typename E, int DKP> __global__ __launch_bounds__(NT) void sfda_delta_
     const int t0 = blk * C, rows = L.T - t0 < C ? L.T - t0 : C, cnt = len - t0 < 0 ? 0 : len - t0 < C ? len - t0 : C;
     const int dk = L.dk, dv = L.dv;
     const long long cells = static_cast<long long>(dk) * dv;
+    const bool whole = dv % 4 == 0;
 
     E* const dqp = static_cast<E*>(L.dq) + b * L.dq_s[0] + hk * L.dq_s[1] + t0 * L.dq_s[2];
     E* const dkp = static_cast<E*>(L.dk_out) + b * L.dk_s[0] + hk * L.dk_s[1] + t0 * L.dk_s[2];
@@ -115,10 +136,11 @@ template <typename E, int DKP> __global__ __launch_bounds__(NT) void sfda_delta_
         for (int t = 0; t < CT; ++t) dq[i][t] = dkk[i][t] = zero4();
 
 #ifdef SFDA_LDS_POISON
-    lds_poison(&M, sizeof(M_), tid, NT);
+    lds_poison(&M, sizeof(M_), threadIdx.x, NT);
     __syncthreads();
 #endif
     {   // the upper tiles of c D . dO u^T stay zero
+        const int tid = thread();
         u32x4* z = reinterpret_cast<u32x4*>(M.w);
         const u32x4 zero = {0, 0, 0, 0};
         for (int i = tid; i < P * TPL / 8; i += NT) z[i] = zero;
@@ -136,19 +158,31 @@ template <typename E, int DKP> __global__ __launch_bounds__(NT) void sfda_delta_
         float* const dlp = L.dlog_decay + b * L.dl_s[0] + h * L.dl_s[1] + t0 * L.dl_s[2];
         float* const dbp = L.dbeta + b * L.db_s[0] + h * L.db_s[1] + t0 * L.db_s[2];
 
+        const int tid = thread();
         if (cnt == 0) {                 // nothing there: zeros
             for (int i = tid; i < rows * SLAB / 4; i += NT)
                 for (int col = 4 * (i % (SLAB / 4)); col < dv; col += SLAB) put_four(dvp + (i / (SLAB / 4)) * L.dv_s[2], col, dv, zero4());
             if (tid < rows) dlp[tid * L.dl_s[2]] = dbp[tid * L.db_s[2]] = 0.f;
             continue;
         }
-        RowTile<E, DKP, C, SK> tk, tq;
-        tk.load(reinterpret_cast<const char*>(static_cast<const E*>(L.k) + b * L.k_s[0] + hk * L.k_s[1] + t0 * L.k_s[2]), static_cast<uint32_t>(L.k_s[2] * ES), cnt, dk, tid);
-        tq.load(reinterpret_cast<const char*>(static_cast<const E*>(L.q) + b * L.q_s[0] + hk * L.q_s[1] + t0 * L.q_s[2]), static_cast<uint32_t>(L.q_s[2] * ES), cnt, dk, tid);
+        RowTile<E, DKP, C, SK, NT> tk, tq;
+        auto keys = [&] {
+            tk.load(reinterpret_cast<const char*>(static_cast<const E*>(L.k) + b * L.k_s[0] + hk * L.k_s[1] + t0 * L.k_s[2]), static_cast<uint32_t>(L.k_s[2] * ES), cnt, dk, tid);
+            tq.load(reinterpret_cast<const char*>(static_cast<const E*>(L.q) + b * L.q_s[0] + hk * L.q_s[1] + t0 * L.q_s[2]), static_cast<uint32_t>(L.q_s[2] * ES), cnt, dk, tid);
+        };
+        if (DW == 1) keys();            // (ahead where there are the registers, here and below)
 
-        __syncthreads();                // (the last head's tokens and keys are read)
+        float4 sc = {0.f, 0.f, 0.f, 0.f};
+        float decay = 0.f, od = 0.f;
         if (tid < C) {
-            const float4 sc = L.scalars[row0 + tid];
+            sc = L.scalars[row0 + tid];
+            decay = L.log_decay[b * L.l_s[0] + h * L.l_s[1] + (t0 + (tid < cnt ? tid : 0)) * L.l_s[2]];
+        }
+        for (int p = tid / C; p < L.parts; p += NT / C)         // (a part of 16 columns for a thread, or two)
+            od += tid % C < cnt ? L.odo[(head * L.parts + p) * (static_cast<long long>(L.blocks) * C) + t0 + tid % C] : 0.f;
+        __syncthreads();                // (the last head's tokens and keys are read)
+        M.od[tid] = od;
+        if (tid < C) {
             const float eh = __shfl(sc.x, C - 1), el = __shfl(sc.y, C - 1);
             M.gh[tid] = sc.x;
             M.gl[tid] = sc.y;
@@ -156,74 +190,123 @@ template <typename E, int DKP> __global__ __launch_bounds__(NT) void sfda_delta_
             M.e[tid] = expf(sc.x + sc.y);
             M.wt[tid] = expf((eh - sc.x) + (el - sc.y));
         }
-        f32x4 de[DW][CT], dO[DW][CT], db[DW][CT], ws[TW], ms[TW], md[TW];
-#pragma unroll
-        for (int i = 0; i < DW; ++i)
-#pragma unroll
-            for (int t = 0; t < CT; ++t) de[i][t] = dO[i][t] = db[i][t] = zero4();
+        float dot = 0.f;
+        f32x4 ws[TW], ms[TW], md[TW];
 #pragma unroll
         for (int i = 0; i < TW; ++i) ws[i] = ms[i] = md[i] = zero4();
-        float sdb[N] = {}, svd[N] = {}, dot = 0.f;
+        float sdb[N] = {}, svd[N] = {};
 
         for (int n0 = 0; n0 < dv; n0 += SLAB) {
+            const int tid = thread(), c = tid & 15, g = (tid & 63) >> 4;
+            // all of the slab's loads are on their way before the first is waited for
+            f32x4 lu[N], lr[N], lv[N], lo[N], st[SLAB / 32][DW][4];
+            auto states = [&](int f, auto whole) {
+                constexpr bool W = decltype(whole)::value;
+#pragma unroll
+                for (int i = 0; i < DW; ++i) {
+                    const int ch = 16 * (w * DW + i) + c, col = n0 + 32 * f + 8 * g;
+                    const bool there = ch < dk;
+                    const uint32_t off = there ? static_cast<uint32_t>(ch) * dv : 0;
+                    st[f][i][0] = four<W>(S + off, col, dv, there);
+                    st[f][i][1] = four<W>(S + off, col + 4, dv, there);
+                    st[f][i][2] = four<W>(U + off, col, dv, there);
+                    st[f][i][3] = four<W>(U + off, col + 4, dv, there);
+                }
+            };
+            auto fetch = [&](auto whole) {
+                constexpr bool W = decltype(whole)::value;
+#pragma unroll
+                for (int u = 0; u < N; ++u) {
+                    const int r = tid / (SLAB / 4) + u * RPP, rr = r < cnt ? r : cnt - 1, col = n0 + 4 * (tid % (SLAB / 4));
+                    const bool there = r < cnt;
+                    lu[u] = four<W>(L.rec_du + row0 * dv + static_cast<uint32_t>(rr) * dv, col, dv, there);
+                    lr[u] = four<W>(L.rec_R + row0 * dv + static_cast<uint32_t>(rr) * dv, col, dv, there);
+                    lv[u] = four<W>(vp + rr * L.v_s[2], col, dv, there);
+                    lo[u] = four<W>(gp + rr * L.g_s[2], col, dv, there);
+                }
+                if (DW == 1) {
+#pragma unroll
+                    for (int f = 0; f < SLAB / 32; ++f) states(f, whole);
+                }
+            };
+            if (whole) fetch(std::true_type());
+            else fetch(std::false_type());
+            if (n0 == 0) {              // S' . U
+                const int size = static_cast<int>(cells);
+                if (whole) {
+#pragma unroll 4
+                    for (int i = 4 * tid; i < size; i += 4 * NT) {
+                        const f32x4 x = *reinterpret_cast<const f32x4*>(S + cells + i), y = *reinterpret_cast<const f32x4*>(U + i);
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) dot = __builtin_fmaf(x[r], y[r], dot);
+                    }
+                } else {
+#pragma unroll 4
+                    for (int i = tid; i < size; i += NT) dot = __builtin_fmaf(S[cells + i], U[i], dot);
+                }
+            }
             __syncthreads();            // (the last columns' rows are read, the tokens' factors written)
 #pragma unroll
             for (int u = 0; u < N; ++u) {
                 const int r = tid / (SLAB / 4) + u * RPP, col = n0 + 4 * (tid % (SLAB / 4));
-                const bool there = r < cnt;
-                f32x4 du = four(L.rec_du + (row0 + r) * dv, col, dv, there), R = four(L.rec_R + (row0 + r) * dv, col, dv, there);
-                const f32x4 vv = four(vp + r * L.v_s[2], col, dv, there), go = four(gp + r * L.g_s[2], col, dv, there);
-                const float be = M.beta[r];
+                const float be = M.beta[r], fe = M.e[r], fw = M.wt[r];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    sdb[u] = __builtin_fmaf(du[i], R[i], sdb[u]);
-                    du[i] *= be;
-                    R[i] *= be;
-                    svd[u] = __builtin_fmaf(vv[i], du[i], svd[u]);
+                    sdb[u] = __builtin_fmaf(lu[u][i], lr[u][i], sdb[u]);
+                    lu[u][i] *= be;
+                    lr[u][i] *= be;
+                    svd[u] = __builtin_fmaf(lv[u][i], lu[u][i], svd[u]);
                 }
-                if (r < rows && col < dv) put_four(dvp + r * L.dv_s[2], col, dv, du);
+                if (r < rows && col < dv) put_four(dvp + r * L.dv_s[2], col, dv, lu[u]);
                 const int at = r * SV + 4 * (tid % (SLAB / 4));
-                Ops<E>::put4(M.row.o + at, VPL, go);
-                Ops<E>::put4(M.row.v + at, VPL, du);
-                Ops<E>::put4(M.row.u + at, VPL, R);
+                Ops<E>::put4(M.row.o + at, VPL, lo[u]);
+                Ops<E>::put4(M.row.v + at, VPL, lu[u]);
+                Ops<E>::put4(M.row.u + at, VPL, lr[u]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    lo[u][i] *= L.scale * fe;
+                    lu[u][i] *= -fe;
+                    lr[u][i] *= fw;
+                }
+                Ops<E>::put4(M.row.eo + at, VPL, lo[u]);
+                Ops<E>::put4(M.row.ev + at, VPL, lu[u]);
+                Ops<E>::put4(M.row.wu + at, VPL, lr[u]);
             }
             __syncthreads();
 #pragma unroll
             for (int f = 0; f < SLAB / 32; ++f) {
                 if (n0 + 32 * f >= dv) break;
-                const int at = 32 * f + 8 * g, col = n0 + at;
+                const int at = 32 * f + 8 * g;
                 // dq, dk from the states: a wave's channels
-                Op<P> bo[CT], bv[CT], bu[CT];
-#pragma unroll
-                for (int t = 0; t < CT; ++t) {
-                    bo[t] = op_rows<P>(M.row.o + (16 * t + c) * SV + at, VPL);
-                    bv[t] = op_rows<P>(M.row.v + (16 * t + c) * SV + at, VPL);
-                    bu[t] = op_rows<P>(M.row.u + (16 * t + c) * SV + at, VPL);
+                if (DW > 1) {
+                    if (whole) states(f, std::true_type());
+                    else states(f, std::false_type());
                 }
+                Op<P> so[DW], uo[DW];
 #pragma unroll
                 for (int i = 0; i < DW; ++i) {
-                    const int ch = 16 * (w * DW + i) + c;
-                    const bool there = ch < dk;
-                    const long long off = there ? static_cast<long long>(ch) * dv : 0;
-                    const f32x4 s0 = four(S + off, col, dv, there), s1 = four(S + off, col + 4, dv, there);
-                    const f32x4 u0 = four(U + off, col, dv, there), u1 = four(U + off, col + 4, dv, there);
-                    const f32x4 n1 = four(S + cells + off, col, dv, there), n2 = four(S + cells + off, col + 4, dv, there);
+                    so[i] = op_of<P>(st[f][i][0], st[f][i][1]);
+                    uo[i] = op_of<P>(st[f][i][2], st[f][i][3]);
+                }
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) dot = __builtin_fmaf(n1[r], u0[r], __builtin_fmaf(n2[r], u1[r], dot));
-                    const Op<P> so = op_of<P>(s0, s1), uo = op_of<P>(u0, u1);
+                for (int t = 0; t < CT; ++t) {
+                    const int p = (16 * t + c) * SV + at;
+                    const Op<P> bo = op_rows<P>(M.row.eo + p, VPL), bv = op_rows<P>(M.row.ev + p, VPL), bu = op_rows<P>(M.row.wu + p, VPL);
 #pragma unroll
-                    for (int x = 0; x < PAIRS<P, P>; ++x)
+                    for (int y = 0; y < PAIRS<P, P>; ++y)
 #pragma unroll
-                        for (int t = 0; t < CT; ++t) {
-                            mm<P, P>(x, dO[i][t], so, bo[t]);
-                            mm<P, P>(x, de[i][t], so, bv[t]);
-                            mm<P, P>(x, db[i][t], uo, bu[t]);
+                        for (int i = 0; i < DW; ++i) {
+                            mm<P, P>(y, dq[i][t], so[i], bo);
+                            mm<P, P>(y, dkk[i][t], so[i], bv);
+                            mm<P, P>(y, dkk[i][t], uo[i], bu);
                         }
+                    __builtin_amdgcn_sched_barrier(0);      // (mixed, the tiles' operands take more registers than there are)
                 }
                 // scores (rows j, columns i): dO_i . u_j below the diagonal, dv_i . u_j on both sides of it
 #pragma unroll
                 for (int x = 0; x < TW; ++x) {
                     const int ti = (w + NW * x) / CT, tj = (w + NW * x) % CT;
+                    if (ti >= CT) break;
                     const Op<P> uj = op_rows<P>(M.row.u + (16 * tj + c) * SV + at, VPL), vj = op_rows<P>(M.row.v + (16 * tj + c) * SV + at, VPL);
                     const Op<P> oi = op_rows<P>(M.row.o + (16 * ti + c) * SV + at, VPL), vi = op_rows<P>(M.row.v + (16 * ti + c) * SV + at, VPL);
                     const Op<P> ui = op_rows<P>(M.row.u + (16 * ti + c) * SV + at, VPL);
@@ -233,15 +316,19 @@ template <typename E, int DKP> __global__ __launch_bounds__(NT) void sfda_delta_
                         if (ti >= tj) mm<P, P>(y, ms[x], uj, vi);
                         if (ti <= tj) mm<P, P>(y, md[x], vj, ui);
                     }
+                    __builtin_amdgcn_sched_barrier(0);
                 }
             }
         }
+        if (DW > 1) keys();
         __syncthreads();                // (the rows are read: keys and queries take their place)
         tk.store(M.key.k, cnt, dk, tid);
         tq.store(M.key.q, cnt, dk, tid);
+        const int lane = thread() & 63, c = lane & 15, g = lane >> 4;
 #pragma unroll
         for (int x = 0; x < TW; ++x) {
             const int ti = (w + NW * x) / CT, tj = (w + NW * x) % CT, i = 16 * ti + c;
+            if (ti >= CT) break;
             f32x4 a, m;
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
@@ -273,7 +360,8 @@ template <typename E, int DKP> __global__ __launch_bounds__(NT) void sfda_delta_
         if (tid < C) {
             float x = 0.f;
             if (tid < cnt) {
-                for (int p = 0; p < L.parts; ++p) x += L.odo[(head * L.parts + p) * (static_cast<long long>(L.blocks) * C) + t0 + tid];
+#pragma unroll
+                for (int p = 0; p < NT / C; ++p) x += M.od[p * C + tid];
                 x -= M.vd[tid];
             }
 #pragma unroll
@@ -281,26 +369,15 @@ template <typename E, int DKP> __global__ __launch_bounds__(NT) void sfda_delta_
                 const float y = __shfl_down(x, d);
                 if (tid + d < C) x += y;
             }
-            x += (M.dot[0] + M.dot[1]) + (M.dot[2] + M.dot[3]);
+#pragma unroll
+            for (int i = 0; i < NW; ++i) x += M.dot[i];
             if (tid < rows) {
                 const bool there = tid < cnt;
-                const float a = there ? L.log_decay[b * L.l_s[0] + h * L.l_s[1] + (t0 + tid) * L.l_s[2]] : 0.f;
-                dlp[tid * L.dl_s[2]] = !there || a < -128.f ? 0.f : x;      // (such a decay is 0, and so is its gradient)
+                dlp[tid * L.dl_s[2]] = !there || decay < -128.f ? 0.f : x;      // (such a decay is 0, and so is its gradient)
                 dbp[tid * L.db_s[2]] = there ? M.db[tid] : 0.f;
             }
         }
-        // the rows' factors, then the products over tokens
-#pragma unroll
-        for (int t = 0; t < CT; ++t) {
-            const float fe = M.e[16 * t + c], fw = M.wt[16 * t + c];
-#pragma unroll
-            for (int i = 0; i < DW; ++i)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    dq[i][t][r] = __builtin_fmaf(L.scale * fe, dO[i][t][r], dq[i][t][r]);
-                    dkk[i][t][r] += fw * db[i][t][r] - fe * de[i][t][r];
-                }
-        }
+        // the products over tokens
 #pragma unroll
         for (int f = 0; f < CF; ++f) {
             const int row = (32 * f + 8 * g + (c >> 2)) * SK + 4 * (c & 3);
@@ -331,9 +408,11 @@ template <typename E, int DKP> __global__ __launch_bounds__(NT) void sfda_delta_
 #pragma unroll
                         for (int i = 0; i < DW; ++i) mm<P, P>(x, dkk[i][t], qc[i], wt);
                 }
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
     }
+    const int c = thread() & 15, g = (threadIdx.x & 63) >> 4;
 #pragma unroll
     for (int t = 0; t < CT; ++t) {
         if (16 * t + c >= rows) continue;
@@ -350,13 +429,14 @@ template <typename E, int DKP> __global__ __launch_bounds__(NT) void sfda_delta_
 template <typename E, int DKP> hipError_t bwd(const DeltaLaunch& L, hipStream_t st)
 {
     constexpr size_t scans = scan_bytes<E, DKP>(), grad = sizeof(GradMem<E, DKP>);
+    constexpr int threads = GradMem<E, DKP>::NT;
     static_assert(scans <= 160 * 1024 && grad <= 160 * 1024, "one compute unit's LDS");
     const int slices = (L.dv + SLICE - 1) / SLICE;
     hipLaunchKernelGGL((sfda_delta_scans<E, DKP>), dim3(static_cast<unsigned>(L.heads) * slices, 2), dim3(NT), scans, st, L, slices);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || L.blocks == 0) return e;
     const unsigned keys = static_cast<unsigned>(L.heads / (L.H / L.Hk));
-    hipLaunchKernelGGL((sfda_delta_grad<E, DKP>), dim3(keys * L.blocks), dim3(NT), grad, st, L);
+    hipLaunchKernelGGL((sfda_delta_grad<E, DKP>), dim3(keys * L.blocks), dim3(threads), grad, st, L);
     return hipGetLastError();
 }
 template <typename E> hipError_t bwd_any(const DeltaLaunch& L, hipStream_t st)
