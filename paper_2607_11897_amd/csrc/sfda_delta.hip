@@ -206,7 +206,7 @@ template <typename E> __global__ __launch_bounds__(NT) void sfda_delta_prep(Delt
 
 // ------------------------------------------------------------------ the forward scan
 
-template <typename E, int DKP> __global__ __launch_bounds__(NT) void sfda_delta_fwd(DeltaLaunch L, int slices)
+template <typename E, int DKP> __global__ __launch_bounds__((Scan<E, DKP, FWD>::THREADS)) void sfda_delta_fwd(DeltaLaunch L, int slices)
 {
     extern __shared__ __align__(16) unsigned char smem[];
     long head;
@@ -214,15 +214,14 @@ template <typename E, int DKP> __global__ __launch_bounds__(NT) void sfda_delta_
     head_slice(blockIdx.x, slices, L.heads, head, sl);
     head = static_cast<long>(same_for_all(static_cast<uint64_t>(head)));
     sl = __builtin_amdgcn_readfirstlane(sl);
-    scan<E, DKP, FWD>(L, head, sl, smem);
+    Scan<E, DKP, FWD>::run(L, head, sl, smem);
 }
 
 template <typename E, int DKP> hipError_t fwd(const DeltaLaunch& L, hipStream_t st)
 {
-    constexpr size_t bytes = sizeof(Mem<E, DKP, FWD>);
-    static_assert(bytes <= 160 * 1024, "one compute unit's LDS");
+    typedef Scan<E, DKP, FWD> Sc;
     const int slices = (L.dv + SLICE - 1) / SLICE;
-    hipLaunchKernelGGL((sfda_delta_fwd<E, DKP>), dim3(static_cast<unsigned>(L.heads) * slices), dim3(NT), bytes, st, L, slices);
+    hipLaunchKernelGGL((sfda_delta_fwd<E, DKP>), dim3(static_cast<unsigned>(L.heads) * slices), dim3(Sc::THREADS), Sc::BYTES, st, L, slices);
     return hipGetLastError();
 }
 template <typename E> hipError_t fwd_any(const DeltaLaunch& L, hipStream_t st)

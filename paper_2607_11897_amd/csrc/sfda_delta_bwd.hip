@@ -17,12 +17,15 @@ hipError_t prep(const DeltaLaunch& L, int inverses, hipStream_t st);
 
 namespace {
 
-template <typename E, int DKP> constexpr size_t scan_bytes()
-{
-    return sizeof(Mem<E, DKP, RECORD>) > sizeof(Mem<E, DKP, ADJOINT>) ? sizeof(Mem<E, DKP, RECORD>) : sizeof(Mem<E, DKP, ADJOINT>);
-}
+template <typename E, int DKP> struct Scans {
+    typedef Scan<E, DKP, RECORD> Rec;
+    typedef Scan<E, DKP, ADJOINT> Adj;
+    static_assert(Rec::THREADS == Adj::THREADS, "roles of one launch");
+    static constexpr int THREADS = Rec::THREADS;
+    static constexpr size_t BYTES = Rec::BYTES > Adj::BYTES ? Rec::BYTES : Adj::BYTES;
+};
 
-template <typename E, int DKP> __global__ __launch_bounds__(NT) void sfda_delta_scans(DeltaLaunch L, int slices)
+template <typename E, int DKP> __global__ __launch_bounds__((Scans<E, DKP>::THREADS)) void sfda_delta_scans(DeltaLaunch L, int slices)
 {
     extern __shared__ __align__(16) unsigned char smem[];
     long head;
@@ -30,8 +33,8 @@ template <typename E, int DKP> __global__ __launch_bounds__(NT) void sfda_delta_
     head_slice(blockIdx.x, slices, L.heads, head, sl);
     head = static_cast<long>(same_for_all(static_cast<uint64_t>(head)));
     sl = __builtin_amdgcn_readfirstlane(sl);
-    if (blockIdx.y == 0) scan<E, DKP, RECORD>(L, head, sl, smem);
-    else scan<E, DKP, ADJOINT>(L, head, sl, smem);
+    if (blockIdx.y == 0) Scans<E, DKP>::Rec::run(L, head, sl, smem);
+    else Scans<E, DKP>::Adj::run(L, head, sl, smem);
 }
 
 // ------------------------------------------------------------------ the blocks' gradients
@@ -428,11 +431,12 @@ template <typename E, int DKP> __global__ __launch_bounds__((GradMem<E, DKP>::NT
 
 template <typename E, int DKP> hipError_t bwd(const DeltaLaunch& L, hipStream_t st)
 {
-    constexpr size_t scans = scan_bytes<E, DKP>(), grad = sizeof(GradMem<E, DKP>);
+    typedef Scans<E, DKP> Sc;
+    constexpr size_t grad = sizeof(GradMem<E, DKP>);
     constexpr int threads = GradMem<E, DKP>::NT;
-    static_assert(scans <= 160 * 1024 && grad <= 160 * 1024, "one compute unit's LDS");
+    static_assert(grad <= 160 * 1024, "one compute unit's LDS");
     const int slices = (L.dv + SLICE - 1) / SLICE;
-    hipLaunchKernelGGL((sfda_delta_scans<E, DKP>), dim3(static_cast<unsigned>(L.heads) * slices, 2), dim3(NT), scans, st, L, slices);
+    hipLaunchKernelGGL((sfda_delta_scans<E, DKP>), dim3(static_cast<unsigned>(L.heads) * slices, 2), dim3(Sc::THREADS), Sc::BYTES, st, L, slices);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || L.blocks == 0) return e;
     const unsigned keys = static_cast<unsigned>(L.heads / (L.H / L.Hk));
