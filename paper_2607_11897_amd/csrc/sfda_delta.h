@@ -89,6 +89,20 @@ template <int P> __device__ __forceinline__ Op<P> op_cols(const uint16_t* p, int
     }
     return o;
 }
+// the same with the lane's rows 8 g + c / 4 and 4 further given apart
+template <int P> __device__ __forceinline__ Op<P> op_cols2(const uint16_t* p, const uint16_t* q, int plane)
+{
+    typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+    Op<P> o;
+#pragma unroll
+    for (int s = 0; s < P; ++s) {
+        u32x4 w;
+        w.lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + s * plane)));
+        w.hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(q + s * plane)));
+        o.p[s] = __builtin_bit_cast(bf16x8, w);
+    }
+    return o;
+}
 // the products of parts that reach 2^-22 of the whole, the small ones first; a loop over tiles inside one over these has no product
 // wait for the last
 template <int PA, int PB> constexpr int PAIRS = PA * PB < 9 ? PA * PB : 6;
@@ -117,40 +131,56 @@ template <int P> __device__ __forceinline__ void put_parts(uint16_t* to, int pla
             for (int i = 0; i < 4; ++i) a[i] -= i & 1 ? hi_f32(p[i / 2]) : lo_f32(p[i / 2]);
     }
 }
+// exp(x) by the hardware's power of 2: off by an ulp and by |x| 2^-24 of itself, x negative
+__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504089f); }
+// The decays between token `one` and tokens four .. four + 3 of a block, from the sums of the log decays: of those that come later
+// (earlier, if `back`) the reciprocals.  Without branches: the compiler makes a branch of a masked result's every load and exponential
+// (12 of them took 2 us of a block).
+__device__ __forceinline__ void decays(float (&d)[4], const float* hi, const float* lo, int one, int four, bool back)
+{
+    const f32x4 h4 = *reinterpret_cast<const f32x4*>(hi + four), l4 = *reinterpret_cast<const f32x4*>(lo + four);
+    const float h1 = hi[one], l1 = lo[one];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) d[r] = pin(exp_of(back ? (h4[r] - h1) + (l4[r] - l1) : (h1 - h4[r]) + (l1 - l4[r])));
+}
 __device__ __forceinline__ int row_of(int f, int h, int c) { return 32 * f + 8 * (c >> 2) + 4 * h + (c & 3); }     // of a tile's row c
+
+// Rows of keys and queries in LDS, DKP channels each: the 16-byte units of row i change places by x(i) = 4 (i % 4) + i / 4 % 4, so that what
+// is read at a time lies on different banks: one unit of 8 rows (i .. i + 7, or two fours 8 apart), or four neighbouring
+// units of 4 rows (of 64 channels, whose rows are 8 units long, by x(i) / 2).  An index of channel 32 f of a row is that of
+// channel 0 with 32 f in exclusive or.
+template <int DKP> struct KeyRows {
+    static constexpr int MASK = DKP >= 128 ? 15 : 7, SHIFT = DKP >= 128 ? 0 : 1;
+    static __device__ __forceinline__ int at(int row, int unit) { return row * DKP + 8 * (unit ^ ((4 * (row & 3) + (row >> 2 & 3)) >> SHIFT)); }
+};
+
+// A value that the compiler takes for another one at each call: what is computed from it is not kept over a loop (and spilled; a
+// reload waits for all loads before it)
+__device__ __forceinline__ int anew(int x)
+{
+    asm volatile("" : "+v"(x));
+    return x;
+}
 
 // A block's rows of one tensor on their way to LDS: C tokens x COLS channels (padded), 16-byte vectors held in registers between the
 // load and the write.  The vector that would cross a row's end is moved back to end with it and into place when it is written; rows
 // shorter than a vector are read by elements.  Rows past the n that are there are read as the last one and written as zeros; the
 // padding's zeros in LDS are never written.
-template <typename E, int COLS, int C, int STRIDE, int THREADS = NT> struct RowTile {
+template <typename E, int COLS, int C, int STRIDE, int THREADS = NT, bool SWAPPED = false> struct RowTile {
     static constexpr int VE = Ops<E>::VE, ES = sizeof(E), VPR = COLS / VE, RPP = THREADS / VPR, N = C / RPP, PLANE = C * STRIDE;
     static_assert(THREADS % VPR == 0 && C % RPP == 0 && N >= 1, "whole passes");
     u32x4 x[N];
 
-    __device__ __forceinline__ void load(const char* base, uint32_t st, int n, int cols, int tid)
+    __device__ __forceinline__ void load(const char* base, uint32_t st, int n, int cols, int thread)
     {
-        const int col = (tid % VPR) * VE, r0 = tid / VPR;
-        if (cols < VE) {
+        const int tid = anew(thread), col = (tid % VPR) * VE, r0 = tid / VPR;
+        const uint32_t at = (col + VE <= cols ? col : col >= cols || cols < VE ? 0 : cols - VE) * ES;
 #pragma unroll
-            for (int u = 0; u < N; ++u) {
-                const int r = r0 + u * RPP;
-                x[u] = u32x4{0, 0, 0, 0};
-                if (col == 0) x[u] = short_row<E>(base + static_cast<uint64_t>(r < n ? r : n - 1) * st, cols);
-            }
-            return;
-        }
-        const uint32_t at = (col + VE <= cols ? col : col >= cols ? 0 : cols - VE) * ES;
-        if (n == C) {
-            const uint32_t lane = r0 * st + at;
-#pragma unroll
-            for (int u = 0; u < N; ++u) x[u] = load16(base + static_cast<uint64_t>(u * RPP) * st + lane);
-        } else {
-#pragma unroll
-            for (int u = 0; u < N; ++u) {
-                const int r = r0 + u * RPP;
-                x[u] = load16(base + ((r < n ? r : n - 1) * st + at));
-            }
+        for (int u = 0; u < N; ++u) {
+            const int r = r0 + u * RPP;
+            const uint32_t off = (r < n ? r : n - 1) * st + at;
+            if (cols >= VE) x[u] = load16(base + off);
+            else x[u] = col == 0 ? short_row<E>(base + off, cols) : u32x4{0, 0, 0, 0};
         }
     }
     __device__ __forceinline__ void store(uint16_t* lds, int n, int cols, int tid) const
@@ -162,7 +192,8 @@ template <typename E, int COLS, int C, int STRIDE, int THREADS = NT> struct RowT
             const int r = tid / VPR + u * RPP;
             u32x4 w = r < n ? x[u] : u32x4{0, 0, 0, 0};
             if (cols % VE != 0 && past > 0) w = move_down<E>(w, past);
-            Ops<E>::put(lds + r * STRIDE + col, PLANE, w);
+            uint16_t* to = lds + (SWAPPED ? KeyRows<COLS>::at(r, col / 8) + col % 8 : r * STRIDE + col);
+            Ops<E>::put(to, PLANE, w);
         }
     }
 };
@@ -190,7 +221,7 @@ template <typename E, int COUNT, typename First>
 __device__ __forceinline__ void column(uint32_t (&x)[COUNT], const char* base, uint32_t col, uint32_t st, int n, int whole, int g, First first)
 {
     if (n == whole) {
-        const uint32_t lane = 8 * g * st + col;
+        const uint32_t lane = 8 * anew(g) * st + col;
 #pragma unroll
         for (int i = 0; i < COUNT; ++i) x[i] = bits<E>(base + static_cast<uint64_t>(first(i)) * st + lane);
     } else {
@@ -240,11 +271,11 @@ template <typename E, int DKP, int MODE> __device__ __forceinline__ void scan(co
     const uint32_t gst = MODE == FWD ? 0 : static_cast<uint32_t>(L.g_s[2] * ES);
     const uint32_t col = (in ? n : dv - 1) * ES;
     const float* const tmat = (BACK ? L.inv_back : L.inv) + head * L.blocks * static_cast<long long>(TILES * 256);
-    const float4* const scal = L.scalars + head * L.blocks * static_cast<long long>(C);
+    const float4* const scal = L.scalars + 2 * (head * L.blocks * static_cast<long long>(C));
 
     RowTile<E, DKP, C, SK> tk, tq;
     f32x4 tt[(TILES * 64 + NT - 1) / NT];
-    float4 sc = {0.f, 0.f, 0.f, 0.f};
+    float4 sc[2];
     uint32_t vr[CT * 4];                    // V, or dO
     auto fetch = [&](int blk) {
         const int t0 = blk * C, cnt = len - t0 < C ? len - t0 : C;
@@ -255,7 +286,9 @@ template <typename E, int DKP, int MODE> __device__ __forceinline__ void scan(co
             const int at = tid + u * NT < TILES * 64 ? tid + u * NT : 0;
             tt[u] = *reinterpret_cast<const f32x4*>(tmat + static_cast<long long>(blk) * TILES * 256 + 4 * at);
         }
-        if (tid < C) sc = scal[static_cast<long long>(blk) * C + tid];
+        const int tok = tid < C ? tid : 0;
+        sc[0] = scal[2 * (static_cast<long long>(blk) * C + tok)];
+        sc[1] = scal[2 * (static_cast<long long>(blk) * C + tok) + 1];
         if (on) {
             if constexpr (BACK) column<E>(vr, gp + static_cast<long long>(t0) * gst, col, gst, cnt, C, g, [](int i) { return 32 * (i / 8) + i % 8; });
             else column<E>(vr, vp + static_cast<long long>(t0) * vst, col, vst, cnt, C, g, [](int i) { return 32 * (i / 8) + i % 8; });
@@ -310,19 +343,14 @@ template <typename E, int DKP, int MODE> __device__ __forceinline__ void scan(co
             if (tile < TILES) Ops<float>::put4(M.t + (16 * (BACK ? tj : ti) + row) * ST + 16 * (BACK ? ti : tj) + c4, TPL, tt[u]);
         }
         if (tid < C) {
-            const float eh = __shfl(sc.x, C - 1), el = __shfl(sc.y, C - 1);
-            M.gh[tid] = sc.x;
-            M.gl[tid] = sc.y;
-            M.beta[tid] = sc.z;
-            M.e[tid] = expf(sc.x + sc.y);
-            M.w[tid] = expf((eh - sc.x) + (el - sc.y));
+            M.gh[tid] = sc[0].x;
+            M.gl[tid] = sc[0].y;
+            M.beta[tid] = sc[0].z;
+            M.e[tid] = sc[0].w;
+            M.w[tid] = sc[1].x;
             if (tid == 0) {
-                // the block's decay as hi + lo: a state that lives for thousands of blocks keeps its 24 bits
-                const float x = eh + el;
-                const bool near = x > -0.5f && x < 0.5f;
-                const float m = near ? expm1f(x) : 0.f, hi = near ? 1.f + m : expf(x);
-                M.end[0] = hi;
-                M.end[1] = near ? m - (hi - 1.f) : 0.f;
+                M.end[0] = sc[1].z;
+                M.end[1] = sc[1].w;
             }
         }
         __syncthreads();
@@ -343,11 +371,12 @@ template <typename E, int DKP, int MODE> __device__ __forceinline__ void scan(co
 #pragma unroll
                 for (int i = 0; i < PAIRS<P, P>; ++i) mm<P, P>(i, s, a, bb);
             }
+            float decay[4];
+            decays(decay, M.gh, M.gl, 16 * (BACK ? tj : ti) + c, 16 * (BACK ? ti : tj) + 4 * g, BACK);
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const int i = 16 * ti + (BACK ? 4 * g + r : c), j = 16 * tj + (BACK ? c : 4 * g + r);
-                const float d = expf((M.gh[i] - M.gh[j]) + (M.gl[i] - M.gl[j]));
-                s[r] = j <= i ? s[r] * (d * (BACK ? L.scale : L.scale * M.beta[j])) : 0.f;
+                s[r] = masked(j <= i, s[r] * (decay[r] * (BACK ? L.scale : L.scale * M.beta[j])));
             }
             uint16_t* to = BACK ? M.p + (16 * tj + c) * ST + 16 * ti + 4 * g : M.p + (16 * ti + c) * ST + 16 * tj + 4 * g;
             if constexpr (PP == 1) Ops<uint16_t>::put4(to, 0, s);
@@ -602,7 +631,7 @@ template <typename E, int DKP, int MODE> struct PairMem {
     // results (0.0017 their own rounding), P in two 0.0024
     static constexpr int C = B::C, P = B::P, OP = MODE == FWD ? P : 3, PP = MODE == FWD && P == 1 ? 2 : 3;
     typedef Tri<C, BACK> T;
-    static constexpr int SK = DKP + 8, KPL = C * SK, TPL = T::SIZE, DF = DKP / 32, DT = DKP / 16;
+    static constexpr int KPL = C * DKP, TPL = T::SIZE, DF = DKP / 32, DT = DKP / 16;
     uint16_t k[P * KPL], q[P * KPL], t[3 * TPL], p[PP * TPL];
     union {
         struct { u32x4 s[NW][DF * OP][64], r[NW][B::CF * OP][64]; } fwd;        // the state and R
@@ -620,8 +649,9 @@ template <typename E, int DKP, int MODE, bool chain> __device__ __forceinline__ 
     typedef Block<E> B;
     typedef PairMem<E, DKP, MODE> M_;
     typedef typename M_::T Tr;
+    typedef KeyRows<DKP> Key;
     constexpr int C = B::C, CT = B::CT, CF = B::CF, P = B::P, PP = M_::PP, OP = M_::OP, TILES = B::TILES, ES = sizeof(E);
-    constexpr int DT = DKP / 16, DF = DKP / 32, SK = M_::SK, KPL = M_::KPL, TPL = M_::TPL, NTT = (TILES * 64 + PAIR_NT - 1) / PAIR_NT;
+    constexpr int DT = DKP / 16, DF = DKP / 32, KPL = M_::KPL, TPL = M_::TPL, NTT = (TILES * 64 + NT - 1) / NT;
     constexpr int NSC = (TILES + NW - 1) / NW;      // tiles of P of a helper
     constexpr bool BACK = MODE == ADJOINT;
     M_& M = *reinterpret_cast<M_*>(smem);
@@ -644,22 +674,26 @@ template <typename E, int DKP, int MODE, bool chain> __device__ __forceinline__ 
     const uint32_t gst = MODE == FWD ? 0 : static_cast<uint32_t>(L.g_s[2] * ES);
     const uint32_t col = (in ? n : dv - 1) * ES;
     const float* const tmat = (BACK ? L.inv_back : L.inv) + head * L.blocks * static_cast<long long>(TILES * 256);
-    const float4* const scal = L.scalars + head * L.blocks * static_cast<long long>(C);
+    const float4* const scal = L.scalars + 2 * (head * L.blocks * static_cast<long long>(C));
 
-    RowTile<E, DKP, C, SK, PAIR_NT> tk, tq;
+    RowTile<E, DKP, C, DKP, PAIR_NT, true> tk, tq;
     f32x4 tt[NTT];
-    float4 sc = {0.f, 0.f, 0.f, 0.f};
+    float4 sc[2];
     uint32_t vr[CT * 4];                    // V, or dO
     auto fetch = [&](int blk) {
         const int t0 = blk * C, cnt = len - t0 < C ? len - t0 : C;
         tk.load(kp + static_cast<long long>(t0) * kst, kst, cnt, dk, tid);
         tq.load(qp + static_cast<long long>(t0) * qst, qst, cnt, dk, tid);
+        if constexpr (!chain) {
 #pragma unroll
-        for (int u = 0; u < NTT; ++u) {
-            const int at = tid + u * PAIR_NT < TILES * 64 ? tid + u * PAIR_NT : 0;
-            tt[u] = *reinterpret_cast<const f32x4*>(tmat + static_cast<long long>(blk) * TILES * 256 + 4 * at);
+            for (int u = 0; u < NTT; ++u) {
+                const int at = tid - NT + u * NT < TILES * 64 ? tid - NT + u * NT : 0;
+                tt[u] = *reinterpret_cast<const f32x4*>(tmat + static_cast<long long>(blk) * TILES * 256 + 4 * at);
+            }
+            const int tok = tid - NT < C ? tid - NT : 0;
+            sc[0] = scal[2 * (static_cast<long long>(blk) * C + tok)];
+            sc[1] = scal[2 * (static_cast<long long>(blk) * C + tok) + 1];
         }
-        if (tid < C) sc = scal[static_cast<long long>(blk) * C + tid];
         if (!on) return;
         // tile (f, h) row 4 g + r is token 32 f + 8 g + 4 h + r: the 8 neighbours of a lane are i = 4 h + r of both tiles
         if constexpr (BACK) {
@@ -693,22 +727,22 @@ template <typename E, int DKP, int MODE, bool chain> __device__ __forceinline__ 
             for (int r = 0; r < 4; ++r)
                 if (in && channel(d, r) < dk) S[d][r] = src[channel(d, r) * dv + n];
     }
+    // (addresses the same for all lanes, and 32-bit offsets)
+    auto put = [](float* to, int at, float x) { *reinterpret_cast<float*>(reinterpret_cast<char*>(to) + static_cast<uint32_t>(4 * at)) = x; };
     auto record = [&](float* to) {
-        float* const at = to + (8 * g) * dv + n;
-        if (dk == DKP) {
-            if (in)
+        int at = 8 * g * dv + n;
+        const int most = in ? dk - 8 * g : 0;           // (channels of the lane's)
+        asm volatile("" : "+v"(at));
 #pragma unroll
-                for (int d = 0; d < DT; ++d)
+        for (int d = 0; d < DT; ++d)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) at[(32 * (d / 2) + 4 * (d & 1) + r) * dv] = S[d][r];
-        } else {
-#pragma unroll
-            for (int d = 0; d < DT; ++d)
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    if (in && channel(d, r) < dk) at[(32 * (d / 2) + 4 * (d & 1) + r) * dv] = S[d][r];
-        }
+            for (int r = 0; r < 4; ++r) {
+                const int ch = 32 * (d / 2) + 4 * (d & 1) + r;
+                if (ch < most) put(to + ch * dv, at, S[d][r]);
+            }
     };
+    // a row of R or du
+    auto rows_of = [&](float* rec, int t0) { return rec + (head * (static_cast<long long>(L.blocks) * C) + t0) * dv; };
     // P's tile `x` of the helper: row and column tile
     auto tile_row = [](int tile) { return tile < 1 ? 0 : tile < 3 ? 1 : tile < 6 ? 2 : 3; };
 
@@ -716,77 +750,79 @@ template <typename E, int DKP, int MODE, bool chain> __device__ __forceinline__ 
     f32x4 x[BACK ? 1 : CT], ps[NSC];        // outputs and tiles of P, of the helpers
     float et[BACK ? 1 : CT];
 
+    Op<3> s3[chain ? DF : 1];               // the state as an operand
+    auto split = [&](int f) { s3[f] = op_of<3>(S[2 * f], S[2 * f + 1]); };
+    if constexpr (chain) {
+#pragma unroll
+        for (int f = 0; f < DF; ++f) split(f);
+    }
+
 #pragma clang loop unroll(disable)
-    for (int it = 0; it <= blocks; ++it) {
+    for (int it = 0; it < (BACK ? blocks : blocks + 1); ++it) {
         const bool work = it < blocks;
         const int blk = BACK ? blocks - 1 - it : it, t0 = blk * C, cnt = len - t0 < C ? len - t0 : C;
+        // a lane's elements of keys and queries: by columns, rows 8 g + c / 4 and 4 further; by rows, of a tile's h = 0 and 1 and of 16 rows in
+        // their order.  (Given anew for each block, or their places for all channels are kept over the blocks, and spilled.)
+        int at0 = Key::at(8 * g + (c >> 2), c & 3), at1 = Key::at(8 * g + 4 + (c >> 2), c & 3);
+        int row0 = Key::at(row_of(0, 0, c), g), row1 = Key::at(row_of(0, 1, c), g), rown = Key::at(c, g);
+        asm volatile("" : "+v"(at0), "+v"(at1), "+v"(row0), "+v"(row1), "+v"(rown));
         __syncthreads();                    // (the last block's operands are read)
         if (work) {
             tk.store(M.k, cnt, dk, tid);
             tq.store(M.q, cnt, dk, tid);
-#pragma unroll
-            for (int u = 0; u < NTT; ++u) {
-                const int at = tid + u * PAIR_NT, tile = at >> 6, row = (at & 63) >> 2, c4 = 4 * (at & 3);
-                const int ti = tile_row(tile), tj = tile - ti * (ti + 1) / 2;
-                if (tile < TILES) put_parts<3>(M.t + Tr::row(16 * (BACK ? tj : ti) + row) + 16 * (BACK ? ti : tj) + c4, TPL, tt[u]);
-            }
-            if (tid < C) {
-                const float eh = __shfl(sc.x, C - 1), el = __shfl(sc.y, C - 1);
-                M.gh[tid] = sc.x;
-                M.gl[tid] = sc.y;
-                M.beta[tid] = sc.z;
-                M.e[tid] = expf(sc.x + sc.y);
-                M.w[tid] = expf((eh - sc.x) + (el - sc.y));
-                if (tid == 0) {
-                    // the block's decay as hi + lo: a state that lives for thousands of blocks keeps its 24 bits
-                    const float s = eh + el;
-                    const bool near = s > -0.5f && s < 0.5f;
-                    const float m = near ? expm1f(s) : 0.f, hi = near ? 1.f + m : expf(s);
-                    M.end[0] = hi;
-                    M.end[1] = near ? m - (hi - 1.f) : 0.f;
-                }
-            }
         }
-        Op<3> s3[DF];
-        if (chain && on) {
-            if constexpr (BACK) {
-                if (it > 0) {
+        if constexpr (chain) {
+            if (on) {
+                if constexpr (!BACK) {
+                    if (it > 0) {
 #pragma unroll
-                    for (int d = 0; d < DT; ++d) {
-                        const f32x4 y = M.add[w][d][lane];
+                        for (int f = 0; f < CF; ++f)
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) S[d][r] += y[r];
+                            for (int s = 0; s < OP; ++s) M.fwd.r[w][f * OP + s][lane] = __builtin_bit_cast(u32x4, ro[f].p[s]);
+                    }
+                    if (work) {
+#pragma unroll
+                        for (int f = 0; f < DF; ++f)
+#pragma unroll
+                            for (int s = 0; s < OP; ++s) M.fwd.s[w][f * OP + s][lane] = __builtin_bit_cast(u32x4, s3[f].p[s]);
                     }
                 }
-            } else if (it > 0) {
-#pragma unroll
-                for (int f = 0; f < CF; ++f)
-#pragma unroll
-                    for (int s = 0; s < OP; ++s) M.fwd.r[w][f * OP + s][lane] = __builtin_bit_cast(u32x4, ro[f].p[s]);
-            }
-            if (work) {
-#pragma unroll
-                for (int f = 0; f < DF; ++f) {
-                    s3[f] = op_of<3>(S[2 * f], S[2 * f + 1]);
-                    if constexpr (!BACK) {
-#pragma unroll
-                        for (int s = 0; s < OP; ++s) M.fwd.s[w][f * OP + s][lane] = __builtin_bit_cast(u32x4, s3[f].p[s]);
-                    }
+                if constexpr (MODE == RECORD) {
+                    if (work) record(L.rec_S + (head * (L.blocks + 1) + blk) * cells);
                 }
-                if constexpr (MODE == RECORD) record(L.rec_S + (head * (L.blocks + 1) + blk) * cells);
                 if constexpr (MODE == ADJOINT) record(L.rec_U + (head * L.blocks + blk) * cells);
             }
-        }
-        if constexpr (!BACK) {
-            if (!chain && it > 0) {
+        } else {
+            if (work) {
+                const int htid = tid - NT;
 #pragma unroll
-                for (int i = 0; i < NSC; ++i) {
-                    const int tile = w + NW * i, ti = tile_row(tile), tj = tile - ti * (ti + 1) / 2;
-                    if (tile < TILES) put_parts<PP>(M.p + Tr::row(16 * ti + c) + 16 * tj + 4 * g, TPL, ps[i]);
+                for (int u = 0; u < NTT; ++u) {
+                    const int at = htid + u * NT, tile = at >> 6, row = (at & 63) >> 2, c4 = 4 * (at & 3);
+                    const int ti = tile_row(tile), tj = tile - ti * (ti + 1) / 2;
+                    if (tile < TILES) put_parts<3>(M.t + Tr::row(16 * (BACK ? tj : ti) + row) + 16 * (BACK ? ti : tj) + c4, TPL, tt[u]);
+                }
+                if (htid < C) {
+                    M.gh[htid] = sc[0].x;
+                    M.gl[htid] = sc[0].y;
+                    M.beta[htid] = sc[0].z;
+                    M.e[htid] = sc[0].w;
+                    M.w[htid] = BACK ? sc[1].x : sc[1].y;       // (forward: w beta)
+                    if (htid == 0) {
+                        M.end[0] = sc[1].z;
+                        M.end[1] = sc[1].w;
+                    }
+                }
+            }
+            if constexpr (!BACK) {
+                if (it > 0) {
+#pragma unroll
+                    for (int i = 0; i < NSC; ++i) {
+                        const int tile = w + NW * i, ti = tile_row(tile), tj = tile - ti * (ti + 1) / 2;
+                        if (tile < TILES) put_parts<PP>(M.p + Tr::row(16 * ti + c) + 16 * tj + 4 * g, TPL, ps[i]);
+                    }
                 }
             }
         }
-        if (BACK && !work) break;
         __syncthreads();
         uint32_t vv[CT * 4];
 #pragma unroll
@@ -795,121 +831,182 @@ template <typename E, int DKP, int MODE, bool chain> __device__ __forceinline__ 
 
         // tiles of P [i][j] times c beta_j, or of P^T times c
         auto scores = [&] {
+            constexpr int AHEAD = P == 1 ? 2 : 1;       // (float32: the registers of one tile's operands)
+            Op<P> kf[AHEAD][DF], qf[AHEAD][DF];
+            auto operands = [&](int x) {
+                const int tile = w + NW * x < TILES ? w + NW * x : 0, ti = tile_row(tile), tj = tile - ti * (ti + 1) / 2;
+                const int ki = 16 * tj * DKP + rown, qi = 16 * ti * DKP + rown;
+#pragma unroll
+                for (int f = 0; f < DF; ++f) {
+                    kf[x % AHEAD][f] = op_rows<P>(M.k + (ki ^ 32 * f), KPL);
+                    qf[x % AHEAD][f] = op_rows<P>(M.q + (qi ^ 32 * f), KPL);
+                }
+            };
+            operands(0);                                // (C is 64: each wave has two tiles or three; 32: three waves have one)
 #pragma unroll
             for (int x = 0; x < NSC; ++x) {
                 const int tile = w + NW * x, ti = tile_row(tile), tj = tile - ti * (ti + 1) / 2;
                 if (tile >= TILES) break;
-                const uint16_t *pa = BACK ? M.q + (16 * ti + c) * SK : M.k + (16 * tj + c) * SK;
-                const uint16_t *pb = BACK ? M.k + (16 * tj + c) * SK : M.q + (16 * ti + c) * SK;
-                f32x4 s = zero4();
+                float decay[4];
+                decays(decay, M.gh, M.gl, 16 * (BACK ? tj : ti) + c, 16 * (BACK ? ti : tj) + 4 * g, BACK);
+                const f32x4 beta = *reinterpret_cast<const f32x4*>(M.beta + 16 * tj + 4 * g);
+                if (AHEAD > 1 && x + 1 < NSC && tile + NW < TILES) operands(x + 1);
+                __builtin_amdgcn_sched_barrier(0);
+                f32x4 s = zero4(), s2 = zero4();        // (two sums: half as many products wait for the last)
 #pragma unroll
-                for (int f = 0; f < DF; ++f) {
-                    const Op<P> a = op_rows<P>(pa + 32 * f + 8 * g, KPL), bb = op_rows<P>(pb + 32 * f + 8 * g, KPL);
+                for (int f = 0; f < DF; f += 2)
 #pragma unroll
-                    for (int i = 0; i < PAIRS<P, P>; ++i) mm<P, P>(i, s, a, bb);
-                }
+                    for (int i = 0; i < PAIRS<P, P>; ++i) {
+                        mm<P, P>(i, s, BACK ? qf[x % AHEAD][f] : kf[x % AHEAD][f], BACK ? kf[x % AHEAD][f] : qf[x % AHEAD][f]);
+                        mm<P, P>(i, s2, BACK ? qf[x % AHEAD][f + 1] : kf[x % AHEAD][f + 1], BACK ? kf[x % AHEAD][f + 1] : qf[x % AHEAD][f + 1]);
+                    }
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const int i = 16 * ti + (BACK ? 4 * g + r : c), j = 16 * tj + (BACK ? c : 4 * g + r);
-                    const float d = expf((M.gh[i] - M.gh[j]) + (M.gl[i] - M.gl[j]));
-                    s[r] = j <= i ? s[r] * (d * (BACK ? L.scale : L.scale * M.beta[j])) : 0.f;
+                    s[r] = masked(j <= i, (s[r] + s2[r]) * (decay[r] * (BACK ? L.scale : L.scale * beta[r])));
                 }
                 ps[x] = s;
                 if constexpr (BACK) put_parts<3>(M.p + Tr::row(16 * tj + c) + 16 * ti + 4 * g, TPL, s);
+                if (AHEAD == 1 && x + 1 < NSC && tile + NW < TILES) operands(x + 1);
             }
         };
-        // K S, tokens x columns
-        f32x4 z[CT];
-        auto held = [&] {
+        // The chain's products, each one's operands on their way from LDS before the product before it: the compiler leaves them where
+        // they are used, and a wave waits 130 cycles and more for each.  Barriers for the scheduler alone keep them apart; between two, vector
+        // instructions fill the matrix instructions' time.
+        typedef Op<P> KeyOp[4];
+        typedef Op<3> InvOp[2];
+        f32x4 z[CT], R[CT];
+        auto key_rows = [&](KeyOp& k, int f) {
 #pragma unroll
-            for (int t = 0; t < CT; ++t) z[t] = zero4();
+            for (int t = 0; t < CT; ++t) k[t] = op_rows<P>(M.k + (t / 2) * 32 * DKP + ((t & 1 ? row1 : row0) ^ 32 * f), KPL);
+        };
+        auto key_cols = [&](const uint16_t* from, KeyOp& k, int f, int d2) {
 #pragma unroll
-            for (int f = 0; f < DF; ++f) {
-                Op<P> kr[CT];
-#pragma unroll
-                for (int t = 0; t < CT; ++t) kr[t] = op_rows<P>(M.k + row_of(t / 2, t & 1, c) * SK + 32 * f + 8 * g, KPL);
-#pragma unroll
-                for (int i = 0; i < PAIRS<P, 3>; ++i)
-#pragma unroll
-                    for (int t = 0; t < CT; ++t) mm<P, 3>(i, z[t], kr[t], s3[f]);
+            for (int d = 0; d < 4; ++d) {
+                const int x = 32 * ((d2 + d) / 2);
+                k[d] = op_cols2<P>(from + 32 * f * DKP + (at0 ^ x) + 4 * (d & 1), from + 32 * f * DKP + (at1 ^ x) + 4 * (d & 1), KPL);
             }
+        };
+        auto inverse = [&](InvOp& a, int t2, int f) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t) a[t] = op_rows<3>(M.t + Tr::at(t2 / 2, row_of(0, t, c)) + 32 * f + 8 * g, TPL);
+        };
+        auto solve = [&](const InvOp& a, int t2, const Op<3>& y) {
+#pragma unroll
+            for (int i = 0; i < 6; ++i)
+#pragma unroll
+                for (int t = 0; t < 2; ++t) mm<3, 3>(i, R[t2 + t], a[t], y);
         };
         // what the lane's tokens have in `from`
         auto factors = [&](const float* from, int t) { return *reinterpret_cast<const f32x4*>(from + 32 * (t / 2) + 8 * g + 4 * (t & 1)); };
-        // the inverse (or its transpose) times Z
-        auto solve = [&](f32x4 (&R)[CT]) {
-            Op<3> zo[CF];
+        // K S, tokens x columns; the state decays meanwhile
+        auto held = [&] {
+            KeyOp k[2];
+            key_rows(k[0], 0);
 #pragma unroll
-            for (int f = 0; f < CF; ++f) zo[f] = op_of<3>(z[2 * f], z[2 * f + 1]);
-#pragma unroll
-            for (int t = 0; t < CT; ++t) R[t] = zero4();
-#pragma unroll
-            for (int t2 = 0; t2 < CT; t2 += 2)
-#pragma unroll
-                for (int f = BACK ? t2 / 2 : 0; f <= (BACK ? CF - 1 : t2 / 2); ++f) {
-                    Op<3> a[2];
-#pragma unroll
-                    for (int t = 0; t < 2; ++t) a[t] = op_rows<3>(M.t + Tr::at(t2 / 2, row_of(0, t, c)) + 32 * f + 8 * g, TPL);
-#pragma unroll
-                    for (int i = 0; i < 6; ++i)
-#pragma unroll
-                        for (int t = 0; t < 2; ++t) mm<3, 3>(i, R[t2 + t], a[t], zo[f]);
-                }
-        };
-        // S <- e_C S + K^T y
-        auto update = [&](const f32x4 (&y)[CT]) {
+            for (int t = 0; t < CT; ++t) z[t] = R[t] = zero4();
             const float ghi = M.end[0], glo = M.end[1];
 #pragma unroll
-            for (int d = 0; d < DT; ++d)
+            for (int f = 0; f < DF; ++f) {
+                if (f + 1 < DF) key_rows(k[(f + 1) & 1], f + 1);
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int r = 0; r < 4; ++r) S[d][r] = __builtin_fmaf(S[d][r], ghi, S[d][r] * glo);
+                for (int i = 0; i < PAIRS<P, 3>; ++i)
 #pragma unroll
-            for (int f = 0; f < CF; ++f) {
-                const Op<3> u = op_of<3>(y[2 * f], y[2 * f + 1]);
-                const uint16_t* at = M.k + (32 * f + 8 * g + (c >> 2)) * SK + 8 * (c & 3);
+                    for (int t = 0; t < CT; ++t) mm<P, 3>(i, z[t], k[f & 1][t], s3[f]);
 #pragma unroll
-                for (int d2 = 0; d2 < DT; d2 += 4) {
-                    Op<P> kc[4];
+                for (int d = 2 * f; d < 2 * f + 2; ++d)
 #pragma unroll
-                    for (int d = 0; d < 4; ++d) kc[d] = op_cols<P>(at + 32 * ((d2 + d) / 2) + 4 * (d & 1), SK, KPL);
+                    for (int r = 0; r < 4; ++r) S[d][r] = __builtin_fmaf(S[d][r], ghi, S[d][r] * glo);
+            }
+        };
+        // S += K^T y, y the operands of the tokens' blocks of 32 in the order that they come in; the state's next operand on the way
+        auto update = [&](KeyOp (&k)[2], int first, const Op<3>& y, bool last, int f) {
 #pragma unroll
-                    for (int i = 0; i < PAIRS<P, 3>; ++i)
+            for (int d2 = 0; d2 < DT; d2 += 4) {
+                const int x = first + d2 / 4;
+                if (d2 + 4 < DT) key_cols(M.k, k[(x + 1) & 1], f, d2 + 4);
+                else if (!last) key_cols(M.k, k[(x + 1) & 1], BACK ? f - 1 : f + 1, 0);
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                        for (int d = 0; d < 4; ++d) mm<P, 3>(i, S[d2 + d], kc[d], u);
+                for (int i = 0; i < PAIRS<P, 3>; ++i)
+#pragma unroll
+                    for (int d = 0; d < 4; ++d) mm<P, 3>(i, S[d2 + d], k[x & 1][d], y);
+                if (last && d2 > 0) {
+                    split(d2 / 2 - 2);
+                    split(d2 / 2 - 1);
                 }
+            }
+            if (last) {
+                split(DF - 2);
+                split(DF - 1);
             }
         };
 
         if constexpr (!BACK) {
-            if (chain && work && on) {
+            if constexpr (chain) {
+                if (!work || !on) continue;
                 held();
+                InvOp a[2];
+                inverse(a[0], 0, 0);
+                f32x4 fe[CT], fw[CT];
 #pragma unroll
                 for (int t = 0; t < CT; ++t) {
-                    const f32x4 te = factors(M.e, t);
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) z[t][r] = float_of<E>(vv[4 * t + r]) - te[r] * z[t][r];
+                    fe[t] = factors(M.e, t);
+                    fw[t] = factors(M.w, t);
                 }
-                f32x4 R[CT];
-                solve(R);
+                auto lack = [&](int f) {
 #pragma unroll
-                for (int f = 0; f < CF; ++f) ro[f] = op_of<OP>(R[2 * f], R[2 * f + 1]);
-                if constexpr (MODE == RECORD) {
+                    for (int t = 2 * f; t < 2 * f + 2; ++t)
 #pragma unroll
-                    for (int t = 0; t < CT; ++t)
+                        for (int r = 0; r < 4; ++r) z[t][r] = float_of<E>(vv[4 * t + r]) - fe[t][r] * z[t][r];
+                    return op_of<3>(z[2 * f], z[2 * f + 1]);
+                };
+                // R's tokens of a block of 32: the outputs' operand and the state's
+                auto written = [&](int f) {
+                    ro[f] = op_of<OP>(R[2 * f], R[2 * f + 1]);
+                    int at = 8 * g * dv + n;
+                    const int most = in ? cnt - 8 * g : 0;
+                    asm volatile("" : "+v"(at));
+                    float y[8];
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) {
-                            const int tok = 32 * (t / 2) + 8 * g + 4 * (t & 1) + r;
-                            if (in && tok < cnt) L.rec_R[(head * (static_cast<long long>(L.blocks) * C) + t0 + tok) * dv + n] = R[t][r];
+                    for (int i = 0; i < 8; ++i) {
+                        const int t = 2 * f + i / 4, r = i % 4;
+                        if constexpr (MODE == RECORD) {
+                            if (32 * f + i < most) put(rows_of(L.rec_R, t0) + (32 * f + i) * dv, at, R[t][r]);
                         }
+                        y[i] = R[t][r] * fw[t][r];
+                    }
+                    return op_of<3>(y);
+                };
+                KeyOp k[2];
+                if constexpr (CF == 2) {
+                    inverse(a[1], 2, 0);
+                    const Op<3> z0 = lack(0);
+                    __builtin_amdgcn_sched_barrier(0);
+                    solve(a[0], 0, z0);
+                    const Op<3> z1 = lack(1);
+                    inverse(a[0], 2, 1);
+                    __builtin_amdgcn_sched_barrier(0);
+                    solve(a[1], 2, z0);
+                    const Op<3> u0 = written(0);
+                    key_cols(M.k, k[0], 0, 0);
+                    __builtin_amdgcn_sched_barrier(0);
+                    solve(a[0], 2, z1);
+                    update(k, 0, u0, false, 0);
+                    const Op<3> u1 = written(1);
+                    __builtin_amdgcn_sched_barrier(0);
+                    update(k, DT / 4, u1, true, 1);
+                } else {
+                    const Op<3> z0 = lack(0);
+                    key_cols(M.k, k[0], 0, 0);
+                    __builtin_amdgcn_sched_barrier(0);
+                    solve(a[0], 0, z0);
+                    const Op<3> u0 = written(0);
+                    __builtin_amdgcn_sched_barrier(0);
+                    update(k, 0, u0, true, 0);
                 }
-#pragma unroll
-                for (int t = 0; t < CT; ++t) {
-                    const f32x4 tw = factors(M.w, t), tb = factors(M.beta, t);
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) R[t][r] *= tw[r] * tb[r];
-                }
-                update(R);
-            } else if (!chain) {
+            } else {
                 if (it > 0 && on) {         // the block before: x += P R
                     const int tb = t0 - C, left = dv - n0 - 4 * g, last = len - tb < C ? len - tb : C;
                     Op<OP> rr[CF];
@@ -990,7 +1087,7 @@ template <typename E, int DKP, int MODE, bool chain> __device__ __forceinline__ 
 #pragma unroll
                             for (int s = 0; s < OP; ++s) so.p[s] = __builtin_bit_cast(bf16x8, M.fwd.s[w][f * OP + s][lane]);
 #pragma unroll
-                            for (int t = 0; t < CT; ++t) qr[t] = op_rows<P>(M.q + (16 * t + c) * SK + 32 * f + 8 * g, KPL);
+                            for (int t = 0; t < CT; ++t) qr[t] = op_rows<P>(M.q + 16 * t * DKP + (rown ^ 32 * f), KPL);
 #pragma unroll
                             for (int i = 0; i < PAIRS<OP, P>; ++i)
 #pragma unroll
@@ -1000,68 +1097,127 @@ template <typename E, int DKP, int MODE, bool chain> __device__ __forceinline__ 
                 }
             }
         } else {
-            if (chain && on) held();
-            if (!chain) scores();
-            __syncthreads();                // (P^T is written)
-            if (!on) continue;
-            if (chain) {
+            if constexpr (!chain) {
+                scores();
+                if (on) {                   // Q^T (c e dO)
+                    f32x4 add[DT];
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) add[d] = zero4();
+                    KeyOp k[2];
+                    key_cols(M.q, k[0], 0, 0);
+#pragma unroll
+                    for (int f = 0; f < CF; ++f) {
+                        float y[8];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) y[i] = float_of<E>(vv[8 * f + i]) * (L.scale * M.e[32 * f + 8 * g + i]);
+                        const Op<3> o3 = op_of<3>(y);
+#pragma unroll
+                        for (int d2 = 0; d2 < DT; d2 += 4) {
+                            const int x = f * (DT / 4) + d2 / 4;
+                            if (d2 + 4 < DT) key_cols(M.q, k[(x + 1) & 1], f, d2 + 4);
+                            else if (f + 1 < CF) key_cols(M.q, k[(x + 1) & 1], f + 1, 0);
+                            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                            for (int i = 0; i < PAIRS<P, 3>; ++i)
+#pragma unroll
+                                for (int d = 0; d < 4; ++d) mm<P, 3>(i, add[d2 + d], k[x & 1][d], o3);
+                        }
+                    }
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) M.add[w][d][lane] = add[d];
+                }
+            } else if (on) {
+                held();
+            }
+            __syncthreads();                // (P^T and Q^T (c e dO) are written)
+            if constexpr (chain) {
+                if (!on) continue;
+                InvOp a[2];
+                Op<3> pa[CT];
+                Op<P> go[CF];
+                f32x4 fe[CT], fb[CT], fw[CT];
 #pragma unroll
                 for (int t = 0; t < CT; ++t) {
-                    const f32x4 tw = factors(M.w, t);
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) z[t][r] *= tw[r];
+                    pa[t] = op_rows<3>(M.p + Tr::at(t / 2, row_of(0, t & 1, c)) + 32 * (CF - 1) + 8 * g, TPL);
+                    fe[t] = factors(M.e, t);
+                    fb[t] = factors(M.beta, t);
+                    fw[t] = factors(M.w, t);
                 }
+                inverse(a[0], CT - 2, CF - 1);
+#pragma unroll
+                for (int t = 0; t < CT; ++t)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) z[t][r] *= fw[t][r];
 #pragma unroll
                 for (int f = 0; f < CF; ++f) {
                     float y[8];
 #pragma unroll
                     for (int i = 0; i < 8; ++i) y[i] = float_of<E>(vv[8 * f + i]);
-                    const Op<P> go = op_of<P>(y);
-                    Op<3> a[CT];
+                    go[f] = op_of<P>(y);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+                // c P^T dO: the last 32 tokens reach all rows, the first 32 their own
 #pragma unroll
-                    for (int t = 0; t < 2 * f + 2; ++t) a[t] = op_rows<3>(M.p + Tr::at(t / 2, row_of(0, t & 1, c)) + 32 * f + 8 * g, TPL);
+                for (int i = 0; i < PAIRS<3, P>; ++i)
+#pragma unroll
+                    for (int t = 0; t < CT; ++t) mm<3, P>(i, z[t], pa[t], go[CF - 1]);
+                auto written = [&](int f) {
+                    int at = 8 * g * dv + n;
+                    const int most = in ? cnt - 8 * g : 0;
+                    asm volatile("" : "+v"(at));
+                    float y[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const int t = 2 * f + i / 4, r = i % 4;
+                        if (32 * f + i < most) put(rows_of(L.rec_du, t0) + (32 * f + i) * dv, at, R[t][r]);
+                        y[i] = R[t][r] * (-fe[t][r] * fb[t][r]);
+                    }
+                    return op_of<3>(y);
+                };
+                auto plus = [&] {           // Q^T (c e dO)
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) {
+                        const f32x4 y = M.add[w][d][lane];
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) S[d][r] += y[r];
+                    }
+                };
+                KeyOp k[2];
+                if constexpr (CF == 2) {
+                    Op<3> pb[2];
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) pb[t] = op_rows<3>(M.p + Tr::at(0, row_of(0, t, c)) + 8 * g, TPL);
+                    const Op<3> z1 = op_of<3>(z[2], z[3]);
+                    inverse(a[1], 0, 1);
+                    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                     for (int i = 0; i < PAIRS<3, P>; ++i)
 #pragma unroll
-                        for (int t = 0; t < 2 * f + 2; ++t) mm<3, P>(i, z[t], a[t], go);
+                        for (int t = 0; t < 2; ++t) mm<3, P>(i, z[t], pb[t], go[0]);
+                    solve(a[0], 2, z1);
+                    const Op<3> z0 = op_of<3>(z[0], z[1]);
+                    inverse(a[0], 0, 0);
+                    __builtin_amdgcn_sched_barrier(0);
+                    solve(a[1], 0, z1);
+                    const Op<3> u1 = written(1);
+                    plus();
+                    key_cols(M.k, k[0], 1, 0);
+                    __builtin_amdgcn_sched_barrier(0);
+                    solve(a[0], 0, z0);
+                    update(k, 0, u1, false, 1);
+                    const Op<3> u0 = written(0);
+                    __builtin_amdgcn_sched_barrier(0);
+                    update(k, DT / 4, u0, true, 0);
+                } else {
+                    const Op<3> z0 = op_of<3>(z[0], z[1]);
+                    plus();
+                    key_cols(M.k, k[0], 0, 0);
+                    __builtin_amdgcn_sched_barrier(0);
+                    solve(a[0], 0, z0);
+                    const Op<3> u0 = written(0);
+                    __builtin_amdgcn_sched_barrier(0);
+                    update(k, 0, u0, true, 0);
                 }
-                f32x4 du[CT];
-                solve(du);
-#pragma unroll
-                for (int t = 0; t < CT; ++t) {
-                    const f32x4 te = factors(M.e, t), tb = factors(M.beta, t);
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const int tok = 32 * (t / 2) + 8 * g + 4 * (t & 1) + r;
-                        if (in && tok < cnt) L.rec_du[(head * (static_cast<long long>(L.blocks) * C) + t0 + tok) * dv + n] = du[t][r];
-                        du[t][r] *= -te[r] * tb[r];
-                    }
-                }
-                update(du);
-            } else {
-                f32x4 add[DT];
-#pragma unroll
-                for (int d = 0; d < DT; ++d) add[d] = zero4();
-#pragma unroll
-                for (int f = 0; f < CF; ++f) {
-                    float y[8];
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) y[i] = float_of<E>(vv[8 * f + i]) * (L.scale * M.e[32 * f + 8 * g + i]);
-                    const Op<3> o3 = op_of<3>(y);
-                    const uint16_t* at = M.q + (32 * f + 8 * g + (c >> 2)) * SK + 8 * (c & 3);
-#pragma unroll
-                    for (int d2 = 0; d2 < DT; d2 += 4) {
-                        Op<P> qc[4];
-#pragma unroll
-                        for (int d = 0; d < 4; ++d) qc[d] = op_cols<P>(at + 32 * ((d2 + d) / 2) + 4 * (d & 1), SK, KPL);
-#pragma unroll
-                        for (int i = 0; i < PAIRS<P, 3>; ++i)
-#pragma unroll
-                            for (int d = 0; d < 4; ++d) mm<P, 3>(i, add[d2 + d], qc[d], o3);
-                    }
-                }
-#pragma unroll
-                for (int d = 0; d < DT; ++d) M.add[w][d][lane] = add[d];
             }
         }
     }

@@ -95,11 +95,20 @@ template <typename E> __global__ __launch_bounds__(NT) void sfda_delta_prep(Delt
             if (lane >= d) s += o;
         }
         const float hi = static_cast<float>(s), lo = static_cast<float>(s - hi);
+        const float eh = __shfl(hi, C - 1), el = __shfl(lo, C - 1), bt = there ? be : 0.f;
         if (lane < C) {
             tok[w][0][lane] = hi;
             tok[w][1][lane] = lo;
-            tok[w][2][lane] = there ? be : 0.f;
-            if (live && !by_row) L.scalars[(head * static_cast<long long>(L.blocks) + blk) * C + lane] = float4{hi, lo, there ? be : 0.f, 0.f};
+            tok[w][2][lane] = bt;
+            if (live && !by_row) {
+                // the block's decay as hi + lo: a state that lives for thousands of blocks keeps its 24 bits
+                const float x = eh + el, wt = expf((eh - hi) + (el - lo));
+                const bool near = x > -0.5f && x < 0.5f;
+                const float m = near ? expm1f(x) : 0.f, end = near ? 1.f + m : expf(x);
+                float4* to = L.scalars + 2 * ((head * static_cast<long long>(L.blocks) + blk) * C + lane);
+                to[0] = float4{hi, lo, bt, expf(hi + lo)};
+                to[1] = float4{wt, wt * bt, end, near ? m - (end - 1.f) : 0.f};
+            }
         }
     }
 
@@ -127,13 +136,14 @@ template <typename E> __global__ __launch_bounds__(NT) void sfda_delta_prep(Delt
 #pragma unroll
     for (int ti = 0; ti < CT; ++ti)
 #pragma unroll
-        for (int tj = 0; tj <= ti; ++tj)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int i = 16 * ti + c, j = 16 * tj + 4 * g + r;
-                const float d = expf((tok[w][0][i] - tok[w][0][j]) + (tok[w][1][i] - tok[w][1][j]));
+        for (int tj = 0; tj <= ti; ++tj) {
+                float d[4];
+                decays(d, tok[w][0], tok[w][1], 16 * ti + c, 16 * tj + 4 * g, false);
+                const f32x4 bj = *reinterpret_cast<const f32x4*>(&tok[w][2][16 * tj + 4 * g]);
+                const float bi = tok[w][2][16 * ti + c];
                 f32x4& x = X[tile_at(ti, tj)];
-                x[r] = j < i ? -x[r] * (d * tok[w][2][by_row ? i : j]) : 0.f;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) x[r] = masked(16 * tj + 4 * g + r < 16 * ti + c, -x[r] * (d[r] * (by_row ? bi : bj[r])));
             }
 
     // row c at 4 g .. to column c at 4 g .., and back

@@ -44,7 +44,7 @@ constexpr int SLAB = 64;        // value columns at a time
 template <typename E, int DKP> struct GradMem {
     typedef Block<E> B;
     static constexpr int NW = DKP == 64 ? 4 : 8, NT = 64 * NW;
-    static constexpr int C = B::C, P = B::P, SK = DKP + 8, SV = SLAB + 8, ST = C + 8;
+    static constexpr int C = B::C, P = B::P, SK = DKP + 16, SV = SLAB + 8, ST = C + 8;
     static constexpr int KPL = C * SK, VPL = C * SV, TPL = C * ST;
     union {
         // dO, dv, u, and times c e, -e, w: [token][value column]
@@ -98,14 +98,8 @@ template <typename E> __device__ __forceinline__ void put_four(E* row, int col, 
     }
 }
 
-// The thread's number, as a value of its own at each call: what is computed from it is not kept over the loops (spilled, it took
-// 1.9 of the 2.3 GB that the kernel wrote).
-__device__ __forceinline__ int thread()
-{
-    int x = threadIdx.x;
-    asm volatile("" : "+v"(x));
-    return x;
-}
+// (what is computed from it is not kept over the loops: spilled, it took 1.9 of the 2.3 GB that the kernel wrote)
+__device__ __forceinline__ int thread() { return anew(threadIdx.x); }
 
 // One workgroup for a block of a key head, its value heads one after the other.  A wave owns one or two tiles of 16 channels of dq and dk
 // (rows; tokens are the columns), whose rows of the states it alone reads.
@@ -175,10 +169,11 @@ template <typename E, int DKP> __global__ __launch_bounds__((GradMem<E, DKP>::NT
         };
         if (DW == 1) keys();            // (ahead where there are the registers, here and below)
 
-        float4 sc = {0.f, 0.f, 0.f, 0.f};
+        float4 sc[2];
         float decay = 0.f, od = 0.f;
         if (tid < C) {
-            sc = L.scalars[row0 + tid];
+            sc[0] = L.scalars[2 * (row0 + tid)];
+            sc[1] = L.scalars[2 * (row0 + tid) + 1];
             decay = L.log_decay[b * L.l_s[0] + h * L.l_s[1] + (t0 + (tid < cnt ? tid : 0)) * L.l_s[2]];
         }
         for (int p = tid / C; p < L.parts; p += NT / C)         // (a part of 16 columns for a thread, or two)
@@ -186,12 +181,11 @@ template <typename E, int DKP> __global__ __launch_bounds__((GradMem<E, DKP>::NT
         __syncthreads();                // (the last head's tokens and keys are read)
         M.od[tid] = od;
         if (tid < C) {
-            const float eh = __shfl(sc.x, C - 1), el = __shfl(sc.y, C - 1);
-            M.gh[tid] = sc.x;
-            M.gl[tid] = sc.y;
-            M.beta[tid] = sc.z;
-            M.e[tid] = expf(sc.x + sc.y);
-            M.wt[tid] = expf((eh - sc.x) + (el - sc.y));
+            M.gh[tid] = sc[0].x;
+            M.gl[tid] = sc[0].y;
+            M.beta[tid] = sc[0].z;
+            M.e[tid] = sc[0].w;
+            M.wt[tid] = sc[1].x;
         }
         float dot = 0.f;
         f32x4 ws[TW], ms[TW], md[TW];
@@ -333,12 +327,14 @@ template <typename E, int DKP> __global__ __launch_bounds__((GradMem<E, DKP>::NT
             const int ti = (w + NW * x) / CT, tj = (w + NW * x) % CT, i = 16 * ti + c;
             if (ti >= CT) break;
             f32x4 a, m;
+            float down[4], up[4];
+            decays(down, M.gh, M.gl, i, 16 * tj + 4 * g, false);
+            decays(up, M.gh, M.gl, i, 16 * tj + 4 * g, true);
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const int jj = 16 * tj + 4 * g + r, hi = i > jj ? i : jj, lo = i > jj ? jj : i;
-                const float d = expf((M.gh[hi] - M.gh[lo]) + (M.gl[hi] - M.gl[lo]));
-                a[r] = jj <= i ? ws[x][r] * (L.scale * d) : 0.f;
-                m[r] = jj == i ? 0.f : -d * (jj < i ? ms[x][r] : md[x][r]);
+                const int jj = 16 * tj + 4 * g + r;
+                a[r] = masked(jj <= i, ws[x][r] * (L.scale * down[r]));
+                m[r] = masked(jj != i, -(jj < i ? ms[x][r] * down[r] : md[x][r] * up[r]));
             }
             if (ti >= tj) Ops<E>::put4(M.w + i * ST + 16 * tj + 4 * g, TPL, a);
             Ops<E>::put4(M.m + i * ST + 16 * tj + 4 * g, TPL, m);

@@ -672,7 +672,7 @@ static bool delta_launches(ll heads, ll blocks, int dv) { return heads * std::ma
 // the forward's part of a workspace for `heads` value heads: inverses and scalars
 static ll delta_prep_bytes(ll heads, ll blocks, bool bf16, int inverses)
 {
-    return heads * blocks * (inverses * sfda::delta_tiles(bf16) * 1024LL + sfda::delta_block(bf16) * 16LL);
+    return heads * blocks * (inverses * sfda::delta_tiles(bf16) * 1024LL + sfda::delta_block(bf16) * 32LL);
 }
 
 size_t sfda_delta_attn_fwd_workspace_bytes(int B, int H, int T, int dk, int dv, sfda_dtype_t dtype)
@@ -802,7 +802,7 @@ sfda_status_t sfda_delta_attn_bwd(const void* q, const void* k, const void* v, c
         float* p = static_cast<float*>(workspace);
         L.inv = p; p += inv;
         L.inv_back = p; p += inv;
-        L.scalars = reinterpret_cast<float4*>(p); p += n * blocks * C * 4;
+        L.scalars = reinterpret_cast<float4*>(p); p += n * blocks * C * 8;
         L.rec_S = p; p += up(n * (blocks + 1) * dk * dv);
         L.rec_U = p; p += up(n * blocks * dk * dv);
         L.rec_R = p; p += up(n * blocks * C * dv);
