@@ -22,6 +22,8 @@
 
 #include <stddef.h>
 
+#include <type_traits>
+
 namespace sfda {
 namespace delta {
 
@@ -143,6 +145,24 @@ __device__ __forceinline__ void decays(float (&d)[4], const float* hi, const flo
 #pragma unroll
     for (int r = 0; r < 4; ++r) d[r] = pin(exp_of(back ? (h4[r] - h1) + (l4[r] - l1) : (h1 - h4[r]) + (l1 - l4[r])));
 }
+// Lanes (c, g) hold rows 4 g + r of column c; then they hold columns 4 (c / 4) + r of row 4 g + c % 4: 4 x 4 in each four lanes.
+__device__ __forceinline__ void turn4(f32x4& a, int c)
+{
+    auto from = [](float x, auto ctrl) { return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), decltype(ctrl)::value, 0xF, 0xF, false)); };
+    const bool odd = c & 1, two = c & 2;
+#pragma unroll
+    for (int x = 0; x < 4; x += 2) {
+        const float got = from(odd ? a[x] : a[x + 1], std::integral_constant<int, 0xB1>());        // quad [1, 0, 3, 2]
+        a[x] = odd ? got : a[x];
+        a[x + 1] = odd ? a[x + 1] : got;
+    }
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+        const float got = from(two ? a[x] : a[x + 2], std::integral_constant<int, 0x4E>());        // quad [2, 3, 0, 1]
+        a[x] = two ? got : a[x];
+        a[x + 2] = two ? a[x + 2] : got;
+    }
+}
 __device__ __forceinline__ int row_of(int f, int h, int c) { return 32 * f + 8 * (c >> 2) + 4 * h + (c & 3); }     // of a tile's row c
 
 // Rows of keys and queries in LDS, DKP channels each: the 16-byte units of row i change places by x(i) = 4 (i % 4) + i / 4 % 4, so that what
@@ -181,6 +201,18 @@ template <typename E, int COLS, int C, int STRIDE, int THREADS = NT, bool SWAPPE
             const uint32_t off = (r < n ? r : n - 1) * st + at;
             if (cols >= VE) x[u] = load16(base + off);
             else x[u] = col == 0 ? short_row<E>(base + off, cols) : u32x4{0, 0, 0, 0};
+        }
+    }
+    // as they lie in memory, rows STRIDE elements apart, zeros past the columns too
+    __device__ __forceinline__ void store_raw(E* lds, int n, int cols, int tid) const
+    {
+        const int col = (tid % VPR) * VE, past = cols < VE ? 0 : col + VE - cols;
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
+            const int r = tid / VPR + u * RPP;
+            u32x4 w = r < n && col < cols ? x[u] : u32x4{0, 0, 0, 0};
+            if (cols % VE != 0 && past > 0 && past < VE) w = move_down<E>(w, past);
+            *reinterpret_cast<u32x4*>(lds + r * STRIDE + col) = w;
         }
     }
     __device__ __forceinline__ void store(uint16_t* lds, int n, int cols, int tid) const
@@ -271,10 +303,11 @@ template <typename E, int DKP, int MODE> __device__ __forceinline__ void scan(co
     const uint32_t gst = MODE == FWD ? 0 : static_cast<uint32_t>(L.g_s[2] * ES);
     const uint32_t col = (in ? n : dv - 1) * ES;
     const float* const tmat = (BACK ? L.inv_back : L.inv) + head * L.blocks * static_cast<long long>(TILES * 256);
+    const float* const pmat = (BACK ? L.scores_back : L.scores) + head * L.blocks * static_cast<long long>(TILES * 256);
     const float4* const scal = L.scalars + 2 * (head * L.blocks * static_cast<long long>(C));
 
     RowTile<E, DKP, C, SK> tk, tq;
-    f32x4 tt[(TILES * 64 + NT - 1) / NT];
+    f32x4 tt[(TILES * 64 + NT - 1) / NT], pp[(TILES * 64 + NT - 1) / NT];
     float4 sc[2];
     uint32_t vr[CT * 4];                    // V, or dO
     auto fetch = [&](int blk) {
@@ -285,6 +318,7 @@ template <typename E, int DKP, int MODE> __device__ __forceinline__ void scan(co
         for (int u = 0; u < (TILES * 64 + NT - 1) / NT; ++u) {
             const int at = tid + u * NT < TILES * 64 ? tid + u * NT : 0;
             tt[u] = *reinterpret_cast<const f32x4*>(tmat + static_cast<long long>(blk) * TILES * 256 + 4 * at);
+            pp[u] = *reinterpret_cast<const f32x4*>(pmat + static_cast<long long>(blk) * TILES * 256 + 4 * at);
         }
         const int tok = tid < C ? tid : 0;
         sc[0] = scal[2 * (static_cast<long long>(blk) * C + tok)];
@@ -340,7 +374,11 @@ template <typename E, int DKP, int MODE> __device__ __forceinline__ void scan(co
         for (int u = 0; u < (TILES * 64 + NT - 1) / NT; ++u) {
             const int at = tid + u * NT, tile = at >> 6, row = (at & 63) >> 2, c4 = 4 * (at & 3);
             const int ti = tile < 1 ? 0 : tile < 3 ? 1 : tile < 6 ? 2 : 3, tj = tile - ti * (ti + 1) / 2;
-            if (tile < TILES) Ops<float>::put4(M.t + (16 * (BACK ? tj : ti) + row) * ST + 16 * (BACK ? ti : tj) + c4, TPL, tt[u]);
+            const int to = (16 * (BACK ? tj : ti) + row) * ST + 16 * (BACK ? ti : tj) + c4;
+            if (tile < TILES) {
+                put_parts<3>(M.t + to, TPL, tt[u]);
+                put_parts<PP>(M.p + to, TPL, pp[u]);
+            }
         }
         if (tid < C) {
             M.gh[tid] = sc[0].x;
@@ -358,30 +396,6 @@ template <typename E, int DKP, int MODE> __device__ __forceinline__ void scan(co
 #pragma unroll
         for (int i = 0; i < CT * 4; ++i) vv[i] = on ? float_of<E>(vr[i]) : 0.f;
         if (it + 1 < blocks) fetch(BACK ? blk - 1 : blk + 1);
-
-        // P [i][j] (forward: times c beta_j), or its transpose: a tile of 16 x 16 for a wave at a time
-        for (int tile = w; tile < TILES; tile += NW) {
-            const int ti = tile < 1 ? 0 : tile < 3 ? 1 : tile < 6 ? 2 : 3, tj = tile - ti * (ti + 1) / 2;
-            const uint16_t *pa = BACK ? M.q + (16 * ti + c) * SK : M.k + (16 * tj + c) * SK;
-            const uint16_t *pb = BACK ? M.k + (16 * tj + c) * SK : M.q + (16 * ti + c) * SK;
-            f32x4 s = zero4();
-#pragma unroll
-            for (int f = 0; f < DF; ++f) {
-                const Op<P> a = op_rows<P>(pa + 32 * f + 8 * g, KPL), bb = op_rows<P>(pb + 32 * f + 8 * g, KPL);
-#pragma unroll
-                for (int i = 0; i < PAIRS<P, P>; ++i) mm<P, P>(i, s, a, bb);
-            }
-            float decay[4];
-            decays(decay, M.gh, M.gl, 16 * (BACK ? tj : ti) + c, 16 * (BACK ? ti : tj) + 4 * g, BACK);
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int i = 16 * ti + (BACK ? 4 * g + r : c), j = 16 * tj + (BACK ? c : 4 * g + r);
-                s[r] = masked(j <= i, s[r] * (decay[r] * (BACK ? L.scale : L.scale * M.beta[j])));
-            }
-            uint16_t* to = BACK ? M.p + (16 * tj + c) * ST + 16 * ti + 4 * g : M.p + (16 * ti + c) * ST + 16 * tj + 4 * g;
-            if constexpr (PP == 1) Ops<uint16_t>::put4(to, 0, s);
-            else Ops<float>::put4(to, TPL, s);
-        }
 
         f32x4 z[CT], x[BACK ? 1 : CT];
         if (on) {
@@ -417,7 +431,6 @@ template <typename E, int DKP, int MODE> __device__ __forceinline__ void scan(co
                 }
             }
         }
-        __syncthreads();                    // (P is written)
         if (!on) continue;
 
         // e, w, beta of the lane's tokens
@@ -612,9 +625,9 @@ template <typename E, int DKP, int MODE> __device__ __forceinline__ void scan(co
 }
 
 // ------------------------------------------------------------------ the scan by two kinds of waves
-// The same scan with eight waves: four hold the state and run the chain alone, four help.  Forward, the helpers form P and the
+// The same scan with eight waves: four hold the state and run the chain alone, four help.  Forward, the helpers form the
 // outputs, a block behind the chain, from the state and R as operands that the chain's waves leave in LDS fragment by fragment (as
-// the lane has them: 16 bytes a lane, no two on one bank).  Backward, they form P^T and Q^T (c e dO), which do not depend on the state.
+// the lane has them: 16 bytes a lane, no two on one bank).  Backward, they form Q^T (c e dO), which does not depend on the state.
 
 // rows of a triangular matrix in LDS: 32 rows of a block row are as long as the block columns that they have
 template <int C, bool UPPER> struct Tri {
@@ -632,7 +645,9 @@ template <typename E, int DKP, int MODE> struct PairMem {
     static constexpr int C = B::C, P = B::P, OP = MODE == FWD ? P : 3, PP = MODE == FWD && P == 1 ? 2 : 3;
     typedef Tri<C, BACK> T;
     static constexpr int KPL = C * DKP, TPL = T::SIZE, DF = DKP / 32, DT = DKP / 16;
+    static constexpr int SV = SLICE + (sizeof(E) == 2 ? 16 : 4);
     uint16_t k[P * KPL], q[P * KPL], t[3 * TPL], p[PP * TPL];
+    E v[C * SV];                // V, or dO, of the slice
     union {
         struct { u32x4 s[NW][DF * OP][64], r[NW][B::CF * OP][64]; } fwd;        // the state and R
         f32x4 add[NW][BACK ? DT : 1][64];                                       // Q^T (c e dO)
@@ -652,7 +667,6 @@ template <typename E, int DKP, int MODE, bool chain> __device__ __forceinline__ 
     typedef KeyRows<DKP> Key;
     constexpr int C = B::C, CT = B::CT, CF = B::CF, P = B::P, PP = M_::PP, OP = M_::OP, TILES = B::TILES, ES = sizeof(E);
     constexpr int DT = DKP / 16, DF = DKP / 32, KPL = M_::KPL, TPL = M_::TPL, NTT = (TILES * 64 + NT - 1) / NT;
-    constexpr int NSC = (TILES + NW - 1) / NW;      // tiles of P of a helper
     constexpr bool BACK = MODE == ADJOINT;
     M_& M = *reinterpret_cast<M_*>(smem);
 
@@ -672,14 +686,17 @@ template <typename E, int DKP, int MODE, bool chain> __device__ __forceinline__ 
     const char* const gp = MODE == FWD ? nullptr : static_cast<const char*>(L.dO) + (b * L.g_s[0] + h * L.g_s[1]) * ES;
     const uint32_t kst = static_cast<uint32_t>(L.k_s[2] * ES), qst = static_cast<uint32_t>(L.q_s[2] * ES), vst = static_cast<uint32_t>(L.v_s[2] * ES);
     const uint32_t gst = MODE == FWD ? 0 : static_cast<uint32_t>(L.g_s[2] * ES);
-    const uint32_t col = (in ? n : dv - 1) * ES;
     const float* const tmat = (BACK ? L.inv_back : L.inv) + head * L.blocks * static_cast<long long>(TILES * 256);
+    const float* const pmat = (BACK ? L.scores_back : L.scores) + head * L.blocks * static_cast<long long>(TILES * 256);
     const float4* const scal = L.scalars + 2 * (head * L.blocks * static_cast<long long>(C));
 
     RowTile<E, DKP, C, DKP, PAIR_NT, true> tk, tq;
-    f32x4 tt[NTT];
+    f32x4 tt[NTT], pp[NTT];
     float4 sc[2];
-    uint32_t vr[CT * 4];                    // V, or dO
+    RowTile<E, SLICE, C, M_::SV, NT> tv;    // V, or dO, by the helpers
+    const int cols = dv - sl * SLICE < SLICE ? dv - sl * SLICE : SLICE;
+    const char* const wp = (BACK ? gp : vp) + sl * SLICE * ES;
+    const uint32_t wst = BACK ? gst : vst;
     auto fetch = [&](int blk) {
         const int t0 = blk * C, cnt = len - t0 < C ? len - t0 : C;
         tk.load(kp + static_cast<long long>(t0) * kst, kst, cnt, dk, tid);
@@ -689,18 +706,13 @@ template <typename E, int DKP, int MODE, bool chain> __device__ __forceinline__ 
             for (int u = 0; u < NTT; ++u) {
                 const int at = tid - NT + u * NT < TILES * 64 ? tid - NT + u * NT : 0;
                 tt[u] = *reinterpret_cast<const f32x4*>(tmat + static_cast<long long>(blk) * TILES * 256 + 4 * at);
+                pp[u] = *reinterpret_cast<const f32x4*>(pmat + static_cast<long long>(blk) * TILES * 256 + 4 * at);
             }
             const int tok = tid - NT < C ? tid - NT : 0;
             sc[0] = scal[2 * (static_cast<long long>(blk) * C + tok)];
             sc[1] = scal[2 * (static_cast<long long>(blk) * C + tok) + 1];
         }
-        if (!on) return;
-        // tile (f, h) row 4 g + r is token 32 f + 8 g + 4 h + r: the 8 neighbours of a lane are i = 4 h + r of both tiles
-        if constexpr (BACK) {
-            column<E>(vr, gp + static_cast<long long>(t0) * gst, col, gst, cnt, C, g, [](int i) { return 32 * (i / 8) + i % 8; });
-        } else if (chain) {
-            column<E>(vr, vp + static_cast<long long>(t0) * vst, col, vst, cnt, C, g, [](int i) { return 32 * (i / 8) + i % 8; });
-        }
+        if constexpr (!chain) tv.load(wp + static_cast<long long>(t0) * wst, wst, cnt, cols, tid - NT);
     };
     if (blocks > 0) fetch(BACK ? blocks - 1 : 0);
 
@@ -727,28 +739,32 @@ template <typename E, int DKP, int MODE, bool chain> __device__ __forceinline__ 
             for (int r = 0; r < 4; ++r)
                 if (in && channel(d, r) < dk) S[d][r] = src[channel(d, r) * dv + n];
     }
-    // (addresses the same for all lanes, and 32-bit offsets)
-    auto put = [](float* to, int at, float x) { *reinterpret_cast<float*>(reinterpret_cast<char*>(to) + static_cast<uint32_t>(4 * at)) = x; };
-    auto record = [&](float* to) {
-        int at = 8 * g * dv + n;
-        const int most = in ? dk - 8 * g : 0;           // (channels of the lane's)
-        asm volatile("" : "+v"(at));
+    // Rows of 4 g + r neighbours to memory, by 16 bytes where the columns are whole (a lane's four rows, each in another line, take four
+    // times as many stores, which bound the scans that record).  Addresses the same for all lanes, and 32-bit offsets.
+    const bool whole = dv % 4 == 0;
+    auto put = [&](float* to, int row, int most, f32x4 x) {     // row: the first of four
+        if (whole) {
+            const int r = row + (c & 3), at = anew(r * dv + n0 + 4 * (c >> 2));
+            turn4(x, c);
+            if (r < most && n0 + 4 * (c >> 2) < dv) store16(reinterpret_cast<char*>(to) + static_cast<uint32_t>(4 * at), __builtin_bit_cast(u32x4, x));
+        } else {
+            const int at = anew(row * dv + n);
 #pragma unroll
-        for (int d = 0; d < DT; ++d)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int ch = 32 * (d / 2) + 4 * (d & 1) + r;
-                if (ch < most) put(to + ch * dv, at, S[d][r]);
-            }
+            for (int r = 0; r < 4; ++r)
+                if (in && row + r < most) *reinterpret_cast<float*>(reinterpret_cast<char*>(to + r * dv) + static_cast<uint32_t>(4 * at)) = x[r];
+        }
     };
-    // a row of R or du
-    auto rows_of = [&](float* rec, int t0) { return rec + (head * (static_cast<long long>(L.blocks) * C) + t0) * dv; };
+    auto record = [&](float* to) {
+#pragma unroll
+        for (int d = 0; d < DT; ++d) put(to, channel(d, 0), dk, S[d]);
+    };
     // P's tile `x` of the helper: row and column tile
     auto tile_row = [](int tile) { return tile < 1 ? 0 : tile < 3 ? 1 : tile < 6 ? 2 : 3; };
 
     Op<OP> ro[BACK ? 1 : CF];               // R, of the chain's waves
-    f32x4 x[BACK ? 1 : CT], ps[NSC];        // outputs and tiles of P, of the helpers
+    f32x4 x[BACK ? 1 : CT], pk[NTT];        // outputs, and the last block's P, of the helpers
     float et[BACK ? 1 : CT];
+    uint32_t dr[MODE == RECORD ? CT : 1][ES];       // their dO: 4 neighbours
 
     Op<3> s3[chain ? DF : 1];               // the state as an operand
     auto split = [&](int f) { s3[f] = op_of<3>(S[2 * f], S[2 * f + 1]); };
@@ -795,11 +811,14 @@ template <typename E, int DKP, int MODE, bool chain> __device__ __forceinline__ 
         } else {
             if (work) {
                 const int htid = tid - NT;
+                tv.store_raw(M.v, cnt, cols, htid);
 #pragma unroll
                 for (int u = 0; u < NTT; ++u) {
                     const int at = htid + u * NT, tile = at >> 6, row = (at & 63) >> 2, c4 = 4 * (at & 3);
                     const int ti = tile_row(tile), tj = tile - ti * (ti + 1) / 2;
-                    if (tile < TILES) put_parts<3>(M.t + Tr::row(16 * (BACK ? tj : ti) + row) + 16 * (BACK ? ti : tj) + c4, TPL, tt[u]);
+                    const int to = Tr::row(16 * (BACK ? tj : ti) + row) + 16 * (BACK ? ti : tj) + c4;
+                    if (tile < TILES) put_parts<3>(M.t + to, TPL, tt[u]);
+                    if (BACK && tile < TILES) put_parts<3>(M.p + to, TPL, pp[u]);
                 }
                 if (htid < C) {
                     M.gh[htid] = sc[0].x;
@@ -813,61 +832,29 @@ template <typename E, int DKP, int MODE, bool chain> __device__ __forceinline__ 
                     }
                 }
             }
-            if constexpr (!BACK) {
-                if (it > 0) {
+            if constexpr (!BACK) {          // P of the block before
 #pragma unroll
-                    for (int i = 0; i < NSC; ++i) {
-                        const int tile = w + NW * i, ti = tile_row(tile), tj = tile - ti * (ti + 1) / 2;
-                        if (tile < TILES) put_parts<PP>(M.p + Tr::row(16 * ti + c) + 16 * tj + 4 * g, TPL, ps[i]);
-                    }
+                for (int u = 0; u < NTT; ++u) {
+                    const int at = tid - NT + u * NT, tile = at >> 6, row = (at & 63) >> 2, c4 = 4 * (at & 3);
+                    const int ti = tile_row(tile), tj = tile - ti * (ti + 1) / 2;
+                    if (it > 0 && tile < TILES) put_parts<PP>(M.p + Tr::row(16 * ti + row) + 16 * tj + c4, TPL, pk[u]);
+                    pk[u] = pp[u];
                 }
             }
         }
         __syncthreads();
-        uint32_t vv[CT * 4];
-#pragma unroll
-        for (int i = 0; i < CT * 4; ++i) vv[i] = vr[i];
         if (it + 1 < blocks) fetch(BACK ? blk - 1 : blk + 1);
 
-        // tiles of P [i][j] times c beta_j, or of P^T times c
-        auto scores = [&] {
-            constexpr int AHEAD = P == 1 ? 2 : 1;       // (float32: the registers of one tile's operands)
-            Op<P> kf[AHEAD][DF], qf[AHEAD][DF];
-            auto operands = [&](int x) {
-                const int tile = w + NW * x < TILES ? w + NW * x : 0, ti = tile_row(tile), tj = tile - ti * (ti + 1) / 2;
-                const int ki = 16 * tj * DKP + rown, qi = 16 * ti * DKP + rown;
+        // the wave's column c of V or dO: 8 neighbouring tokens
+        auto tokens8 = [&](float (&y)[8], int f) {
+            if constexpr (ES == 2) {
+                const Op<1> o = op_cols<1>(M.v + (32 * f + 8 * g + (c >> 2)) * M_::SV + 16 * w + 4 * (c & 3), M_::SV, 0);
+                const u32x4 x = __builtin_bit_cast(u32x4, o.p[0]);
 #pragma unroll
-                for (int f = 0; f < DF; ++f) {
-                    kf[x % AHEAD][f] = op_rows<P>(M.k + (ki ^ 32 * f), KPL);
-                    qf[x % AHEAD][f] = op_rows<P>(M.q + (qi ^ 32 * f), KPL);
-                }
-            };
-            operands(0);                                // (C is 64: each wave has two tiles or three; 32: three waves have one)
+                for (int i = 0; i < 8; ++i) y[i] = i & 1 ? hi_f32(x[i / 2]) : lo_f32(x[i / 2]);
+            } else {
 #pragma unroll
-            for (int x = 0; x < NSC; ++x) {
-                const int tile = w + NW * x, ti = tile_row(tile), tj = tile - ti * (ti + 1) / 2;
-                if (tile >= TILES) break;
-                float decay[4];
-                decays(decay, M.gh, M.gl, 16 * (BACK ? tj : ti) + c, 16 * (BACK ? ti : tj) + 4 * g, BACK);
-                const f32x4 beta = *reinterpret_cast<const f32x4*>(M.beta + 16 * tj + 4 * g);
-                if (AHEAD > 1 && x + 1 < NSC && tile + NW < TILES) operands(x + 1);
-                __builtin_amdgcn_sched_barrier(0);
-                f32x4 s = zero4(), s2 = zero4();        // (two sums: half as many products wait for the last)
-#pragma unroll
-                for (int f = 0; f < DF; f += 2)
-#pragma unroll
-                    for (int i = 0; i < PAIRS<P, P>; ++i) {
-                        mm<P, P>(i, s, BACK ? qf[x % AHEAD][f] : kf[x % AHEAD][f], BACK ? kf[x % AHEAD][f] : qf[x % AHEAD][f]);
-                        mm<P, P>(i, s2, BACK ? qf[x % AHEAD][f + 1] : kf[x % AHEAD][f + 1], BACK ? kf[x % AHEAD][f + 1] : qf[x % AHEAD][f + 1]);
-                    }
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int i = 16 * ti + (BACK ? 4 * g + r : c), j = 16 * tj + (BACK ? c : 4 * g + r);
-                    s[r] = masked(j <= i, (s[r] + s2[r]) * (decay[r] * (BACK ? L.scale : L.scale * beta[r])));
-                }
-                ps[x] = s;
-                if constexpr (BACK) put_parts<3>(M.p + Tr::row(16 * tj + c) + 16 * ti + 4 * g, TPL, s);
-                if (AHEAD == 1 && x + 1 < NSC && tile + NW < TILES) operands(x + 1);
+                for (int i = 0; i < 8; ++i) y[i] = M.v[(32 * f + 8 * g + i) * M_::SV + 16 * w + c];
             }
         };
         // The chain's products, each one's operands on their way from LDS before the product before it: the compiler leaves them where
@@ -896,6 +883,12 @@ template <typename E, int DKP, int MODE, bool chain> __device__ __forceinline__ 
             for (int i = 0; i < 6; ++i)
 #pragma unroll
                 for (int t = 0; t < 2; ++t) mm<3, 3>(i, R[t2 + t], a[t], y);
+        };
+        // R or du of 32 tokens
+        auto record_rows = [&](float* rec, int f) {
+            float* const to = rec + (head * (static_cast<long long>(L.blocks) * C) + t0) * dv;
+            put(to, 32 * f + 8 * g, cnt, R[2 * f]);
+            put(to, 32 * f + 8 * g + 4, cnt, R[2 * f + 1]);
         };
         // what the lane's tokens have in `from`
         auto factors = [&](const float* from, int t) { return *reinterpret_cast<const f32x4*>(from + 32 * (t / 2) + 8 * g + 4 * (t & 1)); };
@@ -955,26 +948,24 @@ template <typename E, int DKP, int MODE, bool chain> __device__ __forceinline__ 
                     fe[t] = factors(M.e, t);
                     fw[t] = factors(M.w, t);
                 }
+                float val[CF][8];
+#pragma unroll
+                for (int f = 0; f < CF; ++f) tokens8(val[f], f);
                 auto lack = [&](int f) {
 #pragma unroll
                     for (int t = 2 * f; t < 2 * f + 2; ++t)
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) z[t][r] = float_of<E>(vv[4 * t + r]) - fe[t][r] * z[t][r];
+                        for (int r = 0; r < 4; ++r) z[t][r] = val[f][4 * (t & 1) + r] - fe[t][r] * z[t][r];
                     return op_of<3>(z[2 * f], z[2 * f + 1]);
                 };
                 // R's tokens of a block of 32: the outputs' operand and the state's
                 auto written = [&](int f) {
                     ro[f] = op_of<OP>(R[2 * f], R[2 * f + 1]);
-                    int at = 8 * g * dv + n;
-                    const int most = in ? cnt - 8 * g : 0;
-                    asm volatile("" : "+v"(at));
+                    if constexpr (MODE == RECORD) record_rows(L.rec_R, f);
                     float y[8];
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
                         const int t = 2 * f + i / 4, r = i % 4;
-                        if constexpr (MODE == RECORD) {
-                            if (32 * f + i < most) put(rows_of(L.rec_R, t0) + (32 * f + i) * dv, at, R[t][r]);
-                        }
                         y[i] = R[t][r] * fw[t][r];
                     }
                     return op_of<3>(y);
@@ -1010,24 +1001,25 @@ template <typename E, int DKP, int MODE, bool chain> __device__ __forceinline__ 
                 if (it > 0 && on) {         // the block before: x += P R
                     const int tb = t0 - C, left = dv - n0 - 4 * g, last = len - tb < C ? len - tb : C;
                     Op<OP> rr[CF];
+                    Op<PP> ps[CF][CT];
 #pragma unroll
-                    for (int f = 0; f < CF; ++f)
+                    for (int f = 0; f < CF; ++f) {
 #pragma unroll
                         for (int s = 0; s < OP; ++s) rr[f].p[s] = __builtin_bit_cast(bf16x8, M.fwd.r[w][f * OP + s][lane]);
+#pragma unroll
+                        for (int t = 2 * f; t < CT; ++t) ps[f][t] = op_rows<PP>(M.p + Tr::at(t / 2, 16 * (t & 1) + c) + 32 * f + 8 * g, TPL);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                     for (int t = 0; t < CT; ++t)
 #pragma unroll
                         for (int r = 0; r < 4; ++r) x[t][r] *= et[t];
 #pragma unroll
-                    for (int f = 0; f < CF; ++f) {
-                        Op<PP> p[CT];
-#pragma unroll
-                        for (int t = 2 * f; t < CT; ++t) p[t] = op_rows<PP>(M.p + Tr::at(t / 2, 16 * (t & 1) + c) + 32 * f + 8 * g, TPL);
+                    for (int f = 0; f < CF; ++f)
 #pragma unroll
                         for (int i = 0; i < PAIRS<OP, PP>; ++i)
 #pragma unroll
-                            for (int t = 2 * f; t < CT; ++t) mm<OP, PP>(i, x[t], rr[f], p[t]);
-                    }
+                            for (int t = 2 * f; t < CT; ++t) mm<OP, PP>(i, x[t], rr[f], ps[f][t]);
                     if constexpr (MODE == FWD) {
                         char* const op = static_cast<char*>(L.o) + (b * L.o_s[0] + h * L.o_s[1] + tb * L.o_s[2] + n0 + 4 * g) * ES;
 #pragma unroll
@@ -1054,7 +1046,10 @@ template <typename E, int DKP, int MODE, bool chain> __device__ __forceinline__ 
                             const int tok = 16 * t + c;
                             float s = 0.f;
 #pragma unroll
-                            for (int r = 0; r < 4; ++r) s = __builtin_fmaf(r < left ? x[t][r] : 0.f, float_of<E>(vr[4 * t + r]), s);
+                            for (int r = 0; r < 4; ++r) {
+                                const uint32_t y = dr[t][r * ES / 4];
+                                s = __builtin_fmaf(r < left ? x[t][r] : 0.f, ES == 4 ? __uint_as_float(y) : r & 1 ? hi_f32(y) : lo_f32(y), s);
+                            }
                             s += __shfl_xor(s, 16);
                             s += __shfl_xor(s, 32);
                             if (g == 0 && tok < last) L.odo[(head * L.parts + n0 / 16) * (static_cast<long long>(L.blocks) * C) + tb + tok] = s;
@@ -1066,14 +1061,16 @@ template <typename E, int DKP, int MODE, bool chain> __device__ __forceinline__ 
 #pragma unroll
                         for (int t = 0; t < CT; ++t) {
                             const int tok = 16 * t + c < cnt ? 16 * t + c : cnt - 1;
+                            const char* const from = gp + static_cast<long long>(t0) * gst;
+                            if (dv % 4 == 0) {
+                                memcpy(&dr[t], from + (tok * gst + (n0 + 4 * g < dv ? n0 + 4 * g : 0) * ES), 4 * ES);
+                            } else {
 #pragma unroll
-                            for (int r = 0; r < 4; ++r) {
-                                const int at = n0 + 4 * g + r < dv ? n0 + 4 * g + r : dv - 1;
-                                vr[4 * t + r] = bits<E>(gp + static_cast<long long>(t0) * gst + (tok * gst + at * ES));
+                                for (int r = 0; r < 4; ++r)
+                                    dr[t][r * ES / 4] = (r * ES % 4 ? dr[t][r * ES / 4] : 0) | bits<E>(from + (tok * gst + (n0 + 4 * g + r < dv ? n0 + 4 * g + r : dv - 1) * ES)) << (r * ES % 4 * 8);
                             }
                         }
                     }
-                    scores();
                     if (on) {
 #pragma unroll
                         for (int t = 0; t < CT; ++t) {
@@ -1098,7 +1095,6 @@ template <typename E, int DKP, int MODE, bool chain> __device__ __forceinline__ 
             }
         } else {
             if constexpr (!chain) {
-                scores();
                 if (on) {                   // Q^T (c e dO)
                     f32x4 add[DT];
 #pragma unroll
@@ -1108,8 +1104,10 @@ template <typename E, int DKP, int MODE, bool chain> __device__ __forceinline__ 
 #pragma unroll
                     for (int f = 0; f < CF; ++f) {
                         float y[8];
+                        tokens8(y, f);
+                        const f32x4 e0 = *reinterpret_cast<const f32x4*>(M.e + 32 * f + 8 * g), e1 = *reinterpret_cast<const f32x4*>(M.e + 32 * f + 8 * g + 4);
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) y[i] = float_of<E>(vv[8 * f + i]) * (L.scale * M.e[32 * f + 8 * g + i]);
+                        for (int i = 0; i < 8; ++i) y[i] *= L.scale * (i < 4 ? e0[i % 4] : e1[i % 4]);
                         const Op<3> o3 = op_of<3>(y);
 #pragma unroll
                         for (int d2 = 0; d2 < DT; d2 += 4) {
@@ -1129,7 +1127,7 @@ template <typename E, int DKP, int MODE, bool chain> __device__ __forceinline__ 
             } else if (on) {
                 held();
             }
-            __syncthreads();                // (P^T and Q^T (c e dO) are written)
+            __syncthreads();                // (Q^T (c e dO) is written)
             if constexpr (chain) {
                 if (!on) continue;
                 InvOp a[2];
@@ -1151,8 +1149,7 @@ template <typename E, int DKP, int MODE, bool chain> __device__ __forceinline__ 
 #pragma unroll
                 for (int f = 0; f < CF; ++f) {
                     float y[8];
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) y[i] = float_of<E>(vv[8 * f + i]);
+                    tokens8(y, f);
                     go[f] = op_of<P>(y);
                 }
                 __builtin_amdgcn_sched_barrier(0);
@@ -1162,14 +1159,11 @@ template <typename E, int DKP, int MODE, bool chain> __device__ __forceinline__ 
 #pragma unroll
                     for (int t = 0; t < CT; ++t) mm<3, P>(i, z[t], pa[t], go[CF - 1]);
                 auto written = [&](int f) {
-                    int at = 8 * g * dv + n;
-                    const int most = in ? cnt - 8 * g : 0;
-                    asm volatile("" : "+v"(at));
+                    record_rows(L.rec_du, f);
                     float y[8];
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
                         const int t = 2 * f + i / 4, r = i % 4;
-                        if (32 * f + i < most) put(rows_of(L.rec_du, t0) + (32 * f + i) * dv, at, R[t][r]);
                         y[i] = R[t][r] * (-fe[t][r] * fb[t][r]);
                     }
                     return op_of<3>(y);

@@ -60,8 +60,8 @@ __device__ __forceinline__ void mul16(f32x4& d, const f32x4& a, const f32x4& b)
 
 constexpr int tile_at(int i, int j) { return i * (i + 1) / 2 + j; }
 
-// (I + L diag(beta))^(-1) of every block, for the forward, and with blockIdx.y 1 the transpose of (I + diag(beta) L)^(-1), for the
-// backward: one wave for a block.  Diagonal tiles by substitution, then pairs of them joined, [A 0; X B]^(-1) having -B^(-1) X A^(-1)
+// (I + L diag(beta))^(-1) and c D . Q K^T diag(beta) of every block, for the forward, and with blockIdx.y 1 the transposes of
+// (I + diag(beta) L)^(-1) and c D . Q K^T, for the adjoint scan: one wave for a block.  Diagonal tiles by substitution, then pairs of them joined, [A 0; X B]^(-1) having -B^(-1) X A^(-1)
 // in its corner, all in float32 (on its matrix instructions), where the states' 24 bits come from.
 template <typename E> __global__ __launch_bounds__(NT) void sfda_delta_prep(DeltaLaunch L)
 {
@@ -112,18 +112,20 @@ template <typename E> __global__ __launch_bounds__(NT) void sfda_delta_prep(Delt
         }
     }
 
-    // lane (c, g) of tile (i, j): row c, columns 4 g + r of K K^T
-    f32x4 X[TILES];
+    // lane (c, g) of tile (i, j): row c, columns 4 g + r of K K^T and of Q K^T, or of K Q^T: row c of tile (j, i)
+    f32x4 X[TILES], Y[TILES];
 #pragma unroll
-    for (int t = 0; t < TILES; ++t) X[t] = zero4();
+    for (int t = 0; t < TILES; ++t) X[t] = Y[t] = zero4();
+    const char* const qp = static_cast<const char*>(L.q) + (b * L.q_s[0] + hk * L.q_s[1] + t0 * L.q_s[2]) * ES;
     const char* const kp = static_cast<const char*>(L.k) + (b * L.k_s[0] + hk * L.k_s[1] + t0 * L.k_s[2]) * ES;
 #pragma clang loop unroll(disable)
     for (int f = 0; 32 * f < L.dk; ++f) {
-        Op<P> k[CT];
+        Op<P> k[CT], q[CT];
 #pragma unroll
         for (int t = 0; t < CT; ++t) {
             const int r = 16 * t + c;
             k[t] = key_frag<E>(kp + (r < cnt ? r : cnt - 1) * (L.k_s[2] * ES), 32 * f + 8 * g, L.dk, r < cnt);
+            q[t] = key_frag<E>(qp + (r < cnt ? r : cnt - 1) * (L.q_s[2] * ES), 32 * f + 8 * g, L.dk, r < cnt);
         }
 #pragma unroll
         for (int i = 0; i < PAIRS<P, P>; ++i)
@@ -131,17 +133,43 @@ template <typename E> __global__ __launch_bounds__(NT) void sfda_delta_prep(Delt
             for (int ti = 0; ti < CT; ++ti)
 #pragma unroll
                 for (int tj = 0; tj <= ti; ++tj) mm<P, P>(i, X[tile_at(ti, tj)], k[tj], k[ti]);
+        if (by_row) {
+#pragma unroll
+            for (int i = 0; i < PAIRS<P, P>; ++i)
+#pragma unroll
+                for (int ti = 0; ti < CT; ++ti)
+#pragma unroll
+                    for (int tj = 0; tj <= ti; ++tj) mm<P, P>(i, Y[tile_at(ti, tj)], q[ti], k[tj]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < PAIRS<P, P>; ++i)
+#pragma unroll
+                for (int ti = 0; ti < CT; ++ti)
+#pragma unroll
+                    for (int tj = 0; tj <= ti; ++tj) mm<P, P>(i, Y[tile_at(ti, tj)], k[tj], q[ti]);
+        }
     }
     __syncthreads();
+    float* const pout = (by_row ? L.scores_back : L.scores) + (head * static_cast<long long>(L.blocks) + blk) * (TILES * 256);
 #pragma unroll
     for (int ti = 0; ti < CT; ++ti)
 #pragma unroll
         for (int tj = 0; tj <= ti; ++tj) {
-                float d[4];
+                float d[4], e[4];
                 decays(d, tok[w][0], tok[w][1], 16 * ti + c, 16 * tj + 4 * g, false);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) e[r] = d[r];
+                if (by_row) decays(e, tok[w][0], tok[w][1], 16 * tj + c, 16 * ti + 4 * g, true);
                 const f32x4 bj = *reinterpret_cast<const f32x4*>(&tok[w][2][16 * tj + 4 * g]);
                 const float bi = tok[w][2][16 * ti + c];
-                f32x4& x = X[tile_at(ti, tj)];
+                f32x4 &x = X[tile_at(ti, tj)], &y = Y[tile_at(ti, tj)];
+                // c D . Q K^T diag(beta), for the outputs, or c (D . Q K^T)^T
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const bool lower = by_row ? 16 * tj + c <= 16 * ti + 4 * g + r : 16 * tj + 4 * g + r <= 16 * ti + c;
+                    y[r] = masked(lower, y[r] * (L.scale * e[r] * (by_row ? 1.f : bj[r])));
+                }
+                if (live) *reinterpret_cast<f32x4*>(pout + tile_at(ti, tj) * 256 + c * 16 + 4 * g) = y;
 #pragma unroll
                 for (int r = 0; r < 4; ++r) x[r] = masked(16 * tj + 4 * g + r < 16 * ti + c, -x[r] * (d[r] * (by_row ? bi : bj[r])));
             }

@@ -74,6 +74,7 @@ struct DeltaLaunch {
     long long first;
     int heads, blocks;
     float *inv, *inv_back;   // [heads][blocks][tiles of the lower triangle][16][16]
+    float *scores, *scores_back;    // as these
     float4* scalars;         // [heads][blocks * block][2]: sum of the block's log decays (hi, lo), beta, e; w, w beta, the block's decay (hi, lo)
     float *rec_S, *rec_U;    // states before each block and after the last; their gradients after each block
     float *rec_R, *rec_du;   // [heads][blocks * block][dv]

@@ -669,10 +669,10 @@ static bool delta_sizes(int B, int H, int Hk, int T, int dk, int dv)
 static ll delta_blocks(int T, bool bf16) { return (static_cast<ll>(T) + sfda::delta_block(bf16) - 1) / sfda::delta_block(bf16); }
 static bool delta_launches(ll heads, ll blocks, int dv) { return heads * std::max(blocks + 4, (dv + 63LL) / 64) < (1LL << 32) / 256; }
 
-// the forward's part of a workspace for `heads` value heads: inverses and scalars
+// the forward's part of a workspace for `heads` value heads: inverses, scores and scalars
 static ll delta_prep_bytes(ll heads, ll blocks, bool bf16, int inverses)
 {
-    return heads * blocks * (inverses * sfda::delta_tiles(bf16) * 1024LL + sfda::delta_block(bf16) * 32LL);
+    return heads * blocks * (inverses * sfda::delta_tiles(bf16) * 2048LL + sfda::delta_block(bf16) * 32LL);
 }
 
 size_t sfda_delta_attn_fwd_workspace_bytes(int B, int H, int T, int dk, int dv, sfda_dtype_t dtype)
@@ -721,7 +721,8 @@ sfda_status_t sfda_delta_attn_fwd(const void* q, const void* k, const void* v, c
     L.B = B; L.H = H; L.Hk = Hk; L.T = T; L.dk = dk; L.dv = dv; L.scale = scale; L.bf16 = bf16;
     L.heads = static_cast<int>(heads); L.blocks = static_cast<int>(blocks);
     L.inv = static_cast<float*>(workspace);
-    L.scalars = reinterpret_cast<float4*>(L.inv + heads * blocks * sfda::delta_tiles(bf16) * 256);
+    L.scores = L.inv + heads * blocks * sfda::delta_tiles(bf16) * 256;
+    L.scalars = reinterpret_cast<float4*>(L.scores + heads * blocks * sfda::delta_tiles(bf16) * 256);
     return sfda::launch_delta_fwd(L, static_cast<hipStream_t>(stream)) == hipSuccess ? SFDA_OK : SFDA_ERR_HIP;
 }
 
@@ -802,6 +803,8 @@ sfda_status_t sfda_delta_attn_bwd(const void* q, const void* k, const void* v, c
         float* p = static_cast<float*>(workspace);
         L.inv = p; p += inv;
         L.inv_back = p; p += inv;
+        L.scores = p; p += inv;
+        L.scores_back = p; p += inv;
         L.scalars = reinterpret_cast<float4*>(p); p += n * blocks * C * 8;
         L.rec_S = p; p += up(n * (blocks + 1) * dk * dv);
         L.rec_U = p; p += up(n * blocks * dk * dv);
