@@ -230,6 +230,32 @@ template <typename E, int COLS, int C, int STRIDE, int THREADS = NT, bool SWAPPE
     }
 };
 
+// The parts of a block's triangular matrices on their way to LDS: 16 bytes are half a tile's row.  HALVES of a part for THREADS
+// threads; the first `parts` of them are there.
+template <int TILES, int PARTS, int THREADS> struct Matrix {
+    static constexpr int HALVES = TILES * 32, N = (PARTS * HALVES + THREADS - 1) / THREADS;
+    u32x4 x[N];
+    __device__ __forceinline__ void load(const uint16_t* from, int thread)
+    {
+        const int tid = anew(thread);
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
+            const int i = tid + u * THREADS;
+            x[u] = *reinterpret_cast<const u32x4*>(from + static_cast<uint32_t>(8 * (i < PARTS * HALVES ? i : 0)));
+        }
+    }
+    // place(part, row tile, column tile, row, column) of 8 neighbours; UPPER: tile (i, j) of the triangle has column tile i
+    template <bool UPPER, typename Place> __device__ __forceinline__ void store(int thread, Place place) const
+    {
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
+            const int i = thread + u * THREADS, part = i / HALVES, j = i - part * HALVES, tile = j >> 5;
+            const int ti = tile < 1 ? 0 : tile < 3 ? 1 : tile < 6 ? 2 : 3, tj = tile - ti * (ti + 1) / 2;
+            if (i < PARTS * HALVES) *reinterpret_cast<u32x4*>(place(part, 16 * (UPPER ? tj : ti) + (j >> 1 & 15), 16 * (UPPER ? ti : tj) + 8 * (j & 1))) = x[u];
+        }
+    }
+};
+
 template <typename E> __device__ __forceinline__ float value(const char* p)
 {
     E x;
@@ -302,24 +328,21 @@ template <typename E, int DKP, int MODE> __device__ __forceinline__ void scan(co
     const uint32_t kst = static_cast<uint32_t>(L.k_s[2] * ES), qst = static_cast<uint32_t>(L.q_s[2] * ES), vst = static_cast<uint32_t>(L.v_s[2] * ES);
     const uint32_t gst = MODE == FWD ? 0 : static_cast<uint32_t>(L.g_s[2] * ES);
     const uint32_t col = (in ? n : dv - 1) * ES;
-    const float* const tmat = (BACK ? L.inv_back : L.inv) + head * L.blocks * static_cast<long long>(TILES * 256);
-    const float* const pmat = (BACK ? L.scores_back : L.scores) + head * L.blocks * static_cast<long long>(TILES * 256);
+    const uint16_t* const tmat = (BACK ? L.inv_back : L.inv) + head * L.blocks * static_cast<long long>(3 * TILES * 256);
+    const uint16_t* const pmat = (BACK ? L.scores_back : L.scores) + head * L.blocks * static_cast<long long>(3 * TILES * 256);
     const float4* const scal = L.scalars + 2 * (head * L.blocks * static_cast<long long>(C));
 
     RowTile<E, DKP, C, SK> tk, tq;
-    f32x4 tt[(TILES * 64 + NT - 1) / NT], pp[(TILES * 64 + NT - 1) / NT];
+    Matrix<TILES, 3, NT> tt;
+    Matrix<TILES, PP, NT> pp;
     float4 sc[2];
     uint32_t vr[CT * 4];                    // V, or dO
     auto fetch = [&](int blk) {
         const int t0 = blk * C, cnt = len - t0 < C ? len - t0 : C;
         tk.load(kp + static_cast<long long>(t0) * kst, kst, cnt, dk, tid);
         tq.load(qp + static_cast<long long>(t0) * qst, qst, cnt, dk, tid);
-#pragma unroll
-        for (int u = 0; u < (TILES * 64 + NT - 1) / NT; ++u) {
-            const int at = tid + u * NT < TILES * 64 ? tid + u * NT : 0;
-            tt[u] = *reinterpret_cast<const f32x4*>(tmat + static_cast<long long>(blk) * TILES * 256 + 4 * at);
-            pp[u] = *reinterpret_cast<const f32x4*>(pmat + static_cast<long long>(blk) * TILES * 256 + 4 * at);
-        }
+        tt.load(tmat + static_cast<long long>(blk) * (3 * TILES * 256), tid);
+        pp.load(pmat + static_cast<long long>(blk) * (3 * TILES * 256), tid);
         const int tok = tid < C ? tid : 0;
         sc[0] = scal[2 * (static_cast<long long>(blk) * C + tok)];
         sc[1] = scal[2 * (static_cast<long long>(blk) * C + tok) + 1];
@@ -370,16 +393,8 @@ template <typename E, int DKP, int MODE> __device__ __forceinline__ void scan(co
         __syncthreads();                    // (the last block's operands are read)
         tk.store(M.k, cnt, dk, tid);
         tq.store(M.q, cnt, dk, tid);
-#pragma unroll
-        for (int u = 0; u < (TILES * 64 + NT - 1) / NT; ++u) {
-            const int at = tid + u * NT, tile = at >> 6, row = (at & 63) >> 2, c4 = 4 * (at & 3);
-            const int ti = tile < 1 ? 0 : tile < 3 ? 1 : tile < 6 ? 2 : 3, tj = tile - ti * (ti + 1) / 2;
-            const int to = (16 * (BACK ? tj : ti) + row) * ST + 16 * (BACK ? ti : tj) + c4;
-            if (tile < TILES) {
-                put_parts<3>(M.t + to, TPL, tt[u]);
-                put_parts<PP>(M.p + to, TPL, pp[u]);
-            }
-        }
+        tt.template store<BACK>(tid, [&](int s, int row, int col) { return M.t + s * TPL + row * ST + col; });
+        pp.template store<BACK>(tid, [&](int s, int row, int col) { return M.p + s * TPL + row * ST + col; });
         if (tid < C) {
             M.gh[tid] = sc[0].x;
             M.gl[tid] = sc[0].y;
@@ -659,14 +674,14 @@ constexpr int PAIR_NT = 2 * NT;
 
 // chain: the wave holds the state.  (Each kind of wave runs a copy of its own, with the other kind's registers free; all have the same
 // barriers.)
-template <typename E, int DKP, int MODE, bool chain> __device__ __forceinline__ void pair_scan(const DeltaLaunch& L, long head, int sl, unsigned char* smem)
+template <typename E, int DKP, int MODE, bool chain, bool whole> __device__ __forceinline__ void pair_scan(const DeltaLaunch& L, long head, int sl, unsigned char* smem)
 {
     typedef Block<E> B;
     typedef PairMem<E, DKP, MODE> M_;
     typedef typename M_::T Tr;
     typedef KeyRows<DKP> Key;
     constexpr int C = B::C, CT = B::CT, CF = B::CF, P = B::P, PP = M_::PP, OP = M_::OP, TILES = B::TILES, ES = sizeof(E);
-    constexpr int DT = DKP / 16, DF = DKP / 32, KPL = M_::KPL, TPL = M_::TPL, NTT = (TILES * 64 + NT - 1) / NT;
+    constexpr int DT = DKP / 16, DF = DKP / 32, KPL = M_::KPL, TPL = M_::TPL;
     constexpr bool BACK = MODE == ADJOINT;
     M_& M = *reinterpret_cast<M_*>(smem);
 
@@ -686,12 +701,13 @@ template <typename E, int DKP, int MODE, bool chain> __device__ __forceinline__ 
     const char* const gp = MODE == FWD ? nullptr : static_cast<const char*>(L.dO) + (b * L.g_s[0] + h * L.g_s[1]) * ES;
     const uint32_t kst = static_cast<uint32_t>(L.k_s[2] * ES), qst = static_cast<uint32_t>(L.q_s[2] * ES), vst = static_cast<uint32_t>(L.v_s[2] * ES);
     const uint32_t gst = MODE == FWD ? 0 : static_cast<uint32_t>(L.g_s[2] * ES);
-    const float* const tmat = (BACK ? L.inv_back : L.inv) + head * L.blocks * static_cast<long long>(TILES * 256);
-    const float* const pmat = (BACK ? L.scores_back : L.scores) + head * L.blocks * static_cast<long long>(TILES * 256);
+    const uint16_t* const tmat = (BACK ? L.inv_back : L.inv) + head * L.blocks * static_cast<long long>(3 * TILES * 256);
+    const uint16_t* const pmat = (BACK ? L.scores_back : L.scores) + head * L.blocks * static_cast<long long>(3 * TILES * 256);
     const float4* const scal = L.scalars + 2 * (head * L.blocks * static_cast<long long>(C));
 
     RowTile<E, DKP, C, DKP, PAIR_NT, true> tk, tq;
-    f32x4 tt[NTT], pp[NTT];
+    Matrix<TILES, 3, NT> tt;                // the inverse and P, by the helpers
+    Matrix<TILES, PP, NT> pp;
     float4 sc[2];
     RowTile<E, SLICE, C, M_::SV, NT> tv;    // V, or dO, by the helpers
     const int cols = dv - sl * SLICE < SLICE ? dv - sl * SLICE : SLICE;
@@ -702,12 +718,8 @@ template <typename E, int DKP, int MODE, bool chain> __device__ __forceinline__ 
         tk.load(kp + static_cast<long long>(t0) * kst, kst, cnt, dk, tid);
         tq.load(qp + static_cast<long long>(t0) * qst, qst, cnt, dk, tid);
         if constexpr (!chain) {
-#pragma unroll
-            for (int u = 0; u < NTT; ++u) {
-                const int at = tid - NT + u * NT < TILES * 64 ? tid - NT + u * NT : 0;
-                tt[u] = *reinterpret_cast<const f32x4*>(tmat + static_cast<long long>(blk) * TILES * 256 + 4 * at);
-                pp[u] = *reinterpret_cast<const f32x4*>(pmat + static_cast<long long>(blk) * TILES * 256 + 4 * at);
-            }
+            tt.load(tmat + static_cast<long long>(blk) * (3 * TILES * 256), tid - NT);
+            if (BACK || blk > 0) pp.load(pmat + static_cast<long long>(BACK ? blk : blk - 1) * (3 * TILES * 256), tid - NT);
             const int tok = tid - NT < C ? tid - NT : 0;
             sc[0] = scal[2 * (static_cast<long long>(blk) * C + tok)];
             sc[1] = scal[2 * (static_cast<long long>(blk) * C + tok) + 1];
@@ -739,30 +751,29 @@ template <typename E, int DKP, int MODE, bool chain> __device__ __forceinline__ 
             for (int r = 0; r < 4; ++r)
                 if (in && channel(d, r) < dk) S[d][r] = src[channel(d, r) * dv + n];
     }
-    // Rows of 4 g + r neighbours to memory, by 16 bytes where the columns are whole (a lane's four rows, each in another line, take four
-    // times as many stores, which bound the scans that record).  Addresses the same for all lanes, and 32-bit offsets.
-    const bool whole = dv % 4 == 0;
+    // Rows of 4 g + r neighbours to memory: with `whole` columns by 16 bytes (a lane's four rows, each in another line, take four
+    // times as many stores, which bound the scans that record).  Stores past the resource's range are dropped: a store that a branch
+    // skips would make the waits for loads before it waits for all stores too.
+    constexpr uint32_t NOWHERE = 0x80000000u;
     auto put = [&](float* to, int row, int most, f32x4 x) {     // row: the first of four
-        if (whole) {
+        const From<true> out(reinterpret_cast<const char*>(to));
+        if constexpr (whole) {
             const int r = row + (c & 3), at = anew(r * dv + n0 + 4 * (c >> 2));
             turn4(x, c);
-            if (r < most && n0 + 4 * (c >> 2) < dv) store16(reinterpret_cast<char*>(to) + static_cast<uint32_t>(4 * at), __builtin_bit_cast(u32x4, x));
+            out.store(r < most && n0 + 4 * (c >> 2) < dv ? static_cast<uint32_t>(4 * at) : NOWHERE, 0, __builtin_bit_cast(u32x4, x));
         } else {
             const int at = anew(row * dv + n);
 #pragma unroll
             for (int r = 0; r < 4; ++r)
-                if (in && row + r < most) *reinterpret_cast<float*>(reinterpret_cast<char*>(to + r * dv) + static_cast<uint32_t>(4 * at)) = x[r];
+                __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(x[r]), out.r, in && row + r < most ? static_cast<uint32_t>(4 * (at + r * dv)) : NOWHERE, 0, 0);
         }
     };
     auto record = [&](float* to) {
 #pragma unroll
         for (int d = 0; d < DT; ++d) put(to, channel(d, 0), dk, S[d]);
     };
-    // P's tile `x` of the helper: row and column tile
-    auto tile_row = [](int tile) { return tile < 1 ? 0 : tile < 3 ? 1 : tile < 6 ? 2 : 3; };
-
     Op<OP> ro[BACK ? 1 : CF];               // R, of the chain's waves
-    f32x4 x[BACK ? 1 : CT], pk[NTT];        // outputs, and the last block's P, of the helpers
+    f32x4 x[BACK ? 1 : CT];                 // outputs, of the helpers
     float et[BACK ? 1 : CT];
     uint32_t dr[MODE == RECORD ? CT : 1][ES];       // their dO: 4 neighbours
 
@@ -812,14 +823,7 @@ template <typename E, int DKP, int MODE, bool chain> __device__ __forceinline__ 
             if (work) {
                 const int htid = tid - NT;
                 tv.store_raw(M.v, cnt, cols, htid);
-#pragma unroll
-                for (int u = 0; u < NTT; ++u) {
-                    const int at = htid + u * NT, tile = at >> 6, row = (at & 63) >> 2, c4 = 4 * (at & 3);
-                    const int ti = tile_row(tile), tj = tile - ti * (ti + 1) / 2;
-                    const int to = Tr::row(16 * (BACK ? tj : ti) + row) + 16 * (BACK ? ti : tj) + c4;
-                    if (tile < TILES) put_parts<3>(M.t + to, TPL, tt[u]);
-                    if (BACK && tile < TILES) put_parts<3>(M.p + to, TPL, pp[u]);
-                }
+                tt.template store<BACK>(htid, [&](int s, int row, int col) { return M.t + s * TPL + Tr::row(row) + col; });
                 if (htid < C) {
                     M.gh[htid] = sc[0].x;
                     M.gl[htid] = sc[0].y;
@@ -832,18 +836,12 @@ template <typename E, int DKP, int MODE, bool chain> __device__ __forceinline__ 
                     }
                 }
             }
-            if constexpr (!BACK) {          // P of the block before
-#pragma unroll
-                for (int u = 0; u < NTT; ++u) {
-                    const int at = tid - NT + u * NT, tile = at >> 6, row = (at & 63) >> 2, c4 = 4 * (at & 3);
-                    const int ti = tile_row(tile), tj = tile - ti * (ti + 1) / 2;
-                    if (it > 0 && tile < TILES) put_parts<PP>(M.p + Tr::row(16 * ti + row) + 16 * tj + c4, TPL, pk[u]);
-                    pk[u] = pp[u];
-                }
-            }
+            // (forward: of the block before)
+            if (BACK || it > 0) pp.template store<BACK>(tid - NT, [&](int s, int row, int col) { return M.p + s * TPL + Tr::row(row) + col; });
         }
         __syncthreads();
         if (it + 1 < blocks) fetch(BACK ? blk - 1 : blk + 1);
+        else if (!BACK && !chain && work) pp.load(pmat + static_cast<long long>(blk) * (3 * TILES * 256), tid - NT);
 
         // the wave's column c of V or dO: 8 neighbouring tokens
         auto tokens8 = [&](float (&y)[8], int f) {
@@ -1021,11 +1019,19 @@ template <typename E, int DKP, int MODE, bool chain> __device__ __forceinline__ 
 #pragma unroll
                             for (int t = 2 * f; t < CT; ++t) mm<OP, PP>(i, x[t], rr[f], ps[f][t]);
                     if constexpr (MODE == FWD) {
-                        char* const op = static_cast<char*>(L.o) + (b * L.o_s[0] + h * L.o_s[1] + tb * L.o_s[2] + n0 + 4 * g) * ES;
+                        char* const op = static_cast<char*>(L.o) + (b * L.o_s[0] + h * L.o_s[1] + tb * L.o_s[2] + n0) * ES;
+                        const From<true> out(op);
+                        const uint32_t ost = static_cast<uint32_t>(L.o_s[2] * ES);
 #pragma unroll
                         for (int t = 0; t < CT; ++t) {
+                            if constexpr (whole) {
+                                const uint32_t off = 16 * t + c < last && left > 0 ? anew(16 * t + c) * ost + 4 * g * ES : NOWHERE;
+                                if constexpr (ES == 2) __builtin_amdgcn_raw_buffer_store_b64(u32x2{pack2(x[t][0], x[t][1]), pack2(x[t][2], x[t][3])}, out.r, off, 0, 0);
+                                else out.store(off, 0, __builtin_bit_cast(u32x4, x[t]));
+                                continue;
+                            }
                             if (16 * t + c >= last) continue;
-                            char* to = op + (16 * t + c) * (L.o_s[2] * ES);
+                            char* to = op + 4 * g * ES + static_cast<uint64_t>((16 * t + c) * ost);
                             if (left >= 4) {
                                 if constexpr (ES == 2) {
                                     const u32x2 y = {pack2(x[t][0], x[t][1]), pack2(x[t][2], x[t][3])};
@@ -1041,6 +1047,7 @@ template <typename E, int DKP, int MODE, bool chain> __device__ __forceinline__ 
                         }
                     } else {
                         // o . dO over the wave's columns
+                        const From<true> sums(reinterpret_cast<const char*>(L.odo + (head * L.parts + n0 / 16) * (static_cast<long long>(L.blocks) * C) + tb));
 #pragma unroll
                         for (int t = 0; t < CT; ++t) {
                             const int tok = 16 * t + c;
@@ -1052,7 +1059,7 @@ template <typename E, int DKP, int MODE, bool chain> __device__ __forceinline__ 
                             }
                             s += __shfl_xor(s, 16);
                             s += __shfl_xor(s, 32);
-                            if (g == 0 && tok < last) L.odo[(head * L.parts + n0 / 16) * (static_cast<long long>(L.blocks) * C) + tb + tok] = s;
+                            __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(s), sums.r, g == 0 && tok < last ? 4u * tok : NOWHERE, 0, 0);
                         }
                     }
                 }
@@ -1062,7 +1069,7 @@ template <typename E, int DKP, int MODE, bool chain> __device__ __forceinline__ 
                         for (int t = 0; t < CT; ++t) {
                             const int tok = 16 * t + c < cnt ? 16 * t + c : cnt - 1;
                             const char* const from = gp + static_cast<long long>(t0) * gst;
-                            if (dv % 4 == 0) {
+                            if constexpr (whole) {
                                 memcpy(&dr[t], from + (tok * gst + (n0 + 4 * g < dv ? n0 + 4 * g : 0) * ES), 4 * ES);
                             } else {
 #pragma unroll
@@ -1237,8 +1244,11 @@ template <typename E, int DKP, int MODE> struct Scan {
     static __device__ __forceinline__ void run(const DeltaLaunch& L, long head, int sl, unsigned char* smem)
     {
         if constexpr (PAIR) {
-            if (__builtin_amdgcn_readfirstlane(threadIdx.x) < NT) pair_scan<E, DKP, MODE, true>(L, head, sl, smem);
-            else pair_scan<E, DKP, MODE, false>(L, head, sl, smem);
+            const bool chain = __builtin_amdgcn_readfirstlane(threadIdx.x) < NT;
+            if (chain && L.whole) pair_scan<E, DKP, MODE, true, true>(L, head, sl, smem);
+            else if (chain) pair_scan<E, DKP, MODE, true, false>(L, head, sl, smem);
+            else if (L.whole) pair_scan<E, DKP, MODE, false, true>(L, head, sl, smem);
+            else pair_scan<E, DKP, MODE, false, false>(L, head, sl, smem);
         } else scan<E, DKP, MODE>(L, head, sl, smem);
     }
 };

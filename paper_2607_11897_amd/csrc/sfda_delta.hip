@@ -60,14 +60,24 @@ __device__ __forceinline__ void mul16(f32x4& d, const f32x4& a, const f32x4& b)
 
 constexpr int tile_at(int i, int j) { return i * (i + 1) / 2 + j; }
 
-// (I + L diag(beta))^(-1) and c D . Q K^T diag(beta) of every block, for the forward, and with blockIdx.y 1 the transposes of
-// (I + diag(beta) L)^(-1) and c D . Q K^T, for the adjoint scan: one wave for a block.  Diagonal tiles by substitution, then pairs of them joined, [A 0; X B]^(-1) having -B^(-1) X A^(-1)
-// in its corner, all in float32 (on its matrix instructions), where the states' 24 bits come from.
-template <typename E> __global__ __launch_bounds__(NT) void sfda_delta_prep(DeltaLaunch L)
+// What a block's scan needs apart from the state, one wave for a block and one of
+//   0  (I + L diag(beta))^(-1), and the tokens' factors     1  c D . Q K^T diag(beta)
+//   2  the transpose of (I + diag(beta) L)^(-1)              3  that of c D . Q K^T
+// (0 and 1 for the forward scan, 2 and 3 for the adjoint one).  Inverses: diagonal tiles by substitution, then pairs of them joined,
+// [A 0; X B]^(-1) having -B^(-1) X A^(-1) in its corner, all in float32 (on its matrix instructions), where the states' 24 bits
+// come from.  The results go out as the bfloat16 parts that the scans multiply, tile by tile.  Bound by latencies: the rows' loads are
+// all on their way first, and nothing waits for another wave.
+__device__ __forceinline__ void wave_sync()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+template <typename E, int DKP> __global__ __launch_bounds__(NT) void sfda_delta_prep(DeltaLaunch L)
 {
     typedef Block<E> B;
-    constexpr int C = B::C, CT = B::CT, P = B::P, TILES = B::TILES, ES = sizeof(E);
-    constexpr int ROW = 20;
+    constexpr int C = B::C, CT = B::CT, P = B::P, TILES = B::TILES, ES = sizeof(E), ROW = 20;
+    constexpr int AHEAD = DKP / 32 < 4 ? DKP / 32 : sizeof(E) == 2 ? 4 : 2;        // fragments' channels loaded at a time, 32 each
     __shared__ __align__(16) float scratch[NW][16 * ROW];
     __shared__ __align__(16) float tok[NW][3][C];
 
@@ -76,17 +86,34 @@ template <typename E> __global__ __launch_bounds__(NT) void sfda_delta_prep(Delt
     const unsigned head = blockIdx.x / static_cast<unsigned>(groups), first = (blockIdx.x - head * groups) * NW;
     const long long bh = L.first + head;
     const int b = static_cast<int>(bh / L.H), h = static_cast<int>(bh - static_cast<long long>(b) * L.H), hk = h / (L.H / L.Hk);
-    const int len = __builtin_amdgcn_readfirstlane(seq_length(L.lengths, b, L.T)), blocks = (len + C - 1) / C;
-    if (static_cast<int>(first) >= blocks) return;
-    const bool live = static_cast<int>(first) + w < blocks, by_row = blockIdx.y != 0;
-    const int blk = live ? first + w : blocks - 1, t0 = blk * C, cnt = len - t0 < C ? len - t0 : C;     // (others do the last one again)
+    const int len = __builtin_amdgcn_readfirstlane(seq_length(L.lengths, b, L.T)), blocks = (len + C - 1) / C, blk = first + w;
+    if (blk >= blocks) return;              // (no barriers below)
+    const int what = blockIdx.y, t0 = blk * C, cnt = len - t0 < C ? len - t0 : C;
+    const bool by_row = what >= 2, inverse = (what & 1) == 0;
     float* const buf = scratch[w];
 
+    // 8 channels of 16 tokens' rows for a lane, both operands of all tiles; a: rows of the first operand
+    const char* const kp = static_cast<const char*>(L.k) + (b * L.k_s[0] + hk * L.k_s[1] + t0 * L.k_s[2]) * ES;
+    const char* const qp = static_cast<const char*>(L.q) + (b * L.q_s[0] + hk * L.q_s[1] + t0 * L.q_s[2]) * ES;
+    const uint32_t kst = static_cast<uint32_t>(L.k_s[2] * ES), qst = static_cast<uint32_t>(L.q_s[2] * ES);
+    Op<P> kf[AHEAD][CT], qf[AHEAD][CT];
+    auto fetch = [&](int f0) {
+#pragma unroll
+        for (int f = 0; f < AHEAD; ++f)
+#pragma unroll
+            for (int t = 0; t < CT; ++t) {
+                const int r = 16 * t + c, rr = r < cnt ? r : cnt - 1;
+                kf[f][t] = key_frag<E>(kp + static_cast<uint64_t>(rr * kst), 32 * (f0 + f) + 8 * g, L.dk, r < cnt);
+                if (!inverse) qf[f][t] = key_frag<E>(qp + static_cast<uint64_t>(rr * qst), 32 * (f0 + f) + 8 * g, L.dk, r < cnt);
+            }
+    };
+    const bool there = lane < cnt;
+    const int token = t0 + (there ? lane : 0);
+    float a = L.log_decay[b * L.l_s[0] + h * L.l_s[1] + token * L.l_s[2]];
+    const float be = L.beta[b * L.b_s[0] + h * L.b_s[1] + token * L.b_s[2]];
+    fetch(0);
+
     {   // sums of the log decays as hi + lo; past -128 a decay is 0 in any case, and sums of such stay finite
-        const bool there = lane < cnt;
-        const int t = t0 + (there ? lane : 0);
-        float a = L.log_decay[b * L.l_s[0] + h * L.l_s[1] + t * L.l_s[2]];
-        const float be = L.beta[b * L.b_s[0] + h * L.b_s[1] + t * L.b_s[2]];
         if (a < -128.f) a = -128.f;
         double s = there ? a : 0.f;
 #pragma unroll
@@ -100,7 +127,7 @@ template <typename E> __global__ __launch_bounds__(NT) void sfda_delta_prep(Delt
             tok[w][0][lane] = hi;
             tok[w][1][lane] = lo;
             tok[w][2][lane] = bt;
-            if (live && !by_row) {
+            if (what == 0) {
                 // the block's decay as hi + lo: a state that lives for thousands of blocks keeps its 24 bits
                 const float x = eh + el, wt = expf((eh - hi) + (el - lo));
                 const bool near = x > -0.5f && x < 0.5f;
@@ -112,74 +139,71 @@ template <typename E> __global__ __launch_bounds__(NT) void sfda_delta_prep(Delt
         }
     }
 
-    // lane (c, g) of tile (i, j): row c, columns 4 g + r of K K^T and of Q K^T, or of K Q^T: row c of tile (j, i)
-    f32x4 X[TILES], Y[TILES];
+    // lane (c, g) of tile (i, j): row c, columns 4 g + r; of K K^T, of Q K^T, or of K Q^T (tile (j, i))
+    f32x4 X[TILES];
 #pragma unroll
-    for (int t = 0; t < TILES; ++t) X[t] = Y[t] = zero4();
-    const char* const qp = static_cast<const char*>(L.q) + (b * L.q_s[0] + hk * L.q_s[1] + t0 * L.q_s[2]) * ES;
-    const char* const kp = static_cast<const char*>(L.k) + (b * L.k_s[0] + hk * L.k_s[1] + t0 * L.k_s[2]) * ES;
-#pragma clang loop unroll(disable)
-    for (int f = 0; 32 * f < L.dk; ++f) {
-        Op<P> k[CT], q[CT];
+    for (int t = 0; t < TILES; ++t) X[t] = zero4();
 #pragma unroll
-        for (int t = 0; t < CT; ++t) {
-            const int r = 16 * t + c;
-            k[t] = key_frag<E>(kp + (r < cnt ? r : cnt - 1) * (L.k_s[2] * ES), 32 * f + 8 * g, L.dk, r < cnt);
-            q[t] = key_frag<E>(qp + (r < cnt ? r : cnt - 1) * (L.q_s[2] * ES), 32 * f + 8 * g, L.dk, r < cnt);
+    for (int f0 = 0; f0 < DKP / 32; f0 += AHEAD) {
+        if (f0 > 0) {
+            if (32 * f0 >= L.dk) break;
+            fetch(f0);
         }
 #pragma unroll
-        for (int i = 0; i < PAIRS<P, P>; ++i)
-#pragma unroll
-            for (int ti = 0; ti < CT; ++ti)
-#pragma unroll
-                for (int tj = 0; tj <= ti; ++tj) mm<P, P>(i, X[tile_at(ti, tj)], k[tj], k[ti]);
-        if (by_row) {
+        for (int f = 0; f < AHEAD; ++f)
 #pragma unroll
             for (int i = 0; i < PAIRS<P, P>; ++i)
 #pragma unroll
                 for (int ti = 0; ti < CT; ++ti)
 #pragma unroll
-                    for (int tj = 0; tj <= ti; ++tj) mm<P, P>(i, Y[tile_at(ti, tj)], q[ti], k[tj]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < PAIRS<P, P>; ++i)
-#pragma unroll
-                for (int ti = 0; ti < CT; ++ti)
-#pragma unroll
-                    for (int tj = 0; tj <= ti; ++tj) mm<P, P>(i, Y[tile_at(ti, tj)], k[tj], q[ti]);
-        }
+                    for (int tj = 0; tj <= ti; ++tj) {
+                        f32x4& x = X[tile_at(ti, tj)];
+                        if (inverse) mm<P, P>(i, x, kf[f][tj], kf[f][ti]);
+                        else if (by_row) mm<P, P>(i, x, qf[f][ti], kf[f][tj]);
+                        else mm<P, P>(i, x, kf[f][tj], qf[f][ti]);
+                    }
     }
-    __syncthreads();
-    float* const pout = (by_row ? L.scores_back : L.scores) + (head * static_cast<long long>(L.blocks) + blk) * (TILES * 256);
+    wave_sync();
+    // rows of 16 to memory as parts: part s of tile t at s * TILES + t
+    auto put = [&](uint16_t* to, const f32x4& x, int parts) {
+        float y[4] = {x[0], x[1], x[2], x[3]};
+#pragma unroll
+        for (int s = 0; s < 3; ++s) {
+            if (s >= parts) break;
+            uint32_t p[2] = {pack2(y[0], y[1]), pack2(y[2], y[3])};
+            asm("" : "+v"(p[0]), "+v"(p[1]));
+            *reinterpret_cast<u32x2*>(to + s * (TILES * 256) + c * 16 + 4 * g) = u32x2{p[0], p[1]};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) y[i] -= i & 1 ? hi_f32(p[i / 2]) : lo_f32(p[i / 2]);
+        }
+    };
+    const long long at = (head * static_cast<long long>(L.blocks) + blk) * (3 * TILES * 256);
 #pragma unroll
     for (int ti = 0; ti < CT; ++ti)
 #pragma unroll
         for (int tj = 0; tj <= ti; ++tj) {
-                float d[4], e[4];
-                decays(d, tok[w][0], tok[w][1], 16 * ti + c, 16 * tj + 4 * g, false);
+            const bool back = by_row && !inverse;           // (rows are the earlier tokens)
+            const int one = 16 * (back ? tj : ti) + c, four = 16 * (back ? ti : tj) + 4 * g;
+            float d[4];
+            decays(d, tok[w][0], tok[w][1], one, four, back);
+            const f32x4 b4 = *reinterpret_cast<const f32x4*>(&tok[w][2][four]);
+            const float b1 = tok[w][2][one];
+            f32x4& x = X[tile_at(ti, tj)];
 #pragma unroll
-                for (int r = 0; r < 4; ++r) e[r] = d[r];
-                if (by_row) decays(e, tok[w][0], tok[w][1], 16 * tj + c, 16 * ti + 4 * g, true);
-                const f32x4 bj = *reinterpret_cast<const f32x4*>(&tok[w][2][16 * tj + 4 * g]);
-                const float bi = tok[w][2][16 * ti + c];
-                f32x4 &x = X[tile_at(ti, tj)], &y = Y[tile_at(ti, tj)];
-                // c D . Q K^T diag(beta), for the outputs, or c (D . Q K^T)^T
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const bool lower = by_row ? 16 * tj + c <= 16 * ti + 4 * g + r : 16 * tj + 4 * g + r <= 16 * ti + c;
-                    y[r] = masked(lower, y[r] * (L.scale * e[r] * (by_row ? 1.f : bj[r])));
-                }
-                if (live) *reinterpret_cast<f32x4*>(pout + tile_at(ti, tj) * 256 + c * 16 + 4 * g) = y;
-#pragma unroll
-                for (int r = 0; r < 4; ++r) x[r] = masked(16 * tj + 4 * g + r < 16 * ti + c, -x[r] * (d[r] * (by_row ? bi : bj[r])));
+            for (int r = 0; r < 4; ++r) {
+                if (inverse) x[r] = masked(four + r < one, -x[r] * (d[r] * (by_row ? b1 : b4[r])));
+                else x[r] = masked(back ? one <= four + r : four + r <= one, x[r] * (L.scale * d[r] * (back ? 1.f : b4[r])));
             }
+            if (!inverse) put((back ? L.scores_back : L.scores) + at + tile_at(ti, tj) * 256, x, back ? 3 : L.score_parts);
+        }
+    if (!inverse) return;
 
     // row c at 4 g .. to column c at 4 g .., and back
     auto turn = [&](const f32x4& x) {
         f32x4 y;
-        __syncthreads();
+        wave_sync();
         *reinterpret_cast<f32x4*>(buf + c * ROW + 4 * g) = x;
-        __syncthreads();
+        wave_sync();
 #pragma unroll
         for (int r = 0; r < 4; ++r) y[r] = buf[(4 * g + r) * ROW + c];
         return y;
@@ -187,9 +211,9 @@ template <typename E> __global__ __launch_bounds__(NT) void sfda_delta_prep(Delt
     f32x4 rows[CT], T[TILES];               // diagonal tiles by rows; all tiles by columns
 #pragma unroll
     for (int t = 0; t < CT; ++t) {
-        __syncthreads();
+        wave_sync();
         *reinterpret_cast<f32x4*>(buf + c * ROW + 4 * g) = X[tile_at(t, t)];
-        __syncthreads();
+        wave_sync();
         float x[16], n[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -223,22 +247,21 @@ template <typename E> __global__ __launch_bounds__(NT) void sfda_delta_prep(Delt
             }
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            f32x4 a = zero4(), d = zero4();
-            mul16(a, rows[2], m[0][j]);
+            f32x4 y = zero4(), d = zero4();
+            mul16(y, rows[2], m[0][j]);
             mul16(d, r32, m[0][j]);
             mul16(d, rows[3], m[1][j]);
-            T[tile_at(2, j)] = a;
+            T[tile_at(2, j)] = y;
             T[tile_at(3, j)] = d;
         }
     }
-    float* const out = (by_row ? L.inv_back : L.inv) + (head * static_cast<long long>(L.blocks) + blk) * (TILES * 256);
 #pragma unroll
     for (int ti = 0; ti < CT; ++ti)
 #pragma unroll
         for (int tj = 0; tj <= ti; ++tj) {
             f32x4 x = T[tile_at(ti, tj)];
             if (!by_row) x = ti == tj ? rows[ti] : turn(x);
-            if (live) *reinterpret_cast<f32x4*>(out + tile_at(ti, tj) * 256 + c * 16 + 4 * g) = x;
+            put((by_row ? L.inv_back : L.inv) + at + tile_at(ti, tj) * 256, x, 3);
         }
 }
 
@@ -378,12 +401,13 @@ template <typename E> hipError_t step(const DeltaStepLaunch& L, hipStream_t st)
 
 }  // namespace
 
-hipError_t prep(const DeltaLaunch& L, int inverses, hipStream_t st)
+hipError_t prep(const DeltaLaunch& L, int scans, hipStream_t st)
 {
     if (L.blocks == 0) return hipSuccess;
-    const dim3 grid(static_cast<unsigned>(L.heads) * ((L.blocks + NW - 1) / NW), inverses);
-    if (L.bf16) hipLaunchKernelGGL(sfda_delta_prep<uint16_t>, grid, dim3(NT), 0, st, L);
-    else hipLaunchKernelGGL(sfda_delta_prep<float>, grid, dim3(NT), 0, st, L);
+    const dim3 grid(static_cast<unsigned>(L.heads) * ((L.blocks + NW - 1) / NW), 2 * scans);
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(NT), 0, st, L); };
+    if (L.bf16) L.dk <= 64 ? go(sfda_delta_prep<uint16_t, 64>) : L.dk <= 128 ? go(sfda_delta_prep<uint16_t, 128>) : go(sfda_delta_prep<uint16_t, 256>);
+    else L.dk <= 64 ? go(sfda_delta_prep<float, 64>) : L.dk <= 128 ? go(sfda_delta_prep<float, 128>) : go(sfda_delta_prep<float, 256>);
     return hipGetLastError();
 }
 

@@ -5,6 +5,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cstddef>
+#include <cstdint>
 
 namespace sfda {
 
@@ -73,13 +74,15 @@ struct DeltaLaunch {
     float scale;
     long long first;
     int heads, blocks;
-    float *inv, *inv_back;   // [heads][blocks][tiles of the lower triangle][16][16]
-    float *scores, *scores_back;    // as these
+    uint16_t *inv, *inv_back;       // [heads][blocks][3 parts][tiles of the lower triangle][16][16]
+    uint16_t *scores, *scores_back;
+    int score_parts;         // of the forward scan's scores that are read
     float4* scalars;         // [heads][blocks * block][2]: sum of the block's log decays (hi, lo), beta, e; w, w beta, the block's decay (hi, lo)
     float *rec_S, *rec_U;    // states before each block and after the last; their gradients after each block
     float *rec_R, *rec_du;   // [heads][blocks * block][dv]
     float* odo;              // [heads][parts][blocks * block]
     int parts;               // 16 columns each
+    bool whole;              // value columns are whole fours, at 4-byte addresses where o is concerned
     bool bf16;
 };
 constexpr int delta_block(bool bf16) { return bf16 ? 64 : 32; }

@@ -670,9 +670,9 @@ static ll delta_blocks(int T, bool bf16) { return (static_cast<ll>(T) + sfda::de
 static bool delta_launches(ll heads, ll blocks, int dv) { return heads * std::max(blocks + 4, (dv + 63LL) / 64) < (1LL << 32) / 256; }
 
 // the forward's part of a workspace for `heads` value heads: inverses, scores and scalars
-static ll delta_prep_bytes(ll heads, ll blocks, bool bf16, int inverses)
+static ll delta_prep_bytes(ll heads, ll blocks, bool bf16, int scans)
 {
-    return heads * blocks * (inverses * sfda::delta_tiles(bf16) * 2048LL + sfda::delta_block(bf16) * 32LL);
+    return heads * blocks * (scans * 2 * sfda::delta_tiles(bf16) * 1536LL + sfda::delta_block(bf16) * 32LL);
 }
 
 size_t sfda_delta_attn_fwd_workspace_bytes(int B, int H, int T, int dk, int dv, sfda_dtype_t dtype)
@@ -701,7 +701,7 @@ sfda_status_t sfda_delta_attn_fwd(const void* q, const void* k, const void* v, c
     strides3(L.l_s, strides, 3, B, H, T, 1);
     strides3(L.b_s, strides, 4, B, H, T, 1);
     strides3(L.o_s, strides, 5, B, H, T, dv);
-    if (!rows_fit(L.q_s, e) || !rows_fit(L.k_s, e) || !rows_fit(L.v_s, e)) return SFDA_ERR_SHAPE;
+    if (!rows_fit(L.q_s, e) || !rows_fit(L.k_s, e) || !rows_fit(L.v_s, e) || !rows_fit(L.o_s, e)) return SFDA_ERR_SHAPE;
     const size_t need = sfda_delta_attn_fwd_workspace_bytes(B, H, T, dk, dv, dtype);
     Call c;
     c.input(box(q, e, dk, {B, Hk, T}, L.q_s), e);
@@ -720,9 +720,13 @@ sfda_status_t sfda_delta_attn_fwd(const void* q, const void* k, const void* v, c
     L.q = q; L.k = k; L.v = v; L.log_decay = log_decay; L.beta = beta; L.lengths = lengths; L.S0 = S0; L.o = o; L.S_T = S_T;
     L.B = B; L.H = H; L.Hk = Hk; L.T = T; L.dk = dk; L.dv = dv; L.scale = scale; L.bf16 = bf16;
     L.heads = static_cast<int>(heads); L.blocks = static_cast<int>(blocks);
-    L.inv = static_cast<float*>(workspace);
-    L.scores = L.inv + heads * blocks * sfda::delta_tiles(bf16) * 256;
-    L.scalars = reinterpret_cast<float4*>(L.scores + heads * blocks * sfda::delta_tiles(bf16) * 256);
+    const ll matrices = heads * blocks * sfda::delta_tiles(bf16) * 768;
+    L.inv = static_cast<uint16_t*>(workspace);
+    L.scores = L.inv + matrices;
+    L.scalars = reinterpret_cast<float4*>(L.scores + matrices);
+    L.score_parts = bf16 ? 2 : 3;
+    L.whole = dv % 4 == 0 && reinterpret_cast<uintptr_t>(o) % 4 == 0;
+    for (ll st : L.o_s) L.whole = L.whole && st * e % 4 == 0;
     return sfda::launch_delta_fwd(L, static_cast<hipStream_t>(stream)) == hipSuccess ? SFDA_OK : SFDA_ERR_HIP;
 }
 
@@ -795,16 +799,16 @@ sfda_status_t sfda_delta_attn_bwd(const void* q, const void* k, const void* v, c
     L.q = q; L.k = k; L.v = v; L.dO = dO; L.log_decay = log_decay; L.beta = beta; L.lengths = lengths; L.S0 = S0; L.dS_T = dS_T;
     L.dq = dq; L.dk_out = dk_out; L.dv_out = dv_out; L.dlog_decay = dlog_decay; L.dbeta = dbeta; L.dS0 = dS0;
     L.B = B; L.H = H; L.Hk = Hk; L.T = T; L.dk = dk; L.dv = dv; L.scale = scale; L.bf16 = bf16;
-    L.blocks = static_cast<int>(blocks); L.parts = (dv + 15) / 16;
+    L.blocks = static_cast<int>(blocks); L.parts = (dv + 15) / 16; L.score_parts = 3; L.whole = dv % 4 == 0;
     for (ll g = 0; g < groups; g += fit) {
-        const ll n = std::min(fit, groups - g) * per, C = sfda::delta_block(bf16), inv = n * blocks * sfda::delta_tiles(bf16) * 256;
+        const ll n = std::min(fit, groups - g) * per, C = sfda::delta_block(bf16), matrices = n * blocks * sfda::delta_tiles(bf16) * 768;
         auto up = [](ll x) { return (x + 3) / 4 * 4; };         // (16 bytes)
         L.first = g * per; L.heads = static_cast<int>(n);
-        float* p = static_cast<float*>(workspace);
-        L.inv = p; p += inv;
-        L.inv_back = p; p += inv;
-        L.scores = p; p += inv;
-        L.scores_back = p; p += inv;
+        L.inv = static_cast<uint16_t*>(workspace);
+        L.inv_back = L.inv + matrices;
+        L.scores = L.inv_back + matrices;
+        L.scores_back = L.scores + matrices;
+        float* p = reinterpret_cast<float*>(L.scores_back + matrices);
         L.scalars = reinterpret_cast<float4*>(p); p += n * blocks * C * 8;
         L.rec_S = p; p += up(n * (blocks + 1) * dk * dv);
         L.rec_U = p; p += up(n * blocks * dk * dv);
