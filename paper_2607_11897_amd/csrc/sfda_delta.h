@@ -713,20 +713,30 @@ template <typename E, int DKP, int MODE, bool chain, bool whole> __device__ __fo
     const int cols = dv - sl * SLICE < SLICE ? dv - sl * SLICE : SLICE;
     const char* const wp = (BACK ? gp : vp) + sl * SLICE * ES;
     const uint32_t wst = BACK ? gst : vst;
-    auto fetch = [&](int blk) {
+    // A block's loads.  A compute unit takes in some 20 bytes a cycle, and a wave whose loads find no room stands still: forward,
+    // where they are due sooner, all go out first; backward, the matrices' and values' after the helpers' products.
+    auto fetch_keys = [&](int blk) {
         const int t0 = blk * C, cnt = len - t0 < C ? len - t0 : C;
         tk.load(kp + static_cast<long long>(t0) * kst, kst, cnt, dk, tid);
         tq.load(qp + static_cast<long long>(t0) * qst, qst, cnt, dk, tid);
-        if constexpr (!chain) {
-            tt.load(tmat + static_cast<long long>(blk) * (3 * TILES * 256), tid - NT);
-            if (BACK || blk > 0) pp.load(pmat + static_cast<long long>(BACK ? blk : blk - 1) * (3 * TILES * 256), tid - NT);
-            const int tok = tid - NT < C ? tid - NT : 0;
-            sc[0] = scal[2 * (static_cast<long long>(blk) * C + tok)];
-            sc[1] = scal[2 * (static_cast<long long>(blk) * C + tok) + 1];
-        }
-        if constexpr (!chain) tv.load(wp + static_cast<long long>(t0) * wst, wst, cnt, cols, tid - NT);
     };
-    if (blocks > 0) fetch(BACK ? blocks - 1 : 0);
+    auto fetch_matrices = [&](int blk) {        // (by the helpers; forward, P is that of the block before)
+        if (blk < blocks) tt.load(tmat + static_cast<long long>(blk) * (3 * TILES * 256), tid - NT);
+        if (BACK || blk > 0) pp.load(pmat + static_cast<long long>(BACK ? blk : blk - 1) * (3 * TILES * 256), tid - NT);
+    };
+    auto fetch_values = [&](int blk) {          // (by the helpers)
+        const int t0 = blk * C, cnt = len - t0 < C ? len - t0 : C, tok = tid - NT < C ? tid - NT : 0;
+        sc[0] = scal[2 * (static_cast<long long>(blk) * C + tok)];
+        sc[1] = scal[2 * (static_cast<long long>(blk) * C + tok) + 1];
+        tv.load(wp + static_cast<long long>(t0) * wst, wst, cnt, cols, tid - NT);
+    };
+    if (blocks > 0) {
+        fetch_keys(BACK ? blocks - 1 : 0);
+        if constexpr (!chain) {
+            fetch_matrices(BACK ? blocks - 1 : 0);
+            fetch_values(BACK ? blocks - 1 : 0);
+        }
+    }
 
 #ifdef SFDA_LDS_POISON
     lds_poison(&M, sizeof(M_), tid, PAIR_NT);
@@ -840,8 +850,8 @@ template <typename E, int DKP, int MODE, bool chain, bool whole> __device__ __fo
             if (BACK || it > 0) pp.template store<BACK>(tid - NT, [&](int s, int row, int col) { return M.p + s * TPL + Tr::row(row) + col; });
         }
         __syncthreads();
-        if (it + 1 < blocks) fetch(BACK ? blk - 1 : blk + 1);
-        else if (!BACK && !chain && work) pp.load(pmat + static_cast<long long>(blk) * (3 * TILES * 256), tid - NT);
+        const bool more = it + 1 < blocks;
+        const int next = BACK ? blk - 1 : blk + 1;
 
         // the wave's column c of V or dO: 8 neighbouring tokens
         auto tokens8 = [&](float (&y)[8], int f) {
@@ -936,7 +946,9 @@ template <typename E, int DKP, int MODE, bool chain, bool whole> __device__ __fo
 
         if constexpr (!BACK) {
             if constexpr (chain) {
-                if (!work || !on) continue;
+                if (!work) continue;
+                if (more) fetch_keys(next);
+                if (!on) continue;
                 held();
                 InvOp a[2];
                 inverse(a[0], 0, 0);
@@ -996,6 +1008,9 @@ template <typename E, int DKP, int MODE, bool chain, bool whole> __device__ __fo
                     update(k, 0, u0, true, 0);
                 }
             } else {
+                if (more) fetch_keys(next);
+                if (work) fetch_matrices(next);
+                if (more) fetch_values(next);
                 if (it > 0 && on) {         // the block before: x += P R
                     const int tb = t0 - C, left = dv - n0 - 4 * g, last = len - tb < C ? len - tb : C;
                     Op<OP> rr[CF];
@@ -1102,6 +1117,7 @@ template <typename E, int DKP, int MODE, bool chain, bool whole> __device__ __fo
             }
         } else {
             if constexpr (!chain) {
+                if (more) fetch_keys(next);
                 if (on) {                   // Q^T (c e dO)
                     f32x4 add[DT];
 #pragma unroll
@@ -1131,11 +1147,17 @@ template <typename E, int DKP, int MODE, bool chain, bool whole> __device__ __fo
 #pragma unroll
                     for (int d = 0; d < DT; ++d) M.add[w][d][lane] = add[d];
                 }
-            } else if (on) {
-                held();
+            } else {
+                if (on) held();
+                if (more) fetch_keys(next);
             }
             __syncthreads();                // (Q^T (c e dO) is written)
-            if constexpr (chain) {
+            if constexpr (!chain) {
+                if (more) {
+                    fetch_matrices(next);
+                    fetch_values(next);
+                }
+            } else {
                 if (!on) continue;
                 InvOp a[2];
                 Op<3> pa[CT];

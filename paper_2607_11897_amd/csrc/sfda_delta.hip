@@ -73,22 +73,25 @@ __device__ __forceinline__ void wave_sync()
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
-template <typename E, int DKP> __global__ __launch_bounds__(NT) void sfda_delta_prep(DeltaLaunch L)
+template <typename E, int DKP> __global__ __launch_bounds__(NT, 4) void sfda_delta_prep(DeltaLaunch L, unsigned units, int kinds)
 {
     typedef Block<E> B;
     constexpr int C = B::C, CT = B::CT, P = B::P, TILES = B::TILES, ES = sizeof(E), ROW = 20;
-    constexpr int AHEAD = DKP / 32 < 4 ? DKP / 32 : sizeof(E) == 2 ? 4 : 2;        // fragments' channels loaded at a time, 32 each
+    constexpr int AHEAD = 2;                // times 32 channels loaded at a time
     __shared__ __align__(16) float scratch[NW][16 * ROW];
     __shared__ __align__(16) float tok[NW][3][C];
 
     const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int groups = (L.blocks + NW - 1) / NW;
-    const unsigned head = blockIdx.x / static_cast<unsigned>(groups), first = (blockIdx.x - head * groups) * NW;
+    // what is formed of the same blocks runs on one XCD, whose L2 has their rows
+    const unsigned eights = blockIdx.x / 8u, kind = eights % static_cast<unsigned>(kinds), unit = eights / static_cast<unsigned>(kinds) * 8u + blockIdx.x % 8u;
+    if (unit >= units) return;
+    const unsigned head = unit / static_cast<unsigned>(groups), first = (unit - head * groups) * NW;
     const long long bh = L.first + head;
     const int b = static_cast<int>(bh / L.H), h = static_cast<int>(bh - static_cast<long long>(b) * L.H), hk = h / (L.H / L.Hk);
     const int len = __builtin_amdgcn_readfirstlane(seq_length(L.lengths, b, L.T)), blocks = (len + C - 1) / C, blk = first + w;
     if (blk >= blocks) return;              // (no barriers below)
-    const int what = blockIdx.y, t0 = blk * C, cnt = len - t0 < C ? len - t0 : C;
+    const int what = static_cast<int>(kind), t0 = blk * C, cnt = len - t0 < C ? len - t0 : C;
     const bool by_row = what >= 2, inverse = (what & 1) == 0;
     float* const buf = scratch[w];
 
@@ -404,8 +407,9 @@ template <typename E> hipError_t step(const DeltaStepLaunch& L, hipStream_t st)
 hipError_t prep(const DeltaLaunch& L, int scans, hipStream_t st)
 {
     if (L.blocks == 0) return hipSuccess;
-    const dim3 grid(static_cast<unsigned>(L.heads) * ((L.blocks + NW - 1) / NW), 2 * scans);
-    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(NT), 0, st, L); };
+    const unsigned units = static_cast<unsigned>(L.heads) * ((L.blocks + NW - 1) / NW);
+    const dim3 grid((units + 7) / 8 * 8 * (2 * scans));
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(NT), 0, st, L, units, 2 * scans); };
     if (L.bf16) L.dk <= 64 ? go(sfda_delta_prep<uint16_t, 64>) : L.dk <= 128 ? go(sfda_delta_prep<uint16_t, 128>) : go(sfda_delta_prep<uint16_t, 256>);
     else L.dk <= 64 ? go(sfda_delta_prep<float, 64>) : L.dk <= 128 ? go(sfda_delta_prep<float, 128>) : go(sfda_delta_prep<float, 256>);
     return hipGetLastError();

@@ -667,7 +667,7 @@ static bool delta_sizes(int B, int H, int Hk, int T, int dk, int dv)
 }
 // blocks of a sequence; heads times them stay below 2^31, launches below 2^32 threads
 static ll delta_blocks(int T, bool bf16) { return (static_cast<ll>(T) + sfda::delta_block(bf16) - 1) / sfda::delta_block(bf16); }
-static bool delta_launches(ll heads, ll blocks, int dv) { return heads * std::max(blocks + 4, (dv + 63LL) / 64) < (1LL << 32) / 256; }
+static bool delta_launches(ll heads, ll blocks, int dv) { return heads * std::max(blocks + 32, (dv + 63LL) / 64 * 2) < (1LL << 32) / 512; }
 
 // the forward's part of a workspace for `heads` value heads: inverses, scores and scalars
 static ll delta_prep_bytes(ll heads, ll blocks, bool bf16, int scans)
