@@ -291,7 +291,7 @@ __device__ __forceinline__ void column(uint32_t (&x)[COUNT], const char* base, u
     }
 }
 
-enum Mode { FWD, RECORD, ADJOINT };
+enum Mode { FWD, RECORD, ADJOINT, STATES };      // STATES: a segment's end state alone, and what it makes of its start state
 
 template <typename E, int DKP, int MODE> struct Mem {
     typedef Block<E> B;
@@ -657,7 +657,7 @@ template <typename E, int DKP, int MODE> struct PairMem {
     static constexpr bool BACK = MODE == ADJOINT;
     // parts of the state and of R as operands of the outputs, and of P.  bfloat16 outputs: one part each leaves an error of 0.0027 of the
     // results (0.0017 their own rounding), P in two 0.0024
-    static constexpr int C = B::C, P = B::P, OP = MODE == FWD ? P : 3, PP = MODE == FWD && P == 1 ? 2 : 3;
+    static constexpr int C = B::C, P = B::P, OP = MODE == FWD ? P : MODE == STATES ? 1 : 3, PP = MODE == STATES ? 1 : MODE == FWD && P == 1 ? 2 : 3;
     typedef Tri<C, BACK> T;
     static constexpr int KPL = C * DKP, TPL = T::SIZE, DF = DKP / 32, DT = DKP / 16;
     static constexpr int SV = SLICE + (sizeof(E) == 2 ? 16 : 4);
@@ -674,7 +674,7 @@ constexpr int PAIR_NT = 2 * NT;
 
 // chain: the wave holds the state.  (Each kind of wave runs a copy of its own, with the other kind's registers free; all have the same
 // barriers.)
-template <typename E, int DKP, int MODE, bool chain, bool whole> __device__ __forceinline__ void pair_scan(const DeltaLaunch& L, long head, int sl, unsigned char* smem)
+template <typename E, int DKP, int MODE, bool chain, bool whole> __device__ __forceinline__ void pair_scan(const DeltaLaunch& L, long head, int sl, int seg, unsigned char* smem)
 {
     typedef Block<E> B;
     typedef PairMem<E, DKP, MODE> M_;
@@ -691,9 +691,16 @@ template <typename E, int DKP, int MODE, bool chain, bool whole> __device__ __fo
     const int b = __builtin_amdgcn_readfirstlane(static_cast<int>(bh / L.H)), h = __builtin_amdgcn_readfirstlane(static_cast<int>(bh - static_cast<long long>(b) * L.H));
     const int hk = h / (L.H / L.Hk), dk = L.dk, dv = L.dv;
     const int len = __builtin_amdgcn_readfirstlane(seq_length(L.lengths, b, L.T));
-    const int blocks = (len + C - 1) / C;
+    // the segment's blocks
+    const int all = (len + C - 1) / C, begin = BACK || MODE == RECORD ? 0 : min(seg * L.seg_blocks, all);
+    const int end = BACK || MODE == RECORD ? all : min(begin + L.seg_blocks, all), blocks = end - begin;
+    // a segment's state after it is what it makes of the state before it, M S, plus what its tokens write, N.  Slices past those of the
+    // value columns take M's: the same scan from the unit matrix with values of zero.
+    const bool unit = MODE == STATES && sl >= L.slices;
+    if (unit) sl -= L.slices;
+    const int width = unit ? dk : dv;
     const int n0 = sl * SLICE + 16 * w, n = n0 + c;         // the wave's columns, the lane's
-    const bool on = n0 < dv, in = n < dv;
+    const bool on = n0 < width, in = n < width;
 
     const char* const kp = static_cast<const char*>(L.k) + (b * L.k_s[0] + hk * L.k_s[1]) * ES;
     const char* const qp = static_cast<const char*>(L.q) + (b * L.q_s[0] + hk * L.q_s[1]) * ES;
@@ -710,7 +717,7 @@ template <typename E, int DKP, int MODE, bool chain, bool whole> __device__ __fo
     Matrix<TILES, PP, NT> pp;
     float4 sc[2];
     RowTile<E, SLICE, C, M_::SV, NT> tv;    // V, or dO, by the helpers
-    const int cols = dv - sl * SLICE < SLICE ? dv - sl * SLICE : SLICE;
+    const int cols = width - sl * SLICE < SLICE ? width - sl * SLICE : SLICE;
     const char* const wp = (BACK ? gp : vp) + sl * SLICE * ES;
     const uint32_t wst = BACK ? gst : vst;
     // A block's loads.  A compute unit takes in some 20 bytes a cycle, and a wave whose loads find no room stands still: forward,
@@ -718,23 +725,23 @@ template <typename E, int DKP, int MODE, bool chain, bool whole> __device__ __fo
     auto fetch_keys = [&](int blk) {
         const int t0 = blk * C, cnt = len - t0 < C ? len - t0 : C;
         tk.load(kp + static_cast<long long>(t0) * kst, kst, cnt, dk, tid);
-        tq.load(qp + static_cast<long long>(t0) * qst, qst, cnt, dk, tid);
+        if (MODE != STATES) tq.load(qp + static_cast<long long>(t0) * qst, qst, cnt, dk, tid);
     };
     auto fetch_matrices = [&](int blk) {        // (by the helpers; forward, P is that of the block before)
-        if (blk < blocks) tt.load(tmat + static_cast<long long>(blk) * (3 * TILES * 256), tid - NT);
-        if (BACK || blk > 0) pp.load(pmat + static_cast<long long>(BACK ? blk : blk - 1) * (3 * TILES * 256), tid - NT);
+        if (blk < end) tt.load(tmat + static_cast<long long>(blk) * (3 * TILES * 256), tid - NT);
+        if (MODE != STATES && (BACK || blk > begin)) pp.load(pmat + static_cast<long long>(BACK ? blk : blk - 1) * (3 * TILES * 256), tid - NT);
     };
     auto fetch_values = [&](int blk) {          // (by the helpers)
         const int t0 = blk * C, cnt = len - t0 < C ? len - t0 : C, tok = tid - NT < C ? tid - NT : 0;
         sc[0] = scal[2 * (static_cast<long long>(blk) * C + tok)];
         sc[1] = scal[2 * (static_cast<long long>(blk) * C + tok) + 1];
-        tv.load(wp + static_cast<long long>(t0) * wst, wst, cnt, cols, tid - NT);
+        if (!unit) tv.load(wp + static_cast<long long>(t0) * wst, wst, cnt, cols, tid - NT);
     };
     if (blocks > 0) {
-        fetch_keys(BACK ? blocks - 1 : 0);
+        fetch_keys(BACK ? end - 1 : begin);
         if constexpr (!chain) {
-            fetch_matrices(BACK ? blocks - 1 : 0);
-            fetch_values(BACK ? blocks - 1 : 0);
+            fetch_matrices(BACK ? end - 1 : begin);
+            fetch_values(BACK ? end - 1 : begin);
         }
     }
 
@@ -753,13 +760,23 @@ template <typename E, int DKP, int MODE, bool chain, bool whole> __device__ __fo
     auto channel = [&](int d, int r) { return 32 * (d / 2) + 8 * g + 4 * (d & 1) + r; };
 #pragma unroll
     for (int d = 0; d < DT; ++d) S[d] = zero4();
-    if (chain && (BACK ? L.dS_T : L.S0) != nullptr) {
-        const float* const src = (BACK ? L.dS_T : L.S0) + bh * cells;
+    if (chain && MODE == STATES) {
 #pragma unroll
         for (int d = 0; d < DT; ++d)
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
-                if (in && channel(d, r) < dk) S[d][r] = src[channel(d, r) * dv + n];
+            for (int r = 0; r < 4; ++r) S[d][r] = unit && channel(d, r) == n ? 1.f : 0.f;
+    } else if (chain) {
+        const float* src = BACK ? L.dS_T : L.S0;
+        if (src != nullptr) src += bh * cells;
+        // (the state that enters a segment lies where N of the one before it lay)
+        if (MODE == FWD && seg > 0) src = L.seg_N + ((seg - 1) * static_cast<long long>(L.heads) + head) * cells;
+        if (src != nullptr) {
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (in && channel(d, r) < dk) S[d][r] = src[channel(d, r) * dv + n];
+        }
     }
     // Rows of 4 g + r neighbours to memory: with `whole` columns by 16 bytes (a lane's four rows, each in another line, take four
     // times as many stores, which bound the scans that record).  Stores past the resource's range are dropped: a store that a branch
@@ -768,14 +785,14 @@ template <typename E, int DKP, int MODE, bool chain, bool whole> __device__ __fo
     auto put = [&](float* to, int row, int most, f32x4 x) {     // row: the first of four
         const From<true> out(reinterpret_cast<const char*>(to));
         if constexpr (whole) {
-            const int r = row + (c & 3), at = anew(r * dv + n0 + 4 * (c >> 2));
+            const int r = row + (c & 3), at = anew(r * width + n0 + 4 * (c >> 2));
             turn4(x, c);
-            out.store(r < most && n0 + 4 * (c >> 2) < dv ? static_cast<uint32_t>(4 * at) : NOWHERE, 0, __builtin_bit_cast(u32x4, x));
+            out.store(r < most && n0 + 4 * (c >> 2) < width ? static_cast<uint32_t>(4 * at) : NOWHERE, 0, __builtin_bit_cast(u32x4, x));
         } else {
-            const int at = anew(row * dv + n);
+            const int at = anew(row * width + n);
 #pragma unroll
             for (int r = 0; r < 4; ++r)
-                __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(x[r]), out.r, in && row + r < most ? static_cast<uint32_t>(4 * (at + r * dv)) : NOWHERE, 0, 0);
+                __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(x[r]), out.r, in && row + r < most ? static_cast<uint32_t>(4 * (at + r * width)) : NOWHERE, 0, 0);
         }
     };
     auto record = [&](float* to) {
@@ -795,9 +812,9 @@ template <typename E, int DKP, int MODE, bool chain, bool whole> __device__ __fo
     }
 
 #pragma clang loop unroll(disable)
-    for (int it = 0; it < (BACK ? blocks : blocks + 1); ++it) {
+    for (int it = 0; it < (BACK || MODE == STATES ? blocks : blocks + 1); ++it) {
         const bool work = it < blocks;
-        const int blk = BACK ? blocks - 1 - it : it, t0 = blk * C, cnt = len - t0 < C ? len - t0 : C;
+        const int blk = BACK ? end - 1 - it : begin + it, t0 = blk * C, cnt = len - t0 < C ? len - t0 : C;
         // a lane's elements of keys and queries: by columns, rows 8 g + c / 4 and 4 further; by rows, of a tile's h = 0 and 1 and of 16 rows in
         // their order.  (Given anew for each block, or their places for all channels are kept over the blocks, and spilled.)
         int at0 = Key::at(8 * g + (c >> 2), c & 3), at1 = Key::at(8 * g + 4 + (c >> 2), c & 3);
@@ -806,11 +823,11 @@ template <typename E, int DKP, int MODE, bool chain, bool whole> __device__ __fo
         __syncthreads();                    // (the last block's operands are read)
         if (work) {
             tk.store(M.k, cnt, dk, tid);
-            tq.store(M.q, cnt, dk, tid);
+            if (MODE != STATES) tq.store(M.q, cnt, dk, tid);
         }
         if constexpr (chain) {
             if (on) {
-                if constexpr (!BACK) {
+                if constexpr (!BACK && MODE != STATES) {
                     if (it > 0) {
 #pragma unroll
                         for (int f = 0; f < CF; ++f)
@@ -832,7 +849,7 @@ template <typename E, int DKP, int MODE, bool chain, bool whole> __device__ __fo
         } else {
             if (work) {
                 const int htid = tid - NT;
-                tv.store_raw(M.v, cnt, cols, htid);
+                tv.store_raw(M.v, unit ? 0 : cnt, cols, htid);
                 tt.template store<BACK>(htid, [&](int s, int row, int col) { return M.t + s * TPL + Tr::row(row) + col; });
                 if (htid < C) {
                     M.gh[htid] = sc[0].x;
@@ -847,7 +864,7 @@ template <typename E, int DKP, int MODE, bool chain, bool whole> __device__ __fo
                 }
             }
             // (forward: of the block before)
-            if (BACK || it > 0) pp.template store<BACK>(tid - NT, [&](int s, int row, int col) { return M.p + s * TPL + Tr::row(row) + col; });
+            if (MODE != STATES && (BACK || it > 0)) pp.template store<BACK>(tid - NT, [&](int s, int row, int col) { return M.p + s * TPL + Tr::row(row) + col; });
         }
         __syncthreads();
         const bool more = it + 1 < blocks;
@@ -970,7 +987,7 @@ template <typename E, int DKP, int MODE, bool chain, bool whole> __device__ __fo
                 };
                 // R's tokens of a block of 32: the outputs' operand and the state's
                 auto written = [&](int f) {
-                    ro[f] = op_of<OP>(R[2 * f], R[2 * f + 1]);
+                    if constexpr (MODE != STATES) ro[f] = op_of<OP>(R[2 * f], R[2 * f + 1]);
                     if constexpr (MODE == RECORD) record_rows(L.rec_R, f);
                     float y[8];
 #pragma unroll
@@ -1011,6 +1028,7 @@ template <typename E, int DKP, int MODE, bool chain, bool whole> __device__ __fo
                 if (more) fetch_keys(next);
                 if (work) fetch_matrices(next);
                 if (more) fetch_values(next);
+                if (MODE == STATES) continue;
                 if (it > 0 && on) {         // the block before: x += P R
                     const int tb = t0 - C, left = dv - n0 - 4 * g, last = len - tb < C ? len - tb : C;
                     Op<OP> rr[CF];
@@ -1246,14 +1264,20 @@ template <typename E, int DKP, int MODE, bool chain, bool whole> __device__ __fo
     }
 
     if (chain && on) {
-        float* dst = BACK ? L.dS0 : L.S_T;
-        if (dst != nullptr) record(dst + bh * cells);
-        if constexpr (MODE == RECORD) record(L.rec_S + (head * (L.blocks + 1) + blocks) * cells);
+        if constexpr (MODE == STATES) {
+            const long long at = seg * static_cast<long long>(L.heads) + head;
+            record(unit ? L.seg_M + at * dk * dk : L.seg_N + at * cells);
+        } else {
+            float* dst = BACK ? L.dS0 : L.S_T;
+            if (dst != nullptr && (MODE != FWD || seg == L.segments - 1)) record(dst + bh * cells);
+            if constexpr (MODE == RECORD) record(L.rec_S + (head * (L.blocks + 1) + all) * cells);
+        }
     }
-    if constexpr (MODE == FWD) {            // tokens past the sequence's length
+    if constexpr (MODE == FWD) {            // the segment's tokens past the sequence's length
         E* const op = static_cast<E*>(L.o) + b * L.o_s[0] + h * L.o_s[1] + sl * SLICE;
+        const long long lo = static_cast<long long>(seg) * L.seg_blocks * C, hi = seg == L.segments - 1 ? L.T : min(lo + static_cast<long long>(L.seg_blocks) * C, static_cast<long long>(L.T));
         if (lane < dv - sl * SLICE)
-            for (long long t = len + wave; t < L.T; t += 2 * NW) Ops<E>::store1(op + t * L.o_s[2] + lane, 0.f);
+            for (long long t = (lo < len ? len : lo) + wave; t < hi; t += 2 * NW) Ops<E>::store1(op + t * L.o_s[2] + lane, 0.f);
     }
 }
 
@@ -1263,14 +1287,16 @@ template <typename E, int DKP, int MODE> struct Scan {
     static constexpr int THREADS = PAIR ? PAIR_NT : NT;
     static constexpr size_t BYTES = PAIR ? sizeof(PairMem<E, DKP, MODE>) : sizeof(Mem<E, DKP, MODE>);
     static_assert(BYTES <= 160 * 1024, "one compute unit's LDS");
-    static __device__ __forceinline__ void run(const DeltaLaunch& L, long head, int sl, unsigned char* smem)
+    static_assert(PAIR || MODE != STATES, "segments");
+    static __device__ __forceinline__ void run(const DeltaLaunch& L, long head, int sl, int seg, unsigned char* smem)
     {
         if constexpr (PAIR) {
+            const bool whole = MODE == STATES ? (L.dk | L.dv) % 4 == 0 : L.whole;
             const bool chain = __builtin_amdgcn_readfirstlane(threadIdx.x) < NT;
-            if (chain && L.whole) pair_scan<E, DKP, MODE, true, true>(L, head, sl, smem);
-            else if (chain) pair_scan<E, DKP, MODE, true, false>(L, head, sl, smem);
-            else if (L.whole) pair_scan<E, DKP, MODE, false, true>(L, head, sl, smem);
-            else pair_scan<E, DKP, MODE, false, false>(L, head, sl, smem);
+            if (chain && whole) pair_scan<E, DKP, MODE, true, true>(L, head, sl, seg, smem);
+            else if (chain) pair_scan<E, DKP, MODE, true, false>(L, head, sl, seg, smem);
+            else if (whole) pair_scan<E, DKP, MODE, false, true>(L, head, sl, seg, smem);
+            else pair_scan<E, DKP, MODE, false, false>(L, head, sl, seg, smem);
         } else scan<E, DKP, MODE>(L, head, sl, smem);
     }
 };

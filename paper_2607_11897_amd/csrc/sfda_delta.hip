@@ -270,7 +270,7 @@ template <typename E, int DKP> __global__ __launch_bounds__(NT, 4) void sfda_del
 
 // ------------------------------------------------------------------ the forward scan
 
-template <typename E, int DKP> __global__ __launch_bounds__((Scan<E, DKP, FWD>::THREADS)) void sfda_delta_fwd(DeltaLaunch L, int slices)
+template <typename E, int DKP, int MODE> __global__ __launch_bounds__((Scan<E, DKP, MODE>::THREADS)) void sfda_delta_fwd(DeltaLaunch L, int slices)
 {
     extern __shared__ __align__(16) unsigned char smem[];
     long head;
@@ -278,14 +278,90 @@ template <typename E, int DKP> __global__ __launch_bounds__((Scan<E, DKP, FWD>::
     head_slice(blockIdx.x, slices, L.heads, head, sl);
     head = static_cast<long>(same_for_all(static_cast<uint64_t>(head)));
     sl = __builtin_amdgcn_readfirstlane(sl);
-    Scan<E, DKP, FWD>::run(L, head, sl, smem);
+    Scan<E, DKP, MODE>::run(L, head, sl, blockIdx.y, smem);
 }
 
-template <typename E, int DKP> hipError_t fwd(const DeltaLaunch& L, hipStream_t st)
+// The states that enter the segments, S <- N + M S one after the other: a wave for a head and 16 value columns, the state in
+// accumulators as in the scan, M's rows as operands of three parts.
+template <int DKP> __global__ __launch_bounds__(NT) void sfda_delta_join(DeltaLaunch L)
+{
+    constexpr int DT = DKP / 16, DF = DKP / 32;
+    const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const long head = blockIdx.x / static_cast<unsigned>(L.slices);
+    const int n0 = static_cast<int>(blockIdx.x - head * L.slices) * SLICE + 16 * w, n = n0 + c, dk = L.dk, dv = L.dv;
+    if (n0 >= dv) return;
+    const bool in = n < dv;
+    const long long cells = static_cast<long long>(dk) * dv;
+    auto channel = [&](int d, int r) { return 32 * (d / 2) + 8 * g + 4 * (d & 1) + r; };
+    f32x4 S[DT];
+    const float* const S0 = L.S0 == nullptr ? nullptr : L.S0 + (L.first + head) * cells;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) S[d][r] = S0 != nullptr && in && channel(d, r) < dk ? S0[channel(d, r) * dv + n] : 0.f;
+    for (int seg = 0; seg + 1 < L.segments; ++seg) {
+        const long long at = seg * static_cast<long long>(L.heads) + head;
+        float* const N = L.seg_N + at * cells;
+        const float* const M = L.seg_M + at * dk * dk;
+        f32x4 y[DT];
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) y[d][r] = in && channel(d, r) < dk ? N[channel(d, r) * dv + n] : 0.f;
+#pragma unroll
+        for (int f = 0; f < DF; ++f) {
+            if (32 * f >= dk) break;
+            const Op<3> s = op_of<3>(S[2 * f], S[2 * f + 1]);
+#pragma unroll
+            for (int d2 = 0; d2 < DT; d2 += 4) {
+                Op<3> m[4];
+#pragma unroll
+                for (int d = 0; d < 4; ++d) {
+                    const int row = row_of((d2 + d) / 2, d & 1, c), col = 32 * f + 8 * g;
+                    const float* const p = M + (row < dk ? row : 0) * dk;
+                    float x[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const float e = p[col + i < dk ? col + i : 0];
+                        x[i] = row < dk && col + i < dk ? e : 0.f;
+                    }
+                    m[d] = op_of<3>(x);
+                }
+#pragma unroll
+                for (int i = 0; i < 6; ++i)
+#pragma unroll
+                    for (int d = 0; d < 4; ++d) mm<3, 3>(i, y[d2 + d], m[d], s);
+            }
+        }
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+            S[d] = y[d];
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (in && channel(d, r) < dk) N[channel(d, r) * dv + n] = S[d][r];
+        }
+    }
+}
+
+template <typename E, int DKP> hipError_t fwd(DeltaLaunch L, hipStream_t st)
 {
     typedef Scan<E, DKP, FWD> Sc;
-    const int slices = (L.dv + SLICE - 1) / SLICE;
-    hipLaunchKernelGGL((sfda_delta_fwd<E, DKP>), dim3(static_cast<unsigned>(L.heads) * slices), dim3(Sc::THREADS), Sc::BYTES, st, L, slices);
+    L.slices = (L.dv + SLICE - 1) / SLICE;
+    if constexpr (Sc::PAIR) {
+        if (L.segments > 1) {
+            typedef Scan<E, DKP, STATES> Ss;
+            const int slices = L.slices + (L.dk + SLICE - 1) / SLICE;
+            hipLaunchKernelGGL((sfda_delta_fwd<E, DKP, STATES>), dim3(static_cast<unsigned>(L.heads) * slices, L.segments - 1), dim3(Ss::THREADS), Ss::BYTES, st, L, slices);
+            hipError_t e = hipGetLastError();
+            if (e != hipSuccess) return e;
+            hipLaunchKernelGGL((sfda_delta_join<DKP>), dim3(static_cast<unsigned>(L.heads) * L.slices), dim3(NT), 0, st, L);
+            e = hipGetLastError();
+            if (e != hipSuccess) return e;
+        }
+    } else if (L.segments > 1) {
+        return hipErrorInvalidValue;
+    }
+    hipLaunchKernelGGL((sfda_delta_fwd<E, DKP, FWD>), dim3(static_cast<unsigned>(L.heads) * L.slices, L.segments), dim3(Sc::THREADS), Sc::BYTES, st, L, L.slices);
     return hipGetLastError();
 }
 template <typename E> hipError_t fwd_any(const DeltaLaunch& L, hipStream_t st)

@@ -33,8 +33,8 @@ template <typename E, int DKP> __global__ __launch_bounds__((Scans<E, DKP>::THRE
     head_slice(blockIdx.x, slices, L.heads, head, sl);
     head = static_cast<long>(same_for_all(static_cast<uint64_t>(head)));
     sl = __builtin_amdgcn_readfirstlane(sl);
-    if (blockIdx.y == 0) Scans<E, DKP>::Rec::run(L, head, sl, smem);
-    else Scans<E, DKP>::Adj::run(L, head, sl, smem);
+    if (blockIdx.y == 0) Scans<E, DKP>::Rec::run(L, head, sl, 0, smem);
+    else Scans<E, DKP>::Adj::run(L, head, sl, 0, smem);
 }
 
 // ------------------------------------------------------------------ the blocks' gradients

@@ -77,6 +77,8 @@ struct DeltaLaunch {
     uint16_t *inv, *inv_back;       // [heads][blocks][3 parts][tiles of the lower triangle][16][16]
     uint16_t *scores, *scores_back;
     int score_parts;         // of the forward scan's scores that are read
+    int segments, seg_blocks, slices;       // forward: of a sequence, blocks of one, workgroups over the value columns
+    float *seg_N, *seg_M;    // [segments - 1][heads][dk][dv], [dk][dk]: a segment's end state is N + M times its start state
     float4* scalars;         // [heads][blocks * block][2]: sum of the block's log decays (hi, lo), beta, e; w, w beta, the block's decay (hi, lo)
     float *rec_S, *rec_U;    // states before each block and after the last; their gradients after each block
     float *rec_R, *rec_du;   // [heads][blocks * block][dv]
@@ -87,6 +89,7 @@ struct DeltaLaunch {
 };
 constexpr int delta_block(bool bf16) { return bf16 ? 64 : 32; }
 constexpr int delta_tiles(bool bf16) { return bf16 ? 10 : 3; }
+constexpr bool delta_segments(bool bf16, int dk) { return bf16 || dk <= 128; }      // whether sequences may be cut
 hipError_t launch_delta_fwd(const DeltaLaunch& L, hipStream_t st);
 hipError_t launch_delta_bwd(const DeltaLaunch& L, hipStream_t st);
 

@@ -675,11 +675,36 @@ static ll delta_prep_bytes(ll heads, ll blocks, bool bf16, int scans)
     return heads * blocks * (scans * 2 * sfda::delta_tiles(bf16) * 1536LL + sfda::delta_block(bf16) * 32LL);
 }
 
+// Segments of a sequence, where its heads leave compute units idle: the segments' states (of the value columns and of the unit
+// matrix), a join, then all segments side by side.  us of a block for a round of workgroups that fill the units, and of a join's step.
+constexpr double DELTA_STEP = 5., DELTA_STATES = 4., DELTA_JOIN = 6.;
+struct DeltaCut { int segments, blocks; };
+DeltaCut delta_cut(ll heads, ll blocks, int dk, int dv, bool bf16)
+{
+    DeltaCut best{1, static_cast<int>(std::max(blocks, 1LL))};
+    if (!sfda::delta_segments(bf16, dk) || blocks < 4) return best;
+    const ll sv = (dv + 63) / 64, sm = (dk + 63) / 64;
+    auto rounds = [](ll groups) { return static_cast<double>((groups + cus() - 1) / cus()); };
+    double least = 0.9 * rounds(heads * sv) * blocks * DELTA_STEP;
+    for (ll s = 2; s <= 64 && 2 * s <= blocks; ++s) {
+        const ll each = (blocks + s - 1) / s, segs = (blocks + each - 1) / each;
+        const double us = each * (rounds((segs - 1) * heads * (sv + sm)) * DELTA_STATES + rounds(segs * heads * sv) * DELTA_STEP) + segs * DELTA_JOIN + 15.;
+        if (us < least) {
+            least = us;
+            best = {static_cast<int>(segs), static_cast<int>(each)};
+        }
+    }
+    return best;
+}
+ll delta_segment_bytes(ll heads, int segments, int dk, int dv) { return heads * (segments - 1) * dk * (static_cast<ll>(dk) + dv) * 4; }
+
 size_t sfda_delta_attn_fwd_workspace_bytes(int B, int H, int T, int dk, int dv, sfda_dtype_t dtype)
 {
     if (!dtype_ok(dtype) || !decay_sizes(B, H, T, dk, dv)) return 0;
     const bool bf16 = dtype == SFDA_BF16;
-    return static_cast<size_t>(delta_prep_bytes(static_cast<ll>(B) * H, delta_blocks(T, bf16), bf16, 1));
+    const ll heads = static_cast<ll>(B) * H, blocks = delta_blocks(T, bf16);
+    if (heads == 0) return 0;
+    return static_cast<size_t>(delta_prep_bytes(heads, blocks, bf16, 1) + delta_segment_bytes(heads, delta_cut(heads, blocks, dk, dv, bf16).segments, dk, dv));
 }
 
 sfda_status_t sfda_delta_attn_fwd(const void* q, const void* k, const void* v, const float* log_decay, const float* beta,
@@ -725,6 +750,10 @@ sfda_status_t sfda_delta_attn_fwd(const void* q, const void* k, const void* v, c
     L.scores = L.inv + matrices;
     L.scalars = reinterpret_cast<float4*>(L.scores + matrices);
     L.score_parts = bf16 ? 2 : 3;
+    const DeltaCut cut = delta_cut(heads, blocks, dk, dv, bf16);
+    L.segments = cut.segments; L.seg_blocks = cut.blocks;
+    L.seg_N = reinterpret_cast<float*>(L.scalars + 2 * heads * blocks * sfda::delta_block(bf16));
+    L.seg_M = L.seg_N + heads * (cut.segments - 1) * dk * dv;
     L.whole = dv % 4 == 0 && reinterpret_cast<uintptr_t>(o) % 4 == 0;
     for (ll st : L.o_s) L.whole = L.whole && st * e % 4 == 0;
     return sfda::launch_delta_fwd(L, static_cast<hipStream_t>(stream)) == hipSuccess ? SFDA_OK : SFDA_ERR_HIP;

@@ -353,3 +353,22 @@ def test_bwd_against_differences():
         # forward's rounding, 2^-22 of a loss of some tens over h
         scale = float(got["d" + name].double().norm())
         assert abs(want - have) <= 2e-2 * scale, (name, want, have)
+
+
+@pytest.mark.parametrize("B,H,Hk,T,dk,dv,dtype,lengths", [
+    (1, 1, 1, 1500, 64, 64, "f32", None), (1, 2, 1, 2000, 96, 70, "f32", None), (1, 2, 2, 2113, 128, 128, "bf16", None),
+    (2, 2, 1, 3001, 37, 50, "bf16", [3001, 1203]), (3, 1, 1, 1999, 80, 12, "f32", [0, 1999, 64]), (1, 1, 1, 2500, 200, 130, "bf16", None),
+    (2, 1, 1, 2048, 100, 66, "bf16", [5, 2047]),
+])
+def test_fwd_segments(B, H, Hk, T, dk, dv, dtype, lengths):
+    """Sequences long enough, and heads few enough, that they are cut into segments."""
+    from paper_2607_11897_amd import sfda
+    say("segments", B, H, Hk, T, dk, dv, dtype, lengths)
+    whole = sfda.delta_attn_fwd_workspace_bytes(B, 512, T, dk, dv, dtype) // 512
+    assert sfda.delta_attn_fwd_workspace_bytes(B, H, T, dk, dv, dtype) > H * whole
+    x = attn(T, B, H, Hk, T, dk, dv, dtype, True, lengths)
+    o, S = run_fwd(x, dtype, "bthd", dk ** -0.5, float("nan") if lengths else None)
+    ro, rS = O.delta_attn(**names(x), scale=dk ** -0.5)
+    assert rel_err(o, ro) <= ATTN[dtype] and rel_err(S, rS) <= SUM
+    for i, n in enumerate(lengths or ()):
+        assert not o[i, :, n:].any()
