@@ -281,65 +281,85 @@ template <typename E, int DKP, int MODE> __global__ __launch_bounds__((Scan<E, D
     Scan<E, DKP, MODE>::run(L, head, sl, blockIdx.y, smem);
 }
 
-// The states that enter the segments, S <- N + M S one after the other: a wave for a head and 16 value columns, the state in
-// accumulators as in the scan, M's rows as operands of three parts.
-template <int DKP> __global__ __launch_bounds__(NT) void sfda_delta_join(DeltaLaunch L)
+// The states that enter the segments, S <- N + M S one after the other.  One workgroup for a head and 16 value columns, a quarter of
+// the state's rows in a wave; M's rows, which do not wait for the state, are a segment ahead, and the state goes round through
+// LDS.
+template <int DKP> __global__ __launch_bounds__(NT) void sfda_delta_join(DeltaLaunch L, int columns)
 {
-    constexpr int DT = DKP / 16, DF = DKP / 32;
+    constexpr int DT = DKP / 16, DF = DKP / 32, DW = DT / NW;
+    __shared__ float state[2][DKP][17];
     const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const long head = blockIdx.x / static_cast<unsigned>(L.slices);
-    const int n0 = static_cast<int>(blockIdx.x - head * L.slices) * SLICE + 16 * w, n = n0 + c, dk = L.dk, dv = L.dv;
-    if (n0 >= dv) return;
+    const long head = blockIdx.x / static_cast<unsigned>(columns);
+    const int n = 16 * static_cast<int>(blockIdx.x - head * columns) + c, dk = L.dk, dv = L.dv;
     const bool in = n < dv;
     const long long cells = static_cast<long long>(dk) * dv;
-    auto channel = [&](int d, int r) { return 32 * (d / 2) + 8 * g + 4 * (d & 1) + r; };
-    f32x4 S[DT];
     const float* const S0 = L.S0 == nullptr ? nullptr : L.S0 + (L.first + head) * cells;
-#pragma unroll
-    for (int d = 0; d < DT; ++d)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) S[d][r] = S0 != nullptr && in && channel(d, r) < dk ? S0[channel(d, r) * dv + n] : 0.f;
-    for (int seg = 0; seg + 1 < L.segments; ++seg) {
+    for (int i = threadIdx.x; i < DKP * 16; i += NT) {
+        const int ch = i / 16, col = n - c + i % 16;
+        state[0][ch][i % 16] = S0 != nullptr && ch < dk && col < dv ? S0[ch * dv + col] : 0.f;
+    }
+    float m[DW][DF][8], y[DW][4];           // the wave's rows of M (tile row c, 8 channels) and of N (rows 4 g + r, column c)
+    auto fetch = [&](int seg) {
         const long long at = seg * static_cast<long long>(L.heads) + head;
-        float* const N = L.seg_N + at * cells;
         const float* const M = L.seg_M + at * dk * dk;
-        f32x4 y[DT];
+        const float* const N = L.seg_N + at * cells;
 #pragma unroll
-        for (int d = 0; d < DT; ++d)
+        for (int d = 0; d < DW; ++d) {
+            const int row = 16 * (w * DW + d) + c;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) y[d][r] = in && channel(d, r) < dk ? N[channel(d, r) * dv + n] : 0.f;
+            for (int f = 0; f < DF; ++f) {
+                const int col = 32 * f + 8 * g;
+                const float* const p = M + (row < dk ? row : 0) * dk;
+                if (dk % 8 == 0) {
+                    const u32x4 a = load16(p + (col < dk ? col : 0)), b = load16(p + (col < dk ? col : 0) + 4);
 #pragma unroll
-        for (int f = 0; f < DF; ++f) {
-            if (32 * f >= dk) break;
-            const Op<3> s = op_of<3>(S[2 * f], S[2 * f + 1]);
+                    for (int i = 0; i < 8; ++i) m[d][f][i] = __uint_as_float(i < 4 ? a[i % 4] : b[i % 4]);
+                } else {
 #pragma unroll
-            for (int d2 = 0; d2 < DT; d2 += 4) {
-                Op<3> m[4];
-#pragma unroll
-                for (int d = 0; d < 4; ++d) {
-                    const int row = row_of((d2 + d) / 2, d & 1, c), col = 32 * f + 8 * g;
-                    const float* const p = M + (row < dk ? row : 0) * dk;
-                    float x[8];
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const float e = p[col + i < dk ? col + i : 0];
-                        x[i] = row < dk && col + i < dk ? e : 0.f;
-                    }
-                    m[d] = op_of<3>(x);
+                    for (int i = 0; i < 8; ++i) m[d][f][i] = p[col + i < dk ? col + i : 0];
                 }
+            }
 #pragma unroll
-                for (int i = 0; i < 6; ++i)
-#pragma unroll
-                    for (int d = 0; d < 4; ++d) mm<3, 3>(i, y[d2 + d], m[d], s);
+            for (int r = 0; r < 4; ++r) {
+                const int ch = 16 * (w * DW + d) + 4 * g + r;
+                y[d][r] = N[(ch < dk ? ch : 0) * dv + (in ? n : 0)];
             }
         }
+    };
+    if (L.segments > 1) fetch(0);
+    for (int seg = 0; seg + 1 < L.segments; ++seg) {
+        __syncthreads();                    // (the state is written; the other buffer's readers are past it)
+        Op<3> s[DF];
 #pragma unroll
-        for (int d = 0; d < DT; ++d) {
-            S[d] = y[d];
+        for (int f = 0; f < DF; ++f) {
+            float x[8];
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
-                if (in && channel(d, r) < dk) N[channel(d, r) * dv + n] = S[d][r];
+            for (int i = 0; i < 8; ++i) x[i] = state[seg & 1][32 * f + 8 * g + i][c];     // (rows past dk are zero)
+            s[f] = op_of<3>(x);
         }
+        f32x4 z[DW];
+#pragma unroll
+        for (int d = 0; d < DW; ++d) z[d] = f32x4{y[d][0], y[d][1], y[d][2], y[d][3]};
+#pragma unroll
+        for (int f = 0; f < DF; ++f) {
+            Op<3> a[DW];
+#pragma unroll
+            for (int d = 0; d < DW; ++d) a[d] = op_of<3>(m[d][f]);
+#pragma unroll
+            for (int i = 0; i < 6; ++i)
+#pragma unroll
+                for (int d = 0; d < DW; ++d) mm<3, 3>(i, z[d], a[d], s[f]);
+        }
+        if (seg + 2 < L.segments) fetch(seg + 1);
+        float* const N = L.seg_N + (seg * static_cast<long long>(L.heads) + head) * cells;
+#pragma unroll
+        for (int d = 0; d < DW; ++d)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int ch = 16 * (w * DW + d) + 4 * g + r;
+                state[(seg & 1) ^ 1][ch][c] = ch < dk ? z[d][r] : 0.f;
+                if (in && ch < dk) N[ch * dv + n] = z[d][r];
+            }
     }
 }
 
@@ -354,7 +374,7 @@ template <typename E, int DKP> hipError_t fwd(DeltaLaunch L, hipStream_t st)
             hipLaunchKernelGGL((sfda_delta_fwd<E, DKP, STATES>), dim3(static_cast<unsigned>(L.heads) * slices, L.segments - 1), dim3(Ss::THREADS), Ss::BYTES, st, L, slices);
             hipError_t e = hipGetLastError();
             if (e != hipSuccess) return e;
-            hipLaunchKernelGGL((sfda_delta_join<DKP>), dim3(static_cast<unsigned>(L.heads) * L.slices), dim3(NT), 0, st, L);
+            hipLaunchKernelGGL((sfda_delta_join<DKP>), dim3(static_cast<unsigned>(L.heads) * ((L.dv + 15) / 16)), dim3(NT), 0, st, L, (L.dv + 15) / 16);
             e = hipGetLastError();
             if (e != hipSuccess) return e;
         }

@@ -356,8 +356,8 @@ def test_bwd_against_differences():
 
 
 @pytest.mark.parametrize("B,H,Hk,T,dk,dv,dtype,lengths", [
-    (1, 1, 1, 1500, 64, 64, "f32", None), (1, 2, 1, 2000, 96, 70, "f32", None), (1, 2, 2, 2113, 128, 128, "bf16", None),
-    (2, 2, 1, 3001, 37, 50, "bf16", [3001, 1203]), (3, 1, 1, 1999, 80, 12, "f32", [0, 1999, 64]), (1, 1, 1, 2500, 200, 130, "bf16", None),
+    (1, 1, 1, 3000, 64, 64, "f32", None), (1, 2, 1, 4000, 96, 70, "f32", None), (1, 2, 2, 2113, 128, 128, "bf16", None),
+    (2, 2, 1, 3001, 37, 50, "bf16", [3001, 1203]), (3, 1, 1, 3999, 80, 12, "f32", [0, 3999, 64]), (1, 1, 1, 2500, 200, 130, "bf16", None),
     (2, 1, 1, 2048, 100, 66, "bf16", [5, 2047]),
 ])
 def test_fwd_segments(B, H, Hk, T, dk, dv, dtype, lengths):
@@ -372,3 +372,155 @@ def test_fwd_segments(B, H, Hk, T, dk, dv, dtype, lengths):
     assert rel_err(o, ro) <= ATTN[dtype] and rel_err(S, rS) <= SUM
     for i, n in enumerate(lengths or ()):
         assert not o[i, :, n:].any()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,H,Hk,T,dk,dv", [(9, 16, 16, 200, 128, 128), (4, 16, 4, 131, 64, 72), (3, 8, 8, 97, 200, 256)])
+def test_many_heads(B, H, Hk, T, dk, dv, dtype):
+    """More workgroups than compute units, forward and backward, against the recurrence."""
+    say("many heads", B, H, Hk, T, dk, dv, dtype)
+    x = attn(71 + T, B, H, Hk, T, dk, dv, dtype, grads=True)
+    scale = dk ** -0.5
+    o, S = run_fwd(x, dtype, "bthd", scale)
+    ro, rS = O.delta_attn(**names(x), scale=scale)
+    assert rel_err(o, ro) <= ATTN[dtype] and rel_err(S, rS) <= SUM
+    check_bwd(run_bwd(x, dtype, "bthd", scale), O.delta_attn_backward(**names(x, "dO", "dS_T"), scale=scale), dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_broadcast_inputs(dtype):
+    """Inputs whose batches, heads or tokens lie in one place: the gradients are those of every element by itself."""
+    import torch
+    from paper_2607_11897_amd import sfda
+    say("broadcast", dtype)
+    B, H, Hk, T, dk, dv = 3, 4, 2, 70, 48, 40
+    gen = torch.Generator(device="cuda").manual_seed(6)
+    unit = lambda *s: torch.nn.functional.normalize(torch.randn(*s, generator=gen, device="cuda"), dim=-1).to(dt(dtype))  # noqa: E731
+    q, k = unit(1, Hk, T, dk).expand(B, -1, -1, -1), unit(B, 1, T, dk).expand(-1, Hk, -1, -1)
+    v, dO = (torch.randn(B, H, 1, dv, generator=gen, device="cuda").to(dt(dtype)).expand(-1, -1, T, -1) for _ in range(2))
+    g, beta = torch.full((1, 1, 1), -0.05, device="cuda").expand(B, H, T), torch.rand(1, H, 1, generator=gen, device="cuda").expand(B, -1, T)
+    wide = [x.contiguous() for x in (q, k, v, g, beta)]
+    for a, b in zip(sfda.delta_attn_fwd(q, k, v, g, beta, scale=0.3), sfda.delta_attn_fwd(*wide, scale=0.3)):
+        assert torch.equal(a, b)
+    a, b = sfda.delta_attn_bwd(q, k, v, g, beta, None, dO, scale=0.3), sfda.delta_attn_bwd(*wide, None, dO.contiguous(), scale=0.3)
+    for n in a:
+        assert torch.equal(a[n], b[n]), n
+
+
+def test_non_finite_values_stay_in_their_heads_and_after_their_blocks():
+    import torch
+    from paper_2607_11897_amd import sfda
+    say("non finite")
+    B, H, T, d = 2, 3, 256, 32
+    gen = torch.Generator(device="cuda").manual_seed(7)
+    for dtype, block in ((torch.float32, 32), (torch.bfloat16, 64)):
+        q, k = (torch.nn.functional.normalize(torch.randn(B, H, T, d, generator=gen, device="cuda"), dim=-1).to(dtype) for _ in range(2))
+        v = torch.randn(B, H, T, d, generator=gen, device="cuda").to(dtype)
+        g, beta = -torch.rand(B, H, T, generator=gen, device="cuda"), torch.rand(B, H, T, generator=gen, device="cuda")
+        want, _ = sfda.delta_attn_fwd(q, k, v, g, beta)
+        for name in ("q", "k", "v", "g", "beta"):
+            for bad in (float("nan"), INF):
+                x = dict(q=q, k=k, v=v, g=g, beta=beta)
+                x[name] = x[name].clone()
+                x[name][1, 2, 130] = bad
+                o, S = sfda.delta_attn_fwd(x["q"], x["k"], x["v"], x["g"], x["beta"])
+                assert torch.equal(o[0], want[0]) and torch.equal(o[1, :2], want[1, :2])
+                assert torch.equal(o[1, 2, : 130 // block * block], want[1, 2, : 130 // block * block])
+                assert not torch.isfinite(o[1, 2, 130]).all(), (name, bad)
+
+
+def calls(gen, dtype):
+    """Every operator once, on tensors that a graph may hold: (inputs, call)."""
+    import torch
+    from paper_2607_11897_amd import sfda
+    B, H, Hk, T, dk, dv = 2, 4, 2, 150, 64, 72
+
+    def rand(*s, to=dt(dtype)):
+        return torch.randn(*s, generator=gen, device="cuda").to(to)
+    f = torch.float32
+    cos, sin = sfda.rotary_tables(200, 32)
+    x = dict(q=rand(B, Hk, T, dk) / 8, k=rand(B, Hk, T, dk) / 8, v=rand(B, H, T, dv), dO=rand(B, H, T, dv), g=-rand(B, H, T, to=f).abs(),
+             beta=torch.sigmoid(rand(B, H, T, to=f)), S0=rand(B, H, dk, dv, to=f), dS=rand(B, H, dk, dv, to=f), x=rand(B, T, 300), r=rand(B, T, 300),
+             w=rand(300, to=f), b=rand(300, to=f), at=torch.randint(0, 200, (3, B, T), generator=gen, device="cuda", dtype=torch.int32),
+             long=rand(1, 1, 4000, dk) / 8, lv=rand(1, 1, 4000, dv), lg=-rand(1, 1, 4000, to=f).abs(), lb=torch.sigmoid(rand(1, 1, 4000, to=f)))
+
+    def call(stream=None):
+        s = dict(stream=stream)
+        out = list(sfda.delta_attn_fwd(x["q"], x["k"], x["v"], x["g"], x["beta"], x["S0"], scale=0.5, **s))
+        out += list(sfda.delta_attn_fwd(x["long"], x["long"], x["lv"], x["lg"], x["lb"], **s))          # in segments
+        out += list(sfda.delta_attn_bwd(x["q"], x["k"], x["v"], x["g"], x["beta"], x["S0"], x["dO"], x["dS"], scale=0.5, **s).values())
+        y, t = sfda.layer_norm(x["x"], x["w"], x["b"], x["r"], **s)
+        out += [y, t, *sfda.layer_norm_bwd(x["x"], t, x["w"], x["b"], x["r"], **s).values()]
+        out += list(sfda.rotary_axes(x["q"], x["k"], cos, sin, x["at"], (6, 5, 5), cyclic=True, **s))
+        return out
+    return x, call
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_replayed_graphs(dtype):
+    """Captured, and replayed several times on new inputs with eager calls and synchronisations between: the eager results, bit by bit."""
+    import torch
+    say("graph", dtype)
+    gen = torch.Generator(device="cuda").manual_seed(8)
+    x, call = calls(gen, dtype)
+    call()
+    torch.cuda.synchronize()
+    graphs = []
+    for _ in range(2):                      # two graphs whose workspaces come from one pool of their own each
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out = call()
+        graphs.append((graph, out))
+    for turn in range(4):
+        for n in ("q", "v", "dO", "x", "S0", "lv"):
+            x[n].copy_(x[n].flip(-1) * (1.0 + 0.125 * turn))
+        for graph, _ in graphs:
+            graph.replay()
+        want = call()
+        torch.cuda.synchronize()
+        for _, out in graphs:
+            assert len(out) == len(want)
+            for a, b in zip(out, want):
+                assert torch.equal(a, b), turn
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_other_streams(dtype):
+    """Two streams at once, each with tensors of its own, against the current one."""
+    import torch
+    say("streams", dtype)
+    gen = torch.Generator(device="cuda").manual_seed(9)
+    jobs = [calls(gen, dtype)[1] for _ in range(2)]
+    want = [job() for job in jobs]
+    torch.cuda.synchronize()
+    sides = [torch.cuda.Stream() for _ in jobs]
+    for _ in range(3):
+        got = [job(stream=s) for job, s in zip(jobs, sides)]
+        torch.cuda.synchronize()
+        for a, b in zip(got, want):
+            for p, q in zip(a, b):
+                assert torch.equal(p, q)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_lds_poison(dtype):
+    """On the LDS-poison build, whose scans and gradients fill their whole LDS with NaN words at entry: the normal build's results, bit
+    by bit.  Channels that fill their padded width and that do not, blocks that are whole and that are not, segments."""
+    import os
+    import torch
+    from paper_2607_11897_amd import build, sfda
+    if not os.path.exists(build.POISON_LIB):
+        build.build(verbose=False, poison=True, out=build.POISON_LIB)
+    for B, H, Hk, T, dk, dv, lengths in ((2, 2, 1, 75, 128, 128, None), (3, 1, 1, 130, 40, 24, [130, 0, 7]), (1, 2, 2, 97, 37, 101, None),
+                                         (2, 1, 1, 150, 256, 192, [1, 149]), (1, 2, 1, 33, 3, 2, None), (1, 1, 1, 4000, 64, 64, None)):
+        say("poison", dtype, B, H, Hk, T, dk, dv, lengths)
+        x = attn(T, B, H, Hk, T, dk, dv, dtype, True, lengths, grads=True)
+
+        def outputs():
+            return [*run_fwd(x, dtype, "bthd", 0.5), *run_bwd(x, dtype, "bthd", 0.5).values()]
+        want = outputs()
+        with sfda.library(build.POISON_LIB):
+            got = outputs()
+            torch.cuda.synchronize()
+        for a, b in zip(want, got):
+            assert np.isfinite(a).all() and np.array_equal(a, b)
