@@ -4,7 +4,7 @@
 // units, then over the inner one of the heads and tokens; a thread takes IPT rows of the outer one, their
 // loads before their arithmetic.  With several axes a pair's row is that of its axis' position: a lane reads the rows of the axes that its own
 // pairs follow, most often one, and selects.  bfloat16 q and k of B8 H16 T4096 d 128: 106 us, 5.1 TB/s (a large copy: 4.8); one token of 32 x 16
-// rows: 4 us, a launch's.
+// rows: 4 us, a launch's.  Three axes in runs, the same size: 112 us (141 by a loop over the axes, each waited for alone).
 #include "sfda_layer.h"
 #include "sfda_vec.h"
 
@@ -93,26 +93,39 @@ __device__ __forceinline__ void turn(const RotaryLaunch& L, const RotarySide& S,
             if (HIN || i == 0) {
                 bool there = true;
                 if constexpr (AXES) {
-                    // 2 bits for each of the lane's pairs
-                    const unsigned axes = L.axis[first >> 4] >> (2 * (first & 15)) & ((1u << 2 * PAIRS) - 1);
-#pragma unroll
-                    for (int p = 0; p < PAIRS; ++p) c[p] = s[p] = 0.f;
-                    for (int a = 0; a < L.axes; ++a) {
-                        unsigned mine = axes ^ (a * 0x5555u & ((1u << 2 * PAIRS) - 1));     // (00 where a pair follows this axis)
-                        mine = ~(mine | mine >> 1) & 0x5555u & ((1u << 2 * PAIRS) - 1);
-                        if (half - first < PAIRS) mine &= (1u << 2 * (half - first)) - 1;
-                        if (mine == 0) continue;
+                    // 2 bits for each of the lane's pairs.  The axis of its first pair is every lane's first, so that lanes with one axis, as in
+                    // runs, wait for their angles once; then those of lanes that have more.
+                    constexpr unsigned ALL = (1u << 2 * PAIRS) - 1;
+                    const unsigned axes = L.axis[first >> 4] >> (2 * (first & 15)) & ALL;
+                    unsigned left = 0x5555u & ALL;
+                    if (half - first < PAIRS) left &= (1u << 2 * (half - first)) - 1;
+                    auto angles_of = [&](unsigned a, unsigned mine) {
                         const long long at = a * L.pos_a + b * L.pos_b + tok[i];
                         const long long pos = L.pos64 ? static_cast<const long long*>(L.positions)[at] : static_cast<const int*>(L.positions)[at];
                         const bool ok = pos >= 0 && pos < L.P;
                         float ca[PAIRS], sa[PAIRS];
                         angles<PAIRS>(L, ok ? pos : 0, first, half, ca, sa);
 #pragma unroll
-                        for (int p = 0; p < PAIRS; ++p)
-                            if (mine >> 2 * p & 1) {
-                                c[p] = ok ? ca[p] : __builtin_nanf("");
-                                s[p] = ok ? sa[p] : __builtin_nanf("");
-                            }
+                        for (int p = 0; p < PAIRS; ++p) {
+                            const bool set = mine >> 2 * p & 1;
+                            c[p] = set ? ok ? ca[p] : __builtin_nanf("") : c[p];
+                            s[p] = set ? ok ? sa[p] : __builtin_nanf("") : s[p];
+                        }
+                    };
+                    auto pairs_of = [&](unsigned a) {
+                        const unsigned other = axes ^ (a * 0x5555u & ALL);      // (00 where a pair follows this axis)
+                        return ~(other | other >> 1) & left;
+                    };
+#pragma unroll
+                    for (int p = 0; p < PAIRS; ++p) c[p] = s[p] = 0.f;
+                    const unsigned a0 = axes & 3u, mine = pairs_of(a0);
+                    angles_of(a0, mine);
+                    left &= ~mine;
+                    for (int a = 0; a < L.axes && left != 0; ++a) {
+                        const unsigned more = pairs_of(a);
+                        if (more == 0) continue;
+                        angles_of(a, more);
+                        left &= ~more;
                     }
                 } else {
                     long long pos = L.offset + tok[i];
