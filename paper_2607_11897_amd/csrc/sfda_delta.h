@@ -768,8 +768,9 @@ template <typename E, int DKP, int MODE, bool chain, bool whole> __device__ __fo
     } else if (chain) {
         const float* src = BACK ? L.dS_T : L.S0;
         if (src != nullptr) src += bh * cells;
-        // (the state that enters a segment lies where N of the one before it lay)
-        if (MODE == FWD && seg > 0) src = L.seg_N + ((seg - 1) * static_cast<long long>(L.heads) + head) * cells;
+        // the state that enters a segment lies where N of the one before it lay; a copy of S0, which the last segment may write (as S_T)
+        // before the first one reads it, lies behind them
+        if (MODE == FWD && L.segments > 1 && (seg > 0 || src != nullptr)) src = L.seg_N + (((seg > 0 ? seg : L.segments) - 1) * static_cast<long long>(L.heads) + head) * cells;
         if (src != nullptr) {
 #pragma unroll
             for (int d = 0; d < DT; ++d)

@@ -296,7 +296,10 @@ template <int DKP> __global__ __launch_bounds__(NT) void sfda_delta_join(DeltaLa
     const float* const S0 = L.S0 == nullptr ? nullptr : L.S0 + (L.first + head) * cells;
     for (int i = threadIdx.x; i < DKP * 16; i += NT) {
         const int ch = i / 16, col = n - c + i % 16;
-        state[0][ch][i % 16] = S0 != nullptr && ch < dk && col < dv ? S0[ch * dv + col] : 0.f;
+        const bool there = S0 != nullptr && ch < dk && col < dv;
+        const float x = there ? S0[ch * dv + col] : 0.f;
+        state[0][ch][i % 16] = x;
+        if (there) L.seg_N[((L.segments - 1) * static_cast<long long>(L.heads) + head) * cells + ch * dv + col] = x;
     }
     float m[DW][DF][8], y[DW][4];           // the wave's rows of M (tile row c, 8 channels) and of N (rows 4 g + r, column c)
     auto fetch = [&](int seg) {

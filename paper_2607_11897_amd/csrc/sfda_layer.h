@@ -78,7 +78,7 @@ struct DeltaLaunch {
     uint16_t *scores, *scores_back;
     int score_parts;         // of the forward scan's scores that are read
     int segments, seg_blocks, slices;       // forward: of a sequence, blocks of one, workgroups over the value columns
-    float *seg_N, *seg_M;    // [segments - 1][heads][dk][dv], [dk][dk]: a segment's end state is N + M times its start state
+    float *seg_N, *seg_M;    // [segments - 1][heads][dk][dv], [dk][dk]: a segment's end state is N + M times its start state (and behind N, S0)
     float4* scalars;         // [heads][blocks * block][2]: sum of the block's log decays (hi, lo), beta, e; w, w beta, the block's decay (hi, lo)
     float *rec_S, *rec_U;    // states before each block and after the last; their gradients after each block
     float *rec_R, *rec_du;   // [heads][blocks * block][dv]

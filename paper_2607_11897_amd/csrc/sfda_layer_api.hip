@@ -698,7 +698,10 @@ DeltaCut delta_cut(ll heads, ll blocks, int dk, int dv, bool bf16)
     }
     return best;
 }
-ll delta_segment_bytes(ll heads, int segments, int dk, int dv) { return heads * (segments - 1) * dk * (static_cast<ll>(dk) + dv) * 4; }
+ll delta_segment_bytes(ll heads, int segments, int dk, int dv)
+{
+    return segments == 1 ? 0 : heads * dk * 4 * ((segments - 1) * (static_cast<ll>(dk) + dv) + dv);
+}
 
 size_t sfda_delta_attn_fwd_workspace_bytes(int B, int H, int T, int dk, int dv, sfda_dtype_t dtype)
 {
@@ -755,7 +758,7 @@ sfda_status_t sfda_delta_attn_fwd(const void* q, const void* k, const void* v, c
     const DeltaCut cut = delta_cut(heads, blocks, dk, dv, bf16);
     L.segments = cut.segments; L.seg_blocks = cut.blocks;
     L.seg_N = reinterpret_cast<float*>(L.scalars + 2 * heads * blocks * sfda::delta_block(bf16));
-    L.seg_M = L.seg_N + heads * (cut.segments - 1) * dk * dv;
+    L.seg_M = L.seg_N + heads * cut.segments * dk * dv;
     L.whole = dv % 4 == 0 && reinterpret_cast<uintptr_t>(o) % 4 == 0;
     for (ll st : L.o_s) L.whole = L.whole && st * e % 4 == 0;
     return sfda::launch_delta_fwd(L, static_cast<hipStream_t>(stream)) == hipSuccess ? SFDA_OK : SFDA_ERR_HIP;

@@ -375,6 +375,22 @@ def test_fwd_segments(B, H, Hk, T, dk, dv, dtype, lengths):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_fwd_segments_in_place(dtype):
+    """S_T in S0's memory: the last segments, empty ones among them, write what the first ones start from."""
+    from paper_2607_11897_amd import sfda
+    B, H, T, dk, dv = 2, 12, 4500, 64, 64
+    say("segments in place", dtype)
+    whole = sfda.delta_attn_fwd_workspace_bytes(B, 512, T, dk, dv, dtype) // 512
+    assert sfda.delta_attn_fwd_workspace_bytes(B, H, T, dk, dv, dtype) > H * whole
+    x = attn(5, B, H, H, T, dk, dv, dtype, True, [3, T - 1])
+    a = [dev(x[n]).to(dt(dtype)) for n in "qkv"] + [f32(x[n]) for n in ("log_decay", "beta")]
+    S = f32(x["S0"])
+    o, want = sfda.delta_attn_fwd(*a, S, lengths=dev(x["lengths"]))
+    o2, have = sfda.delta_attn_fwd(*a, S, lengths=dev(x["lengths"]), S_T=S)
+    assert have.data_ptr() == S.data_ptr() and want.equal(S) and o.equal(o2)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("B,H,Hk,T,dk,dv", [(9, 16, 16, 200, 128, 128), (4, 16, 4, 131, 64, 72), (3, 8, 8, 97, 200, 256)])
 def test_many_heads(B, H, Hk, T, dk, dv, dtype):
     """More workgroups than compute units, forward and backward, against the recurrence."""
