@@ -540,7 +540,7 @@ sfda_status_t sfda_rotary_axes(const void* q, const void* k, const float* cos, c
  *          0 there and S_T is the state after the last token (S0 at length 0).
  *   S0, S_T : [B, H, dk, dv] contiguous float32, each may be NULL (zero state; not wanted).  S_T == S0 is allowed.
  *   workspace : at least sfda_delta_attn_fwd_workspace_bytes(...) bytes (SFDA_ERR_SHAPE if smaller), 16-byte aligned.
- *   1 <= dk, dv <= 256; 64 tokens' rows of q, k or v lie within 2^31 bytes (SFDA_ERR_SHAPE otherwise).
+ *   1 <= dk, dv <= 256; 64 tokens' rows of q, k, v and o (dO) lie within 2^31 bytes (SFDA_ERR_SHAPE otherwise).
  *   Products that reach a state are those of operands as three bfloat16 parts, to 2^-22, with sums in float32, for both types.
  *   bfloat16: the products that give o alone take the state, the scores and the writes rounded to bfloat16.
  *   A token with a value that is not finite may make its whole block (32 or 64 tokens) NaN, and what follows; magnitudes past
@@ -559,7 +559,7 @@ sfda_status_t sfda_delta_attn_fwd(const void* q, const void* k, const void* v,
  * sfda_delta_attn_bwd -- gradients of a real loss through sfda_delta_attn_fwd, given dO = dL/do and dS_T = dL/dS_T (NULL: zero).
  *   dq, dk [B, Hk, T, dk] (sums over the value heads that share a key head), dv [B, H, T, dv] as the inputs' type; dlog_decay, dbeta
  *          [B, H, T] float32; zero past a sequence's length.  dS0 [B, H, dk, dv] float32 or NULL.
- *   strides: (b, h, t) of q, k, v, log_decay, beta, dO, dq, dk, dv, dlog_decay, dbeta; those of dO's tokens as q's.
+ *   strides: (b, h, t) of q, k, v, log_decay, beta, dO, dq, dk, dv, dlog_decay, dbeta.
  *   workspace : 16-byte aligned; with sfda_delta_attn_bwd_workspace_bytes(B, H, ...) bytes all heads run at once, with less in passes
  *          over groups of key heads, as many as fit; at least what the call takes for one, sfda_delta_attn_bwd_workspace_bytes(1,
  *          H / Hk, 1, ...) (SFDA_ERR_SHAPE if smaller).  The results do not depend on it.

@@ -170,7 +170,7 @@ __device__ __forceinline__ int row_of(int f, int h, int c) { return 32 * f + 8 *
 // units of 4 rows (of 64 channels, whose rows are 8 units long, by x(i) / 2).  An index of channel 32 f of a row is that of
 // channel 0 with 32 f in exclusive or.
 template <int DKP> struct KeyRows {
-    static constexpr int MASK = DKP >= 128 ? 15 : 7, SHIFT = DKP >= 128 ? 0 : 1;
+    static constexpr int SHIFT = DKP >= 128 ? 0 : 1;
     static __device__ __forceinline__ int at(int row, int unit) { return row * DKP + 8 * (unit ^ ((4 * (row & 3) + (row >> 2 & 3)) >> SHIFT)); }
 };
 

@@ -154,7 +154,7 @@ struct LayerNormLaunch {
     bool bf16;
 };
 constexpr int LAYER_NORM_MAX = 16384;
-int layer_norm_strips(long long rows, int D, bool bf16);    // workgroups
+int layer_norm_strips(long long rows, int D, bool bf16, bool bwd);    // workgroups
 hipError_t launch_layer_norm(const LayerNormLaunch& L, hipStream_t st);
 hipError_t launch_layer_norm_bwd(const LayerNormLaunch& L, hipStream_t st);
 hipError_t launch_norm(const NormLaunch& L, hipStream_t st);

@@ -625,7 +625,7 @@ sfda_status_t sfda_layer_norm(const void* x, const float* weight, const float* b
 size_t sfda_layer_norm_bwd_workspace_bytes(int B, int T, int D, sfda_dtype_t dtype)
 {
     if (!dtype_ok(dtype) || !layer_norm_sizes(B, T, D, 0.f)) return 0;
-    return static_cast<size_t>(sfda::layer_norm_strips(static_cast<ll>(B) * T, D, dtype == SFDA_BF16)) * 2 * D * 4;
+    return static_cast<size_t>(sfda::layer_norm_strips(static_cast<ll>(B) * T, D, dtype == SFDA_BF16, true)) * 2 * D * 4;
 }
 
 sfda_status_t sfda_layer_norm_bwd(const void* dy, const void* x, const float* weight, const void* dtotal, void* dx, float* dweight,
