@@ -6,6 +6,8 @@
 //   dlog_decay_t = S' . U + sum_(s >= t, in the block) (dO_s . o_s - v_s . dv_s).
 // Three launches after the inverses: the forward scan again, which records the states and the rows R, and the adjoint scan,
 // which records U and du, side by side as roles of one; then all blocks at once form the products above.
+// bfloat16 B8 H16 T4096 of 128 channels: inverses and scores 250 us, scans 880 (256 compute units, each a head's 64 columns of one
+// direction after the other's), gradients 990.
 #include "sfda_delta.h"
 
 #include <type_traits>
@@ -102,7 +104,9 @@ template <typename E> __device__ __forceinline__ void put_four(E* row, int col, 
 __device__ __forceinline__ int thread() { return anew(threadIdx.x); }
 
 // One workgroup for a block of a key head, its value heads one after the other.  A wave owns one or two tiles of 16 channels of dq and dk
-// (rows; tokens are the columns), whose rows of the states it alone reads.
+// (rows; tokens are the columns), whose rows of the states it alone reads.  Reads both states, R and du: 2.2 GB at the size above, twice the
+// time that they take, since the registers leave a compute unit one workgroup (at half of them 127 to 263 spill), whose loads and products
+// overlap little.  Neighbouring blocks on one XCD, for the state that both read: no gain (1012 us).
 template <typename E, int DKP> __global__ __launch_bounds__((GradMem<E, DKP>::NT)) void sfda_delta_grad(DeltaLaunch L)
 {
     typedef Block<E> B;

@@ -4,7 +4,7 @@
 // Memory-bound.  The lanes of a row hold it in registers (two-pass variance, float32): up to a wave of them by lane moves alone, more
 // waves through LDS.  A workgroup keeps its lanes' weights, and in the backward their gradients, in registers over its strip of rows;
 // the next row's vectors are requested before a row's arithmetic.  bfloat16, B8 T4096 of 2048 channels: with the residual sum 112 us, 4.8 TB/s, a
-// large copy's rate; the backward with dtotal 128 us, 4.2 TB/s, of which 5 are the join's launch.
+// large copy's rate; the backward with dtotal 128 us, 4.2 TB/s, 7 of it the join.
 #include "sfda_layer.h"
 #include "sfda_rows.h"
 #include "sfda_vec.h"
