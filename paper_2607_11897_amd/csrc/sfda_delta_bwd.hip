@@ -104,9 +104,9 @@ template <typename E> __device__ __forceinline__ void put_four(E* row, int col, 
 __device__ __forceinline__ int thread() { return anew(threadIdx.x); }
 
 // One workgroup for a block of a key head, its value heads one after the other.  A wave owns one or two tiles of 16 channels of dq and dk
-// (rows; tokens are the columns), whose rows of the states it alone reads.  Reads both states, R and du: 2.2 GB at the size above, twice the
-// time that they take, since the registers leave a compute unit one workgroup (at half of them 127 to 263 spill), whose loads and products
-// overlap little.  Neighbouring blocks on one XCD, for the state that both read: no gain (1012 us).
+// (rows; tokens are the columns), whose rows of the states it alone reads.  Reads three states, R and du, 3.0 GB at the size above, and
+// writes 0.4: 3.4 TB/s, since the registers leave a compute unit one workgroup (at half of them 127 to 263 spill; four waves with two tiles
+// each spill 147), whose loads and products overlap little.  Neighbouring blocks on one XCD, for the state that both read: no gain (1012 us).
 template <typename E, int DKP> __global__ __launch_bounds__((GradMem<E, DKP>::NT)) void sfda_delta_grad(DeltaLaunch L)
 {
     typedef Block<E> B;

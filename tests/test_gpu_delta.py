@@ -540,3 +540,38 @@ def test_lds_poison(dtype):
             torch.cuda.synchronize()
         for a, b in zip(want, got):
             assert np.isfinite(a).all() and np.array_equal(a, b)
+
+
+def test_offsets_past_32_bits():
+    """Rows so far apart that the last ones lie past 2^31 elements (4 GiB): the results of packed rows, bit by bit."""
+    import torch
+    from paper_2607_11897_amd import sfda
+    B, H, T, d, apart = 1, 2, 135, 64, (16 << 20) - 1024       # (64 rows within 2^31 bytes)
+    say("offsets", apart)
+    mem = torch.empty((T - 1) * apart + 8192, dtype=torch.bfloat16, device="cuda")
+    assert (T - 1) * apart > 1 << 31
+
+    def spread(slot, x=None, columns=H * d, rows=T):
+        t = mem.as_strided((B, rows, columns), (0, apart, 1), slot * 512)
+        if x is not None:
+            t.copy_(x.transpose(1, 2).reshape(B, rows, columns) if x.dim() == 4 else x)
+        return t.view(B, rows, H, d).transpose(1, 2) if columns == H * d else t
+    x = attn(3, B, H, H, T, d, d, "bf16", True, grads=True)
+    q, k, v, dO = (dev(x[n]).to(torch.bfloat16) for n in ("q", "k", "v", "dO"))
+    g, be, S0, dS = (f32(x[n]) for n in ("log_decay", "beta", "S0", "dS_T"))
+    far = [spread(i, t) for i, t in enumerate((q, k, v, dO))]
+    o, S = sfda.delta_attn_fwd(q, k, v, g, be, S0)
+    of, Sf = sfda.delta_attn_fwd(*far[:3], g, be, S0, o=spread(4))
+    assert o.equal(of) and S.equal(Sf)
+    r = sfda.delta_attn_bwd(q, k, v, g, be, S0, dO, dS)
+    f = sfda.delta_attn_bwd(*far[:3], g, be, S0, far[3], dS, dq=spread(4), dk=spread(5), dv=spread(6))
+    assert all(r[n].equal(f[n]) for n in r)
+    rows = torch.randn(B, T, 200, device="cuda").to(torch.bfloat16)
+    more = torch.randn(B, T, 200, device="cuda").to(torch.bfloat16)
+    w = torch.randn(200, device="cuda")
+    y, t = sfda.layer_norm(rows, w, None, more)
+    yf, tf = sfda.layer_norm(spread(0, rows, 200), w, None, spread(1, more, 200), y=spread(2, None, 200), total=spread(3, None, 200))
+    assert y.equal(yf) and t.equal(tf)
+    r = sfda.layer_norm_bwd(rows, t, w, None, more)
+    f = sfda.layer_norm_bwd(spread(0, None, 200), tf, w, None, spread(1, None, 200), dx=spread(4, None, 200))
+    assert r["dx"].equal(f["dx"]) and r["dweight"].equal(f["dweight"])
