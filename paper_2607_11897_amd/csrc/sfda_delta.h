@@ -105,15 +105,17 @@ template <int P> __device__ __forceinline__ Op<P> op_cols2(const uint16_t* p, co
     }
     return o;
 }
-// the products of parts that reach 2^-22 of the whole, the small ones first; a loop over tiles inside one over these has no product
+// the products of parts that reach 2^-22 of the whole (of two parts 2^-16), the small ones first; a loop over tiles inside one over these has no product
 // wait for the last
-template <int PA, int PB> constexpr int PAIRS = PA * PB < 9 ? PA * PB : 6;
+template <int PA, int PB> constexpr int PAIRS = PA == 2 && PB == 2 ? 3 : PA * PB < 9 ? PA * PB : 6;
 template <int PA, int PB> __device__ __forceinline__ void mm(int i, f32x4& d, const Op<PA>& a, const Op<PB>& b)
 {
-    static_assert(PA == 1 || PB == 1 || (PA == 3 && PB == 3), "parts");
+    static_assert(PA == 1 || PB == 1 || PA == PB, "parts");
     if constexpr (PA == 3 && PB == 3) {
         constexpr int A[6] = {2, 0, 1, 1, 0, 0}, B[6] = {0, 2, 1, 0, 1, 0};
         mfma(d, a.p[A[i]], b.p[B[i]]);
+    } else if constexpr (PA == 2 && PB == 2) {
+        mfma(d, a.p[i == 0], b.p[i == 1]);
     } else {
         mfma(d, a.p[PA > 1 ? PA - 1 - i : 0], b.p[PB > 1 ? PB - 1 - i : 0]);
     }

@@ -46,11 +46,13 @@ constexpr int SLAB = 64;        // value columns at a time
 template <typename E, int DKP> struct GradMem {
     typedef Block<E> B;
     static constexpr int NW = DKP == 64 ? 4 : 8, NT = 64 * NW;
-    static constexpr int C = B::C, P = B::P, SK = DKP + 16, SV = SLAB + 8, ST = C + 8;
+    // SP: parts of the states and of the rows that meet them in dk.  bfloat16: with all in one part dq and dk are off by 0.0031 of themselves, the
+    // states in two 0.0026, these rows too 0.0022 (0.0017 their own rounding), for 15 us of 2100
+    static constexpr int C = B::C, P = B::P, SP = P == 1 ? 2 : 3, SK = DKP + 16, SV = SLAB + 8, ST = C + 8;
     static constexpr int KPL = C * SK, VPL = C * SV, TPL = C * ST;
     union {
         // dO, dv, u, and dv times -e, u times w: [token][value column]
-        struct { uint16_t o[P * VPL], v[P * VPL], u[P * VPL], ev[P * VPL], wu[P * VPL]; } row;
+        struct { uint16_t o[P * VPL], v[P * VPL], u[P * VPL], ev[SP * VPL], wu[SP * VPL]; } row;
         struct { uint16_t k[P * KPL], q[P * KPL]; } key;
     };
     uint16_t w[P * TPL], m[P * TPL];                                    // c D . dO u^T, and -(M + M^T): [i][j]
@@ -112,7 +114,7 @@ template <typename E, int DKP> __global__ __launch_bounds__((GradMem<E, DKP>::NT
     typedef Block<E> B;
     typedef GradMem<E, DKP> M_;
     constexpr int NW = M_::NW, NT = M_::NT, C = B::C, CT = B::CT, CF = B::CF, P = B::P, ES = sizeof(E), DW = DKP / 16 / NW;
-    constexpr int SK = M_::SK, SV = M_::SV, ST = M_::ST, KPL = M_::KPL, VPL = M_::VPL, TPL = M_::TPL;
+    constexpr int SP = M_::SP, SK = M_::SK, SV = M_::SV, ST = M_::ST, KPL = M_::KPL, VPL = M_::VPL, TPL = M_::TPL;
     constexpr int RPP = NT / (SLAB / 4), N = C / RPP, TW = (CT * CT + NW - 1) / NW;    // rows of a pass, passes, tiles of scores of a wave
     extern __shared__ __align__(16) unsigned char smem[];
     M_& M = *reinterpret_cast<M_*>(smem);
@@ -272,8 +274,8 @@ template <typename E, int DKP> __global__ __launch_bounds__((GradMem<E, DKP>::NT
                     lu[u][i] *= -fe;
                     lr[u][i] *= fw;
                 }
-                Ops<E>::put4(M.row.ev + at, VPL, lu[u]);
-                Ops<E>::put4(M.row.wu + at, VPL, lr[u]);
+                put_parts<SP>(M.row.ev + at, VPL, lu[u]);
+                put_parts<SP>(M.row.wu + at, VPL, lr[u]);
             }
             __syncthreads();
 #pragma unroll
@@ -285,8 +287,6 @@ template <typename E, int DKP> __global__ __launch_bounds__((GradMem<E, DKP>::NT
                     if (whole) states(f, std::true_type());
                     else states(f, std::false_type());
                 }
-                // (bfloat16: in two parts, which takes the error of dq and dk from 0.0031 of them to 0.0026, at no time)
-                constexpr int SP = P == 1 ? 2 : 3;
                 Op<SP> so[DW], uo[DW];
 #pragma unroll
                 for (int i = 0; i < DW; ++i) {
@@ -296,14 +296,18 @@ template <typename E, int DKP> __global__ __launch_bounds__((GradMem<E, DKP>::NT
 #pragma unroll
                 for (int t = 0; t < CT; ++t) {
                     const int p = (16 * t + c) * SV + at;
-                    const Op<P> bo = op_rows<P>(M.row.o + p, VPL), bv = op_rows<P>(M.row.ev + p, VPL), bu = op_rows<P>(M.row.wu + p, VPL);
+                    const Op<P> bo = op_rows<P>(M.row.o + p, VPL);
+                    const Op<SP> bv = op_rows<SP>(M.row.ev + p, VPL), bu = op_rows<SP>(M.row.wu + p, VPL);
 #pragma unroll
                     for (int y = 0; y < PAIRS<SP, P>; ++y)
 #pragma unroll
+                        for (int i = 0; i < DW; ++i) mm<SP, P>(y, held[i][t], so[i], bo);
+#pragma unroll
+                    for (int y = 0; y < PAIRS<SP, SP>; ++y)
+#pragma unroll
                         for (int i = 0; i < DW; ++i) {
-                            mm<SP, P>(y, held[i][t], so[i], bo);
-                            mm<SP, P>(y, dkk[i][t], so[i], bv);
-                            mm<SP, P>(y, dkk[i][t], uo[i], bu);
+                            mm<SP, SP>(y, dkk[i][t], so[i], bv);
+                            mm<SP, SP>(y, dkk[i][t], uo[i], bu);
                         }
                     __builtin_amdgcn_sched_barrier(0);      // (mixed, the tiles' operands take more registers than there are)
                 }
