@@ -542,7 +542,7 @@ sfda_status_t sfda_rotary_axes(const void* q, const void* k, const float* cos, c
  *   workspace : at least sfda_delta_attn_fwd_workspace_bytes(...) bytes (SFDA_ERR_SHAPE if smaller), 16-byte aligned.
  *   1 <= dk, dv <= 256; 64 tokens' rows of q, k, v and o (dO) lie within 2^31 bytes (SFDA_ERR_SHAPE otherwise).
  *   Products that reach a state are those of operands as three bfloat16 parts, to 2^-22, with sums in float32, for both types.
- *   bfloat16: the products that give o alone take the state, the scores and the writes rounded to bfloat16.
+ *   bfloat16: the products that give o alone take the state, the scores and the writes as two bfloat16 parts, to 2^-16 of each term.
  *   A token with a value that is not finite may make its whole block (32 or 64 tokens) NaN, and what follows; magnitudes past
  *   3.38e38 are taken for infinities.
  */

@@ -295,9 +295,14 @@ __device__ __forceinline__ void column(uint32_t (&x)[COUNT], const char* base, u
 
 enum Mode { FWD, RECORD, ADJOINT, STATES };      // STATES: a segment's end state alone, and what it makes of its start state
 
+// Parts of the state, of R and of P as operands of the outputs, for inputs of P parts.  A bfloat16 output's terms may cancel (keys that
+// are alike, strengths past 1), so that one part of 8 bits each leaves an error of up to 0.016 of the results; two leave their own rounding,
+// 0.0017.  The rows of R and the sums of outputs that the backward records are float32.
+template <int P, int MODE> constexpr int OUT_PARTS = MODE == FWD && P == 1 ? 2 : 3;
+
 template <typename E, int DKP, int MODE> struct Mem {
     typedef Block<E> B;
-    static constexpr int C = B::C, P = B::P, PP = MODE == FWD ? P : 3, SK = DKP + 8, ST = C + 8;
+    static constexpr int C = B::C, P = B::P, PP = OUT_PARTS<P, MODE>, SK = DKP + 8, ST = C + 8;
     static constexpr int KPL = C * SK, TPL = C * ST;        // planes
     uint16_t k[P * KPL], q[P * KPL], t[3 * TPL], p[PP * TPL];
     float e[C], w[C], beta[C], gh[C], gl[C], end[4];
@@ -312,7 +317,7 @@ template <typename E, int DKP, int MODE> __device__ __forceinline__ void scan(co
     constexpr int C = B::C, CT = B::CT, CF = B::CF, P = B::P, PP = M_::PP, TILES = B::TILES, ES = sizeof(E);
     constexpr int DT = DKP / 16, DF = DKP / 32, SK = M_::SK, ST = M_::ST, KPL = M_::KPL, TPL = M_::TPL;
     constexpr bool BACK = MODE == ADJOINT;
-    constexpr int OP = MODE == FWD ? P : 3;         // parts of the state and of R as operands of the outputs
+    constexpr int OP = PP;
     M_& M = *reinterpret_cast<M_*>(smem);
 
     const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, g = lane >> 4, w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -661,16 +666,16 @@ template <int C, bool UPPER> struct Tri {
 template <typename E, int DKP, int MODE> struct PairMem {
     typedef Block<E> B;
     static constexpr bool BACK = MODE == ADJOINT;
-    // parts of the state and of R as operands of the outputs, and of P.  bfloat16 outputs: one part each leaves an error of 0.0027 of the
-    // results (0.0017 their own rounding), P in two 0.0024
-    static constexpr int C = B::C, P = B::P, OP = MODE == FWD ? P : MODE == STATES ? 1 : 3, PP = MODE == STATES ? 1 : MODE == FWD && P == 1 ? 2 : 3;
+    static constexpr int C = B::C, P = B::P, OP = MODE == STATES ? 1 : OUT_PARTS<P, MODE>, PP = OP;
     typedef Tri<C, BACK> T;
     static constexpr int KPL = C * DKP, TPL = T::SIZE, DF = DKP / 32, DT = DKP / 16;
+    // fragments of the state that the helpers have at a time: of more than 128 bfloat16 channels one half, then the other
+    static constexpr int SF = MODE == FWD && P == 1 && DKP > 128 ? DF / 2 : DF;
     static constexpr int SV = SLICE + (sizeof(E) == 2 ? 16 : 4);
     uint16_t k[P * KPL], q[P * KPL], t[3 * TPL], p[PP * TPL];
     E v[C * SV];                // V, or dO, of the slice
     union {
-        struct { u32x4 s[NW][DF * OP][64], r[NW][B::CF * OP][64]; } fwd;        // the state and R
+        struct { u32x4 s[NW][SF * OP][64], r[NW][B::CF * OP][64]; } fwd;        // the state and R
         f32x4 add[NW][BACK ? DT : 1][64];                                       // Q^T (c e dO)
     };
     float e[C], w[C], beta[C], gh[C], gl[C], end[4];
@@ -687,7 +692,7 @@ template <typename E, int DKP, int MODE, bool chain, bool whole> __device__ __fo
     typedef typename M_::T Tr;
     typedef KeyRows<DKP> Key;
     constexpr int C = B::C, CT = B::CT, CF = B::CF, P = B::P, PP = M_::PP, OP = M_::OP, TILES = B::TILES, ES = sizeof(E);
-    constexpr int DT = DKP / 16, DF = DKP / 32, KPL = M_::KPL, TPL = M_::TPL;
+    constexpr int DT = DKP / 16, DF = DKP / 32, SF = M_::SF, KPL = M_::KPL, TPL = M_::TPL;
     constexpr bool BACK = MODE == ADJOINT;
     M_& M = *reinterpret_cast<M_*>(smem);
 
@@ -817,6 +822,12 @@ template <typename E, int DKP, int MODE, bool chain, bool whole> __device__ __fo
 #pragma unroll
         for (int f = 0; f < DF; ++f) split(f);
     }
+    auto give = [&](int first) {            // the state's fragments from `first` on to the helpers
+#pragma unroll
+        for (int f = 0; f < SF; ++f)
+#pragma unroll
+            for (int s = 0; s < OP; ++s) M.fwd.s[w][f * OP + s][lane] = __builtin_bit_cast(u32x4, s3[first + f].p[s]);
+    };
 
 #pragma clang loop unroll(disable)
     for (int it = 0; it < (BACK || MODE == STATES ? blocks : blocks + 1); ++it) {
@@ -841,12 +852,7 @@ template <typename E, int DKP, int MODE, bool chain, bool whole> __device__ __fo
 #pragma unroll
                             for (int s = 0; s < OP; ++s) M.fwd.r[w][f * OP + s][lane] = __builtin_bit_cast(u32x4, ro[f].p[s]);
                     }
-                    if (work) {
-#pragma unroll
-                        for (int f = 0; f < DF; ++f)
-#pragma unroll
-                            for (int s = 0; s < OP; ++s) M.fwd.s[w][f * OP + s][lane] = __builtin_bit_cast(u32x4, s3[f].p[s]);
-                    }
+                    if (work) give(0);
                 }
                 if constexpr (MODE == RECORD) {
                     if (work) record(L.rec_S + (head * (L.blocks + 1) + blk) * cells);
@@ -972,8 +978,13 @@ template <typename E, int DKP, int MODE, bool chain, bool whole> __device__ __fo
             if constexpr (chain) {
                 if (!work) continue;
                 if (more) fetch_keys(next);
+                if (on) held();
+                if constexpr (SF < DF) {
+                    __syncthreads();        // (the first half is read)
+                    if (on) give(SF);
+                    __syncthreads();
+                }
                 if (!on) continue;
-                held();
                 InvOp a[2];
                 inverse(a[0], 0, 0);
                 f32x4 fe[CT], fw[CT];
@@ -1118,25 +1129,33 @@ template <typename E, int DKP, int MODE, bool chain, bool whole> __device__ __fo
                             }
                         }
                     }
+                    auto times = [&](int first) {           // Q S, columns x tokens
+#pragma unroll
+                        for (int f = 0; f < SF; ++f) {
+                            Op<OP> so;
+                            Op<P> qr[CT];
+#pragma unroll
+                            for (int s = 0; s < OP; ++s) so.p[s] = __builtin_bit_cast(bf16x8, M.fwd.s[w][f * OP + s][lane]);
+#pragma unroll
+                            for (int t = 0; t < CT; ++t) qr[t] = op_rows<P>(M.q + 16 * t * DKP + (rown ^ 32 * (first + f)), KPL);
+#pragma unroll
+                            for (int i = 0; i < PAIRS<OP, P>; ++i)
+#pragma unroll
+                                for (int t = 0; t < CT; ++t) mm<OP, P>(i, x[t], so, qr[t]);
+                        }
+                    };
                     if (on) {
 #pragma unroll
                         for (int t = 0; t < CT; ++t) {
                             x[t] = zero4();
                             et[t] = L.scale * M.e[16 * t + c];
                         }
-#pragma unroll
-                        for (int f = 0; f < DF; ++f) {      // Q S, columns x tokens
-                            Op<OP> so;
-                            Op<P> qr[CT];
-#pragma unroll
-                            for (int s = 0; s < OP; ++s) so.p[s] = __builtin_bit_cast(bf16x8, M.fwd.s[w][f * OP + s][lane]);
-#pragma unroll
-                            for (int t = 0; t < CT; ++t) qr[t] = op_rows<P>(M.q + 16 * t * DKP + (rown ^ 32 * f), KPL);
-#pragma unroll
-                            for (int i = 0; i < PAIRS<OP, P>; ++i)
-#pragma unroll
-                                for (int t = 0; t < CT; ++t) mm<OP, P>(i, x[t], so, qr[t]);
-                        }
+                        times(0);
+                    }
+                    if constexpr (SF < DF) {
+                        __syncthreads();
+                        __syncthreads();    // (the second half is there)
+                        if (on) times(SF);
                     }
                 }
             }
