@@ -563,8 +563,8 @@ sfda_status_t sfda_delta_attn_fwd(const void* q, const void* k, const void* v,
  *   workspace : 16-byte aligned; with sfda_delta_attn_bwd_workspace_bytes(B, H, ...) bytes all heads run at once, with less in passes
  *          over groups of key heads, as many as fit; at least what the call takes for one, sfda_delta_attn_bwd_workspace_bytes(1,
  *          H / Hk, 1, ...) (SFDA_ERR_SHAPE if smaller).  The results do not depend on it.
- *   bfloat16: dq and dk are sums of products whose operands are rounded to one or two bfloat16 parts; dv, dlog_decay, dbeta and
- *   dS0 come from products to 2^-22.  Other arguments as the forward's.
+ *   bfloat16: dq and dk are sums of products whose operands are two bfloat16 parts, to 2^-16 of each term; dv, dlog_decay, dbeta
+ *   and dS0 come from products to 2^-22.  Other arguments as the forward's.
  */
 size_t sfda_delta_attn_bwd_workspace_bytes(int B, int H, int Hk, int T, int dk, int dv,
                                            sfda_dtype_t dtype);

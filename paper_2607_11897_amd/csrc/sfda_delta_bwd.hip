@@ -46,16 +46,16 @@ constexpr int SLAB = 64;        // value columns at a time
 template <typename E, int DKP> struct GradMem {
     typedef Block<E> B;
     static constexpr int NW = DKP == 64 ? 4 : 8, NT = 64 * NW;
-    // SP: parts of the states and of the rows that meet them in dk.  bfloat16: with all in one part dq and dk are off by 0.0031 of themselves, the
-    // states in two 0.0026, these rows too 0.0022 (0.0017 their own rounding), for 15 us of 2100
+    // SP: parts of the states, of the rows of dv and u, and of the scores.  bfloat16: two of each leave dq and dk their own rounding, 0.0017 of
+    // themselves; the rows and scores in one part 0.0022, and up to 0.016 where keys are alike and terms cancel
     static constexpr int C = B::C, P = B::P, SP = P == 1 ? 2 : 3, SK = DKP + 16, SV = SLAB + 8, ST = C + 8;
     static constexpr int KPL = C * SK, VPL = C * SV, TPL = C * ST;
     union {
         // dO, dv, u, and dv times -e, u times w: [token][value column]
-        struct { uint16_t o[P * VPL], v[P * VPL], u[P * VPL], ev[SP * VPL], wu[SP * VPL]; } row;
+        struct { uint16_t o[P * VPL], v[SP * VPL], u[SP * VPL], ev[SP * VPL], wu[SP * VPL]; } row;
         struct { uint16_t k[P * KPL], q[P * KPL]; } key;
     };
-    uint16_t w[P * TPL], m[P * TPL];                                    // c D . dO u^T, and -(M + M^T): [i][j]
+    uint16_t w[SP * TPL], m[SP * TPL];                                  // c D . dO u^T, and -(M + M^T): [i][j]
     float e[C], wt[C], beta[C], gh[C], gl[C], db[C], vd[C], dot[NW], od[NT];
 };
 
@@ -146,7 +146,7 @@ template <typename E, int DKP> __global__ __launch_bounds__((GradMem<E, DKP>::NT
         const int tid = thread();
         u32x4* z = reinterpret_cast<u32x4*>(M.w);
         const u32x4 zero = {0, 0, 0, 0};
-        for (int i = tid; i < P * TPL / 8; i += NT) z[i] = zero;
+        for (int i = tid; i < SP * TPL / 8; i += NT) z[i] = zero;
     }
 
     for (int j = 0; j < per; ++j) {
@@ -267,8 +267,8 @@ template <typename E, int DKP> __global__ __launch_bounds__((GradMem<E, DKP>::NT
                 if (r < rows && col < dv) put_four(dvp + r * L.dv_s[2], col, dv, lu[u]);
                 const int at = r * SV + 4 * (tid % (SLAB / 4));
                 Ops<E>::put4(M.row.o + at, VPL, lo[u]);
-                Ops<E>::put4(M.row.v + at, VPL, lu[u]);
-                Ops<E>::put4(M.row.u + at, VPL, lr[u]);
+                put_parts<SP>(M.row.v + at, VPL, lu[u]);
+                put_parts<SP>(M.row.u + at, VPL, lr[u]);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     lu[u][i] *= -fe;
@@ -316,14 +316,14 @@ template <typename E, int DKP> __global__ __launch_bounds__((GradMem<E, DKP>::NT
                 for (int x = 0; x < TW; ++x) {
                     const int ti = (w + NW * x) / CT, tj = (w + NW * x) % CT;
                     if (ti >= CT) break;
-                    const Op<P> uj = op_rows<P>(M.row.u + (16 * tj + c) * SV + at, VPL), vj = op_rows<P>(M.row.v + (16 * tj + c) * SV + at, VPL);
-                    const Op<P> oi = op_rows<P>(M.row.o + (16 * ti + c) * SV + at, VPL), vi = op_rows<P>(M.row.v + (16 * ti + c) * SV + at, VPL);
-                    const Op<P> ui = op_rows<P>(M.row.u + (16 * ti + c) * SV + at, VPL);
+                    const Op<SP> uj = op_rows<SP>(M.row.u + (16 * tj + c) * SV + at, VPL), vj = op_rows<SP>(M.row.v + (16 * tj + c) * SV + at, VPL);
+                    const Op<P> oi = op_rows<P>(M.row.o + (16 * ti + c) * SV + at, VPL);
+                    const Op<SP> vi = op_rows<SP>(M.row.v + (16 * ti + c) * SV + at, VPL), ui = op_rows<SP>(M.row.u + (16 * ti + c) * SV + at, VPL);
 #pragma unroll
-                    for (int y = 0; y < PAIRS<P, P>; ++y) {
-                        if (ti >= tj) mm<P, P>(y, ws[x], uj, oi);
-                        if (ti >= tj) mm<P, P>(y, ms[x], uj, vi);
-                        if (ti <= tj) mm<P, P>(y, md[x], vj, ui);
+                    for (int y = 0; y < PAIRS<SP, SP>; ++y) {
+                        if (ti >= tj && y < PAIRS<SP, P>) mm<SP, P>(y, ws[x], uj, oi);
+                        if (ti >= tj) mm<SP, SP>(y, ms[x], uj, vi);
+                        if (ti <= tj) mm<SP, SP>(y, md[x], vj, ui);
                     }
                     __builtin_amdgcn_sched_barrier(0);
                 }
@@ -348,8 +348,8 @@ template <typename E, int DKP> __global__ __launch_bounds__((GradMem<E, DKP>::NT
                 a[r] = masked(jj <= i, ws[x][r] * (L.scale * down[r]));
                 m[r] = masked(jj != i, -(jj < i ? ms[x][r] * down[r] : md[x][r] * up[r]));
             }
-            if (ti >= tj) Ops<E>::put4(M.w + i * ST + 16 * tj + 4 * g, TPL, a);
-            Ops<E>::put4(M.m + i * ST + 16 * tj + 4 * g, TPL, m);
+            if (ti >= tj) put_parts<SP>(M.w + i * ST + 16 * tj + 4 * g, TPL, a);
+            put_parts<SP>(M.m + i * ST + 16 * tj + 4 * g, TPL, m);
         }
         // sums of the tokens' rows over their 16 threads, and of S' . U over all
 #pragma unroll
@@ -408,24 +408,24 @@ template <typename E, int DKP> __global__ __launch_bounds__((GradMem<E, DKP>::NT
             }
 #pragma unroll
             for (int t = 0; t < CT; ++t) {
-                const Op<P> mt = op_rows<P>(M.m + (16 * t + c) * ST + 32 * f + 8 * g, TPL);
+                const Op<SP> mt = op_rows<SP>(M.m + (16 * t + c) * ST + 32 * f + 8 * g, TPL);
 #pragma unroll
-                for (int x = 0; x < PAIRS<P, P>; ++x)
+                for (int x = 0; x < PAIRS<P, SP>; ++x)
 #pragma unroll
-                    for (int i = 0; i < DW; ++i) mm<P, P>(x, dkk[i][t], kc[i], mt);
+                    for (int i = 0; i < DW; ++i) mm<P, SP>(x, dkk[i][t], kc[i], mt);
                 if (f <= t / 2) {
-                    const Op<P> wt = op_rows<P>(M.w + (16 * t + c) * ST + 32 * f + 8 * g, TPL);
+                    const Op<SP> wt = op_rows<SP>(M.w + (16 * t + c) * ST + 32 * f + 8 * g, TPL);
 #pragma unroll
-                    for (int x = 0; x < PAIRS<P, P>; ++x)
+                    for (int x = 0; x < PAIRS<P, SP>; ++x)
 #pragma unroll
-                        for (int i = 0; i < DW; ++i) mm<P, P>(x, dq[i][t], kc[i], wt);
+                        for (int i = 0; i < DW; ++i) mm<P, SP>(x, dq[i][t], kc[i], wt);
                 }
                 if (f >= t / 2) {
-                    const Op<P> wt = op_cols<P>(M.w + (32 * f + 8 * g + (c >> 2)) * ST + 16 * t + 4 * (c & 3), ST, TPL);
+                    const Op<SP> wt = op_cols<SP>(M.w + (32 * f + 8 * g + (c >> 2)) * ST + 16 * t + 4 * (c & 3), ST, TPL);
 #pragma unroll
-                    for (int x = 0; x < PAIRS<P, P>; ++x)
+                    for (int x = 0; x < PAIRS<P, SP>; ++x)
 #pragma unroll
-                        for (int i = 0; i < DW; ++i) mm<P, P>(x, dkk[i][t], qc[i], wt);
+                        for (int i = 0; i < DW; ++i) mm<P, SP>(x, dkk[i][t], qc[i], wt);
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }

@@ -16,7 +16,7 @@ import pytest
 
 from gpu_util import ensure_built, rel_err
 from oracle import delta as O
-from test_gpu_delta import names, run_fwd, say, stored_as
+from test_gpu_delta import names, run_bwd, run_fwd, say, stored_as
 from test_gpu_layer import stored
 
 pytestmark = pytest.mark.gpu
@@ -46,6 +46,8 @@ def alike(seed, B, H, Hk, T, dk, dv, dtype, cosine, low, high, state, decay=0.0)
     for n in ("log_decay", "beta"):
         x[n] = x[n].astype(np.float32).astype(np.float64)
     x["S0"] = stored(rng, (B, H, dk, dv), "f32") if state else None
+    x["dO"] = stored(rng, (B, H, T, dv), dtype)
+    x["dS_T"] = stored(rng, (B, H, dk, dv), "f32") if state else None
     x["lengths"] = None
     return x
 
@@ -80,6 +82,19 @@ def test_fwd_of_keys_that_are_alike(B, H, Hk, T, dk, dv, state, cosine, low, hig
     o, S = run_fwd(x, dtype, "bthd", scale)
     ro, rS = O.delta_attn(**names(x), scale=scale)
     good = [close("o", o, ro, dtype, True), close("S_T", S, rS, dtype, False)]
+    assert all(good)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("cosine,low,high,decay", KEYS)
+@pytest.mark.parametrize("B,H,Hk,T,dk,dv,state", SIZES)
+def test_bwd_of_keys_that_are_alike(B, H, Hk, T, dk, dv, state, cosine, low, high, decay, dtype):
+    say("alike bwd", B, H, Hk, T, dk, dv, state, cosine, low, high, decay, dtype)
+    x = alike(T + dk, B, H, Hk, T, dk, dv, dtype, cosine, low, high, state, decay)
+    scale = dk ** -0.5
+    got = run_bwd(x, dtype, "bthd", scale)
+    ref = O.delta_attn_backward(**names(x, "dO", "dS_T"), scale=scale)
+    good = [close(n, got[n], y, dtype, n in ("dq", "dk", "dv")) for n, y in ref.items()]
     assert all(good)
 
 
