@@ -560,9 +560,11 @@ sfda_status_t sfda_delta_attn_fwd(const void* q, const void* k, const void* v,
  *   dq, dk [B, Hk, T, dk] (sums over the value heads that share a key head), dv [B, H, T, dv] as the inputs' type; dlog_decay, dbeta
  *          [B, H, T] float32; zero past a sequence's length.  dS0 [B, H, dk, dv] float32 or NULL.
  *   strides: (b, h, t) of q, k, v, log_decay, beta, dO, dq, dk, dv, dlog_decay, dbeta.
- *   workspace : 16-byte aligned; with sfda_delta_attn_bwd_workspace_bytes(B, H, ...) bytes all heads run at once, with less in passes
- *          over groups of key heads, as many as fit; at least what the call takes for one, sfda_delta_attn_bwd_workspace_bytes(1,
- *          H / Hk, 1, ...) (SFDA_ERR_SHAPE if smaller).  The results do not depend on it.
+ *   workspace : 16-byte aligned; with sfda_delta_attn_bwd_workspace_bytes(B, H, ...) bytes all heads run at once, or as many as a
+ *          launch takes, with less in passes over groups of key heads, as many as fit; at least what the call takes for one,
+ *          sfda_delta_attn_bwd_workspace_bytes(1, H / Hk, 1, ...) (SFDA_ERR_SHAPE if smaller).  The results do not depend on it.
+ *   A launch takes (2^23 - 1) / (blocks + 32) value heads, blocks of 64 tokens in bfloat16 and 32 in float32; those of a key head have
+ *   to be in one (SFDA_ERR_SHAPE and a size of 0 otherwise).
  *   bfloat16: dq and dk are sums of products whose operands are two bfloat16 parts, to 2^-16 of each term; dv, dlog_decay, dbeta
  *   and dS0 come from products to 2^-22.  Other arguments as the forward's.
  */

@@ -665,9 +665,9 @@ static bool delta_sizes(int B, int H, int Hk, int T, int dk, int dv)
 {
     return Hk >= 0 && (H == 0 || (Hk > 0 && H > 0 && H % Hk == 0)) && decay_sizes(B, H, T, dk, dv);
 }
-// blocks of a sequence; heads times them stay below 2^31, launches below 2^32 threads
 static ll delta_blocks(int T, bool bf16) { return (static_cast<ll>(T) + sfda::delta_block(bf16) - 1) / sfda::delta_block(bf16); }
-static bool delta_launches(ll heads, ll blocks, int dv) { return heads * std::max(blocks + 32, (dv + 63LL) / 64 * 2) < (1LL << 32) / 512; }
+// heads of a launch, whose threads (512 for a head and block, of 32 blocks and more) stay below 2^32; a call of more heads is several
+static ll delta_heads(ll blocks) { return ((1LL << 32) / 512 - 1) / (blocks + 32); }
 
 // the forward's part of a workspace for `heads` value heads: inverses, scores and scalars
 static ll delta_prep_bytes(ll heads, ll blocks, bool bf16, int scans)
@@ -723,7 +723,7 @@ sfda_status_t sfda_delta_attn_fwd(const void* q, const void* k, const void* v, c
     const bool bf16 = dtype == SFDA_BF16;
     if (heads == 0) return SFDA_OK;
     const ll blocks = delta_blocks(T, bf16);
-    if (!delta_launches(heads, blocks, dv)) return SFDA_ERR_SHAPE;
+    if (heads > delta_heads(blocks)) return SFDA_ERR_SHAPE;
     sfda::DeltaLaunch L{};
     strides3(L.q_s, strides, 0, B, Hk, T, dk);
     strides3(L.k_s, strides, 1, B, Hk, T, dk);
@@ -775,7 +775,10 @@ size_t sfda_delta_attn_bwd_workspace_bytes(int B, int H, int Hk, int T, int dk, 
 {
     if (!dtype_ok(dtype) || !delta_sizes(B, H, Hk, T, dk, dv)) return 0;
     const bool bf16 = dtype == SFDA_BF16;
-    return static_cast<size_t>(delta_bwd_bytes(static_cast<ll>(B) * H, delta_blocks(T, bf16), dk, dv, bf16));
+    const ll blocks = delta_blocks(T, bf16);
+    if (B == 0 || H == 0) return static_cast<size_t>(delta_bwd_bytes(0, blocks, dk, dv, bf16));
+    const ll most = std::min(delta_heads(blocks) / (H / Hk), static_cast<ll>(B) * Hk);       // (key heads)
+    return most < 1 ? 0 : static_cast<size_t>(delta_bwd_bytes(most * (H / Hk), blocks, dk, dv, bf16));
 }
 
 sfda_status_t sfda_delta_attn_bwd(const void* q, const void* k, const void* v, const float* log_decay, const float* beta,
@@ -789,8 +792,8 @@ sfda_status_t sfda_delta_attn_bwd(const void* q, const void* k, const void* v, c
     const ll heads = static_cast<ll>(B) * H, e = esize(dtype), state = heads * dk * dv * 4;
     const bool bf16 = dtype == SFDA_BF16;
     if (heads == 0) return SFDA_OK;
-    const ll blocks = delta_blocks(T, bf16);
-    if (!delta_launches(heads, blocks, dv)) return SFDA_ERR_SHAPE;
+    const ll blocks = delta_blocks(T, bf16), per = H / Hk, groups = static_cast<ll>(B) * Hk, most = std::min(delta_heads(blocks) / per, groups);
+    if (most < 1) return SFDA_ERR_SHAPE;
     sfda::DeltaLaunch L{};
     strides3(L.q_s, strides, 0, B, Hk, T, dk);
     strides3(L.k_s, strides, 1, B, Hk, T, dk);
@@ -805,10 +808,10 @@ sfda_status_t sfda_delta_attn_bwd(const void* q, const void* k, const void* v, c
     strides3(L.db_s, strides, 10, B, H, T, 1);
     if (!rows_fit(L.q_s, e) || !rows_fit(L.k_s, e) || !rows_fit(L.v_s, e) || !rows_fit(L.g_s, e)) return SFDA_ERR_SHAPE;
     // key heads of a pass
-    const ll per = H / Hk, one = delta_bwd_bytes(per, blocks, dk, dv, bf16), groups = static_cast<ll>(B) * Hk;
-    ll fit = groups;
-    if (workspace_bytes < static_cast<size_t>(delta_bwd_bytes(heads, blocks, dk, dv, bf16)))
-        fit = static_cast<ll>(std::min<size_t>(workspace_bytes / static_cast<size_t>(one), static_cast<size_t>(groups)));
+    const ll one = delta_bwd_bytes(per, blocks, dk, dv, bf16);
+    ll fit = most;
+    if (workspace_bytes < static_cast<size_t>(delta_bwd_bytes(most * per, blocks, dk, dv, bf16)))
+        fit = static_cast<ll>(std::min<size_t>(workspace_bytes / static_cast<size_t>(one), static_cast<size_t>(most)));
     const ll used = delta_bwd_bytes(std::max(fit, 1LL) * per, blocks, dk, dv, bf16);
     Call c;
     c.input(box(q, e, dk, {B, Hk, T}, L.q_s), e);
@@ -862,8 +865,7 @@ sfda_status_t sfda_delta_attn_step(const void* q, const void* k, const void* v, 
     if (!delta_sizes(B, H, Hk, 1, dk, dv)) return SFDA_ERR_SHAPE;
     const ll heads = static_cast<ll>(B) * H, e = esize(dtype);
     if (heads == 0) return SFDA_OK;
-    if (!delta_launches(heads, 0, dv)) return SFDA_ERR_SHAPE;
-    sfda::DeltaStepLaunch L{};
+    sfda::DeltaStepLaunch L{};              // (4 workgroups of 256 threads for a head at most: less than 2^32 threads)
     ll (*to[6])[2] = {&L.q_s, &L.k_s, &L.v_s, &L.l_s, &L.b_s, &L.o_s};
     for (int i = 0; i < 6; ++i) {
         const ll D = i < 2 ? dk : i == 3 || i == 4 ? 1 : dv, n = i < 2 ? Hk : H;

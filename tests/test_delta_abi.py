@@ -102,6 +102,20 @@ def test_workspaces(lib):
     assert g(2, 5, 16, 0) >= 2 * 16 * 4 and g(2, 5, 16385, 0) == 0 and g(2, 5, 16, 9) == 0 and g(0, 5, 16, 0) > 0
 
 
+def test_more_heads_than_a_launch_takes(lib):
+    """262144 heads: what is refused is the missing pointer behind the sizes.  A head that no launch takes is refused for its length,
+    and its workspace, which 64 bits do not count, is 0."""
+    z = ctypes.c_void_p(None)
+    assert lib.sfda_delta_attn_step(z, 2 * A, 3 * A, 4 * A, 5 * A, 6 * A, 7 * A, 8192, 32, 32, 4, 4, 1.0, None, 0, None) == 1
+    many = dict(B=8192, H=32, Hk=32, T=64, dk=4, dv=4, q=None)
+    assert bwd(lib, **many) == 1 and bwd(lib, **(many | dict(H=64, Hk=1))) == 1
+    assert bwd(lib, B=1, H=600000, Hk=1, T=64, dk=4, dv=4, q=None) == 2
+    b = lib.sfda_delta_attn_bwd_workspace_bytes
+    for Hk in (1, 600000):
+        assert b(1, 600000, Hk, (1 << 31) - 1025, 256, 256, 0) == 0
+    assert b(8192, 32, 32, 64, 4, 4, 1) >= 200000 * b(1, 1, 1, 64, 4, 4, 1) - (200000 << 6)
+
+
 def norm(lib, **kw):
     a = dict(x=A, w=2 * A, b=3 * A, r=4 * A, y=5 * A, t=6 * A, B=1, T=8, D=16, eps=1e-5, strides=None, dt=0) | kw
     return lib.sfda_layer_norm(*(a[x] for x in ("x", "w", "b", "r", "y", "t", "B", "T", "D")), a["eps"], a["strides"], a["dt"], None)

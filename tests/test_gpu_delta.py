@@ -575,3 +575,28 @@ def test_offsets_past_32_bits():
     r = sfda.layer_norm_bwd(rows, t, w, None, more)
     f = sfda.layer_norm_bwd(spread(0, None, 200), tf, w, None, spread(1, None, 200), dx=spread(4, None, 200))
     assert r["dx"].equal(f["dx"]) and r["dweight"].equal(f["dweight"])
+
+
+def test_more_heads_than_a_launch_takes():
+    """8193 sequences of 32 heads: the results of each half of the sequences, bit by bit, and the recurrence's for the last ones."""
+    import torch
+    from paper_2607_11897_amd import sfda
+    say("many sequences")
+    B, H, T, dk, dv = 8193, 32, 3, 5, 4
+    x = attn(21, B, H, H, T, dk, dv, "f32", grads=True)
+    q, k, v, g, be, S0, dO, dS = (f32(x[n]) for n in ("q", "k", "v", "log_decay", "beta", "S0", "dO", "dS_T"))
+    last = {n: None if x[n] is None else x[n][-2:] for n in x}
+    halves = (slice(0, B // 2), slice(B // 2, B))
+    S, parts = S0.clone(), [S0[h].clone() for h in halves]
+    for t in range(T):
+        o = sfda.delta_attn_step(q[:, :, t], k[:, :, t], v[:, :, t], g[:, :, t], be[:, :, t], S)
+        for h, p in zip(halves, parts):
+            assert torch.equal(o[h], sfda.delta_attn_step(q[h, :, t], k[h, :, t], v[h, :, t], g[h, :, t], be[h, :, t], p))
+    assert torch.equal(S, torch.cat(parts))
+    assert rel_err(S[-2:].double().cpu().numpy(), O.delta_attn(**names(last))[1]) <= SUM
+    got = sfda.delta_attn_bwd(q, k, v, g, be, S0, dO, dS)
+    for h in halves:
+        half = sfda.delta_attn_bwd(*(t[h] for t in (q, k, v, g, be, S0, dO, dS)))
+        for n in got:
+            assert torch.equal(got[n][h], half[n]), n
+    check_bwd({n: y[-2:].double().cpu().numpy() for n, y in got.items()}, O.delta_attn_backward(**names(last, "dO", "dS_T")), "f32")
