@@ -539,7 +539,11 @@ sfda_status_t sfda_rotary_axes(const void* q, const void* k, const float* cos, c
  *   lengths : [B] int32 or NULL.  Sequence b has min(max(lengths[b], 0), T) tokens; what the tensors hold past them is not used, o is
  *          0 there and S_T is the state after the last token (S0 at length 0).
  *   S0, S_T : [B, H, dk, dv] contiguous float32, each may be NULL (zero state; not wanted).  S_T == S0 is allowed.
- *   workspace : at least sfda_delta_attn_fwd_workspace_bytes(...) bytes (SFDA_ERR_SHAPE if smaller), 16-byte aligned.
+ *   workspace : 16-byte aligned; with sfda_delta_attn_fwd_workspace_bytes(...) bytes all heads run at once, or as many as a launch
+ *          takes, with less in passes over them, as many as fit; at least those bytes / (B H), one head's (SFDA_ERR_SHAPE if
+ *          smaller).  The results do not depend on it.  Some 512 bytes for each token and value head, whatever dk and dv.
+ *   A launch takes (2^23 - 1) / (blocks + 32) value heads, blocks of 64 tokens in bfloat16 and 32 in float32 (SFDA_ERR_SHAPE if
+ *   that is none).
  *   1 <= dk, dv <= 256; 64 tokens' rows of q, k, v and o (dO) lie within 2^31 bytes (SFDA_ERR_SHAPE otherwise).
  *   Products that reach a state are those of operands as three bfloat16 parts, to 2^-22, with sums in float32, for both types.
  *   bfloat16: the products that give o alone take the state, the scores and the writes as two bfloat16 parts, to 2^-16 of each term.
@@ -563,8 +567,7 @@ sfda_status_t sfda_delta_attn_fwd(const void* q, const void* k, const void* v,
  *   workspace : 16-byte aligned; with sfda_delta_attn_bwd_workspace_bytes(B, H, ...) bytes all heads run at once, or as many as a
  *          launch takes, with less in passes over groups of key heads, as many as fit; at least what the call takes for one,
  *          sfda_delta_attn_bwd_workspace_bytes(1, H / Hk, 1, ...) (SFDA_ERR_SHAPE if smaller).  The results do not depend on it.
- *   A launch takes (2^23 - 1) / (blocks + 32) value heads, blocks of 64 tokens in bfloat16 and 32 in float32; those of a key head have
- *   to be in one (SFDA_ERR_SHAPE and a size of 0 otherwise).
+ *   The value heads of a key head have to be in one launch (SFDA_ERR_SHAPE and a size of 0 otherwise).
  *   bfloat16: dq and dk are sums of products whose operands are two bfloat16 parts, to 2^-16 of each term; dv, dlog_decay, dbeta
  *   and dS0 come from products to 2^-22.  Other arguments as the forward's.
  */

@@ -698,9 +698,10 @@ DeltaCut delta_cut(ll heads, ll blocks, int dk, int dv, bool bf16)
     }
     return best;
 }
-ll delta_segment_bytes(ll heads, int segments, int dk, int dv)
+// the forward's workspace for `heads` value heads (so many times one head's)
+ll delta_fwd_bytes(ll heads, ll blocks, int segments, int dk, int dv, bool bf16)
 {
-    return segments == 1 ? 0 : heads * dk * 4 * ((segments - 1) * (static_cast<ll>(dk) + dv) + dv);
+    return delta_prep_bytes(heads, blocks, bf16, 1) + (segments == 1 ? 0 : heads * dk * 4 * ((segments - 1) * (static_cast<ll>(dk) + dv) + dv));
 }
 
 size_t sfda_delta_attn_fwd_workspace_bytes(int B, int H, int T, int dk, int dv, sfda_dtype_t dtype)
@@ -709,7 +710,7 @@ size_t sfda_delta_attn_fwd_workspace_bytes(int B, int H, int T, int dk, int dv, 
     const bool bf16 = dtype == SFDA_BF16;
     const ll heads = static_cast<ll>(B) * H, blocks = delta_blocks(T, bf16);
     if (heads == 0) return 0;
-    return static_cast<size_t>(delta_prep_bytes(heads, blocks, bf16, 1) + delta_segment_bytes(heads, delta_cut(heads, blocks, dk, dv, bf16).segments, dk, dv));
+    return static_cast<size_t>(delta_fwd_bytes(heads, blocks, delta_cut(heads, blocks, dk, dv, bf16).segments, dk, dv, bf16));
 }
 
 sfda_status_t sfda_delta_attn_fwd(const void* q, const void* k, const void* v, const float* log_decay, const float* beta,
@@ -722,8 +723,8 @@ sfda_status_t sfda_delta_attn_fwd(const void* q, const void* k, const void* v, c
     const ll heads = static_cast<ll>(B) * H, e = esize(dtype), state = heads * dk * dv * 4;
     const bool bf16 = dtype == SFDA_BF16;
     if (heads == 0) return SFDA_OK;
-    const ll blocks = delta_blocks(T, bf16);
-    if (heads > delta_heads(blocks)) return SFDA_ERR_SHAPE;
+    const ll blocks = delta_blocks(T, bf16), most = std::min(delta_heads(blocks), heads);
+    if (most < 1) return SFDA_ERR_SHAPE;
     sfda::DeltaLaunch L{};
     strides3(L.q_s, strides, 0, B, Hk, T, dk);
     strides3(L.k_s, strides, 1, B, Hk, T, dk);
@@ -732,7 +733,11 @@ sfda_status_t sfda_delta_attn_fwd(const void* q, const void* k, const void* v, c
     strides3(L.b_s, strides, 4, B, H, T, 1);
     strides3(L.o_s, strides, 5, B, H, T, dv);
     if (!rows_fit(L.q_s, e) || !rows_fit(L.k_s, e) || !rows_fit(L.v_s, e) || !rows_fit(L.o_s, e)) return SFDA_ERR_SHAPE;
-    const size_t need = sfda_delta_attn_fwd_workspace_bytes(B, H, T, dk, dv, dtype);
+    // the segments are those of all heads, whatever a pass holds, so that the results are the same
+    const DeltaCut cut = delta_cut(heads, blocks, dk, dv, bf16);
+    const ll one = delta_fwd_bytes(1, blocks, cut.segments, dk, dv, bf16);
+    const ll fit = workspace_bytes < static_cast<size_t>(most * one) ? static_cast<ll>(workspace_bytes / static_cast<size_t>(one)) : most;  // heads of a pass
+    const ll need = std::max(fit, 1LL) * one;
     Call c;
     c.input(box(q, e, dk, {B, Hk, T}, L.q_s), e);
     c.input(box(k, e, dk, {B, Hk, T}, L.k_s), e);
@@ -743,25 +748,27 @@ sfda_status_t sfda_delta_attn_fwd(const void* q, const void* k, const void* v, c
     const int s0 = c.input(flat(S0, state), 4, false);
     c.output(box(o, e, dv, {B, H, T}, L.o_s), e);
     c.output(flat(S_T, state), 4, false, s0);
-    if (need > 0) c.output(flat(workspace, static_cast<ll>(need)), 16);
+    if (need > 0) c.output(flat(workspace, need), 16);
     sfda_status_t st = c.done();
-    if (st == SFDA_OK && workspace_bytes < need) st = SFDA_ERR_SHAPE;
+    if (st == SFDA_OK && fit < 1) st = SFDA_ERR_SHAPE;
     if (st != SFDA_OK) return st;
     L.q = q; L.k = k; L.v = v; L.log_decay = log_decay; L.beta = beta; L.lengths = lengths; L.S0 = S0; L.o = o; L.S_T = S_T;
     L.B = B; L.H = H; L.Hk = Hk; L.T = T; L.dk = dk; L.dv = dv; L.scale = scale; L.bf16 = bf16;
-    L.heads = static_cast<int>(heads); L.blocks = static_cast<int>(blocks);
-    const ll matrices = heads * blocks * sfda::delta_tiles(bf16) * 768;
-    L.inv = static_cast<uint16_t*>(workspace);
-    L.scores = L.inv + matrices;
-    L.scalars = reinterpret_cast<float4*>(L.scores + matrices);
-    L.score_parts = bf16 ? 2 : 3;
-    const DeltaCut cut = delta_cut(heads, blocks, dk, dv, bf16);
+    L.blocks = static_cast<int>(blocks); L.score_parts = bf16 ? 2 : 3;
     L.segments = cut.segments; L.seg_blocks = cut.blocks;
-    L.seg_N = reinterpret_cast<float*>(L.scalars + 2 * heads * blocks * sfda::delta_block(bf16));
-    L.seg_M = L.seg_N + heads * cut.segments * dk * dv;
     L.whole = dv % 4 == 0 && reinterpret_cast<uintptr_t>(o) % 4 == 0;
     for (ll st : L.o_s) L.whole = L.whole && st * e % 4 == 0;
-    return sfda::launch_delta_fwd(L, static_cast<hipStream_t>(stream)) == hipSuccess ? SFDA_OK : SFDA_ERR_HIP;
+    for (ll first = 0; first < heads; first += fit) {
+        const ll n = std::min(fit, heads - first), matrices = n * blocks * sfda::delta_tiles(bf16) * 768;
+        L.first = first; L.heads = static_cast<int>(n);
+        L.inv = static_cast<uint16_t*>(workspace);
+        L.scores = L.inv + matrices;
+        L.scalars = reinterpret_cast<float4*>(L.scores + matrices);
+        L.seg_N = reinterpret_cast<float*>(L.scalars + 2 * n * blocks * sfda::delta_block(bf16));
+        L.seg_M = L.seg_N + n * cut.segments * dk * dv;
+        if (sfda::launch_delta_fwd(L, static_cast<hipStream_t>(stream)) != hipSuccess) return SFDA_ERR_HIP;
+    }
+    return SFDA_OK;
 }
 
 // what one key head's value heads take: both inverses, the states and their gradients, the rows of R and du, the outputs' parts

@@ -908,8 +908,9 @@ def delta_attn_fwd(q, k, v, log_decay, beta, S0=None, *, scale: float = 1.0, len
     S_t = a_t S_(t-1) + k_t u_t^T, u_t = beta_t (v_t - a_t S_(t-1)^T k_t), o_t = scale S_t^T q_t.  q, k: [B,Hk,T,dk]; v: [B,H,T,dv]
     (float32 or bfloat16, any strides with a contiguous last axis: a [B,T,H,D] projection is passed as its transpose(1, 2));
     H a multiple of Hk; log_decay, beta: [B,H,T] float32 of any strides; S0: [B,H,dk,dv] float32 or None; lengths: [B] int32 or
-    None (all T).  Returns (o [B,H,T,dv], S_T [B,H,dk,dv] float32 or None).  `workspace`: a uint8 device tensor of at least
-    delta_attn_fwd_workspace_bytes(...) bytes, allocated here if it is None."""
+    None (all T).  Returns (o [B,H,T,dv], S_T [B,H,dk,dv] float32 or None).  `workspace`: a uint8 device tensor; with
+    delta_attn_fwd_workspace_bytes(...) bytes all heads run at once, with less (one head's at least, a B H-th) in passes over them, with
+    the same results.  If it is None it is allocated here, as much as the device has room for."""
     import torch
     lib = load_library()
     if q.dim() != 4 or v.dim() != 4:
@@ -929,7 +930,11 @@ def delta_attn_fwd(q, k, v, log_decay, beta, S0=None, *, scale: float = 1.0, len
          ("S0", S0, ts), ("o", o, tv), ("S_T", S_T, ts), ("workspace", workspace, workspace.shape if workspace is not None else ()))
     if workspace is None:
         nws = lib.sfda_delta_attn_fwd_workspace_bytes(B, H, T, dk, dv, code)
-        workspace = _workspace(nws, q.device, stream) if nws else None
+        n = B * H                       # heads of a pass
+        while nws and workspace is None:
+            part = nws // (B * H) * n
+            workspace = _try_workspace(part, q.device, stream) if n > 1 else _workspace(part, q.device, stream)
+            n = (n + 3) // 4
     st = lib.sfda_delta_attn_fwd(_rows(q), _rows(k), _rows(v), _scalars(log_decay), _scalars(beta), _ptr(lengths), _ptr(S0), _rows(o),
                                  _ptr(S_T), B, H, Hk, T, dk, dv, scale, _strides(3, q, k, v, log_decay, beta, o), code,
                                  _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
@@ -983,7 +988,8 @@ def delta_attn_bwd(q, k, v, log_decay, beta, S0, dO, dS_T=None, *, scale: float 
 
 
 def delta_attn_fwd_workspace_bytes(B: int, H: int, T: int, dk: int, dv: int, dtype: str = "f32") -> int:
-    """The workspace of delta_attn_fwd; dtype: the activations' ("f32" or "bf16")."""
+    """The workspace at which delta_attn_fwd runs all heads at once; the least is a B H-th of it.  dtype: the activations' ("f32" or
+    "bf16")."""
     code = {"f32": SFDA_F32, "bf16": SFDA_BF16}[dtype]
     return int(load_library().sfda_delta_attn_fwd_workspace_bytes(B, H, T, dk, dv, code))
 

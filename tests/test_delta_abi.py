@@ -113,6 +113,11 @@ def test_more_heads_than_a_launch_takes(lib):
     b = lib.sfda_delta_attn_bwd_workspace_bytes
     for Hk in (1, 600000):
         assert b(1, 600000, Hk, (1 << 31) - 1025, 256, 256, 0) == 0
+    # forward: passes over as many heads as a launch takes, or as the workspace holds
+    assert fwd(lib, **(many | dict(nws=1 << 40))) == 1 and fwd(lib, B=1, H=600000, Hk=1, T=64, dk=4, dv=4, q=None) == 1
+    assert fwd(lib, T=(1 << 31) - 1025, nws=1 << 60, q=None) == 2
+    one = lib.sfda_delta_attn_fwd_workspace_bytes(1, 4, 8, 16, 8, 0) // 4
+    assert fwd(lib, nws=one - 1) == 2 and fwd(lib, nws=one, q=None) == 1
     assert b(8192, 32, 32, 64, 4, 4, 1) >= 200000 * b(1, 1, 1, 64, 4, 4, 1) - (200000 << 6)
 
 

@@ -600,3 +600,41 @@ def test_more_heads_than_a_launch_takes():
         for n in got:
             assert torch.equal(got[n][h], half[n]), n
     check_bwd({n: y[-2:].double().cpu().numpy() for n, y in got.items()}, O.delta_attn_backward(**names(last, "dO", "dS_T")), "f32")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,H,Hk,T,dk,dv,lengths", [(2, 6, 3, 100, 33, 70, None), (2, 3, 1, 2500, 64, 64, [3, 2499]), (1, 2, 1, 0, 8, 8, None)])
+def test_fwd_in_passes(dtype, B, H, Hk, T, dk, dv, lengths):
+    """Groups of heads, as many as the workspace holds, in segments too and with S_T in S0's memory: the same results, bit by bit."""
+    import torch
+    from paper_2607_11897_amd import sfda
+    say("fwd passes", dtype, T)
+    x = attn(4, B, H, Hk, T, dk, dv, dtype, True, lengths)
+    o, S = run_fwd(x, dtype, "bthd", 0.3)
+    whole = sfda.delta_attn_fwd_workspace_bytes(B, H, T, dk, dv, dtype)
+    one = whole // (B * H)
+    assert whole == one * B * H and (T < 1000) == (one == sfda.delta_attn_fwd_workspace_bytes(B, 4096, T, dk, dv, dtype) // (4096 * B))
+    for n in (1, 2, 5):
+        again = run_fwd(x, dtype, "bthd", 0.3, workspace=torch.full((n * one + 15,), 255, dtype=torch.uint8, device="cuda"))
+        assert np.array_equal(again[0], o) and np.array_equal(again[1], S), n
+    if T > 0:
+        with pytest.raises(sfda.SfdaError, match="SHAPE"):
+            run_fwd(x, dtype, "bthd", 0.3, workspace=torch.empty(one - 16, dtype=torch.uint8, device="cuda"))
+        t = [dev(x[n]).to(dt(dtype)) for n in "qkv"] + [f32(x[n]) for n in ("log_decay", "beta", "S0")]
+        room = torch.empty(2 * one, dtype=torch.uint8, device="cuda")
+        o2, S2 = sfda.delta_attn_fwd(*t, scale=0.3, lengths=dev(x["lengths"]), S_T=t[-1], workspace=room)
+        assert np.array_equal(o2.double().cpu().numpy(), o) and np.array_equal(t[-1].double().cpu().numpy(), S) and S2 is t[-1]
+
+
+def test_fwd_of_more_heads_than_a_launch_takes():
+    """8193 sequences of 32 heads: the results of each half of the sequences, bit by bit."""
+    import torch
+    from paper_2607_11897_amd import sfda
+    say("many sequences forward")
+    B, H, T, dk, dv = 8193, 32, 3, 5, 4
+    x = attn(22, B, H, H, T, dk, dv, "f32")
+    t = [f32(x[n]) for n in ("q", "k", "v", "log_decay", "beta", "S0")]
+    o, S = sfda.delta_attn_fwd(*t)
+    for h in (slice(0, B // 2), slice(B // 2, B)):
+        for a, b in zip((o, S), sfda.delta_attn_fwd(*(y[h] for y in t))):
+            assert torch.equal(a[h], b)
