@@ -686,7 +686,8 @@ DeltaCut delta_cut(ll heads, ll blocks, int dk, int dv, bool bf16)
     if (!sfda::delta_segments(bf16, dk) || blocks < 4) return best;
     const ll sv = (dv + 63) / 64, sm = (dk + 63) / 64;
     const double step = bf16 ? 4.4 : 1.9, states = bf16 ? 2.9 : 1.4, join = 4.5, launches = 35.;
-    auto rounds = [](ll groups) { return static_cast<double>((groups + cus() - 1) / cus()); };
+    const ll units = cus();
+    auto rounds = [&](ll groups) { return static_cast<double>((groups + units - 1) / units); };
     double least = 0.9 * rounds(heads * sv) * blocks * step;
     for (ll s = 2; s <= 64 && 2 * s <= blocks; ++s) {
         const ll each = (blocks + s - 1) / s, segs = (blocks + each - 1) / each;
