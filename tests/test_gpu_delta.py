@@ -638,3 +638,39 @@ def test_fwd_of_more_heads_than_a_launch_takes():
     for h in (slice(0, B // 2), slice(B // 2, B)):
         for a, b in zip((o, S), sfda.delta_attn_fwd(*(y[h] for y in t))):
             assert torch.equal(a[h], b)
+
+
+def directions(y, gen):
+    """Six of them, of entries of size 1: a derivative along one is of the gradient's norm, and an input's gradient that were zero, or off by a
+    third, would stand out along all but a hundredth of them."""
+    import torch
+    return [torch.randn(y.shape, generator=gen, device=y.device) for _ in range(6)]
+
+
+@pytest.mark.parametrize("H,Hk", [(2, 1), (3, 3)])
+def test_bwd_against_differences_along_many_directions(H, Hk):
+    """float32 gradients against central differences, each bar in units of what is compared.  The loss is linear in q, v and S0: with
+    steps of 1 a difference is off by the forward's rounding alone, 2^-22 in sums of a few thousand terms: 1e-3 of the gradient.  Keys,
+    decays and strengths, steps of 1e-3: h^2 / 6 of a third derivative, in which 40 tokens' steps of 3e-3 of a key meet, 3e-4 of
+    the gradient; the rounding, 1e-6 of the loss over h, 1e-3 of it at a loss of the gradient's size: 1e-2."""
+    import torch
+    from paper_2607_11897_amd import sfda
+    say("many directions", H, Hk)
+    x = attn(13, 1, H, Hk, 40, 8, 6, "f32", grads=True)
+    t = {n: f32(x[n]) for n in ("q", "k", "v", "log_decay", "beta", "S0")}
+    t["log_decay"][0, 0, 20] = -0.4         # (no reset: its difference is not a number)
+    dO, dS = f32(x["dO"]), f32(x["dS_T"])
+    gen = torch.Generator(device="cuda").manual_seed(1)
+
+    def loss(**kw):
+        o, S = sfda.delta_attn_fwd(**kw, scale=0.6)
+        return float((o.double() * dO).sum() + (S.double() * dS).sum())
+    got = sfda.delta_attn_bwd(**t, dO=dO, dS_T=dS, scale=0.6)
+    for name, y in t.items():
+        g = got["d" + name].double()
+        h, bar = (1.0, 1e-3) if name in ("q", "v", "S0") else (1e-3, 1e-2)
+        for d in directions(y, gen):
+            up, down = y + h * d, y - h * d         # (the steps that the inputs hold)
+            want = loss(**{**t, name: up}) - loss(**{**t, name: down})
+            have = float((g * (up.double() - down.double())).sum())
+            assert abs(want - have) <= bar * 2 * h * float(g.norm()), (name, want, have)
