@@ -305,7 +305,7 @@ template <typename E, int DKP, int MODE> struct Mem {
     static constexpr int C = B::C, P = B::P, PP = OUT_PARTS<P, MODE>, SK = DKP + 8, ST = C + 8;
     static constexpr int KPL = C * SK, TPL = C * ST;        // planes
     uint16_t k[P * KPL], q[P * KPL], t[3 * TPL], p[PP * TPL];
-    float e[C], w[C], beta[C], gh[C], gl[C], end[4];
+    float e[C], w[C], beta[C], end[4];
 };
 
 // One workgroup scans one head for 64 value columns, 16 in a wave.  (For float32 of more than 128 channels, and the bfloat16 backward
@@ -404,8 +404,6 @@ template <typename E, int DKP, int MODE> __device__ __forceinline__ void scan(co
         tt.template store<BACK>(tid, [&](int s, int row, int col) { return M.t + s * TPL + row * ST + col; });
         pp.template store<BACK>(tid, [&](int s, int row, int col) { return M.p + s * TPL + row * ST + col; });
         if (tid < C) {
-            M.gh[tid] = sc[0].x;
-            M.gl[tid] = sc[0].y;
             M.beta[tid] = sc[0].z;
             M.e[tid] = sc[0].w;
             M.w[tid] = sc[1].x;
@@ -678,7 +676,7 @@ template <typename E, int DKP, int MODE> struct PairMem {
         struct { u32x4 s[NW][SF * OP][64], r[NW][B::CF * OP][64]; } fwd;        // the state and R
         f32x4 add[NW][BACK ? DT : 1][64];                                       // Q^T (c e dO)
     };
-    float e[C], w[C], beta[C], gh[C], gl[C], end[4];
+    float e[C], w[C], beta[C], end[4];
 };
 
 constexpr int PAIR_NT = 2 * NT;
@@ -865,8 +863,6 @@ template <typename E, int DKP, int MODE, bool chain, bool whole> __device__ __fo
                 tv.store_raw(M.v, unit ? 0 : cnt, cols, htid);
                 tt.template store<BACK>(htid, [&](int s, int row, int col) { return M.t + s * TPL + Tr::row(row) + col; });
                 if (htid < C) {
-                    M.gh[htid] = sc[0].x;
-                    M.gl[htid] = sc[0].y;
                     M.beta[htid] = sc[0].z;
                     M.e[htid] = sc[0].w;
                     M.w[htid] = BACK ? sc[1].x : sc[1].y;       // (forward: w beta)
