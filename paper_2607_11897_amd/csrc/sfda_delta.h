@@ -296,7 +296,7 @@ __device__ __forceinline__ void column(uint32_t (&x)[COUNT], const char* base, u
 enum Mode { FWD, RECORD, ADJOINT, STATES };      // STATES: a segment's end state alone, and what it makes of its start state
 
 // Parts of the state, of R and of P as operands of the outputs, for inputs of P parts.  A bfloat16 output's terms may cancel (keys that
-// are alike, strengths past 1), so that one part of 8 bits each leaves an error of up to 0.016 of the results; two leave their own rounding,
+// are alike, strengths past 1), so that one part of 8 bits each leaves an error of up to 0.017 of the results; two leave their own rounding,
 // 0.0017.  The rows of R and the sums of outputs that the backward records are float32.
 template <int P, int MODE> constexpr int OUT_PARTS = MODE == FWD && P == 1 ? 2 : 3;
 
@@ -649,9 +649,9 @@ template <typename E, int DKP, int MODE> __device__ __forceinline__ void scan(co
 // The same scan with eight waves: four hold the state and run the chain alone, four help.  Forward, the helpers form the
 // outputs, a block behind the chain, from the state and R as operands that the chain's waves leave in LDS fragment by fragment (as
 // the lane has them: 16 bytes a lane, no two on one bank).  Backward, they form Q^T (c e dO), which does not depend on the state.
-// Bound by the chain: bfloat16, 128 channels, 8300 to 10500 cycles for 64 tokens, of which K S takes 800, the solve 1900, the update 2000, and
-// waits for the rows that come from memory (20 bytes a cycle on a compute unit) most of the rest.  B8 H16 T4096: forward 320 us (four
-// waves for all of it: 545), the two scans of the backward 880 (1689).
+// Bound by the chain: bfloat16, 128 channels, 8300 to 11000 cycles for 64 tokens, of which K S takes 800, the solve 1900, the update 2000, and
+// waits for operands most of the rest: for rows from memory (20 bytes a cycle on a compute unit) and for the LDS.  B8 H16 T4096: forward 345 us
+// (with outputs of one part 320, and 545 by four waves for all of it), the two scans of the backward 900 (1689).
 
 // rows of a triangular matrix in LDS: 32 rows of a block row are as long as the block columns that they have
 template <int C, bool UPPER> struct Tri {

@@ -285,7 +285,7 @@ template <typename E, int DKP, int MODE> __global__ __launch_bounds__((Scan<E, D
 
 // The states that enter the segments, S <- N + M S one after the other.  One workgroup for a head and 16 value columns, a quarter of
 // the state's rows in a wave; M's rows, which do not wait for the state, are a segment ahead, and the state goes round through
-// LDS.  4.5 us a segment at 128 channels: a load of M and N, two waits for LDS.  S0 is kept behind the segments' states.
+// LDS.  4.7 us a segment at 128 channels: a load of M and N, two waits for LDS.  S0 is kept behind the segments' states.
 template <int DKP> __global__ __launch_bounds__(NT) void sfda_delta_join(DeltaLaunch L, int columns)
 {
     constexpr int DT = DKP / 16, DF = DKP / 32, DW = DT / NW;

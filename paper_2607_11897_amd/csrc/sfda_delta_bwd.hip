@@ -6,8 +6,8 @@
 //   dlog_decay_t = S' . U + sum_(s >= t, in the block) (dO_s . o_s - v_s . dv_s).
 // Three launches after the inverses: the forward scan again, which records the states and the rows R, and the adjoint scan,
 // which records U and du, side by side as roles of one; then all blocks at once form the products above.
-// bfloat16 B8 H16 T4096 of 128 channels: inverses and scores 250 us, scans 880 (256 compute units, each a head's 64 columns of one
-// direction after the other's), gradients 990.
+// bfloat16 B8 H16 T4096 of 128 channels: inverses and scores 250 us, scans 900 (256 compute units, each a head's 64 columns of one
+// direction after the other's), gradients 1130.
 #include "sfda_delta.h"
 
 #include <type_traits>
@@ -47,7 +47,7 @@ template <typename E, int DKP> struct GradMem {
     typedef Block<E> B;
     static constexpr int NW = DKP == 64 ? 4 : 8, NT = 64 * NW;
     // SP: parts of the states, of the rows of dv and u, and of the scores.  bfloat16: two of each leave dq and dk their own rounding, 0.0017 of
-    // themselves; the rows and scores in one part 0.0022, and up to 0.016 where keys are alike and terms cancel
+    // themselves; the rows and scores in one part 0.0022, and up to 0.011 where keys are alike and terms cancel
     static constexpr int C = B::C, P = B::P, SP = P == 1 ? 2 : 3, SK = DKP + 16, SV = SLAB + 8, ST = C + 8;
     static constexpr int KPL = C * SK, VPL = C * SV, TPL = C * ST;
     union {
@@ -107,8 +107,8 @@ __device__ __forceinline__ int thread() { return anew(threadIdx.x); }
 
 // One workgroup for a block of a key head, its value heads one after the other.  A wave owns one or two tiles of 16 channels of dq and dk
 // (rows; tokens are the columns), whose rows of the states it alone reads.  Reads three states, R and du, 3.0 GB at the size above, and
-// writes 0.4: 3.4 TB/s, since the registers leave a compute unit one workgroup (at half of them 127 to 263 spill; four waves with two tiles
-// each spill 147), whose loads and products overlap little.  Neighbouring blocks on one XCD, for the state that both read: no gain (1012 us).
+// writes 0.4: 3.0 TB/s, since the registers leave a compute unit one workgroup (at half of them 127 to 263 spill; four waves with two tiles
+// each spill 147), whose loads and products overlap little (waves wait 69% of their time, matrix units are busy 8%).  Neighbouring blocks on one XCD, for the state that both read: no gain (1012 us).
 template <typename E, int DKP> __global__ __launch_bounds__((GradMem<E, DKP>::NT)) void sfda_delta_grad(DeltaLaunch L)
 {
     typedef Block<E> B;

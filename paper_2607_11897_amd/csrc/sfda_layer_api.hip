@@ -677,8 +677,13 @@ static ll delta_prep_bytes(ll heads, ll blocks, bool bf16, int scans)
 
 // Segments of a sequence, where its heads leave compute units idle: the segments' states (of the value columns and of the unit
 // matrix), a join, then all segments side by side.  Estimates in us: a block of a round of workgroups that fill the units, forward and
-// for the states alone, a step of the join, and what the launches and their first loads take.  Measured, whole / cut: bfloat16, 16
-// heads of 128 channels, T 32768 1920/894; float32, 18 heads, keys of 88 and values of 74, T 1003 88/99 (left whole).
+// for the states alone, a step of the join, and what the launches and their first loads take: those of 128 channels for all widths.  From
+// 4096 tokens on what they choose takes at most 1.11 of the best number of segments' time in bfloat16 (d 64, 128 and 256) and 1.28 in
+// float32 (d 64, 128), and never more than the whole sequence.  Measured, whole / cut, us: bfloat16, 16 heads of T
+// 16384, d 64 807/202, d 128 1097/430, d 256 2976/2324; 4 heads of T 4096 215/78, 275/116, 700/353; float32, 16 heads of T 16384, d 64
+// 1510/326, d 128 2229/761.  Left whole, with the best cut: 64 heads of T 8192, bfloat16 d 128 684/631; 32 heads of T 4096, d 256 787/1022; 48
+// heads of T 4096, float32 d 128 621/555; 4 heads of T 1024, bfloat16 70/48, 87/73 and 204/185, float32 105/52 and 141/90 (short
+// sequences: the launches are estimated high).
 struct DeltaCut { int segments, blocks; };
 DeltaCut delta_cut(ll heads, ll blocks, int dk, int dv, bool bf16)
 {

@@ -210,9 +210,11 @@ __global__ __launch_bounds__(JOIN_NT) void layer_norm_join_kernel(LayerNormLaunc
     }
 }
 
-// Vectors of a lane, then lanes, then vectors.  The backward starts with two, since in bfloat16 four take 256 registers and leave a SIMD one
-// wave (B8 T4096: 2048 channels 128 us and 150, 4096 139 and 177; one vector 126 and 139, but float32 of 1024 without dtotal 103
-// where two take 91).
+// Vectors of a lane, then lanes, then vectors.  The backward starts with two: in bfloat16 four take 256 registers and leave a SIMD one
+// wave, and in float32 one has too few loads on their way.  One / two / four, us: bfloat16 with dtotal, 32768 rows of 2048 130 / 131 / 153,
+// 16384 of 4096 141 / 141 / 180, 32768 of 1024 68 / 66 / 66; float32, 32768 rows of 1024 without dtotal 104 / 93 / 91, with it 115 / 119 / 113,
+// 32768 of 512 57 / 55 / 55.  Past 8192 channels 1024 threads have 128 registers each, too few for the backward, which spills (144
+// bytes a lane in bfloat16, 284 in float32): 4096 rows of 12288 with dtotal 304 and 560 us, where a copy takes 83 and 165.
 struct Shape { int lpr, v, nt; };
 Shape shape_of(int D, bool bf16, bool bwd)
 {
