@@ -541,7 +541,7 @@ sfda_status_t sfda_rotary_axes(const void* q, const void* k, const float* cos, c
  *   S0, S_T : [B, H, dk, dv] contiguous float32, each may be NULL (zero state; not wanted).  S_T == S0 is allowed.
  *   workspace : 16-byte aligned; with sfda_delta_attn_fwd_workspace_bytes(...) bytes all heads run at once, or as many as a launch
  *          takes, with less in passes over them, as many as fit; at least those bytes / (B H), one head's (SFDA_ERR_SHAPE if
- *          smaller).  The results do not depend on it.  Some 512 bytes for each token and value head, whatever dk and dv.
+ *          smaller).  The results do not depend on it.  Some 512 bytes (float32: 320) for each token and value head, whatever dk and dv.
  *   A launch takes (2^23 - 1) / (blocks + 32) value heads, blocks of 64 tokens in bfloat16 and 32 in float32 (SFDA_ERR_SHAPE if
  *   that is none).
  *   1 <= dk, dv <= 256; 64 tokens' rows of q, k, v and o (dO) lie within 2^31 bytes (SFDA_ERR_SHAPE otherwise).
@@ -569,7 +569,8 @@ sfda_status_t sfda_delta_attn_fwd(const void* q, const void* k, const void* v,
  *          sfda_delta_attn_bwd_workspace_bytes(1, H / Hk, 1, ...) (SFDA_ERR_SHAPE if smaller).  The results do not depend on it.
  *   The value heads of a key head have to be in one launch (SFDA_ERR_SHAPE and a size of 0 otherwise).
  *   bfloat16: dq and dk are sums of products whose operands are two bfloat16 parts, to 2^-16 of each term; dv, dlog_decay, dbeta
- *   and dS0 come from products to 2^-22.  Other arguments as the forward's.
+ *   and dS0 come from products to 2^-22.  dlog_decay is what sums over a block's tokens leave of each other: its error is float32's of
+ *   those sums, also where a strong decay leaves little of it.  Other arguments as the forward's.
  */
 size_t sfda_delta_attn_bwd_workspace_bytes(int B, int H, int Hk, int T, int dk, int dv,
                                            sfda_dtype_t dtype);
